@@ -511,6 +511,122 @@ FF_API ff_status ff_forward_noalloc(const void* x, const float* row_scale, const
 FF_API ff_status ff_layer_selftest_wait(ff_layer* layer, unsigned int timeout_us, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Operators of a normalised, regularised dense layer that is trained or
+ * served in 8 bits.  The paper's layers have none of them; they stand beside
+ * the FF layers for heads and comparison nets trained by backpropagation on
+ * the layers' activities.  They keep no state: every buffer is the caller's,
+ * nothing is allocated, and calls on different streams are independent as
+ * long as their outputs and workspaces are.  Matrices are row-major with a
+ * row stride in elements; `prec` is the type of the large buffers (float or
+ * bfloat16), every sum and statistic is fp32.  Empty calls (no rows) return
+ * FF_OK.  Strides need no alignment (16-byte aligned rows are faster).
+ * ------------------------------------------------------------------------- */
+typedef enum { FF_ACT_NONE = 0, FF_ACT_RELU = 1, FF_ACT_SILU = 2 } ff_activation; /* u, max(u, 0), u / (1 + e^-u) */
+
+/* Bytes of workspace that ff_group_norm_act (backward = 0) or its gradient
+ * (backward = 1) needs for these sizes (0: none; pass NULL then); -1 on sizes
+ * that the call would refuse. */
+FF_API long long ff_group_norm_workspace(int n, int spatial, int channels, int groups, ff_precision prec,
+                                         int backward);
+
+/* Group norm with an activation, channels last.  x holds n samples of
+ * `spatial` positions: row b * spatial + s of the matrix x [n * spatial,
+ * channels] (row stride ldx) is position s of sample b; spatial = 1 normalises
+ * the rows of an activity.  Group g covers channels [g C/G, (g+1) C/G); over
+ * each sample's group (spatial * C/G values)
+ *   mean = average x, rstd = 1 / sqrt(average (x - mean)^2 + eps),
+ *   y = act(gamma[c] * (x - mean) * rstd + beta[c])   (rounded once, to prec).
+ * gamma, beta [channels] fp32, NULL: ones, zeros.  y [n * spatial, channels]
+ * (row stride ldy) may be x itself.  mean, rstd [n, groups] fp32 or NULL
+ * (both or neither): what the gradient needs; zero when spatial == 0.
+ * A NaN or an infinity in a group makes that group's outputs NaN.
+ * eps > 0.  FF_ERR_INVALID_ARG also when the workspace is smaller than
+ * ff_group_norm_workspace(..., 0) or not 16-byte aligned. */
+FF_API ff_status ff_group_norm_act(const void* x, long long ldx, int n, int spatial, int channels, int groups,
+                                   const float* gamma, const float* beta, float eps, ff_activation act,
+                                   ff_precision prec, void* y, long long ldy, float* mean, float* rstd,
+                                   void* workspace, long long workspace_bytes, void* stream);
+
+/* Its gradient, from dy and the forward call's x, mean and rstd (all as
+ * there).  With h = (x - mean) rstd, u = gamma h + beta, du = dy act'(u):
+ *   dbeta = sum du, dgamma = sum du h          (over all rows; [channels] fp32)
+ *   dx = rstd (gamma du - <gamma du> - h <gamma du h>)
+ * where <.> averages over the sample's group; act' of ReLU is 0 at 0.
+ * dx may be dy or x itself; dx NULL skips it, dgamma and dbeta NULL (both or
+ * neither) skip them.  Sums have a fixed order: the same call gives the same
+ * bits. */
+FF_API ff_status ff_group_norm_act_backward(const void* dy, long long lddy, const void* x, long long ldx, int n,
+                                            int spatial, int channels, int groups, const float* mean,
+                                            const float* rstd, const float* gamma, const float* beta,
+                                            ff_activation act, ff_precision prec, void* dx, long long lddx,
+                                            float* dgamma, float* dbeta, void* workspace,
+                                            long long workspace_bytes, void* stream);
+
+/* Dropout with a mask that is never stored: y = residual + keep * x / (1 - p)
+ * (residual NULL: none), keep drawn anew from the counter wherever it is
+ * needed.  Its gradient is the same call on dy with the same seed and offset
+ * and no residual (the residual's gradient is dy).
+ * Element (r, j) takes 16 bits, at bit 16 (j mod 4), of word
+ *   offset + *offset_dev + r * ceil(cols / 4) + j / 4
+ * of the library's counter-based SplitMix64 generator, stream (seed, 7): with
+ * state = mix((seed << 8) | 7), word i is mix(state + (i + 1) * gamma).  It is
+ * kept when these bits are >= t = round(65536 p), and scaled by
+ * 65536 / (65536 - t): p is taken to the nearest multiple of 2^-16.  A dropped
+ * element is zero whatever x holds.  p = 1 drops everything.
+ *   offset_dev: device pointer or NULL; read when the kernel runs, so that a
+ *   captured CUDA graph can draw a new mask on every replay.
+ *   seed: its low 56 bits count.  Use offsets ff_dropout_words apart for
+ *   independent masks of one seed.
+ * x, residual, y: [rows, cols] with row strides ldx, ldr, ldy; y may be x or
+ * the residual itself. 0 <= p <= 1. */
+FF_API ff_status ff_dropout(const void* x, long long ldx, long long rows, long long cols, double p,
+                            unsigned long long seed, unsigned long long offset,
+                            const unsigned long long* offset_dev, const void* residual, long long ldr,
+                            ff_precision prec, void* y, long long ldy, void* stream);
+/* Words of the generator that a mask of rows x cols takes: rows * ceil(cols / 4). */
+FF_API long long ff_dropout_words(long long rows, long long cols);
+
+/* 8-bit matrices.  A matrix [rows, k] is held as e4m3 values q [rows,
+ * ff_fp8_stride(k)] (bytes; the pad columns are written as zero) and fp32
+ * scales, one for each block of 128 consecutive k of
+ *   FF_FP8_ROWS   one row:            scale [ceil(k/128), rows]
+ *   FF_FP8_TILES  128 rows from a multiple of 128: scale [ceil(k/128), ceil(rows/128)]
+ * k-block-major and dense, so that x[r, c] ~ q[r, c] * scale[c/128, r or r/128].
+ * Rows suit activities and gradients, tiles weights: their transpose has the
+ * same blocks. */
+typedef enum { FF_FP8_ROWS = 0, FF_FP8_TILES = 1 } ff_fp8_blocks;
+
+/* Row stride, in bytes, of an 8-bit matrix with k columns: k rounded up to 16. */
+FF_API int ff_fp8_stride(int k);
+
+/* Quantizes x [rows, k] (row stride ldx).  Per block: amax = max |x|,
+ * scale = max(amax / 448, 2^-126), q = e4m3(x * (1 / scale)), each an fp32
+ * operation rounded to nearest, the cast to nearest even and saturating.
+ * q, scale: x in blocks along k.  qt, scale_t: x's transpose [k, rows] in
+ * blocks along the rows, as the weight-gradient product needs it.  Either pair
+ * may be NULL, not both; x is read once for both.  A block that holds a NaN
+ * gets a NaN scale, one that holds an infinity an infinite one: every product
+ * that reads such a block is NaN. */
+FF_API ff_status ff_fp8_quantize(const void* x, long long ldx, int rows, int k, ff_precision prec,
+                                 ff_fp8_blocks blocks, void* q, float* scale, void* qt, float* scale_t,
+                                 void* stream);
+
+/* C [m, n] = act(A B^T + bias): A [m, k] in FF_FP8_ROWS blocks, B [n, k] in
+ * either kind (`b_blocks`), as ff_fp8_quantize leaves them (q 16-byte
+ * aligned).  Products and sums of a k-block are formed on the tensor cores in
+ * fp32, then scaled by the block's two scales and added up in fp32; bias [n]
+ * fp32 or NULL, relu != 0: max(., 0); C has type out_prec and row stride ldc.
+ * The layer's three products: y = x w^T with A = rows(x), B = tiles(w);
+ * dx = dy w with A = rows(dy), B = the transposed tiles of w; dw = dy^T x with
+ * A and B = the transposed rows of dy and x.
+ * k >= 1; m == 0 or n == 0 is a no-op.  device_status [1] int or NULL: OR-ed
+ * with 1 (never cleared) if a kernel wait timed out, in which case C is not
+ * valid.  Needs an sm_100-family GPU (FF_ERR_UNSUPPORTED otherwise). */
+FF_API ff_status ff_fp8_matmul(const void* a, const float* a_scale, const void* b, const float* b_scale,
+                               ff_fp8_blocks b_blocks, int m, int n, int k, const float* bias, int relu,
+                               ff_precision out_prec, void* c, long long ldc, int* device_status, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Instrumentation (not part of the method).
  * Every kernel launch libff makes is counted; ff_kernel_launches returns the
  * process-wide total so far.  ff_profile_enable(1) clears earlier records and

@@ -377,15 +377,6 @@ __global__ void __launch_bounds__(256) k_adam(AdamArgs a, int w_blocks) {
 }
 
 // --------------------------------------------------------------------- init
-// SplitMix64 (Steele, Lea, Flood 2014; finaliser constants of Vigna's
-// splitmix64.c), used counter-based: output i of a stream with initial
-// state s0 is mix(s0 + (i + 1) * gamma).
-__device__ __host__ __forceinline__ unsigned long long sm64_mix(unsigned long long z) {
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-constexpr unsigned long long kGamma = 0x9E3779B97F4A7C15ull;
 constexpr unsigned long long kStreamWeights = 4;
 
 __global__ void k_init_weights(float* __restrict__ W, long long total, unsigned long long s0, double bound) {

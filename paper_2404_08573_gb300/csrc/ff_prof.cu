@@ -24,7 +24,8 @@ const char* const kNames[K_NUM] = {"overlay",     "row_scale",    "fwd_gemm_tc",
                                    "adam",        "init_weights", "to_bf16",       "label_columns",
                                    "store_gemm_tc", "store_gemm_simt", "expand",   "argmax",
                                    "head_logits", "head_wgrad",   "head_adam",
-                                   "epoch_gemm_tc"};
+                                   "epoch_gemm_tc", "group_norm", "group_norm_grad", "dropout",
+                                   "fp8_quantize", "fp8_gemm_tc"};
 
 struct Rec {
   int kind;

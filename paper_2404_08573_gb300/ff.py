@@ -7,14 +7,16 @@ is no fallback: if libff.so is missing or the GPU cannot run it, calls raise.
 Names follow the C ABI in include/ff.h:
 ``Layer`` (ff_layer_*), ``overlay_label``, ``predict``, ``adaptive_negatives``,
 ``Net`` (ff_net_*), ``Head`` (ff_head_*), ``Pff`` (ff_pff_*), ``po_train_step_raw``/
-``po_train_step_act``/``po_predict`` (ff_po_*), ``forward_noalloc``.
+``po_train_step_act``/``po_predict`` (ff_po_*), ``forward_noalloc``; the
+layer operators ``group_norm_act`` and its backward pass, ``dropout``,
+``fp8_quantize`` and ``fp8_matmul`` (ff_group_norm_*, ff_dropout, ff_fp8_*).
 """
 
 from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_float, c_int, c_longlong, c_ulonglong, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_longlong, c_ulonglong, c_void_p
 
 import numpy as np
 import torch
@@ -120,11 +122,27 @@ def lib():
             "ff_pff_wait": [c_void_p, ctypes.c_uint],
             "ff_net_wait": [c_void_p, ctypes.c_uint],
             "ff_pff_run": [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p],
+            "ff_group_norm_act": [c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_float, c_int,
+                                  c_int, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p, c_longlong, c_void_p],
+            "ff_group_norm_act_backward": [c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_int, c_int, c_int,
+                                           c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_longlong,
+                                           c_void_p, c_void_p, c_void_p, c_longlong, c_void_p],
+            "ff_dropout": [c_void_p, c_longlong, c_longlong, c_longlong, c_double, c_ulonglong, c_ulonglong, c_void_p,
+                           c_void_p, c_longlong, c_int, c_void_p, c_longlong, c_void_p],
+            "ff_fp8_stride": [c_int],
+            "ff_fp8_quantize": [c_void_p, c_longlong, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                c_void_p],
+            "ff_fp8_matmul": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_int, c_int,
+                              c_void_p, c_longlong, c_void_p, c_void_p],
         }
         for name, args in sig.items():
             f = getattr(L, name)
             f.restype = c_int
             f.argtypes = args
+        L.ff_group_norm_workspace.restype = c_longlong
+        L.ff_group_norm_workspace.argtypes = [c_int] * 6
+        L.ff_dropout_words.restype = c_longlong
+        L.ff_dropout_words.argtypes = [c_longlong, c_longlong]
         _lib = L
     return _lib
 
@@ -658,3 +676,297 @@ class PoNet(Net):
                                           n, _ptr(loss, torch.float32, "loss"), c_void_p(_stream(stream))),
                "ff_net_po_train_step")
 
+
+# ------------------------------------------------------------ layer operators
+_PREC = {torch.bfloat16: FF_BF16, torch.float32: FF_FP32}
+_ACT = {"none": 0, "relu": 1, "silu": 2}
+_INT_MAX = 0x7FFFFFFF
+
+
+class _On:
+    """The stream of an operator call, and the buffers it allocates.  A buffer
+    allocated while another stream is current is marked as used on this one,
+    so that its memory is not handed out again before the call has run."""
+
+    __slots__ = ("ptr", "other")
+
+    def __init__(self, stream, device):
+        current = torch.cuda.current_stream(device)
+        self.ptr, self.other = current.cuda_stream, None
+        if stream is not None:
+            ptr = _stream(stream)
+            if ptr != self.ptr:
+                self.other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(ptr, device)
+                self.ptr = ptr
+
+    def empty(self, shape, dtype, device):
+        t = torch.empty(shape, dtype=dtype, device=device)
+        if self.other is not None:
+            t.record_stream(self.other)
+        return t
+
+
+def _prec(x, what):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a torch.Tensor")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    prec = _PREC.get(x.dtype)
+    if prec is None:
+        raise TypeError(f"{what} must be torch.bfloat16 or torch.float32, got {x.dtype}")
+    return prec
+
+
+def _row_stride_of(x, what):
+    """Row stride of x seen as a matrix [rows, last dimension]; raises where its rows are not evenly spaced."""
+    if x.is_contiguous():
+        return x.shape[-1]
+    shape, stride = x.shape, x.stride()
+    if x.numel() == 0:
+        return shape[-1]
+    if stride[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    ld, span = None, 1
+    for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = step
+        elif step != ld * span:
+            raise ValueError(f"{what}: the rows must be evenly spaced")
+        span *= size
+    ld = shape[-1] if ld is None else ld
+    if ld < shape[-1]:
+        raise ValueError(f"{what}: rows overlap (row stride {ld} < {shape[-1]})")
+    return ld
+
+
+def _vector(t, size, what, device):
+    if t is None:
+        return None
+    if t.numel() != size:
+        raise ValueError(f"{what} must have {size} values")
+    _same_device(t, device, what)
+    return _ptr(t, torch.float32, what)
+
+
+def _same_device(t, device, what):
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}")
+
+
+def _like(t, x, what):
+    """Checks an optional buffer that must match x in shape, type and device; returns its row stride."""
+    if not isinstance(t, torch.Tensor) or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+        raise ValueError(f"{what} must match the input's shape, type and device")
+    return _row_stride_of(t, what)
+
+
+def _norm_args(x, groups, act):
+    if x.dim() < 2:
+        raise ValueError("x must be [n, channels] or [n, ..., channels]")
+    if act not in _ACT:
+        raise ValueError(f"act must be one of {sorted(_ACT)}")
+    n, C = x.shape[0], x.shape[-1]
+    groups = int(groups)
+    if groups < 1 or C < 1 or C % groups:
+        raise ValueError("groups must divide the channels")
+    spatial = 1
+    for d in x.shape[1:-1]:
+        spatial *= d
+    if max(n, spatial, C) > _INT_MAX:
+        raise ValueError("n, positions and channels must each fit 32 bits")
+    return n, spatial, C, groups
+
+
+def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 1e-5, out=None, mean=None, rstd=None,
+                   stream=None):
+    """ff_group_norm_act: y = act(gamma * (x - mean) * rstd + beta) over channel
+    groups, channels last.  x [n, channels] or [n, ..., channels] (bf16 or
+    fp32, evenly spaced rows); gamma, beta fp32 [channels] or None.  Returns
+    (y, mean, rstd), mean and rstd fp32 [n, groups]; out may be x."""
+    prec = _prec(x, "x")
+    n, spatial, C, groups = _norm_args(x, groups, act)
+    dev = x.device
+    with torch.cuda.device(dev):
+        on = _On(stream, dev)
+        ldx = _row_stride_of(x, "x")
+        if out is None:
+            out, ldy = on.empty(x.shape, x.dtype, dev), C
+        else:
+            ldy = _like(out, x, "out")
+        if mean is None:
+            mean = on.empty((n, groups), torch.float32, dev)
+        if rstd is None:
+            rstd = on.empty((n, groups), torch.float32, dev)
+        L = lib()
+        need = L.ff_group_norm_workspace(n, spatial, C, groups, prec, 0)
+        ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+        _check(L.ff_group_norm_act(
+            x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
+            eps, _ACT[act], prec, out.data_ptr(), ldy, _vector(mean, n * groups, "mean", dev),
+            _vector(rstd, n * groups, "rstd", dev), None if ws is None else ws.data_ptr(), max(need, 0), on.ptr),
+            "ff_group_norm_act")
+    return out, mean, rstd
+
+
+def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: str = "silu", out=None, stream=None):
+    """ff_group_norm_act_backward: the gradient of group_norm_act at (x, gamma,
+    beta), with the mean and rstd it returned.  Returns (dx, dgamma, dbeta);
+    out may be dy or x."""
+    prec = _prec(x, "x")
+    n, spatial, C, groups = _norm_args(x, groups, act)
+    dev = x.device
+    with torch.cuda.device(dev):
+        on = _On(stream, dev)
+        ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
+        if out is None:
+            out, lddx = on.empty(x.shape, x.dtype, dev), C
+        else:
+            lddx = _like(out, x, "out")
+        dgamma = on.empty((C,), torch.float32, dev)
+        dbeta = on.empty((C,), torch.float32, dev)
+        if mean is None or rstd is None:
+            raise ValueError("mean and rstd of the forward pass are needed")
+        L = lib()
+        need = L.ff_group_norm_workspace(n, spatial, C, groups, prec, 1)
+        ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+        _check(L.ff_group_norm_act_backward(
+            dy.data_ptr(), lddy, x.data_ptr(), ldx, n, spatial, C, groups, _vector(mean, n * groups, "mean", dev),
+            _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
+            _ACT[act], prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
+            None if ws is None else ws.data_ptr(), max(need, 0), on.ptr), "ff_group_norm_act_backward")
+    return out, dgamma, dbeta
+
+
+def dropout_words(rows: int, cols: int) -> int:
+    """ff_dropout_words: generator words that a mask of rows x cols takes."""
+    return int(lib().ff_dropout_words(int(rows), int(cols)))
+
+
+def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=None):
+    """ff_dropout: residual + keep * x / (1 - p) with the mask drawn from the
+    counter-based generator at (seed, offset), never stored; its gradient is
+    the same call on dy without a residual.  x [..., cols] (bf16 or fp32,
+    evenly spaced rows).  offset: an int, or a one-element int64 CUDA tensor
+    that is read when the kernel runs (for CUDA graphs).  out may be x or the
+    residual."""
+    prec = _prec(x, "x")
+    if x.dim() < 1:
+        raise ValueError("x must have at least one dimension")
+    dev = x.device
+    with torch.cuda.device(dev):
+        on = _On(stream, dev)
+        cols = x.shape[-1]
+        rows = x.numel() // cols if cols else 0
+        ldx = _row_stride_of(x, "x")
+        ldr = _like(residual, x, "residual") if residual is not None else 0
+        if out is None:
+            out, ldy = on.empty(x.shape, x.dtype, dev), cols
+        else:
+            ldy = _like(out, x, "out")
+        odev, host = None, 0
+        if isinstance(offset, torch.Tensor):
+            if offset.numel() != 1:
+                raise ValueError("offset must have one element")
+            _same_device(offset, dev, "offset")
+            odev = _ptr(offset, torch.int64, "offset")
+        else:
+            host = int(offset) & 0xFFFFFFFFFFFFFFFF
+        _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
+                                None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
+                                on.ptr), "ff_dropout")
+    return out
+
+
+class Fp8Matrix:
+    """An 8-bit matrix [rows, k]: e4m3 values q [rows, ff_fp8_stride(k)] and
+    fp32 scales, [ceil(k / 128), rows] or, tile=True, [ceil(k / 128),
+    ceil(rows / 128)] (see ff_fp8_blocks in include/ff.h)."""
+
+    __slots__ = ("q", "scale", "rows", "k", "tile")
+
+    def __init__(self, q, scale, rows: int, k: int, tile: bool = False):
+        self.q, self.scale, self.rows, self.k, self.tile = q, scale, rows, k, tile
+        if k < 1 or q.shape != (rows, (k + 15) & ~15) or q.element_size() != 1 or not q.is_contiguous() or not q.is_cuda:
+            raise ValueError("q must be a contiguous one-byte CUDA tensor [rows, ff_fp8_stride(k)]")
+        if (scale.shape != ((k + 127) // 128, (rows + 127) // 128 if tile else rows) or scale.dtype != torch.float32
+                or not scale.is_contiguous() or scale.device != q.device):
+            raise ValueError("scale must be contiguous fp32 [ceil(k / 128), rows or row blocks] beside q")
+
+    @property
+    def blocks(self):
+        """ff_fp8_blocks of the matrix."""
+        return 1 if self.tile else 0
+
+
+def _fp8_new(on, rows, k, tile, dev):
+    q = on.empty((rows, (k + 15) & ~15), torch.float8_e4m3fn, dev)
+    scale = on.empty(((k + 127) // 128, (rows + 127) // 128 if tile else rows), torch.float32, dev)
+    return Fp8Matrix(q, scale, rows, k, tile)
+
+
+def _fp8_quantize(x, tile, straight, transposed, stream):
+    prec = _prec(x, "x")
+    if x.dim() != 2 or x.shape[1] < 1:
+        raise ValueError("x must be [rows, k] with k >= 1")
+    dev = x.device
+    with torch.cuda.device(dev):
+        on = _On(stream, dev)
+        rows, k = x.shape
+        if max(rows, k) > _INT_MAX:
+            raise ValueError("rows and k must each fit 32 bits")
+        if transposed and rows < 1:
+            raise ValueError("the transpose needs at least one row")
+        ldx = _row_stride_of(x, "x")
+        a = _fp8_new(on, rows, k, tile, dev) if straight else None
+        t = _fp8_new(on, k, rows, tile, dev) if transposed else None
+        _check(lib().ff_fp8_quantize(x.data_ptr(), ldx, rows, k, prec, 1 if tile else 0,
+                                     a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
+                                     t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on.ptr),
+               "ff_fp8_quantize")
+    return a, t
+
+
+def fp8_quantize(x, tile: bool = False, transpose: bool = False, stream=None):
+    """ff_fp8_quantize: x [rows, k] (bf16 or fp32, evenly spaced rows) as an
+    Fp8Matrix in row blocks or 128 x 128 tiles; transpose=True gives x's
+    transpose instead."""
+    return _fp8_quantize(x, tile, not transpose, transpose, stream)[1 if transpose else 0]
+
+
+def fp8_quantize_both(x, tile: bool = False, stream=None):
+    """ff_fp8_quantize, both ways round from one read of x: (x, x's transpose)."""
+    return _fp8_quantize(x, tile, True, True, stream)
+
+
+def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bfloat16, status=None, stream=None):
+    """ff_fp8_matmul: act(a b^T + bias) of two Fp8Matrix (a in row blocks).
+    Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
+    out's type; bias fp32 [b.rows]; status: a one-element int32 CUDA tensor
+    that is OR-ed with 1 if a kernel wait timed out."""
+    if a.k != b.k:
+        raise ValueError("a and b must have the same k")
+    if a.tile:
+        raise ValueError("a must be quantized in row blocks")
+    dev = a.q.device
+    _same_device(b.q, dev, "b")
+    with torch.cuda.device(dev):
+        on = _On(stream, dev)
+        m, n = a.rows, b.rows
+        if out is None:
+            if out_dtype not in _PREC:
+                raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
+            out, ldc = on.empty((m, n), out_dtype, dev), n
+        else:
+            if out.shape != (m, n):
+                raise ValueError("out must be [a.rows, b.rows]")
+            _same_device(out, dev, "out")
+            ldc = _row_stride_of(out, "out")
+        prec = _prec(out, "out")
+        if status is not None:
+            _same_device(status, dev, "status")
+        _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
+                                   n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
+                                   _ptr(status, torch.int32, "status"), on.ptr), "ff_fp8_matmul")
+    return out
