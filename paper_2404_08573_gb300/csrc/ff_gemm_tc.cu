@@ -151,7 +151,7 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// Row-major matrix [rows, cols] of bf16 (esize 2) or fp32 (esize 4) with row
+// Row-major matrix [rows, cols] of bytes (esize 1), bf16 (2) or fp32 (4) with row
 // stride ld (elements), tiled in boxes of box_rows x box_cols with 128-byte
 // swizzle; out-of-range elements of a box read as zero and are not written.
 bool encode_map(CUtensorMap* m, const void* ptr, int esize, int cols, int rows, int ld, int box_cols, int box_rows,
@@ -163,7 +163,11 @@ bool encode_map(CUtensorMap* m, const void* ptr, int esize, int cols, int rows, 
   cuuint64_t strides[1] = {(cuuint64_t)ld * esize};
   cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  return enc(m, esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
+  return enc(m,
+             esize == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+             : esize == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                          : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+             2,
              const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
