@@ -19,7 +19,6 @@
 // copies and MMAs land before it frees TMEM and exits.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "ff_api_internal.h"
 #include "ff_fp8.h"
@@ -47,46 +46,58 @@ __device__ __forceinline__ const float* scale_ptr(const Scales& s, int kb, int i
   return s.p + (long long)kb * s.stride + (i >> s.shift);
 }
 
-// acc += factor * p over CPW columns of this warp's TMEM lanes, p read 8 to
-// 32 columns at a time with the next read in flight under the arithmetic.
-// COLS: each column has a factor of its own beside the row's, cs[0..CPW) in
-// shared memory.
+// Reads LD of this warp's TMEM columns into registers (asynchronous).
+template <int LD>
+__device__ __forceinline__ void tmem_read(uint32_t taddr, uint32_t (&r)[LD]) {
+  if constexpr (LD == 8)
+    ptx::tmem_ld8(taddr, r);
+  else if constexpr (LD == 16)
+    ptx::tmem_ld16(taddr, r);
+  else
+    ptx::tmem_ld32(taddr, r);
+}
+
+// acc[0..LD) += row * cs[.] * p, on pairs.  COLS: each column has a factor of
+// its own, cs in shared memory; else the row's is all.
+template <int LD, bool COLS>
+__device__ __forceinline__ void scaled_add(float* acc, const uint32_t (&p)[LD], uint64_t row2, const float* cs) {
+#pragma unroll
+  for (int i = 0; i < LD; i += 4) {
+    float* d = acc + i;
+    uint64_t f0 = row2, f1 = row2, lo = ptx::pack2(d[0], d[1]), hi = ptx::pack2(d[2], d[3]);
+    if constexpr (COLS) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(cs + i);
+      f0 = ptx::mul2(row2, v.x);
+      f1 = ptx::mul2(row2, v.y);
+    }
+    ptx::fma2(lo, f0, ptx::pack2(p[i], p[i + 1]));
+    ptx::fma2(hi, f1, ptx::pack2(p[i + 2], p[i + 3]));
+    const float2 x = ptx::unpack2(lo), y = ptx::unpack2(hi);
+    d[0] = x.x;
+    d[1] = x.y;
+    d[2] = y.x;
+    d[3] = y.y;
+  }
+}
+
+// One k-block: acc += scaled product over the CPW columns at TMEM address
+// `at`, a chunk's read in flight under the arithmetic of the one before it.
 // release() runs once the last columns are in registers.
 template <int CPW, bool COLS, typename Release>
-__device__ __forceinline__ void promote(float (&acc)[CPW], uint32_t taddr, float row, const float* cs,
-                                        Release release) {
+__device__ __forceinline__ void promote(float (&acc)[CPW], uint32_t at, float row, const float* cs, Release release) {
   constexpr int LD = CPW < 16 ? 8 : CPW < 128 ? 16 : 32;
   constexpr int NC = CPW / LD;
   uint32_t r[2][LD];
-  auto load = [&](int c, uint32_t (&d)[LD]) {
-    if constexpr (LD == 8)
-      ptx::tmem_ld8(taddr + c * LD, d);
-    else if constexpr (LD == 16)
-      ptx::tmem_ld16(taddr + c * LD, d);
-    else
-      ptx::tmem_ld32(taddr + c * LD, d);
-  };
-  load(0, r[0]);
+  const uint64_t row2 = ptx::pack2(row, row);
+  tmem_read<LD>(at, r[0]);
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     ptx::tmem_ld_wait_for(r[c & 1]);
     if (c + 1 < NC)
-      load(c + 1, r[(c + 1) & 1]);
+      tmem_read<LD>(at + (c + 1) * LD, r[(c + 1) & 1]);
     else
       release();
-#pragma unroll
-    for (int i = 0; i < LD; i += 4) {
-      float f[4] = {row, row, row, row};
-      if constexpr (COLS) {
-        const float4 v = *reinterpret_cast<const float4*>(cs + c * LD + i);
-        f[0] *= v.x;
-        f[1] *= v.y;
-        f[2] *= v.z;
-        f[3] *= v.w;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[c * LD + i + e] = fmaf(f[e], __uint_as_float(r[c & 1][i + e]), acc[c * LD + i + e]);
-    }
+    scaled_add<LD, COLS>(acc + c * LD, r[c & 1], row2, cs + c * LD);
   }
 }
 
@@ -99,29 +110,34 @@ struct Args {
   long long ldc;
   int* err;
   int ntp, ntq;      // tiles
+  int tma_c;         // pair kernel: C goes out by TMA
 };
 
 __device__ __forceinline__ float finish(float v, int relu) { return relu && v < 0.f ? 0.f : v; }  // keeps NaN
 
 // ------------------------------------------------------- large products
 // CTA pairs (cta_group::2) on 256 x 256 tiles: each CTA loads 128 rows of A
-// and half of B's 256 columns per k-block (32 KB for 8.4 MMAC) and promotes its
-// own 128 x 256 accumulator.  Persistent: the MMAs of the next tile's first
-// k-blocks run under the last promotions and the store of this one.
+// and half of B's 256 columns per k-block (32 KB for 4.2 MMAC) and promotes its
+// own 128 x 256 accumulator.  A k-block's MMAs run as two halves of 128
+// columns, each with its own TMEM buffers and its own four epilogue warps, so
+// that a buffer is handed back after half a k-block's MMAs and the two
+// epilogue warps of a scheduler work in turn.  Persistent: the MMAs of the
+// next tile's first k-blocks run under the store of this one.
 constexpr int LN = 256;
-constexpr int LSTAGES = 5;
+constexpr int LSTAGES = 4;
 constexpr int LSTAGE = (BM + LN / 2) * KB;
 constexpr int LCPW = LN / 2;  // columns per epilogue warp
-constexpr int LSTAGING = 32 * 128;  // per epilogue warp: 32 rows x 128 bytes of C
-constexpr int LSLOTS = 8;           // k-blocks of scales in flight or in use
-constexpr int LSLOT = BM + LN;      // the CTA's rows' and the tile's columns' scales
-// Three warpgroups: producer, MMA and two scale-loading warps, and two of
+constexpr int LSTAGING = 2 * 32 * 128;  // per epilogue warp: two blocks of 32 rows x 128 bytes of C
+constexpr int LGROUP = 4;           // k-blocks of scales per barrier
+constexpr int LGROUPS = 2;          // groups in flight or in use
+constexpr int LSLOT = BM + LN;      // a k-block's: the CTA's rows' and the tile's columns' scales
+// Three warpgroups: producer, two MMA and a scale-loading warp, and two of
 // epilogue warps, which take the registers the first gives up: a launch of
 // 168 a thread is split 40 / 232 / 232.
 constexpr int LTHREADS = 384;
 constexpr int LREGS = 168, LREGS_LOW = 40, LREGS_EPI = 232;
 static_assert(LREGS_LOW + 2 * LREGS_EPI <= 3 * LREGS, "the split must fit what the launch holds");
-constexpr int L_SMEM = 1024 + LSTAGES * LSTAGE + EPI * LSTAGING + LSLOTS * LSLOT * 4 + 512;
+constexpr int L_SMEM = 1024 + LSTAGES * LSTAGE + EPI * LSTAGING + LGROUPS * LGROUP * LSLOT * 4 + EPI * LCPW * 4 + 512;
 static_assert(L_SMEM > 113 * 1024 && L_SMEM <= 227 * 1024, "one GEMM CTA per SM, so that no TMEM allocation waits on another's");
 
 // Tile t of the raster: groups of 8 row tiles, columns outermost within a
@@ -136,19 +152,21 @@ __device__ __forceinline__ void tile_of(int t, int ntp, int ntq, int& tp, int& t
 
 template <bool COLS>
 __global__ void __launch_bounds__(LTHREADS, 1)
-    k_fp8_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, Args g) {
+    k_fp8_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+               const __grid_constant__ CUtensorMap tmC, Args g) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_s = ptx::smem_u32(smem_raw);
   uint8_t* smem = smem_raw + ((1024u - (raw_s & 1023u)) & 1023u);
   uint8_t* staging = smem + LSTAGES * LSTAGE;
-  float* slots = reinterpret_cast<float*>(staging + EPI * LSTAGING);  // [LSLOTS][LSLOT]
-  uint64_t* full = reinterpret_cast<uint64_t*>(slots + LSLOTS * LSLOT);
+  float* slots = reinterpret_cast<float*>(staging + EPI * LSTAGING);  // [LGROUPS * LGROUP][LSLOT]
+  float* sbias = slots + LGROUPS * LGROUP * LSLOT;                    // [epilogue warp][LCPW]
+  uint64_t* full = reinterpret_cast<uint64_t*>(sbias + EPI * LCPW);
   uint64_t* empty = full + LSTAGES;
-  uint64_t* tfull = empty + LSTAGES;   // [2] a TMEM buffer holds a k-block's product
-  uint64_t* tempty = tfull + 2;        // [2] both CTAs have read it
-  uint64_t* sfull = tempty + 2;        // [LSLOTS] a slot holds a k-block's scales
-  uint64_t* sempty = sfull + LSLOTS;   // [LSLOTS] the epilogue has used them
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(sempty + LSLOTS);
+  uint64_t* tfull = empty + LSTAGES;    // [2 * half + buffer] holds a k-block's product
+  uint64_t* tempty = tfull + 4;         // [2 * half + buffer] both CTAs have read it
+  uint64_t* sfull = tempty + 4;         // [LGROUPS] a group holds its k-blocks' scales
+  uint64_t* sempty = sfull + LGROUPS;   // [LGROUPS] the epilogue has used them
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(sempty + LGROUPS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tslot + 1);
   volatile int* never_set = reinterpret_cast<volatile int*>(tslot + 2);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -161,14 +179,14 @@ __global__ void __launch_bounds__(LTHREADS, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < LSTAGES; ++s) {
       ptx::mbar_init(&full[s], 1);
-      ptx::mbar_init(&empty[s], 1);
+      ptx::mbar_init(&empty[s], 2);  // the MMAs of both halves
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 4; ++b) {
       ptx::mbar_init(&tfull[b], 1);
-      ptx::mbar_init(&tempty[b], 2 * EPI);
+      ptx::mbar_init(&tempty[b], EPI);  // four warps of each CTA
     }
-    for (int i = 0; i < LSLOTS; ++i) {
-      ptx::mbar_init(&sfull[i], 64);
+    for (int i = 0; i < LGROUPS; ++i) {
+      ptx::mbar_init(&sfull[i], 32);
       ptx::mbar_init(&sempty[i], EPI);
     }
     *abort_flag = 0;
@@ -176,6 +194,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
     ptx::fence_mbar_init();
     ptx::prefetch_tmap(&tmA);
     ptx::prefetch_tmap(&tmB);
+    ptx::prefetch_tmap(&tmC);
   }
   if (warp == 1) {
     ptx::tmem_alloc_pair(tslot, 512);
@@ -197,7 +216,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       for (int t = pair; t < ntiles && !*abort_flag; t += npairs) {
         int tp, tq;
         tile_of(t, g.ntp, g.ntq, tp, tq);
-        const int ar = tp * 2 * BM + (int)crank * BM, br = tq * LN + (int)crank * (LN / 2);
+        const int ar = tp * 2 * BM + (int)crank * BM, br = tq * LN + (int)crank * (LN / 4);
         for (int kb = 0; kb < nkb; ++kb, ++it) {
           const int s = it % LSTAGES;
           if (!ptx::mbar_wait(&empty[s], (((uint32_t)(it / LSTAGES)) & 1u) ^ 1u, kWaitTimeoutNs, abort_flag)) {
@@ -207,7 +226,9 @@ __global__ void __launch_bounds__(LTHREADS, 1)
           if (lead) ptx::mbar_arrive_expect_tx(&full[s], 2 * LSTAGE);
           uint8_t* a = smem + s * LSTAGE;
           ptx::tma_load_2d_pair(a, &tmA, full0 + 8u * (uint32_t)s, kb * KB, ar);
+          // this CTA's 64 of each half's 128 columns
           ptx::tma_load_2d_pair(a + BM * KB, &tmB, full0 + 8u * (uint32_t)s, kb * KB, br);
+          ptx::tma_load_2d_pair(a + BM * KB + LN / 4 * KB, &tmB, full0 + 8u * (uint32_t)s, kb * KB, br + LN / 2);
         }
       }
       if (!*abort_flag) {
@@ -231,36 +252,39 @@ __global__ void __launch_bounds__(LTHREADS, 1)
         }
       }
     }
-  } else if (warp == 1) {
+  } else if (warp <= 2) {
     if (lead) {
-      // Few instructions between the MMAs: this warp shares its scheduler with
-      // two epilogue warps, and while it lags the tensor cores stand still.
+      // Warp 1 issues the MMAs of the first half of the columns, warp 2 those
+      // of the second: a k-block's waits and issues take one warp longer than
+      // its MMAs run, since it shares its scheduler with two epilogue warps.
       // The whole warp walks the loop, so that its variables are uniform, and
       // one lane issues.  Descriptors differ from the first stage's by their
       // address field only (16-byte units).
-      constexpr uint32_t idesc = ptx::idesc_e4m3_f32(2 * BM, LN);
+      constexpr uint32_t idesc = ptx::idesc_e4m3_f32(2 * BM, LN / 2);
+      const int h = warp - 1;
       const uint64_t ad0 = ptx::sdesc_sw128(ptx::smem_u32(smem), 16, 1024);
-      const uint64_t bd0 = ptx::sdesc_sw128(ptx::smem_u32(smem + BM * KB), 16, 1024);
+      const uint64_t bd0 = ptx::sdesc_sw128(ptx::smem_u32(smem + BM * KB + h * (LN / 4) * KB), 16, 1024);
       const int total = ntiles > pair ? (ntiles - pair + npairs - 1) / npairs * nkb : 0;
+      uint64_t *te = &tempty[2 * h], *tf = &tfull[2 * h];
       int s = 0;
-      uint32_t ph = 0, tph = 1;  // parities of full[s] and tempty[b]
+      uint32_t ph = 0, tph = 1;  // parities of full[s] and te[b]
       for (int it = 0; it < total; ++it) {
         const uint32_t b = (uint32_t)it & 1u;
-        const bool ok = ptx::mbar_wait(&tempty[b], tph, kWaitTimeoutNs, abort_flag) &&
-                        ptx::mbar_wait(&full[s], ph, kWaitTimeoutNs, abort_flag);
+        const bool ok = ptx::mbar_wait(&full[s], ph, kWaitTimeoutNs, abort_flag) &&
+                        ptx::mbar_wait(&te[b], tph, kWaitTimeoutNs, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) {
           latch(g.err, abort_flag);
           break;
         }
         ptx::tc_fence_after();
         const uint64_t ad = ad0 + (uint64_t)(s * (LSTAGE >> 4)), bd = bd0 + (uint64_t)(s * (LSTAGE >> 4));
-        const uint32_t d = tmem + b * LN;
+        const uint32_t d = tmem + (uint32_t)h * LN + b * (LN / 2);
         if (ptx::elect_one()) {
           ptx::umma_f8_pair(d, ad, bd, idesc, 0u);
 #pragma unroll
           for (int k = 1; k < KB / 32; ++k) ptx::umma_f8_pair(d, ad + 2 * k, bd + 2 * k, idesc, 1u);
+          ptx::umma_commit_pair(&tf[b], 3);
           ptx::umma_commit_pair(&empty[s], 3);
-          ptx::umma_commit_pair(&tfull[b], 3);
         }
         __syncwarp();
         tph ^= b;
@@ -273,30 +297,30 @@ __global__ void __launch_bounds__(LTHREADS, 1)
   } else if (warp < 4) {
     // Scales of the k-blocks to come: this CTA's rows', and the columns' of
     // the tile (COLS) or of its two 128-column halves.
-    const int l = (int)threadIdx.x - 64;  // 0 .. 63
+    const int total = ntiles > pair ? (ntiles - pair + npairs - 1) / npairs * nkb : 0;
     int it = 0;
     for (int t = pair; t < ntiles && !*abort_flag; t += npairs) {
       int tp, tq;
       tile_of(t, g.ntp, g.ntq, tp, tq);
-      const int row = tp * 2 * BM + (int)crank * BM + l, col = tq * LN;
+      const int row = tp * 2 * BM + (int)crank * BM, col = tq * LN;
       for (int kb = 0; kb < nkb; ++kb, ++it) {
-        const int s = it % LSLOTS;
-        if (!ptx::mbar_wait(&sempty[s], (((uint32_t)(it / LSLOTS)) & 1u) ^ 1u, kWaitTimeoutNs, abort_flag)) {
+        const int gr = (it / LGROUP) % LGROUPS;
+        if (it % LGROUP == 0 && !ptx::mbar_wait(&sempty[gr], (((uint32_t)(it / (LGROUP * LGROUPS))) & 1u) ^ 1u,
+                                                kWaitTimeoutNs, abort_flag)) {
           latch(g.err, abort_flag);
           break;
         }
-        float* d = slots + s * LSLOT;
+        float* d = slots + it % (LGROUP * LGROUPS) * LSLOT;
         // rows and columns past the matrix hold zeros: any scale will do
-        ptx::cp_async4(d + l, scale_ptr(g.sp, kb, min(row, g.P - 1)));
-        ptx::cp_async4(d + 64 + l, scale_ptr(g.sp, kb, min(row + 64, g.P - 1)));
+#pragma unroll
+        for (int e = lane; e < BM; e += 32) ptx::cp_async4(d + e, scale_ptr(g.sp, kb, min(row + e, g.P - 1)));
         if constexpr (COLS) {
 #pragma unroll
-          for (int e = 0; e < LN; e += 64)
-            ptx::cp_async4(d + BM + e + l, scale_ptr(g.sq, kb, min(col + e + l, g.Q - 1)));
+          for (int e = lane; e < LN; e += 32) ptx::cp_async4(d + BM + e, scale_ptr(g.sq, kb, min(col + e, g.Q - 1)));
         } else {
-          if (l < 2) ptx::cp_async4(d + BM + l, scale_ptr(g.sq, kb, min(col + l * LCPW, g.Q - 1)));
+          if (lane < 2) ptx::cp_async4(d + BM + lane, scale_ptr(g.sq, kb, min(col + lane * LCPW, g.Q - 1)));
         }
-        ptx::cp_async_arrive(&sfull[s]);
+        if (it % LGROUP == LGROUP - 1 || it == total - 1) ptx::cp_async_arrive(&sfull[gr]);
       }
     }
     ptx::cp_async_commit();
@@ -305,12 +329,13 @@ __global__ void __launch_bounds__(LTHREADS, 1)
   } else {
     ptx::regs_inc<LREGS_EPI>();
     const int q = warp & 3, ew = warp - 4, half = ew / 4;
-    const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * LCPW);
-    const uint32_t te0 = ptx::mapa_shared(ptx::smem_u32(&tempty[0]), 0);
+    const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * LN);
+    const uint32_t te0 = ptx::mapa_shared(ptx::smem_u32(&tempty[2 * half]), 0);
     uint8_t* stage = staging + ew * LSTAGING;
-    int it = 0;
-    bool live = true;
-    for (int t = pair; t < ntiles && live; t += npairs) {
+    float* bias = sbias + ew * LCPW;
+    uint64_t* tf = &tfull[2 * half];
+    uint32_t it = 0;
+    for (int t = pair; t < ntiles; t += npairs) {
       int tp, tq;
       tile_of(t, g.ntp, g.ntq, tp, tq);
       const int rbase = tp * 2 * BM + (int)crank * BM + q * 32;
@@ -318,112 +343,139 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       float acc[LCPW];
 #pragma unroll
       for (int i = 0; i < LCPW; ++i) acc[i] = 0.f;
+      __syncwarp();  // the last tile's bias has been read
+#pragma unroll
+      for (int e = 0; e < LCPW; e += 32)
+        bias[e + lane] = g.bias && cbase + e + lane < g.Q ? __ldg(g.bias + cbase + e + lane) : 0.f;
+      // Between a k-block's last read and the next one's first, the tensor
+      // cores may be waiting for this warp: the next k-block's scales are read
+      // and its barrier is tested before the last chunk's arithmetic, and its
+      // first read is issued there if its product is already in.
+      constexpr int LD = 32, NC = LCPW / LD;
+      static_assert(NC % 2 == 0, "each k-block starts with the same registers");
+      uint32_t r[2][LD];
+      uint64_t row2 = 0;
+      const float* cs = nullptr;
+      bool ok = true;
+      auto scales = [&](uint32_t j) {  // of k-block j, counted over the tiles
+        if (j % LGROUP == 0)
+          ok = ptx::mbar_wait(&sfull[(j / LGROUP) % LGROUPS], (j / (LGROUP * LGROUPS)) & 1u, kWaitTimeoutNs, abort_flag);
+        const float* d = slots + j % (LGROUP * LGROUPS) * LSLOT;
+        float f = d[q * 32 + lane];
+        if constexpr (!COLS) f *= d[BM + half];
+        row2 = ptx::pack2(f, f);
+        cs = d + BM + half * LCPW;
+      };
+      scales(it);
+      bool early = false, live = true;
       for (int kb = 0; kb < nkb; ++kb, ++it) {
-        const int b = it & 1;
-        const int sl = it % LSLOTS;
-        const float* d = slots + sl * LSLOT;
-        bool ok = ptx::mbar_wait(&sfull[sl], (uint32_t)(it / LSLOTS) & 1u, kWaitTimeoutNs, abort_flag);
-        float row = d[q * 32 + lane];
-        if constexpr (!COLS) row *= d[BM + half];
-        ok = ok && ptx::mbar_wait(&tfull[b], (uint32_t)(it >> 1) & 1u, kWaitTimeoutNs, abort_flag);
-        if (!ok) latch(g.err, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) {
-          live = false;
-          break;
+        const uint32_t b = it & 1u, at = trow + b * LCPW;
+        if (!early) {
+          ok = ok && ptx::mbar_wait(&tf[b], (it >> 1) & 1u, kWaitTimeoutNs, abort_flag);
+          if (!ok) latch(g.err, abort_flag);
+          live = __all_sync(0xffffffffu, ok);
+          if (!live) break;
+          ptx::tc_fence_after();
+          tmem_read<LD>(at, r[0]);
         }
-        ptx::tc_fence_after();
-        promote<LCPW, COLS>(acc, trow + (uint32_t)(b * LN), row, d + BM + half * LCPW, [&]() {
-          ptx::tc_fence_before();
-          __syncwarp();
-          // the arrival orders TMEM reads only (the fence above), so it needs
-          // no cluster-wide release of memory
-          if (lane == 0) ptx::mbar_arrive_at(te0 + 8u * (uint32_t)b);
-        });
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sempty[sl]);
+        const uint64_t now2 = row2;
+        const float* nowc = cs;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          ptx::tmem_ld_wait_for(r[c & 1]);
+          if (c + 1 < NC) {
+            tmem_read<LD>(at + (c + 1) * LD, r[(c + 1) & 1]);
+          } else {
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              // the arrival orders TMEM reads only (the fence above), so it
+              // needs no cluster-wide release of memory
+              ptx::mbar_arrive_at(te0 + 8u * b);
+              // the scales of the group before this k-block are used up
+              if (it % LGROUP == 0 && it > 0) ptx::mbar_arrive(&sempty[(it / LGROUP - 1) % LGROUPS]);
+            }
+            early = false;
+            if (kb + 1 < nkb) {
+              scales(it + 1);
+              early = __all_sync(0xffffffffu, ok && ptx::mbar_test(&tf[b ^ 1u], ((it + 1) >> 1) & 1u));
+              if (early) {
+                ptx::tc_fence_after();
+                tmem_read<LD>(trow + (b ^ 1u) * LCPW, r[0]);
+              }
+            }
+          }
+          scaled_add<LD, COLS>(acc + c * LD, r[c & 1], now2, nowc + c * LD);
+        }
       }
       if (!live) break;
       if (t + npairs >= ntiles && threadIdx.x == 128) ptx::griddep_launch_dependents();
       // Store: 128 bytes of each of the warp's 32 rows at a time through the
-      // swizzled staging block, then whole row segments.
+      // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
+      // clips what lies past the matrix, and the warp need not wait for the
+      // memory), else element by element along the rows.
       const int es = g.out_bf16 ? 2 : 4;
-      const bool vec = ((reinterpret_cast<uintptr_t>(g.c) | (uintptr_t)(g.ldc * es)) & 15) == 0;
-      auto flush = [&](int col0, int cols) {  // staged columns col0 .. col0 + cols of C
-        __syncwarp();
-        if (vec) {
-          const int u = lane & 7, per = 16 / es, col = col0 + u * per;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int rr = i * 4 + (lane >> 3);
-            const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((u ^ (rr & 7)) << 4));
-            if (rbase + rr >= g.P || col >= g.Q) continue;
-            char* dst = static_cast<char*>(g.c) + ((long long)(rbase + rr) * g.ldc + col) * es;
-            if (col + per <= g.Q) {
-              *reinterpret_cast<uint4*>(dst) = w;
-            } else if (es == 2) {
-              const uint32_t h[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (col + e < g.Q) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
-            } else {
-              const uint32_t h[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (col + e < g.Q) reinterpret_cast<uint32_t*>(dst)[e] = h[e];
-            }
-          }
-        } else {
-          for (int rr = 0; rr < 32 && rbase + rr < g.P; ++rr)
-            for (int j = lane; j < cols && col0 + j < g.Q; j += 32) {
-              const int byte = j * es;
-              const uint8_t* src = stage + rr * 128 + (((byte >> 4) ^ (rr & 7)) << 4) + (byte & 15);
-              const long long at = (long long)(rbase + rr) * g.ldc + col0 + j;
-              if (es == 2)
-                static_cast<uint16_t*>(g.c)[at] = *reinterpret_cast<const uint16_t*>(src);
-              else
-                static_cast<uint32_t*>(g.c)[at] = *reinterpret_cast<const uint32_t*>(src);
-            }
+      auto block = [&](int ch) {  // staging block of chunk ch, free again
+        if (g.tma_c) {
+          if (lane == 0) ptx::bulk_wait_read1();
         }
         __syncwarp();
+        return stage + (ch & 1) * (LSTAGING / 2);
       };
-      auto value = [&](int i, int col) {  // accumulator pair i with bias and activation
-        float2 v = make_float2(acc[2 * i], acc[2 * i + 1]);
-        if (g.bias) {
-          v.x += col < g.Q ? __ldg(g.bias + col) : 0.f;
-          v.y += col + 1 < g.Q ? __ldg(g.bias + col + 1) : 0.f;
+      auto flush = [&](uint8_t* from, int col0, int cols) {  // staged columns col0 .. col0 + cols of C
+        if (g.tma_c) {
+          ptx::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (rbase < g.P && col0 < g.Q) ptx::tma_store_2d(&tmC, from, col0, rbase);
+            ptx::bulk_commit();
+          }
+          return;
         }
-        return make_float2(finish(v.x, g.relu), finish(v.y, g.relu));
+        __syncwarp();
+        for (int rr = 0; rr < 32 && rbase + rr < g.P; ++rr)
+          for (int j = lane; j < cols && col0 + j < g.Q; j += 32) {
+            const int byte = j * es;
+            const uint8_t* src = from + rr * 128 + (((byte >> 4) ^ (rr & 7)) << 4) + (byte & 15);
+            const long long at = (long long)(rbase + rr) * g.ldc + col0 + j;
+            if (es == 2)
+              static_cast<uint16_t*>(g.c)[at] = *reinterpret_cast<const uint16_t*>(src);
+            else
+              static_cast<uint32_t*>(g.c)[at] = *reinterpret_cast<const uint32_t*>(src);
+          }
+      };
+      // four accumulators with bias and activation
+      auto value = [&](int i) {
+        const float4 v = *reinterpret_cast<const float4*>(bias + i);
+        return make_float4(finish(acc[i] + v.x, g.relu), finish(acc[i + 1] + v.y, g.relu),
+                           finish(acc[i + 2] + v.z, g.relu), finish(acc[i + 3] + v.w, g.relu));
       };
       if (g.out_bf16) {
 #pragma unroll
         for (int ch = 0; ch < LCPW / 64; ++ch) {
+          uint8_t* to = block(ch);
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int i = ch * 32 + u * 4 + e;
-              const float2 v = value(i, cbase + 2 * i);
-              const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
-              w[e] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            *reinterpret_cast<uint4*>(stage + lane * 128 + ((u ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            const float4 v = value(ch * 64 + u * 8), w = value(ch * 64 + u * 8 + 4);
+            const __nv_bfloat162 h[4] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w),
+                                         __floats2bfloat162_rn(w.x, w.y), __floats2bfloat162_rn(w.z, w.w)};
+            *reinterpret_cast<uint4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(h);
           }
-          flush(cbase + ch * 64, 64);
+          flush(to, cbase + ch * 64, 64);
         }
       } else {
 #pragma unroll
         for (int ch = 0; ch < LCPW / 32; ++ch) {
+          uint8_t* to = block(ch);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int i = ch * 16 + u * 2;
-            const float2 v = value(i, cbase + 2 * i), w = value(i + 1, cbase + 2 * i + 2);
-            *reinterpret_cast<float4*>(stage + lane * 128 + ((u ^ (lane & 7)) << 4)) = make_float4(v.x, v.y, w.x, w.y);
-          }
-          flush(cbase + ch * 32, 32);
+          for (int u = 0; u < 8; ++u)
+            *reinterpret_cast<float4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = value(ch * 32 + u * 4);
+          flush(to, cbase + ch * 32, 32);
         }
       }
     }
+    if (lane == 0) ptx::bulk_wait_read0();
+    __syncwarp();
   }
 
   ptx::tc_fence_before();
@@ -456,7 +508,7 @@ struct SCfg {
   static constexpr uint32_t ACC = BN < 32 ? 32 : BN;      // TMEM columns of a buffer
   static constexpr uint32_t TCOLS = BUFS * ACC;
   static constexpr int PITCH = BM + 1;                    // floats per column of the exchange buffer
-  static constexpr int SLOTS = 4;                         // as LSLOTS
+  static constexpr int SLOTS = 4;                         // k-blocks of scales in flight or in use
   static constexpr int SLOT = 32 + (CPW < 32 ? 32 : CPW);
   static constexpr int SLOT_BYTES = EPI * SLOTS * SLOT * 4;
   static constexpr int SMEM = 1024 + STAGES * STAGE + SLOT_BYTES + 512;
@@ -574,7 +626,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int prow = min(p0 + q * 32 + lane, g.P - 1);
     const int cbase = q0 + half * C::CPW;
     float* sl = slots + ew * C::SLOTS * C::SLOT;
-    // scales three k-blocks ahead of their use, as in the pair kernel
+    // scales three k-blocks ahead of their use
     auto fetch = [&](int it) {
       if (it < nkb) {
         float* d = sl + (it % C::SLOTS) * C::SLOT;
@@ -594,7 +646,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int it = 0; it < nkb; ++it) {
       const int b = it % C::BUFS;
       ptx::cp_async_wait<C::SLOTS - 2>();
-      __syncwarp();
+      __syncwarp();  // every lane's copies of this slot, and its use of the slot filled next
       const float* d = sl + (it % C::SLOTS) * C::SLOT;
       float row = d[lane];
       if constexpr (!COLS) row *= d[32 + lane];
@@ -675,9 +727,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // ------------------------------------------------------------------- host
-template <typename F>
-cudaError_t launch(F* kernel, unsigned grid, int threads, int cluster, int smem, cudaStream_t st, const CUtensorMap& p,
-                   const CUtensorMap& q, const Args& g, int ks_log = -1) {
+template <typename F, typename... A>
+cudaError_t launch(F* kernel, unsigned grid, int threads, int cluster, int smem, cudaStream_t st, const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3((unsigned)threads);
@@ -691,10 +742,7 @@ cudaError_t launch(F* kernel, unsigned grid, int threads, int cluster, int smem,
   at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  if constexpr (std::is_invocable_v<F, CUtensorMap, CUtensorMap, Args, int>)
-    return cudaLaunchKernelEx(&cfg, kernel, p, q, g, ks_log);
-  else
-    return cudaLaunchKernelEx(&cfg, kernel, p, q, g);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 // CTA pairs the GPU holds at once (one CTA per SM; an SM without a partner in
@@ -806,21 +854,24 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
   if ((long long)g.ntp * g.ntq << pl.ks_log > 0x3FFFFFFFll) return FF_ERR_UNSUPPORTED;
   CUtensorMap p, q;
   if (!make_sw128_map(&p, pl.swap ? f.b : f.a, 1, f.K, g.P, ld, KB, BM) ||
-      !make_sw128_map(&q, pl.swap ? f.a : f.b, 1, f.K, g.Q, ld, KB, pairk ? LN / 2 : pl.bn))
+      !make_sw128_map(&q, pl.swap ? f.a : f.b, 1, f.K, g.Q, ld, KB, pairk ? LN / 4 : pl.bn))
     return FF_ERR_INVALID_ARG;
+  const int es = f.out_bf16 ? 2 : 4;
+  CUtensorMap c = p;
+  g.tma_c = pairk && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N && make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
   const double work = 2.0 * f.M * f.N * f.K;
   auto go = [&]() -> cudaError_t {
     if (pairk) {
       const unsigned grid = 2u * (unsigned)std::min((long long)pairs, (long long)g.ntp * g.ntq);
-      return cols ? launch(k_fp8_pair<true>, grid, LTHREADS, 2, L_SMEM, st, p, q, g)
-                  : launch(k_fp8_pair<false>, grid, LTHREADS, 2, L_SMEM, st, p, q, g);
+      return cols ? launch(k_fp8_pair<true>, grid, LTHREADS, 2, L_SMEM, st, p, q, c, g)
+                  : launch(k_fp8_pair<false>, grid, LTHREADS, 2, L_SMEM, st, p, q, c, g);
     }
-    const bool c = cols || pl.swap;
+    const bool each = cols || pl.swap;
     switch (pl.bn) {
       case 16: return run_split<16, true>(p, q, g, pl.ks_log, st);
       case 32: return run_split<32, true>(p, q, g, pl.ks_log, st);
       case 64: return run_split<64, true>(p, q, g, pl.ks_log, st);
-      default: return c ? run_split<128, true>(p, q, g, pl.ks_log, st) : run_split<128, false>(p, q, g, pl.ks_log, st);
+      default: return each ? run_split<128, true>(p, q, g, pl.ks_log, st) : run_split<128, false>(p, q, g, pl.ks_log, st);
     }
   };
   FF_LAUNCH(K_FP8_GEMM, work, st, go(), "8-bit matrix product");
