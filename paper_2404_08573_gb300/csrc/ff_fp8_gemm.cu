@@ -504,7 +504,7 @@ struct SCfg {
   static constexpr int STAGE = (BM + BN) * KB;
   static constexpr int STAGES = BN >= 128 ? 6 : BN >= 64 ? 8 : 9;
   static constexpr int CPW = BN / 2;
-  static constexpr int BUFS = 2;                          // TMEM buffers (the loops count on two)
+  static constexpr int BUFS = 4;                          // TMEM buffers (a power of 2)
   static constexpr uint32_t ACC = BN < 32 ? 32 : BN;      // TMEM columns of a buffer
   static constexpr uint32_t TCOLS = BUFS * ACC;
   static constexpr int PITCH = BM + 1;                    // floats per column of the exchange buffer
@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int s = 0;
       uint32_t ph = 0, tph = 1;
       for (int it = 0; it < nkb; ++it) {
-        const uint32_t b = (uint32_t)it & 1u;
+        const uint32_t b = (uint32_t)it % C::BUFS;
         const bool ok = ptx::mbar_wait(&tempty[b], tph, kWaitTimeoutNs, abort_flag) &&
                         ptx::mbar_wait(&full[s], ph, kWaitTimeoutNs, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) {
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           ptx::umma_commit(&tfull[b]);
         }
         __syncwarp();
-        tph ^= b;
+        tph ^= b == C::BUFS - 1 ? 1u : 0u;
         if (++s == C::STAGES) {
           s = 0;
           ph ^= 1u;
@@ -696,12 +696,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     ptx::cluster_sync();
   else
     __syncthreads();
+  const int qs = q0 + rank * share;
   auto total = [&](int col, int row) {
     float v = buf[col * C::PITCH + row];
     for (int r = 1; r < ks; ++r) v += buf[(r * share + col) * C::PITCH + row];
     return v;
   };
-  const int qs = q0 + rank * share;
   auto put = [&](long long at, float v) {
     if (g.out_bf16)
       static_cast<bf16*>(g.c)[at] = __float2bfloat16_rn(v);
@@ -713,15 +713,20 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int row = threadIdx.x & (BM - 1), n = p0 + row;
     if (threadIdx.x < 2 * BM && n < g.P) {
       const float bias = g.bias ? __ldg(g.bias + n) : 0.f;
-      for (int col = threadIdx.x >> 7; col < share && qs + col < g.Q; col += 2)
+      const int cols = min(share, g.Q - qs);
+#pragma unroll 4
+      for (int col = threadIdx.x >> 7; col < cols; col += 2)
         put((long long)(qs + col) * g.ldc + n, finish(total(col, row) + bias, g.relu));
     }
   } else {
-    for (int i = threadIdx.x; i < BM * share; i += THREADS) {
-      const int row = i / share, col = i - row * share;
-      if (p0 + row < g.P && qs + col < g.Q)
-        put((long long)(p0 + row) * g.ldc + qs + col,
-            finish(total(col, row) + (g.bias ? __ldg(g.bias + qs + col) : 0.f), g.relu));
+    // lanes along the tile's columns, 32 (or the share) of a row at a time
+    const int w = share < 32 ? share : 32, per = 32 / w;
+    for (int c0 = lane & (w - 1); c0 < share; c0 += 32) {
+      if (qs + c0 >= g.Q) break;
+      const float bias = g.bias ? __ldg(g.bias + qs + c0) : 0.f;
+#pragma unroll 4
+      for (int row = warp * per + lane / w; row < BM; row += THREADS / 32 * per)
+        if (p0 + row < g.P) put((long long)(p0 + row) * g.ldc + qs + c0, finish(total(c0, row) + bias, g.relu));
     }
   }
 }
@@ -788,41 +793,79 @@ cudaError_t run_split(const CUtensorMap& p, const CUtensorMap& q, const Args& g,
                 ks_log);
 }
 
-// The shape of a product: tile and split with the least estimated time, in
-// clocks.  A CTA spends on a k-block the longest of its MMAs (8192 MAC a
-// clock), its operand feed (about 73 bytes a clock) and its share of HBM, and
-// a fixed cost per launch wave.
+// Clusters of a split kernel the GPU holds at once.
+template <int BN, bool COLS>
+int resident_clusters(int ks_log) {
+  struct Counts { int n[4]; };
+  static const Counts c = [] {
+    Counts r{};
+    if (split_attr<BN, COLS>() != cudaSuccess) return r;
+    for (int l = 0; l < 4; ++l) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(1u << l);
+      cfg.blockDim = dim3(THREADS);
+      cfg.dynamicSmemBytes = SCfg<BN>::SMEM;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = 1u << l;
+      at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&r.n[l], k_fp8_split<BN, COLS>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        r.n[l] = 0;
+      }
+    }
+    return r;
+  }();
+  return c.n[ks_log];
+}
+int clusters_of(int bn, bool each, int ks_log) {
+  switch (bn) {
+    case 16: return resident_clusters<16, true>(ks_log);
+    case 32: return resident_clusters<32, true>(ks_log);
+    case 64: return resident_clusters<64, true>(ks_log);
+    default: return each ? resident_clusters<128, true>(ks_log) : resident_clusters<128, false>(ks_log);
+  }
+}
+
+// The shape of a product: tile, orientation and split with the least
+// estimated time.  The constants (us) are least-squares readings of a sweep of
+// all shapes over 23 sizes from 1 x 2000 x 2000 to 512 x 8192 x 8192: a wave
+// of tiles takes a time per k-block and a fixed one (launch, fill, exchange,
+// store), and no shape moves its operands faster than about 9 TB/s.
 struct Plan {
   int bn;      // 256: the pair kernel
   bool swap;
   int ks_log;
 };
-Plan plan(int M, int N, int K, int pairs) {
+Plan plan(int M, int N, int K, bool cols, int pairs) {
   const double nkb = cdiv(K, KB);
   Plan best{LN, false, 0};
   double t = 1e30;
   if (pairs > 0) {
     const double tiles = (double)cdiv(M, 2 * BM) * cdiv(N, LN);
-    t = std::max(1.0, std::ceil(tiles / pairs)) * (nkb * 560 + 1500) + 3000;
+    t = 3.5 + std::ceil(tiles / pairs) * (nkb * (cols ? 0.62 : 0.38) + 1.0);
   }
-  const int sizes[4] = {16, 32, 64, 128};
-  for (int swap = 0; swap < 2; ++swap)
-    for (int bn : sizes) {
-      if (!swap && bn != 128) continue;
-      const int P = swap ? N : M, Q = swap ? M : N;
-      const double tiles = (double)cdiv(P, BM) * cdiv(Q, bn);
-      for (int l = 0; l < 4; ++l) {
-        if ((1 << l) > nkb) break;
-        const double per = std::ceil(nkb / (1 << l));
-        const double ctas = tiles * (1 << l), waves = std::ceil(ctas / 144);  // clusters of 8 do not use every SM
-        const double step = std::max(2.0 * bn, (BM + bn) * KB / 73.0);
-        const double c = waves * (per * step + 2000) + 3000 + (l ? 800 : 0) + bn * 8.0;
-        if (c < t) {
-          t = c;
-          best = Plan{bn, swap != 0, l};
-        }
+  struct Shape { int bn; bool swap; double step, fixed; };
+  const Shape shapes[5] = {
+      {16, true, 0.24, 2.9}, {32, true, 0.30, 3.2}, {64, true, 0.28, 4.6}, {128, true, 0.42, 6.0},
+      {128, false, cols ? 0.42 : 0.31, 7.0}};
+  for (const Shape& sh : shapes) {
+    const int P = sh.swap ? N : M, Q = sh.swap ? M : N;
+    const double tiles = (double)cdiv(P, BM) * cdiv(Q, sh.bn);
+    const double moved = tiles * nkb * (BM + sh.bn) * KB / 9e6;
+    for (int l = 0; l < 4; ++l) {
+      const int room = clusters_of(sh.bn, sh.swap || cols, l);
+      if ((1 << l) > nkb || room < 1) break;
+      const double waves = std::ceil(tiles / room), per = std::ceil(nkb / (1 << l));
+      const double c = sh.fixed + (l ? 0.5 : 0.0) + std::max(moved, waves * per * sh.step + (waves - 1) * sh.fixed);
+      if (c < t) {
+        t = c;
+        best = Plan{sh.bn, sh.swap, l};
       }
     }
+  }
   return best;
 }
 
@@ -832,7 +875,7 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
   const int ld = fp8_stride(f.K);
   const bool cols = !f.b_tiles;
   const int pairs = cols ? resident_pairs<true>() : resident_pairs<false>();
-  const Plan pl = plan(f.M, f.N, f.K, pairs);
+  const Plan pl = plan(f.M, f.N, f.K, cols, pairs);
   Args g{};
   const Scales sa{f.sa, f.M, 0};
   const Scales sb{f.sb, f.b_tiles ? cdiv(f.N, KB) : f.N, f.b_tiles ? 7 : 0};
