@@ -4,6 +4,7 @@
 
 #include "ff_api_internal.h"
 #include "ff_fp8.h"
+#include "ff_ptx.cuh"
 #include "ff_vec.cuh"
 
 namespace ff {
@@ -19,53 +20,93 @@ __device__ __forceinline__ float scale_of(uint32_t amax_bits) {
   const float s = __fdiv_rn(__uint_as_float(amax_bits), kE4m3Max);
   return s < kScaleMin ? kScaleMin : s;  // keeps NaN
 }
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 // Two values as e4m3 (to nearest even, saturating; NaN stays NaN), a in the low byte.
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
+__device__ __forceinline__ uint2 e4m3x8(const float (&v)[8]) {
+  return make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+}
+
+// Eight values of a row as loaded: bf16 in pairs (the low half first), or fp32.
+// Magnitudes are compared as integers, bf16 two at a time.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16> {
+  static constexpr int WORDS = 4, PER = 2;  // PER: values per word
+  static constexpr uint32_t ABS = 0x7FFF7FFFu;
+  static __device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float value(const uint32_t (&w)[WORDS], int e) {
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  }
+  // the magnitude in half `h` of a word, as the bits of a float
+  static __device__ __forceinline__ uint32_t bits(uint32_t w, int h) { return h ? w & 0xFFFF0000u : w << 16; }
+};
+template <>
+struct Eight<float> {
+  static constexpr int WORDS = 8, PER = 1;
+  static constexpr uint32_t ABS = 0x7FFFFFFFu;
+  static __device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return max(a, b); }
+  static __device__ __forceinline__ float value(const uint32_t (&w)[WORDS], int e) { return __uint_as_float(w[e]); }
+  static __device__ __forceinline__ uint32_t bits(uint32_t w, int) { return w; }
+};
 
 constexpr int QB = 128;          // a block of the matrix: 128 x 128
 constexpr int kQThreads = 256;
-constexpr int kTPitch = QB + 8;  // bytes per column of the transposed tile in shared memory
 
 // One thread block per 128 x 128 tile.  Thread (rg, cg) holds rows
-// 8 rg .. 8 rg + 7 of columns 8 cg .. 8 cg + 7 in registers: a row block's
-// maximum is 8 values and a shuffle over the 16 threads of a row group, a
-// column block's 8 values and one pass over the 16 row groups, and both
-// orientations are formed from one read.
+// 8 rg .. 8 rg + 7 of columns 8 cg .. 8 cg + 7 as loaded (all loads in flight
+// together).  A row block's maximum is formed by the 16 threads of a row
+// group, each step handing half of the rows to the partner, so that a thread
+// ends with one row, divides once, and passes the reciprocal round; a column
+// block's by one pass over the 16 row groups in shared memory.  Both
+// orientations come from one read.  Bound by HBM: x once, each orientation
+// once.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kQThreads) k_fp8_quantize(const T* x, long long ldx, int rows, int k, int tile,
-                                                            uint8_t* q, float* scale, uint8_t* qt, float* scale_t,
-                                                            int ldq, int ldqt, int kblocks, int rblocks) {
-  __shared__ uint32_t cmax[16][QB];
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
+    k_fp8_quantize(const T* x, long long ldx, int rows, int k, int tile, uint8_t* q, float* scale, uint8_t* qt,
+                   float* scale_t, int ldq, int ldqt, int kblocks, int rblocks) {
+  using E = Eight<T>;
+  constexpr int W = E::WORDS, PER = E::PER;
+  __shared__ uint32_t cmax[16][QB / PER];
   __shared__ float cinv[QB];
   __shared__ uint32_t wmax[kQThreads / 32];
-  __shared__ __align__(16) uint8_t tq[QB * kTPitch];
+  // the transposed tile: 128 bytes per column, its 8-byte units permuted so
+  // that the 16 column groups of a warp's writes fall into different banks
+  __shared__ __align__(16) uint8_t tq[QB * QB];
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
   const int kb = blockIdx.x % kblocks, rb = blockIdx.x / kblocks;
   const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
   const int row0 = rb * QB + rg * 8, c0 = kb * QB + cg * 8;
-  float v[8][8];
+  uint32_t v[8][W];
+  if (VEC && c0 + 8 <= k) {
+    const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = row0 + i;
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-    if (r < rows) {
-      const T* p = x + (long long)r * ldx + c0;
-      if (VEC && c0 + 8 <= k) {
-        Vec8<T>::load(p, v[i]);
-      } else {
+      for (int j = 0; j < W / 4; ++j)
+        *reinterpret_cast<uint4*>(&v[i][4 * j]) =
+            row0 + i < rows ? reinterpret_cast<const uint4*>(p + i * ldx)[j] : make_uint4(0, 0, 0, 0);
+  } else {
+    const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c0 + e < k) {
-            float one[1];
-            Vec<T, 1>::unpack(Vec<T, 1>::load(p + e), one);
-            v[i][e] = one[0];
-          }
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int h = 0; h < PER; ++h)
+          if (row0 + i < rows && c0 + j * PER + h < k)
+            w |= (uint32_t)Vec<T, 1>::load(p + i * ldx + j * PER + h) << (16 * h);
+        v[i][j] = w;
       }
-    }
   }
   float inv_tile = 0.f;
   if (tile) {
@@ -73,7 +114,8 @@ __global__ void __launch_bounds__(kQThreads) k_fp8_quantize(const T* x, long lon
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, abs_bits(v[i][e]));
+      for (int j = 0; j < W; ++j) m = E::max_of(m, v[i][j] & E::ABS);
+    m = max(E::bits(m, 0), E::bits(m, 1));
     m = __reduce_max_sync(0xffffffffu, m);
     if ((threadIdx.x & 31) == 0) wmax[threadIdx.x >> 5] = m;
     __syncthreads();
@@ -87,45 +129,69 @@ __global__ void __launch_bounds__(kQThreads) k_fp8_quantize(const T* x, long lon
     }
   }
   if (q) {
+    float inv_row = inv_tile;
+    if (!tile) {
+      // word j of m: rows j PER .. (one per half of the word)
+      uint32_t m[8 / PER];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t t = v[i][0] & E::ABS;
+#pragma unroll
+        for (int j = 1; j < W; ++j) t = E::max_of(t, v[i][j] & E::ABS);
+        if constexpr (PER == 2) {
+          t = max(t & 0xFFFFu, t >> 16);
+          m[i / 2] = i & 1 ? m[i / 2] | t << 16 : t;
+        } else {
+          m[i] = t;
+        }
+      }
+      int bit = 8;
+#pragma unroll
+      for (int n = 8 / PER; n > 1; n /= 2) {
+#pragma unroll
+        for (int j = 0; j < n / 2; ++j) {
+          const bool up = (cg & bit) != 0;
+          const uint32_t give = up ? m[j] : m[j + n / 2], keep = up ? m[j + n / 2] : m[j];
+          m[j] = E::max_of(keep, __shfl_xor_sync(0xffffffffu, give, bit));
+        }
+        bit >>= 1;
+      }
+      for (; bit > 0; bit >>= 1) m[0] = E::max_of(m[0], __shfl_xor_sync(0xffffffffu, m[0], bit));
+      // this thread's row: the bits of cg that chose, from the top (bf16: 8, 4,
+      // and bit 0 picks the half; fp32: 8, 4, 2)
+      const int mine = PER == 2 ? (cg >> 3 & 1) * 4 + (cg >> 2 & 1) * 2 + (cg & 1) : cg >> 1;
+      const float s = scale_of(E::bits(m[0], cg & 1));
+      inv_row = __frcp_rn(s);
+      const bool writer = PER == 2 ? (cg & 2) == 0 : (cg & 1) == 0;
+      if (writer && row0 + mine < rows) scale[(long long)kb * rows + row0 + mine] = s;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+      const int src = PER == 2 ? (i >> 2) * 8 + (i >> 1 & 1) * 4 + (i & 1) : i * 2;
+      const float inv = tile ? inv_tile : __shfl_sync(0xffffffffu, inv_row, (threadIdx.x & 16) | src);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(E::value(v[i], e), inv);
       const int r = row0 + i;
-      float inv = inv_tile;
-      if (!tile) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, abs_bits(v[i][e]));
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const float s = scale_of(m);
-        inv = __frcp_rn(s);
-        if (cg == 0 && r < rows) scale[(long long)kb * rows + r] = s;
-      }
-      if (r < rows && c0 < ldq) {  // ldq is a multiple of 16: a group of 8 columns lies inside or outside
-        uint2 w;
-        w.x = e4m3x2(__fmul_rn(v[i][0], inv), __fmul_rn(v[i][1], inv)) |
-              e4m3x2(__fmul_rn(v[i][2], inv), __fmul_rn(v[i][3], inv)) << 16;
-        w.y = e4m3x2(__fmul_rn(v[i][4], inv), __fmul_rn(v[i][5], inv)) |
-              e4m3x2(__fmul_rn(v[i][6], inv), __fmul_rn(v[i][7], inv)) << 16;
-        *reinterpret_cast<uint2*>(q + (long long)r * ldq + c0) = w;
-      }
+      // ldq is a multiple of 16: a group of 8 columns lies inside or outside
+      if (r < rows && c0 < ldq) *reinterpret_cast<uint2*>(q + (long long)r * ldq + c0) = e4m3x8(f);
     }
   }
   if (qt) {
     if (!tile) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t m = 0;
+      for (int j = 0; j < W; ++j) {
+        uint32_t m = v[0][j] & E::ABS;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i][e]));
-        cmax[rg][cg * 8 + e] = m;
+        for (int i = 1; i < 8; ++i) m = E::max_of(m, v[i][j] & E::ABS);
+        cmax[rg][cg * W + j] = m;
       }
       __syncthreads();
       if (threadIdx.x < QB) {
         uint32_t m = 0;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) m = max(m, cmax[t][threadIdx.x]);
-        const float s = scale_of(m);
+        for (int t = 0; t < 16; ++t) m = E::max_of(m, cmax[t][threadIdx.x / PER]);
+        const float s = scale_of(E::bits(m, threadIdx.x & 1));
         cinv[threadIdx.x] = __frcp_rn(s);
         const int c = kb * QB + threadIdx.x;
         if (c < k) scale_t[(long long)rb * k + c] = s;
@@ -135,20 +201,24 @@ __global__ void __launch_bounds__(kQThreads) k_fp8_quantize(const T* x, long lon
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float inv = tile ? inv_tile : cinv[cg * 8 + e];
-      uint2 w;
-      w.x = e4m3x2(__fmul_rn(v[0][e], inv), __fmul_rn(v[1][e], inv)) |
-            e4m3x2(__fmul_rn(v[2][e], inv), __fmul_rn(v[3][e], inv)) << 16;
-      w.y = e4m3x2(__fmul_rn(v[4][e], inv), __fmul_rn(v[5][e], inv)) |
-            e4m3x2(__fmul_rn(v[6][e], inv), __fmul_rn(v[7][e], inv)) << 16;
-      *reinterpret_cast<uint2*>(tq + (cg * 8 + e) * kTPitch + rg * 8) = w;
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(E::value(v[i], e), inv);
+      *reinterpret_cast<uint2*>(tq + (cg * 8 + e) * QB + ((rg ^ cg) << 3)) = e4m3x8(f);
     }
     __syncthreads();
-    // 16 threads per column of the tile, 8 bytes each
-    for (int c = threadIdx.x >> 4; c < QB; c += kQThreads / 16) {
-      const int col = kb * QB + c, r = rb * QB + (threadIdx.x & 15) * 8;
-      if (col < k && r < ldqt)
-        *reinterpret_cast<uint2*>(qt + (long long)col * ldqt + r) =
-            *reinterpret_cast<const uint2*>(tq + c * kTPitch + (threadIdx.x & 15) * 8);
+    // 8 threads per column of the tile, 16 bytes each (ldqt is a multiple of 16)
+    const int u = threadIdx.x & 7, r = rb * QB + u * 16;
+    if (r < ldqt) {
+#pragma unroll
+      for (int c = threadIdx.x >> 3; c < QB; c += kQThreads / 8) {
+        const int col = kb * QB + c;
+        if (col >= k) break;
+        const uint8_t* t = tq + c * QB;
+        const uint2 a = *reinterpret_cast<const uint2*>(t + (((2 * u) ^ (c >> 3)) << 3));
+        const uint2 b = *reinterpret_cast<const uint2*>(t + (((2 * u + 1) ^ (c >> 3)) << 3));
+        *reinterpret_cast<uint4*>(qt + (long long)col * ldqt + r) = make_uint4(a.x, a.y, b.x, b.y);
+      }
     }
   }
 }
@@ -162,12 +232,12 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, int tile, uint8
   const double bytes = (double)rows * k * (sizeof(T) + (q ? 1 : 0) + (qt ? 1 : 0));
   const int ldq = fp8_stride(k), ldqt = fp8_stride(rows);
   const bool vec = rows_aligned(x, ldx, sizeof(T), 16);
+  PdlLaunch l(dim3((unsigned)blocks), dim3(kQThreads), st);
   FF_LAUNCH(K_FP8_QUANT, bytes, st,
-            ((vec ? k_fp8_quantize<T, true><<<(unsigned)blocks, kQThreads, 0, st>>>(
-                        x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq, ldqt, kblocks, rblocks)
-                  : k_fp8_quantize<T, false><<<(unsigned)blocks, kQThreads, 0, st>>>(
-                        x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq, ldqt, kblocks, rblocks)),
-             cudaGetLastError()),
+            vec ? cudaLaunchKernelEx(&l.cfg, k_fp8_quantize<T, true>, x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq,
+                                     ldqt, kblocks, rblocks)
+                : cudaLaunchKernelEx(&l.cfg, k_fp8_quantize<T, false>, x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq,
+                                     ldqt, kblocks, rblocks),
             "8-bit quantize");
   return FF_OK;
 }
