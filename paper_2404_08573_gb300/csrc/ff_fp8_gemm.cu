@@ -70,8 +70,8 @@ __device__ __forceinline__ void scaled_add(float* acc, const uint32_t (&p)[LD], 
       f0 = ptx::mul2(row2, v.x);
       f1 = ptx::mul2(row2, v.y);
     }
-    ptx::fma2(lo, f0, ptx::pack2(p[i], p[i + 1]));
-    ptx::fma2(hi, f1, ptx::pack2(p[i + 2], p[i + 3]));
+    ptx::fma2_to(lo, f0, ptx::pack2(p[i], p[i + 1]));
+    ptx::fma2_to(hi, f1, ptx::pack2(p[i + 2], p[i + 3]));
     const float2 x = ptx::unpack2(lo), y = ptx::unpack2(hi);
     d[0] = x.x;
     d[1] = x.y;

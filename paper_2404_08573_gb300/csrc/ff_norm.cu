@@ -13,36 +13,15 @@
 // column sums over chunks of positions (k_gn_colstats, k_gn_grad_colsums), a
 // small fold per group, and an element-wise pass -- whatever the group's
 // width, since a 16-byte vector may span groups.
+//
+// Groups that fit registers take one of two faster paths, which read x (and
+// dy) once: rows (ff_norm_rows.cu) and clusters (ff_norm_cluster.cu).
 #include <cmath>
 
-#include "ff_api_internal.h"
-#include "ff_ptx.cuh"
-#include "ff_vec.cuh"
+#include "ff_norm.cuh"
 
 namespace ff {
 namespace {
-
-struct GnShape {
-  int n, S, C, G, Cg;
-  long long ldx, ldy, lddy;  // forward: x -> y; gradient: (dy, x) -> dx with ldy the stride of dx
-  float eps;
-  int act;
-};
-
-__device__ __forceinline__ float act_of(float u, int act) {
-  if (act == FF_ACT_RELU) return u < 0.f ? 0.f : u;  // keeps NaN
-  if (act == FF_ACT_SILU) return u * __fdividef(1.f, 1.f + __expf(-u));
-  return u;
-}
-// dy act'(u)
-__device__ __forceinline__ float act_grad(float dy, float u, int act) {
-  if (act == FF_ACT_RELU) return u > 0.f ? dy : 0.f;
-  if (act == FF_ACT_SILU) {
-    const float p = __fdividef(1.f, 1.f + __expf(-u));
-    return dy * (p * fmaf(u, 1.f - p, 1.f));
-  }
-  return dy;
-}
 
 // ------------------------------------------------------------ general path
 constexpr int kColThreads = 256;
@@ -51,24 +30,51 @@ constexpr int kRowsPerThread = 64; // bounds the rounding of a thread's one-pass
 
 struct ColGeom {
   int CV, TC, TR, ctiles, chunk, chunks;
+  int wide;                              // gamma and beta are 16-byte aligned
+  FastDiv by_tiles, by_chunks, by_TC, by_Cg, by_G;
 };
 // Blocks of TC vector columns x TR thread rows; `chunk` positions per block,
 // enough blocks to fill the GPU several times where the work allows.
-ColGeom col_geom(int n, int S, int C, int V) {
+ColGeom col_geom(const GnShape& s, int V, const float* gamma, const float* beta) {
   ColGeom g;
-  g.CV = C / V;
+  g.CV = s.C / V;
   g.TC = g.CV < kColVecs ? g.CV : kColVecs;
   g.TR = kColThreads / g.TC;
   g.ctiles = cdiv(g.CV, g.TC);
   const long long want = 152 * 8;
-  long long chunks = (want + (long long)n * g.ctiles - 1) / ((long long)n * g.ctiles);
-  long long chunk = (S + chunks - 1) / chunks;
-  const long long lo = (long long)g.TR * 4, hi = (long long)g.TR * kRowsPerThread;
+  const long long chunks = (want + (long long)s.n * g.ctiles - 1) / ((long long)s.n * g.ctiles);
+  long long chunk = (s.S + chunks - 1) / chunks;
+  const long long lo = (long long)g.TR * 8, hi = (long long)g.TR * kRowsPerThread;
   chunk = chunk < lo ? lo : chunk > hi ? hi : chunk;
-  g.chunk = (int)(chunk < S ? chunk : S);
-  g.chunks = cdiv(S, g.chunk);
+  g.chunk = (int)(chunk < s.S ? chunk : s.S);
+  g.chunks = cdiv(s.S, g.chunk);
+  g.wide = ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) & 15) == 0;
+  g.by_tiles = FastDiv(g.ctiles);
+  g.by_chunks = FastDiv(g.chunks);
+  g.by_TC = FastDiv(g.TC);
+  g.by_Cg = FastDiv(s.Cg);
+  g.by_G = FastDiv(s.G);
   return g;
 }
+// A thread's place: sample, chunk, its column of V channels and its positions
+// r0, r0 + TR, .. below r1.  The second passes take the blocks from the last
+// to the first, since what the first pass read last is still in L2.
+struct ColPlace {
+  int b, ch, tc, tr, col, r0, r1;
+  bool on;
+  __device__ __forceinline__ ColPlace(const GnShape& s, const ColGeom& g, bool backwards) {
+    const uint32_t i = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const uint32_t rest = g.by_tiles.div(i);
+    b = (int)g.by_chunks.div(rest);
+    ch = (int)rest - b * g.chunks;
+    tr = (int)g.by_TC.div(threadIdx.x);
+    tc = (int)threadIdx.x - tr * g.TC;
+    col = (int)(i - rest * g.ctiles) * g.TC + tc;
+    on = tr < g.TR && col < g.CV;
+    r0 = ch * g.chunk + tr;
+    r1 = min(s.S, (ch + 1) * g.chunk);
+  }
+};
 
 template <typename T>
 __device__ __forceinline__ float group_pivot(const T* x, const GnShape& s, int b, int g) {
@@ -87,60 +93,70 @@ __device__ __forceinline__ float group_pivot(const T* x, const GnShape& s, int b
 // rounding units of that total.
 template <typename T, int V>
 __global__ void __launch_bounds__(kColThreads) k_gn_colstats(const T* x, GnShape s, ColGeom g, float2* part) {
+  using PV = Pairs<V>;
   __shared__ float2 red[kColThreads * V];
-  __shared__ int cnt[kColThreads];
   ptx::griddep_wait();
-  const int ct = blockIdx.x % g.ctiles;
-  const int rest = blockIdx.x / g.ctiles;
-  const int ch = rest % g.chunks, b = rest / g.chunks;
-  const int tc = threadIdx.x % g.TC, tr = threadIdx.x / g.TC;
-  const int col = ct * g.TC + tc;
-  const int r0 = ch * g.chunk, r1 = min(s.S, r0 + g.chunk);
-  const bool on = tr < g.TR && col < g.CV;
-  float piv[V], P[V], a1[V], a2[V];
+  ptx::griddep_launch_dependents();
+  const ColPlace p(s, g, false);
+  uint64_t np[PV::N], a1[PV::N], a2[PV::N];
 #pragma unroll
-  for (int e = 0; e < V; ++e) piv[e] = P[e] = a1[e] = a2[e] = 0.f;
-  int m = 0;
-  if (on) {
-    const T* p = x + ((long long)b * s.S) * s.ldx + (long long)col * V;
+  for (int e = 0; e < PV::N; ++e) np[e] = a1[e] = a2[e] = 0;
+  float piv[V], P[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) P[e] = group_pivot(x, s, b, (col * V + e) / s.Cg);
-    if (r0 + tr < r1) Vec<T, V>::unpack(Vec<T, V>::load(p + (long long)(r0 + tr) * s.ldx), piv);
+  for (int e = 0; e < V; ++e) piv[e] = P[e] = 0.f;
+  if (p.on) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) P[e] = group_pivot(x, s, p.b, (int)g.by_Cg.div((uint32_t)(p.col * V + e)));
+    const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
+    const long long step = (long long)g.TR * s.ldx;
+    if (p.r0 < p.r1) {
+      Vec<T, V>::unpack(Vec<T, V>::load(q), piv);
+      float m[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[e] = -piv[e];
+      PV::of(m, np);
+    }
 #pragma unroll 4
-    for (int r = r0 + tr; r < r1; r += g.TR, ++m) {
+    for (int r = p.r0; r < p.r1; r += g.TR, q += step) {
       float v[V];
-      Vec<T, V>::unpack(Vec<T, V>::load(p + (long long)r * s.ldx), v);
+      uint64_t d[PV::N];
+      Vec<T, V>::unpack(Vec<T, V>::load(q), v);
+      PV::of(v, d);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = v[e] - piv[e];
-        a1[e] += d;
-        a2[e] = fmaf(d, d, a2[e]);
+      for (int e = 0; e < PV::N; ++e) {
+        d[e] = ptx::add2(d[e], np[e]);
+        a1[e] = ptx::add2(a1[e], d[e]);
+        a2[e] = ptx::fma2(d[e], d[e], a2[e]);
       }
     }
   }
+  const int rows = p.r1 - p.ch * g.chunk;
+  // thread row t has rows / TR positions, one more below the remainder
+  const int lo = rows / g.TR, rem = rows - lo * g.TR, m = lo + (p.tr < rem ? 1 : 0);
+  float s1[V], s2[V];
+  PV::to(a1, s1);
+  PV::to(a2, s2);
   const float inv = m > 0 ? 1.f / (float)m : 0.f;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float dm = a1[e] * inv;
-    red[threadIdx.x * V + e] = make_float2((piv[e] - P[e]) + dm, a2[e] - a1[e] * dm);
+    const float dm = s1[e] * inv;
+    red[threadIdx.x * V + e] = make_float2((piv[e] - P[e]) + dm, s2[e] - s1[e] * dm);
   }
-  cnt[threadIdx.x] = m;
   __syncthreads();
-  if (on && tr == 0) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float mean = 0.f, M2 = 0.f, k = 0.f;
-      for (int t = 0; t < g.TR; ++t) {
-        const int i = t * g.TC + tc;
-        if (!cnt[i]) continue;
-        const float2 q = red[i * V + e];
-        const float kt = (float)cnt[i], d = q.x - mean, kn = k + kt;
-        mean = fmaf(d, kt / kn, mean);
-        M2 += q.y + d * d * (k * kt / kn);
-        k = kn;
-      }
-      part[((long long)b * g.chunks + ch) * s.C + (long long)col * V + e] = make_float2(mean, M2);
+  // one thread per channel: the thread rows together
+  const int width = g.TC * V, c0 = (p.col - p.tc) * V;
+  const int used = lo > 0 ? g.TR : rem;
+  const float tot = 1.f / (float)rows;
+  for (int c = threadIdx.x; c < width && c0 + c < s.C; c += kColThreads) {
+    float mean = 0.f, M2 = 0.f;
+    for (int t = 0; t < used; ++t) mean = fmaf(red[t * width + c].x, (float)(lo + (t < rem ? 1 : 0)), mean);
+    mean *= tot;
+    for (int t = 0; t < used; ++t) {
+      const float2 q = red[t * width + c];
+      const float d = q.x - mean;
+      M2 += fmaf(d * d, (float)(lo + (t < rem ? 1 : 0)), q.y);
     }
+    part[((long long)p.b * g.chunks + p.ch) * s.C + c0 + c] = make_float2(mean, M2);
   }
 }
 
@@ -160,25 +176,31 @@ __global__ void __launch_bounds__(128) k_gn_fold(const T* x, const float2* part,
                                                  float* mean_out, float* rstd_out) {
   __shared__ float sm[4];
   ptx::griddep_wait();
-  const int b = blockIdx.x / s.G, gr = blockIdx.x % s.G;
-  const long long cells = (long long)g.chunks * s.Cg;
+  ptx::griddep_launch_dependents();
+  const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
   const float2* p = part + (long long)b * g.chunks * s.C + gr * s.Cg;
   const float total = (float)s.S * (float)s.Cg;
-  float sum = 0.f;
-  for (long long i = threadIdx.x; i < cells; i += blockDim.x) {
-    const int ch = (int)(i / s.Cg), c = (int)(i % s.Cg);
-    const float rows = (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk);
-    sum = fmaf(p[(long long)ch * s.C + c].x, rows, sum);
-  }
+  // the chunks' columns, walked without divisions: cell (ch, c) of chunks x Cg
+  const int dch = 128 / s.Cg, dc = 128 - dch * s.Cg;
+  const int ch0 = (int)g.by_Cg.div(threadIdx.x), c0 = (int)threadIdx.x - ch0 * s.Cg;
+  auto walk = [&](auto f) {
+    for (int ch = ch0, c = c0; ch < g.chunks;) {
+      f(p[(long long)ch * s.C + c], (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
+      ch += dch;
+      c += dc;
+      if (c >= s.Cg) {
+        c -= s.Cg;
+        ++ch;
+      }
+    }
+  };
+  float sum = 0.f, M2 = 0.f;
+  walk([&](float2 q, float rows) { sum = fmaf(q.x, rows, sum); });
   const float mean = block_sum(sum, sm) / total;
-  float M2 = 0.f;
-  for (long long i = threadIdx.x; i < cells; i += blockDim.x) {
-    const int ch = (int)(i / s.Cg), c = (int)(i % s.Cg);
-    const float rows = (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk);
-    const float2 q = p[(long long)ch * s.C + c];
+  walk([&](float2 q, float rows) {
     const float d = q.x - mean;
     M2 += fmaf(d * d, rows, q.y);
-  }
+  });
   const float var = block_sum(M2, sm) / total;
   if (threadIdx.x == 0) {
     mean_out[blockIdx.x] = group_pivot(x, s, b, gr) + mean;
@@ -190,32 +212,82 @@ template <typename T, int V>
 __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s, ColGeom g, const float* gamma,
                                                           const float* beta, const float* mean, const float* rstd,
                                                           T* y) {
+  using PV = Pairs<V>;
   ptx::griddep_wait();
-  const int ct = blockIdx.x % g.ctiles;
-  const int rest = blockIdx.x / g.ctiles;
-  const int ch = rest % g.chunks, b = rest / g.chunks;
-  const int tc = threadIdx.x % g.TC, tr = threadIdx.x / g.TC;
-  const int col = ct * g.TC + tc;
-  const int r0 = ch * g.chunk, r1 = min(s.S, r0 + g.chunk);
-  if (tr >= g.TR || col >= g.CV) return;
-  float mu[V], a[V], bt[V];
+  ptx::griddep_launch_dependents();
+  const ColPlace p(s, g, true);
+  if (!p.on) return;
+  float a[V], b[V];
+  load_params<V>(a, gamma, p.col * V, 1.f, g.wide);
+  load_params<V>(b, beta, p.col * V, 0.f, g.wide);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const int c = col * V + e, st = b * s.G + c / s.Cg;
-    mu[e] = mean[st];
-    a[e] = rstd[st] * (gamma ? gamma[c] : 1.f);
-    bt[e] = beta ? beta[c] : 0.f;
+    const int st = p.b * s.G + (int)g.by_Cg.div((uint32_t)(p.col * V + e));
+    a[e] *= rstd[st];
+    b[e] = fmaf(-mean[st], a[e], b[e]);
   }
-  const long long row0 = (long long)b * s.S;
-#pragma unroll 4
-  for (int r = r0 + tr; r < r1; r += g.TR) {
-    float v[V];
-    Vec<T, V>::unpack(Vec<T, V>::load(x + (row0 + r) * s.ldx + (long long)col * V), v);
+  uint64_t A[PV::N], B[PV::N];
+  PV::of(a, A);
+  PV::of(b, B);
+  const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
+  T* o = y + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
+  const long long sx = (long long)g.TR * s.ldx, so = (long long)g.TR * s.ldy;
+  constexpr int U = 4;  // vectors in flight
+  for (int r = p.r0; r < p.r1; r += U * g.TR) {
+    typename Vec<T, V>::Raw raw[U];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = act_of(fmaf(v[e] - mu[e], a[e], bt[e]), s.act);
-    Vec<T, V>::store(y + (row0 + r) * s.ldy + (long long)col * V, v);
+    for (int u = 0; u < U; ++u)
+      if (r + u * g.TR < p.r1) raw[u] = Vec<T, V>::load(q + u * sx);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r + u * g.TR < p.r1) {
+        float v[V];
+        uint64_t d[PV::N];
+        Vec<T, V>::unpack(raw[u], v);
+        PV::of(v, d);
+#pragma unroll
+        for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(d[e], A[e], B[e]);
+        act_pairs<V>(d, s.act);
+        PV::to(d, v);
+        Vec<T, V>::store(o + u * so, v);
+      }
+    q += U * sx;
+    o += U * so;
   }
 }
+
+// What the gradient's passes share: a column's constants.  h = x rs + o,
+// u = gamma h + beta.
+template <int V>
+struct GradCols {
+  uint64_t rs[Pairs<V>::N], o[Pairs<V>::N], ga[Pairs<V>::N], be[Pairs<V>::N];
+  __device__ __forceinline__ GradCols(const GnShape& s, const ColGeom& g, const ColPlace& p, const float* mean,
+                                      const float* rstd, const float* gamma, const float* beta) {
+    float r[V], m[V], a[V], b[V];
+    load_params<V>(a, gamma, p.col * V, 1.f, g.wide);
+    load_params<V>(b, beta, p.col * V, 0.f, g.wide);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int st = p.b * s.G + (int)g.by_Cg.div((uint32_t)(p.col * V + e));
+      r[e] = rstd[st];
+      m[e] = -mean[st] * r[e];
+    }
+    Pairs<V>::of(r, rs);
+    Pairs<V>::of(m, o);
+    Pairs<V>::of(a, ga);
+    Pairs<V>::of(b, be);
+  }
+  // x and dy of a position to h and du
+  __device__ __forceinline__ void forms(uint64_t (&x)[Pairs<V>::N], uint64_t (&d)[Pairs<V>::N], int act) const {
+    uint64_t u[Pairs<V>::N];
+#pragma unroll
+    for (int e = 0; e < Pairs<V>::N; ++e) {
+      x[e] = ptx::fma2(x[e], rs[e], o[e]);
+      u[e] = ptx::fma2(x[e], ga[e], be[e]);
+    }
+    act_grad_pairs<V>(d, u, act);
+  }
+};
 
 // Column sums (du, du h) over a chunk of a sample's positions.
 template <typename T, int V>
@@ -223,57 +295,62 @@ __global__ void __launch_bounds__(kColThreads) k_gn_grad_colsums(const T* dy, co
                                                                  const float* mean, const float* rstd,
                                                                  const float* gamma, const float* beta,
                                                                  float2* part) {
+  using PV = Pairs<V>;
   __shared__ float2 red[kColThreads * V];
   ptx::griddep_wait();
-  const int ct = blockIdx.x % g.ctiles;
-  const int rest = blockIdx.x / g.ctiles;
-  const int ch = rest % g.chunks, b = rest / g.chunks;
-  const int tc = threadIdx.x % g.TC, tr = threadIdx.x / g.TC;
-  const int col = ct * g.TC + tc;
-  const int r0 = ch * g.chunk, r1 = min(s.S, r0 + g.chunk);
-  const bool on = tr < g.TR && col < g.CV;
-  float p0[V], p1[V];
+  ptx::griddep_launch_dependents();
+  const ColPlace p(s, g, false);
+  uint64_t p0[PV::N], p1[PV::N];
 #pragma unroll
-  for (int e = 0; e < V; ++e) p0[e] = p1[e] = 0.f;
-  if (on) {
-    float mu[V], rs[V], ga[V], bt[V];
+  for (int e = 0; e < PV::N; ++e) p0[e] = p1[e] = 0;
+  if (p.on) {
+    const GradCols<V> k(s, g, p, mean, rstd, gamma, beta);
+    const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
+    const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
+    const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy;
+    constexpr int U = 2;
+    for (int r = p.r0; r < p.r1; r += U * g.TR) {
+      typename Vec<T, V>::Raw rx[U], rd[U];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int c = col * V + e, st = b * s.G + c / s.Cg;
-      mu[e] = mean[st];
-      rs[e] = rstd[st];
-      ga[e] = gamma ? gamma[c] : 1.f;
-      bt[e] = beta ? beta[c] : 0.f;
-    }
-    const long long row0 = (long long)b * s.S;
-#pragma unroll 2
-    for (int r = r0 + tr; r < r1; r += g.TR) {
-      float v[V], d[V];
-      Vec<T, V>::unpack(Vec<T, V>::load(x + (row0 + r) * s.ldx + (long long)col * V), v);
-      Vec<T, V>::unpack(Vec<T, V>::load(dy + (row0 + r) * s.lddy + (long long)col * V), d);
+      for (int u = 0; u < U; ++u)
+        if (r + u * g.TR < p.r1) {
+          rx[u] = Vec<T, V>::load(qx + u * sx);
+          rd[u] = Vec<T, V>::load(qd + u * sd);
+        }
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float h = (v[e] - mu[e]) * rs[e];
-        const float du = act_grad(d[e], fmaf(ga[e], h, bt[e]), s.act);
-        p0[e] += du;
-        p1[e] = fmaf(du, h, p1[e]);
-      }
+      for (int u = 0; u < U; ++u)
+        if (r + u * g.TR < p.r1) {
+          float v[V], w[V];
+          uint64_t h[PV::N], d[PV::N];
+          Vec<T, V>::unpack(rx[u], v);
+          Vec<T, V>::unpack(rd[u], w);
+          PV::of(v, h);
+          PV::of(w, d);
+          k.forms(h, d, s.act);
+#pragma unroll
+          for (int e = 0; e < PV::N; ++e) {
+            p0[e] = ptx::add2(p0[e], d[e]);
+            p1[e] = ptx::fma2(d[e], h[e], p1[e]);
+          }
+        }
+      qx += U * sx;
+      qd += U * sd;
     }
   }
+  float s0[V], s1[V];
+  PV::to(p0, s0);
+  PV::to(p1, s1);
 #pragma unroll
-  for (int e = 0; e < V; ++e) red[threadIdx.x * V + e] = make_float2(p0[e], p1[e]);
+  for (int e = 0; e < V; ++e) red[threadIdx.x * V + e] = make_float2(s0[e], s1[e]);
   __syncthreads();
-  if (on && tr == 0) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float2 t = make_float2(0.f, 0.f);
-      for (int k = 0; k < g.TR; ++k) {
-        const float2 q = red[(k * g.TC + tc) * V + e];
-        t.x += q.x;
-        t.y += q.y;
-      }
-      part[((long long)b * g.chunks + ch) * s.C + (long long)col * V + e] = t;
+  const int width = g.TC * V, c0 = (p.col - p.tc) * V;
+  for (int c = threadIdx.x; c < width && c0 + c < s.C; c += kColThreads) {
+    float2 t = red[c];
+    for (int r = 1; r < g.TR; ++r) {
+      t.x += red[r * width + c].x;
+      t.y += red[r * width + c].y;
     }
+    part[((long long)p.b * g.chunks + p.ch) * s.C + c0 + c] = t;
   }
 }
 
@@ -282,16 +359,23 @@ __global__ void __launch_bounds__(128) k_gn_grad_fold(const float2* part, GnShap
                                                       float2* avg) {
   __shared__ float sm[4];
   ptx::griddep_wait();
-  const int b = blockIdx.x / s.G, gr = blockIdx.x % s.G;
-  const long long cells = (long long)g.chunks * s.Cg;
+  ptx::griddep_launch_dependents();
+  const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
   const float2* p = part + (long long)b * g.chunks * s.C + gr * s.Cg;
+  const int dch = 128 / s.Cg, dc = 128 - dch * s.Cg;
+  int ch = (int)g.by_Cg.div(threadIdx.x), c = (int)threadIdx.x - ch * s.Cg;
   float m1 = 0.f, m2 = 0.f;
-  for (long long i = threadIdx.x; i < cells; i += blockDim.x) {
-    const int ch = (int)(i / s.Cg), c = (int)(i % s.Cg);
+  while (ch < g.chunks) {
     const float2 q = p[(long long)ch * s.C + c];
     const float ga = gamma ? gamma[gr * s.Cg + c] : 1.f;
     m1 = fmaf(ga, q.x, m1);
     m2 = fmaf(ga, q.y, m2);
+    ch += dch;
+    c += dc;
+    if (c >= s.Cg) {
+      c -= s.Cg;
+      ++ch;
+    }
   }
   const float total = (float)s.S * (float)s.Cg;
   m1 = block_sum(m1, sm);
@@ -300,9 +384,10 @@ __global__ void __launch_bounds__(128) k_gn_grad_fold(const float2* part, GnShap
 }
 
 // dbeta and dgamma: the partial column sums [rows, C] added up, in an order
-// that depends on the sizes only.
-constexpr int kFoldCols = 32, kFoldRows = 16;
-__global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const float2* part, long long rows, int C,
+// that depends on the sizes only.  Few columns and many row threads per
+// block: the sums are short and latency is what they cost.
+constexpr int kFoldCols = 8, kFoldRows = 64;
+__global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const float2* part, GnFold f, int C,
                                                                         float* dgamma, float* dbeta) {
   __shared__ float2 red[kFoldRows][kFoldCols];
   ptx::griddep_wait();
@@ -310,6 +395,11 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
   const int c = blockIdx.x * kFoldCols + tc;
   float2 t = make_float2(0.f, 0.f);
   if (c < C) {
+    long long rows = f.rows;
+    if (f.units > 0) {
+      const long long first = (long long)(c / f.W) * f.n;
+      rows = ((first + f.n - 1) / f.units - first / f.units + 1) * f.K;
+    }
 #pragma unroll 8
     for (long long r = tr; r < rows; r += kFoldRows) {
       const float2 q = part[r * C + c];
@@ -318,14 +408,16 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
     }
   }
   red[tr][tc] = t;
-  __syncthreads();
-  if (tr == 0 && c < C) {
-    for (int k = 1; k < kFoldRows; ++k) {
-      t.x += red[k][tc].x;
-      t.y += red[k][tc].y;
+  for (int half = kFoldRows / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (tr < half) {
+      red[tr][tc].x += red[tr + half][tc].x;
+      red[tr][tc].y += red[tr + half][tc].y;
     }
-    dbeta[c] = t.x;
-    dgamma[c] = t.y;
+  }
+  if (tr == 0 && c < C) {
+    dbeta[c] = red[0][tc].x;
+    dgamma[c] = red[0][tc].y;
   }
 }
 
@@ -334,38 +426,57 @@ __global__ void __launch_bounds__(kColThreads) k_gn_grad_apply(const T* dy, cons
                                                                const float* mean, const float* rstd,
                                                                const float* gamma, const float* beta,
                                                                const float2* avg, T* dx) {
+  using PV = Pairs<V>;
   ptx::griddep_wait();
-  const int ct = blockIdx.x % g.ctiles;
-  const int rest = blockIdx.x / g.ctiles;
-  const int ch = rest % g.chunks, b = rest / g.chunks;
-  const int tc = threadIdx.x % g.TC, tr = threadIdx.x / g.TC;
-  const int col = ct * g.TC + tc;
-  const int r0 = ch * g.chunk, r1 = min(s.S, r0 + g.chunk);
-  if (tr >= g.TR || col >= g.CV) return;
-  float mu[V], rs[V], ga[V], bt[V], m1[V], m2[V];
+  ptx::griddep_launch_dependents();
+  const ColPlace p(s, g, true);
+  if (!p.on) return;
+  const GradCols<V> k(s, g, p, mean, rstd, gamma, beta);
+  // dx = rs (gamma du - <.> - h <.>) = du (gamma rs) + (h c2 + c1)
+  float f1[V], f2[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const int c = col * V + e, st = b * s.G + c / s.Cg;
-    mu[e] = mean[st];
-    rs[e] = rstd[st];
-    ga[e] = gamma ? gamma[c] : 1.f;
-    bt[e] = beta ? beta[c] : 0.f;
-    m1[e] = avg[st].x;
-    m2[e] = avg[st].y;
+    const int st = p.b * s.G + (int)g.by_Cg.div((uint32_t)(p.col * V + e));
+    const float2 m = avg[st];
+    f1[e] = -rstd[st] * m.x;
+    f2[e] = -rstd[st] * m.y;
   }
-  const long long row0 = (long long)b * s.S;
-#pragma unroll 2
-  for (int r = r0 + tr; r < r1; r += g.TR) {
-    float v[V], d[V];
-    Vec<T, V>::unpack(Vec<T, V>::load(x + (row0 + r) * s.ldx + (long long)col * V), v);
-    Vec<T, V>::unpack(Vec<T, V>::load(dy + (row0 + r) * s.lddy + (long long)col * V), d);
+  uint64_t c1[PV::N], c2[PV::N], gr[PV::N];
+  PV::of(f1, c1);
+  PV::of(f2, c2);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float h = (v[e] - mu[e]) * rs[e];
-      const float du = act_grad(d[e], fmaf(ga[e], h, bt[e]), s.act);
-      v[e] = rs[e] * (fmaf(ga[e], du, -m1[e]) - h * m2[e]);
-    }
-    Vec<T, V>::store(dx + (row0 + r) * s.ldy + (long long)col * V, v);
+  for (int e = 0; e < PV::N; ++e) gr[e] = ptx::mul2(k.ga[e], k.rs[e]);
+  const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
+  const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
+  T* o = dx + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
+  const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy, so = (long long)g.TR * s.ldy;
+  constexpr int U = 2;
+  for (int r = p.r0; r < p.r1; r += U * g.TR) {
+    typename Vec<T, V>::Raw rx[U], rd[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r + u * g.TR < p.r1) {
+        rx[u] = Vec<T, V>::load(qx + u * sx);
+        rd[u] = Vec<T, V>::load(qd + u * sd);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (r + u * g.TR < p.r1) {
+        float v[V], w[V];
+        uint64_t h[PV::N], d[PV::N];
+        Vec<T, V>::unpack(rx[u], v);
+        Vec<T, V>::unpack(rd[u], w);
+        PV::of(v, h);
+        PV::of(w, d);
+        k.forms(h, d, s.act);
+#pragma unroll
+        for (int e = 0; e < PV::N; ++e) h[e] = ptx::fma2(d[e], gr[e], ptx::fma2(h[e], c2[e], c1[e]));
+        PV::to(h, v);
+        Vec<T, V>::store(o + u * so, v);
+      }
+    qx += U * sx;
+    qd += U * sd;
+    o += U * so;
   }
 }
 
@@ -389,102 +500,136 @@ int vec_of(int C, int esize, const void* a, long long lda, const void* b, long l
   return v;
 }
 
-// The partials' chunks depend on the vector width, so the workspace covers
-// the width that needs most.
-long long partial_bytes(int n, int S, int C, ff_precision prec) {
-  long long most = 0;
-  for (int v = 16 / (prec == FF_BF16 ? 2 : 4); v >= 1; v /= 2) {
-    if (C % v) continue;
-    const long long b = (long long)n * col_geom(n, S, C, v).chunks * C * (long long)sizeof(float2);
-    most = b > most ? b : most;
+// What a call runs: decided by its sizes, its type and the alignment of its
+// rows.
+enum Path { ROWS, CLUSTER, GENERAL };
+struct Plan {
+  Path path;
+  int V;              // values per access
+  GnClusterPlan cl;
+  long long bytes;    // workspace
+};
+
+// v: the widest access that the rows' alignment allows.  Within the two
+// register paths a vector must lie in one group; they have accesses of 16
+// bytes, of 4 (bf16) and of one value.
+Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
+  Plan p{GENERAL, v, {}, 0};
+  const int wide = 16 / esize;
+  int in_group = v;
+  while (s.Cg % in_group) in_group /= 2;
+  const int V = in_group == wide ? wide : esize == 2 && in_group >= 2 ? 2 : 1;
+  const long long values = (long long)s.S * s.Cg;
+  // A few positions of narrow groups would be fetched a fraction of a 32-byte
+  // sector at a time: those go to slabs of several groups.
+  const bool narrow = s.S > 1 && s.Cg * esize < 32 && s.G > 1;
+  const bool near = (long long)s.S * (s.ldx > s.ldy ? s.ldx : s.ldy) < 0x3FFFFFFF &&
+                    (long long)s.S * s.lddy < 0x3FFFFFFF;  // offsets within a sample fit 32 bits
+  const bool rows_fit = values <= kRowsMax && near;
+  if (rows_fit && !narrow) p.path = ROWS;
+  if (p.path == GENERAL) {
+    p.cl = gn_cluster_plan(s, V, esize, grad);
+    if (p.cl.T > 0)
+      p.path = CLUSTER;
+    else if (rows_fit)
+      p.path = ROWS;
   }
-  return align_up(most);
+  if (p.path == GENERAL) {
+    p.bytes = align_up((long long)s.n * col_geom(s, v, nullptr, nullptr).chunks * s.C * (long long)sizeof(float2)) +
+              align_up((long long)s.n * s.G * (long long)sizeof(float2));
+    return p;
+  }
+  p.V = V;
+  if (grad) {
+    const long long rows =
+        p.path == ROWS ? (long long)gn_rows_plan(s, V, true).P * s.S
+                       : ((long long)(s.n - 1) / p.cl.units + 2) * p.cl.K;  // clusters that share a slab
+    p.bytes = align_up(rows * s.C * (long long)sizeof(float2));
+  }
+  return p;
 }
-long long stats_bytes(int n, int G) { return align_up((long long)n * G * (long long)sizeof(float2)); }
 
 template <typename T, int V>
-ff_status norm_general(const T* x, const GnShape& s, const float* gamma, const float* beta, T* y, float* mean,
-                       float* rstd, void* ws, cudaStream_t st) {
-  const ColGeom g = col_geom(s.n, s.S, s.C, V);
+ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
+  const GnShape& s = a.s;
+  const ColGeom g = col_geom(s, V, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
   if (blocks > 0x7FFFFFFFll || (long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
-  float2* part = static_cast<float2*>(ws);
+  float2* part = static_cast<float2*>(a.ws);
+  float *mean = a.mean, *rstd = a.rstd;
   if (!mean) {
-    mean = reinterpret_cast<float*>(static_cast<char*>(ws) + partial_bytes(s.n, s.S, s.C, sizeof(T) == 2 ? FF_BF16 : FF_FP32));
+    mean = reinterpret_cast<float*>(static_cast<char*>(a.ws) +
+                                    align_up((long long)s.n * g.chunks * s.C * (long long)sizeof(float2)));
     rstd = mean + (long long)s.n * s.G;
   }
   const double bytes = (double)s.n * s.S * s.C * sizeof(T);
   PdlLaunch l1(dim3((unsigned)blocks), dim3(kColThreads), st);
-  FF_LAUNCH(K_GNORM, bytes, st, cudaLaunchKernelEx(&l1.cfg, k_gn_colstats<T, V>, x, s, g, part), "group norm sums");
+  FF_LAUNCH(K_GNORM, bytes, st, cudaLaunchKernelEx(&l1.cfg, k_gn_colstats<T, V>, a.x, s, g, part), "group norm sums");
   PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(128), st);
   FF_LAUNCH(K_GNORM, 0, st,
-            cudaLaunchKernelEx(&l2.cfg, k_gn_fold<T>, x, static_cast<const float2*>(part), s, g, mean, rstd),
+            cudaLaunchKernelEx(&l2.cfg, k_gn_fold<T>, a.x, static_cast<const float2*>(part), s, g, mean, rstd),
             "group norm fold");
   PdlLaunch l3(dim3((unsigned)blocks), dim3(kColThreads), st);
   FF_LAUNCH(K_GNORM, 2 * bytes, st,
-            cudaLaunchKernelEx(&l3.cfg, k_gn_apply<T, V>, x, s, g, gamma, beta, static_cast<const float*>(mean),
-                               static_cast<const float*>(rstd), y),
+            cudaLaunchKernelEx(&l3.cfg, k_gn_apply<T, V>, a.x, s, g, a.gamma, a.beta, static_cast<const float*>(mean),
+                               static_cast<const float*>(rstd), a.out),
             "group norm apply");
   return FF_OK;
 }
 
 template <typename T, int V>
-ff_status grad_general(const T* dy, const T* x, const GnShape& s, const float* mean, const float* rstd,
-                       const float* gamma, const float* beta, T* dx, float* dgamma, float* dbeta, void* ws,
-                       cudaStream_t st) {
-  const ColGeom g = col_geom(s.n, s.S, s.C, V);
+ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
+  const GnShape& s = a.s;
+  const ColGeom g = col_geom(s, V, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
   if (blocks > 0x7FFFFFFFll || (long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
-  float2* part = static_cast<float2*>(ws);
-  float2* avg = reinterpret_cast<float2*>(static_cast<char*>(ws) +
-                                          partial_bytes(s.n, s.S, s.C, sizeof(T) == 2 ? FF_BF16 : FF_FP32));
+  float2* part = static_cast<float2*>(a.ws);
+  float2* avg = reinterpret_cast<float2*>(static_cast<char*>(a.ws) +
+                                          align_up((long long)s.n * g.chunks * s.C * (long long)sizeof(float2)));
+  const float *mean = a.mean, *rstd = a.rstd;
   const double bytes = (double)s.n * s.S * s.C * sizeof(T);
   PdlLaunch l1(dim3((unsigned)blocks), dim3(kColThreads), st);
   FF_LAUNCH(K_GNORM_GRAD, 2 * bytes, st,
-            cudaLaunchKernelEx(&l1.cfg, k_gn_grad_colsums<T, V>, dy, x, s, g, mean, rstd, gamma, beta, part),
+            cudaLaunchKernelEx(&l1.cfg, k_gn_grad_colsums<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta, part),
             "group norm gradient sums");
-  if (dx) {
+  if (a.dgamma) {
+    const ff_status e = gn_param_fold(part, GnFold{(long long)s.n * g.chunks, 0, 0, 0, 0}, s.C, a.dgamma, a.dbeta, st);
+    if (e != FF_OK) return e;
+  }
+  if (a.out) {
     PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(128), st);
     FF_LAUNCH(K_GNORM_GRAD, 0, st,
-              cudaLaunchKernelEx(&l2.cfg, k_gn_grad_fold, static_cast<const float2*>(part), s, g, gamma, avg),
+              cudaLaunchKernelEx(&l2.cfg, k_gn_grad_fold, static_cast<const float2*>(part), s, g, a.gamma, avg),
               "group norm gradient fold");
     PdlLaunch l3(dim3((unsigned)blocks), dim3(kColThreads), st);
     FF_LAUNCH(K_GNORM_GRAD, 3 * bytes, st,
-              cudaLaunchKernelEx(&l3.cfg, k_gn_grad_apply<T, V>, dy, x, s, g, mean, rstd, gamma, beta,
-                                 static_cast<const float2*>(avg), dx),
+              cudaLaunchKernelEx(&l3.cfg, k_gn_grad_apply<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta,
+                                 static_cast<const float2*>(avg), a.out),
               "group norm gradient apply");
-  }
-  if (dgamma) {
-    PdlLaunch l4(dim3((unsigned)cdiv(s.C, kFoldCols)), dim3(kFoldCols * kFoldRows), st);
-    FF_LAUNCH(K_GNORM_GRAD, 0, st,
-              cudaLaunchKernelEx(&l4.cfg, k_gn_param_fold, static_cast<const float2*>(part),
-                                 (long long)s.n * g.chunks, s.C, dgamma, dbeta),
-              "group norm parameter gradients");
   }
   return FF_OK;
 }
 
-template <typename T>
-ff_status norm_t(const T* x, const GnShape& s, const float* gamma, const float* beta, T* y, float* mean, float* rstd,
-                 void* ws, cudaStream_t st) {
-  const int v = vec_of(s.C, sizeof(T), x, s.ldx, y, s.ldy, y, s.ldy);
-  if constexpr (sizeof(T) == 2)
-    if (v == 8) return norm_general<T, 8>(x, s, gamma, beta, y, mean, rstd, ws, st);
-  if (v >= 4) return norm_general<T, 4>(x, s, gamma, beta, y, mean, rstd, ws, st);
-  if (v == 2) return norm_general<T, 2>(x, s, gamma, beta, y, mean, rstd, ws, st);
-  return norm_general<T, 1>(x, s, gamma, beta, y, mean, rstd, ws, st);
+template <typename T, int V>
+ff_status general(const GnArgs<T>& a, bool grad, cudaStream_t st) {
+  return grad ? grad_general<T, V>(a, st) : norm_general<T, V>(a, st);
 }
 
 template <typename T>
-ff_status grad_t(const T* dy, const T* x, const GnShape& s, const float* mean, const float* rstd, const float* gamma,
-                 const float* beta, T* dx, float* dgamma, float* dbeta, void* ws, cudaStream_t st) {
-  const T* out = dx ? dx : x;
-  const int v = vec_of(s.C, sizeof(T), x, s.ldx, dy, s.lddy, out, dx ? s.ldy : s.ldx);
+ff_status call(const GnArgs<T>& a, long long ws_bytes, bool grad, cudaStream_t st) {
+  const GnShape& s = a.s;
+  const int v = grad ? vec_of(s.C, sizeof(T), a.x, s.ldx, a.dy, s.lddy, a.out ? a.out : a.x, a.out ? s.ldy : s.ldx)
+                     : vec_of(s.C, sizeof(T), a.x, s.ldx, a.out, s.ldy, a.out, s.ldy);
+  const Plan p = plan_of(s, sizeof(T), v, grad);
+  if (p.bytes > 0 && (!a.ws || ws_bytes < p.bytes || reinterpret_cast<uintptr_t>(a.ws) % kAlign))
+    return FF_ERR_INVALID_ARG;
+  if (p.path == ROWS) return gn_rows(a, p.V, grad, st);
+  if (p.path == CLUSTER) return gn_cluster(a, p.V, p.cl, grad, st);
   if constexpr (sizeof(T) == 2)
-    if (v == 8) return grad_general<T, 8>(dy, x, s, mean, rstd, gamma, beta, dx, dgamma, dbeta, ws, st);
-  if (v >= 4) return grad_general<T, 4>(dy, x, s, mean, rstd, gamma, beta, dx, dgamma, dbeta, ws, st);
-  if (v == 2) return grad_general<T, 2>(dy, x, s, mean, rstd, gamma, beta, dx, dgamma, dbeta, ws, st);
-  return grad_general<T, 1>(dy, x, s, mean, rstd, gamma, beta, dx, dgamma, dbeta, ws, st);
+    if (v == 8) return general<T, 8>(a, grad, st);
+  if (v >= 4) return general<T, 4>(a, grad, st);
+  if (v == 2) return general<T, 2>(a, grad, st);
+  return general<T, 1>(a, grad, st);
 }
 
 bool good_act(ff_activation a) { return a == FF_ACT_NONE || a == FF_ACT_RELU || a == FF_ACT_SILU; }
@@ -493,16 +638,38 @@ bool good_matrix(const void* p, long long ld, long long rows, int C, int esize) 
 }
 
 }  // namespace
+
+ff_status gn_param_fold(const float2* part, const GnFold& f, int C, float* dgamma, float* dbeta, cudaStream_t st) {
+  PdlLaunch l(dim3((unsigned)cdiv(C, kFoldCols)), dim3(kFoldCols * kFoldRows), st);
+  FF_LAUNCH(K_GNORM_GRAD, 0, st, cudaLaunchKernelEx(&l.cfg, k_gn_param_fold, part, f, C, dgamma, dbeta),
+            "group norm parameter gradients");
+  return FF_OK;
+}
+
 }  // namespace ff
 
 using namespace ff;
 
+// The workspace of the path that needs most among those that some alignment
+// of the rows leads to.
 extern "C" FF_API long long ff_group_norm_workspace(int n, int spatial, int channels, int groups, ff_precision prec,
                                                     int backward) {
-  (void)backward;
   if (!good_shape(n, spatial, channels, groups, prec)) return -1;
   if (n == 0 || spatial == 0) return 0;
-  return partial_bytes(n, spatial, channels, prec) + stats_bytes(n, groups);
+  const int es = prec == FF_BF16 ? 2 : 4;
+  // the strides only say whether a sample's offsets fit 32 bits: both ways count
+  const GnShape tight{n, spatial, channels, groups, channels / groups, channels, channels, channels, 0.f, 0};
+  GnShape wide = tight;
+  wide.ldx = wide.ldy = wide.lddy = 0x7FFFFFFF;
+  long long most = 0;
+  for (int v = 16 / es; v >= 1; v /= 2) {
+    if (channels % v) continue;
+    for (const GnShape* s : {&tight, static_cast<const GnShape*>(&wide)}) {
+      const long long b = plan_of(*s, es, v, backward != 0).bytes;
+      most = b > most ? b : most;
+    }
+  }
+  return most;
 }
 
 extern "C" FF_API ff_status ff_group_norm_act(const void* x, long long ldx, int n, int spatial, int channels,
@@ -525,13 +692,15 @@ extern "C" FF_API ff_status ff_group_norm_act(const void* x, long long ldx, int 
   const long long rows = (long long)n * spatial;
   const int es = prec == FF_BF16 ? 2 : 4;
   if (!good_matrix(x, ldx, rows, channels, es) || !good_matrix(y, ldy, rows, channels, es)) return FF_ERR_INVALID_ARG;
-  const long long need = ff_group_norm_workspace(n, spatial, channels, groups, prec, 0);
-  if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % kAlign))
-    return FF_ERR_INVALID_ARG;
-  const GnShape s{n, spatial, channels, groups, channels / groups, ldx, ldy, 0, eps, (int)act};
+  if (rows == 1) ldx = ldy = channels;
+  const GnShape s{n, spatial, channels, groups, channels / groups, ldx, ldy, channels, eps, (int)act};
   if (prec == FF_BF16)
-    return norm_t(static_cast<const bf16*>(x), s, gamma, beta, static_cast<bf16*>(y), mean, rstd, workspace, st);
-  return norm_t(static_cast<const float*>(x), s, gamma, beta, static_cast<float*>(y), mean, rstd, workspace, st);
+    return call(GnArgs<bf16>{s, static_cast<const bf16*>(x), nullptr, static_cast<bf16*>(y), gamma, beta, mean, rstd,
+                             nullptr, nullptr, workspace},
+                workspace_bytes, false, st);
+  return call(GnArgs<float>{s, static_cast<const float*>(x), nullptr, static_cast<float*>(y), gamma, beta, mean, rstd,
+                            nullptr, nullptr, workspace},
+              workspace_bytes, false, st);
 }
 
 extern "C" FF_API ff_status ff_group_norm_act_backward(const void* dy, long long lddy, const void* x, long long ldx,
@@ -557,13 +726,14 @@ extern "C" FF_API ff_status ff_group_norm_act_backward(const void* dy, long long
   if (!good_matrix(x, ldx, rows, channels, es) || !good_matrix(dy, lddy, rows, channels, es) ||
       (dx && !good_matrix(dx, lddx, rows, channels, es)) || !mean || !rstd)
     return FF_ERR_INVALID_ARG;
-  const long long need = ff_group_norm_workspace(n, spatial, channels, groups, prec, 1);
-  if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % kAlign))
-    return FF_ERR_INVALID_ARG;
-  const GnShape s{n, spatial, channels, groups, channels / groups, ldx, lddx, lddy, 0.f, (int)act};
+  if (rows == 1) ldx = lddy = lddx = channels;
+  const GnShape s{n, spatial, channels, groups, channels / groups, ldx, dx ? lddx : channels, lddy, 0.f, (int)act};
+  float *mu = const_cast<float*>(mean), *rs = const_cast<float*>(rstd);  // read only by the gradient
   if (prec == FF_BF16)
-    return grad_t(static_cast<const bf16*>(dy), static_cast<const bf16*>(x), s, mean, rstd, gamma, beta,
-                  static_cast<bf16*>(dx), dgamma, dbeta, workspace, st);
-  return grad_t(static_cast<const float*>(dy), static_cast<const float*>(x), s, mean, rstd, gamma, beta,
-                static_cast<float*>(dx), dgamma, dbeta, workspace, st);
+    return call(GnArgs<bf16>{s, static_cast<const bf16*>(x), static_cast<const bf16*>(dy), static_cast<bf16*>(dx), gamma,
+                             beta, mu, rs, dgamma, dbeta, workspace},
+                workspace_bytes, true, st);
+  return call(GnArgs<float>{s, static_cast<const float*>(x), static_cast<const float*>(dy), static_cast<float*>(dx),
+                            gamma, beta, mu, rs, dgamma, dbeta, workspace},
+              workspace_bytes, true, st);
 }

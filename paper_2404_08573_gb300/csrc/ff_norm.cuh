@@ -1,0 +1,205 @@
+// Group norm with an activation: what its kernel files share.  Sizes, the
+// activation and its slope, and the three paths' entry points (ff_norm.cu
+// picks one by sizes and alignment).
+#pragma once
+
+#include "ff_api_internal.h"
+#include "ff_ptx.cuh"
+#include "ff_vec.cuh"
+
+namespace ff {
+
+struct GnShape {
+  int n, S, C, G, Cg;
+  long long ldx, ldy, lddy;  // forward: x -> y; gradient: (dy, x) -> dx with ldy the stride of dx
+  float eps;
+  int act;
+};
+
+// Everything a call passes; mean and rstd are outputs of the forward pass
+// (or null) and inputs of the gradient.
+template <typename T>
+struct GnArgs {
+  GnShape s;
+  const T *x, *dy;
+  T* out;                    // y or dx (null: no dx)
+  const float *gamma, *beta; // or null: ones, zeros
+  float *mean, *rstd;
+  float *dgamma, *dbeta;     // or null
+  void* ws;
+};
+
+// The rows path: groups of at most kRowsMax values.  `lanes` lanes per group
+// (a power of 2), sets of 32 / lanes groups per warp.
+constexpr int kRowsMax = 512;
+struct GnRowsPlan {
+  int lanes, sets, P;  // P: blocks along the samples
+};
+// The cluster path: a slab of whole groups of one sample stays in the shared
+// memory of a cluster.
+struct GnClusterPlan {
+  int T, GS, K, nv;      // threads, groups per slab, CTAs per cluster, vectors per thread; T = 0: does not fit
+  int per_sm;            // CTAs an SM holds
+  int clusters, units;   // clusters launched, and (sample, slab) units each takes
+};
+
+GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad);
+GnClusterPlan gn_cluster_plan(const GnShape& s, int V, int esize, bool grad);
+
+template <typename T>
+ff_status gn_rows(const GnArgs<T>& a, int V, bool grad, cudaStream_t st);
+template <typename T>
+ff_status gn_cluster(const GnArgs<T>& a, int V, const GnClusterPlan& p, bool grad, cudaStream_t st);
+// dbeta and dgamma from partial column sums (du, du h) [., C]: `rows` of them,
+// or, with units > 0, as many as the clusters that took the column's slab
+// (slabs of W columns, n units each; `units` consecutive ones per cluster, K
+// rows per cluster).
+struct GnFold {
+  long long rows;
+  int units, n, W, K;
+};
+ff_status gn_param_fold(const float2* part, const GnFold& f, int C, float* dgamma, float* dbeta, cudaStream_t st);
+
+// Division of non-negative 31-bit numbers by a number fixed per launch
+// (Granlund and Montgomery's multiply-and-shift): q = (hi(n mul) + n) >> s.
+struct FastDiv {
+  uint32_t d, mul;
+  int s;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t by) : d(by), s(0) {
+    while ((1ull << s) < by) ++s;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << s) - by)) / by + 1);
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, mul) + n) >> s; }
+};
+
+__device__ __forceinline__ uint64_t both(float v) { return ptx::pack2(v, v); }
+// 1 / (1 + e^-u) of a pair, with the approximate exponential and one
+// approximate reciprocal for both: with a = 1 + e^-u and r = 1 / (a b), 1 / a is
+// r b and 1 / b is r a.  (These units take 16 values a clock and SM, and with
+// two calls a value they, not HBM, would bound the silu forms.)  The exponent
+// is held below 60, so the product of the two cannot overflow: beyond, the
+// result is 2^-60 in place of less.  Neither a nor r is ever subnormal.
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
+  const float2 t = ptx::unpack2(ptx::mul2(u, both(-1.44269504f)));
+  float x, y, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(fminf(t.x, 60.f)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fminf(t.y, 60.f)));
+  const uint64_t a = ptx::add2(ptx::pack2(x, y), both(1.f));
+  const float2 f = ptx::unpack2(a);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(f.x * f.y));
+  return ptx::mul2(ptx::pack2(f.y, f.x), both(r));
+}
+__device__ __forceinline__ float max0(float u) {  // max(u, 0), NaN kept
+  float r;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(u));
+  return r;
+}
+__device__ __forceinline__ float sigmoid1(float u) {
+  float e, p;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(u * -1.44269504f, 60.f)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
+  return p;
+}
+
+// A vector of V values as pairs (V = 1: one pair whose second value is zero).
+template <int V>
+struct Pairs {
+  static constexpr int N = V < 2 ? 1 : V / 2;
+  static __device__ __forceinline__ void of(const float (&v)[V], uint64_t (&p)[N]) {
+    if constexpr (V == 1) {
+      p[0] = ptx::pack2(v[0], 0.f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = ptx::pack2(v[2 * i], v[2 * i + 1]);
+    }
+  }
+  static __device__ __forceinline__ void to(const uint64_t (&p)[N], float (&v)[V]) {
+    if constexpr (V == 1) {
+      v[0] = ptx::unpack2(p[0]).x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float2 f = ptx::unpack2(p[i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+      }
+    }
+  }
+};
+
+// u = act(u) and d = d act'(u) over pairs (V = 1: the first value only).
+template <int V>
+__device__ __forceinline__ void act_pairs(uint64_t (&u)[Pairs<V>::N], int act) {
+  constexpr int N = Pairs<V>::N;
+  if (act == FF_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      u[i] = V == 1 ? ptx::pack2(ptx::unpack2(u[i]).x * sigmoid1(ptx::unpack2(u[i]).x), 0.f)
+                    : ptx::mul2(u[i], sigmoid2(u[i]));
+  } else if (act == FF_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 v = ptx::unpack2(u[i]);
+      u[i] = ptx::pack2(max0(v.x), max0(v.y));
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void act_grad_pairs(uint64_t (&d)[Pairs<V>::N], const uint64_t (&u)[Pairs<V>::N], int act) {
+  constexpr int N = Pairs<V>::N;
+  if (act == FF_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint64_t p = V == 1 ? ptx::pack2(sigmoid1(ptx::unpack2(u[i]).x), 0.f) : sigmoid2(u[i]);
+      const uint64_t q = ptx::fma2(p, both(-1.f), both(1.f));  // 1 - p
+      d[i] = ptx::mul2(d[i], ptx::mul2(p, ptx::fma2(u[i], q, both(1.f))));
+    }
+  } else if (act == FF_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 v = ptx::unpack2(u[i]), t = ptx::unpack2(d[i]);
+      d[i] = ptx::pack2(v.x > 0.f ? t.x : 0.f, v.y > 0.f ? t.y : 0.f);
+    }
+  }
+}
+// The same over plain arrays.
+template <int V>
+__device__ __forceinline__ void act_values(float (&u)[V], int act) {
+  uint64_t p[Pairs<V>::N];
+  Pairs<V>::of(u, p);
+  act_pairs<V>(p, act);
+  Pairs<V>::to(p, u);
+}
+template <int V>
+__device__ __forceinline__ void act_grad_values(float (&d)[V], const float (&u)[V], int act) {
+  uint64_t p[Pairs<V>::N], q[Pairs<V>::N];
+  Pairs<V>::of(d, p);
+  Pairs<V>::of(u, q);
+  act_grad_pairs<V>(p, q, act);
+  Pairs<V>::to(p, d);
+}
+
+// V parameters from index c (a multiple of V), or `none` everywhere; wide: p
+// is 16-byte aligned.
+template <int V>
+__device__ __forceinline__ void load_params(float (&v)[V], const float* p, long long c, float none, bool wide) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = none;
+  } else if (V % 4 == 0 && wide) {
+#pragma unroll
+    for (int e = 0; e + 3 < V; e += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(p + c + e));
+      v[e] = f.x;
+      v[e + 1] = f.y;
+      v[e + 2] = f.z;
+      v[e + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = __ldg(p + c + e);
+  }
+}
+
+}  // namespace ff

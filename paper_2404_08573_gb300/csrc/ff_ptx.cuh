@@ -123,6 +123,14 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Its two halves: work between them overlaps the wait for the others.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+// (without ordering any memory: that the others have started is all it says)
+__device__ __forceinline__ void cluster_arrive_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // Arrives (release, cluster scope) on the mbarrier at the offset of
 // `local_bar` in the CTA of cluster rank `rank`.
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t* local_bar, uint32_t rank) {
@@ -156,6 +164,23 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
     if (*abort) return false;
     if (globaltimer() - t0 > timeout_ns) return false;
   }
+}
+// Asynchronous stores into the variable at the offset of `local` in the CTA of
+// cluster rank `rank`, counted there (in bytes) by the mbarrier at the offset of
+// `local_bar`: who waits on that barrier sees the values, and the sender orders
+// none of its other memory accesses.
+__device__ __forceinline__ void st_async4(float4* local, uint64_t* local_bar, uint32_t rank, float4 v) {
+  asm volatile(
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+          mapa_shared(smem_u32(local), rank)),
+      "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(mapa_shared(smem_u32(local_bar), rank))
+      : "memory");
+}
+__device__ __forceinline__ void st_async2(float2* local, uint64_t* local_bar, uint32_t rank, float2 v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
+                   mapa_shared(smem_u32(local), rank)),
+               "f"(v.x), "f"(v.y), "r"(mapa_shared(smem_u32(local_bar), rank))
+               : "memory");
 }
 // Stores into the variable at the offset of `local_slot` in the CTA of cluster rank `rank`.
 __device__ __forceinline__ void st_remote_u1(int* local_slot, uint32_t rank, int v) {
@@ -313,6 +338,10 @@ __device__ __forceinline__ void cp_async4(void* dst, const void* src) {
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+// The same for 16 bytes (both addresses 16-byte aligned), past L1.
+__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
@@ -442,8 +471,18 @@ __device__ __forceinline__ float2 unpack2(uint64_t v) {
   asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
   return make_float2(__uint_as_float(lo), __uint_as_float(hi));
 }
-__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) {
+__device__ __forceinline__ void fma2_to(uint64_t& d, uint64_t a, uint64_t b) {  // d += a b
   asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
