@@ -27,7 +27,7 @@ CHECKED_BUILD_DIR = os.path.join(HERE, "_build_checked")
 CHECKED_LIB_PATH = os.path.join(HERE, "libff_checked.so")
 
 SOURCES = ["ff_api.cu", "ff_net.cu", "ff_elem.cu", "ff_gemm_tc.cu", "ff_gemm_simt.cu", "ff_prof.cu", "ff_noalloc.cu",
-           "ff_head.cu", "ff_pff.cu", "ff_epoch.cu", "ff_norm.cu", "ff_norm_rows.cu", "ff_norm_cluster.cu",
+           "ff_head.cu", "ff_pff.cu", "ff_epoch.cu", "ff_norm.cu", "ff_norm_rows.cu", "ff_norm_block.cu",
            "ff_dropout.cu", "ff_fp8.cu",
            "ff_fp8_gemm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

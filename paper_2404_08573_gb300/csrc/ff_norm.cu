@@ -14,8 +14,8 @@
 // small fold per group, and an element-wise pass -- whatever the group's
 // width, since a 16-byte vector may span groups.
 //
-// Groups that fit registers take one of two faster paths, which read x (and
-// dy) once: rows (ff_norm_rows.cu) and clusters (ff_norm_cluster.cu).
+// Groups that fit registers or shared memory may take one of two paths that
+// read x (and dy) once: rows (ff_norm_rows.cu) and blocks (ff_norm_block.cu).
 #include <cmath>
 
 #include "ff_norm.cuh"
@@ -92,7 +92,7 @@ __device__ __forceinline__ float group_pivot(const T* x, const GnShape& s, int b
 // it measures, and over at most 64 rows the difference loses at most 64
 // rounding units of that total.
 template <typename T, int V>
-__global__ void __launch_bounds__(kColThreads) k_gn_colstats(const T* x, GnShape s, ColGeom g, float2* part) {
+__global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnShape s, ColGeom g, float2* part) {
   using PV = Pairs<V>;
   __shared__ float2 red[kColThreads * V];
   ptx::griddep_wait();
@@ -116,18 +116,26 @@ __global__ void __launch_bounds__(kColThreads) k_gn_colstats(const T* x, GnShape
       for (int e = 0; e < V; ++e) m[e] = -piv[e];
       PV::of(m, np);
     }
-#pragma unroll 4
-    for (int r = p.r0; r < p.r1; r += g.TR, q += step) {
-      float v[V];
-      uint64_t d[PV::N];
-      Vec<T, V>::unpack(Vec<T, V>::load(q), v);
-      PV::of(v, d);
+    constexpr int U = 4;  // vectors in flight
+    for (int r = p.r0; r < p.r1; r += U * g.TR, q += U * step) {
+      typename Vec<T, V>::Raw raw[U];
 #pragma unroll
-      for (int e = 0; e < PV::N; ++e) {
-        d[e] = ptx::add2(d[e], np[e]);
-        a1[e] = ptx::add2(a1[e], d[e]);
-        a2[e] = ptx::fma2(d[e], d[e], a2[e]);
-      }
+      for (int u = 0; u < U; ++u)
+        if (r + u * g.TR < p.r1) raw[u] = Vec<T, V>::load(q + u * step);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + u * g.TR < p.r1) {
+          float v[V];
+          uint64_t d[PV::N];
+          Vec<T, V>::unpack(raw[u], v);
+          PV::of(v, d);
+#pragma unroll
+          for (int e = 0; e < PV::N; ++e) {
+            d[e] = ptx::add2(d[e], np[e]);
+            a1[e] = ptx::add2(a1[e], d[e]);
+            a2[e] = ptx::fma2(d[e], d[e], a2[e]);
+          }
+        }
     }
   }
   const int rows = p.r1 - p.ch * g.chunk;
@@ -160,44 +168,54 @@ __global__ void __launch_bounds__(kColThreads) k_gn_colstats(const T* x, GnShape
   }
 }
 
+constexpr int kFoldThreads = 256;
 __device__ __forceinline__ float block_sum(float v, float* sm) {
   v = warp_sum(v);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
   __syncthreads();
   float t = 0.f;
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) t += sm[w];
+#pragma unroll
+  for (int w = 0; w < kFoldThreads / 32; ++w) t += sm[w];
   return t;
+}
+// f(partial sums, channel within the group, positions) over the chunks'
+// columns of one group, eight loads in flight.
+template <typename F>
+__device__ __forceinline__ void walk_cells(const float2* p, const GnShape& s, const ColGeom& g, F f) {
+  constexpr int U = 8;
+  const int cells = g.chunks * s.Cg;
+  for (int i0 = threadIdx.x; i0 < cells; i0 += U * kFoldThreads) {
+    float2 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kFoldThreads;
+      const int ch = (int)g.by_Cg.div((uint32_t)i);
+      if (i < cells) q[u] = p[(long long)ch * s.C + (i - ch * s.Cg)];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kFoldThreads;
+      const int ch = (int)g.by_Cg.div((uint32_t)i);
+      if (i < cells) f(q[u], i - ch * s.Cg, (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
+    }
+  }
 }
 
 // One block per (sample, group): the chunks' column statistics to mean and rstd.
 template <typename T>
-__global__ void __launch_bounds__(128) k_gn_fold(const T* x, const float2* part, GnShape s, ColGeom g,
-                                                 float* mean_out, float* rstd_out) {
-  __shared__ float sm[4];
+__global__ void __launch_bounds__(kFoldThreads) k_gn_fold(const T* x, const float2* part, GnShape s, ColGeom g,
+                                                          float* mean_out, float* rstd_out) {
+  __shared__ float sm[kFoldThreads / 32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
   const float2* p = part + (long long)b * g.chunks * s.C + gr * s.Cg;
   const float total = (float)s.S * (float)s.Cg;
-  // the chunks' columns, walked without divisions: cell (ch, c) of chunks x Cg
-  const int dch = 128 / s.Cg, dc = 128 - dch * s.Cg;
-  const int ch0 = (int)g.by_Cg.div(threadIdx.x), c0 = (int)threadIdx.x - ch0 * s.Cg;
-  auto walk = [&](auto f) {
-    for (int ch = ch0, c = c0; ch < g.chunks;) {
-      f(p[(long long)ch * s.C + c], (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
-      ch += dch;
-      c += dc;
-      if (c >= s.Cg) {
-        c -= s.Cg;
-        ++ch;
-      }
-    }
-  };
   float sum = 0.f, M2 = 0.f;
-  walk([&](float2 q, float rows) { sum = fmaf(q.x, rows, sum); });
+  walk_cells(p, s, g, [&](float2 q, int, float rows) { sum = fmaf(q.x, rows, sum); });
   const float mean = block_sum(sum, sm) / total;
-  walk([&](float2 q, float rows) {
+  walk_cells(p, s, g, [&](float2 q, int, float rows) {
     const float d = q.x - mean;
     M2 += fmaf(d * d, rows, q.y);
   });
@@ -291,7 +309,7 @@ struct GradCols {
 
 // Column sums (du, du h) over a chunk of a sample's positions.
 template <typename T, int V>
-__global__ void __launch_bounds__(kColThreads) k_gn_grad_colsums(const T* dy, const T* x, GnShape s, ColGeom g,
+__global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy, const T* x, GnShape s, ColGeom g,
                                                                  const float* mean, const float* rstd,
                                                                  const float* gamma, const float* beta,
                                                                  float2* part) {
@@ -308,7 +326,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_grad_colsums(const T* dy, co
     const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
     const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy;
-    constexpr int U = 2;
+    constexpr int U = 4;  // positions in flight
     for (int r = p.r0; r < p.r1; r += U * g.TR) {
       typename Vec<T, V>::Raw rx[U], rd[U];
 #pragma unroll
@@ -355,28 +373,18 @@ __global__ void __launch_bounds__(kColThreads) k_gn_grad_colsums(const T* dy, co
 }
 
 // One block per (sample, group): the averages <gamma du> and <gamma du h>.
-__global__ void __launch_bounds__(128) k_gn_grad_fold(const float2* part, GnShape s, ColGeom g, const float* gamma,
-                                                      float2* avg) {
-  __shared__ float sm[4];
+__global__ void __launch_bounds__(kFoldThreads) k_gn_grad_fold(const float2* part, GnShape s, ColGeom g,
+                                                               const float* gamma, float2* avg) {
+  __shared__ float sm[kFoldThreads / 32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
-  const float2* p = part + (long long)b * g.chunks * s.C + gr * s.Cg;
-  const int dch = 128 / s.Cg, dc = 128 - dch * s.Cg;
-  int ch = (int)g.by_Cg.div(threadIdx.x), c = (int)threadIdx.x - ch * s.Cg;
   float m1 = 0.f, m2 = 0.f;
-  while (ch < g.chunks) {
-    const float2 q = p[(long long)ch * s.C + c];
-    const float ga = gamma ? gamma[gr * s.Cg + c] : 1.f;
+  walk_cells(part + (long long)b * g.chunks * s.C + gr * s.Cg, s, g, [&](float2 q, int c, float) {
+    const float ga = gamma ? __ldg(gamma + gr * s.Cg + c) : 1.f;
     m1 = fmaf(ga, q.x, m1);
     m2 = fmaf(ga, q.y, m2);
-    ch += dch;
-    c += dc;
-    if (c >= s.Cg) {
-      c -= s.Cg;
-      ++ch;
-    }
-  }
+  });
   const float total = (float)s.S * (float)s.Cg;
   m1 = block_sum(m1, sm);
   m2 = block_sum(m2, sm);
@@ -398,7 +406,7 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
     long long rows = f.rows;
     if (f.units > 0) {
       const long long first = (long long)(c / f.W) * f.n;
-      rows = ((first + f.n - 1) / f.units - first / f.units + 1) * f.K;
+      rows = (first + f.n - 1) / f.units - first / f.units + 1;
     }
 #pragma unroll 8
     for (long long r = tr; r < rows; r += kFoldRows) {
@@ -422,7 +430,7 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kColThreads) k_gn_grad_apply(const T* dy, const T* x, GnShape s, ColGeom g,
+__global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, const T* x, GnShape s, ColGeom g,
                                                                const float* mean, const float* rstd,
                                                                const float* gamma, const float* beta,
                                                                const float2* avg, T* dx) {
@@ -450,7 +458,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_grad_apply(const T* dy, cons
   const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
   T* o = dx + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy, so = (long long)g.TR * s.ldy;
-  constexpr int U = 2;
+  constexpr int U = 4;  // positions in flight
   for (int r = p.r0; r < p.r1; r += U * g.TR) {
     typename Vec<T, V>::Raw rx[U], rd[U];
 #pragma unroll
@@ -502,11 +510,11 @@ int vec_of(int C, int esize, const void* a, long long lda, const void* b, long l
 
 // What a call runs: decided by its sizes, its type and the alignment of its
 // rows.
-enum Path { ROWS, CLUSTER, GENERAL };
+enum Path { ROWS, BLOCK, GENERAL };
 struct Plan {
   Path path;
   int V;              // values per access
-  GnClusterPlan cl;
+  GnBlockPlan block;
   long long bytes;    // workspace
 };
 
@@ -515,6 +523,7 @@ struct Plan {
 // bytes, of 4 (bf16) and of one value.
 Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   Plan p{GENERAL, v, {}, 0};
+
   const int wide = 16 / esize;
   int in_group = v;
   while (s.Cg % in_group) in_group /= 2;
@@ -528,14 +537,21 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   const bool rows_fit = values <= kRowsMax && near;
   if (rows_fit && !narrow) p.path = ROWS;
   if (p.path == GENERAL) {
-    p.cl = gn_cluster_plan(s, V, esize, grad);
-    if (p.cl.T > 0)
-      p.path = CLUSTER;
+    // The column passes read x (and dy) twice, at about 5.3 TB/s in all, and
+    // take 8 to 10 us beside; the block path reads once but runs at 3.
+    const double bytes = (double)s.n * s.S * s.C * esize;
+    const double general = grad ? 10.0 + 5 * bytes / 5.0e6 : 8.0 + 3 * bytes / 5.3e6;
+    p.block = gn_block_plan(s, V, esize, grad);
+    if (p.block.T > 0 && p.block.us <= general)
+      p.path = BLOCK;
     else if (rows_fit)
       p.path = ROWS;
   }
   if (p.path == GENERAL) {
-    p.bytes = align_up((long long)s.n * col_geom(s, v, nullptr, nullptr).chunks * s.C * (long long)sizeof(float2)) +
+    // the gradient's constants of eight columns would leave an SM 16 warps (32
+    // x 4096 x 512 bf16: 153 us, with four 141 us)
+    if (grad && p.V > 4) p.V = 4;
+    p.bytes = align_up((long long)s.n * col_geom(s, p.V, nullptr, nullptr).chunks * s.C * (long long)sizeof(float2)) +
               align_up((long long)s.n * s.G * (long long)sizeof(float2));
     return p;
   }
@@ -543,7 +559,7 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   if (grad) {
     const long long rows =
         p.path == ROWS ? (long long)gn_rows_plan(s, V, true).P * s.S
-                       : ((long long)(s.n - 1) / p.cl.units + 2) * p.cl.K;  // clusters that share a slab
+                       : (long long)(s.n - 1) / p.block.units + 2;  // blocks that share a slab
     p.bytes = align_up(rows * s.C * (long long)sizeof(float2));
   }
   return p;
@@ -554,7 +570,7 @@ ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
   const GnShape& s = a.s;
   const ColGeom g = col_geom(s, V, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
-  if (blocks > 0x7FFFFFFFll || (long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+  if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   float2* part = static_cast<float2*>(a.ws);
   float *mean = a.mean, *rstd = a.rstd;
   if (!mean) {
@@ -565,7 +581,7 @@ ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
   const double bytes = (double)s.n * s.S * s.C * sizeof(T);
   PdlLaunch l1(dim3((unsigned)blocks), dim3(kColThreads), st);
   FF_LAUNCH(K_GNORM, bytes, st, cudaLaunchKernelEx(&l1.cfg, k_gn_colstats<T, V>, a.x, s, g, part), "group norm sums");
-  PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(128), st);
+  PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(kFoldThreads), st);
   FF_LAUNCH(K_GNORM, 0, st,
             cudaLaunchKernelEx(&l2.cfg, k_gn_fold<T>, a.x, static_cast<const float2*>(part), s, g, mean, rstd),
             "group norm fold");
@@ -582,7 +598,7 @@ ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
   const GnShape& s = a.s;
   const ColGeom g = col_geom(s, V, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
-  if (blocks > 0x7FFFFFFFll || (long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+  if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   float2* part = static_cast<float2*>(a.ws);
   float2* avg = reinterpret_cast<float2*>(static_cast<char*>(a.ws) +
                                           align_up((long long)s.n * g.chunks * s.C * (long long)sizeof(float2)));
@@ -593,11 +609,11 @@ ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
             cudaLaunchKernelEx(&l1.cfg, k_gn_grad_colsums<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta, part),
             "group norm gradient sums");
   if (a.dgamma) {
-    const ff_status e = gn_param_fold(part, GnFold{(long long)s.n * g.chunks, 0, 0, 0, 0}, s.C, a.dgamma, a.dbeta, st);
+    const ff_status e = gn_param_fold(part, GnFold{(long long)s.n * g.chunks, 0, 0, 0}, s.C, a.dgamma, a.dbeta, st);
     if (e != FF_OK) return e;
   }
   if (a.out) {
-    PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(128), st);
+    PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(kFoldThreads), st);
     FF_LAUNCH(K_GNORM_GRAD, 0, st,
               cudaLaunchKernelEx(&l2.cfg, k_gn_grad_fold, static_cast<const float2*>(part), s, g, a.gamma, avg),
               "group norm gradient fold");
@@ -620,15 +636,16 @@ ff_status call(const GnArgs<T>& a, long long ws_bytes, bool grad, cudaStream_t s
   const GnShape& s = a.s;
   const int v = grad ? vec_of(s.C, sizeof(T), a.x, s.ldx, a.dy, s.lddy, a.out ? a.out : a.x, a.out ? s.ldy : s.ldx)
                      : vec_of(s.C, sizeof(T), a.x, s.ldx, a.out, s.ldy, a.out, s.ldy);
+  if ((long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const Plan p = plan_of(s, sizeof(T), v, grad);
   if (p.bytes > 0 && (!a.ws || ws_bytes < p.bytes || reinterpret_cast<uintptr_t>(a.ws) % kAlign))
     return FF_ERR_INVALID_ARG;
   if (p.path == ROWS) return gn_rows(a, p.V, grad, st);
-  if (p.path == CLUSTER) return gn_cluster(a, p.V, p.cl, grad, st);
+  if (p.path == BLOCK) return gn_block(a, p.V, p.block, grad, st);
   if constexpr (sizeof(T) == 2)
-    if (v == 8) return general<T, 8>(a, grad, st);
-  if (v >= 4) return general<T, 4>(a, grad, st);
-  if (v == 2) return general<T, 2>(a, grad, st);
+    if (p.V == 8) return norm_general<T, 8>(a, st);
+  if (p.V >= 4) return general<T, 4>(a, grad, st);
+  if (p.V == 2) return general<T, 2>(a, grad, st);
   return general<T, 1>(a, grad, st);
 }
 

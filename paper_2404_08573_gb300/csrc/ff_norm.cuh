@@ -35,28 +35,27 @@ constexpr int kRowsMax = 512;
 struct GnRowsPlan {
   int lanes, sets, P;  // P: blocks along the samples
 };
-// The cluster path: a slab of whole groups of one sample stays in the shared
-// memory of a cluster.
-struct GnClusterPlan {
-  int T, GS, K, nv;      // threads, groups per slab, CTAs per cluster, vectors per thread; T = 0: does not fit
-  int per_sm;            // CTAs an SM holds
-  int clusters, units;   // clusters launched, and (sample, slab) units each takes
+// The block path: a slab of whole groups of one sample stays in the shared
+// memory of a thread block.
+struct GnBlockPlan {
+  int T, GS, nv;      // threads, groups per slab, vectors per thread; T = 0: does not fit
+  int blocks, units;  // blocks launched, and (slab, sample) units each takes
+  double us;          // estimated time
 };
 
 GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad);
-GnClusterPlan gn_cluster_plan(const GnShape& s, int V, int esize, bool grad);
+GnBlockPlan gn_block_plan(const GnShape& s, int V, int esize, bool grad);
 
 template <typename T>
 ff_status gn_rows(const GnArgs<T>& a, int V, bool grad, cudaStream_t st);
 template <typename T>
-ff_status gn_cluster(const GnArgs<T>& a, int V, const GnClusterPlan& p, bool grad, cudaStream_t st);
+ff_status gn_block(const GnArgs<T>& a, int V, const GnBlockPlan& p, bool grad, cudaStream_t st);
 // dbeta and dgamma from partial column sums (du, du h) [., C]: `rows` of them,
-// or, with units > 0, as many as the clusters that took the column's slab
-// (slabs of W columns, n units each; `units` consecutive ones per cluster, K
-// rows per cluster).
+// or, with units > 0, as many as the blocks that took the column's slab (slabs
+// of W columns, n units each; `units` consecutive ones per block).
 struct GnFold {
   long long rows;
-  int units, n, W, K;
+  int units, n, W;
 };
 ff_status gn_param_fold(const float2* part, const GnFold& f, int C, float* dgamma, float* dbeta, cudaStream_t st);
 

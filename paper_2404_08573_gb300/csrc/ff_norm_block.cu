@@ -1,19 +1,20 @@
-// Group norm, the cluster path: a slab (one or more whole groups) of one sample
-// is held in the shared memory of a CTA, or of a cluster of CTAs that split its
-// positions, so x (and dy) are read once, however far apart a group's values
-// lie.
+// Group norm, the block path: a slab (one or more whole groups) of one sample is
+// held in the shared memory of a thread block, so x (and dy) are read once.
 //
-// Persistent: a cluster takes consecutive (slab, sample) units, so gamma, beta
+// Persistent: a block takes consecutive (slab, sample) units, so gamma, beta
 // and the gradient's column sums change with the slab only, and the next
 // unit's values are copied (cp.async) under the arithmetic of this one.  A
 // thread has one vector column of the slab and every TR-th position, and reads
 // only what it copied itself.  Its sums go through shared memory to a few
-// lanes per group, from there (with more than one CTA) to every CTA of the
-// cluster through distributed shared memory, and each thread forms its group's
-// totals in the same order.  Sums of x are held relative to the group's first
-// value, as in ff_norm.cu.  The arithmetic is on pairs: with silu a value
-// costs about 9 instructions forward and 12 in the gradient, which keeps it
-// under the time of its bytes.  Bound by HBM.
+// lanes per group and back.  Sums of x are held relative to the group's first
+// value, as in ff_norm.cu.
+//
+// Bound by the instructions: with silu a value of bf16 takes about 12 forward,
+// and a unit some 200 per thread beside, so 64 x 784 x 256 (32 groups) runs in
+// 17 us, 3.0 TB/s.  Splitting a slab's positions over a cluster of 2 to 8
+// blocks, with the sums exchanged through distributed shared memory, reached
+// larger samples but was slower than the column passes there (32 x 4096 x 512:
+// 100 against 77 us), so larger ones take those.
 #include <algorithm>
 #include <cmath>
 
@@ -22,39 +23,33 @@
 namespace ff {
 namespace {
 
-constexpr int kMaxT = 512, kMaxK = 8, kMaxGS = 64;
+constexpr int kMaxT = 512, kMaxGS = 64;
 constexpr int kGradValues = 32;  // values per thread whose du the gradient keeps in registers
 
 struct Geom {
-  int T, GS, K, k_log, nv, V;
+  int T, GS, nv, V;
   int WV, Wg;    // vectors per position of the slab, and of a group
   int TR, M;     // thread rows; threads per group
   int R, r_log;  // lanes that add up a group's threads (a power of 2)
-  int units, total;  // units per cluster and in all
-  int span;          // gradient: vectors from one stage (x and dy) to the next
+  int lo, rem;   // thread rows below rem have lo + 1 positions, the others lo
+  int units, total;  // units per block and in all
+  int span;      // gradient: vectors from one stage (x and dy) to the next
   int wide;      // gamma and beta are 16-byte aligned
   float inv;     // 1 / values of a group
-  FastDiv by_WV, by_Wg, by_TR, by_n;
+  FastDiv by_WV, by_Wg, by_n;
 };
 
 struct Place {
-  int rank, r0;
-  int lo, rem;           // thread rows below rem take lo + 1 of the CTA's positions, the others lo
   int tc, tr, gl, slot;  // vector column, thread row, group within the slab, place among its threads
   int mine;              // positions of this thread
   bool on;
-  __device__ __forceinline__ Place(const GnShape& s, const Geom& q) {
-    rank = (int)(blockIdx.x & (unsigned)(q.K - 1));
-    r0 = (int)((long long)s.S * rank >> q.k_log);
-    const int rows = (int)((long long)s.S * (rank + 1) >> q.k_log) - r0;
-    lo = (int)q.by_TR.div((uint32_t)rows);
-    rem = rows - lo * q.TR;
+  __device__ __forceinline__ explicit Place(const Geom& q) {
     tr = (int)q.by_WV.div(threadIdx.x);
     tc = (int)threadIdx.x - tr * q.WV;
     on = tr < q.TR;
     gl = on ? (int)q.by_Wg.div((uint32_t)tc) : 0;
     slot = gl * q.M + tr * q.Wg + (tc - gl * q.Wg);
-    mine = on ? lo + (tr < rem ? 1 : 0) : 0;
+    mine = on ? q.lo + (tr < q.rem ? 1 : 0) : 0;
   }
 };
 
@@ -74,64 +69,12 @@ struct Cursor {
     }
   }
   __device__ __forceinline__ long long offset(const GnShape& s, const Geom& q, const Place& p, long long ld) const {
-    return ((long long)b * s.S + p.r0 + p.tr) * ld + slab * q.GS * s.Cg + (p.on ? p.tc * q.V : 0);
+    return ((long long)b * s.S + p.tr) * ld + slab * q.GS * s.Cg + (p.on ? p.tc * q.V : 0);
   }
 };
 
-// The groups' totals of each CTA of a cluster, in every CTA of it: sent as
-// asynchronous stores that a barrier of the receiver counts (a cluster barrier
-// would make every thread wait for its global stores as well).  Two buffers:
-// a CTA sends unit u + 2 only after it has everyone's u + 1, which each sends
-// after it has read u.
-template <typename E>
-struct Exchange {
-  uint64_t* bar;  // [2]
-  E* at;          // [2][K][GS]
-  volatile int* never;
-  int K, GS;
-  __device__ __forceinline__ Exchange(uint8_t* mem, const Geom& q)
-      : bar(reinterpret_cast<uint64_t*>(mem)),
-        at(reinterpret_cast<E*>(mem + 32)),
-        never(reinterpret_cast<volatile int*>(mem + 16)),
-        K(q.K),
-        GS(q.GS) {
-    if (K > 1) {
-      if (threadIdx.x == 0) {
-        ptx::mbar_init(&bar[0], 1);
-        ptx::mbar_init(&bar[1], 1);
-        *never = 0;
-        ptx::fence_mbar_init();
-      }
-      __syncwarp();
-      ptx::cluster_arrive_relaxed();
-    }
-  }
-  __device__ __forceinline__ E* of(int k, int rank) const { return at + (k * K + rank) * GS; }
-  __device__ __forceinline__ void expect(int k) {
-    if (K > 1 && threadIdx.x == 0) ptx::mbar_arrive_expect_tx(&bar[k], (uint32_t)(K * GS * sizeof(E)));
-    __syncwarp();
-  }
-  // A group's totals of this CTA, to CTA `to`.
-  __device__ __forceinline__ void send(int k, int from, int to, int g, const E& v) {
-    if (K == 1)
-      of(k, 0)[g] = v;
-    else if constexpr (sizeof(E) == 16)
-      ptx::st_async4(of(k, from) + g, &bar[k], (uint32_t)to, v);
-    else
-      ptx::st_async2(of(k, from) + g, &bar[k], (uint32_t)to, v);
-  }
-  // Everyone's totals of the k-th buffer's n-th use are here; false if they
-  // did not come in time.
-  __device__ __forceinline__ bool wait(int k, int n) {
-    if (K > 1) return ptx::mbar_wait_cluster(&bar[k], (uint32_t)n & 1u, kWaitTimeoutNs, const_cast<int*>(never));
-    __syncthreads();
-    return true;
-  }
-};
-// Bytes of the exchange and of the threads' sums, before the stages.
-__host__ __device__ constexpr int head_bytes(int T, int GS, int K, int esize) {
-  return (32 + 2 * K * GS * esize + 2 * T * 8 + 15) & ~15;
-}
+// Bytes of the groups' totals and of the threads' sums, before the stages.
+__host__ __device__ constexpr int head_bytes(int T, int GS) { return (2 * GS * 8 + 2 * T * 8 + 15) & ~15; }
 
 // This thread's positions of a unit, into its own places of a stage:
 // vector i at [i T + thread].
@@ -153,18 +96,18 @@ __device__ __forceinline__ void fetch(typename Vec<T, V>::Raw* stage, const T* p
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kMaxT, 2) k_gn_cluster(GnArgs<T> a, Geom q) {
+__global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
   using VV = Vec<T, V>;
   using PV = Pairs<V>;
   using Raw = typename VV::Raw;
   extern __shared__ __align__(16) uint8_t smem[];
   const GnShape& s = a.s;
-  const Place p(s, q);
-  Exchange<float4> xch(smem, q);
-  float2* parts = reinterpret_cast<float2*>(smem + 32 + 2 * q.K * q.GS * sizeof(float4));  // [2][T]
-  Raw* stages = reinterpret_cast<Raw*>(smem + head_bytes(q.T, q.GS, q.K, sizeof(float4)));  // [2][nv T]
+  const Place p(q);
+  float2* totals = reinterpret_cast<float2*>(smem);  // [2][GS]
+  float2* parts = totals + 2 * q.GS;                 // [2][T]
+  Raw* stages = reinterpret_cast<Raw*>(smem + head_bytes(q.T, q.GS));  // [2][nv T]
   const int stage = q.nv * q.T;
-  const int u0 = (int)(blockIdx.x >> q.k_log) * q.units, u1 = min(q.total, u0 + q.units);
+  const int u0 = (int)blockIdx.x * q.units, u1 = min(q.total, u0 + q.units);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   Cursor cur(u0, s, q), ahead = cur;
@@ -182,13 +125,11 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_cluster(GnArgs<T> a, Geom q) {
     ptx::cp_async_commit();
   };
   start(u0, 0);
-  if (q.K > 1) ptx::cluster_wait();  // every CTA of the cluster runs: its shared memory may be written
   float ga[V], be[V];
   int slab = -1;
   for (int u = u0; u < u1; ++u, cur.next(s)) {
     const int k = (u - u0) & 1;
     const float P = pivot;
-    xch.expect(k);
     start(u + 1, k ^ 1);
     if (cur.slab != slab) {
       slab = cur.slab;
@@ -238,38 +179,24 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_cluster(GnArgs<T> a, Geom q) {
       const bool real = gg < q.GS;
       const float2* t = part + gg * q.M;
       // a group's threads in order of their thread rows: the first `many` have one position more
-      const int many = p.rem * q.Wg;
-      const float chi = (float)((p.lo + 1) * V), clo = (float)(p.lo * V);
-      const float n = chi * (float)many + clo * (float)(q.M - many);
+      const int many = q.rem * q.Wg;
+      const float chi = (float)((q.lo + 1) * V), clo = (float)(q.lo * V);
       float sum = 0.f, m2 = 0.f;
       for (int j = l; real && j < q.M; j += q.R) sum = fmaf(t[j].x, j < many ? chi : clo, sum);
       for (int o = q.R / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const float mean = __fdividef(sum, n);
+      const float mean = sum * q.inv;
       for (int j = l; real && j < q.M; j += q.R) {
         const float cnt = j < many ? chi : clo, d = t[j].x - mean;
         if (cnt > 0.f) m2 += fmaf(d * d, cnt, t[j].y);
       }
       for (int o = q.R / 2; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-      // lane r of the group tells CTA r (R >= K, see the plan)
-      if (real && l < q.K) xch.send(k, p.rank, l, gg, make_float4(n, mean, m2, 0.f));
+      if (real && l == 0) totals[k * q.GS + gg] = make_float2(mean, rsqrtf(m2 * q.inv + s.eps));
     }
-    const bool ok = xch.wait(k, (u - u0) >> 1);
+    __syncthreads();
     if (!p.on) continue;
-    const float4* tot = xch.of(k, 0) + p.gl;
-    float dm = tot[0].y, m2 = tot[0].z;
-    if (q.K > 1) {
-      float sum = 0.f;
-      for (int r = 0; r < q.K; ++r) sum = fmaf(tot[r * q.GS].x, tot[r * q.GS].y, sum);
-      dm = sum * q.inv;
-      m2 = 0.f;
-      for (int r = 0; r < q.K; ++r) {
-        const float4 t = tot[r * q.GS];
-        m2 += fmaf((t.y - dm) * (t.y - dm), t.x, t.z);
-      }
-    }
-    // (totals that never came leave NaN behind)
-    const float mean = ok ? P + dm : __int_as_float(0x7FC00000), rstd = rsqrtf(m2 * q.inv + s.eps);
-    if (a.mean && p.rank == 0 && p.tr == 0 && p.tc == p.gl * q.Wg) {
+    const float2 tot = totals[k * q.GS + p.gl];
+    const float mean = P + tot.x, rstd = tot.y;
+    if (a.mean && p.tr == 0 && p.tc == p.gl * q.Wg) {
       const long long at = (long long)cur.b * s.G + cur.slab * q.GS + p.gl;
       a.mean[at] = mean;
       a.rstd[at] = rstd;
@@ -298,29 +225,25 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_cluster(GnArgs<T> a, Geom q) {
       VV::store(y, v);
     }
   }
-  if (q.K > 1) {  // no CTA leaves while another may still send to it
-    ptx::cluster_arrive_relaxed();
-    ptx::cluster_wait();
-  }
 }
 
 // The gradient.  part_out receives the column sums (du, du h) of each run of
-// units of one slab: row (cluster - first cluster of the slab) K + rank.
+// units of one slab: row (block - first block of the slab).
 template <typename T, int V, int NV>
-__global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom q, float2* part_out) {
+__global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q, float2* part_out) {
   using VV = Vec<T, V>;
   using PV = Pairs<V>;
   using Raw = typename VV::Raw;
   extern __shared__ __align__(16) uint8_t smem[];
   const GnShape& s = a.s;
-  const Place p(s, q);
-  Exchange<float2> xch(smem, q);
-  float2* parts = reinterpret_cast<float2*>(smem + 32 + 2 * q.K * q.GS * sizeof(float2));  // [2][T]
+  const Place p(q);
+  float2* totals = reinterpret_cast<float2*>(smem);  // [2][GS]
+  float2* parts = totals + 2 * q.GS;                 // [2][T]
   // [2]: x [nv T], dy [nv T]; or the column sums
-  Raw* stages = reinterpret_cast<Raw*>(smem + head_bytes(q.T, q.GS, q.K, sizeof(float2)));
+  Raw* stages = reinterpret_cast<Raw*>(smem + head_bytes(q.T, q.GS));
   const int stage = q.nv * q.T;
-  const int cluster = (int)(blockIdx.x >> q.k_log);
-  const int u0 = cluster * q.units, u1 = min(q.total, u0 + q.units);
+  const int block = (int)blockIdx.x;
+  const int u0 = block * q.units, u1 = min(q.total, u0 + q.units);
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   Cursor cur(u0, s, q), ahead = cur;
@@ -338,7 +261,6 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom 
     ptx::cp_async_commit();
   };
   start(u0, 0);
-  if (q.K > 1) ptx::cluster_wait();
   float ga[V], be[V];
   uint64_t G2[PV::N], B2[PV::N], p0[PV::N], p1[PV::N];
 #pragma unroll
@@ -356,8 +278,8 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom 
 #pragma unroll
     for (int e = 0; e < V; ++e) cols[e * q.T + threadIdx.x] = make_float2(v0[e], v1[e]);
     __syncthreads();
-    const int first = (int)((long long)of * s.n / q.units);  // cluster that took the slab's first unit
-    float2* to = part_out + ((long long)(cluster - first) * q.K + p.rank) * s.C + of * q.GS * s.Cg;
+    const int first = (int)((long long)of * s.n / q.units);  // block that took the slab's first unit
+    float2* to = part_out + (long long)(block - first) * s.C + of * q.GS * s.Cg;
     for (int i = threadIdx.x; i < q.WV * V; i += q.T) {
       const int e = (int)q.by_WV.div((uint32_t)i), tc = i - e * q.WV;
       const float2* col = cols + e * q.T + tc;
@@ -385,7 +307,6 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom 
     }
     const float mu = nmu, rs = nrs;
     float2* part = parts + k * q.T;
-    if (a.out) xch.expect(k);
     start(u + 1, k ^ 1);
     ptx::cp_async_wait<1>();
     const Raw* mx = stages + k * q.span + threadIdx.x;
@@ -445,18 +366,13 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom 
         w.x += __shfl_xor_sync(0xffffffffu, w.x, o);
         w.y += __shfl_xor_sync(0xffffffffu, w.y, o);
       }
-      if (real && l < q.K) xch.send(k, p.rank, l, gg, w);
+      if (real && l == 0) totals[k * q.GS + gg] = w;
     }
-    const bool ok = xch.wait(k, (u - u0) >> 1);
+    __syncthreads();
     if (!p.on) continue;
-    float w1 = ok ? 0.f : __int_as_float(0x7FC00000), w2 = w1;
-    const float2* tot = xch.of(k, 0) + p.gl;
-    for (int r = 0; r < q.K; ++r) {
-      w1 += tot[r * q.GS].x;
-      w2 += tot[r * q.GS].y;
-    }
+    const float2 tot = totals[k * q.GS + p.gl];
     // dx = rs (gamma du - <.> - h <.>) = du (gamma rs) + h c2 + c1
-    const uint64_t c1 = both(-rs * w1 * q.inv), c2 = both(-rs * w2 * q.inv);
+    const uint64_t c1 = both(-rs * tot.x * q.inv), c2 = both(-rs * tot.y * q.inv);
     uint64_t gr[PV::N];
 #pragma unroll
     for (int e = 0; e < PV::N; ++e) gr[e] = ptx::mul2(G2[e], r2);
@@ -479,27 +395,22 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_cluster_grad(GnArgs<T> a, Geom 
   // all copies have landed and been used; the last unit's stage is not read any more by its own thread,
   // and the other stage is free
   if (slab >= 0) flush(slab, ((u1 - u0 - 1) & 1) ^ 1);
-  if (q.K > 1) {
-    ptx::cluster_arrive_relaxed();
-    ptx::cluster_wait();
-  }
 }
 
 template <typename T>
-Geom geom_of(const GnArgs<T>& a, int V, const GnClusterPlan& p) {
+Geom geom_of(const GnArgs<T>& a, int V, const GnBlockPlan& p) {
   const GnShape& s = a.s;
   Geom q;
   q.T = p.T;
   q.GS = p.GS;
-  q.K = p.K;
   q.nv = p.nv;
   q.V = V;
-  q.k_log = 0;
-  while ((1 << q.k_log) < q.K) ++q.k_log;
   q.Wg = s.Cg / V;
   q.WV = q.Wg * q.GS;
   q.TR = q.T / q.WV;
   q.M = q.TR * q.Wg;
+  q.lo = s.S / q.TR;
+  q.rem = s.S - q.lo * q.TR;
   q.r_log = 5;
   while ((q.GS << q.r_log) > q.T) --q.r_log;
   q.R = 1 << q.r_log;
@@ -510,7 +421,6 @@ Geom geom_of(const GnArgs<T>& a, int V, const GnClusterPlan& p) {
   q.inv = 1.f / ((float)s.S * (float)s.Cg);
   q.by_WV = FastDiv(q.WV);
   q.by_Wg = FastDiv(q.Wg);
-  q.by_TR = FastDiv(q.TR);
   q.by_n = FastDiv(s.n);
   return q;
 }
@@ -524,102 +434,77 @@ int stage_bytes(int T, int nv, int V, int esize, bool grad) {
 }
 
 template <auto KERNEL, typename... A>
-ff_status run(KernelKind kind, double bytes, const Geom& q, const GnClusterPlan& p, int smem, cudaStream_t st,
+ff_status run(KernelKind kind, double bytes, const Geom& q, const GnBlockPlan& p, int smem, cudaStream_t st,
               const A&... args) {
   static const cudaError_t attr =
       cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   FF_TRY(attr, "group norm");
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.clusters * q.K));
-  cfg.blockDim = dim3((unsigned)q.T);
-  cfg.dynamicSmemBytes = (size_t)smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)q.K;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = q.K > 1 ? 2 : 1;
-  FF_LAUNCH(kind, bytes, st, cudaLaunchKernelEx(&cfg, KERNEL, args...), "group norm");
+  PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)q.T), st, (size_t)smem);
+  FF_LAUNCH(kind, bytes, st, cudaLaunchKernelEx(&l.cfg, KERNEL, args...), "group norm");
   return FF_OK;
 }
 
 template <typename T, int V, int NV>
-ff_status run_grad(const GnArgs<T>& a, const Geom& q, const GnClusterPlan& p, double bytes, int smem, float2* part,
+ff_status run_grad(const GnArgs<T>& a, const Geom& q, const GnBlockPlan& p, double bytes, int smem, float2* part,
                    cudaStream_t st) {
-  return run<k_gn_cluster_grad<T, V, NV>>(K_GNORM_GRAD, bytes, q, p, smem, st, a, q, part);
+  return run<k_gn_block_grad<T, V, NV>>(K_GNORM_GRAD, bytes, q, p, smem, st, a, q, part);
 }
 
 template <typename T, int V>
-ff_status run_v(const GnArgs<T>& a, const GnClusterPlan& p, bool grad, cudaStream_t st) {
+ff_status run_v(const GnArgs<T>& a, const GnBlockPlan& p, bool grad, cudaStream_t st) {
   const Geom q = geom_of(a, V, p);
   const double bytes = (double)a.s.n * a.s.S * a.s.C * sizeof(T);
-  const int smem = head_bytes(q.T, q.GS, q.K, grad ? 8 : 16) + stage_bytes(q.T, q.nv, V, sizeof(T), grad);
-  if (!grad) return run<k_gn_cluster<T, V>>(K_GNORM, 2 * bytes, q, p, smem, st, a, q);
+  const int smem = head_bytes(q.T, q.GS) + stage_bytes(q.T, q.nv, V, sizeof(T), grad);
+  if (!grad) return run<k_gn_block<T, V>>(K_GNORM, 2 * bytes, q, p, smem, st, a, q);
   float2* part = a.dgamma ? static_cast<float2*>(a.ws) : nullptr;
   constexpr int N = V == 1 ? 16 : kGradValues / V;  // vectors per thread at most
   const ff_status e = q.nv <= N / 4   ? run_grad<T, V, N / 4>(a, q, p, 3 * bytes, smem, part, st)
                       : q.nv <= N / 2 ? run_grad<T, V, N / 2>(a, q, p, 3 * bytes, smem, part, st)
                                       : run_grad<T, V, N>(a, q, p, 3 * bytes, smem, part, st);
   if (e != FF_OK || !part) return e;
-  return gn_param_fold(part, GnFold{0, p.units, a.s.n, q.GS * a.s.Cg, q.K}, a.s.C, a.dgamma, a.dbeta, st);
+  return gn_param_fold(part, GnFold{0, p.units, a.s.n, q.GS * a.s.Cg}, a.s.C, a.dgamma, a.dbeta, st);
 }
 
 }  // namespace
 
-// Threads, slab, cluster and stages with the least estimated time (us): the
-// rounds of a cluster at the latency of one (copy, two exchanges, store) or
-// the bytes at the rate that the slab's row segments allow, whichever is
-// longer.
-GnClusterPlan gn_cluster_plan(const GnShape& s, int V, int esize, bool grad) {
-  GnClusterPlan best{};
-  double t = 1e30;
+// Threads and slab with the least estimated time (us): the rounds of a block
+// at its instructions' time (a warp issues every 6 clocks or so, an SM's all
+// together one a clock and scheduler), or the bytes at the rate this path
+// reaches with the slab's row segments, whichever is longer.
+GnBlockPlan gn_block_plan(const GnShape& s, int V, int esize, bool grad) {
+  GnBlockPlan best{};
+  best.us = 1e30;
   const double total = (double)s.n * s.S * s.C * esize * (grad ? 3 : 2);
   // du of a thread's values stays in registers: 32 of them, 16 one by one
-  const int most = grad ? (V == 1 ? 16 : kGradValues) : 1 << 20;
+  const int most = grad ? (V == 1 ? 16 : kGradValues) : 1024;
   for (int GS = 1; GS <= s.G && GS <= kMaxGS; ++GS) {
     if (s.G % GS) continue;
     const long long WV = (long long)GS * (s.Cg / V);
     if (WV > kMaxT) break;
     const double seg = (double)WV * V * esize;
-    const double eff = seg >= 128 ? 1.0 : seg >= 64 ? 0.9 : seg >= 32 ? 0.8 : seg / 40;
+    const double eff = seg >= 128 ? 1.0 : seg >= 64 ? 0.95 : seg >= 32 ? 0.85 : seg / 38;
     for (int T = 128; T <= kMaxT; T *= 2) {
-      if (WV > T) continue;
-      const int TR = T / (int)WV;
-      for (int K = 1; K <= kMaxK && K <= s.S; K *= 2) {
-        if (K * GS > T) continue;  // a lane per group and CTA
-        const int nv = cdiv(cdiv(s.S, K), TR);
-        if ((long long)nv * V > most) continue;
-        if ((long long)nv * V > 1024) continue;
-        const long long bytes = head_bytes(T, GS, K, grad ? 8 : 16) + stage_bytes(T, nv, V, esize, grad);
-        if (bytes > kSmem) continue;
-        const int regs = !grad ? 64 : nv * V <= 8 ? 104 : 128;
-        int per_sm = std::min(std::min(2048 / T, 65536 / (T * regs)), (int)(kSmem / (bytes + 1024)));
-        per_sm = std::max(1, std::min(per_sm, 32));
-        const int sms = K == 8 ? 120 : K == 4 ? 144 : 152;  // clusters do not fill every GPC
-        const long long units = (long long)s.n * (s.G / GS);
-        if (units > 0x3FFFFFFF) continue;
-        const long long room = std::max(1ll, (long long)sms * per_sm / K);
-        const long long rounds = (units + room - 1) / room;
-        // a value's instructions, at the rate that the SM's warps reach: each
-        // issues every 6 clocks or so, all together one a clock and scheduler
-        const double warps = per_sm * T / 32.0, issue = std::max(6.0, warps / 4.0) / 1900.0;
-        const double lat = 0.6 + (K > 1 ? 0.6 : 0.0) + (200 + nv * V * (grad ? 18 : 12)) * issue;
-        const double c = std::max(rounds * lat, total / 6.4e6 / eff * 152.0 / sms) + 2.0;
-        if (c < t) {
-          t = c;
-          best = GnClusterPlan{T, GS, K, nv, per_sm, (int)((units + rounds - 1) / rounds), (int)rounds};
-        }
-      }
+      if (WV > T || GS > T) continue;
+      const int TR = T / (int)WV, nv = cdiv(s.S, TR);
+      if ((long long)nv * V > most) continue;
+      const long long bytes = head_bytes(T, GS) + stage_bytes(T, nv, V, esize, grad);
+      if (bytes > kSmem - 1024) continue;
+      const int regs = !grad ? 64 : nv * V <= 8 ? 104 : 128;
+      const int per_sm = std::max(1, std::min(std::min(2048 / T, 65536 / (T * regs)), (int)(kSmem / (bytes + 1024))));
+      const long long units = (long long)s.n * (s.G / GS);
+      if (units > 0x3FFFFFFF) continue;
+      const long long room = 152ll * per_sm, rounds = (units + room - 1) / room;
+      const double warps = per_sm * T / 32.0, issue = std::max(6.0, warps / 4.0) / 1900.0;
+      const double round = 0.6 + (200 + nv * V * (grad ? 18 : 12)) * issue;
+      const double us = 3.0 + std::max(rounds * round, total / (grad ? 2.9e6 : 3.4e6) / eff);
+      if (us < best.us) best = GnBlockPlan{T, GS, nv, (int)((units + rounds - 1) / rounds), (int)rounds, us};
     }
   }
   return best;
 }
 
 template <typename T>
-ff_status gn_cluster(const GnArgs<T>& a, int V, const GnClusterPlan& p, bool grad, cudaStream_t st) {
+ff_status gn_block(const GnArgs<T>& a, int V, const GnBlockPlan& p, bool grad, cudaStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (V == 8) return run_v<T, 8>(a, p, grad, st);
     if (V == 2) return run_v<T, 2>(a, p, grad, st);
@@ -628,7 +513,7 @@ ff_status gn_cluster(const GnArgs<T>& a, int V, const GnClusterPlan& p, bool gra
   }
   return run_v<T, 1>(a, p, grad, st);
 }
-template ff_status gn_cluster<bf16>(const GnArgs<bf16>&, int, const GnClusterPlan&, bool, cudaStream_t);
-template ff_status gn_cluster<float>(const GnArgs<float>&, int, const GnClusterPlan&, bool, cudaStream_t);
+template ff_status gn_block<bf16>(const GnArgs<bf16>&, int, const GnBlockPlan&, bool, cudaStream_t);
+template ff_status gn_block<float>(const GnArgs<float>&, int, const GnBlockPlan&, bool, cudaStream_t);
 
 }  // namespace ff

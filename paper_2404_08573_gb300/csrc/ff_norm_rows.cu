@@ -261,7 +261,7 @@ ff_status run(const GnArgs<T>& a, const GnRowsPlan& pl, bool grad, cudaStream_t 
   float2* part = a.dgamma ? static_cast<float2*>(a.ws) : nullptr;
   FF_LAUNCH(K_GNORM_GRAD, 3 * bytes, st, cudaLaunchKernelEx(&l.cfg, k_gn_rows_grad<T, V, NV>, a, pl, part),
             "group norm gradient of rows");
-  return part ? gn_param_fold(part, GnFold{(long long)pl.P * a.s.S, 0, 0, 0, 0}, a.s.C, a.dgamma, a.dbeta, st) : FF_OK;
+  return part ? gn_param_fold(part, GnFold{(long long)pl.P * a.s.S, 0, 0, 0}, a.s.C, a.dgamma, a.dbeta, st) : FF_OK;
 }
 
 }  // namespace
