@@ -528,13 +528,12 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   int in_group = v;
   while (s.Cg % in_group) in_group /= 2;
   const int V = in_group == wide ? wide : esize == 2 && in_group >= 2 ? 2 : 1;
-  const long long values = (long long)s.S * s.Cg;
   // A few positions of narrow groups would be fetched a fraction of a 32-byte
   // sector at a time: those go to slabs of several groups.
   const bool narrow = s.S > 1 && s.Cg * esize < 32 && s.G > 1;
   const bool near = (long long)s.S * (s.ldx > s.ldy ? s.ldx : s.ldy) < 0x3FFFFFFF &&
                     (long long)s.S * s.lddy < 0x3FFFFFFF;  // offsets within a sample fit 32 bits
-  const bool rows_fit = values <= kRowsMax && near;
+  const bool rows_fit = gn_rows_fit(s) && near;
   if (rows_fit && !narrow) p.path = ROWS;
   if (p.path == GENERAL) {
     // The column passes read x (and dy) twice, at about 5.3 TB/s in all, and

@@ -29,12 +29,12 @@ struct GnArgs {
   void* ws;
 };
 
-// The rows path: groups of at most kRowsMax values.  `lanes` lanes per group
-// (a power of 2), sets of 32 / lanes groups per warp.
-constexpr int kRowsMax = 512;
+// The rows path: groups in the registers of up to a warp, or of a block.
+// `lanes` lanes per group (a power of 2), sets of groups side by side.
 struct GnRowsPlan {
   int lanes, sets, P;  // P: blocks along the samples
 };
+bool gn_rows_fit(const GnShape& s);
 // The block path: a slab of whole groups of one sample stays in the shared
 // memory of a thread block.
 struct GnBlockPlan {

@@ -78,6 +78,7 @@ SHAPES = [
     (1, 1, 1, 1), (3, 1, 8, 8), (5, 1, 500, 10), (7, 1, 2000, 16), (4, 1, 2000, 8), (2, 1, 6000, 1), (70, 1, 96, 3),
     (2, 3, 30, 2), (2, 2, 1000, 4), (3, 7, 48, 6), (1, 100, 24, 2), (2, 257, 40, 4), (3, 1000, 64, 32), (1, 5000, 16, 1),
     (2, 4100, 320, 32), (1, 20001, 8, 2), (1, 3, 9000, 3), (9, 33, 130, 13), (1, 70000, 4, 2), (1, 9000, 256, 2),
+    (33, 1, 8192, 1), (700, 1, 2001, 1), (6, 1, 4100, 2), (900, 1, 8200, 1), (3, 1, 1200, 2), (40, 49, 256, 32), (300, 784, 64, 8),
 ]
 
 
