@@ -630,6 +630,24 @@ ff_status general(const GnArgs<T>& a, bool grad, cudaStream_t st) {
   return grad ? grad_general<T, V>(a, st) : norm_general<T, V>(a, st);
 }
 
+// The workspace of the path that needs most among those that some stride or
+// alignment of the rows leads to.
+long long workspace_of(int n, int spatial, int channels, int groups, int esize, bool grad) {
+  // the strides only say whether a sample's offsets fit 32 bits: both ways count
+  const GnShape tight{n, spatial, channels, groups, channels / groups, channels, channels, channels, 0.f, 0};
+  GnShape wide = tight;
+  wide.ldx = wide.ldy = wide.lddy = 0x7FFFFFFF;
+  long long most = 0;
+  for (int v = 16 / esize; v >= 1; v /= 2) {
+    if (channels % v) continue;
+    for (const GnShape* s : {&tight, static_cast<const GnShape*>(&wide)}) {
+      const long long b = plan_of(*s, esize, v, grad).bytes;
+      most = b > most ? b : most;
+    }
+  }
+  return most;
+}
+
 template <typename T>
 ff_status call(const GnArgs<T>& a, long long ws_bytes, bool grad, cudaStream_t st) {
   const GnShape& s = a.s;
@@ -637,8 +655,10 @@ ff_status call(const GnArgs<T>& a, long long ws_bytes, bool grad, cudaStream_t s
                      : vec_of(s.C, sizeof(T), a.x, s.ldx, a.out, s.ldy, a.out, s.ldy);
   if ((long long)s.n * s.G > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const Plan p = plan_of(s, sizeof(T), v, grad);
-  if (p.bytes > 0 && (!a.ws || ws_bytes < p.bytes || reinterpret_cast<uintptr_t>(a.ws) % kAlign))
-    return FF_ERR_INVALID_ARG;
+  // what the query promises for the shape, whether or not these rows' strides
+  // and alignment need all of it: a buffer is too small for all calls or none
+  const long long need = workspace_of(s.n, s.S, s.C, s.G, sizeof(T), grad);
+  if (need > 0 && (!a.ws || ws_bytes < need || reinterpret_cast<uintptr_t>(a.ws) % kAlign)) return FF_ERR_INVALID_ARG;
   if (p.path == ROWS) return gn_rows(a, p.V, grad, st);
   if (p.path == BLOCK) return gn_block(a, p.V, p.block, grad, st);
   if constexpr (sizeof(T) == 2)
@@ -666,26 +686,10 @@ ff_status gn_param_fold(const float2* part, const GnFold& f, int C, float* dgamm
 
 using namespace ff;
 
-// The workspace of the path that needs most among those that some alignment
-// of the rows leads to.
 extern "C" FF_API long long ff_group_norm_workspace(int n, int spatial, int channels, int groups, ff_precision prec,
                                                     int backward) {
   if (!good_shape(n, spatial, channels, groups, prec)) return -1;
-  if (n == 0 || spatial == 0) return 0;
-  const int es = prec == FF_BF16 ? 2 : 4;
-  // the strides only say whether a sample's offsets fit 32 bits: both ways count
-  const GnShape tight{n, spatial, channels, groups, channels / groups, channels, channels, channels, 0.f, 0};
-  GnShape wide = tight;
-  wide.ldx = wide.ldy = wide.lddy = 0x7FFFFFFF;
-  long long most = 0;
-  for (int v = 16 / es; v >= 1; v /= 2) {
-    if (channels % v) continue;
-    for (const GnShape* s : {&tight, static_cast<const GnShape*>(&wide)}) {
-      const long long b = plan_of(*s, es, v, backward != 0).bytes;
-      most = b > most ? b : most;
-    }
-  }
-  return most;
+  return n == 0 || spatial == 0 ? 0 : workspace_of(n, spatial, channels, groups, prec == FF_BF16 ? 2 : 4, backward != 0);
 }
 
 extern "C" FF_API ff_status ff_group_norm_act(const void* x, long long ldx, int n, int spatial, int channels,

@@ -271,6 +271,38 @@ def test_refusals():
         ff.group_norm_act_backward(y, x, None, None, None, None, 3)
 
 
+@pytest.mark.parametrize("shape", [(2, 100, 8, 2), (16, 1, 500, 10), (4, 50000, 8, 2)])
+def test_a_short_workspace_is_refused(shape):
+    """Less than the size query's answer is refused for every stride and
+    alignment, also where this call's own path would need less.  The buffers
+    are real and of full size: only the size that is stated is too small."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    L = ff.lib()
+    n, S, C, G = shape
+    x = torch.randn(n * S, C, device="cuda")
+    y, dg, db = torch.zeros_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    m, r = torch.zeros(n, G, device="cuda"), torch.ones(n, G, device="cuda")
+    f, g = (L.ff_group_norm_workspace(n, S, C, G, 0, b) for b in (0, 1))
+    ws = torch.empty(max(f, g) + 16, dtype=torch.uint8, device="cuda")
+
+    def forward(p, size):
+        return L.ff_group_norm_act(x.data_ptr(), C, n, S, C, G, None, None, 1e-5, 2, 0, y.data_ptr(), C, m.data_ptr(),
+                                   r.data_ptr(), p, size, None)
+
+    def backward(p, size):
+        return L.ff_group_norm_act_backward(x.data_ptr(), C, x.data_ptr(), C, n, S, C, G, m.data_ptr(), r.data_ptr(),
+                                            None, None, 2, 0, y.data_ptr(), C, dg.data_ptr(), db.data_ptr(), p, size,
+                                            None)
+
+    for call, need in ((forward, f), (backward, g)):
+        if need:
+            for p, size in ((ws.data_ptr(), need - 1), (ws.data_ptr() + 8, need), (None, need)):
+                assert call(p, size) == 1
+        assert call(ws.data_ptr() if need else None, need) == 0
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("shape", [(64, 1, 500, 10), (8, 1024, 64, 8), (1, 60000, 16, 2)])
 def test_another_stream_and_a_captured_graph(shape):
     """On a side stream that is behind, with the caller's stream free to reuse

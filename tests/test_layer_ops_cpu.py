@@ -4,8 +4,13 @@ host, before anything is enqueued, and size helpers follow their formulas."""
 import ctypes
 
 import pytest
+import torch
 
 from .gpu_common import lib_ready
+
+# The addresses are invented: where a GPU could act on a call that is not
+# refused, nothing here runs.
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="invented addresses: without a GPU only")
 
 P = 4096  # a 16-byte aligned address that no refused call may touch
 OK, BAD = 0, 1
