@@ -15,6 +15,7 @@ layer operators ``group_norm_act`` and its backward pass, ``dropout``,
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_double, c_float, c_int, c_longlong, c_ulonglong, c_void_p
 
@@ -691,8 +692,7 @@ class _On:
     __slots__ = ("ptr", "other")
 
     def __init__(self, stream, device):
-        current = torch.cuda.current_stream(device)
-        self.ptr, self.other = current.cuda_stream, None
+        self.ptr, self.other = torch._C._cuda_getCurrentRawStream(device.index), None
         if stream is not None:
             ptr = _stream(stream)
             if ptr != self.ptr:
@@ -704,6 +704,21 @@ class _On:
         if self.other is not None:
             t.record_stream(self.other)
         return t
+
+
+def _on_device_of_first(f):
+    """Runs an operator with its first argument's device current (the kernels launch on the current device)."""
+
+    @functools.wraps(f)
+    def call(*args, **kwargs):
+        x = args[0] if args else next(iter(kwargs.values()), None)
+        device = x.q.device if type(x) is Fp8Matrix else getattr(x, "device", None)
+        if device is None or device.type != "cuda" or device.index == torch.cuda.current_device():
+            return f(*args, **kwargs)
+        with torch.cuda.device(device):
+            return f(*args, **kwargs)
+
+    return call
 
 
 def _prec(x, what):
@@ -755,6 +770,11 @@ def _same_device(t, device, what):
         raise ValueError(f"{what} must be on {device}")
 
 
+@functools.lru_cache(maxsize=4096)
+def _norm_workspace(n, spatial, C, groups, prec, backward):
+    return lib().ff_group_norm_workspace(n, spatial, C, groups, prec, backward)
+
+
 def _like(t, x, what):
     """Checks an optional buffer that must match x in shape, type and device; returns its row stride."""
     if not isinstance(t, torch.Tensor) or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
@@ -779,6 +799,7 @@ def _norm_args(x, groups, act):
     return n, spatial, C, groups
 
 
+@_on_device_of_first
 def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 1e-5, out=None, mean=None, rstd=None,
                    stream=None):
     """ff_group_norm_act: y = act(gamma * (x - mean) * rstd + beta) over channel
@@ -788,28 +809,27 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     prec = _prec(x, "x")
     n, spatial, C, groups = _norm_args(x, groups, act)
     dev = x.device
-    with torch.cuda.device(dev):
-        on = _On(stream, dev)
-        ldx = _row_stride_of(x, "x")
-        if out is None:
-            out, ldy = on.empty(x.shape, x.dtype, dev), C
-        else:
-            ldy = _like(out, x, "out")
-        if mean is None:
-            mean = on.empty((n, groups), torch.float32, dev)
-        if rstd is None:
-            rstd = on.empty((n, groups), torch.float32, dev)
-        L = lib()
-        need = L.ff_group_norm_workspace(n, spatial, C, groups, prec, 0)
-        ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
-        _check(L.ff_group_norm_act(
-            x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
-            eps, _ACT[act], prec, out.data_ptr(), ldy, _vector(mean, n * groups, "mean", dev),
-            _vector(rstd, n * groups, "rstd", dev), None if ws is None else ws.data_ptr(), max(need, 0), on.ptr),
-            "ff_group_norm_act")
+    on = _On(stream, dev)
+    ldx = _row_stride_of(x, "x")
+    if out is None:
+        out, ldy = on.empty(x.shape, x.dtype, dev), C
+    else:
+        ldy = _like(out, x, "out")
+    if mean is None:
+        mean = on.empty((n, groups), torch.float32, dev)
+    if rstd is None:
+        rstd = on.empty((n, groups), torch.float32, dev)
+    need = _norm_workspace(n, spatial, C, groups, prec, 0)
+    ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+    _check(lib().ff_group_norm_act(
+        x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
+        eps, _ACT[act], prec, out.data_ptr(), ldy, _vector(mean, n * groups, "mean", dev),
+        _vector(rstd, n * groups, "rstd", dev), None if ws is None else ws.data_ptr(), max(need, 0), on.ptr),
+        "ff_group_norm_act")
     return out, mean, rstd
 
 
+@_on_device_of_first
 def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: str = "silu", out=None, stream=None):
     """ff_group_norm_act_backward: the gradient of group_norm_act at (x, gamma,
     beta), with the mean and rstd it returned.  Returns (dx, dgamma, dbeta);
@@ -817,25 +837,23 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     prec = _prec(x, "x")
     n, spatial, C, groups = _norm_args(x, groups, act)
     dev = x.device
-    with torch.cuda.device(dev):
-        on = _On(stream, dev)
-        ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
-        if out is None:
-            out, lddx = on.empty(x.shape, x.dtype, dev), C
-        else:
-            lddx = _like(out, x, "out")
-        dgamma = on.empty((C,), torch.float32, dev)
-        dbeta = on.empty((C,), torch.float32, dev)
-        if mean is None or rstd is None:
-            raise ValueError("mean and rstd of the forward pass are needed")
-        L = lib()
-        need = L.ff_group_norm_workspace(n, spatial, C, groups, prec, 1)
-        ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
-        _check(L.ff_group_norm_act_backward(
-            dy.data_ptr(), lddy, x.data_ptr(), ldx, n, spatial, C, groups, _vector(mean, n * groups, "mean", dev),
-            _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
-            _ACT[act], prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
-            None if ws is None else ws.data_ptr(), max(need, 0), on.ptr), "ff_group_norm_act_backward")
+    on = _On(stream, dev)
+    ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
+    if out is None:
+        out, lddx = on.empty(x.shape, x.dtype, dev), C
+    else:
+        lddx = _like(out, x, "out")
+    dgamma = on.empty((C,), torch.float32, dev)
+    dbeta = on.empty((C,), torch.float32, dev)
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd of the forward pass are needed")
+    need = _norm_workspace(n, spatial, C, groups, prec, 1)
+    ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+    _check(lib().ff_group_norm_act_backward(
+        dy.data_ptr(), lddy, x.data_ptr(), ldx, n, spatial, C, groups, _vector(mean, n * groups, "mean", dev),
+        _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
+        _ACT[act], prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
+        None if ws is None else ws.data_ptr(), max(need, 0), on.ptr), "ff_group_norm_act_backward")
     return out, dgamma, dbeta
 
 
@@ -844,6 +862,7 @@ def dropout_words(rows: int, cols: int) -> int:
     return int(lib().ff_dropout_words(int(rows), int(cols)))
 
 
+@_on_device_of_first
 def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=None):
     """ff_dropout: residual + keep * x / (1 - p) with the mask drawn from the
     counter-based generator at (seed, offset), never stored; its gradient is
@@ -855,27 +874,26 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     if x.dim() < 1:
         raise ValueError("x must have at least one dimension")
     dev = x.device
-    with torch.cuda.device(dev):
-        on = _On(stream, dev)
-        cols = x.shape[-1]
-        rows = x.numel() // cols if cols else 0
-        ldx = _row_stride_of(x, "x")
-        ldr = _like(residual, x, "residual") if residual is not None else 0
-        if out is None:
-            out, ldy = on.empty(x.shape, x.dtype, dev), cols
-        else:
-            ldy = _like(out, x, "out")
-        odev, host = None, 0
-        if isinstance(offset, torch.Tensor):
-            if offset.numel() != 1:
-                raise ValueError("offset must have one element")
-            _same_device(offset, dev, "offset")
-            odev = _ptr(offset, torch.int64, "offset")
-        else:
-            host = int(offset) & 0xFFFFFFFFFFFFFFFF
-        _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
-                                None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
-                                on.ptr), "ff_dropout")
+    on = _On(stream, dev)
+    cols = x.shape[-1]
+    rows = x.numel() // cols if cols else 0
+    ldx = _row_stride_of(x, "x")
+    ldr = _like(residual, x, "residual") if residual is not None else 0
+    if out is None:
+        out, ldy = on.empty(x.shape, x.dtype, dev), cols
+    else:
+        ldy = _like(out, x, "out")
+    odev, host = None, 0
+    if isinstance(offset, torch.Tensor):
+        if offset.numel() != 1:
+            raise ValueError("offset must have one element")
+        _same_device(offset, dev, "offset")
+        odev = _ptr(offset, torch.int64, "offset")
+    else:
+        host = int(offset) & 0xFFFFFFFFFFFFFFFF
+    _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
+                            None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
+                            on.ptr), "ff_dropout")
     return out
 
 
@@ -901,30 +919,32 @@ class Fp8Matrix:
 
 
 def _fp8_new(on, rows, k, tile, dev):
-    q = on.empty((rows, (k + 15) & ~15), torch.float8_e4m3fn, dev)
-    scale = on.empty(((k + 127) // 128, (rows + 127) // 128 if tile else rows), torch.float32, dev)
-    return Fp8Matrix(q, scale, rows, k, tile)
+    m = object.__new__(Fp8Matrix)
+    m.q = on.empty((rows, (k + 15) & ~15), torch.float8_e4m3fn, dev)
+    m.scale = on.empty(((k + 127) // 128, (rows + 127) // 128 if tile else rows), torch.float32, dev)
+    m.rows, m.k, m.tile = rows, k, tile
+    return m
 
 
+@_on_device_of_first
 def _fp8_quantize(x, tile, straight, transposed, stream):
     prec = _prec(x, "x")
     if x.dim() != 2 or x.shape[1] < 1:
         raise ValueError("x must be [rows, k] with k >= 1")
     dev = x.device
-    with torch.cuda.device(dev):
-        on = _On(stream, dev)
-        rows, k = x.shape
-        if max(rows, k) > _INT_MAX:
-            raise ValueError("rows and k must each fit 32 bits")
-        if transposed and rows < 1:
-            raise ValueError("the transpose needs at least one row")
-        ldx = _row_stride_of(x, "x")
-        a = _fp8_new(on, rows, k, tile, dev) if straight else None
-        t = _fp8_new(on, k, rows, tile, dev) if transposed else None
-        _check(lib().ff_fp8_quantize(x.data_ptr(), ldx, rows, k, prec, 1 if tile else 0,
-                                     a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
-                                     t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on.ptr),
-               "ff_fp8_quantize")
+    on = _On(stream, dev)
+    rows, k = x.shape
+    if max(rows, k) > _INT_MAX:
+        raise ValueError("rows and k must each fit 32 bits")
+    if transposed and rows < 1:
+        raise ValueError("the transpose needs at least one row")
+    ldx = _row_stride_of(x, "x")
+    a = _fp8_new(on, rows, k, tile, dev) if straight else None
+    t = _fp8_new(on, k, rows, tile, dev) if transposed else None
+    _check(lib().ff_fp8_quantize(x.data_ptr(), ldx, rows, k, prec, 1 if tile else 0,
+                                 a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
+                                 t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on.ptr),
+           "ff_fp8_quantize")
     return a, t
 
 
@@ -940,6 +960,7 @@ def fp8_quantize_both(x, tile: bool = False, stream=None):
     return _fp8_quantize(x, tile, True, True, stream)
 
 
+@_on_device_of_first
 def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bfloat16, status=None, stream=None):
     """ff_fp8_matmul: act(a b^T + bias) of two Fp8Matrix (a in row blocks).
     Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
@@ -951,22 +972,21 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
         raise ValueError("a must be quantized in row blocks")
     dev = a.q.device
     _same_device(b.q, dev, "b")
-    with torch.cuda.device(dev):
-        on = _On(stream, dev)
-        m, n = a.rows, b.rows
-        if out is None:
-            if out_dtype not in _PREC:
-                raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-            out, ldc = on.empty((m, n), out_dtype, dev), n
-        else:
-            if out.shape != (m, n):
-                raise ValueError("out must be [a.rows, b.rows]")
-            _same_device(out, dev, "out")
-            ldc = _row_stride_of(out, "out")
-        prec = _prec(out, "out")
-        if status is not None:
-            _same_device(status, dev, "status")
-        _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
-                                   n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
-                                   _ptr(status, torch.int32, "status"), on.ptr), "ff_fp8_matmul")
+    on = _On(stream, dev)
+    m, n = a.rows, b.rows
+    if out is None:
+        if out_dtype not in _PREC:
+            raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
+        out, ldc = on.empty((m, n), out_dtype, dev), n
+    else:
+        if out.shape != (m, n):
+            raise ValueError("out must be [a.rows, b.rows]")
+        _same_device(out, dev, "out")
+        ldc = _row_stride_of(out, "out")
+    prec = _prec(out, "out")
+    if status is not None:
+        _same_device(status, dev, "status")
+    _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
+                               n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
+                               _ptr(status, torch.int32, "status"), on.ptr), "ff_fp8_matmul")
     return out
