@@ -16,6 +16,7 @@
 //
 // Groups that fit registers or shared memory may take one of two paths that
 // read x (and dy) once: rows (ff_norm_rows.cu) and blocks (ff_norm_block.cu).
+#include <algorithm>
 #include <cmath>
 
 #include "ff_norm.cuh"
@@ -531,8 +532,9 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   // A few positions of narrow groups would be fetched a fraction of a 32-byte
   // sector at a time: those go to slabs of several groups.
   const bool narrow = s.S > 1 && s.Cg * esize < 32 && s.G > 1;
-  const bool near = (long long)s.S * (s.ldx > s.ldy ? s.ldx : s.ldy) < 0x3FFFFFFF &&
-                    (long long)s.S * s.lddy < 0x3FFFFFFF;  // offsets within a sample fit 32 bits
+  // offsets within a sample fit 32 bits (a lone position has no stride)
+  const long long ld = std::max(std::max(s.ldx, s.ldy), s.lddy);
+  const bool near = s.S == 1 || (ld < 0x3FFFFFFF && s.S * ld < 0x3FFFFFFF);
   const bool rows_fit = gn_rows_fit(s) && near;
   if (rows_fit && !narrow) p.path = ROWS;
   if (p.path == GENERAL) {

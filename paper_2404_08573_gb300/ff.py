@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import inspect
 import os
 from ctypes import POINTER, c_double, c_float, c_int, c_longlong, c_ulonglong, c_void_p
 
@@ -684,48 +685,50 @@ _ACT = {"none": 0, "relu": 1, "silu": 2}
 _INT_MAX = 0x7FFFFFFF
 
 
-class _On:
-    """The stream of an operator call, and the buffers it allocates.  A buffer
-    allocated while another stream is current is marked as used on this one,
-    so that its memory is not handed out again before the call has run."""
+def _on(stream, device):
+    """The stream of an operator call, and what allocates its buffers.  A
+    buffer allocated while another stream is current is marked as used on this
+    one, so that its memory is not handed out again before the call has run."""
+    current = torch._C._cuda_getCurrentRawStream(device.index)
+    if stream is None:
+        return current, torch.empty
+    ptr = _stream(stream)
+    if ptr == current:
+        return current, torch.empty
+    other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(ptr, device)
 
-    __slots__ = ("ptr", "other")
-
-    def __init__(self, stream, device):
-        self.ptr, self.other = torch._C._cuda_getCurrentRawStream(device.index), None
-        if stream is not None:
-            ptr = _stream(stream)
-            if ptr != self.ptr:
-                self.other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(ptr, device)
-                self.ptr = ptr
-
-    def empty(self, shape, dtype, device):
+    def empty(shape, dtype, device):
         t = torch.empty(shape, dtype=dtype, device=device)
-        if self.other is not None:
-            t.record_stream(self.other)
+        t.record_stream(other)
         return t
+
+    return ptr, empty
 
 
 def _on_device_of_first(f):
     """Runs an operator with its first argument's device current (the kernels launch on the current device)."""
 
+    first = next(iter(inspect.signature(f).parameters))
+
     @functools.wraps(f)
     def call(*args, **kwargs):
-        x = args[0] if args else next(iter(kwargs.values()), None)
-        device = x.q.device if type(x) is Fp8Matrix else getattr(x, "device", None)
-        if device is None or device.type != "cuda" or device.index == torch.cuda.current_device():
+        x = args[0] if args else kwargs.get(first)
+        if type(x) is Fp8Matrix:
+            x = x.q
+        if not isinstance(x, torch.Tensor):
+            raise TypeError(f"{first} must be a torch.Tensor" if x is not None else f"{first} is missing")
+        if not x.is_cuda:
+            raise ValueError(f"{first} must be a CUDA tensor")
+        index = x.get_device()
+        if index == torch._C._cuda_getDevice():
             return f(*args, **kwargs)
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             return f(*args, **kwargs)
 
     return call
 
 
 def _prec(x, what):
-    if not isinstance(x, torch.Tensor):
-        raise TypeError(f"{what} must be a torch.Tensor")
-    if not x.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
     prec = _PREC.get(x.dtype)
     if prec is None:
         raise TypeError(f"{what} must be torch.bfloat16 or torch.float32, got {x.dtype}")
@@ -759,10 +762,11 @@ def _row_stride_of(x, what):
 def _vector(t, size, what, device):
     if t is None:
         return None
+    ptr = _ptr(t, torch.float32, what)
     if t.numel() != size:
         raise ValueError(f"{what} must have {size} values")
     _same_device(t, device, what)
-    return _ptr(t, torch.float32, what)
+    return ptr
 
 
 def _same_device(t, device, what):
@@ -809,22 +813,27 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     prec = _prec(x, "x")
     n, spatial, C, groups = _norm_args(x, groups, act)
     dev = x.device
-    on = _On(stream, dev)
+    on, empty = _on(stream, dev)
     ldx = _row_stride_of(x, "x")
     if out is None:
-        out, ldy = on.empty(x.shape, x.dtype, dev), C
+        out, ldy = empty(x.shape, dtype=x.dtype, device=dev), C
     else:
         ldy = _like(out, x, "out")
     if mean is None:
-        mean = on.empty((n, groups), torch.float32, dev)
+        mean = empty((n, groups), dtype=torch.float32, device=dev)
+        pm = mean.data_ptr()
+    else:
+        pm = _vector(mean, n * groups, "mean", dev)
     if rstd is None:
-        rstd = on.empty((n, groups), torch.float32, dev)
+        rstd = empty((n, groups), dtype=torch.float32, device=dev)
+        pr = rstd.data_ptr()
+    else:
+        pr = _vector(rstd, n * groups, "rstd", dev)
     need = _norm_workspace(n, spatial, C, groups, prec, 0)
-    ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+    ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
     _check(lib().ff_group_norm_act(
         x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
-        eps, _ACT[act], prec, out.data_ptr(), ldy, _vector(mean, n * groups, "mean", dev),
-        _vector(rstd, n * groups, "rstd", dev), None if ws is None else ws.data_ptr(), max(need, 0), on.ptr),
+        eps, _ACT[act], prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
         "ff_group_norm_act")
     return out, mean, rstd
 
@@ -837,23 +846,23 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     prec = _prec(x, "x")
     n, spatial, C, groups = _norm_args(x, groups, act)
     dev = x.device
-    on = _On(stream, dev)
+    on, empty = _on(stream, dev)
     ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
     if out is None:
-        out, lddx = on.empty(x.shape, x.dtype, dev), C
+        out, lddx = empty(x.shape, dtype=x.dtype, device=dev), C
     else:
         lddx = _like(out, x, "out")
-    dgamma = on.empty((C,), torch.float32, dev)
-    dbeta = on.empty((C,), torch.float32, dev)
+    dgamma = empty((C,), dtype=torch.float32, device=dev)
+    dbeta = empty((C,), dtype=torch.float32, device=dev)
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward pass are needed")
     need = _norm_workspace(n, spatial, C, groups, prec, 1)
-    ws = on.empty((need,), torch.uint8, dev) if need > 0 else None
+    ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
     _check(lib().ff_group_norm_act_backward(
         dy.data_ptr(), lddy, x.data_ptr(), ldx, n, spatial, C, groups, _vector(mean, n * groups, "mean", dev),
         _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
         _ACT[act], prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
-        None if ws is None else ws.data_ptr(), max(need, 0), on.ptr), "ff_group_norm_act_backward")
+        None if ws is None else ws.data_ptr(), need, on), "ff_group_norm_act_backward")
     return out, dgamma, dbeta
 
 
@@ -874,13 +883,13 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     if x.dim() < 1:
         raise ValueError("x must have at least one dimension")
     dev = x.device
-    on = _On(stream, dev)
+    on, empty = _on(stream, dev)
     cols = x.shape[-1]
     rows = x.numel() // cols if cols else 0
     ldx = _row_stride_of(x, "x")
     ldr = _like(residual, x, "residual") if residual is not None else 0
     if out is None:
-        out, ldy = on.empty(x.shape, x.dtype, dev), cols
+        out, ldy = empty(x.shape, dtype=x.dtype, device=dev), cols
     else:
         ldy = _like(out, x, "out")
     odev, host = None, 0
@@ -893,7 +902,7 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
         host = int(offset) & 0xFFFFFFFFFFFFFFFF
     _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
                             None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
-                            on.ptr), "ff_dropout")
+                            on), "ff_dropout")
     return out
 
 
@@ -918,10 +927,10 @@ class Fp8Matrix:
         return 1 if self.tile else 0
 
 
-def _fp8_new(on, rows, k, tile, dev):
+def _fp8_new(empty, rows, k, tile, dev):
     m = object.__new__(Fp8Matrix)
-    m.q = on.empty((rows, (k + 15) & ~15), torch.float8_e4m3fn, dev)
-    m.scale = on.empty(((k + 127) // 128, (rows + 127) // 128 if tile else rows), torch.float32, dev)
+    m.q = empty((rows, (k + 15) & ~15), dtype=torch.float8_e4m3fn, device=dev)
+    m.scale = empty(((k + 127) // 128, (rows + 127) // 128 if tile else rows), dtype=torch.float32, device=dev)
     m.rows, m.k, m.tile = rows, k, tile
     return m
 
@@ -932,18 +941,18 @@ def _fp8_quantize(x, tile, straight, transposed, stream):
     if x.dim() != 2 or x.shape[1] < 1:
         raise ValueError("x must be [rows, k] with k >= 1")
     dev = x.device
-    on = _On(stream, dev)
+    on, empty = _on(stream, dev)
     rows, k = x.shape
     if max(rows, k) > _INT_MAX:
         raise ValueError("rows and k must each fit 32 bits")
     if transposed and rows < 1:
         raise ValueError("the transpose needs at least one row")
     ldx = _row_stride_of(x, "x")
-    a = _fp8_new(on, rows, k, tile, dev) if straight else None
-    t = _fp8_new(on, k, rows, tile, dev) if transposed else None
+    a = _fp8_new(empty, rows, k, tile, dev) if straight else None
+    t = _fp8_new(empty, k, rows, tile, dev) if transposed else None
     _check(lib().ff_fp8_quantize(x.data_ptr(), ldx, rows, k, prec, 1 if tile else 0,
                                  a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
-                                 t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on.ptr),
+                                 t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on),
            "ff_fp8_quantize")
     return a, t
 
@@ -966,18 +975,20 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
     out's type; bias fp32 [b.rows]; status: a one-element int32 CUDA tensor
     that is OR-ed with 1 if a kernel wait timed out."""
+    if type(a) is not Fp8Matrix or type(b) is not Fp8Matrix:
+        raise TypeError("a and b must be Fp8Matrix")
     if a.k != b.k:
         raise ValueError("a and b must have the same k")
     if a.tile:
         raise ValueError("a must be quantized in row blocks")
     dev = a.q.device
     _same_device(b.q, dev, "b")
-    on = _On(stream, dev)
+    on, empty = _on(stream, dev)
     m, n = a.rows, b.rows
     if out is None:
         if out_dtype not in _PREC:
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-        out, ldc = on.empty((m, n), out_dtype, dev), n
+        out, ldc = empty((m, n), dtype=out_dtype, device=dev), n
     else:
         if out.shape != (m, n):
             raise ValueError("out must be [a.rows, b.rows]")
@@ -988,5 +999,5 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
         _same_device(status, dev, "status")
     _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
                                n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
-                               _ptr(status, torch.int32, "status"), on.ptr), "ff_fp8_matmul")
+                               _ptr(status, torch.int32, "status"), on), "ff_fp8_matmul")
     return out
