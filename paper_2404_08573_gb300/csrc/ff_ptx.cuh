@@ -123,14 +123,6 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Its two halves: work between them overlaps the wait for the others.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-// (without ordering any memory: that the others have started is all it says)
-__device__ __forceinline__ void cluster_arrive_relaxed() {
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // Arrives (release, cluster scope) on the mbarrier at the offset of
 // `local_bar` in the CTA of cluster rank `rank`.
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t* local_bar, uint32_t rank) {
@@ -164,23 +156,6 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
     if (*abort) return false;
     if (globaltimer() - t0 > timeout_ns) return false;
   }
-}
-// Asynchronous stores into the variable at the offset of `local` in the CTA of
-// cluster rank `rank`, counted there (in bytes) by the mbarrier at the offset of
-// `local_bar`: who waits on that barrier sees the values, and the sender orders
-// none of its other memory accesses.
-__device__ __forceinline__ void st_async4(float4* local, uint64_t* local_bar, uint32_t rank, float4 v) {
-  asm volatile(
-      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
-          mapa_shared(smem_u32(local), rank)),
-      "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(mapa_shared(smem_u32(local_bar), rank))
-      : "memory");
-}
-__device__ __forceinline__ void st_async2(float2* local, uint64_t* local_bar, uint32_t rank, float2 v) {
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
-                   mapa_shared(smem_u32(local), rank)),
-               "f"(v.x), "f"(v.y), "r"(mapa_shared(smem_u32(local_bar), rank))
-               : "memory");
 }
 // Stores into the variable at the offset of `local_slot` in the CTA of cluster rank `rank`.
 __device__ __forceinline__ void st_remote_u1(int* local_slot, uint32_t rank, int v) {
