@@ -24,30 +24,47 @@
 namespace ff {
 namespace {
 
+constexpr long long kAlign = 16;
+long long align_up(long long v, long long to = kAlign) { return (v + to - 1) / to * to; }
+
 // ------------------------------------------------------------ general path
 constexpr int kColThreads = 256;
 constexpr int kColVecs = 32;       // at most this many vectors of columns per block
-constexpr int kRowsPerThread = 64; // bounds the rounding of a thread's one-pass sums (see k_gn_colstats)
+// A thread's positions at most: they bound the rounding of its one-pass sums
+// (see k_gn_colstats) and, in the gradient, of its plain ones.
+constexpr int kRowsPerThread = 64, kGradRowsPerThread = 128;
 
 struct ColGeom {
   int CV, TC, TR, ctiles, chunk, chunks;
   int wide;                              // gamma and beta are 16-byte aligned
   FastDiv by_tiles, by_chunks, by_TC, by_Cg, by_G;
 };
-// Blocks of TC vector columns x TR thread rows; `chunk` positions per block,
-// enough blocks to fill the GPU several times where the work allows.
-ColGeom col_geom(const GnShape& s, int V, const float* gamma, const float* beta) {
+// Blocks of TC vector columns x TR thread rows; `chunk` positions per block.
+// The rounds of 4 (gradient: 3) blocks per SM cost what their slowest thread
+// does: its positions and, for constants and the sums' way out, about 6 more.
+// Whole rounds count more than their number (32 x 3136 x 320 bf16, gradient:
+// 2.5 rounds of 29 positions 83 us, 4 whole ones of 19 80 us).
+ColGeom col_geom(const GnShape& s, int V, int esize, bool grad, const float* gamma, const float* beta) {
   ColGeom g;
   g.CV = s.C / V;
-  g.TC = g.CV < kColVecs ? g.CV : kColVecs;
-  g.TR = kColThreads / g.TC;
+  g.ctiles = cdiv(g.CV, kColVecs);
+  // tiles of equal width, whole 32-byte sectors where a row has them
+  g.TC = std::min(g.CV, (int)align_up(cdiv(g.CV, g.ctiles), std::max(1, 32 / (V * esize))));
   g.ctiles = cdiv(g.CV, g.TC);
-  const long long want = 152 * 8;
-  const long long chunks = (want + (long long)s.n * g.ctiles - 1) / ((long long)s.n * g.ctiles);
-  long long chunk = (s.S + chunks - 1) / chunks;
-  const long long lo = (long long)g.TR * 8, hi = (long long)g.TR * kRowsPerThread;
-  chunk = chunk < lo ? lo : chunk > hi ? hi : chunk;
-  g.chunk = (int)(chunk < s.S ? chunk : s.S);
+  g.TR = kColThreads / g.TC;
+  const long long room = 152 * (grad ? 3 : 4), tiles = (long long)s.n * g.ctiles;
+  const int most = grad ? kGradRowsPerThread : kRowsPerThread;
+  long long chunk = std::min<long long>(s.S, (long long)g.TR * most), least = 0;
+  for (int k = 0; k <= 16; ++k) {
+    // k = 0: the largest chunks, where even 16 rounds are too few
+    const long long cut = cdiv(s.S, (int)std::min<long long>(s.S, std::max(1ll, k * room / tiles)));
+    const long long c = k == 0 ? chunk : std::min<long long>(s.S, std::max(cut, g.TR * 8ll));  // (the fold reads every chunk)
+    const int rows = cdiv((int)c, g.TR);
+    if (rows > most) continue;
+    const long long blocks = tiles * cdiv(s.S, (int)c), cost = (blocks + room - 1) / room * (rows + 6);
+    if (least == 0 || cost < least) least = cost, chunk = c;
+  }
+  g.chunk = (int)chunk;
   g.chunks = cdiv(s.S, g.chunk);
   g.wide = ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) & 15) == 0;
   g.by_tiles = FastDiv(g.ctiles);
@@ -169,7 +186,7 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
   }
 }
 
-constexpr int kFoldThreads = 256;
+template <int THREADS>
 __device__ __forceinline__ float block_sum(float v, float* sm) {
   v = warp_sum(v);
   __syncthreads();
@@ -177,50 +194,64 @@ __device__ __forceinline__ float block_sum(float v, float* sm) {
   __syncthreads();
   float t = 0.f;
 #pragma unroll
-  for (int w = 0; w < kFoldThreads / 32; ++w) t += sm[w];
+  for (int w = 0; w < THREADS / 32; ++w) t += sm[w];
   return t;
 }
-// f(partial sums, channel within the group, positions) over the chunks'
-// columns of one group, eight loads in flight.
-template <typename F>
-__device__ __forceinline__ void walk_cells(const float2* p, const GnShape& s, const ColGeom& g, F f) {
-  constexpr int U = 8;
-  const int cells = g.chunks * s.Cg;
-  for (int i0 = threadIdx.x; i0 < cells; i0 += U * kFoldThreads) {
-    float2 q[U];
+// f(partial sums, which of kKept, channel within the group, positions) over the
+// chunks' columns of one group, kKept loads in flight.  The first `kept` of them stay
+// with the thread for a second walk.
+constexpr int kKept = 4;
+template <int THREADS>
+struct Cells {
+  const float2* p;
+  float2 kept[kKept];
+  __device__ __forceinline__ explicit Cells(const float2* p) : p(p) {}
+  template <bool AGAIN, typename F>
+  __device__ __forceinline__ void walk(const GnShape& s, const ColGeom& g, F f) {
+    const int cells = g.chunks * s.Cg;
+    for (int i0 = threadIdx.x; i0 < cells; i0 += kKept * THREADS) {
+      const bool first = i0 == (int)threadIdx.x;
+      float2 q[kKept];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kFoldThreads;
-      const int ch = (int)g.by_Cg.div((uint32_t)i);
-      if (i < cells) q[u] = p[(long long)ch * s.C + (i - ch * s.Cg)];
-    }
+      for (int u = 0; u < kKept; ++u) {
+        const int i = i0 + u * THREADS;
+        const int ch = (int)g.by_Cg.div((uint32_t)i);
+        if (i < cells) q[u] = AGAIN && first ? kept[u] : p[(long long)ch * s.C + (i - ch * s.Cg)];
+        if (!AGAIN && first) kept[u] = q[u];
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kFoldThreads;
-      const int ch = (int)g.by_Cg.div((uint32_t)i);
-      if (i < cells) f(q[u], i - ch * s.Cg, (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
+      for (int u = 0; u < kKept; ++u) {
+        const int i = i0 + u * THREADS;
+        const int ch = (int)g.by_Cg.div((uint32_t)i);
+        if (i < cells) f(q[u], u, i - ch * s.Cg, (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
+      }
     }
   }
-}
+};
+
+// Threads of the folds' blocks, one block per (sample, group): many where
+// blocks are few (4 x 4096 x 130 in one group: 18 us with 128, all in all).
+constexpr int kFoldMany = 512, kFoldFew = 128;
+int fold_threads(const GnShape& s) { return (long long)s.n * s.G < 152 * 4 ? kFoldMany : kFoldFew; }
 
 // One block per (sample, group): the chunks' column statistics to mean and rstd.
-template <typename T>
-__global__ void __launch_bounds__(kFoldThreads) k_gn_fold(const T* x, const float2* part, GnShape s, ColGeom g,
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_gn_fold(const T* x, const float2* part, GnShape s, ColGeom g,
                                                           float* mean_out, float* rstd_out) {
-  __shared__ float sm[kFoldThreads / 32];
+  __shared__ float sm[THREADS / 32];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
-  const float2* p = part + (long long)b * g.chunks * s.C + gr * s.Cg;
+  Cells<THREADS> cells(part + (long long)b * g.chunks * s.C + gr * s.Cg);
   const float total = (float)s.S * (float)s.Cg;
-  float sum = 0.f, M2 = 0.f;
-  walk_cells(p, s, g, [&](float2 q, int, float rows) { sum = fmaf(q.x, rows, sum); });
-  const float mean = block_sum(sum, sm) / total;
-  walk_cells(p, s, g, [&](float2 q, int, float rows) {
+  float sum[kKept] = {}, M2[kKept] = {};  // short sums: less rounding
+  cells.walk<false>(s, g, [&](float2 q, int u, int, float rows) { sum[u] = fmaf(q.x, rows, sum[u]); });
+  const float mean = block_sum<THREADS>((sum[0] + sum[1]) + (sum[2] + sum[3]), sm) / total;
+  cells.walk<true>(s, g, [&](float2 q, int u, int, float rows) {
     const float d = q.x - mean;
-    M2 += fmaf(d * d, rows, q.y);
+    M2[u] += fmaf(d * d, rows, q.y);
   });
-  const float var = block_sum(M2, sm) / total;
+  const float var = block_sum<THREADS>((M2[0] + M2[1]) + (M2[2] + M2[3]), sm) / total;
   if (threadIdx.x == 0) {
     mean_out[blockIdx.x] = group_pivot(x, s, b, gr) + mean;
     rstd_out[blockIdx.x] = 1.f / sqrtf(var + s.eps);
@@ -373,35 +404,16 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
   }
 }
 
-// One block per (sample, group): the averages <gamma du> and <gamma du h>.
-__global__ void __launch_bounds__(kFoldThreads) k_gn_grad_fold(const float2* part, GnShape s, ColGeom g,
-                                                               const float* gamma, float2* avg) {
-  __shared__ float sm[kFoldThreads / 32];
-  ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
-  const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
-  float m1 = 0.f, m2 = 0.f;
-  walk_cells(part + (long long)b * g.chunks * s.C + gr * s.Cg, s, g, [&](float2 q, int c, float) {
-    const float ga = gamma ? __ldg(gamma + gr * s.Cg + c) : 1.f;
-    m1 = fmaf(ga, q.x, m1);
-    m2 = fmaf(ga, q.y, m2);
-  });
-  const float total = (float)s.S * (float)s.Cg;
-  m1 = block_sum(m1, sm);
-  m2 = block_sum(m2, sm);
-  if (threadIdx.x == 0) avg[blockIdx.x] = make_float2(m1 / total, m2 / total);
-}
-
-// dbeta and dgamma: the partial column sums [rows, C] added up, in an order
-// that depends on the sizes only.  Few columns and many row threads per
-// block: the sums are short and latency is what they cost.
-constexpr int kFoldCols = 8, kFoldRows = 64;
-__global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const float2* part, GnFold f, int C,
-                                                                        float* dgamma, float* dbeta) {
-  __shared__ float2 red[kFoldRows][kFoldCols];
-  ptx::griddep_wait();
+// dbeta and dgamma of kFoldCols channels: the partial column sums [rows, C]
+// added up, in an order that depends on the sizes only.  Few columns and many
+// row threads per block: the sums are short and latency is what they cost.
+constexpr int kFoldCols = 8;
+template <int ROWS>
+__device__ __forceinline__ void param_fold(int block, const float2* part, const GnFold& f, int C, float* dgamma,
+                                           float* dbeta) {
+  __shared__ float2 red[ROWS][kFoldCols];
   const int tc = threadIdx.x % kFoldCols, tr = threadIdx.x / kFoldCols;
-  const int c = blockIdx.x * kFoldCols + tc;
+  const int c = block * kFoldCols + tc;
   float2 t = make_float2(0.f, 0.f);
   if (c < C) {
     long long rows = f.rows;
@@ -410,14 +422,14 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
       rows = (first + f.n - 1) / f.units - first / f.units + 1;
     }
 #pragma unroll 8
-    for (long long r = tr; r < rows; r += kFoldRows) {
+    for (long long r = tr; r < rows; r += ROWS) {
       const float2 q = part[r * C + c];
       t.x += q.x;
       t.y += q.y;
     }
   }
   red[tr][tc] = t;
-  for (int half = kFoldRows / 2; half > 0; half /= 2) {
+  for (int half = ROWS / 2; half > 0; half /= 2) {
     __syncthreads();
     if (tr < half) {
       red[tr][tc].x += red[tr + half][tc].x;
@@ -428,6 +440,40 @@ __global__ void __launch_bounds__(kFoldCols * kFoldRows) k_gn_param_fold(const f
     dbeta[c] = red[0][tc].x;
     dgamma[c] = red[0][tc].y;
   }
+}
+constexpr int kParamRows = 64;
+__global__ void __launch_bounds__(kFoldCols * kParamRows) k_gn_param_fold(const float2* part, GnFold f, int C,
+                                                                         float* dgamma, float* dbeta) {
+  ptx::griddep_wait();
+  param_fold<kParamRows>((int)blockIdx.x, part, f, C, dgamma, dbeta);
+}
+
+// One block per (sample, group): the averages <gamma du> and <gamma du h>; the
+// first blocks, where the parameters' gradients are wanted, take those.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_gn_grad_fold(const float2* part, GnShape s, ColGeom g,
+                                                               const float* gamma, float2* avg, int param_blocks,
+                                                               float* dgamma, float* dbeta) {
+  __shared__ float sm[THREADS / 32];
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  if ((int)blockIdx.x < param_blocks) {
+    param_fold<THREADS / kFoldCols>((int)blockIdx.x, part, GnFold{(long long)s.n * g.chunks, 0, 0, 0}, s.C, dgamma,
+                                         dbeta);
+    return;
+  }
+  const int i = (int)blockIdx.x - param_blocks;
+  const int b = (int)g.by_G.div((uint32_t)i), gr = i - b * s.G;
+  float s1[kKept] = {}, s2[kKept] = {};
+  Cells<THREADS>(part + (long long)b * g.chunks * s.C + gr * s.Cg).walk<false>(s, g, [&](float2 q, int u, int c, float) {
+    const float ga = gamma ? __ldg(gamma + gr * s.Cg + c) : 1.f;
+    s1[u] = fmaf(ga, q.x, s1[u]);
+    s2[u] = fmaf(ga, q.y, s2[u]);
+  });
+  const float total = (float)s.S * (float)s.Cg;
+  const float m1 = block_sum<THREADS>((s1[0] + s1[1]) + (s1[2] + s1[3]), sm);
+  const float m2 = block_sum<THREADS>((s2[0] + s2[1]) + (s2[2] + s2[3]), sm);
+  if (threadIdx.x == 0) avg[i] = make_float2(m1 / total, m2 / total);
 }
 
 template <typename T, int V>
@@ -490,8 +536,6 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
 }
 
 // ------------------------------------------------------------------- host
-constexpr long long kAlign = 16;
-long long align_up(long long v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
 bool good_shape(int n, int spatial, int channels, int groups, ff_precision prec) {
   return n >= 0 && spatial >= 0 && channels >= 1 && groups >= 1 && channels % groups == 0 &&
@@ -552,7 +596,7 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
     // the gradient's constants of eight columns would leave an SM 16 warps (32
     // x 4096 x 512 bf16: 153 us, with four 141 us)
     if (grad && p.V > 4) p.V = 4;
-    p.bytes = align_up((long long)s.n * col_geom(s, p.V, nullptr, nullptr).chunks * s.C * (long long)sizeof(float2)) +
+    p.bytes = align_up((long long)s.n * col_geom(s, p.V, esize, grad, nullptr, nullptr).chunks * s.C * (long long)sizeof(float2)) +
               align_up((long long)s.n * s.G * (long long)sizeof(float2));
     return p;
   }
@@ -569,7 +613,7 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
 template <typename T, int V>
 ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
   const GnShape& s = a.s;
-  const ColGeom g = col_geom(s, V, a.gamma, a.beta);
+  const ColGeom g = col_geom(s, V, sizeof(T), false, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   float2* part = static_cast<float2*>(a.ws);
@@ -582,9 +626,10 @@ ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
   const double bytes = (double)s.n * s.S * s.C * sizeof(T);
   PdlLaunch l1(dim3((unsigned)blocks), dim3(kColThreads), st);
   FF_LAUNCH(K_GNORM, bytes, st, cudaLaunchKernelEx(&l1.cfg, k_gn_colstats<T, V>, a.x, s, g, part), "group norm sums");
-  PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(kFoldThreads), st);
+  const int ft = fold_threads(s);
+  PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3((unsigned)ft), st);
   FF_LAUNCH(K_GNORM, 0, st,
-            cudaLaunchKernelEx(&l2.cfg, k_gn_fold<T>, a.x, static_cast<const float2*>(part), s, g, mean, rstd),
+            cudaLaunchKernelEx(&l2.cfg, ft == kFoldMany ? k_gn_fold<T, kFoldMany> : k_gn_fold<T, kFoldFew>, a.x, static_cast<const float2*>(part), s, g, mean, rstd),
             "group norm fold");
   PdlLaunch l3(dim3((unsigned)blocks), dim3(kColThreads), st);
   FF_LAUNCH(K_GNORM, 2 * bytes, st,
@@ -597,7 +642,7 @@ ff_status norm_general(const GnArgs<T>& a, cudaStream_t st) {
 template <typename T, int V>
 ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
   const GnShape& s = a.s;
-  const ColGeom g = col_geom(s, V, a.gamma, a.beta);
+  const ColGeom g = col_geom(s, V, sizeof(T), true, a.gamma, a.beta);
   const long long blocks = (long long)s.n * g.chunks * g.ctiles;
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   float2* part = static_cast<float2*>(a.ws);
@@ -609,21 +654,20 @@ ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
   FF_LAUNCH(K_GNORM_GRAD, 2 * bytes, st,
             cudaLaunchKernelEx(&l1.cfg, k_gn_grad_colsums<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta, part),
             "group norm gradient sums");
-  if (a.dgamma) {
-    const ff_status e = gn_param_fold(part, GnFold{(long long)s.n * g.chunks, 0, 0, 0}, s.C, a.dgamma, a.dbeta, st);
-    if (e != FF_OK) return e;
-  }
-  if (a.out) {
-    PdlLaunch l2(dim3((unsigned)(s.n * s.G)), dim3(kFoldThreads), st);
-    FF_LAUNCH(K_GNORM_GRAD, 0, st,
-              cudaLaunchKernelEx(&l2.cfg, k_gn_grad_fold, static_cast<const float2*>(part), s, g, a.gamma, avg),
-              "group norm gradient fold");
-    PdlLaunch l3(dim3((unsigned)blocks), dim3(kColThreads), st);
-    FF_LAUNCH(K_GNORM_GRAD, 3 * bytes, st,
-              cudaLaunchKernelEx(&l3.cfg, k_gn_grad_apply<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta,
-                                 static_cast<const float2*>(avg), a.out),
-              "group norm gradient apply");
-  }
+  if (!a.out) return gn_param_fold(part, GnFold{(long long)s.n * g.chunks, 0, 0, 0}, s.C, a.dgamma, a.dbeta, st);
+  const int params = a.dgamma ? cdiv(s.C, kFoldCols) : 0;
+  if ((long long)s.n * s.G + params > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+  const int ft = fold_threads(s);
+  PdlLaunch l2(dim3((unsigned)(s.n * s.G + params)), dim3((unsigned)ft), st);
+  FF_LAUNCH(K_GNORM_GRAD, 0, st,
+            cudaLaunchKernelEx(&l2.cfg, ft == kFoldMany ? k_gn_grad_fold<kFoldMany> : k_gn_grad_fold<kFoldFew>, static_cast<const float2*>(part), s, g, a.gamma, avg, params,
+                               a.dgamma, a.dbeta),
+            "group norm gradient fold");
+  PdlLaunch l3(dim3((unsigned)blocks), dim3(kColThreads), st);
+  FF_LAUNCH(K_GNORM_GRAD, 3 * bytes, st,
+            cudaLaunchKernelEx(&l3.cfg, k_gn_grad_apply<T, V>, a.dy, a.x, s, g, mean, rstd, a.gamma, a.beta,
+                               static_cast<const float2*>(avg), a.out),
+            "group norm gradient apply");
   return FF_OK;
 }
 
@@ -678,7 +722,7 @@ bool good_matrix(const void* p, long long ld, long long rows, int C, int esize) 
 }  // namespace
 
 ff_status gn_param_fold(const float2* part, const GnFold& f, int C, float* dgamma, float* dbeta, cudaStream_t st) {
-  PdlLaunch l(dim3((unsigned)cdiv(C, kFoldCols)), dim3(kFoldCols * kFoldRows), st);
+  PdlLaunch l(dim3((unsigned)cdiv(C, kFoldCols)), dim3(kFoldCols * kParamRows), st);
   FF_LAUNCH(K_GNORM_GRAD, 0, st, cudaLaunchKernelEx(&l.cfg, k_gn_param_fold, part, f, C, dgamma, dbeta),
             "group norm parameter gradients");
   return FF_OK;
