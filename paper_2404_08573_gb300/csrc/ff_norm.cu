@@ -94,6 +94,24 @@ struct ColPlace {
   }
 };
 
+// f(which of kFlight positions are there) over a thread's positions: a run of
+// them without conditions, so that their loads fly and their arithmetic
+// overlaps, and what is left one at a time.
+constexpr int kFlight = 4;
+struct HasAll {
+  __device__ constexpr bool operator()(int) const { return true; }
+};
+struct HasSome {
+  int n;
+  __device__ __forceinline__ bool operator()(int u) const { return u < n; }
+};
+template <typename F>
+__device__ __forceinline__ void walk_rows(int r0, int r1, int step, F f) {
+  int r = r0;
+  for (; r + (kFlight - 1) * step < r1; r += kFlight * step) f(HasAll{});
+  if (r < r1) f(HasSome{(r1 - r + step - 1) / step});
+}
+
 template <typename T>
 __device__ __forceinline__ float group_pivot(const T* x, const GnShape& s, int b, int g) {
   float v[1];
@@ -119,30 +137,24 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
   uint64_t np[PV::N], a1[PV::N], a2[PV::N];
 #pragma unroll
   for (int e = 0; e < PV::N; ++e) np[e] = a1[e] = a2[e] = 0;
-  float piv[V], P[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) piv[e] = P[e] = 0.f;
   if (p.on) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) P[e] = group_pivot(x, s, p.b, (int)g.by_Cg.div((uint32_t)(p.col * V + e)));
     const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const long long step = (long long)g.TR * s.ldx;
     if (p.r0 < p.r1) {
-      Vec<T, V>::unpack(Vec<T, V>::load(q), piv);
       float m[V];
+      Vec<T, V>::unpack(Vec<T, V>::load(q), m);
 #pragma unroll
-      for (int e = 0; e < V; ++e) m[e] = -piv[e];
+      for (int e = 0; e < V; ++e) m[e] = -m[e];
       PV::of(m, np);
     }
-    constexpr int U = 4;  // vectors in flight
-    for (int r = p.r0; r < p.r1; r += U * g.TR, q += U * step) {
-      typename Vec<T, V>::Raw raw[U];
+    walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+      typename Vec<T, V>::Raw raw[kFlight];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * g.TR < p.r1) raw[u] = Vec<T, V>::load(q + u * step);
+      for (int u = 0; u < kFlight; ++u)
+        if (has(u)) raw[u] = Vec<T, V>::load(q + u * step);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * g.TR < p.r1) {
+      for (int u = 0; u < kFlight; ++u)
+        if (has(u)) {
           float v[V];
           uint64_t d[PV::N];
           Vec<T, V>::unpack(raw[u], v);
@@ -154,19 +166,22 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
             a2[e] = ptx::fma2(d[e], d[e], a2[e]);
           }
         }
-    }
+      q += kFlight * step;
+    });
   }
   const int rows = p.r1 - p.ch * g.chunk;
   // thread row t has rows / TR positions, one more below the remainder
   const int lo = rows / g.TR, rem = rows - lo * g.TR, m = lo + (p.tr < rem ? 1 : 0);
-  float s1[V], s2[V];
+  float s1[V], s2[V], minus[V];
   PV::to(a1, s1);
   PV::to(a2, s2);
+  PV::to(np, minus);
   const float inv = m > 0 ? 1.f / (float)m : 0.f;
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     const float dm = s1[e] * inv;
-    red[threadIdx.x * V + e] = make_float2((piv[e] - P[e]) + dm, s2[e] - s1[e] * dm);
+    const float P = p.on ? group_pivot(x, s, p.b, (int)g.by_Cg.div((uint32_t)(p.col * V + e))) : 0.f;
+    red[threadIdx.x * V + e] = make_float2((-minus[e] - P) + dm, s2[e] - s1[e] * dm);
   }
   __syncthreads();
   // one thread per channel: the thread rows together
@@ -282,15 +297,14 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
   const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
   T* o = y + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, so = (long long)g.TR * s.ldy;
-  constexpr int U = 4;  // vectors in flight
-  for (int r = p.r0; r < p.r1; r += U * g.TR) {
-    typename Vec<T, V>::Raw raw[U];
+  walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+    typename Vec<T, V>::Raw raw[kFlight];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (r + u * g.TR < p.r1) raw[u] = Vec<T, V>::load(q + u * sx);
+    for (int u = 0; u < kFlight; ++u)
+      if (has(u)) raw[u] = Vec<T, V>::load(q + u * sx);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (r + u * g.TR < p.r1) {
+    for (int u = 0; u < kFlight; ++u)
+      if (has(u)) {
         float v[V];
         uint64_t d[PV::N];
         Vec<T, V>::unpack(raw[u], v);
@@ -301,9 +315,9 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
         PV::to(d, v);
         Vec<T, V>::store(o + u * so, v);
       }
-    q += U * sx;
-    o += U * so;
-  }
+    q += kFlight * sx;
+    o += kFlight * so;
+  });
 }
 
 // What the gradient's passes share: a column's constants.  h = x rs + o,
@@ -358,18 +372,17 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
     const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
     const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy;
-    constexpr int U = 4;  // positions in flight
-    for (int r = p.r0; r < p.r1; r += U * g.TR) {
-      typename Vec<T, V>::Raw rx[U], rd[U];
+    walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+      typename Vec<T, V>::Raw rx[kFlight], rd[kFlight];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * g.TR < p.r1) {
+      for (int u = 0; u < kFlight; ++u)
+        if (has(u)) {
           rx[u] = Vec<T, V>::load(qx + u * sx);
           rd[u] = Vec<T, V>::load(qd + u * sd);
         }
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (r + u * g.TR < p.r1) {
+      for (int u = 0; u < kFlight; ++u)
+        if (has(u)) {
           float v[V], w[V];
           uint64_t h[PV::N], d[PV::N];
           Vec<T, V>::unpack(rx[u], v);
@@ -383,9 +396,9 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
             p1[e] = ptx::fma2(d[e], h[e], p1[e]);
           }
         }
-      qx += U * sx;
-      qd += U * sd;
-    }
+      qx += kFlight * sx;
+      qd += kFlight * sd;
+    });
   }
   float s0[V], s1[V];
   PV::to(p0, s0);
@@ -505,18 +518,17 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
   const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
   T* o = dx + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy, so = (long long)g.TR * s.ldy;
-  constexpr int U = 4;  // positions in flight
-  for (int r = p.r0; r < p.r1; r += U * g.TR) {
-    typename Vec<T, V>::Raw rx[U], rd[U];
+  walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+    typename Vec<T, V>::Raw rx[kFlight], rd[kFlight];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (r + u * g.TR < p.r1) {
+    for (int u = 0; u < kFlight; ++u)
+      if (has(u)) {
         rx[u] = Vec<T, V>::load(qx + u * sx);
         rd[u] = Vec<T, V>::load(qd + u * sd);
       }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (r + u * g.TR < p.r1) {
+    for (int u = 0; u < kFlight; ++u)
+      if (has(u)) {
         float v[V], w[V];
         uint64_t h[PV::N], d[PV::N];
         Vec<T, V>::unpack(rx[u], v);
@@ -529,10 +541,10 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
         PV::to(h, v);
         Vec<T, V>::store(o + u * so, v);
       }
-    qx += U * sx;
-    qd += U * sd;
-    o += U * so;
-  }
+    qx += kFlight * sx;
+    qd += kFlight * sd;
+    o += kFlight * so;
+  });
 }
 
 // ------------------------------------------------------------------- host
