@@ -578,6 +578,19 @@ struct Plan {
 // v: the widest access that the rows' alignment allows.  Within the two
 // register paths a vector must lie in one group; they have accesses of 16
 // bytes, of 4 (bf16) and of one value.
+// Estimated time of the column passes (us).  They read x (and dy) twice, at
+// about 5.7 TB/s in all where a thread has many positions, and take 5 or 6 us
+// beside; constants and the sums' way out cost as much as a few positions.
+// (1000 x 64 x 128 bf16, 4 positions: 26 us, block path 13; 64 x 784 x 256, 11:
+// 21 and 16; its gradient, 33: 31 and 38.)
+double general_us(const GnShape& s, int V, int esize, bool grad) {
+  const ColGeom g = col_geom(s, V, esize, grad, nullptr, nullptr);
+  const double bytes = (double)s.n * s.S * s.C * esize, rows = cdiv(g.chunk, g.TR);
+  const double more = esize == 2 ? (grad ? 3.5 : 4.5) : (grad ? 1.5 : 2.0);
+  const double us = grad ? 6.0 + 5 * bytes / 5.6e6 : 5.0 + 3 * bytes / 5.8e6;
+  return us * (1.0 + more / rows) * (V == 1 ? 1.3 : 1.0);
+}
+
 Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   Plan p{GENERAL, v, {}, 0};
 
@@ -594,12 +607,8 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   const bool rows_fit = gn_rows_fit(s) && near;
   if (rows_fit && !narrow) p.path = ROWS;
   if (p.path == GENERAL) {
-    // The column passes read x (and dy) twice, at about 5.3 TB/s in all, and
-    // take 8 to 10 us beside; the block path reads once but runs at 3.
-    const double bytes = (double)s.n * s.S * s.C * esize;
-    const double general = grad ? 10.0 + 5 * bytes / 5.0e6 : 8.0 + 3 * bytes / 5.3e6;
     p.block = gn_block_plan(s, V, esize, grad);
-    if (p.block.T > 0 && p.block.us <= general)
+    if (p.block.T > 0 && p.block.us <= general_us(s, grad && v > 4 ? 4 : v, esize, grad))
       p.path = BLOCK;
     else if (rows_fit)
       p.path = ROWS;
