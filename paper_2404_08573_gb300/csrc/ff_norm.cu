@@ -591,7 +591,7 @@ double general_us(const GnShape& s, int V, int esize, bool grad) {
   return us * (1.0 + more / rows) * (V == 1 ? 1.3 : 1.0);
 }
 
-Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
+Plan make_plan(const GnShape& s, int esize, int v, bool grad, bool near) {
   Plan p{GENERAL, v, {}, 0};
 
   const int wide = 16 / esize;
@@ -601,9 +601,6 @@ Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
   // A few positions of narrow groups would be fetched a fraction of a 32-byte
   // sector at a time: those go to slabs of several groups.
   const bool narrow = s.S > 1 && s.Cg * esize < 32 && s.G > 1;
-  // offsets within a sample fit 32 bits (a lone position has no stride)
-  const long long ld = std::max(std::max(s.ldx, s.ldy), s.lddy);
-  const bool near = s.S == 1 || (ld < 0x3FFFFFFF && s.S * ld < 0x3FFFFFFF);
   const bool rows_fit = gn_rows_fit(s) && near;
   if (rows_fit && !narrow) p.path = ROWS;
   if (p.path == GENERAL) {
@@ -695,6 +692,26 @@ ff_status grad_general(const GnArgs<T>& a, cudaStream_t st) {
 template <typename T, int V>
 ff_status general(const GnArgs<T>& a, bool grad, cudaStream_t st) {
   return grad ? grad_general<T, V>(a, st) : norm_general<T, V>(a, st);
+}
+
+// The plan of a call.  It follows from sizes, type, alignment and whether
+// offsets within a sample fit 32 bits (a lone position has no stride); making
+// one takes a microsecond or more, so each thread keeps the last ones.
+Plan plan_of(const GnShape& s, int esize, int v, bool grad) {
+  struct Entry {
+    int n = -1, S, C, G, kind;
+    Plan plan;
+  };
+  thread_local Entry kept[64];
+  const long long ld = std::max(std::max(s.ldx, s.ldy), s.lddy);
+  const bool near = s.S == 1 || (ld < 0x3FFFFFFF && s.S * ld < 0x3FFFFFFF);
+  const int kind = ((esize * 16 + v) * 2 + grad) * 2 + near;
+  uint32_t h = (uint32_t)s.n;
+  for (const int part : {s.S, s.C, s.G, kind}) h = h * 0x9E3779B1u + (uint32_t)part;
+  Entry& e = kept[(h * 0x9E3779B1u) >> 26];
+  if (e.n != s.n || e.S != s.S || e.C != s.C || e.G != s.G || e.kind != kind)
+    e = Entry{s.n, s.S, s.C, s.G, kind, make_plan(s, esize, v, grad, near)};
+  return e.plan;
 }
 
 // The workspace of the path that needs most among those that some stride or
