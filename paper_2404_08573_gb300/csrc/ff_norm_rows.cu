@@ -5,9 +5,11 @@
 // A warp (or block) walks over the samples with its groups fixed, so gamma, beta
 // and the gradient's sums over the samples stay in registers; the next
 // sample's values are loaded under the arithmetic of this one.  Mean and
-// centred sum of squares are two passes over registers.  Bound by HBM where the
-// groups are wide (8192 x 4096, 32 groups, bf16); rows of narrow or odd groups
-// (2000 in 16 groups of 125: one value per access) by instructions.
+// centred sum of squares are two passes over registers.  Bound by the
+// instructions: with silu a value takes about 12 forward and 25 in the
+// gradient, and odd groups are read a value at a time (8192 x 4096 in 32
+// groups, bf16, silu: 40 us, 3.4 TB/s, gradient 60 us; 2048 x 2000 in 16 groups
+// of 125, fp32, relu: 11 and 19 us).
 #include <algorithm>
 
 #include "ff_norm.cuh"
