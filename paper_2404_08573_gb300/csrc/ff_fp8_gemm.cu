@@ -31,6 +31,7 @@ namespace {
 
 constexpr int KB = 128;  // contraction indices (and bytes) per block and per ring stage
 constexpr int BM = 128;  // rows of an accumulator: the TMEM lanes
+static_assert(KB % 16 == 0, "every tiled copy starts a multiple of KB bytes (C: of 128) into its row");
 constexpr int EPI = 8;   // epilogue warps
 constexpr int THREADS = 64 + 32 * EPI;
 

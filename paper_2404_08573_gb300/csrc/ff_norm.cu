@@ -122,19 +122,21 @@ __device__ __forceinline__ void walk_rows(int r0, int r1, int step, F f) {
 
 template <typename T>
 __device__ __forceinline__ float group_pivot(const T* x, const GnShape& s, int b, int g) {
-  float v[1];
-  Vec<T, 1>::unpack(Vec<T, 1>::load(x + (long long)b * s.S * s.ldx + (long long)g * s.Cg), v);
-  return v[0];
+  const T* p = x + (long long)b * s.S * s.ldx + (long long)g * s.Cg;
+  float v[1], w[1];
+  Vec<T, 1>::unpack(Vec<T, 1>::load(p), v);
+  Vec<T, 1>::unpack(Vec<T, 1>::load(p + second_of(s)), w);
+  return pivot_of(v[0], w[0]);
 }
 
 // Column (mean - P, centred sum of squares) over a chunk of a sample's
-// positions, P being the first value of the column's group: what is combined
-// later are differences of means, and those keep their bits when the means
-// are large beside the spread only if they are held relative to a value
-// nearby.  A thread sums x - p and (x - p)^2 with p its own first value: p
-// belongs to the data, so it is off the mean by at most the root of the total
-// it measures, and over at most 64 rows the difference loses at most 64
-// rounding units of that total.
+// positions, P being the pivot of the column's group: what is combined later
+// are differences of means, and those keep their bits when the means are
+// large beside the spread only if they are held relative to a value nearby.  A
+// thread sums x - p and (x - p)^2 with p its own first value: p belongs to the
+// data, so it is off the mean by at most the root of the total it measures,
+// and over at most 64 rows the difference loses at most 64 rounding units of
+// that total.
 template <typename T, int V>
 __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnShape s, ColGeom g, float2* part) {
   using PV = Pairs<V>;

@@ -72,6 +72,16 @@ struct FastDiv {
   __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, mul) + n) >> s; }
 };
 
+// What a group's sums are held relative to, from its first two values: the
+// first where it is large beside their distance, so that a large mean costs
+// the small spread no bits; else zero, since a mean near zero would come out
+// as the difference of two numbers of the spread's size.
+__device__ __forceinline__ float pivot_of(float first, float second) {
+  return fabsf(first) >= 16.f * fabsf(second - first) ? first : 0.f;
+}
+// How far a group's second value lies from its first.
+__device__ __forceinline__ long long second_of(const GnShape& s) { return s.Cg > 1 ? 1 : s.S > 1 ? s.ldx : 0; }
+
 __device__ __forceinline__ uint64_t both(float v) { return ptx::pack2(v, v); }
 // 1 / (1 + e^-u) of a pair, with the approximate exponential and one
 // approximate reciprocal for both: with a = 1 + e^-u and r = 1 / (a b), 1 / a is
@@ -87,7 +97,7 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
   const uint64_t a = ptx::add2(ptx::pack2(x, y), both(1.f));
   const float2 f = ptx::unpack2(a);
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(f.x * f.y));
-  return ptx::mul2(ptx::pack2(f.y, f.x), both(r));
+  return ptx::pack2(f.y * r, f.x * r);
 }
 __device__ __forceinline__ float max0(float u) {  // max(u, 0), NaN kept
   float r;
@@ -161,22 +171,6 @@ __device__ __forceinline__ void act_grad_pairs(uint64_t (&d)[Pairs<V>::N], const
       d[i] = ptx::pack2(v.x > 0.f ? t.x : 0.f, v.y > 0.f ? t.y : 0.f);
     }
   }
-}
-// The same over plain arrays.
-template <int V>
-__device__ __forceinline__ void act_values(float (&u)[V], int act) {
-  uint64_t p[Pairs<V>::N];
-  Pairs<V>::of(u, p);
-  act_pairs<V>(p, act);
-  Pairs<V>::to(p, u);
-}
-template <int V>
-__device__ __forceinline__ void act_grad_values(float (&d)[V], const float (&u)[V], int act) {
-  uint64_t p[Pairs<V>::N], q[Pairs<V>::N];
-  Pairs<V>::of(d, p);
-  Pairs<V>::of(u, q);
-  act_grad_pairs<V>(p, q, act);
-  Pairs<V>::to(p, d);
 }
 
 // V parameters from index c (a multiple of V), or `none` everywhere; wide: p

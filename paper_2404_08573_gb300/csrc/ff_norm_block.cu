@@ -6,8 +6,8 @@
 // unit's values are copied (cp.async) under the arithmetic of this one.  A
 // thread has one vector column of the slab and every TR-th position, and reads
 // only what it copied itself.  Its sums go through shared memory to a few
-// lanes per group and back.  Sums of x are held relative to the group's first
-// value, as in ff_norm.cu.
+// lanes per group and back.  Sums of x are held relative to the group's pivot,
+// as in ff_norm.cu.
 //
 // Bound by the instructions: with silu a value of bf16 takes about 12 forward,
 // and a unit some 200 per thread beside, so 64 x 784 x 256 (32 groups) runs in
@@ -114,14 +114,15 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
   ptx::griddep_launch_dependents();
   Cursor cur(u0, s, q), ahead = cur;
   const long long xstep = (long long)q.TR * s.ldx, ystep = (long long)q.TR * s.ldy;
-  float pivot = 0.f;  // the next unit's group's first value
+  float pivot = 0.f;  // the next unit's group's
   auto start = [&](int u, int k) {
     if (u < u1) {
       fetch<T, V>(stages + k * stage, a.x + ahead.offset(s, q, p, s.ldx), xstep, p.mine, q.T);
-      float v[1];
-      Vec<T, 1>::unpack(
-          Vec<T, 1>::load(a.x + (long long)ahead.b * s.S * s.ldx + (ahead.slab * q.GS + p.gl) * s.Cg), v);
-      pivot = v[0];
+      const T* head = a.x + (long long)ahead.b * s.S * s.ldx + (ahead.slab * q.GS + p.gl) * s.Cg;
+      float v[1], w[1];
+      Vec<T, 1>::unpack(Vec<T, 1>::load(head), v);
+      Vec<T, 1>::unpack(Vec<T, 1>::load(head + second_of(s)), w);
+      pivot = pivot_of(v[0], w[0]);
       ahead.next(s);
     }
     ptx::cp_async_commit();

@@ -6,10 +6,10 @@
 // and the gradient's sums over the samples stay in registers; the next
 // sample's values are loaded under the arithmetic of this one.  Mean and
 // centred sum of squares are two passes over registers.  Bound by the
-// instructions: with silu a value takes about 12 forward and 25 in the
-// gradient, and odd groups are read a value at a time (8192 x 4096 in 32
-// groups, bf16, silu: 40 us, 3.4 TB/s, gradient 60 us; 2048 x 2000 in 16 groups
-// of 125, fp32, relu: 11 and 19 us).
+// instructions: with silu some 30 a value forward, much of it the sums'
+// shuffles, and odd groups are read a value at a time (8192 x 4096 in 32
+// groups, silu: bf16 36 us, 3.8 TB/s, gradient 54 us; fp32 48 us, 5.6 TB/s,
+// and 88 us; 2048 x 2000 in 16 groups of 125, fp32: 11 and 16 us).
 #include <algorithm>
 
 #include "ff_norm.cuh"
@@ -102,16 +102,31 @@ struct Walk {
   }
 };
 
-// gamma and beta of a lane's vectors.
+// gamma and beta of a lane's vectors, its values in pairs.
 template <int V, int NV, typename S, typename T>
-__device__ __forceinline__ void params(float (&ga)[NV][V], float (&be)[NV][V], const GnArgs<T>& a, const S& sl, int c0) {
+__device__ __forceinline__ void params(uint64_t (&ga)[NV * V / 2], uint64_t (&be)[NV * V / 2], const GnArgs<T>& a,
+                                       const S& sl, int c0) {
+  float g[NV * V], o[NV * V];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      ga[i][e] = a.gamma && sl.on(i) ? __ldg(a.gamma + c0 + sl.ch(i) + e) : 1.f;
-      be[i][e] = a.beta && sl.on(i) ? __ldg(a.beta + c0 + sl.ch(i) + e) : 0.f;
+      g[i * V + e] = a.gamma && sl.on(i) ? __ldg(a.gamma + c0 + sl.ch(i) + e) : 1.f;
+      o[i * V + e] = a.beta && sl.on(i) ? __ldg(a.beta + c0 + sl.ch(i) + e) : 0.f;
     }
+  Pairs<NV * V>::of(g, ga);
+  Pairs<NV * V>::of(o, be);
+}
+template <typename T, int V, int NV>
+__device__ __forceinline__ void to_pairs(const typename Vec<T, V>::Raw (&r)[NV], uint64_t (&p)[NV * V / 2]) {
+  float f[NV * V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) Vec<T, V>::unpack(r[i], reinterpret_cast<float(&)[V]>(f[i * V]));
+  Pairs<NV * V>::of(f, p);
+}
+__device__ __forceinline__ float both_of(uint64_t p) {
+  const float2 f = ptx::unpack2(p);
+  return f.x + f.y;
 }
 
 template <typename T, int V, int NV, bool ONE, bool WIDE>
@@ -125,7 +140,8 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps) k_gn_rows(G
   const int c0 = w.active ? w.g * s.Cg : 0;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  float ga[NV][V], be[NV][V];
+  constexpr int N = NV * V / 2;
+  uint64_t ga[N], be[N];
   params<V, NV>(ga, be, a, sl, c0);
   const float inv = 1.f / ((float)s.S * (float)s.Cg);
   // vectors that do not exist stay zero: the activation is formed on pairs,
@@ -145,37 +161,31 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps) k_gn_rows(G
   if (b < s.n) load(cur);
   for (; b < s.n; b += w.step) {
     if (s.n - b > w.step) load(nxt);
-    float sum = 0.f;
+    uint64_t d[N], t = 0;
+    to_pairs<T, V, NV>(cur, d);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v[V];
-      VV::unpack(cur[i], v);
+    for (int i = 0; i < N; ++i) t = ptx::add2(t, d[i]);  // zero where there is no vector
+    const float mean = add(both_of(t)) * inv;
+    const uint64_t minus = both(-mean);
+    t = 0;
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum += v[e];  // zero where there is no vector
+    for (int i = 0; i < N; ++i) {
+      d[i] = ptx::add2(d[i], minus);
+      if constexpr (V == 1) {
+        const float2 f = ptx::unpack2(d[i]);
+        d[i] = ptx::pack2(sl.on(2 * i) ? f.x : 0.f, sl.on(2 * i + 1) ? f.y : 0.f);
+        t = ptx::fma2(d[i], d[i], t);
+      } else if (sl.on(2 * i / V)) {
+        t = ptx::fma2(d[i], d[i], t);
+      }
     }
-    const float mean = add(sum) * inv;
-    float sq = 0.f;
+    const float rstd = rsqrtf(add(both_of(t)) * inv + s.eps);
+    const uint64_t r2 = both(rstd);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v[V];
-      VV::unpack(cur[i], v);
-      if (sl.on(i))
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float d = v[e] - mean;
-          sq = fmaf(d, d, sq);
-        }
-    }
-    const float rstd = rsqrtf(add(sq) * inv + s.eps);
+    for (int i = 0; i < N; ++i) d[i] = ptx::fma2(ptx::mul2(d[i], r2), ga[i], be[i]);
+    act_pairs<NV * V>(d, s.act);
     float y[NV * V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      float v[V];
-      VV::unpack(cur[i], v);
-#pragma unroll
-      for (int e = 0; e < V; ++e) y[i * V + e] = fmaf((v[e] - mean) * rstd, ga[i][e], be[i][e]);
-    }
-    act_values<NV * V>(y, s.act);
+    Pairs<NV * V>::to(d, y);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (sl.on(i)) VV::store(q + sl.at(i, ldy), reinterpret_cast<const float(&)[V]>(y[i * V]));
@@ -204,12 +214,11 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
   const int c0 = w.active ? w.g * s.Cg : 0;
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  float ga[NV][V], be[NV][V], p0[NV][V], p1[NV][V];
+  constexpr int N = NV * V / 2;
+  uint64_t ga[N], be[N], p0[N], p1[N];
   params<V, NV>(ga, be, a, sl, c0);
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-#pragma unroll
-    for (int e = 0; e < V; ++e) p0[i][e] = p1[i][e] = 0.f;
+  for (int i = 0; i < N; ++i) p0[i] = p1[i] = 0;
   const float inv = 1.f / ((float)s.S * (float)s.Cg);
   typename VV::Raw cx[NV] = {}, cy[NV] = {}, nx[NV] = {}, ny[NV] = {};
   const int ldx = (int)s.ldx, lddy = (int)s.lddy, ldo = (int)s.ldy;  // within a sample (near, see plan_of)
@@ -237,47 +246,39 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
   if (b < s.n) load(cx, cy, b, mu, rs);
   for (; b < s.n; b += w.step) {
     if (s.n - b > w.step) load(nx, ny, b + w.step, nmu, nrs);
-    // a vector that does not exist has h = 0 and du = 0
-    float h[NV * V], d[NV * V], m1 = 0.f, m2 = 0.f;
+    // a vector that does not exist has du = 0
+    uint64_t h[N], d[N], t1 = 0, t2 = 0;
     {
-      float u[NV * V];
+      uint64_t u[N];
+      const uint64_t minus = both(-mu), r2 = both(rs);
+      to_pairs<T, V, NV>(cx, h);
+      to_pairs<T, V, NV>(cy, d);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float x[V], t[V];
-        VV::unpack(cx[i], x);
-        VV::unpack(cy[i], t);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int j = i * V + e;
-          h[j] = sl.on(i) ? (x[e] - mu) * rs : 0.f;
-          d[j] = t[e];
-          u[j] = fmaf(ga[i][e], h[j], be[i][e]);
-        }
+      for (int i = 0; i < N; ++i) {
+        h[i] = ptx::mul2(ptx::add2(h[i], minus), r2);
+        u[i] = ptx::fma2(ga[i], h[i], be[i]);
       }
-      act_grad_values<NV * V>(d, u, s.act);
+      act_grad_pairs<NV * V>(d, u, s.act);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int j = i * V + e;
-        p0[i][e] += d[j];
-        p1[i][e] = fmaf(d[j], h[j], p1[i][e]);
-        d[j] *= ga[i][e];
-        m1 += d[j];
-        m2 = fmaf(d[j], h[j], m2);
-      }
+    for (int i = 0; i < N; ++i) {
+      p0[i] = ptx::add2(p0[i], d[i]);
+      p1[i] = ptx::fma2(d[i], h[i], p1[i]);
+      d[i] = ptx::mul2(d[i], ga[i]);
+      t1 = ptx::add2(t1, d[i]);
+      t2 = ptx::fma2(d[i], h[i], t2);
+    }
     if (a.out) {
-      m1 = add(m1) * inv;
-      m2 = add(m2) * inv;
+      const float m1 = add(both_of(t1)) * inv, m2 = add(both_of(t2)) * inv;
+      // dx = rs (gamma du - <.> - h <.>)
+      const uint64_t r2 = both(rs), c1 = both(-rs * m1), c2 = both(-rs * m2);
+      float v[NV * V];
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = ptx::fma2(d[i], r2, ptx::fma2(h[i], c2, c1));
+      Pairs<NV * V>::to(d, v);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (sl.on(i)) {
-          float v[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = rs * (d[i * V + e] - m1 - h[i * V + e] * m2);
-          VV::store(q + sl.at(i, ldo), v);
-        }
+        if (sl.on(i)) VV::store(q + sl.at(i, ldo), reinterpret_cast<const float(&)[V]>(v[i * V]));
       q += so;
     }
 #pragma unroll
@@ -289,18 +290,19 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
     rs = nrs;
   }
   if (!part) return;
+  float s0[NV * V], s1[NV * V];
+  Pairs<NV * V>::to(p0, s0);
+  Pairs<NV * V>::to(p1, s1);
   if constexpr (WIDE) {  // one position, and every thread has its channels alone
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (sl.on(i))
 #pragma unroll
         for (int e = 0; e < V; ++e)
-          part[(long long)w.p * s.C + c0 + sl.ch(i) + e] = make_float2(p0[i][e], p1[i][e]);
+          part[(long long)w.p * s.C + c0 + sl.ch(i) + e] = make_float2(s0[i * V + e], s1[i * V + e]);
   } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) red[threadIdx.x >> 5][i * V + e][threadIdx.x & 31] = make_float2(p0[i][e], p1[i][e]);
+    for (int i = 0; i < NV * V; ++i) red[threadIdx.x >> 5][i][threadIdx.x & 31] = make_float2(s0[i], s1[i]);
     __syncthreads();
     const int per = s.Cg / V, total = s.S * per;
     for (int i = threadIdx.x; i < NV * V * 32; i += 32 * kWarps) {
@@ -346,8 +348,12 @@ ff_status run(const GnArgs<T>& a, const GnRowsPlan& pl, bool grad, cudaStream_t 
 // 8192 of a single one.
 bool gn_rows_fit(const GnShape& s) { return (long long)s.S * s.Cg <= (s.S == 1 ? 16 * kMostThreads : 512); }
 
-// Lanes per group: down to one vector each in narrow groups, up to 16 values
-// each in wide ones.
+// Lanes per group: from four on as few as leave each 8 values where they come
+// in vectors (the sums' shuffles are shared by more of them: 8192 x 4096 in 32
+// groups, fp32, 69 us with 4 values each, 48 with 8; 3000 x 3200 in 32 groups,
+// bf16, 20 with up to 4, 17 with 8), as many as there are values, up to a warp,
+// where they do not (2048 x 2000 in 16 groups, fp32, gradient: 16 us, with 8
+// each 18).
 GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad) {
   GnRowsPlan p;
   const int vecs = s.S * s.Cg / V;
@@ -359,7 +365,8 @@ GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad) {
     p.sets = s.G;
   } else {
     p.lanes = 1;
-    while (p.lanes < 32 && p.lanes < vecs) p.lanes *= 2;
+    const int each = V > 1 ? 8 / V : 1;  // vectors
+    while (p.lanes < 32 && p.lanes < vecs && (p.lanes < 4 || p.lanes * each < vecs)) p.lanes *= 2;
     per = 32 / p.lanes;
     p.sets = cdiv(s.G, per);
     rows = kWarps;

@@ -762,11 +762,13 @@ def _row_stride_of(x, what):
 def _vector(t, size, what, device):
     if t is None:
         return None
-    ptr = _ptr(t, torch.float32, what)
-    if t.numel() != size:
-        raise ValueError(f"{what} must have {size} values")
-    _same_device(t, device, what)
-    return ptr
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.device == device and t.numel() == size
+            and t.is_contiguous()):
+        _ptr(t, torch.float32, what)  # says what is wrong with the tensor itself
+        if t.numel() != size:
+            raise ValueError(f"{what} must have {size} values")
+        _same_device(t, device, what)
+    return t.data_ptr()
 
 
 def _same_device(t, device, what):

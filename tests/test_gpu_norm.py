@@ -271,6 +271,26 @@ def test_refusals():
         ff.group_norm_act_backward(y, x, None, None, None, None, 3)
 
 
+def test_a_mean_near_zero_keeps_its_bits():
+    """Groups of zero mean whose first value is three spreads off: the mean must
+    not come out as a difference of numbers of that size.  A group's mean is
+    averaged from more than 10,000 threads' means of up to 64 values, each off
+    by a few rounding units of the spread and independent of the others, so it
+    is a few hundredths of a unit off; half a unit is asked for.  Held relative
+    to the first value, the sum's own rounding alone is one to three."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    gen = torch.Generator().manual_seed(5)
+    n, S, C, G = 2, 9000, 64, 4
+    x = torch.randn(n, S, C, generator=gen)
+    x -= x.reshape(n, S, G, C // G).mean(dim=(1, 3)).repeat_interleave(C // G, dim=1)[:, None, :]
+    x[:, 0, ::C // G], x[:, 0, 1::C // G] = 3.0, -1.0
+    _, m, _ = ff.group_norm_act(x.cuda(), None, None, G, act="none")
+    x64 = x.double().reshape(n, S, G, C // G)
+    mean, size = x64.mean(dim=(1, 3)), x64.abs().mean(dim=(1, 3))
+    assert torch.all((m.double().cpu() - mean).abs() <= 0.5 * U * size)
+
+
 @pytest.mark.parametrize("shape", [(2, 100, 8, 2), (16, 1, 500, 10), (4, 50000, 8, 2)])
 def test_a_short_workspace_is_refused(shape):
     """Less than the size query's answer is refused for every stride and
