@@ -10,7 +10,8 @@
 // as in ff_norm.cu.
 //
 // Bound by the instructions: with silu a value of bf16 takes about 12 forward,
-// and a unit some 200 per thread beside, so 64 x 784 x 256 (32 groups) runs in
+// and a unit some 450 per thread beside (256 x 49 x 1024, 32 groups: 21 us with
+// 4 vectors a thread, 16 with 7), so 64 x 784 x 256 (32 groups) runs in
 // 16 us, 3.2 TB/s; fp32 moves twice the bytes for them (512 x 196 x 256 in 16
 // groups: 40 us, 5.1 TB/s, gradient 65 us, 4.8 TB/s).  Splitting a slab's
 // positions over a cluster of 2 to 8 blocks, with the sums exchanged through
@@ -498,7 +499,7 @@ GnBlockPlan gn_block_plan(const GnShape& s, int V, int esize, bool grad) {
       if (units > 0x3FFFFFFF) continue;
       const long long room = 152ll * per_sm, rounds = (units + room - 1) / room;
       const double warps = per_sm * T / 32.0, issue = std::max(6.0, warps / 4.0) / 1900.0;
-      const double round = 0.6 + (200 + nv * V * (grad ? 18 : 12)) * issue;
+      const double round = 0.6 + (grad ? 200 + nv * V * 18 : 450 + nv * V * 12) * issue;
       const double rate = esize == 4 && seg >= 128 ? (grad ? 4.8e6 : 5.2e6) : (grad ? 2.9e6 : 3.4e6);
       double us = 3.0 + std::max(rounds * round, total / rate / eff);
       // measured beside the estimate: one block of 512 per SM hides less, and
