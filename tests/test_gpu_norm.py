@@ -271,6 +271,47 @@ def test_refusals():
         ff.group_norm_act_backward(y, x, None, None, None, None, 3)
 
 
+@pytest.mark.parametrize("shape", [(1100000, 1, 2000, 16), (70, 16384, 2048, 32), (70000, 64, 512, 32)])
+def test_more_than_2_31_values(shape):
+    """Rows, column passes and blocks: the last sample of a large batch as that
+    sample alone.  The sums may have another order (statistics a few units of
+    2^-24 apart), so an output may round to the next bf16."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    n, S, C, G = shape
+    assert n * S * C > 1 << 31
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty(n, S, C, device="cuda", dtype=torch.bfloat16).normal_(generator=gen)
+    y, m, r = ff.group_norm_act(x, None, None, G)
+    last = x[-1:].clone()
+    y1, m1, r1 = ff.group_norm_act(last, None, None, G)
+    near = lambda a, b: torch.all((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 1e-5)
+    assert near(y[-1:], y1) and near(m[-1:], m1) and near(r[-1:], r1)
+    assert torch.isfinite(y.view(-1)[::997].float()).all()
+    dx, _, _ = ff.group_norm_act_backward(x, x, m, r, None, None, G, out=y)  # dy = x
+    d1, _, _ = ff.group_norm_act_backward(last, last, m1, r1, None, None, G)
+    assert near(dx[-1:], d1)
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 500, 10), (1, 3, 500, 10), (1, 3, 512, 8)])
+def test_row_strides_past_31_bits(shape):
+    """Rows 2^30 elements and more apart, against the same rows side by side."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    n, S, C, G = shape
+    x = torch.randn(n, S, C, device="cuda")
+    wide = torch.empty(3 * ((1 << 30) + 8), device="cuda")
+    v = wide.as_strided((n, S, C), ((S if n == 1 else 1) * ((1 << 30) + 8), (1 << 30) + 8, 1))
+    v.copy_(x)
+    y, m, r = ff.group_norm_act(x, None, None, G)
+    w, p, q = ff.group_norm_act(v, None, None, G)
+    near = lambda a, b: torch.allclose(a, b, rtol=1e-5, atol=1e-5)
+    assert near(w, y) and near(p, m) and near(q, r)
+    dx, dg, db = ff.group_norm_act_backward(x, x, m, r, None, None, G)
+    dv, eg, eb = ff.group_norm_act_backward(v, v, m, r, None, None, G, out=v)
+    assert near(dv, dx) and near(eg, dg) and near(eb, db)
+
+
 def test_a_mean_near_zero_keeps_its_bits():
     """Groups of zero mean whose first value is three spreads off: the mean must
     not come out as a difference of numbers of that size.  A group's mean is
