@@ -338,7 +338,8 @@ ff_status go(const GnArgs<T>& a, const GnRowsPlan& pl, bool grad, cudaStream_t s
 }
 template <typename T, int V, int NV>
 ff_status run(const GnArgs<T>& a, const GnRowsPlan& pl, bool grad, cudaStream_t st) {
-  if (pl.lanes > 32) return go<T, V, NV, true, true>(a, pl, grad, st);
+  if constexpr (NV * V >= 8)  // a block per group: more than 4 values a thread
+    if (pl.lanes > 32) return go<T, V, NV, true, true>(a, pl, grad, st);
   return a.s.S == 1 ? go<T, V, NV, true, false>(a, pl, grad, st) : go<T, V, NV, false, false>(a, pl, grad, st);
 }
 
