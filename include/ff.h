@@ -524,8 +524,8 @@ FF_API ff_status ff_layer_selftest_wait(ff_layer* layer, unsigned int timeout_us
 typedef enum { FF_ACT_NONE = 0, FF_ACT_RELU = 1, FF_ACT_SILU = 2 } ff_activation; /* u, max(u, 0), u / (1 + e^-u) */
 
 /* Bytes of workspace that ff_group_norm_act (backward = 0) or its gradient
- * (backward = 1) needs for these sizes (0: none; pass NULL then); -1 on sizes
- * that the call would refuse. */
+ * (backward = 1) needs for these sizes, at any strides and alignment (0: none;
+ * pass NULL then); -1 on sizes that the call would refuse. */
 FF_API long long ff_group_norm_workspace(int n, int spatial, int channels, int groups, ff_precision prec,
                                          int backward);
 

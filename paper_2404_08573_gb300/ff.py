@@ -713,13 +713,12 @@ def _on_device_of_first(f):
     @functools.wraps(f)
     def call(*args, **kwargs):
         x = args[0] if args else kwargs.get(first)
-        if type(x) is Fp8Matrix:
-            x = x.q
-        if not isinstance(x, torch.Tensor):
-            raise TypeError(f"{first} must be a torch.Tensor" if x is not None else f"{first} is missing")
-        if not x.is_cuda:
+        try:
+            index = x.get_device()
+        except AttributeError:
+            raise TypeError(f"{first} must be a {'torch.Tensor' if first != 'a' else 'Fp8Matrix'}") from None
+        if index < 0:
             raise ValueError(f"{first} must be a CUDA tensor")
-        index = x.get_device()
         if index == torch._C._cuda_getDevice():
             return f(*args, **kwargs)
         with torch.cuda.device(index):
@@ -776,11 +775,6 @@ def _same_device(t, device, what):
         raise ValueError(f"{what} must be on {device}")
 
 
-@functools.lru_cache(maxsize=4096)
-def _norm_workspace(n, spatial, C, groups, prec, backward):
-    return lib().ff_group_norm_workspace(n, spatial, C, groups, prec, backward)
-
-
 def _like(t, x, what):
     """Checks an optional buffer that must match x in shape, type and device; returns its row stride."""
     if not isinstance(t, torch.Tensor) or t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
@@ -788,21 +782,21 @@ def _like(t, x, what):
     return _row_stride_of(t, what)
 
 
-def _norm_args(x, groups, act):
-    if x.dim() < 2:
+@functools.lru_cache(maxsize=4096)
+def _norm_sizes(shape, groups, act, prec, backward):
+    """n, positions, channels, groups, ff_activation and workspace bytes of a norm over [n, ..., channels]."""
+    if len(shape) < 2:
         raise ValueError("x must be [n, channels] or [n, ..., channels]")
     if act not in _ACT:
         raise ValueError(f"act must be one of {sorted(_ACT)}")
-    n, C = x.shape[0], x.shape[-1]
-    groups = int(groups)
+    n, C, spatial, groups = shape[0], shape[-1], 1, int(groups)
     if groups < 1 or C < 1 or C % groups:
         raise ValueError("groups must divide the channels")
-    spatial = 1
-    for d in x.shape[1:-1]:
+    for d in shape[1:-1]:
         spatial *= d
     if max(n, spatial, C) > _INT_MAX:
         raise ValueError("n, positions and channels must each fit 32 bits")
-    return n, spatial, C, groups
+    return n, spatial, C, groups, _ACT[act], lib().ff_group_norm_workspace(n, spatial, C, groups, prec, backward)
 
 
 @_on_device_of_first
@@ -812,9 +806,8 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     groups, channels last.  x [n, channels] or [n, ..., channels] (bf16 or
     fp32, evenly spaced rows); gamma, beta fp32 [channels] or None.  Returns
     (y, mean, rstd), mean and rstd fp32 [n, groups]; out may be x."""
-    prec = _prec(x, "x")
-    n, spatial, C, groups = _norm_args(x, groups, act)
-    dev = x.device
+    prec, dev = _prec(x, "x"), x.device
+    n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 0)
     on, empty = _on(stream, dev)
     ldx = _row_stride_of(x, "x")
     if out is None:
@@ -831,11 +824,10 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
         pr = rstd.data_ptr()
     else:
         pr = _vector(rstd, n * groups, "rstd", dev)
-    need = _norm_workspace(n, spatial, C, groups, prec, 0)
     ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
     _check(lib().ff_group_norm_act(
         x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
-        eps, _ACT[act], prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
+        eps, kind, prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
         "ff_group_norm_act")
     return out, mean, rstd
 
@@ -845,9 +837,8 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     """ff_group_norm_act_backward: the gradient of group_norm_act at (x, gamma,
     beta), with the mean and rstd it returned.  Returns (dx, dgamma, dbeta);
     out may be dy or x."""
-    prec = _prec(x, "x")
-    n, spatial, C, groups = _norm_args(x, groups, act)
-    dev = x.device
+    prec, dev = _prec(x, "x"), x.device
+    n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 1)
     on, empty = _on(stream, dev)
     ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
     if out is None:
@@ -858,12 +849,11 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     dbeta = empty((C,), dtype=torch.float32, device=dev)
     if mean is None or rstd is None:
         raise ValueError("mean and rstd of the forward pass are needed")
-    need = _norm_workspace(n, spatial, C, groups, prec, 1)
     ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
     _check(lib().ff_group_norm_act_backward(
         dy.data_ptr(), lddy, x.data_ptr(), ldx, n, spatial, C, groups, _vector(mean, n * groups, "mean", dev),
         _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
-        _ACT[act], prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
+        kind, prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
         None if ws is None else ws.data_ptr(), need, on), "ff_group_norm_act_backward")
     return out, dgamma, dbeta
 
@@ -923,6 +913,10 @@ class Fp8Matrix:
                 or not scale.is_contiguous() or scale.device != q.device):
             raise ValueError("scale must be contiguous fp32 [ceil(k / 128), rows or row blocks] beside q")
 
+    def get_device(self):
+        """The CUDA device's index, as of a tensor."""
+        return self.q.get_device()
+
     @property
     def blocks(self):
         """ff_fp8_blocks of the matrix."""
@@ -977,7 +971,7 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
     out's type; bias fp32 [b.rows]; status: a one-element int32 CUDA tensor
     that is OR-ed with 1 if a kernel wait timed out."""
-    if type(a) is not Fp8Matrix or type(b) is not Fp8Matrix:
+    if not isinstance(a, Fp8Matrix) or not isinstance(b, Fp8Matrix):
         raise TypeError("a and b must be Fp8Matrix")
     if a.k != b.k:
         raise ValueError("a and b must have the same k")
@@ -988,15 +982,15 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     on, empty = _on(stream, dev)
     m, n = a.rows, b.rows
     if out is None:
-        if out_dtype not in _PREC:
+        prec = _PREC.get(out_dtype)
+        if prec is None:
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
         out, ldc = empty((m, n), dtype=out_dtype, device=dev), n
     else:
         if out.shape != (m, n):
             raise ValueError("out must be [a.rows, b.rows]")
         _same_device(out, dev, "out")
-        ldc = _row_stride_of(out, "out")
-    prec = _prec(out, "out")
+        prec, ldc = _prec(out, "out"), _row_stride_of(out, "out")
     if status is not None:
         _same_device(status, dev, "status")
     _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
