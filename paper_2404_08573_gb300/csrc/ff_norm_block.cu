@@ -499,11 +499,13 @@ GnBlockPlan gn_block_plan(const GnShape& s, int V, int esize, bool grad) {
       if (units > 0x3FFFFFFF) continue;
       const long long room = 152ll * per_sm, rounds = (units + room - 1) / room;
       const double warps = per_sm * T / 32.0, issue = std::max(6.0, warps / 4.0) / 1900.0;
-      const double round = 0.6 + (grad ? 200 + nv * V * 18 : 450 + nv * V * 12) * issue;
+      // 2-byte copies are not asynchronous: a value waits for its own (100 x 300
+      // x 2000 in 16 groups of 125: 209 us, column passes 75)
+      const double round = 0.6 + (grad ? 200 + nv * V * 18 : 450 + nv * V * (V * esize < 4 ? 60 : 12)) * issue;
       const double rate = esize == 4 && seg >= 128 ? (grad ? 4.8e6 : 5.2e6) : (grad ? 2.9e6 : 3.4e6);
       double us = 3.0 + std::max(rounds * round, total / rate / eff);
       // measured beside the estimate: one block of 512 per SM hides less, and
-      // 2-byte copies are not asynchronous (100 x 100 x 100 in 4 groups: 17 us)
+      // 2-byte copies cost still more (100 x 100 x 100 in 4 groups: 17 us)
       if (grad && T == kMaxT) us *= 1.2;
       if (grad && V * esize < 4) us *= 2.5;
       if (us < best.us) best = GnBlockPlan{T, GS, nv, (int)((units + rounds - 1) / rounds), (int)rounds, us};
