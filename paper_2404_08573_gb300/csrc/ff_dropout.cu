@@ -96,20 +96,38 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(const T* x, const T* r
     const unsigned long long w0 = MODE == DENSE ? (unsigned long long)(rr[u] * s.words + (cc[u] >> 2))
                                                 : (unsigned long long)i * (E / 4);
     const unsigned long long k0 = key(w0);
-    if (MODE == DENSE && (cc[u] + E > s.cols || (i + 1) * E > s.count)) {
-      // across rows, or past the end: element by element
-      long long er = rr[u], ec = cc[u];
-      for (int e = 0; e < E && i * E + e < s.count; ++e) {
-        float v[1], q[1] = {0.f};
-        Vec<T, 1>::unpack(Vec<T, 1>::load(x + i * E + e), v);
-        if constexpr (RES) Vec<T, 1>::unpack(Vec<T, 1>::load(res + i * E + e), q);
-        const unsigned long long m = sm64_mix(key((unsigned long long)(er * s.words + (ec >> 2))));
-        q[0] = one(v[0], q[0], (uint32_t)(m >> (16 * (ec & 3))) & 0xFFFFu);
-        Vec<T, 1>::store(y + i * E + e, q);
-        if (++ec == s.cols) {
-          ec = 0;
-          ++er;
-        }
+    if constexpr (MODE == DENSE) if (cc[u] + E > s.cols || (i + 1) * E > s.count) {
+      // across rows, or past the end: a word whenever the next element is in another
+      const int there = (int)min((long long)E, s.count - i * E);
+      float v[E], q[E];
+      if (there == E) {
+        V::unpack(a[u][0], v);
+        if constexpr (RES) V::unpack(b[u][0], q);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e < there) {
+            Vec<T, 1>::unpack(Vec<T, 1>::load(x + i * E + e), reinterpret_cast<float(&)[1]>(v[e]));
+            if constexpr (RES)
+              Vec<T, 1>::unpack(Vec<T, 1>::load(res + i * E + e), reinterpret_cast<float(&)[1]>(q[e]));
+          }
+      }
+      unsigned long long word = (unsigned long long)(rr[u] * s.words + (cc[u] >> 2)), m = 0;
+      long long ec = cc[u];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (e == 0 || (ec & 3) == 0) m = sm64_mix(key(word));
+        q[e] = one(v[e], RES ? q[e] : 0.f, (uint32_t)(m >> (16 * (ec & 3))) & 0xFFFFu);
+        ++ec;
+        if (ec == s.cols) ec = 0;
+        if ((ec & 3) == 0) ++word;  // the next word of the row, or the first of the next
+      }
+      if (there == E) {
+        V::store(y + i * E, q);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e < there) Vec<T, 1>::store(y + i * E + e, reinterpret_cast<const float(&)[1]>(q[e]));
       }
       continue;
     }

@@ -69,7 +69,8 @@ constexpr int kQThreads = 256;
 // orientations come from one read.  Bound by HBM: x once, each orientation
 // once (4096 x 8192 bf16, both: 23.7 us, 5.7 TB/s; 2000 x 784 fp32 in tiles, both:
 // 4.0 us, a launch and one round of 112 blocks).
-template <typename T, bool VEC>
+// LOAD: bytes of x per access that its rows' alignment allows.
+template <typename T, int LOAD>
 __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
     k_fp8_quantize(const T* x, long long ldx, int rows, int k, int tile, uint8_t* q, float* scale, uint8_t* qt,
                    float* scale_t, int ldq, int ldqt, int kblocks, int rblocks) {
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
   const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
   const int row0 = rb * QB + rg * 8, c0 = kb * QB + cg * 8;
   uint32_t v[8][W];
-  if (VEC && c0 + 8 <= k) {
+  if (LOAD == 16 && c0 + 8 <= k) {
     const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -95,6 +96,13 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
       for (int j = 0; j < W / 4; ++j)
         *reinterpret_cast<uint4*>(&v[i][4 * j]) =
             row0 + i < rows ? reinterpret_cast<const uint4*>(p + i * ldx)[j] : make_uint4(0, 0, 0, 0);
+  } else if (LOAD == 4 && c0 + 8 <= k) {
+    const T* p = x + (long long)row0 * ldx + c0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        v[i][j] = row0 + i < rows ? reinterpret_cast<const uint32_t*>(p + i * ldx)[j] : 0u;
   } else {
     const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
@@ -232,13 +240,14 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, int tile, uint8
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)rows * k * (sizeof(T) + (q ? 1 : 0) + (qt ? 1 : 0));
   const int ldq = fp8_stride(k), ldqt = fp8_stride(rows);
-  const bool vec = rows_aligned(x, ldx, sizeof(T), 16);
   PdlLaunch l(dim3((unsigned)blocks), dim3(kQThreads), st);
+  auto go = [&](auto* kernel) {
+    return cudaLaunchKernelEx(&l.cfg, kernel, x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq, ldqt, kblocks, rblocks);
+  };
   FF_LAUNCH(K_FP8_QUANT, bytes, st,
-            vec ? cudaLaunchKernelEx(&l.cfg, k_fp8_quantize<T, true>, x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq,
-                                     ldqt, kblocks, rblocks)
-                : cudaLaunchKernelEx(&l.cfg, k_fp8_quantize<T, false>, x, ldx, rows, k, tile, q, scale, qt, scale_t, ldq,
-                                     ldqt, kblocks, rblocks),
+            rows_aligned(x, ldx, sizeof(T), 16)  ? go(k_fp8_quantize<T, 16>)
+            : rows_aligned(x, ldx, sizeof(T), 4) ? go(k_fp8_quantize<T, 4>)
+                                                 : go(k_fp8_quantize<T, sizeof(T)>),
             "8-bit quantize");
   return FF_OK;
 }

@@ -158,6 +158,29 @@ __device__ __forceinline__ void tile_of(int t, int ntp, int ntq, int& tp, int& t
   tq = in / rows;
 }
 
+// A warp writes a staged block of 32 rows x 128 bytes (16-byte units swizzled
+// by the row) to C, `rows` and `left` of its rows and columns being there.
+template <typename U>
+__device__ __forceinline__ void rows_out(const uint8_t* from, U* c, long long ldc, int rows, int left, int lane) {
+  constexpr int J = 128 / 32 / (int)sizeof(U);
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += 8) {
+    U v[8][J];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int byte = (lane + 32 * j) * (int)sizeof(U);
+        v[i][j] = *reinterpret_cast<const U*>(from + (r0 + i) * 128 + (((byte >> 4) ^ i) << 4) + (byte & 15));
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (r0 + i < rows && lane + 32 * j < left) c[(r0 + i) * ldc + lane + 32 * j] = v[i][j];
+  }
+}
+
 template <bool COLS>
 __global__ void __launch_bounds__(LTHREADS, 1)
     k_fp8_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -421,8 +444,8 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       // Store: 128 bytes of each of the warp's 32 rows at a time through the
       // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
       // clips what lies past the matrix, and the warp need not wait for the
-      // memory), else element by element along the rows.
-      const int es = g.out_bf16 ? 2 : 4;
+      // memory), else by the lanes along a row, eight rows read before the
+      // first is written (2023 x 2375 x 368, bf16 C: 24 us one by one).
       auto block = [&](int ch) {  // staging block of chunk ch, free again
         if (g.tma_c) {
           if (lane == 0) ptx::bulk_wait_read1();
@@ -430,7 +453,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
         __syncwarp();
         return stage + (ch & 1) * (LSTAGING / 2);
       };
-      auto flush = [&](uint8_t* from, int col0, int cols) {  // staged columns col0 .. col0 + cols of C
+      auto flush = [&](uint8_t* from, int col0) {  // the staged columns of C from col0 on
         if (g.tma_c) {
           ptx::fence_async_smem();
           __syncwarp();
@@ -441,16 +464,11 @@ __global__ void __launch_bounds__(LTHREADS, 1)
           return;
         }
         __syncwarp();
-        for (int rr = 0; rr < 32 && rbase + rr < g.P; ++rr)
-          for (int j = lane; j < cols && col0 + j < g.Q; j += 32) {
-            const int byte = j * es;
-            const uint8_t* src = from + rr * 128 + (((byte >> 4) ^ (rr & 7)) << 4) + (byte & 15);
-            const long long at = (long long)(rbase + rr) * g.ldc + col0 + j;
-            if (es == 2)
-              static_cast<uint16_t*>(g.c)[at] = *reinterpret_cast<const uint16_t*>(src);
-            else
-              static_cast<uint32_t*>(g.c)[at] = *reinterpret_cast<const uint32_t*>(src);
-          }
+        const int rows = g.P - rbase, left = g.Q - col0;
+        if (g.out_bf16)
+          rows_out(from, static_cast<uint16_t*>(g.c) + ((long long)rbase * g.ldc + col0), g.ldc, rows, left, lane);
+        else
+          rows_out(from, static_cast<uint32_t*>(g.c) + ((long long)rbase * g.ldc + col0), g.ldc, rows, left, lane);
       };
       // four accumulators with bias and activation
       auto value = [&](int i) {
@@ -469,7 +487,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
                                          __floats2bfloat162_rn(w.x, w.y), __floats2bfloat162_rn(w.z, w.w)};
             *reinterpret_cast<uint4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(h);
           }
-          flush(to, cbase + ch * 64, 64);
+          flush(to, cbase + ch * 64);
         }
       } else {
 #pragma unroll
@@ -478,7 +496,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
 #pragma unroll
           for (int u = 0; u < 8; ++u)
             *reinterpret_cast<float4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = value(ch * 32 + u * 4);
-          flush(to, cbase + ch * 32, 32);
+          flush(to, cbase + ch * 32);
         }
       }
     }
