@@ -445,7 +445,8 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
       // clips what lies past the matrix, and the warp need not wait for the
       // memory), else by the lanes along a row, eight rows read before the
-      // first is written (2023 x 2375 x 368, bf16 C: 24 us one by one).
+      // first is written (2023 x 2375 x 368, bf16 C: 12.5 us, 24 one by one, 9
+      // for 2376 columns).
       auto block = [&](int ch) {  // staging block of chunk ch, free again
         if (g.tma_c) {
           if (lane == 0) ptx::bulk_wait_read1();
