@@ -352,9 +352,10 @@ bool gn_rows_fit(const GnShape& s) { return (long long)s.S * s.Cg <= (s.S == 1 ?
 // Lanes per group: from four on as few as leave each 8 values where they come
 // in vectors (the sums' shuffles are shared by more of them: 8192 x 4096 in 32
 // groups, fp32, 69 us with 4 values each, 48 with 8; 3000 x 3200 in 32 groups,
-// bf16, 20 with up to 4, 17 with 8), as many as there are values, up to a warp,
-// where they do not (2048 x 2000 in 16 groups, fp32, gradient: 16 us, with 8
-// each 18).
+// bf16, 20 with up to 4, 17 with 8), and 4 values, which a lane has room for
+// anyhow, where they do not (5182 x 1120 in 32 groups of 35, bf16, gradient: 28
+// us, with one or two each 52; 2048 x 2000 in 16 groups of 125, fp32, gradient:
+// 16 us, with 8 each 18).
 GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad) {
   GnRowsPlan p;
   const int vecs = s.S * s.Cg / V;
@@ -366,8 +367,8 @@ GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad) {
     p.sets = s.G;
   } else {
     p.lanes = 1;
-    const int each = V > 1 ? 8 / V : 1;  // vectors
-    while (p.lanes < 32 && p.lanes < vecs && (p.lanes < 4 || p.lanes * each < vecs)) p.lanes *= 2;
+    const int each = V > 1 ? 8 / V : 4, least = V > 1 ? 4 : 2;  // vectors, lanes
+    while (p.lanes < 32 && p.lanes < vecs && (p.lanes < least || p.lanes * each < vecs)) p.lanes *= 2;
     per = 32 / p.lanes;
     p.sets = cdiv(s.G, per);
     rows = kWarps;
