@@ -21,6 +21,7 @@
 // copies and MMAs land before it frees TMEM and exits.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ff_api_internal.h"
 #include "ff_fp8.h"
@@ -113,7 +114,6 @@ struct Args {
   long long ldc;
   int* err;
   int ntp, ntq;      // tiles
-  int tma_c;         // pair kernel: C goes out by TMA
 };
 
 __device__ __forceinline__ float finish(float v, int relu) { return relu && v < 0.f ? 0.f : v; }  // keeps NaN
@@ -128,7 +128,7 @@ __device__ __forceinline__ float finish(float v, int relu) { return relu && v < 
 // next tile's first k-blocks run under the store of this one.
 //
 // Bound by the MMAs: 4096 x 8192 x 8192 with a scale per 128 x 128 tile of B takes
-// 189 us, 2.91 PFLOP/s (0.77 of twice the measured bf16 burst rate, 0.85 of
+// 187 us, 2.94 PFLOP/s (0.78 of twice the measured bf16 burst rate, 0.86 of
 // twice the sustained one).  With a scale per row of B each value of the
 // product takes a second multiplication, and the promotion bounds: 290 us.
 constexpr int LN = 256;
@@ -181,7 +181,10 @@ __device__ __forceinline__ void rows_out(const uint8_t* from, U* c, long long ld
   }
 }
 
-template <bool COLS>
+// TMA_C: C's rows are 16-byte aligned and go out by TMA.  BF16: C's type.
+// (Kernels of their own: with all four stores' code in one the products were 1
+// to 3 % slower.)
+template <bool COLS, bool TMA_C, bool BF16>
 __global__ void __launch_bounds__(LTHREADS, 1)
     k_fp8_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmC, Args g) {
@@ -445,31 +448,30 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
       // clips what lies past the matrix, and the warp need not wait for the
       // memory), else by the lanes along a row, eight rows read before the
-      // first is written (2023 x 2375 x 368, bf16 C: 12.5 us, 24 one by one, 9
+      // first is written (2023 x 2375 x 368, bf16 C: 11.0 us, 24 one by one, 9
       // for 2376 columns).
       auto block = [&](int ch) {  // staging block of chunk ch, free again
-        if (g.tma_c) {
-          if (lane == 0) ptx::bulk_wait_read1();
-        }
+        if (TMA_C && lane == 0) ptx::bulk_wait_read1();
         __syncwarp();
         return stage + (ch & 1) * (LSTAGING / 2);
       };
       auto flush = [&](uint8_t* from, int col0) {  // the staged columns of C from col0 on
-        if (g.tma_c) {
+        if constexpr (TMA_C) {
           ptx::fence_async_smem();
           __syncwarp();
           if (lane == 0) {
             if (rbase < g.P && col0 < g.Q) ptx::tma_store_2d(&tmC, from, col0, rbase);
             ptx::bulk_commit();
           }
-          return;
+        } else {
+          __syncwarp();
+          const int rows = g.P - rbase, left = g.Q - col0;
+          const long long at = (long long)rbase * g.ldc + col0;
+          if constexpr (BF16)
+            rows_out(from, static_cast<uint16_t*>(g.c) + at, g.ldc, rows, left, lane);
+          else
+            rows_out(from, static_cast<uint32_t*>(g.c) + at, g.ldc, rows, left, lane);
         }
-        __syncwarp();
-        const int rows = g.P - rbase, left = g.Q - col0;
-        if (g.out_bf16)
-          rows_out(from, static_cast<uint16_t*>(g.c) + ((long long)rbase * g.ldc + col0), g.ldc, rows, left, lane);
-        else
-          rows_out(from, static_cast<uint32_t*>(g.c) + ((long long)rbase * g.ldc + col0), g.ldc, rows, left, lane);
       };
       // four accumulators with bias and activation
       auto value = [&](int i) {
@@ -477,7 +479,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
         return make_float4(finish(acc[i] + v.x, g.relu), finish(acc[i + 1] + v.y, g.relu),
                            finish(acc[i + 2] + v.z, g.relu), finish(acc[i + 3] + v.w, g.relu));
       };
-      if (g.out_bf16) {
+      if constexpr (BF16) {
 #pragma unroll
         for (int ch = 0; ch < LCPW / 64; ++ch) {
           uint8_t* to = block(ch);
@@ -501,7 +503,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
         }
       }
     }
-    if (lane == 0) ptx::bulk_wait_read0();
+    if (TMA_C && lane == 0) ptx::bulk_wait_read0();
     __syncwarp();
   }
 
@@ -784,12 +786,13 @@ cudaError_t launch(F* kernel, unsigned grid, int threads, int cluster, int smem,
 // CTA pairs the GPU holds at once (one CTA per SM; an SM without a partner in
 // its cluster group stays out); 0 if the pair kernel was not built with the
 // registers that its split counts on, and so must not run.
-template <bool COLS>
+template <bool COLS, bool TMA_C, bool BF16>
 int resident_pairs() {
   static const int n = [] {
     cudaFuncAttributes fa{};
-    if (cudaFuncGetAttributes(&fa, k_fp8_pair<COLS>) != cudaSuccess || fa.numRegs != LREGS) return 0;
-    if (cudaFuncSetAttribute(k_fp8_pair<COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM) != cudaSuccess) return 0;
+    constexpr auto kernel = k_fp8_pair<COLS, TMA_C, BF16>;
+    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs != LREGS) return 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM) != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(LTHREADS);
@@ -801,7 +804,7 @@ int resident_pairs() {
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int c = 0;
-    if (cudaOccupancyMaxActiveClusters(&c, k_fp8_pair<COLS>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&c, kernel, &cfg) != cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
@@ -905,7 +908,12 @@ Plan plan(int M, int N, int K, bool cols, int pairs) {
 ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
   const int ld = fp8_stride(f.K);
   const bool cols = !f.b_tiles;
-  const int pairs = cols ? resident_pairs<true>() : resident_pairs<false>();
+  auto room = [&](auto c, auto b) {
+    return std::min(resident_pairs<c.value, true, b.value>(), resident_pairs<c.value, false, b.value>());
+  };
+  using Y = std::true_type;
+  using N = std::false_type;
+  const int pairs = cols ? (f.out_bf16 ? room(Y{}, Y{}) : room(Y{}, N{})) : (f.out_bf16 ? room(N{}, Y{}) : room(N{}, N{}));
   const Plan pl = plan(f.M, f.N, f.K, cols, pairs);
   Args g{};
   const Scales sa{f.sa, f.M, 0};
@@ -932,13 +940,17 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
     return FF_ERR_INVALID_ARG;
   const int es = f.out_bf16 ? 2 : 4;
   CUtensorMap c = p;
-  g.tma_c = pairk && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N && make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
+  const bool tma_c = pairk && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N && make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
   const double work = 2.0 * f.M * f.N * f.K;
   auto go = [&]() -> cudaError_t {
     if (pairk) {
       const unsigned grid = 2u * (unsigned)std::min((long long)pairs, (long long)g.ntp * g.ntq);
-      return cols ? launch(k_fp8_pair<true>, grid, LTHREADS, 2, L_SMEM, st, p, q, c, g)
-                  : launch(k_fp8_pair<false>, grid, LTHREADS, 2, L_SMEM, st, p, q, c, g);
+      auto* kernel =
+          f.out_bf16 ? (cols ? (tma_c ? k_fp8_pair<true, true, true> : k_fp8_pair<true, false, true>)
+                             : (tma_c ? k_fp8_pair<false, true, true> : k_fp8_pair<false, false, true>))
+                     : (cols ? (tma_c ? k_fp8_pair<true, true, false> : k_fp8_pair<true, false, false>)
+                             : (tma_c ? k_fp8_pair<false, true, false> : k_fp8_pair<false, false, false>));
+      return launch(kernel, grid, LTHREADS, 2, L_SMEM, st, p, q, c, g);
     }
     const bool each = cols || pl.swap;
     switch (pl.bn) {
