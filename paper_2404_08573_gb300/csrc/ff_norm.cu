@@ -82,11 +82,15 @@ ColGeom col_geom(const GnShape& s, int V, int esize, bool grad, const float* gam
   g.by_G = FastDiv(s.G);
   return g;
 }
-// A thread's place: sample, chunk, its column of V channels and its positions
-// r0, r0 + TR, .. below r1.  The second passes take the blocks from the last
-// to the first, since what the first pass read last is still in L2.
+// A thread's place: sample, chunk, its column of V channels, and its positions
+// tr, tr + TR, .. below `rows`, counted from the chunk's first: a chunk's own
+// count stays small, whereas positions counted from the sample's start would
+// pass 2^31 in the last chunk of the longest samples.  The second passes take
+// the blocks from the last to the first, since what the first pass read last
+// is still in L2.
 struct ColPlace {
-  int b, ch, tc, tr, col, r0, r1;
+  int b, ch, tc, tr, col, rows;
+  long long r0;  // the thread's first position, from the sample's first
   bool on;
   __device__ __forceinline__ ColPlace(const GnShape& s, const ColGeom& g, bool backwards) {
     const uint32_t i = backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
@@ -97,8 +101,9 @@ struct ColPlace {
     tc = (int)threadIdx.x - tr * g.TC;
     col = (int)(i - rest * g.ctiles) * g.TC + tc;
     on = tr < g.TR && col < g.CV;
-    r0 = ch * g.chunk + tr;
-    r1 = min(s.S, (ch + 1) * g.chunk);
+    const int first = ch * g.chunk;
+    rows = min(g.chunk, s.S - first);
+    r0 = (long long)first + tr;
   }
 };
 
@@ -150,14 +155,14 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
   if (p.on) {
     const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const long long step = (long long)g.TR * s.ldx;
-    if (p.r0 < p.r1) {
+    if (p.tr < p.rows) {
       float m[V];
       Vec<T, V>::unpack(Vec<T, V>::load(q), m);
 #pragma unroll
       for (int e = 0; e < V; ++e) m[e] = -m[e];
       PV::of(m, np);
     }
-    walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+    walk_rows(p.tr, p.rows, g.TR, [&](auto has) {
       typename Vec<T, V>::Raw raw[kFlight];
 #pragma unroll
       for (int u = 0; u < kFlight; ++u)
@@ -179,7 +184,7 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
       q += kFlight * step;
     });
   }
-  const int rows = p.r1 - p.ch * g.chunk;
+  const int rows = p.rows;
   // thread row t has rows / TR positions, one more below the remainder
   const int lo = rows / g.TR, rem = rows - lo * g.TR, m = lo + (p.tr < rem ? 1 : 0);
   float s1[V], s2[V], minus[V];
@@ -248,7 +253,7 @@ struct Cells {
       for (int u = 0; u < kKept; ++u) {
         const int i = i0 + u * THREADS;
         const int ch = (int)g.by_Cg.div((uint32_t)i);
-        if (i < cells) f(q[u], u, i - ch * s.Cg, (float)(min(s.S, (ch + 1) * g.chunk) - ch * g.chunk));
+        if (i < cells) f(q[u], u, i - ch * s.Cg, (float)min(g.chunk, s.S - ch * g.chunk));
       }
     }
   }
@@ -307,7 +312,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
   const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
   T* o = y + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, so = (long long)g.TR * s.ldy;
-  walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+  walk_rows(p.tr, p.rows, g.TR, [&](auto has) {
     typename Vec<T, V>::Raw raw[kFlight];
 #pragma unroll
     for (int u = 0; u < kFlight; ++u)
@@ -382,7 +387,7 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
     const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
     const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy;
-    walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+    walk_rows(p.tr, p.rows, g.TR, [&](auto has) {
       typename Vec<T, V>::Raw rx[kFlight], rd[kFlight];
 #pragma unroll
       for (int u = 0; u < kFlight; ++u)
@@ -528,7 +533,7 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
   const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
   T* o = dx + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy, so = (long long)g.TR * s.ldy;
-  walk_rows(p.r0, p.r1, g.TR, [&](auto has) {
+  walk_rows(p.tr, p.rows, g.TR, [&](auto has) {
     typename Vec<T, V>::Raw rx[kFlight], rd[kFlight];
 #pragma unroll
     for (int u = 0; u < kFlight; ++u)

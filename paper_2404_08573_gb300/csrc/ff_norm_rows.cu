@@ -157,10 +157,11 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps) k_gn_rows(G
       if (sl.on(i)) r[i] = VV::load(px + sl.at(i, ldx));
     px += dx;
   };
-  int b = w.b;
-  if (b < s.n) load(cur);
-  for (; b < s.n; b += w.step) {
-    if (s.n - b > w.step) load(nxt);
+  // counted down, since the sample after the last could be past 2^31
+  if (w.b < s.n) load(cur);
+  for (int left = s.n - w.b; left > 0; left -= w.step) {
+    const int b = s.n - left;
+    if (left > w.step) load(nxt);
     uint64_t d[N], t = 0;
     to_pairs<T, V, NV>(cur, d);
 #pragma unroll
@@ -222,10 +223,9 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
   const float inv = 1.f / ((float)s.S * (float)s.Cg);
   typename VV::Raw cx[NV] = {}, cy[NV] = {}, nx[NV] = {}, ny[NV] = {};
   const int ldx = (int)s.ldx, lddy = (int)s.lddy, ldo = (int)s.ldy;  // within a sample (near, see plan_of)
-  int b = w.b;
-  const T* px = a.x + (long long)b * s.S * s.ldx + c0;  // the next sample to load
-  const T* py = a.dy + (long long)b * s.S * s.lddy + c0;
-  T* q = a.out + (a.out ? (long long)b * s.S * s.ldy + c0 : 0);
+  const T* px = a.x + (long long)w.b * s.S * s.ldx + c0;  // the next sample to load
+  const T* py = a.dy + (long long)w.b * s.S * s.lddy + c0;
+  T* q = a.out + (a.out ? (long long)w.b * s.S * s.ldy + c0 : 0);
   const long long sx = (long long)w.step * s.S * s.ldx, sy = (long long)w.step * s.S * s.lddy,
                   so = (long long)w.step * s.S * s.ldy;
   float mu = 0.f, rs = 0.f, nmu = 0.f, nrs = 0.f;
@@ -243,9 +243,11 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
       r = __ldg(a.rstd + (long long)b * s.G + w.g);
     }
   };
-  if (b < s.n) load(cx, cy, b, mu, rs);
-  for (; b < s.n; b += w.step) {
-    if (s.n - b > w.step) load(nx, ny, b + w.step, nmu, nrs);
+  // counted down, as in the forward pass
+  if (w.b < s.n) load(cx, cy, w.b, mu, rs);
+  for (int left = s.n - w.b; left > 0; left -= w.step) {
+    const int b = s.n - left;
+    if (left > w.step) load(nx, ny, b + w.step, nmu, nrs);
     // a vector that does not exist has du = 0
     uint64_t h[N], d[N], t1 = 0, t2 = 0;
     {
