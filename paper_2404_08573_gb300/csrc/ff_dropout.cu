@@ -51,7 +51,6 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(const T* x, const T* r
   constexpr int A = MODE == WORDS ? 1 : E;                    // elements of an access
   using V = Vec<T, A>;
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const unsigned long long off = s.offset + (s.offset_dev ? *s.offset_dev : 0ull);
   const long long i0 = (long long)blockIdx.x * (kDropThreads * kDropUnits) + threadIdx.x;
   // row and column (in elements) of this thread's units, one block's width apart

@@ -86,7 +86,6 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
   // that the 16 column groups of a warp's writes fall into different banks
   __shared__ __align__(16) uint8_t tq[QB * QB];
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const int kb = blockIdx.x % kblocks, rb = blockIdx.x / kblocks;
   const int rg = threadIdx.x >> 4, cg = threadIdx.x & 15;
   const int row0 = rb * QB + rg * 8, c0 = kb * QB + cg * 8;

@@ -147,7 +147,6 @@ __global__ void __launch_bounds__(kColThreads, 4) k_gn_colstats(const T* x, GnSh
   using PV = Pairs<V>;
   __shared__ float2 red[kColThreads * V];
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const ColPlace p(s, g, false);
   uint64_t np[PV::N], a1[PV::N], a2[PV::N];
 #pragma unroll
@@ -270,7 +269,6 @@ __global__ void __launch_bounds__(THREADS) k_gn_fold(const T* x, const float2* p
                                                           float* mean_out, float* rstd_out) {
   __shared__ float sm[THREADS / 32];
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const int b = (int)g.by_G.div(blockIdx.x), gr = (int)blockIdx.x - b * s.G;
   Cells<THREADS> cells(part + (long long)b * g.chunks * s.C + gr * s.Cg);
   const float total = (float)s.S * (float)s.Cg;
@@ -294,7 +292,6 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
                                                           T* y) {
   using PV = Pairs<V>;
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const ColPlace p(s, g, true);
   if (!p.on) return;
   float a[V], b[V];
@@ -377,7 +374,6 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
   using PV = Pairs<V>;
   __shared__ float2 red[kColThreads * V];
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const ColPlace p(s, g, false);
   uint64_t p0[PV::N], p1[PV::N];
 #pragma unroll
@@ -484,7 +480,6 @@ __global__ void __launch_bounds__(THREADS) k_gn_grad_fold(const float2* part, Gn
                                                                float* dgamma, float* dbeta) {
   __shared__ float sm[THREADS / 32];
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   if ((int)blockIdx.x < param_blocks) {
     param_fold<THREADS / kFoldCols>((int)blockIdx.x, part, GnFold{(long long)s.n * g.chunks, 0, 0, 0}, s.C, dgamma,
                                          dbeta);
@@ -511,7 +506,6 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
                                                                const float2* avg, T* dx) {
   using PV = Pairs<V>;
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   const ColPlace p(s, g, true);
   if (!p.on) return;
   const GradCols<V> k(s, g, p, mean, rstd, gamma, beta);

@@ -112,7 +112,6 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
   const int stage = q.nv * q.T;
   const int u0 = (int)blockIdx.x * q.units, u1 = min(q.total, u0 + q.units);
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   Cursor cur(u0, s, q), ahead = cur;
   const long long xstep = (long long)q.TR * s.ldx, ystep = (long long)q.TR * s.ldy;
   float pivot = 0.f;  // the next unit's group's
@@ -249,7 +248,6 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q,
   const int block = (int)blockIdx.x;
   const int u0 = block * q.units, u1 = min(q.total, u0 + q.units);
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   Cursor cur(u0, s, q), ahead = cur;
   const long long xstep = (long long)q.TR * s.ldx, dstep = (long long)q.TR * s.lddy, ostep = (long long)q.TR * s.ldy;
   float nmu = 0.f, nrs = 0.f;

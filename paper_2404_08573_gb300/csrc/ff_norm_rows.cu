@@ -139,7 +139,6 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps) k_gn_rows(G
   Adder<WIDE> add{tmp, pl.lanes};
   const int c0 = w.active ? w.g * s.Cg : 0;
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   constexpr int N = NV * V / 2;
   uint64_t ga[N], be[N];
   params<V, NV>(ga, be, a, sl, c0);
@@ -214,7 +213,6 @@ __global__ void __launch_bounds__(WIDE ? kMostThreads : 32 * kWarps)
   Adder<WIDE> add{tmp, pl.lanes};
   const int c0 = w.active ? w.g * s.Cg : 0;
   ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
   constexpr int N = NV * V / 2;
   uint64_t ga[N], be[N], p0[N], p1[N];
   params<V, NV>(ga, be, a, sl, c0);

@@ -76,7 +76,8 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, unsign
 // that kernel has completed and its memory is visible (a no-op for a kernel
 // launched without the attribute).  griddep_launch_dependents() lets the
 // next such kernel start early once every CTA of this grid has issued it or
-// exited.
+// exited; a kernel issues it after its main loop or not at all, never as soon
+// as it has waited.
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void griddep_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
