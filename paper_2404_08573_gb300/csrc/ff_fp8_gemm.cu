@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       for (int it = 0; it < total; ++it) {
         const uint32_t b = (uint32_t)it & 1u;
         const bool ok = ptx::mbar_wait(&full[s], ph, kWaitTimeoutNs, abort_flag) &&
-                        ptx::mbar_wait(&te[b], tph, kWaitTimeoutNs, abort_flag);
+                        ptx::mbar_wait_cluster(&te[b], tph, kWaitTimeoutNs, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) {
           latch(g.err, abort_flag);
           break;
@@ -423,8 +423,9 @@ __global__ void __launch_bounds__(LTHREADS, 1)
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-              // the arrival orders TMEM reads only (the fence above), so it
-              // needs no cluster-wide release of memory
+              // TMEM reads that have completed (the wait above, and the fence):
+              // nothing to release, only an arrival that the issuing CTA sees
+              // (a release at cluster scope: 4096 x 8192 x 8192 in 430 us)
               ptx::mbar_arrive_at(te0 + 8u * b);
               // the scales of the group before this k-block are used up
               if (it % LGROUP == 0 && it > 0) ptx::mbar_arrive(&sempty[(it / LGROUP - 1) % LGROUPS]);

@@ -130,10 +130,11 @@ __device__ __forceinline__ void mbar_arrive_remote(uint64_t* local_bar, uint32_t
   const uint32_t a = mapa_shared(smem_u32(local_bar), rank);
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
 }
-// Arrives on the mbarrier at a shared::cluster address (this or another CTA's)
-// without cluster-scope release.
+// Arrives (cluster scope, no release) on the mbarrier at a shared::cluster
+// address (this or another CTA's): for handing back what this thread has
+// finished reading, where no write of its own has to become visible.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // try_wait with cluster-scope acquire: for phases completed by other CTAs' arrivals.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
