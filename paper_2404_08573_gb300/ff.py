@@ -685,21 +685,33 @@ _ACT = {"none": 0, "relu": 1, "silu": 2}
 _INT_MAX = 0x7FFFFFFF
 
 
-def _on(stream, device):
-    """The stream of an operator call, and what allocates its buffers.  A
-    buffer allocated while another stream is current is marked as used on this
-    one, so that its memory is not handed out again before the call has run."""
+def _on(stream, device, *used):
+    """The stream of an operator call, and what allocates its buffers.  On a
+    stream that is not the current one they come from that stream's own pool,
+    since the current one's may hand out memory that its queued kernels still
+    use; and they count as used on the current one, where the caller goes on
+    with them.  `used`: the caller's tensors, which count as used on the call's
+    stream (so freeing one after the call is safe).  What the stream has to
+    wait for before the call stays the caller's business."""
     current = torch._C._cuda_getCurrentRawStream(device.index)
     if stream is None:
         return current, torch.empty
     ptr = _stream(stream)
     if ptr == current:
         return current, torch.empty
-    other = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(ptr, device)
+    if isinstance(stream, torch.cuda.Stream):
+        other = stream
+    else:
+        other = torch.cuda.ExternalStream(ptr, device) if ptr else torch.cuda.default_stream(device)
+    here = torch.cuda.current_stream(device)
+    for t in used:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(other)
 
     def empty(shape, dtype, device):
-        t = torch.empty(shape, dtype=dtype, device=device)
-        t.record_stream(other)
+        with torch.cuda.stream(other):
+            t = torch.empty(shape, dtype=dtype, device=device)
+        t.record_stream(here)
         return t
 
     return ptr, empty
@@ -808,7 +820,7 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     (y, mean, rstd), mean and rstd fp32 [n, groups]; out may be x."""
     prec, dev = _prec(x, "x"), x.device
     n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 0)
-    on, empty = _on(stream, dev)
+    on, empty = _on(stream, dev, x, gamma, beta, out, mean, rstd)
     ldx = _row_stride_of(x, "x")
     if out is None:
         out, ldy = empty(x.shape, dtype=x.dtype, device=dev), C
@@ -839,7 +851,7 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     out may be dy or x."""
     prec, dev = _prec(x, "x"), x.device
     n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 1)
-    on, empty = _on(stream, dev)
+    on, empty = _on(stream, dev, dy, x, mean, rstd, gamma, beta, out)
     ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
     if out is None:
         out, lddx = empty(x.shape, dtype=x.dtype, device=dev), C
@@ -875,7 +887,7 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     if x.dim() < 1:
         raise ValueError("x must have at least one dimension")
     dev = x.device
-    on, empty = _on(stream, dev)
+    on, empty = _on(stream, dev, x, offset, residual, out)
     cols = x.shape[-1]
     rows = x.numel() // cols if cols else 0
     ldx = _row_stride_of(x, "x")
@@ -937,7 +949,7 @@ def _fp8_quantize(x, tile, straight, transposed, stream):
     if x.dim() != 2 or x.shape[1] < 1:
         raise ValueError("x must be [rows, k] with k >= 1")
     dev = x.device
-    on, empty = _on(stream, dev)
+    on, empty = _on(stream, dev, x)
     rows, k = x.shape
     if max(rows, k) > _INT_MAX:
         raise ValueError("rows and k must each fit 32 bits")
@@ -979,7 +991,7 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
         raise ValueError("a must be quantized in row blocks")
     dev = a.q.device
     _same_device(b.q, dev, "b")
-    on, empty = _on(stream, dev)
+    on, empty = _on(stream, dev, a.q, a.scale, b.q, b.scale, bias, out, status)
     m, n = a.rows, b.rows
     if out is None:
         prec = _PREC.get(out_dtype)
