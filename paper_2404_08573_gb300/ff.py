@@ -185,6 +185,38 @@ def _ptr(t, dtype=None, what="tensor", need_cuda=True):
     return t.data_ptr()
 
 
+def _on(stream, device, *used):
+    """The stream of an operator call, and what allocates its buffers.  On a
+    stream that is not the current one they come from that stream's own pool,
+    since the current one's may hand out memory that its queued kernels still
+    use; and they count as used on the current one, where the caller goes on
+    with them.  `used`: the caller's tensors, which count as used on the call's
+    stream (so freeing one after the call is safe).  What the stream has to
+    wait for before the call stays the caller's business."""
+    current = torch._C._cuda_getCurrentRawStream(device.index)
+    if stream is None:
+        return current, torch.empty
+    ptr = _stream(stream)
+    if ptr == current:
+        return current, torch.empty
+    if isinstance(stream, torch.cuda.Stream):
+        other = stream
+    else:
+        other = torch.cuda.ExternalStream(ptr, device) if ptr else torch.cuda.default_stream(device)
+    here = torch.cuda.current_stream(device)
+    for t in used:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(other)
+
+    def empty(shape, dtype, device):
+        with torch.cuda.stream(other):
+            t = torch.empty(shape, dtype=dtype, device=device)
+        t.record_stream(here)
+        return t
+
+    return ptr, empty
+
+
 def act_dtype(prec: str):
     return torch.bfloat16 if prec == "bf16" else torch.float32
 
@@ -327,11 +359,13 @@ class Layer:
 def overlay_label(x, labels, prec="bf16", out=None, row_scale=None, stream=None):
     """ff_overlay_label: returns the overlaid activation buffer."""
     rows, F = x.shape
+    px = _ptr(x, torch.float32, "x")
+    on, empty = _on(stream, x.device, x, labels, out, row_scale)
     if out is None:
-        out = torch.empty(rows, row_stride(F), dtype=act_dtype(prec), device=x.device)
-    _check(lib().ff_overlay_label(_ptr(x, torch.float32, "x"), _ptr(labels, torch.int32, "labels"), rows, F,
+        out = empty((rows, row_stride(F)), dtype=act_dtype(prec), device=x.device)
+    _check(lib().ff_overlay_label(px, _ptr(labels, torch.int32, "labels"), rows, F,
                                   _ptr(out, act_dtype(prec), "out"), _ptr(row_scale, torch.float32, "row_scale"),
-                                  FF_BF16 if prec == "bf16" else FF_FP32, c_void_p(_stream(stream))),
+                                  FF_BF16 if prec == "bf16" else FF_FP32, c_void_p(on)),
            "ff_overlay_label")
     return out
 
@@ -339,11 +373,13 @@ def overlay_label(x, labels, prec="bf16", out=None, row_scale=None, stream=None)
 def predict(layers, x, pred=None, goodness=None, stream=None):
     """ff_predict: goodness prediction over the 10 label overlays.  Returns (pred, goodness)."""
     n = x.shape[0]
+    px = _ptr(x, torch.float32, "x")
+    on, empty = _on(stream, x.device, x, pred, goodness)
     if pred is None:
-        pred = torch.empty(n, dtype=torch.int32, device=x.device)
+        pred = empty((n,), dtype=torch.int32, device=x.device)
     arr = (c_void_p * len(layers))(*[l.handle.value for l in layers])
-    _check(lib().ff_predict(arr, len(layers), _ptr(x, torch.float32, "x"), n, _ptr(pred, torch.int32, "pred"),
-                            _ptr(goodness, torch.float32, "goodness"), c_void_p(_stream(stream))), "ff_predict")
+    _check(lib().ff_predict(arr, len(layers), px, n, _ptr(pred, torch.int32, "pred"),
+                            _ptr(goodness, torch.float32, "goodness"), c_void_p(on)), "ff_predict")
     return pred, goodness
 
 
@@ -353,12 +389,14 @@ def adaptive_negatives(layers, x, labels, neg=None, goodness=None, stream=None):
     n = x.shape[0]
     if labels.shape[0] != n:
         raise ValueError("labels must have one entry per row of x")
+    px = _ptr(x, torch.float32, "x")
+    on, empty = _on(stream, x.device, x, labels, neg, goodness)
     if neg is None:
-        neg = torch.empty(n, dtype=torch.int32, device=x.device)
+        neg = empty((n,), dtype=torch.int32, device=x.device)
     arr = (c_void_p * len(layers))(*[l.handle.value for l in layers])
-    _check(lib().ff_adaptive_negatives(arr, len(layers), _ptr(x, torch.float32, "x"),
+    _check(lib().ff_adaptive_negatives(arr, len(layers), px,
                                        _ptr(labels, torch.int32, "labels"), n, _ptr(neg, torch.int32, "neg"),
-                                       _ptr(goodness, torch.float32, "goodness"), c_void_p(_stream(stream))),
+                                       _ptr(goodness, torch.float32, "goodness"), c_void_p(on)),
            "ff_adaptive_negatives")
     return neg, goodness
 
@@ -509,11 +547,13 @@ class Head:
     def predict(self, layers, x, pred=None, logits=None, stream=None):
         """Returns (pred, logits)."""
         n = x.shape[0]
+        px = _ptr(x, torch.float32, "x")
+        on, empty = _on(stream, x.device, x, pred, logits)
         if pred is None:
-            pred = torch.empty(n, dtype=torch.int32, device=x.device)
-        _check(lib().ff_head_predict(self._h, _layer_array(layers), len(layers), _ptr(x, torch.float32, "x"), n,
+            pred = empty((n,), dtype=torch.int32, device=x.device)
+        _check(lib().ff_head_predict(self._h, _layer_array(layers), len(layers), px, n,
                                      _ptr(pred, torch.int32, "pred"), _ptr(logits, torch.float32, "logits"),
-                                     c_void_p(_stream(stream))), "ff_head_predict")
+                                     c_void_p(on)), "ff_head_predict")
         return pred, logits
 
     def get_state(self):
@@ -616,11 +656,13 @@ def po_train_step_act(layer, block, x, labels, row_scale=None, h_out=None, next_
 def po_predict(layers, block, x, pred=None, logits=None, stream=None):
     """ff_po_predict: the last layer's block's prediction.  Returns (pred, logits)."""
     n = x.shape[0]
+    px = _ptr(x, torch.float32, "x")
+    on, empty = _on(stream, x.device, x, pred, logits)
     if pred is None:
-        pred = torch.empty(n, dtype=torch.int32, device=x.device)
-    _check(lib().ff_po_predict(_layer_array(layers), len(layers), block._h, _ptr(x, torch.float32, "x"), n,
+        pred = empty((n,), dtype=torch.int32, device=x.device)
+    _check(lib().ff_po_predict(_layer_array(layers), len(layers), block._h, px, n,
                                _ptr(pred, torch.int32, "pred"), _ptr(logits, torch.float32, "logits"),
-                               c_void_p(_stream(stream))), "ff_po_predict")
+                               c_void_p(on)), "ff_po_predict")
     return pred, logits
 
 
@@ -683,38 +725,6 @@ class PoNet(Net):
 _PREC = {torch.bfloat16: FF_BF16, torch.float32: FF_FP32}
 _ACT = {"none": 0, "relu": 1, "silu": 2}
 _INT_MAX = 0x7FFFFFFF
-
-
-def _on(stream, device, *used):
-    """The stream of an operator call, and what allocates its buffers.  On a
-    stream that is not the current one they come from that stream's own pool,
-    since the current one's may hand out memory that its queued kernels still
-    use; and they count as used on the current one, where the caller goes on
-    with them.  `used`: the caller's tensors, which count as used on the call's
-    stream (so freeing one after the call is safe).  What the stream has to
-    wait for before the call stays the caller's business."""
-    current = torch._C._cuda_getCurrentRawStream(device.index)
-    if stream is None:
-        return current, torch.empty
-    ptr = _stream(stream)
-    if ptr == current:
-        return current, torch.empty
-    if isinstance(stream, torch.cuda.Stream):
-        other = stream
-    else:
-        other = torch.cuda.ExternalStream(ptr, device) if ptr else torch.cuda.default_stream(device)
-    here = torch.cuda.current_stream(device)
-    for t in used:
-        if isinstance(t, torch.Tensor) and t.is_cuda:
-            t.record_stream(other)
-
-    def empty(shape, dtype, device):
-        with torch.cuda.stream(other):
-            t = torch.empty(shape, dtype=dtype, device=device)
-        t.record_stream(here)
-        return t
-
-    return ptr, empty
 
 
 def _on_device_of_first(f):

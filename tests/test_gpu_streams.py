@@ -104,3 +104,18 @@ def test_a_stream_given_by_its_number():
         back = ff.dropout(x, 0.3, 5, stream=0)  # the default stream, from another one
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(back, want)
+
+
+def test_labels_and_predictions():
+    torch = torch_cuda()
+    ff = lib_ready()
+    from paper_2404_08573_gb300 import synth
+    layers = [ff.Layer(784, 256, prec="bf16", init_seed=3), ff.Layer(256, 136, prec="bf16", init_seed=4)]
+    x = torch.from_numpy(synth.mnist_like(3000, seed=20)).cuda()
+    y = torch.from_numpy(synth.labels(3000, seed=21)).cuda()
+    head, block = ff.Head(136, lr=1e-3, max_rows=512), ff.Head(136, lr=1e-3)
+    check(lambda s: ff.overlay_label(x, y, stream=s))
+    check(lambda s: ff.predict(layers, x, stream=s)[0])
+    check(lambda s: ff.adaptive_negatives(layers, x, y, stream=s)[0])
+    check(lambda s: head.predict(layers, x, stream=s)[0])
+    check(lambda s: ff.po_predict(layers, block, x, stream=s)[0])
