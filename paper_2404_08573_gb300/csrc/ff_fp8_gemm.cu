@@ -788,12 +788,16 @@ cudaError_t launch(F* kernel, unsigned grid, int threads, int cluster, int smem,
 // its cluster group stays out); 0 if the pair kernel was not built with the
 // registers that its split counts on, and so must not run.
 template <bool COLS, bool TMA_C, bool BF16>
-int resident_pairs() {
-  static const int n = [] {
+int resident_pairs(int dev) {
+  static PerDevice<int> kept;
+  int n = 0;
+  const cudaError_t e = kept.get(dev, &n, [](int* pairs) {
     cudaFuncAttributes fa{};
     constexpr auto kernel = k_fp8_pair<COLS, TMA_C, BF16>;
-    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs != LREGS) return 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM) != cudaSuccess) return 0;
+    cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
+    if (e != cudaSuccess || fa.numRegs != LREGS) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(LTHREADS);
@@ -804,25 +808,15 @@ int resident_pairs() {
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    int c = 0;
-    if (cudaOccupancyMaxActiveClusters(&c, kernel, &cfg) != cudaSuccess) {
-      cudaGetLastError();
-      return 0;
-    }
-    return c;
-  }();
-  return n;
+    return cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg);
+  });
+  if (e != cudaSuccess) cudaGetLastError();  // leave no error behind: the split kernel runs
+  return e == cudaSuccess ? n : 0;
 }
 
 template <int BN, bool COLS>
-cudaError_t split_attr() {
-  static const cudaError_t e =
-      cudaFuncSetAttribute(k_fp8_split<BN, COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SCfg<BN>::SMEM);
-  return e;
-}
-template <int BN, bool COLS>
 cudaError_t run_split(const CUtensorMap& p, const CUtensorMap& q, const Args& g, int ks_log, cudaStream_t st) {
-  const cudaError_t e = split_attr<BN, COLS>();
+  const cudaError_t e = allow_smem<k_fp8_split<BN, COLS>>(SCfg<BN>::SMEM);
   if (e != cudaSuccess) return e;
   return launch(k_fp8_split<BN, COLS>, (unsigned)(g.ntp * g.ntq) << ks_log, THREADS, 1 << ks_log, SCfg<BN>::SMEM, st, p, q, g,
                 ks_log);
@@ -830,11 +824,13 @@ cudaError_t run_split(const CUtensorMap& p, const CUtensorMap& q, const Args& g,
 
 // Clusters of a split kernel the GPU holds at once.
 template <int BN, bool COLS>
-int resident_clusters(int ks_log) {
+int resident_clusters(int dev, int ks_log) {
   struct Counts { int n[4]; };
-  static const Counts c = [] {
-    Counts r{};
-    if (split_attr<BN, COLS>() != cudaSuccess) return r;
+  static PerDevice<Counts> kept;
+  Counts c{};
+  const cudaError_t e = kept.get(dev, &c, [](Counts* r) {
+    cudaError_t e = allow_smem<k_fp8_split<BN, COLS>>(SCfg<BN>::SMEM);
+    if (e != cudaSuccess) return e;
     for (int l = 0; l < 4; ++l) {
       cudaLaunchConfig_t cfg = {};
       cfg.gridDim = dim3(1u << l);
@@ -846,21 +842,20 @@ int resident_clusters(int ks_log) {
       at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
       cfg.attrs = at;
       cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&r.n[l], k_fp8_split<BN, COLS>, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        r.n[l] = 0;
-      }
+      e = cudaOccupancyMaxActiveClusters(&r->n[l], k_fp8_split<BN, COLS>, &cfg);
+      if (e != cudaSuccess) return e;
     }
-    return r;
-  }();
-  return c.n[ks_log];
+    return cudaSuccess;
+  });
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? c.n[ks_log] : 0;
 }
-int clusters_of(int bn, bool each, int ks_log) {
+int clusters_of(int dev, int bn, bool each, int ks_log) {
   switch (bn) {
-    case 16: return resident_clusters<16, true>(ks_log);
-    case 32: return resident_clusters<32, true>(ks_log);
-    case 64: return resident_clusters<64, true>(ks_log);
-    default: return each ? resident_clusters<128, true>(ks_log) : resident_clusters<128, false>(ks_log);
+    case 16: return resident_clusters<16, true>(dev, ks_log);
+    case 32: return resident_clusters<32, true>(dev, ks_log);
+    case 64: return resident_clusters<64, true>(dev, ks_log);
+    default: return each ? resident_clusters<128, true>(dev, ks_log) : resident_clusters<128, false>(dev, ks_log);
   }
 }
 
@@ -874,7 +869,7 @@ struct Plan {
   bool swap;
   int ks_log;
 };
-Plan plan(int M, int N, int K, bool cols, int pairs) {
+Plan plan(int dev, int M, int N, int K, bool cols, int pairs) {
   const double nkb = cdiv(K, KB);
   Plan best{LN, false, 0};
   double t = 1e30;
@@ -891,7 +886,7 @@ Plan plan(int M, int N, int K, bool cols, int pairs) {
     const double tiles = (double)cdiv(P, BM) * cdiv(Q, sh.bn);
     const double moved = tiles * nkb * (BM + sh.bn) * KB / 9e6;
     for (int l = 0; l < 4; ++l) {
-      const int room = clusters_of(sh.bn, sh.swap || cols, l);
+      const int room = clusters_of(dev, sh.bn, sh.swap || cols, l);
       if ((1 << l) > nkb || room < 1) break;
       const double waves = std::ceil(tiles / room), per = std::ceil(nkb / (1 << l));
       const double c = sh.fixed + (l ? 0.5 : 0.0) + std::max(moved, waves * per * sh.step + (waves - 1) * sh.fixed);
@@ -909,13 +904,15 @@ Plan plan(int M, int N, int K, bool cols, int pairs) {
 ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
   const int ld = fp8_stride(f.K);
   const bool cols = !f.b_tiles;
+  int dev = 0;
+  FF_TRY(cudaGetDevice(&dev), "8-bit matrix product");
   auto room = [&](auto c, auto b) {
-    return std::min(resident_pairs<c.value, true, b.value>(), resident_pairs<c.value, false, b.value>());
+    return std::min(resident_pairs<c.value, true, b.value>(dev), resident_pairs<c.value, false, b.value>(dev));
   };
   using Y = std::true_type;
   using N = std::false_type;
   const int pairs = cols ? (f.out_bf16 ? room(Y{}, Y{}) : room(Y{}, N{})) : (f.out_bf16 ? room(N{}, Y{}) : room(N{}, N{}));
-  const Plan pl = plan(f.M, f.N, f.K, cols, pairs);
+  const Plan pl = plan(dev, f.M, f.N, f.K, cols, pairs);
   Args g{};
   const Scales sa{f.sa, f.M, 0};
   const Scales sb{f.sb, f.b_tiles ? cdiv(f.N, KB) : f.N, f.b_tiles ? 7 : 0};
@@ -932,6 +929,7 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
   g.ldc = f.ldc;
   g.err = f.status;
   const bool pairk = pl.bn == LN;
+  if (pairk && pairs < 1) return FF_ERR_UNSUPPORTED;  // no kernel fits this device
   g.ntp = cdiv(g.P, pairk ? 2 * BM : BM);
   g.ntq = cdiv(g.Q, pl.bn);
   if ((long long)g.ntp * g.ntq << pl.ks_log > 0x3FFFFFFFll) return FF_ERR_UNSUPPORTED;

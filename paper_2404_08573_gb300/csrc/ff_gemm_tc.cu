@@ -218,15 +218,14 @@ struct TcLaunch {
     cfg.attrs = at;
     cfg.numAttrs = 2;
   }
-  static auto kernel() {
+  static constexpr auto kernel() {
     if constexpr (KB == 64)
       return k_tc_gemm_r88<BN, A_MN, B_MN, MODE, PAIR, NSTAGE, MT, NT, OPB, KB>;
     else
       return k_tc_gemm<BN, A_MN, B_MN, MODE, PAIR, NSTAGE, MT, NT, OPB, KB>;
   }
   static cudaError_t set_attrs() {
-    static cudaError_t e = cudaFuncSetAttribute(kernel(), cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    return e;
+    return allow_smem<kernel()>(SMEM);
   }
 };
 
@@ -341,25 +340,26 @@ constexpr int kLgMaxColTiles = 4;
 
 bool tc_fwd_lg_supported(int M, int N) {
   if (M <= 0 || N <= 0 || cdiv(N, 2 * FWD_BN) > kLgMaxColTiles) return false;
-  // clusters of 2 x (column tiles) CTAs must fit the GPU (checked once per column-tile count)
-  static int ok[kLgMaxColTiles + 1] = {0, 0, 0, 0, 0};  // 0 unknown, 1 yes, -1 no
+  // clusters of 2 x (column tiles) CTAs must fit the GPU (checked once per device and column-tile count)
+  static PerDevice<int> counts[kLgMaxColTiles + 1];
   const int ct = cdiv(N, 2 * FWD_BN);
-  if (ok[ct] == 0) {
-    int clusters = 0;
+  int dev = 0, clusters = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const cudaError_t found = counts[ct].get(dev, &clusters, [&](int* clusters) {
     cudaError_t e = FwdLg::set_attrs();
     if (e == cudaSuccess) {
       // the occupancy query takes the cluster shape alone (no other launch attributes)
       FwdLg l(2 * BM, ct * 2 * FWD_BN, nullptr);
       l.cfg.numAttrs = 1;
-      e = cudaOccupancyMaxActiveClusters(&clusters, FwdLg::kernel(), &l.cfg);
+      e = cudaOccupancyMaxActiveClusters(clusters, FwdLg::kernel(), &l.cfg);
     }
     if (e != cudaSuccess) cudaGetLastError();  // leave no sticky launch-configuration error behind
     if (std::getenv("FF_DEBUG"))
       std::fprintf(stderr, "[ff] forward with local gradient, %d column tiles: %d clusters of %d CTAs (%s)\n", ct,
-                   clusters, 2 * ct, cudaGetErrorString(e));
-    ok[ct] = e == cudaSuccess && clusters > 0 ? 1 : -1;
-  }
-  return ok[ct] > 0;
+                   *clusters, 2 * ct, cudaGetErrorString(e));
+    return e;
+  });
+  return found == cudaSuccess && clusters > 0;
 }
 
 cudaError_t tc_gemm_fwd_lg(const bf16* A, int lda, const bf16* B, int ldb, int M, int N, int K, const EpiArgs& ep,

@@ -945,11 +945,8 @@ ff_status head_logits(ff_head* hd, const Segs& sg, bool b16, int n, const int* l
   for (int k = 0; k < sg.nseg; ++k)
     if (!make_plain_map(&maps.m[k], sg.H[k], es, sg.ld[k], n, sg.ld[k], 512 / es, kDotRows))
       return FF_ERR_INVALID_ARG;
-  static const cudaError_t attr_b = cudaFuncSetAttribute(k_head_dot<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                         kDotSmem);
-  static const cudaError_t attr_f = cudaFuncSetAttribute(k_head_dot<float>,
-                                                         cudaFuncAttributeMaxDynamicSharedMemorySize, kDotSmem);
-  FF_TRY(b16 ? attr_b : attr_f, "head kernel attributes");
+  FF_TRY(b16 ? allow_smem<k_head_dot<bf16>>(kDotSmem) : allow_smem<k_head_dot<float>>(kDotSmem),
+         "head kernel attributes");
   dim3 grid(S, cdiv(n, kDotRows));
   PdlLaunch l(grid, dim3(256), st, kDotSmem);
   FF_LAUNCH(K_HEAD_LOGITS, (double)n * sg.F_total * es + (double)n * (2 * S + 2) * kClasses * 4, st,

@@ -9,6 +9,7 @@
 #include <cstdint>
 
 #include "ff.h"
+#include "ff_per_device.h"
 
 typedef __nv_bfloat16 bf16;
 
@@ -221,6 +222,20 @@ struct AdamArgs {
 // Adds [p, p + bytes) to the Adam step's dead buffers (its whole 128-byte
 // lines; nothing when p is not 128-byte aligned).
 void add_dead(AdamArgs& a, void* p, size_t bytes);
+
+// Allows launches of KERNEL up to `bytes` of dynamic shared memory on the
+// current device (an attribute belongs to one device).
+template <auto KERNEL>
+cudaError_t allow_smem(int bytes) {
+  static PerDevice<int> allowed;
+  int dev = 0, got = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  return allowed.get(dev, &got, [&](int* v) {
+    *v = bytes;
+    return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  });
+}
 
 // Launch configuration with programmatic stream serialization: the kernel
 // may start while the previous kernel of the stream finishes and waits for it

@@ -438,9 +438,7 @@ int stage_bytes(int T, int nv, int V, int esize, bool grad) {
 template <auto KERNEL, typename... A>
 ff_status run(KernelKind kind, double bytes, const Geom& q, const GnBlockPlan& p, int smem, cudaStream_t st,
               const A&... args) {
-  static const cudaError_t attr =
-      cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-  FF_TRY(attr, "group norm");
+  FF_TRY(allow_smem<KERNEL>(kSmem), "group norm");
   PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)q.T), st, (size_t)smem);
   FF_LAUNCH(kind, bytes, st, cudaLaunchKernelEx(&l.cfg, KERNEL, args...), "group norm");
   return FF_OK;
