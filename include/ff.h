@@ -619,12 +619,24 @@ FF_API ff_status ff_fp8_quantize(const void* x, long long ldx, int rows, int k, 
  * The layer's three products: y = x w^T with A = rows(x), B = tiles(w);
  * dx = dy w with A = rows(dy), B = the transposed tiles of w; dw = dy^T x with
  * A and B = the transposed rows of dy and x.
- * k >= 1; m == 0 or n == 0 is a no-op.  device_status [1] int or NULL: OR-ed
- * with 1 (never cleared) if a kernel wait timed out, in which case C is not
- * valid.  Needs an sm_100-family GPU (FF_ERR_UNSUPPORTED otherwise). */
+ * k >= 1; m == 0 or n == 0 is a no-op.  device_status [1] int: OR-ed with 1
+ * (never cleared) if a kernel wait timed out, in which case C is not valid;
+ * NULL: the device's own word, which ff_fp8_check reads.  The product of two
+ * blocks' scales is formed first and must be finite itself: finite operands
+ * whose largest magnitudes multiply to 2^145 or more may give infinities or
+ * NaN.  Needs an sm_100-family GPU (FF_ERR_UNSUPPORTED otherwise). */
 FF_API ff_status ff_fp8_matmul(const void* a, const float* a_scale, const void* b, const float* b_scale,
                                ff_fp8_blocks b_blocks, int m, int n, int k, const float* bias, int relu,
                                ff_precision out_prec, void* c, long long ldc, int* device_status, void* stream);
+
+/* Waits for `stream` and returns FF_ERR_TIMEOUT if a wait of an 8-bit product
+ * without a device_status of its own timed out on the current device since the
+ * last check (on whatever stream), then clears that. */
+FF_API ff_status ff_fp8_check(void* stream);
+
+/* Self-test of the above: as ff_layer_selftest_wait, latched where
+ * ff_fp8_check reads it. */
+FF_API ff_status ff_fp8_selftest_wait(unsigned int timeout_us, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Instrumentation (not part of the method).

@@ -254,6 +254,20 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, int tile, uint8
   return FF_OK;
 }
 
+// Where products without a status word of the caller's latch a timeout: a word
+// on each device, so that no invalid result goes unreported.
+__device__ int g_fp8_status;
+cudaError_t own_status(int** word) {
+  static PerDevice<void*> kept;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  void* p = nullptr;
+  e = kept.get(dev, &p, [](void** p) { return cudaGetSymbolAddress(p, g_fp8_status); });
+  *word = static_cast<int*>(p);
+  return e;
+}
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
@@ -314,5 +328,25 @@ extern "C" FF_API ff_status ff_fp8_matmul(const void* a, const float* a_scale, c
   g.c = c;
   g.ldc = ldc;
   g.status = device_status;
+  if (!device_status) FF_TRY(own_status(&g.status), "8-bit matrix product");
   return fp8_gemm(g, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" FF_API ff_status ff_fp8_check(void* stream) {
+  int *word = nullptr, err = 0;
+  FF_TRY(own_status(&word), "8-bit check");
+  FF_TRY(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)), "8-bit check");
+  FF_TRY(cudaMemcpy(&err, word, sizeof(int), cudaMemcpyDeviceToHost), "8-bit check");
+  if (!err) return FF_OK;
+  const int zero = 0;
+  FF_TRY(cudaMemcpy(word, &zero, sizeof(int), cudaMemcpyHostToDevice), "8-bit check");
+  return FF_ERR_TIMEOUT;
+}
+
+extern "C" FF_API ff_status ff_fp8_selftest_wait(unsigned int timeout_us, void* stream) {
+  if (timeout_us < 1 || timeout_us > 10000000u) return FF_ERR_INVALID_ARG;
+  int* word = nullptr;
+  FF_TRY(own_status(&word), "8-bit self-test");
+  FF_TRY(launch_wait_selftest(word, 1000ull * timeout_us, static_cast<cudaStream_t>(stream)), "8-bit self-test");
+  return FF_OK;
 }

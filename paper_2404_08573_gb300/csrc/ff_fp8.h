@@ -16,7 +16,7 @@ struct Fp8Gemm {
   bool relu, out_bf16;
   void* c;
   long long ldc;
-  int* status;            // or null
+  int* status;            // latches timeouts
 };
 
 ff_status fp8_gemm(const Fp8Gemm& g, cudaStream_t st);

@@ -17,7 +17,7 @@
 //   warps 2..9  epilogue: TMEM lane quarter warp % 4, half of the columns each
 //
 // Every mbarrier wait is bounded; one that runs out latches DEVERR_TIMEOUT in
-// the caller's status word, stops the other roles, and the CTA lets its
+// the call's status word, stops the other roles, and the CTA lets its
 // copies and MMAs land before it frees TMEM and exits.
 #include <algorithm>
 #include <cmath>
@@ -38,7 +38,7 @@ constexpr int THREADS = 64 + 32 * EPI;
 
 __device__ __forceinline__ void latch(int* err, volatile int* abort_flag) {
   *abort_flag = 1;
-  if (err) atomicOr(err, DEVERR_TIMEOUT);
+  atomicOr(err, DEVERR_TIMEOUT);
 }
 
 // One operand's scales: block kb of row i is p[kb * stride + (i >> shift)].
@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(LTHREADS, 1)
             if (lane == 0) {
               // TMEM reads that have completed (the wait above, and the fence):
               // nothing to release, only an arrival that the issuing CTA sees
-              // (a release at cluster scope: 4096 x 8192 x 8192 in 430 us)
+              // (a release at cluster scope: 4096 x 8192 x 8192 with its quantizer
+              // 461 us in place of 221)
               ptx::mbar_arrive_at(te0 + 8u * b);
               // the scales of the group before this k-block are used up
               if (it % LGROUP == 0 && it > 0) ptx::mbar_arrive(&sempty[(it / LGROUP - 1) % LGROUPS]);

@@ -136,6 +136,8 @@ def lib():
                                 c_void_p],
             "ff_fp8_matmul": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_int, c_int,
                               c_void_p, c_longlong, c_void_p, c_void_p],
+            "ff_fp8_check": [c_void_p],
+            "ff_fp8_selftest_wait": [ctypes.c_uint, c_void_p],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -992,7 +994,8 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     """ff_fp8_matmul: act(a b^T + bias) of two Fp8Matrix (a in row blocks).
     Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
     out's type; bias fp32 [b.rows]; status: a one-element int32 CUDA tensor
-    that is OR-ed with 1 if a kernel wait timed out."""
+    that is OR-ed with 1 if a kernel wait timed out; without one, fp8_check
+    reports it."""
     if not isinstance(a, Fp8Matrix) or not isinstance(b, Fp8Matrix):
         raise TypeError("a and b must be Fp8Matrix")
     if a.k != b.k:
@@ -1019,3 +1022,15 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
                                n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
                                _ptr(status, torch.int32, "status"), on), "ff_fp8_matmul")
     return out
+
+
+def fp8_check(stream=None):
+    """ff_fp8_check: waits for the stream and raises if a wait of an fp8_matmul
+    that was given no status timed out on the current device (its result is
+    not valid)."""
+    _check(lib().ff_fp8_check(c_void_p(_stream(stream))), "ff_fp8_check")
+
+
+def fp8_selftest_wait(timeout_us: int, stream=None):
+    """ff_fp8_selftest_wait: a bounded wait that is made to run out, for fp8_check to report."""
+    _check(lib().ff_fp8_selftest_wait(int(timeout_us), c_void_p(_stream(stream))), "ff_fp8_selftest_wait")
