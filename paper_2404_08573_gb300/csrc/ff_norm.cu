@@ -332,11 +332,13 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
   });
 }
 
-// What the gradient's passes share: a column's constants.  h = x rs + o,
-// u = gamma h + beta.
+// What the gradient's passes share: a column's constants.  h = (x - mean) rs,
+// u = gamma h + beta.  The mean is taken off first: x rs - mean rs in one
+// multiply-add would bring the rounding of mean rs into h, mean / spread
+// rounding units instead of one.
 template <int V>
 struct GradCols {
-  uint64_t rs[Pairs<V>::N], o[Pairs<V>::N], ga[Pairs<V>::N], be[Pairs<V>::N];
+  uint64_t rs[Pairs<V>::N], minus[Pairs<V>::N], ga[Pairs<V>::N], be[Pairs<V>::N];
   __device__ __forceinline__ GradCols(const GnShape& s, const ColGeom& g, const ColPlace& p, const float* mean,
                                       const float* rstd, const float* gamma, const float* beta) {
     float r[V], m[V], a[V], b[V];
@@ -346,10 +348,10 @@ struct GradCols {
     for (int e = 0; e < V; ++e) {
       const int st = p.b * s.G + (int)g.by_Cg.div((uint32_t)(p.col * V + e));
       r[e] = rstd[st];
-      m[e] = -mean[st] * r[e];
+      m[e] = -mean[st];
     }
     Pairs<V>::of(r, rs);
-    Pairs<V>::of(m, o);
+    Pairs<V>::of(m, minus);
     Pairs<V>::of(a, ga);
     Pairs<V>::of(b, be);
   }
@@ -358,7 +360,7 @@ struct GradCols {
     uint64_t u[Pairs<V>::N];
 #pragma unroll
     for (int e = 0; e < Pairs<V>::N; ++e) {
-      x[e] = ptx::fma2(x[e], rs[e], o[e]);
+      x[e] = ptx::mul2(ptx::add2(x[e], minus[e]), rs[e]);
       u[e] = ptx::fma2(x[e], ga[e], be[e]);
     }
     act_grad_pairs<V>(d, u, act);

@@ -313,8 +313,8 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q,
     ptx::cp_async_wait<1>();
     const Raw* mx = stages + k * q.span + threadIdx.x;
     const Raw* my = mx + stage;
-    // h = x rs - mu rs; u = gamma h + beta
-    const uint64_t r2 = both(rs), o2 = both(-mu * rs);
+    // h = (x - mu) rs, the mean taken off first (see GradCols in ff_norm.cu); u = gamma h + beta
+    const uint64_t r2 = both(rs), minus = both(-mu);
     uint64_t du[NV][PV::N], q0[PV::N], q1[PV::N];
 #pragma unroll
     for (int e = 0; e < PV::N; ++e) q0[e] = q1[e] = 0;
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q,
         uint64_t up[PV::N];
 #pragma unroll
         for (int e = 0; e < PV::N; ++e) {
-          hx[e] = ptx::fma2(hx[e], r2, o2);
+          hx[e] = ptx::mul2(ptx::add2(hx[e], minus), r2);
           up[e] = ptx::fma2(hx[e], G2[e], B2[e]);
         }
         act_grad_pairs<V>(dd, up, s.act);
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q,
         PV::of(x, hx);
 #pragma unroll
         for (int e = 0; e < PV::N; ++e)
-          hx[e] = ptx::fma2(du[i][e], gr[e], ptx::fma2(ptx::fma2(hx[e], r2, o2), c2, c1));
+          hx[e] = ptx::fma2(du[i][e], gr[e], ptx::fma2(ptx::mul2(ptx::add2(hx[e], minus), r2), c2, c1));
         PV::to(hx, x);
         VV::store(o, x);
         o += ostep;
