@@ -294,18 +294,20 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
   ptx::griddep_wait();
   const ColPlace p(s, g, true);
   if (!p.on) return;
-  float a[V], b[V];
+  // y = (x - mean) (gamma rstd) + beta, the mean taken off first (see GradCols)
+  float a[V], b[V], m[V];
   load_params<V>(a, gamma, p.col * V, 1.f, g.wide);
   load_params<V>(b, beta, p.col * V, 0.f, g.wide);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     const int st = p.b * s.G + (int)g.by_Cg.div((uint32_t)(p.col * V + e));
     a[e] *= rstd[st];
-    b[e] = fmaf(-mean[st], a[e], b[e]);
+    m[e] = -mean[st];
   }
-  uint64_t A[PV::N], B[PV::N];
+  uint64_t A[PV::N], B[PV::N], M[PV::N];
   PV::of(a, A);
   PV::of(b, B);
+  PV::of(m, M);
   const T* q = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
   T* o = y + ((long long)p.b * s.S + p.r0) * s.ldy + (long long)p.col * V;
   const long long sx = (long long)g.TR * s.ldx, so = (long long)g.TR * s.ldy;
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
         Vec<T, V>::unpack(raw[u], v);
         PV::of(v, d);
 #pragma unroll
-        for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(d[e], A[e], B[e]);
+        for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(ptx::add2(d[e], M[e]), A[e], B[e]);
         act_pairs<V>(d, s.act);
         PV::to(d, v);
         Vec<T, V>::store(o + u * so, v);

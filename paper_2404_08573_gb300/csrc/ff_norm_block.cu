@@ -204,15 +204,22 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
       a.mean[at] = mean;
       a.rstd[at] = rstd;
     }
+    // y = x A + B.  fp32: A = gamma rstd and B = beta with the mean taken off x
+    // first (see GradCols in ff_norm.cu).  bf16: B = beta - mean A, rounded
+    // once: as far off as the rounding of the mean itself brings y, and far
+    // below the output's (with the mean off first 64 x 784 x 256 took 17.9 us
+    // in place of 16.6).
+    constexpr bool FIRST = sizeof(T) == 4;
     float fa[V], fb[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       fa[e] = ga[e] * rstd;
-      fb[e] = fmaf(-mean, fa[e], be[e]);
+      fb[e] = FIRST ? be[e] : fmaf(-mean, fa[e], be[e]);
     }
     uint64_t A[PV::N], B[PV::N];
     PV::of(fa, A);
     PV::of(fb, B);
+    const uint64_t minus = both(-mean);
     T* y = a.out + cur.offset(s, q, p, s.ldy);
     m = mem;
 #pragma unroll 2
@@ -222,7 +229,7 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
       VV::unpack(*m, v);
       PV::of(v, d);
 #pragma unroll
-      for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(d[e], A[e], B[e]);
+      for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(FIRST ? ptx::add2(d[e], minus) : d[e], A[e], B[e]);
       act_pairs<V>(d, s.act);
       PV::to(d, v);
       VV::store(y, v);

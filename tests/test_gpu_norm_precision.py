@@ -60,3 +60,20 @@ def test_gradient_of_a_large_mean(shape, kind):
     dx64 = R * (w - a1 - h * a2)
     tol = R * (Dw + D1 + np.abs(h) * D2 + DH * np.abs(a2) + 4 * U * (np.abs(w) + np.abs(a1) + np.abs(h * a2)))
     assert np.all(np.abs(dx.double().cpu().numpy() - dx64) <= tol + 2.0 ** -23 * np.abs(dx64) + 1e-30)
+
+
+@pytest.mark.parametrize("kind", ["none", "relu", "silu"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_outputs_of_a_large_mean(shape, kind):
+    """With the returned mean and rstd as given; the two may be rounded once more than what the outputs are formed from."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    n, S, C, G = shape
+    x, x64, gen = make(torch, n, S, C, "fp32", seed=SHAPES.index(shape), offset=2000.0)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=gen), 0.3 * torch.randn(C, generator=gen)
+    y, m, r = ff.group_norm_act(x, gamma.cuda(), beta.cuda(), G, act=kind)
+    h = (x64 - per_channel(m.double().cpu().numpy(), S, C)) * per_channel(r.double().cpu().numpy(), S, C)
+    u = h * gamma.double().numpy() + beta.double().numpy()
+    DU = 6 * U * (np.abs(h * gamma.double().numpy()) + np.abs(beta.double().numpy()))
+    y64 = act(u, kind)
+    assert np.all(np.abs(y.double().cpu().numpy() - y64) <= 1.1 * DU + (2.0 ** -23 + 2.0 ** -20) * np.abs(y64) + 1e-30)
