@@ -83,32 +83,38 @@ __device__ __forceinline__ float pivot_of(float first, float second) {
 __device__ __forceinline__ long long second_of(const GnShape& s) { return s.Cg > 1 ? 1 : s.S > 1 ? s.ldx : 0; }
 
 __device__ __forceinline__ uint64_t both(float v) { return ptx::pack2(v, v); }
-// 1 / (1 + e^-u) of a pair, with the approximate exponential and one
-// approximate reciprocal for both: with a = 1 + e^-u and r = 1 / (a b), 1 / a is
-// r b and 1 / b is r a.  (These units take 16 values a clock and SM, and with
-// two calls a value they, not HBM, would bound the silu forms.)  The exponent
-// is held below 60, so the product of the two cannot overflow: beyond, the
-// result is 2^-60 in place of less.  Neither a nor r is ever subnormal.
-__device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
-  const float2 t = ptx::unpack2(ptx::mul2(u, both(-1.44269504f)));
-  float x, y, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(fminf(t.x, 60.f)));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fminf(t.y, 60.f)));
-  const uint64_t a = ptx::add2(ptx::pack2(x, y), both(1.f));
-  const float2 f = ptx::unpack2(a);
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(f.x * f.y));
-  return ptx::pack2(f.y * r, f.x * r);
+// 1 / (1 + e^-u) from e = e^-|u|, which is at most one: 1 / (1 + e) for u >= 0
+// and e / (1 + e) below, so that nothing overflows and the result goes to zero
+// as it should however far out u is.  Approximate exponential; of a pair, one
+// approximate reciprocal for both: with a = 1 + e and r = 1 / (a b), 1 / a is r b
+// and 1 / b is r a.  (These units take 16 values a clock and SM, and with two
+// calls a value they, not HBM, would bound the silu forms.)
+__device__ __forceinline__ float exp2_approx(float t) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+  return r;
 }
+__device__ __forceinline__ float rcp_approx(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
+  const float2 v = ptx::unpack2(u);
+  const float x = exp2_approx(fabsf(v.x) * -1.44269504f), y = exp2_approx(fabsf(v.y) * -1.44269504f);
+  const float a = 1.f + x, b = 1.f + y, r = rcp_approx(a * b);
+  const float p = b * r, q = a * r;
+  return ptx::pack2(v.x < 0.f ? x * p : p, v.y < 0.f ? y * q : q);
+}
+__device__ __forceinline__ float sigmoid1(float u) {
+  const float e = exp2_approx(fabsf(u) * -1.44269504f), r = rcp_approx(1.f + e);
+  return u < 0.f ? e * r : r;
+}
+
 __device__ __forceinline__ float max0(float u) {  // max(u, 0), NaN kept
   float r;
   asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(u));
   return r;
-}
-__device__ __forceinline__ float sigmoid1(float u) {
-  float e, p;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(u * -1.44269504f, 60.f)));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
-  return p;
 }
 
 // A vector of V values as pairs (V = 1: one pair whose second value is zero).
