@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
         PV::of(v, d);
 #pragma unroll
         for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(ptx::add2(d[e], M[e]), A[e], B[e]);
-        act_pairs<V>(d, s.act);
+        act_pairs<T, V>(d, s.act);
         PV::to(d, v);
         Vec<T, V>::store(o + u * so, v);
       }
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kColThreads) k_gn_apply(const T* x, GnShape s,
 // u = gamma h + beta.  The mean is taken off first: x rs - mean rs in one
 // multiply-add would bring the rounding of mean rs into h, mean / spread
 // rounding units instead of one.
-template <int V>
+template <typename T, int V>
 struct GradCols {
   uint64_t rs[Pairs<V>::N], minus[Pairs<V>::N], ga[Pairs<V>::N], be[Pairs<V>::N];
   __device__ __forceinline__ GradCols(const GnShape& s, const ColGeom& g, const ColPlace& p, const float* mean,
@@ -365,7 +365,7 @@ struct GradCols {
       x[e] = ptx::mul2(ptx::add2(x[e], minus[e]), rs[e]);
       u[e] = ptx::fma2(x[e], ga[e], be[e]);
     }
-    act_grad_pairs<V>(d, u, act);
+    act_grad_pairs<T, V>(d, u, act);
   }
 };
 
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
 #pragma unroll
   for (int e = 0; e < PV::N; ++e) p0[e] = p1[e] = 0;
   if (p.on) {
-    const GradCols<V> k(s, g, p, mean, rstd, gamma, beta);
+    const GradCols<T, V> k(s, g, p, mean, rstd, gamma, beta);
     const T* qx = x + ((long long)p.b * s.S + p.r0) * s.ldx + (long long)p.col * V;
     const T* qd = dy + ((long long)p.b * s.S + p.r0) * s.lddy + (long long)p.col * V;
     const long long sx = (long long)g.TR * s.ldx, sd = (long long)g.TR * s.lddy;
@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_apply(const T* dy, c
   ptx::griddep_wait();
   const ColPlace p(s, g, true);
   if (!p.on) return;
-  const GradCols<V> k(s, g, p, mean, rstd, gamma, beta);
+  const GradCols<T, V> k(s, g, p, mean, rstd, gamma, beta);
   // dx = rs (gamma du - <.> - h <.>) = du (gamma rs) + (h c2 + c1)
   float f1[V], f2[V];
 #pragma unroll

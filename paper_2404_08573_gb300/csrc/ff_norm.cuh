@@ -85,32 +85,39 @@ __device__ __forceinline__ long long second_of(const GnShape& s) { return s.Cg >
 __device__ __forceinline__ uint64_t both(float v) { return ptx::pack2(v, v); }
 // 1 / (1 + e^-u) from e = e^-|u|, which is at most one: 1 / (1 + e) for u >= 0
 // and e / (1 + e) below, so that nothing overflows and the result goes to zero
-// as it should however far out u is.  Approximate exponential; of a pair, one
-// approximate reciprocal for both: with a = 1 + e and r = 1 / (a b), 1 / a is r b
-// and 1 / b is r a.  (These units take 16 values a clock and SM, and with two
-// calls a value they, not HBM, would bound the silu forms.)
-__device__ __forceinline__ float exp2_approx(float t) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
-  return r;
-}
-__device__ __forceinline__ float rcp_approx(float v) {
+// as it should however far out u is.  T = float: e by expf, and a reciprocal
+// each (within 2^-21 of itself in all).  T = bf16, where the output's rounding
+// is 2^-9: the approximate exponential, whose rounded argument costs up to
+// 2^-17, and of a pair one approximate reciprocal for both: with a = 1 + e and
+// r = 1 / (a b), 1 / a is r b and 1 / b is r a.  (These units take 16 values a
+// clock and SM, and with two calls a value they, not HBM, would bound the bf16
+// forms.)
+__device__ __forceinline__ float rcp_approx(float v) {  // of 1 to 4: within one unit of the last place
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
+template <typename T>
+__device__ __forceinline__ float exp_minus_abs(float u) {
+  if constexpr (sizeof(T) == 4) return expf(-fabsf(u));
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fabsf(u) * -1.44269504f));
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ float sigmoid1(float u) {
+  const float e = exp_minus_abs<T>(u), r = rcp_approx(1.f + e);
+  return u < 0.f ? e * r : r;
+}
+template <typename T>
 __device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
   const float2 v = ptx::unpack2(u);
-  const float x = exp2_approx(fabsf(v.x) * -1.44269504f), y = exp2_approx(fabsf(v.y) * -1.44269504f);
+  if constexpr (sizeof(T) == 4) return ptx::pack2(sigmoid1<T>(v.x), sigmoid1<T>(v.y));
+  const float x = exp_minus_abs<T>(v.x), y = exp_minus_abs<T>(v.y);
   const float a = 1.f + x, b = 1.f + y, r = rcp_approx(a * b);
   const float p = b * r, q = a * r;
   return ptx::pack2(v.x < 0.f ? x * p : p, v.y < 0.f ? y * q : q);
 }
-__device__ __forceinline__ float sigmoid1(float u) {
-  const float e = exp2_approx(fabsf(u) * -1.44269504f), r = rcp_approx(1.f + e);
-  return u < 0.f ? e * r : r;
-}
-
 __device__ __forceinline__ float max0(float u) {  // max(u, 0), NaN kept
   float r;
   asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(u));
@@ -144,14 +151,14 @@ struct Pairs {
 };
 
 // u = act(u) and d = d act'(u) over pairs (V = 1: the first value only).
-template <int V>
+template <typename T, int V>
 __device__ __forceinline__ void act_pairs(uint64_t (&u)[Pairs<V>::N], int act) {
   constexpr int N = Pairs<V>::N;
   if (act == FF_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      u[i] = V == 1 ? ptx::pack2(ptx::unpack2(u[i]).x * sigmoid1(ptx::unpack2(u[i]).x), 0.f)
-                    : ptx::mul2(u[i], sigmoid2(u[i]));
+      u[i] = V == 1 ? ptx::pack2(ptx::unpack2(u[i]).x * sigmoid1<T>(ptx::unpack2(u[i]).x), 0.f)
+                    : ptx::mul2(u[i], sigmoid2<T>(u[i]));
   } else if (act == FF_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -160,21 +167,21 @@ __device__ __forceinline__ void act_pairs(uint64_t (&u)[Pairs<V>::N], int act) {
     }
   }
 }
-template <int V>
+template <typename T, int V>
 __device__ __forceinline__ void act_grad_pairs(uint64_t (&d)[Pairs<V>::N], const uint64_t (&u)[Pairs<V>::N], int act) {
   constexpr int N = Pairs<V>::N;
   if (act == FF_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint64_t p = V == 1 ? ptx::pack2(sigmoid1(ptx::unpack2(u[i]).x), 0.f) : sigmoid2(u[i]);
+      const uint64_t p = V == 1 ? ptx::pack2(sigmoid1<T>(ptx::unpack2(u[i]).x), 0.f) : sigmoid2<T>(u[i]);
       const uint64_t q = ptx::fma2(p, both(-1.f), both(1.f));  // 1 - p
       d[i] = ptx::mul2(d[i], ptx::mul2(p, ptx::fma2(u[i], q, both(1.f))));
     }
   } else if (act == FF_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float2 v = ptx::unpack2(u[i]), t = ptx::unpack2(d[i]);
-      d[i] = ptx::pack2(v.x > 0.f ? t.x : 0.f, v.y > 0.f ? t.y : 0.f);
+      const float2 v = ptx::unpack2(u[i]), w = ptx::unpack2(d[i]);
+      d[i] = ptx::pack2(v.x > 0.f ? w.x : 0.f, v.y > 0.f ? w.y : 0.f);
     }
   }
 }

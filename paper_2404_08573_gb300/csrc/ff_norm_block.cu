@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kMaxT, 2) k_gn_block(GnArgs<T> a, Geom q) {
       PV::of(v, d);
 #pragma unroll
       for (int e = 0; e < PV::N; ++e) d[e] = ptx::fma2(FIRST ? ptx::add2(d[e], minus) : d[e], A[e], B[e]);
-      act_pairs<V>(d, s.act);
+      act_pairs<T, V>(d, s.act);
       PV::to(d, v);
       VV::store(y, v);
     }
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kMaxT, 1) k_gn_block_grad(GnArgs<T> a, Geom q,
           hx[e] = ptx::mul2(ptx::add2(hx[e], minus), r2);
           up[e] = ptx::fma2(hx[e], G2[e], B2[e]);
         }
-        act_grad_pairs<V>(dd, up, s.act);
+        act_grad_pairs<T, V>(dd, up, s.act);
 #pragma unroll
         for (int e = 0; e < PV::N; ++e) {
           du[i][e] = dd[e];

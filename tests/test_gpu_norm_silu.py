@@ -60,3 +60,16 @@ def test_silu_far_out(shape, dtype):
     with np.errstate(over="ignore", invalid="ignore"):
         tol = 2.0 ** -17 * np.where(p > 0, p * (1 + np.abs(u)), 0.0) + 1e-35
     assert np.all(np.abs(slope - ds) <= tol)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_silu_of_fp32_in_full(shape):
+    """fp32, where results are in the normal range (u >= -80): the exponential within two units, 1 + e and the products
+    half a unit each, the reciprocal one, so a value is within 2^-21 of itself, and a slope of p (1 + |u|)."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    u, y, slope = results(torch, ff, shape, "fp32", 10 + SHAPES.index(shape))
+    want, ds, p = definition(u)
+    at = (u >= -80) & (u <= 1e6)
+    assert np.all(np.abs(y - want)[:, :, at] <= 2.0 ** -21 * np.abs(want[at]))
+    assert np.all(np.abs(slope - ds)[at] <= 2.0 ** -21 * (p * (1 + np.abs(u)))[at])
