@@ -432,31 +432,50 @@ __global__ void __launch_bounds__(kColThreads, 3) k_gn_grad_colsums(const T* dy,
   }
 }
 
+// A sum that keeps what its additions round off (Knuth's two-sum), so that it
+// may be long.  An infinite or NaN sum has no such remainder.
+struct LongSum {
+  float sum = 0.f, lost = 0.f;
+  __device__ __forceinline__ void add(float v) {
+    const float s = sum + v, t = s - sum;
+    lost += (sum - (s - t)) + (v - t);
+    sum = s;
+  }
+  __device__ __forceinline__ float value() const { return lost == lost ? sum + lost : sum; }
+};
+
 // dbeta and dgamma of kFoldCols channels: the partial column sums [rows, C]
 // added up, in an order that depends on the sizes only.  Few columns and many
 // row threads per block: the sums are short and latency is what they cost.
-constexpr int kFoldCols = 8;
+// Long ones (the rows grow with the batch) go eight rows at a time.
+constexpr int kFoldCols = 8, kFoldRows = 8;
 template <int ROWS>
 __device__ __forceinline__ void param_fold(int block, const float2* part, const GnFold& f, int C, float* dgamma,
                                            float* dbeta) {
   __shared__ float2 red[ROWS][kFoldCols];
   const int tc = threadIdx.x % kFoldCols, tr = threadIdx.x / kFoldCols;
   const int c = block * kFoldCols + tc;
-  float2 t = make_float2(0.f, 0.f);
+  LongSum tx, ty;
   if (c < C) {
     long long rows = f.rows;
     if (f.units > 0) {
       const long long first = (long long)(c / f.W) * f.n;
       rows = (first + f.n - 1) / f.units - first / f.units + 1;
     }
-#pragma unroll 8
-    for (long long r = tr; r < rows; r += ROWS) {
-      const float2 q = part[r * C + c];
-      t.x += q.x;
-      t.y += q.y;
+    for (long long r = tr; r < rows; r += kFoldRows * ROWS) {
+      float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < kFoldRows; ++u)
+        if (r + u * ROWS < rows) {
+          const float2 q = part[(r + u * ROWS) * C + c];
+          t.x += q.x;
+          t.y += q.y;
+        }
+      tx.add(t.x);
+      ty.add(t.y);
     }
   }
-  red[tr][tc] = t;
+  red[tr][tc] = make_float2(tx.value(), ty.value());
   for (int half = ROWS / 2; half > 0; half /= 2) {
     __syncthreads();
     if (tr < half) {

@@ -29,6 +29,10 @@ struct GnArgs {
   void* ws;
 };
 
+// Samples whose terms of dgamma and dbeta one thread adds up in a row: the
+// rounding of a plain sum grows with its length, and a batch has no bound.
+constexpr int kGradSamples = 128;
+
 // The rows path: groups in the registers of up to a warp, or of a block.
 // `lanes` lanes per group (a power of 2), sets of groups side by side.
 struct GnRowsPlan {

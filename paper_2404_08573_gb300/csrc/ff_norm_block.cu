@@ -511,7 +511,8 @@ GnBlockPlan gn_block_plan(const GnShape& s, int V, int esize, bool grad) {
       // 2-byte copies cost still more (100 x 100 x 100 in 4 groups: 17 us)
       if (grad && T == kMaxT) us *= 1.2;
       if (grad && V * esize < 4) us *= 2.5;
-      if (us < best.us) best = GnBlockPlan{T, GS, nv, (int)((units + rounds - 1) / rounds), (int)rounds, us};
+      const long long each = grad ? std::min<long long>(rounds, kGradSamples) : rounds;  // (its sums: see kGradSamples)
+      if (us < best.us) best = GnBlockPlan{T, GS, nv, (int)((units + each - 1) / each), (int)each, us};
     }
   }
   return best;

@@ -376,11 +376,13 @@ GnRowsPlan gn_rows_plan(const GnShape& s, int V, bool grad) {
     rows = kWarps;
   }
   // about 8 blocks of 256 threads per SM; the gradient's partial sums grow
-  // with the blocks, so it takes 4
+  // with the blocks, so it takes 4, or as many as leave each thread
+  // kGradSamples samples
   const int threads = p.lanes > 32 ? p.lanes : 32 * kWarps;
   const long long want = 152ll * (grad ? 4 : 8) * (32 * kWarps) / threads / p.sets;
   p.P = cdiv(s.n, rows);
-  if (p.P > want) p.P = want > 1 ? (int)want : 1;
+  const long long least = grad ? cdiv(s.n, rows * kGradSamples) : 1;
+  p.P = (int)std::min<long long>(p.P, std::max(want, least));
   return p;
 }
 
