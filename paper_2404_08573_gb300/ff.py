@@ -18,6 +18,7 @@ import ctypes
 import functools
 import inspect
 import os
+import warnings
 from ctypes import POINTER, c_double, c_float, c_int, c_longlong, c_ulonglong, c_void_p
 
 import numpy as np
@@ -782,6 +783,16 @@ def _row_stride_of(x, what):
     return ld
 
 
+def _unrecorded(name, tensors, depth=4):
+    """Says so where autograd would be expected to record a call: the operators work on the tensors' memory and return
+    plain results.  depth: frames up to the user's call."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            warnings.warn(f"{name} is not recorded by autograd: its result has no gradient (the gradient is a call of "
+                          f"its own; use torch.no_grad() or detach() where that is meant)", stacklevel=depth)
+            return
+
+
 def _vector(t, size, what, device):
     if t is None:
         return None
@@ -829,7 +840,8 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     """ff_group_norm_act: y = act(gamma * (x - mean) * rstd + beta) over channel
     groups, channels last.  x [n, channels] or [n, ..., channels] (bf16 or
     fp32, evenly spaced rows); gamma, beta fp32 [channels] or None.  Returns
-    (y, mean, rstd), mean and rstd fp32 [n, groups]; out may be x."""
+    (y, mean, rstd), mean and rstd fp32 [n, groups]; out may be x.  Not
+    recorded by autograd: its gradient is group_norm_act_backward."""
     prec, dev = _prec(x, "x"), x.device
     n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 0)
     on, empty = _on(stream, dev, x, gamma, beta, out, mean, rstd)
@@ -853,6 +865,7 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
         x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
         eps, kind, prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
         "ff_group_norm_act")
+    _unrecorded("group_norm_act", (x, gamma, beta))
     return out, mean, rstd
 
 
@@ -894,7 +907,7 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     the same call on dy without a residual.  x [..., cols] (bf16 or fp32,
     evenly spaced rows).  offset: an int, or a one-element int64 CUDA tensor
     that is read when the kernel runs (for CUDA graphs).  out may be x or the
-    residual."""
+    residual.  Not recorded by autograd."""
     prec = _prec(x, "x")
     if x.dim() < 1:
         raise ValueError("x must have at least one dimension")
@@ -919,6 +932,7 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
                             None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
                             on), "ff_dropout")
+    _unrecorded("dropout", (x, residual))
     return out
 
 
@@ -974,13 +988,14 @@ def _fp8_quantize(x, tile, straight, transposed, stream):
                                  a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
                                  t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on),
            "ff_fp8_quantize")
+    _unrecorded("fp8_quantize", (x,), depth=5)
     return a, t
 
 
 def fp8_quantize(x, tile: bool = False, transpose: bool = False, stream=None):
     """ff_fp8_quantize: x [rows, k] (bf16 or fp32, evenly spaced rows) as an
     Fp8Matrix in row blocks or 128 x 128 tiles; transpose=True gives x's
-    transpose instead."""
+    transpose instead.  Not recorded by autograd."""
     return _fp8_quantize(x, tile, not transpose, transpose, stream)[1 if transpose else 0]
 
 
@@ -993,9 +1008,10 @@ def fp8_quantize_both(x, tile: bool = False, stream=None):
 def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bfloat16, status=None, stream=None):
     """ff_fp8_matmul: act(a b^T + bias) of two Fp8Matrix (a in row blocks).
     Returns [a.rows, b.rows] in out_dtype (torch.bfloat16 or torch.float32) or
-    out's type; bias fp32 [b.rows]; status: a one-element int32 CUDA tensor
-    that is OR-ed with 1 if a kernel wait timed out; without one, fp8_check
-    reports it."""
+    out's type; bias fp32 [b.rows].  Not recorded by autograd: the gradients
+    are products of their own (see ff_fp8_matmul in include/ff.h).  status: a
+    one-element int32 CUDA tensor that is OR-ed with 1 if a kernel wait timed
+    out; without one, fp8_check reports it."""
     if not isinstance(a, Fp8Matrix) or not isinstance(b, Fp8Matrix):
         raise TypeError("a and b must be Fp8Matrix")
     if a.k != b.k:
@@ -1021,6 +1037,7 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
                                n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
                                _ptr(status, torch.int32, "status"), on), "ff_fp8_matmul")
+    _unrecorded("fp8_matmul", (bias,))
     return out
 
 
