@@ -960,7 +960,7 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
       default: return each ? run_split<128, true>(p, q, g, pl.ks_log, st) : run_split<128, false>(p, q, g, pl.ks_log, st);
     }
   };
-  FF_LAUNCH(K_FP8_GEMM, work, st, go(), "8-bit matrix product");
+  FF_LAUNCH(pairk ? K_FP8_PAIR : K_FP8_GEMM, work, st, go(), "8-bit matrix product");
   return FF_OK;
 }
 
