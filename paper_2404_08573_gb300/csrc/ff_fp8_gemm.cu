@@ -940,7 +940,9 @@ ff_status fp8_gemm(const Fp8Gemm& f, cudaStream_t st) {
     return FF_ERR_INVALID_ARG;
   const int es = f.out_bf16 ? 2 : 4;
   CUtensorMap c = p;
-  const bool tma_c = pairk && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N && make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
+  // whole 16-byte units a row: a row that ends inside one is written to the
+  // unit's end, into what lies between the rows
+  const bool tma_c = pairk && (long long)f.N * es % 16 == 0 && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N && make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
   const double work = 2.0 * f.M * f.N * f.K;
   auto go = [&]() -> cudaError_t {
     if (pairk) {

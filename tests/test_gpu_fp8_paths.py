@@ -71,6 +71,27 @@ def test_pairs_with_several_tiles(size, dtype, tile):
     ff.fp8_check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tile", [False, True])
+def test_pairs_write_only_their_matrix(tile, dtype):
+    """C within larger buffers, at odd strides and starts: the gaps keep what they held."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    m, n, k = 2055, 2001, 784
+    a, b, bias = operands(torch, ff, m, n, k, tile, seed=3)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    want, kinds = launched(ff, lambda: ff.fp8_matmul(a, b, bias=bias, out_dtype=dt))
+    assert kinds == {PAIR: 1}
+    check(torch, want, a, b, bias, False)
+    for pad, lead in ((5, 3), (7, 8), (15, 16), (1, 0)):
+        buf = torch.full((lead + m * (n + pad) + 64,), 7.0, dtype=dt, device="cuda")
+        out = buf[lead:lead + m * (n + pad)].view(m, n + pad)[:, :n]
+        assert ff.fp8_matmul(a, b, bias=bias, out=out) is out
+        assert torch.equal(out, want)
+        out.fill_(7.0)
+        assert bool((buf == 7.0).all())
+
+
 @pytest.mark.parametrize("tile", [False, True])
 def test_the_large_layer(tile):
     torch = torch_cuda()
