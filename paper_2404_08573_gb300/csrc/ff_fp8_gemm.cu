@@ -89,7 +89,7 @@ __device__ __forceinline__ void scaled_add(float* acc, const uint32_t (&p)[LD], 
 // release() runs once the last columns are in registers.
 template <int CPW, bool COLS, typename Release>
 __device__ __forceinline__ void promote(float (&acc)[CPW], uint32_t at, float row, const float* cs, Release release) {
-  constexpr int LD = CPW < 16 ? 8 : CPW < 128 ? 16 : 32;
+  constexpr int LD = CPW < 16 ? 8 : 16;
   constexpr int NC = CPW / LD;
   uint32_t r[2][LD];
   const uint64_t row2 = ptx::pack2(row, row);
