@@ -514,10 +514,10 @@ FF_API ff_status ff_layer_selftest_wait(ff_layer* layer, unsigned int timeout_us
  * Operators of a normalised, regularised dense layer that is trained or
  * served in 8 bits.  The paper's layers have none of them; they stand beside
  * the FF layers for heads and comparison nets trained by backpropagation on
- * the layers' activities.  They keep no state: every buffer is the caller's,
- * nothing is allocated, and calls on different streams are independent as
- * long as their outputs and workspaces are.  Matrices are row-major with a
- * row stride in elements; `prec` is the type of the large buffers (float or
+ * the layers' activities.  They keep no state but the word that ff_fp8_check
+ * reads: every buffer is the caller's, nothing is allocated, and calls on
+ * different streams are independent as long as their outputs and workspaces
+ * are.  Matrices are row-major with a row stride in elements; `prec` is the type of the large buffers (float or
  * bfloat16), every sum and statistic is fp32.  Empty calls (no rows) return
  * FF_OK.  Strides need no alignment (16-byte aligned rows are faster).
  * ------------------------------------------------------------------------- */

@@ -67,7 +67,7 @@ constexpr int kQThreads = 256;
 // ends with one row, divides once, and passes the reciprocal round; a column
 // block's by one pass over the 16 row groups in shared memory.  Both
 // orientations come from one read.  Bound by HBM: x once, each orientation
-// once (4096 x 8192 bf16, both: 23.7 us, 5.7 TB/s; 2000 x 784 fp32 in tiles, both:
+// once (4096 x 8192 bf16, both: 25 us, 5.4 TB/s; 2000 x 784 fp32 in tiles, both:
 // 4.0 us, a launch and one round of 112 blocks).  Rows that start on 4 bytes
 // only are read in pairs (7455 x 7374 bf16, both: 43 us, value by value 64, and
 // 7376 columns 38); odd widths of bf16 stay value by value, since five words

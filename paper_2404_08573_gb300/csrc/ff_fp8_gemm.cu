@@ -128,9 +128,9 @@ __device__ __forceinline__ float finish(float v, int relu) { return relu && v < 
 // next tile's first k-blocks run under the store of this one.
 //
 // Bound by the MMAs: 4096 x 8192 x 8192 with a scale per 128 x 128 tile of B takes
-// 187 us, 2.94 PFLOP/s (0.78 of twice the measured bf16 burst rate, 0.86 of
+// 188 us, 2.92 PFLOP/s (0.78 of twice the measured bf16 burst rate, 0.85 of
 // twice the sustained one).  With a scale per row of B each value of the
-// product takes a second multiplication, and the promotion bounds: 290 us.
+// product takes a second multiplication, and the promotion bounds: 289 us.
 constexpr int LN = 256;
 constexpr int LSTAGES = 4;
 constexpr int LSTAGE = (BM + LN / 2) * KB;
@@ -450,8 +450,8 @@ __global__ void __launch_bounds__(LTHREADS, 1)
       // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
       // clips what lies past the matrix, and the warp need not wait for the
       // memory), else by the lanes along a row, eight rows read before the
-      // first is written (2023 x 2375 x 368, bf16 C: 11.0 us, 24 one by one, 9
-      // for 2376 columns).
+      // first is written (2023 x 2375 x 368, bf16 C: 10.9 us, 24 one by one,
+      // 8.2 for 2376 columns).
       auto block = [&](int ch) {  // staging block of chunk ch, free again
         if (TMA_C && lane == 0) ptx::bulk_wait_read1();
         __syncwarp();
@@ -531,9 +531,10 @@ __global__ void __launch_bounds__(LTHREADS, 1)
 // rank order) and store.  With few rows of A its rows go on the MMA's columns
 // (swap), so that a single row needs 16 columns and not 128 lanes.
 //
-// Bound by the weights' bytes where they are many (1 x 8192 x 8192: 12.4 us, 5.4
+// Bound by the weights' bytes where they are many (1 x 8192 x 8192: 14.9 us, 4.5
 // TB/s), else by latency: launch, ring fill, exchange, store (1 x 2000 x 2000:
-// 4.3 us, 333 x 1999 x 1337: 7.9 us).
+// 5.1 us from operands beyond L2, 4.0 from weights in it; 333 x 1999 x 1337: 7.9
+// us).
 template <int BN>
 struct SCfg {
   static constexpr int STAGE = (BM + BN) * KB;

@@ -15,8 +15,8 @@
 // width, since a 16-byte vector may span groups.
 //
 // Bound by HBM and by what three dependent launches cost: 32 x 4096 x 512 in 32
-// groups (bf16, silu) takes 72 us, 5.6 TB/s over two reads and a write, its
-// gradient 123 us (four reads and a write); 32 x 3136 x 320 39 and 68 us.
+// groups (bf16, silu) takes 74 us, 5.4 TB/s over two reads and a write, its
+// gradient 127 us (four reads and a write); 32 x 3136 x 320 41 and 73 us.
 // Reading once more from L2 instead of HBM was tried in two forms and lost.
 // Passes over a few samples at a time pay about 10 us of ramps for every part
 // (two parts: 87 us).  One persistent kernel that forms a piece's sums some

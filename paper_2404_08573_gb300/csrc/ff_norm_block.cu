@@ -9,11 +9,14 @@
 // lanes per group and back.  Sums of x are held relative to the group's pivot,
 // as in ff_norm.cu.
 //
-// Bound by the instructions: with silu a value of bf16 takes about 12 forward,
-// and a unit some 450 per thread beside (256 x 49 x 1024, 32 groups: 21 us with
-// 4 vectors a thread, 16 with 7), so 64 x 784 x 256 (32 groups) runs in
-// 16 us, 3.2 TB/s; fp32 moves twice the bytes for them (512 x 196 x 256 in 16
-// groups: 40 us, 5.1 TB/s, gradient 65 us, 4.8 TB/s).  Splitting a slab's
+// Bound by latency in bf16: a unit costs two barriers around the fold and some
+// 450 instructions per thread beside the 14 or so of a value with silu (256 x 49
+// x 1024, 32 groups: 21 us with 4 vectors a thread, 16 with 7), and few warps are
+// there to cover them.  64 x 784 x 256 (32 groups) takes 17.5 us, 2.9 TB/s, in
+// 128 blocks of 16 warps: 24 SMs have none, the others a quarter of their
+// warps and issue 52 % of the time.  fp32 moves twice the bytes for the same
+// (512 x 196 x 256 in 16 groups: 40 us, 5.1 TB/s, gradient 61 us, 5.0 TB/s; with
+// silu, whose exponential is the full one there, 46 and 75 us).  Splitting a slab's
 // positions over a cluster of 2 to 8 blocks, with the sums exchanged through
 // distributed shared memory, reached larger samples but was slower than the
 // column passes there (32 x 4096 x 512: 100 against 72 us), so larger ones take

@@ -5,11 +5,13 @@
 // A warp (or block) walks over the samples with its groups fixed, so gamma, beta
 // and the gradient's sums over the samples stay in registers; the next
 // sample's values are loaded under the arithmetic of this one.  Mean and
-// centred sum of squares are two passes over registers.  Bound by the
-// instructions: with silu some 30 a value forward, much of it the sums'
-// shuffles, and odd groups are read a value at a time (8192 x 4096 in 32
-// groups, silu: bf16 36 us, 3.8 TB/s, gradient 54 us; fp32 48 us, 5.6 TB/s,
-// and 88 us; 2048 x 2000 in 16 groups of 125, fp32: 11 and 16 us).
+// centred sum of squares are two passes over registers.  In bf16 neither HBM
+// nor the schedulers are full (8192 x 4096 in 32 groups, silu: 40 us, 3.4 TB/s,
+// issuing 74 % of the time; gradient 58 us, 63 % with 24 % of the warps): some 30
+// instructions a value, and between them the latency of the sums' shuffles.
+// fp32 moves twice the bytes for them: 52 us, 5.1 TB/s, and 92 us.  Odd groups
+// are read a value at a time (2048 x 2000 in 16 groups of 125, fp32, relu: 11 and
+// 15 us).
 #include <algorithm>
 
 #include "ff_norm.cuh"
