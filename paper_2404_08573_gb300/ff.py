@@ -783,14 +783,12 @@ def _row_stride_of(x, what):
     return ld
 
 
-def _unrecorded(name, tensors, depth=4):
-    """Says so where autograd would be expected to record a call: the operators work on the tensors' memory and return
-    plain results.  depth: frames up to the user's call."""
-    for t in tensors:
-        if t is not None and t.requires_grad and torch.is_grad_enabled():
-            warnings.warn(f"{name} is not recorded by autograd: its result has no gradient (the gradient is a call of "
-                          f"its own; use torch.no_grad() or detach() where that is meant)", stacklevel=depth)
-            return
+def _unrecorded(name, depth=4):
+    """Says that a call whose inputs require a gradient is not recorded, where autograd is on: the operators work on the
+    tensors' memory and return plain results.  depth: frames up to the user's call."""
+    if torch.is_grad_enabled():
+        warnings.warn(f"{name} is not recorded by autograd: its result has no gradient (the gradient is a call of its "
+                      f"own; use torch.no_grad() or detach() where that is meant)", stacklevel=depth)
 
 
 def _vector(t, size, what, device):
@@ -865,7 +863,8 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
         x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
         eps, kind, prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
         "ff_group_norm_act")
-    _unrecorded("group_norm_act", (x, gamma, beta))
+    if x.requires_grad or (gamma is not None and gamma.requires_grad) or (beta is not None and beta.requires_grad):
+        _unrecorded("group_norm_act")
     return out, mean, rstd
 
 
@@ -932,7 +931,8 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
                             None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
                             on), "ff_dropout")
-    _unrecorded("dropout", (x, residual))
+    if x.requires_grad or (residual is not None and residual.requires_grad):
+        _unrecorded("dropout")
     return out
 
 
@@ -988,7 +988,8 @@ def _fp8_quantize(x, tile, straight, transposed, stream):
                                  a.q.data_ptr() if a else None, a.scale.data_ptr() if a else None,
                                  t.q.data_ptr() if t else None, t.scale.data_ptr() if t else None, on),
            "ff_fp8_quantize")
-    _unrecorded("fp8_quantize", (x,), depth=5)
+    if x.requires_grad:
+        _unrecorded("fp8_quantize", depth=5)
     return a, t
 
 
@@ -1037,7 +1038,8 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
                                n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
                                _ptr(status, torch.int32, "status"), on), "ff_fp8_matmul")
-    _unrecorded("fp8_matmul", (bias,))
+    if bias is not None and bias.requires_grad:
+        _unrecorded("fp8_matmul")
     return out
 
 
