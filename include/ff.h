@@ -587,8 +587,8 @@ FF_API ff_status ff_dropout(const void* x, long long ldx, long long rows, long l
 FF_API long long ff_dropout_words(long long rows, long long cols);
 
 /* 8-bit matrices.  A matrix [rows, k] is held as e4m3 values q [rows,
- * ff_fp8_stride(k)] (bytes; the pad columns are written as zero) and fp32
- * scales, one for each block of 128 consecutive k of
+ * ff_fp8_stride(k)] (bytes; the pad columns are written as zero, in a block that
+ * holds a NaN as NaN) and fp32 scales, one for each block of 128 consecutive k of
  *   FF_FP8_ROWS   one row:            scale [ceil(k/128), rows]
  *   FF_FP8_TILES  128 rows from a multiple of 128: scale [ceil(k/128), ceil(rows/128)]
  * k-block-major and dense, so that x[r, c] ~ q[r, c] * scale[c/128, r or r/128].
