@@ -638,6 +638,113 @@ FF_API ff_status ff_fp8_check(void* stream);
  * ff_fp8_check reads it. */
 FF_API ff_status ff_fp8_selftest_wait(unsigned int timeout_us, void* stream);
 
+/* RMS norm with the residual's addition, over the rows of x [rows, cols]:
+ *   h = x + residual (rounded to prec; residual NULL: h is x itself),
+ *   rstd = 1 / sqrt(average h^2 + eps), y = gamma[c] * h * rstd.
+ * y: rounded once, to prec.  q, scale: y as an 8-bit matrix in FF_FP8_ROWS blocks
+ * (q [rows, ff_fp8_stride(cols)], 16-byte aligned, scale [ceil(cols/128), rows]),
+ * quantized as ff_fp8_quantize does, from fp32.  Either may be NULL, not both.
+ * gamma [cols] fp32, NULL: ones.  h is required with a residual and NULL
+ * without.  rstd [rows] fp32 or NULL.  y may be x or the residual itself, and
+ * so may h (but not both the same).  Squares are formed in fp32: magnitudes past
+ * 2^63 overflow (rstd is then 0); a NaN in a row makes the whole row NaN. */
+FF_API ff_status ff_rms_norm(const void* x, long long ldx, const void* residual, long long ldr, int rows, int cols,
+                             const float* gamma, float eps, ff_precision prec, void* h, long long ldh, void* y,
+                             long long ldy, void* q, float* scale, float* rstd, void* stream);
+
+/* Bytes of workspace that the gradient below needs for these sizes; -1 on
+ * sizes that it would refuse. */
+FF_API long long ff_rms_norm_workspace(int rows, int cols);
+
+/* Its gradient, from dy and the forward call's h (x without a residual) and
+ * rstd.  With n = h rstd and du = gamma dy, and <.> the average over a row:
+ *   dx = rstd (du - n <du n>) + dh,   dgamma = sum over rows of dy n.
+ * dx is the gradient of x and of the residual alike; dh [rows, cols] is what
+ * the residual stream hands back, or NULL.  dx may be dy, h or dh itself; dx or
+ * dgamma [cols] fp32 may be NULL.  Sums have a fixed order.  No rows: dgamma
+ * is set to zero. */
+FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy, const void* h, long long ldh, int rows, int cols,
+                                      const float* rstd, const float* gamma, const void* dh, long long lddh,
+                                      ff_precision prec, void* dx, long long lddx, float* dgamma, void* workspace,
+                                      long long workspace_bytes, void* stream);
+
+/* Log-probabilities of labels under the softmax of logits x [rows, classes].
+ * With m = max x, s = sum e^(x - m):
+ *   logp[r] = x[r, label] - m - ln s        (0 where labels[r] is outside 0..classes-1)
+ *   entropy[r] = -sum p ln p
+ *   top_index, top_logp [rows, top]: the likeliest classes, the lower index first
+ *     among equals, and their log-probabilities; 0 <= top <= min(32, classes)
+ *   stats [rows, 2] (8-byte aligned): m and ln s, what the gradient needs.
+ * Any of logp, entropy and stats may be NULL; labels (int32) may be with logp.
+ * Classes masked with -infinity have probability zero, as long as one is left:
+ * a row of -infinity only, and one with a NaN or +infinity, has NaN results
+ * (its top_index holds classes all the same). */
+FF_API ff_status ff_label_logprobs(const void* logits, long long ld, int rows, int classes, ff_precision prec,
+                                   const int* labels, float* logp, float* entropy, int top, float* top_logp,
+                                   int* top_index, float* stats, void* stream);
+
+/* Its gradient, from the forward call's logits, labels and stats:
+ *   dx = dlogp (1[label] - p) - dentropy p (ln p + entropy)
+ * dlogp, dentropy [rows] fp32 or NULL (none); dentropy needs the forward call's
+ * entropy, dlogp the labels.  dlogits (type prec) may be the logits.  A row of
+ * which nothing is asked (no label or dlogp 0, and dentropy 0) gets zeros,
+ * whatever its logits hold. */
+FF_API ff_status ff_label_logprobs_backward(const void* logits, long long ld, int rows, int classes, ff_precision prec,
+                                            const int* labels, const float* stats, const float* dlogp,
+                                            const float* entropy, const float* dentropy, void* dlogits,
+                                            long long lddx, void* stream);
+
+/* Bytes of workspace that the next call needs for n tensors; -1 for n < 0. */
+FF_API long long ff_clip_grad_norm_workspace(int n);
+
+/* The 2-norm over n tensors of gradients together, and the tensors scaled so
+ * that it is at most max_norm:  norm = sqrt(sum g^2) [1] fp32 (device),
+ * out = g min(1, max_norm / norm), rounded once.  grads, out, counts (elements)
+ * and precs (an ff_precision each) are HOST arrays of n, read before the call
+ * returns; the pointers in them are device pointers of dense tensors.  out[i]
+ * may be grads[i] (where nothing is clipped it is then not written); other
+ * overlaps of outputs are FF_ERR_INVALID_ARG, so no tensor may come twice.
+ * Squares are formed in fp32 and added up in fp64, in a fixed order: a
+ * magnitude past 2^63 makes the norm infinite (and finite gradients zero), a NaN
+ * everything NaN.  Empty tensors are skipped.  max_norm >= 0 (infinity: only
+ * the norm is wanted). */
+FF_API ff_status ff_clip_grad_norm(const void* const* grads, void* const* out, const long long* counts, const int* precs,
+                                   int n, float max_norm, float* norm, void* workspace, long long workspace_bytes,
+                                   void* stream);
+
+/* 4-bit matrices.  A matrix [rows, k] is held as e2m1 values (0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6 and their negatives), two to a byte, the even column in the low four
+ * bits: q [rows, ff_fp4_stride(k)]; and a power-of-two scale for each block of
+ * 32 consecutive k, a byte e that stands for 2^(e - 127).  The scales come in
+ * tiles of 128 rows and four blocks, [ceil(rows/128), ceil(blocks/4)] of them,
+ * dense: row 32 i + j of a tile and block b of it are byte 16 j + 4 i + b of 512.
+ * Columns and rows that fill up blocks and tiles hold zeros (a scale byte
+ * there must not be 255).  e = 255 marks a block that held an infinity or a
+ * NaN: all of it, and every product that reads it, is NaN. */
+FF_API int ff_fp4_stride(int k);                          /* bytes: 16 ceil(k / 32) */
+FF_API long long ff_fp4_scale_bytes(int rows, int k);     /* 512 ceil(rows/128) ceil(k/128); -1: refused sizes */
+
+/* Quantizes x [rows, k] (row stride ldx).  Per block: the scale is 2 to the power
+ * floor(log2 max |x|) - 2 (at least 2^-127), q = e2m1(x / scale) to nearest even,
+ * at most 6.  q, scale: x in blocks along k; qt, scale_t: x's transpose [k, rows]
+ * in blocks along the rows.  Either pair may be NULL, not both; x is read once
+ * for both.  All four 16-byte aligned. */
+FF_API ff_status ff_fp4_quantize(const void* x, long long ldx, int rows, int k, ff_precision prec, void* q, void* scale,
+                                 void* qt, void* scale_t, void* stream);
+
+/* y [rows, k] (type prec, row stride ldy): what a 4-bit matrix stands for, exactly. */
+FF_API ff_status ff_fp4_dequantize(const void* q, const void* scale, int rows, int k, ff_precision prec, void* y,
+                                   long long ldy, void* stream);
+
+/* C [m, n] = act(A B^T + bias) of two 4-bit matrices A [m, k], B [n, k], as
+ * ff_fp8_matmul otherwise: the tensor cores form products and sums in fp32 and
+ * apply the scales.  A layer's three products: y = x w^T; dx = dy w with the
+ * transposes' form of w; dw = dy^T x with those of dy and x.  A timeout without
+ * a device_status latches where ff_fp8_check reads it. */
+FF_API ff_status ff_fp4_matmul(const void* a, const void* a_scale, const void* b, const void* b_scale, int m, int n, int k,
+                               const float* bias, int relu, ff_precision out_prec, void* c, long long ldc,
+                               int* device_status, void* stream);
+
 /* ---------------------------------------------------------------------------
  * Instrumentation (not part of the method).
  * Every kernel launch libff makes is counted; ff_kernel_launches returns the

@@ -29,7 +29,7 @@ CHECKED_LIB_PATH = os.path.join(HERE, "libff_checked.so")
 SOURCES = ["ff_api.cu", "ff_net.cu", "ff_elem.cu", "ff_gemm_tc.cu", "ff_gemm_simt.cu", "ff_prof.cu", "ff_noalloc.cu",
            "ff_head.cu", "ff_pff.cu", "ff_epoch.cu", "ff_norm.cu", "ff_norm_rows.cu", "ff_norm_block.cu",
            "ff_dropout.cu", "ff_fp8.cu",
-           "ff_fp8_gemm.cu"]
+           "ff_fp8_gemm.cu", "ff_rms.cu", "ff_logprobs.cu", "ff_clip.cu", "ff_fp4.cu", "ff_fp4_gemm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [
     "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-O2", "-Xcompiler", "-fvisibility=hidden",

@@ -1,0 +1,345 @@
+// The 2-norm over many gradients, and the gradients scaled so that it is at
+// most max_norm:  norm = sqrt(sum g^2), out = g min(1, max_norm / norm).
+//
+// The tensors are cut into pieces of 16 KB that thread groups of 256 take in
+// turn.  Few pieces: one cluster of blocks keeps them in registers between the
+// sum and the product (one read).  Many: a pass for the sums, one partial a
+// block, and a pass in the opposite order for the products, which finds the
+// last pieces in L2.
+#include <algorithm>
+#include <vector>
+
+#include "ff_api_internal.h"
+#include "ff_ptx.cuh"
+#include "ff_vec.cuh"
+
+namespace ff {
+namespace {
+
+constexpr int GROUP = 256;             // threads that take a piece
+constexpr int VECS = 4;                // 16-byte vectors of it per thread
+constexpr int PIECE = GROUP * VECS * 16;  // bytes
+constexpr int kTable = 120;            // tensors a launch
+constexpr int kBlocks = 152 * 8;       // blocks of the two passes, one group each
+constexpr int kClusterBlocks = 8, kClusterGroups = 4, kKept = 2;  // pieces kept: 8 * 4 * 2
+
+struct Table {
+  const void* in[kTable];
+  void* out[kTable];
+  long long count[kTable];
+  int first[kTable + 1];  // a tensor's first piece; [n]: all pieces
+  uint8_t bf16s[kTable];
+  int n;
+};
+
+__device__ __forceinline__ int tensor_of(const Table& t, int piece) {
+  int lo = 0, hi = t.n - 1;  // the last tensor whose first piece is not behind this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.first[mid] <= piece) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// One thread's part of a piece, as loaded.  Past the end: zeros.
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / (int)sizeof(T);
+  static __device__ __forceinline__ void load(uint4 (&r)[VECS], const T* p, long long left, int tid, bool wide) {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      const int i = (j * GROUP + tid) * N;
+      if (wide && i + N <= left) {
+        r[j] = *reinterpret_cast<const uint4*>(p + i);
+      } else {
+        T v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = i + e < left ? p[i + e] : T(0.f);
+        memcpy(&r[j], v, 16);
+      }
+    }
+  }
+  static __device__ __forceinline__ float squares(const uint4 (&r)[VECS]) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      float v[N];
+      Vec<T, N>::unpack(r[j], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s = fmaf(v[e], v[e], s);
+    }
+    return s;
+  }
+  static __device__ __forceinline__ void store(const uint4 (&r)[VECS], T* p, long long left, int tid, bool wide, float by) {
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+      const int i = (j * GROUP + tid) * N;
+      float v[N];
+      Vec<T, N>::unpack(r[j], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] *= by;
+      if (wide && i + N <= left) {
+        Vec<T, N>::store(p + i, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float one[1] = {v[e]};
+          if (i + e < left) Vec<T, 1>::store(p + i + e, one);
+        }
+      }
+    }
+  }
+};
+__device__ __forceinline__ bool wide_at(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// What a piece is: its tensor, where it starts and what is left of the tensor from there.
+struct At {
+  int t;
+  long long from, left;
+};
+__device__ __forceinline__ At at_piece(const Table& t, int piece) {
+  At a;
+  a.t = tensor_of(t, piece);
+  a.from = (long long)(piece - t.first[a.t]) * (PIECE / (t.bf16s[a.t] ? 2 : 4));
+  a.left = t.count[a.t] - a.from;
+  return a;
+}
+__device__ __forceinline__ void load_piece(const Table& t, const At& a, uint4 (&r)[VECS], int tid) {
+  const bool wide = wide_at(t.in[a.t]);
+  if (t.bf16s[a.t]) Piece<bf16>::load(r, static_cast<const bf16*>(t.in[a.t]) + a.from, a.left, tid, wide);
+  else Piece<float>::load(r, static_cast<const float*>(t.in[a.t]) + a.from, a.left, tid, wide);
+}
+__device__ __forceinline__ float piece_squares(const Table& t, const At& a, const uint4 (&r)[VECS]) {
+  return t.bf16s[a.t] ? Piece<bf16>::squares(r) : Piece<float>::squares(r);
+}
+__device__ __forceinline__ void store_piece(const Table& t, const At& a, const uint4 (&r)[VECS], int tid, float by) {
+  const bool wide = wide_at(t.out[a.t]);
+  if (t.bf16s[a.t]) Piece<bf16>::store(r, static_cast<bf16*>(t.out[a.t]) + a.from, a.left, tid, wide, by);
+  else Piece<float>::store(r, static_cast<float*>(t.out[a.t]) + a.from, a.left, tid, wide, by);
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// The factor: 1 where nothing is to be clipped; NaN for a NaN norm.
+__device__ __forceinline__ float factor(float norm, float max_norm) {
+  const float by = __fdiv_rn(max_norm, norm);
+  return norm == 0.f || by > 1.f ? 1.f : by;
+}
+
+// All pieces in one cluster's registers.
+__global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
+    k_clip_small(const __grid_constant__ Table t, float max_norm, float* norm_out, int pieces, int nblocks) {
+  __shared__ double part[kClusterBlocks];
+  __shared__ double warps[GROUP * kClusterGroups / 32];
+  if (nblocks > 1) ptx::cluster_arrive();
+  ptx::griddep_wait();
+  const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int groups = blockDim.x / GROUP, tid = threadIdx.x & (GROUP - 1);
+  const int first = rank * groups + threadIdx.x / GROUP, step = groups * nblocks;
+  uint4 r[kKept][VECS];
+  double s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if (first + k * step < pieces) load_piece(t, at_piece(t, first + k * step), r[k], tid);
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if (first + k * step < pieces) s += piece_squares(t, at_piece(t, first + k * step), r[k]);
+  s = warp_sum(s);
+  if (lane == 0) warps[warp] = s;
+  __syncthreads();
+  if (nblocks > 1) ptx::cluster_wait();
+  if (warp == 0) {
+    s = warp_sum(lane < (int)(blockDim.x >> 5) ? warps[lane] : 0.0);
+    if (nblocks == 1) {
+      if (lane == 0) part[0] = s;
+    } else if (lane < nblocks) {
+      const uint2 w = make_uint2((uint32_t)__double2loint(s), (uint32_t)__double2hiint(s));
+      ptx::st_remote_u2(reinterpret_cast<uint2*>(&part[rank]), (uint32_t)lane, w);
+    }
+  }
+  if (nblocks > 1) ptx::cluster_sync();
+  else __syncthreads();
+  s = 0.0;
+  for (int b = 0; b < nblocks; ++b) s += part[b];
+  const float norm = (float)sqrt(s);
+  if (rank == 0 && threadIdx.x == 0) *norm_out = norm;
+  const float by = factor(norm, max_norm);
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if (first + k * step < pieces) {
+      const At a = at_piece(t, first + k * step);
+      if (by != 1.f || t.in[a.t] != t.out[a.t]) store_piece(t, a, r[k], tid, by);
+    }
+}
+
+// part[blockIdx.x] = the sum of squares of the block's pieces.
+__global__ void __launch_bounds__(GROUP) k_clip_sums(const __grid_constant__ Table t, int pieces, double* part) {
+  __shared__ double warps[GROUP / 32];
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double s = 0.0;
+  for (int p = blockIdx.x; p < pieces; p += gridDim.x) {
+    uint4 r[VECS];
+    const At a = at_piece(t, p);
+    load_piece(t, a, r, threadIdx.x);
+    s += piece_squares(t, a, r);
+  }
+  s = warp_sum(s);
+  if (lane == 0) warps[warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < GROUP / 32; ++w) s += warps[w];
+    part[blockIdx.x] = s;
+  }
+}
+__global__ void __launch_bounds__(GROUP)
+    k_clip_scale(const __grid_constant__ Table t, int pieces, const double* part, int parts, float max_norm, float* norm_out) {
+  __shared__ double warps[GROUP / 32];
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += GROUP) s += part[i];
+  s = warp_sum(s);
+  if (lane == 0) warps[warp] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < GROUP / 32; ++w) s += warps[w];
+  const float norm = (float)sqrt(s), by = factor(norm, max_norm);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  for (int p = pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {
+    const At a = at_piece(t, p);
+    if (by == 1.f && t.in[a.t] == t.out[a.t]) continue;
+    uint4 r[VECS];
+    load_piece(t, a, r, threadIdx.x);
+    store_piece(t, a, r, threadIdx.x, by);
+  }
+}
+
+struct Tensor {
+  const void* in;
+  void* out;
+  long long count;
+  bool half;
+  long long bytes() const { return count * (half ? 2 : 4); }
+};
+
+int tables_of(int n) { return n <= kTable ? 1 : cdiv(n, kTable); }
+
+ff_status clip(const std::vector<Tensor>& all, float max_norm, float* norm, double* part, cudaStream_t st) {
+  const int n = (int)all.size(), tables = tables_of(n);
+  std::vector<Table> ts((size_t)tables);
+  std::vector<long long> bytes((size_t)tables, 0);
+  long long total = 0;
+  for (int k = 0; k < tables; ++k) {
+    Table& t = ts[k];
+    t.n = 0;
+    long long pieces = 0;
+    for (int i = k * kTable; i < n && i < (k + 1) * kTable; ++i) {
+      const Tensor& e = all[i];
+      t.in[t.n] = e.in;
+      t.out[t.n] = e.out;
+      t.count[t.n] = e.count;
+      t.bf16s[t.n] = e.half;
+      t.first[t.n++] = (int)pieces;
+      pieces += (e.bytes() + PIECE - 1) / PIECE;
+      if (pieces > 0x7FFF0000ll) return FF_ERR_UNSUPPORTED;
+      bytes[k] += e.bytes();
+    }
+    t.first[t.n] = (int)pieces;
+    total += pieces;
+  }
+  if (tables == 1 && total <= kClusterBlocks * kClusterGroups * kKept) {
+    const int blocks = total <= kClusterGroups ? 1 : total <= 2 * kClusterGroups ? 2 : total <= 4 * kClusterGroups ? 4 : kClusterBlocks;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)(GROUP * std::max(1, (int)std::min<long long>(total, kClusterGroups))));
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)blocks;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    FF_LAUNCH(K_CLIP, 2.0 * bytes[0], st, cudaLaunchKernelEx(&cfg, k_clip_small, ts[0], max_norm, norm, (int)total, blocks),
+              "gradient clipping");
+    return FF_OK;
+  }
+  for (int k = 0; k < tables; ++k) {
+    PdlLaunch l(dim3(kBlocks), dim3(GROUP), st);
+    FF_LAUNCH(K_CLIP, (double)bytes[k], st,
+              cudaLaunchKernelEx(&l.cfg, k_clip_sums, ts[k], ts[k].first[ts[k].n], part + (long long)k * kBlocks),
+              "gradient clipping");
+  }
+  for (int k = tables - 1; k >= 0; --k) {
+    PdlLaunch l(dim3(kBlocks), dim3(GROUP), st);
+    FF_LAUNCH(K_CLIP, 2.0 * bytes[k], st,
+              cudaLaunchKernelEx(&l.cfg, k_clip_scale, ts[k], ts[k].first[ts[k].n], (const double*)part, tables * kBlocks,
+                                 max_norm, norm),
+              "gradient clipping");
+  }
+  return FF_OK;
+}
+
+}  // namespace
+}  // namespace ff
+
+using namespace ff;
+
+extern "C" FF_API long long ff_clip_grad_norm_workspace(int n) {
+  return n < 0 ? -1 : 8ll * kBlocks * tables_of(n);
+}
+
+extern "C" FF_API ff_status ff_clip_grad_norm(const void* const* grads, void* const* out, const long long* counts,
+                                              const int* precs, int n, float max_norm, float* norm, void* workspace,
+                                              long long workspace_bytes, void* stream) {
+  if (n < 0 || !(max_norm >= 0.f) || !norm || reinterpret_cast<uintptr_t>(norm) % 4 != 0 ||
+      (n > 0 && (!grads || !out || !counts || !precs)))
+    return FF_ERR_INVALID_ARG;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || workspace_bytes < ff_clip_grad_norm_workspace(n))
+    return FF_ERR_INVALID_ARG;
+  try {
+    std::vector<Tensor> all;
+    all.reserve((size_t)n);
+    for (int i = 0; i < n; ++i) {
+      if (precs[i] != FF_FP32 && precs[i] != FF_BF16) return FF_ERR_INVALID_ARG;
+      const int es = precs[i] == FF_BF16 ? 2 : 4;
+      if (counts[i] < 0 || counts[i] > (1ll << 60)) return FF_ERR_INVALID_ARG;
+      if (counts[i] == 0) continue;
+      if (!grads[i] || !out[i] || reinterpret_cast<uintptr_t>(grads[i]) % es != 0 ||
+          reinterpret_cast<uintptr_t>(out[i]) % es != 0)
+        return FF_ERR_INVALID_ARG;
+      all.push_back(Tensor{grads[i], out[i], counts[i], precs[i] == FF_BF16});
+    }
+    // An output may be its own gradient; otherwise no output overlaps another
+    // output or any gradient (a piece is read long after others are written).
+    struct Span {
+      uintptr_t from, to;
+      int owner;
+      bool write;
+    };
+    std::vector<Span> spans;
+    spans.reserve(2 * all.size());
+    for (size_t i = 0; i < all.size(); ++i) {
+      const Tensor& e = all[i];
+      const uintptr_t o = reinterpret_cast<uintptr_t>(e.out), g = reinterpret_cast<uintptr_t>(e.in);
+      spans.push_back(Span{o, o + (uintptr_t)e.bytes(), (int)i, true});
+      if (g != o) spans.push_back(Span{g, g + (uintptr_t)e.bytes(), (int)i, false});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t written = 0, read = 0;  // ends of what outputs and gradients have covered so far
+    for (const Span& s : spans) {
+      if (s.from < written || (s.write && s.from < read)) return FF_ERR_INVALID_ARG;
+      if (s.write) written = std::max(written, s.to);
+      else read = std::max(read, s.to);
+    }
+    return clip(all, max_norm, norm, static_cast<double*>(workspace), static_cast<cudaStream_t>(stream));
+  } catch (...) {
+    return FF_ERR_OOM;
+  }
+}

@@ -1,0 +1,363 @@
+// 4-bit matrices (e2m1 values, a power-of-two scale per block of 32 along the
+// contraction): the quantizer, its inverse, and the C entries of all three
+// operations.
+#include <cuda_fp16.h>
+
+#include "ff_api_internal.h"
+#include "ff_fp4.h"
+#include "ff_fp8.h"
+#include "ff_ptx.cuh"
+#include "ff_vec.cuh"
+
+namespace ff {
+namespace {
+
+// The scale of a block by its largest magnitude, given as the exponent field
+// of that float: 2^(floor(log2 amax) - 2), which maps amax to [4, 8), held as
+// its own exponent field and at least 2^-127 (field 0, also for a block of
+// zeros).  255 marks a block that holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t scale_field(uint32_t field) { return field == 255u ? 255u : field < 2u ? 0u : field - 2u; }
+// 1 / scale: 2^(127 - field), exact in fp32 for every field but the mark.
+__device__ __forceinline__ float scale_inverse(uint32_t field) { return __uint_as_float((field > 253u ? 1u : 254u - field) << 23); }
+
+// Eight values as e2m1 codes (to nearest even, saturating), the first lowest.
+__device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+// The two values of a byte, the low four bits' first.
+__device__ __forceinline__ float2 e2m1x2_values(uint32_t byte) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t}"
+      : "=r"(h)
+      : "r"(byte));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Eight values of a row as loaded, as in the 8-bit quantizer: bf16 in pairs
+// (the low half first), or fp32; magnitudes are compared as integers.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16> {
+  static constexpr int WORDS = 4, PER = 2;
+  static constexpr uint32_t ABS = 0x7FFF7FFFu;
+  static __device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float value(const uint32_t (&w)[WORDS], int e) {
+    return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+  }
+  static __device__ __forceinline__ uint32_t field(uint32_t w, int h) { return h ? w >> 23 : (w >> 7) & 0xFFu; }  // of a magnitude
+};
+template <>
+struct Eight<float> {
+  static constexpr int WORDS = 8, PER = 1;
+  static constexpr uint32_t ABS = 0x7FFFFFFFu;
+  static __device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return max(a, b); }
+  static __device__ __forceinline__ float value(const uint32_t (&w)[WORDS], int e) { return __uint_as_float(w[e]); }
+  static __device__ __forceinline__ uint32_t field(uint32_t w, int) { return w >> 23; }
+};
+
+constexpr int QT = 128;  // a tile: 128 x 128 values, one scale tile each way
+constexpr int kQThreads = 256;
+constexpr int kPitch = 17;  // words a staged column: 16, and one against bank conflicts
+
+// One thread block per 128 x 128 tile; a warp takes 32 rows x 64 columns of
+// it, a thread 8 x 8 (all its loads in flight together), so that both a row's
+// block of 32 columns and a column's block of 32 rows lie within a warp and
+// their maxima take two shuffles.
+// LOAD: bytes of x per access that its rows' alignment allows.
+template <typename T, int LOAD>
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
+    k_fp4_quantize(const T* x, long long ldx, int rows, int k, uint8_t* q, uint8_t* scale, uint8_t* qt, uint8_t* scale_t,
+                   int ldq, int ldqt, int ktiles, int rtiles) {
+  using E = Eight<T>;
+  constexpr int W = E::WORDS, PER = E::PER;
+  __shared__ uint32_t tq[QT * kPitch];
+  __shared__ __align__(16) uint8_t sc[kFp4ScaleTile], sct[kFp4ScaleTile];
+  ptx::griddep_wait();
+  const int kt = blockIdx.x % ktiles, rt = blockIdx.x / ktiles;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int wr = warp >> 1, wc = warp & 1, rg = lane >> 3, cg = lane & 7;
+  const int r_in = wr * 32 + rg * 8, c_in = wc * 64 + cg * 8;
+  const int row0 = rt * QT + r_in, c0 = kt * QT + c_in;
+  uint32_t v[8][W];
+  const T* p = x + (long long)row0 * ldx + c0;
+  if (LOAD == 16 && c0 + 8 <= k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < W / 4; ++j)
+        *reinterpret_cast<uint4*>(&v[i][4 * j]) =
+            row0 + i < rows ? reinterpret_cast<const uint4*>(p + i * ldx)[j] : make_uint4(0, 0, 0, 0);
+  } else if (LOAD == 4 && c0 + 8 <= k) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i][j] = row0 + i < rows ? reinterpret_cast<const uint32_t*>(p + i * ldx)[j] : 0u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int h = 0; h < PER; ++h)
+          if (row0 + i < rows && c0 + j * PER + h < k)
+            w |= (uint32_t)Vec<T, 1>::load(p + i * ldx + j * PER + h) << (16 * h);
+        v[i][j] = w;
+      }
+  }
+  if (q) {
+    uint32_t m[8 / PER];  // word j: rows j PER .. (one per half of the word)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t t = v[i][0] & E::ABS;
+#pragma unroll
+      for (int j = 1; j < W; ++j) t = E::max_of(t, v[i][j] & E::ABS);
+      if constexpr (PER == 2) {
+        t = max(t & 0xFFFFu, t >> 16);
+        m[i / 2] = i & 1 ? m[i / 2] | t << 16 : t;
+      } else {
+        m[i] = t;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o <= 2; o *= 2)
+#pragma unroll
+      for (int j = 0; j < 8 / PER; ++j) m[j] = E::max_of(m[j], __shfl_xor_sync(0xffffffffu, m[j], o));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t f = scale_field(E::field(m[i / PER], i % PER));
+      const float inv = scale_inverse(f);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(E::value(v[i], e), inv);
+      // ldq covers whole blocks of 32: eight columns lie inside or outside
+      if (row0 + i < rows && c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(q + (long long)(row0 + i) * ldq + c0 / 2) = e2m1x8(y);
+      if ((cg & 3) == 0) sc[(rg * 8 + i) * 16 + wr * 4 + wc * 2 + (cg >> 2)] = (uint8_t)f;
+    }
+  }
+  if (qt) {
+    uint32_t m[W];  // word j: columns j PER ..
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      m[j] = v[0][j] & E::ABS;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) m[j] = E::max_of(m[j], v[i][j] & E::ABS);
+    }
+#pragma unroll
+    for (int o = 8; o <= 16; o *= 2)
+#pragma unroll
+      for (int j = 0; j < W; ++j) m[j] = E::max_of(m[j], __shfl_xor_sync(0xffffffffu, m[j], o));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t f = scale_field(E::field(m[e / PER], e % PER));
+      const float inv = scale_inverse(f);
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(E::value(v[i], e), inv);
+      const int c = c_in + e;
+      tq[c * kPitch + wr * 4 + rg] = e2m1x8(y);
+      if (rg == 0) sct[(c & 31) * 16 + (c >> 5) * 4 + wr] = (uint8_t)f;
+    }
+  }
+  __syncthreads();
+  if (q && threadIdx.x < 32)
+    reinterpret_cast<uint4*>(scale + ((long long)rt * ktiles + kt) * kFp4ScaleTile)[threadIdx.x] = reinterpret_cast<uint4*>(sc)[threadIdx.x];
+  if (qt) {
+    if (threadIdx.x >= 32 && threadIdx.x < 64)
+      reinterpret_cast<uint4*>(scale_t + ((long long)kt * rtiles + rt) * kFp4ScaleTile)[threadIdx.x - 32] =
+          reinterpret_cast<uint4*>(sct)[threadIdx.x - 32];
+    // 4 threads per column of the tile, 16 bytes (a block of 32 rows) each
+    const int u = threadIdx.x & 3, at = rt * (QT / 2) + u * 16;
+    if (at < ldqt) {
+#pragma unroll
+      for (int c = threadIdx.x >> 2; c < QT; c += kQThreads / 4) {
+        const long long col = (long long)kt * QT + c;
+        if (col >= k) break;
+        const uint32_t* t = tq + c * kPitch + u * 4;
+        *reinterpret_cast<uint4*>(qt + col * ldqt + at) = make_uint4(t[0], t[1], t[2], t[3]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ float scale_value(uint32_t field) {  // 2^(field - 127)
+  return __uint_as_float(field == 0u ? 0x00400000u : field == 255u ? 0x7FC00000u : field << 23);
+}
+__device__ __forceinline__ uint32_t scale_at(const uint8_t* scale, int ktiles, int row, int block) {
+  return __ldg(scale + ((long long)(row >> 7) * ktiles + (block >> 2)) * kFp4ScaleTile + (row & 31) * 16 + (row >> 5 & 3) * 4 +
+               (block & 3));
+}
+
+// y = value * scale, exact in either type.  WIDE: y's rows are 16-byte aligned,
+// and a thread takes 8 values (4 bytes) at a time; else one, the lanes side by
+// side.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256)
+    k_fp4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int k, int ldq, int ktiles, T* y, long long ldy,
+                     int per_row) {
+  ptx::griddep_wait();
+  const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;  // a row's units of 8 columns, 32-bit words of q
+  if constexpr (WIDE) {
+    const long long r = unit / per_row;
+    if (r >= rows) return;
+    const int c = (int)(unit - r * per_row) * 8;
+    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(q + r * ldq + c / 2));
+    const float s = scale_value(scale_at(scale, ktiles, (int)r, c / kFp4Block));
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = e2m1x2_values(w >> (8 * i));
+      v[2 * i] = f.x * s;
+      v[2 * i + 1] = f.y * s;
+    }
+    T* to = y + r * ldy + c;
+    if (c + 8 <= k) {
+#pragma unroll
+      for (int h = 0; h < 8; h += 16 / (int)sizeof(T)) {
+        float t[16 / sizeof(T)];
+#pragma unroll
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) t[e] = v[h + e];
+        Vec<T, 16 / (int)sizeof(T)>::store(to + h, t);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float one[1] = {v[e]};
+        if (c + e < k) Vec<T, 1>::store(to + e, one);
+      }
+    }
+  } else {
+    const long long r = unit / per_row;  // units of one column, padded to whole warps
+    const int c = (int)(unit - r * per_row);
+    if (r >= rows || c >= k) return;
+    const float2 f = e2m1x2_values(__ldg(q + r * ldq + c / 2));
+    const float one[1] = {(c & 1 ? f.y : f.x) * scale_value(scale_at(scale, ktiles, (int)r, c / kFp4Block))};
+    Vec<T, 1>::store(y + r * ldy + c, one);
+  }
+}
+
+template <typename T>
+ff_status quantize_t(const T* x, long long ldx, int rows, int k, uint8_t* q, uint8_t* scale, uint8_t* qt, uint8_t* scale_t,
+                     cudaStream_t st) {
+  const int ktiles = cdiv(k, QT), rtiles = cdiv(rows, QT);
+  const long long blocks = (long long)ktiles * rtiles;
+  if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+  const double bytes = (double)rows * k * (sizeof(T) + (q ? 0.5 : 0) + (qt ? 0.5 : 0));
+  const int ldq = fp4_stride(k), ldqt = fp4_stride(rows);
+  PdlLaunch l(dim3((unsigned)blocks), dim3(kQThreads), st);
+  auto go = [&](auto* kernel) {
+    return cudaLaunchKernelEx(&l.cfg, kernel, x, ldx, rows, k, q, scale, qt, scale_t, ldq, ldqt, ktiles, rtiles);
+  };
+  auto* const kernel = rows_aligned(x, ldx, sizeof(T), 16)  ? k_fp4_quantize<T, 16>
+                       : rows_aligned(x, ldx, sizeof(T), 4) ? k_fp4_quantize<T, 4>
+                                                            : k_fp4_quantize<T, sizeof(T)>;
+  FF_LAUNCH(K_FP4_QUANT, bytes, st, go(kernel), "4-bit quantize");
+  return FF_OK;
+}
+
+template <typename T>
+ff_status dequantize_t(const uint8_t* q, const uint8_t* scale, int rows, int k, T* y, long long ldy, cudaStream_t st) {
+  const bool wide = rows_aligned(y, rows > 1 ? ldy : 0, sizeof(T), 16);
+  const int per_row = wide ? cdiv(k, 8) : cdiv(k, 32) * 32;
+  const long long blocks = ((long long)rows * per_row + 255) / 256;
+  if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+  const double bytes = (double)rows * k * (sizeof(T) + 0.5);
+  PdlLaunch l(dim3((unsigned)blocks), dim3(256), st);
+  auto go = [&](auto* kernel) {
+    return cudaLaunchKernelEx(&l.cfg, kernel, q, scale, rows, k, fp4_stride(k), cdiv(k, QT), y, ldy, per_row);
+  };
+  auto* const kernel = wide ? k_fp4_dequantize<T, true> : k_fp4_dequantize<T, false>;
+  FF_LAUNCH(K_FP4_DEQUANT, bytes, st, go(kernel), "4-bit dequantize");
+  return FF_OK;
+}
+
+bool aligned(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+}  // namespace
+}  // namespace ff
+
+using namespace ff;
+
+constexpr int kMostSize = 0x7FFFFF00;
+
+extern "C" FF_API int ff_fp4_stride(int k) { return k > 0 && k <= kMostSize ? fp4_stride(k) : 0; }
+extern "C" FF_API long long ff_fp4_scale_bytes(int rows, int k) {
+  return rows < 0 || rows > kMostSize || k < 1 || k > kMostSize ? -1 : fp4_scale_bytes(rows, k);
+}
+
+extern "C" FF_API ff_status ff_fp4_quantize(const void* x, long long ldx, int rows, int k, ff_precision prec, void* q, void* scale,
+                                            void* qt, void* scale_t, void* stream) {
+  if (rows < 0 || k < 1 || rows > kMostSize || k > kMostSize || (prec != FF_FP32 && prec != FF_BF16)) return FF_ERR_INVALID_ARG;
+  if (rows == 0) return FF_OK;
+  const int es = prec == FF_BF16 ? 2 : 4;
+  if (!x || !aligned(x, es) || (ldx < k && rows > 1) || (q == nullptr) != (scale == nullptr) ||
+      (qt == nullptr) != (scale_t == nullptr) || (!q && !qt) || !aligned(q, 16) || !aligned(qt, 16) || !aligned(scale, 16) ||
+      !aligned(scale_t, 16))
+    return FF_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto run = [&](auto t) {
+    using T = decltype(t);
+    return quantize_t(static_cast<const T*>(x), ldx, rows, k, static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale),
+                      static_cast<uint8_t*>(qt), static_cast<uint8_t*>(scale_t), st);
+  };
+  return prec == FF_BF16 ? run(bf16{}) : run(float{});
+}
+
+extern "C" FF_API ff_status ff_fp4_dequantize(const void* q, const void* scale, int rows, int k, ff_precision prec, void* y,
+                                              long long ldy, void* stream) {
+  if (rows < 0 || k < 1 || rows > kMostSize || k > kMostSize || (prec != FF_FP32 && prec != FF_BF16)) return FF_ERR_INVALID_ARG;
+  if (rows == 0) return FF_OK;
+  const int es = prec == FF_BF16 ? 2 : 4;
+  if (!q || !scale || !y || !aligned(q, 16) || !aligned(scale, 16) || !aligned(y, es) || (ldy < k && rows > 1))
+    return FF_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const uint8_t *qb = static_cast<const uint8_t*>(q), *sb = static_cast<const uint8_t*>(scale);
+  return prec == FF_BF16 ? dequantize_t(qb, sb, rows, k, static_cast<bf16*>(y), ldy, st)
+                         : dequantize_t(qb, sb, rows, k, static_cast<float*>(y), ldy, st);
+}
+
+extern "C" FF_API ff_status ff_fp4_matmul(const void* a, const void* a_scale, const void* b, const void* b_scale, int m, int n,
+                                          int k, const float* bias, int relu, ff_precision out_prec, void* c, long long ldc,
+                                          int* device_status, void* stream) {
+  if (m < 0 || n < 0 || k < 1 || m > kMostSize || n > kMostSize || k > kMostSize ||
+      (out_prec != FF_FP32 && out_prec != FF_BF16))
+    return FF_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return FF_OK;
+  const int es = out_prec == FF_BF16 ? 2 : 4;
+  if (!a || !a_scale || !b || !b_scale || !c || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 16) ||
+      !aligned(b_scale, 16) || !aligned(bias, 4) || !aligned(device_status, 4) || !aligned(c, es) || (ldc < n && m > 1))
+    return FF_ERR_INVALID_ARG;
+  if (!tc_supported()) return FF_ERR_UNSUPPORTED;
+  Fp4Gemm g{};
+  g.a = static_cast<const uint8_t*>(a);
+  g.b = static_cast<const uint8_t*>(b);
+  g.sa = static_cast<const uint8_t*>(a_scale);
+  g.sb = static_cast<const uint8_t*>(b_scale);
+  g.M = m;
+  g.N = n;
+  g.K = k;
+  g.bias = bias;
+  g.relu = relu != 0;
+  g.out_bf16 = out_prec == FF_BF16;
+  g.c = c;
+  g.ldc = ldc;
+  g.status = device_status;
+  if (!device_status) FF_TRY(own_status(&g.status), "4-bit matrix product");
+  return fp4_gemm(g, static_cast<cudaStream_t>(stream));
+}

@@ -1,8 +1,7 @@
 // 8-bit matrices (e4m3 values, an fp32 scale per block of 128 along the
 // contraction): the quantizer, and the C entries of both operations.
-#include <cuda_fp8.h>
-
 #include "ff_api_internal.h"
+#include "ff_e4m3.cuh"
 #include "ff_fp8.h"
 #include "ff_ptx.cuh"
 #include "ff_vec.cuh"
@@ -10,21 +9,6 @@
 namespace ff {
 namespace {
 
-constexpr float kE4m3Max = 448.f;
-constexpr float kScaleMin = 1.17549435e-38f;  // 2^-126
-
-// The scale of a block whose largest magnitude has these bits (the bits of
-// non-negative floats order like the floats, with infinity and then NaN above
-// all of them, so an integer maximum keeps both).
-__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
-  const float s = __fdiv_rn(__uint_as_float(amax_bits), kE4m3Max);
-  return s < kScaleMin ? kScaleMin : s;  // keeps NaN
-}
-
-// Two values as e4m3 (to nearest even, saturating; NaN stays NaN), a in the low byte.
-__device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-}
 __device__ __forceinline__ uint2 e4m3x8(const float (&v)[8]) {
   return make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
 }
@@ -254,9 +238,17 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, int tile, uint8
   return FF_OK;
 }
 
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+
 // Where products without a status word of the caller's latch a timeout: a word
 // on each device, so that no invalid result goes unreported.
+namespace {
 __device__ int g_fp8_status;
+}  // namespace
+
 cudaError_t own_status(int** word) {
   static PerDevice<void*> kept;
   int dev = 0;
@@ -268,10 +260,6 @@ cudaError_t own_status(int** word) {
   return e;
 }
 
-bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
-
-}  // namespace
 }  // namespace ff
 
 using namespace ff;

@@ -19,6 +19,9 @@ struct Fp8Gemm {
   int* status;            // latches timeouts
 };
 
+// The current device's word for timeouts of 8- and 4-bit products that were given none.
+cudaError_t own_status(int** word);
+
 ff_status fp8_gemm(const Fp8Gemm& g, cudaStream_t st);
 
 }  // namespace ff

@@ -25,7 +25,9 @@ const char* const kNames[K_NUM] = {"overlay",     "row_scale",    "fwd_gemm_tc",
                                    "store_gemm_tc", "store_gemm_simt", "expand",   "argmax",
                                    "head_logits", "head_wgrad",   "head_adam",
                                    "epoch_gemm_tc", "group_norm", "group_norm_grad", "dropout",
-                                   "fp8_quantize", "fp8_gemm_tc", "fp8_gemm_pair_tc"};
+                                   "fp8_quantize", "fp8_gemm_tc", "fp8_gemm_pair_tc",
+                                   "rms_norm", "rms_norm_grad", "label_logprobs", "label_logprobs_grad", "clip_grad_norm",
+                                   "fp4_quantize", "fp4_dequantize", "fp4_gemm_tc", "fp4_gemm_pair_tc"};
 
 struct Rec {
   int kind;

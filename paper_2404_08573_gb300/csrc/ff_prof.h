@@ -9,7 +9,8 @@ enum KernelKind {
   K_OVERLAY, K_ROW_SCALE, K_FWD_TC, K_FWD_SIMT, K_FINALIZE, K_GRAD_PREP, K_WGRAD_TC, K_WGRAD_SIMT,
   K_ADAM, K_INIT, K_TO_BF16, K_LABEL_COLS, K_STORE_TC, K_STORE_SIMT, K_EXPAND, K_ARGMAX,
   K_HEAD_LOGITS, K_HEAD_WGRAD, K_HEAD_ADAM, K_EPOCH,
-  K_GNORM, K_GNORM_GRAD, K_DROPOUT, K_FP8_QUANT, K_FP8_GEMM, K_FP8_PAIR, K_NUM
+  K_GNORM, K_GNORM_GRAD, K_DROPOUT, K_FP8_QUANT, K_FP8_GEMM, K_FP8_PAIR,
+  K_RMS, K_RMS_GRAD, K_LOGPROBS, K_LOGPROBS_GRAD, K_CLIP, K_FP4_QUANT, K_FP4_DEQUANT, K_FP4_GEMM, K_FP4_PAIR, K_NUM
 };
 
 // Counts one launch; when timing is enabled records an event on `st` now and

@@ -9,7 +9,10 @@ Names follow the C ABI in include/ff.h:
 ``Net`` (ff_net_*), ``Head`` (ff_head_*), ``Pff`` (ff_pff_*), ``po_train_step_raw``/
 ``po_train_step_act``/``po_predict`` (ff_po_*), ``forward_noalloc``; the
 layer operators ``group_norm_act`` and its backward pass, ``dropout``,
-``fp8_quantize`` and ``fp8_matmul`` (ff_group_norm_*, ff_dropout, ff_fp8_*).
+``fp8_quantize`` and ``fp8_matmul`` (ff_group_norm_*, ff_dropout, ff_fp8_*),
+``rms_norm``, ``rms_norm_fp8`` and ``label_logprobs`` with their backward
+passes, ``clip_grad_norm``, ``fp4_quantize``, ``fp4_dequantize`` and
+``fp4_matmul`` (ff_rms_norm*, ff_label_logprobs*, ff_clip_grad_norm, ff_fp4_*).
 """
 
 from __future__ import annotations
@@ -139,6 +142,22 @@ def lib():
                               c_void_p, c_longlong, c_void_p, c_void_p],
             "ff_fp8_check": [c_void_p],
             "ff_fp8_selftest_wait": [ctypes.c_uint, c_void_p],
+            "ff_rms_norm": [c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_int, c_void_p, c_float, c_int, c_void_p,
+                            c_longlong, c_void_p, c_longlong, c_void_p, c_void_p, c_void_p, c_void_p],
+            "ff_rms_norm_backward": [c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_int, c_void_p, c_void_p,
+                                     c_void_p, c_longlong, c_int, c_void_p, c_longlong, c_void_p, c_void_p, c_longlong,
+                                     c_void_p],
+            "ff_label_logprobs": [c_void_p, c_longlong, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_void_p,
+                                  c_void_p, c_void_p, c_void_p],
+            "ff_label_logprobs_backward": [c_void_p, c_longlong, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
+                                           c_void_p, c_void_p, c_void_p, c_longlong, c_void_p],
+            "ff_clip_grad_norm": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p, c_longlong,
+                                  c_void_p],
+            "ff_fp4_stride": [c_int],
+            "ff_fp4_quantize": [c_void_p, c_longlong, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p],
+            "ff_fp4_dequantize": [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_longlong, c_void_p],
+            "ff_fp4_matmul": [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_int, c_void_p,
+                              c_longlong, c_void_p, c_void_p],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -148,6 +167,12 @@ def lib():
         L.ff_group_norm_workspace.argtypes = [c_int] * 6
         L.ff_dropout_words.restype = c_longlong
         L.ff_dropout_words.argtypes = [c_longlong, c_longlong]
+        L.ff_rms_norm_workspace.restype = c_longlong
+        L.ff_rms_norm_workspace.argtypes = [c_int, c_int]
+        L.ff_clip_grad_norm_workspace.restype = c_longlong
+        L.ff_clip_grad_norm_workspace.argtypes = [c_int]
+        L.ff_fp4_scale_bytes.restype = c_longlong
+        L.ff_fp4_scale_bytes.argtypes = [c_int, c_int]
         _lib = L
     return _lib
 
@@ -741,7 +766,8 @@ def _on_device_of_first(f):
         try:
             index = x.get_device()
         except AttributeError:
-            raise TypeError(f"{first} must be a {'torch.Tensor' if first != 'a' else 'Fp8Matrix'}") from None
+            kind = {"a": "Fp8Matrix" if f.__name__.startswith("fp8") else "Fp4Matrix", "m": "Fp4Matrix"}
+            raise TypeError(f"{first} must be a {kind.get(first, 'torch.Tensor')}") from None
         if index < 0:
             raise ValueError(f"{first} must be a CUDA tensor")
         if index == torch._C._cuda_getDevice():
@@ -1053,3 +1079,344 @@ def fp8_check(stream=None):
 def fp8_selftest_wait(timeout_us: int, stream=None):
     """ff_fp8_selftest_wait: a bounded wait that is made to run out, for fp8_check to report."""
     _check(lib().ff_fp8_selftest_wait(int(timeout_us), c_void_p(_stream(stream))), "ff_fp8_selftest_wait")
+
+
+# ------------------------------------------------- RMS norm, log-probabilities, clipping
+def _matrix_sizes(x, what):
+    """rows, last dimension and row stride of x seen as a matrix [rows, last dimension]."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{what} must be [..., columns] with at least one column")
+    cols = x.shape[-1]
+    rows = x.numel() // cols
+    if max(rows, cols) > 0x7FFFFF00:
+        raise ValueError(f"{what}: rows and columns must each fit 32 bits")
+    return rows, cols, _row_stride_of(x, what)
+
+
+@functools.lru_cache(maxsize=4096)
+def _rms_workspace(rows, cols):
+    return lib().ff_rms_norm_workspace(rows, cols)
+
+
+def _rms_norm(x, gamma, residual, eps, out, h, fp8, stream):
+    prec, dev = _prec(x, "x"), x.device
+    rows, cols, ldx = _matrix_sizes(x, "x")
+    on, empty = _on(stream, dev, x, gamma, residual, out, h)
+    ldr = ldh = ldy = 0
+    if residual is None:
+        if h is not None:
+            raise ValueError("h goes with a residual (without one it is x)")
+        kept, ph = x, None
+    else:
+        ldr = _like(residual, x, "residual")
+        if h is None:
+            h, ldh = empty(x.shape, dtype=x.dtype, device=dev), cols
+        else:
+            ldh = _like(h, x, "h")
+        kept, ph = h, h.data_ptr()
+    if fp8:
+        out, py = _fp8_new(empty, rows, cols, False, dev), None
+        pq, ps = out.q.data_ptr(), out.scale.data_ptr()
+    else:
+        if out is None:
+            out, ldy = empty(x.shape, dtype=x.dtype, device=dev), cols
+        else:
+            ldy = _like(out, x, "out")
+        py, pq, ps = out.data_ptr(), None, None
+    rstd = empty((rows,), dtype=torch.float32, device=dev)
+    _check(lib().ff_rms_norm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, rows, cols,
+                             _vector(gamma, cols, "gamma", dev), eps, prec, ph, ldh, py, ldy, pq, ps, rstd.data_ptr(), on),
+           "ff_rms_norm")
+    if (x.requires_grad or (gamma is not None and gamma.requires_grad)
+            or (residual is not None and residual.requires_grad)):
+        _unrecorded("rms_norm_fp8" if fp8 else "rms_norm", depth=5)
+    return out, kept, rstd
+
+
+@_on_device_of_first
+def rms_norm(x, gamma, residual=None, eps: float = 1e-5, out=None, h=None, stream=None):
+    """ff_rms_norm: h = x + residual, y = gamma * h * rstd with rstd = 1 /
+    sqrt(mean h^2 + eps) over the last dimension.  x, residual [..., cols] (bf16
+    or fp32, evenly spaced rows), gamma fp32 [cols] or None.  Returns (y, h,
+    rstd): h is x itself without a residual, rstd fp32 [rows].  out and h are
+    optional buffers; either may be x or the residual, not both the same.  Not
+    recorded by autograd: its gradient is rms_norm_backward."""
+    return _rms_norm(x, gamma, residual, eps, out, h, False, stream)
+
+
+@_on_device_of_first
+def rms_norm_fp8(x, gamma, residual=None, eps: float = 1e-5, h=None, stream=None):
+    """ff_rms_norm with its output as an Fp8Matrix in row blocks, for
+    fp8_matmul.  Returns (a, h, rstd) as rms_norm does.  Not recorded by autograd."""
+    return _rms_norm(x, gamma, residual, eps, None, h, True, stream)
+
+
+@_on_device_of_first
+def rms_norm_backward(dy, h, rstd, gamma, dh=None, out=None, stream=None):
+    """ff_rms_norm_backward: the gradient of rms_norm, from the h and rstd that
+    it returned; dh is what the residual stream hands back and is added.
+    Returns (dx, dgamma): dx is the gradient of x and of the residual; out may
+    be dy, h or dh."""
+    prec, dev = _prec(dy, "dy"), dy.device
+    rows, cols, lddy = _matrix_sizes(dy, "dy")
+    on, empty = _on(stream, dev, dy, h, rstd, gamma, dh, out)
+    ldh = _like(h, dy, "h")
+    lddh = 0 if dh is None else _like(dh, dy, "dh")
+    if rstd is None:
+        raise ValueError("rstd of the forward pass is needed")
+    if out is None:
+        out, lddx = empty(dy.shape, dtype=dy.dtype, device=dev), cols
+    else:
+        lddx = _like(out, dy, "out")
+    dgamma = empty((cols,), dtype=torch.float32, device=dev)
+    need = _rms_workspace(rows, cols)
+    ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
+    _check(lib().ff_rms_norm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, rows, cols, _vector(rstd, rows, "rstd", dev),
+                                      _vector(gamma, cols, "gamma", dev), None if dh is None else dh.data_ptr(), lddh, prec,
+                                      out.data_ptr(), lddx, dgamma.data_ptr(), None if ws is None else ws.data_ptr(), need,
+                                      on), "ff_rms_norm_backward")
+    return out, dgamma
+
+
+class LabelLogprobs:
+    """What label_logprobs returns: logp and entropy [rows] fp32, top_logp [rows,
+    top] fp32 and top_index [rows, top] int32, stats [rows, 2] fp32 (the row's
+    maximum and log sum, for the gradient).  logp is None without labels."""
+
+    __slots__ = ("logp", "entropy", "top_logp", "top_index", "stats")
+
+
+def _labels(labels, rows, dev):
+    if not (isinstance(labels, torch.Tensor) and labels.dtype is torch.int32 and labels.device == dev
+            and labels.numel() == rows and labels.is_contiguous()):
+        _ptr(labels, torch.int32, "labels")  # says what is wrong with the tensor itself
+        if labels.numel() != rows:
+            raise ValueError("labels must have one entry per row")
+        _same_device(labels, dev, "labels")
+    return labels.data_ptr()
+
+
+@_on_device_of_first
+def label_logprobs(logits, labels, top: int = 0, stream=None):
+    """ff_label_logprobs: under the softmax of each row of logits [..., classes]
+    (bf16 or fp32, evenly spaced rows), the log-probability of its label (int32
+    [rows]; 0 for a label outside the classes; labels None: not wanted), the
+    entropy, and the `top` (up to 32) likeliest classes with theirs.  Returns a
+    LabelLogprobs.  Not recorded by autograd: its gradient is
+    label_logprobs_backward."""
+    prec, dev = _prec(logits, "logits"), logits.device
+    rows, classes, ld = _matrix_sizes(logits, "logits")
+    top = int(top)
+    if not 0 <= top <= min(32, classes):
+        raise ValueError("top must be 0 .. min(32, classes)")
+    on, empty = _on(stream, dev, logits, labels)
+    r = object.__new__(LabelLogprobs)
+    pl, pp = None, None
+    r.logp = None
+    if labels is not None:
+        pl = _labels(labels, rows, dev)
+        r.logp = empty((rows,), dtype=torch.float32, device=dev)
+        pp = r.logp.data_ptr()
+    r.entropy = empty((rows,), dtype=torch.float32, device=dev)
+    r.top_logp = empty((rows, top), dtype=torch.float32, device=dev)
+    r.top_index = empty((rows, top), dtype=torch.int32, device=dev)
+    r.stats = empty((rows, 2), dtype=torch.float32, device=dev)
+    _check(lib().ff_label_logprobs(logits.data_ptr(), ld, rows, classes, prec, pl, pp, r.entropy.data_ptr(), top,
+                                   r.top_logp.data_ptr(), r.top_index.data_ptr(), r.stats.data_ptr(), on),
+           "ff_label_logprobs")
+    if logits.requires_grad:
+        _unrecorded("label_logprobs")
+    return r
+
+
+@_on_device_of_first
+def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy=None, out=None, stream=None):
+    """ff_label_logprobs_backward: the gradient of label_logprobs at the logits,
+    dlogp (1[label] - p) - dentropy p (ln p + entropy), from its stats (and, for
+    dentropy, its entropy).  dlogp or dentropy fp32 [rows] may be None.  Returns
+    a tensor like logits; out may be the logits."""
+    prec, dev = _prec(logits, "logits"), logits.device
+    rows, classes, ld = _matrix_sizes(logits, "logits")
+    if stats is None:
+        raise ValueError("stats of the forward pass are needed")
+    if dlogp is not None and labels is None:
+        raise ValueError("dlogp needs the labels")
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy needs the forward pass's entropy")
+    on, empty = _on(stream, dev, logits, labels, stats, dlogp, entropy, dentropy, out)
+    if out is None:
+        out, ldo = empty(logits.shape, dtype=logits.dtype, device=dev), classes
+    else:
+        ldo = _like(out, logits, "out")
+    _check(lib().ff_label_logprobs_backward(
+        logits.data_ptr(), ld, rows, classes, prec, None if labels is None else _labels(labels, rows, dev),
+        _vector(stats, 2 * rows, "stats", dev), _vector(dlogp, rows, "dlogp", dev), _vector(entropy, rows, "entropy", dev),
+        _vector(dentropy, rows, "dentropy", dev), out.data_ptr(), ldo, on), "ff_label_logprobs_backward")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _clip_arrays(n):
+    return c_void_p * n, c_longlong * n, c_int * n
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
+    """ff_clip_grad_norm: the 2-norm over all tensors of grads (bf16 or fp32,
+    contiguous, one device) together, and the tensors scaled so that it is at
+    most max_norm, in place or into `out` (a list of tensors like them).
+    Returns the norm before clipping, fp32 [1], without a wait.  A tensor given
+    twice, or outputs that overlap, are refused."""
+    grads = list(grads)
+    n = len(grads)
+    if n == 0 or not isinstance(grads[0], torch.Tensor):
+        raise ValueError("grads must be a non-empty list of tensors")
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise ValueError("grads must be CUDA tensors")
+    if dev.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return clip_grad_norm(grads, max_norm, out, stream)
+    ptrs, sizes, kinds = [], [], []
+    for g in grads:
+        if not isinstance(g, torch.Tensor) or g.device != dev or not g.is_contiguous():
+            raise ValueError(f"grads must be contiguous tensors on {dev}")
+        kinds.append(_prec(g, "grads"))
+        ptrs.append(g.data_ptr())
+        sizes.append(g.numel())
+    to = ptrs
+    if out is not None:
+        to, out = [], list(out)
+        if len(out) != n:
+            raise ValueError("out must have a tensor for each of grads")
+        for o, g in zip(out, grads):
+            if (not isinstance(o, torch.Tensor) or o.shape != g.shape or o.dtype != g.dtype or o.device != dev
+                    or not o.is_contiguous()):
+                raise ValueError("out must match grads in shape, type and device, and be contiguous")
+            to.append(o.data_ptr())
+    on, empty = _on(stream, dev, *grads, *(out or ()))
+    norm = empty((1,), dtype=torch.float32, device=dev)
+    need = lib().ff_clip_grad_norm_workspace(n)
+    ws = empty((need,), dtype=torch.uint8, device=dev)
+    P, N, K = _clip_arrays(n)
+    _check(lib().ff_clip_grad_norm(P(*ptrs), P(*to), N(*sizes), K(*kinds), n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
+                                   on), "ff_clip_grad_norm")
+    return norm
+
+
+# ------------------------------------------------------------ 4-bit matrices
+class Fp4Matrix:
+    """A 4-bit matrix [rows, k]: e2m1 pairs q [rows, ff_fp4_stride(k)] and
+    power-of-two scales [ceil(rows / 128), ceil(k / 128), 32, 4, 4], both bytes
+    (see ff_fp4_quantize in include/ff.h)."""
+
+    __slots__ = ("q", "scale", "rows", "k")
+
+    def __init__(self, q, scale, rows: int, k: int):
+        self.q, self.scale, self.rows, self.k = q, scale, rows, k
+        if (k < 1 or q.shape != (rows, (k + 31) // 32 * 16) or q.element_size() != 1 or not q.is_contiguous()
+                or not q.is_cuda):
+            raise ValueError("q must be a contiguous one-byte CUDA tensor [rows, ff_fp4_stride(k)]")
+        if (scale.shape != ((rows + 127) // 128, (k + 127) // 128, 32, 4, 4) or scale.element_size() != 1
+                or not scale.is_contiguous() or scale.device != q.device):
+            raise ValueError("scale must be contiguous bytes [ceil(rows / 128), ceil(k / 128), 32, 4, 4] beside q")
+
+    def get_device(self):
+        """The CUDA device's index, as of a tensor."""
+        return self.q.get_device()
+
+
+def _fp4_new(empty, rows, k, dev):
+    m = object.__new__(Fp4Matrix)
+    m.q = empty((rows, (k + 31) // 32 * 16), dtype=torch.uint8, device=dev)
+    m.scale = empty(((rows + 127) // 128, (k + 127) // 128, 32, 4, 4), dtype=torch.uint8, device=dev)
+    m.rows, m.k = rows, k
+    return m
+
+
+@_on_device_of_first
+def _fp4_quantize(x, straight, transposed, stream):
+    prec = _prec(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, k] with k >= 1")
+    dev = x.device
+    rows, k, ldx = _matrix_sizes(x, "x")
+    if transposed and rows < 1:
+        raise ValueError("the transpose needs at least one row")
+    on, empty = _on(stream, dev, x)
+    a = _fp4_new(empty, rows, k, dev) if straight else None
+    t = _fp4_new(empty, k, rows, dev) if transposed else None
+    _check(lib().ff_fp4_quantize(x.data_ptr(), ldx, rows, k, prec, a.q.data_ptr() if a else None,
+                                 a.scale.data_ptr() if a else None, t.q.data_ptr() if t else None,
+                                 t.scale.data_ptr() if t else None, on), "ff_fp4_quantize")
+    if x.requires_grad:
+        _unrecorded("fp4_quantize", depth=5)
+    return a, t
+
+
+def fp4_quantize(x, transpose: bool = False, stream=None):
+    """ff_fp4_quantize: x [rows, k] (bf16 or fp32, evenly spaced rows) as an
+    Fp4Matrix; transpose=True gives x's transpose instead.  Not recorded by
+    autograd."""
+    return _fp4_quantize(x, not transpose, transpose, stream)[1 if transpose else 0]
+
+
+def fp4_quantize_both(x, stream=None):
+    """ff_fp4_quantize, both ways round from one read of x: (x, x's transpose)."""
+    return _fp4_quantize(x, True, True, stream)
+
+
+@_on_device_of_first
+def fp4_dequantize(m, out=None, out_dtype=torch.bfloat16, stream=None):
+    """ff_fp4_dequantize: the values [rows, k] that an Fp4Matrix stands for,
+    exactly, in out_dtype (torch.bfloat16 or torch.float32) or out's type."""
+    if not isinstance(m, Fp4Matrix):
+        raise TypeError("m must be a Fp4Matrix")
+    dev = m.q.device
+    on, empty = _on(stream, dev, m.q, m.scale, out)
+    if out is None:
+        prec = _PREC.get(out_dtype)
+        if prec is None:
+            raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
+        out, ldy = empty((m.rows, m.k), dtype=out_dtype, device=dev), m.k
+    else:
+        if out.shape != (m.rows, m.k):
+            raise ValueError("out must be [rows, k]")
+        _same_device(out, dev, "out")
+        prec, ldy = _prec(out, "out"), _row_stride_of(out, "out")
+    _check(lib().ff_fp4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), m.rows, m.k, prec, out.data_ptr(), ldy, on),
+           "ff_fp4_dequantize")
+    return out
+
+
+@_on_device_of_first
+def fp4_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bfloat16, status=None, stream=None):
+    """ff_fp4_matmul: act(a b^T + bias) of two Fp4Matrix, otherwise as
+    fp8_matmul: returns [a.rows, b.rows] in out_dtype or out's type, bias fp32
+    [b.rows], status an optional int32 word for timed-out waits (without one,
+    fp8_check reports them).  Not recorded by autograd."""
+    if not isinstance(a, Fp4Matrix) or not isinstance(b, Fp4Matrix):
+        raise TypeError("a and b must be Fp4Matrix")
+    if a.k != b.k:
+        raise ValueError("a and b must have the same k")
+    dev = a.q.device
+    _same_device(b.q, dev, "b")
+    on, empty = _on(stream, dev, a.q, a.scale, b.q, b.scale, bias, out, status)
+    m, n = a.rows, b.rows
+    if out is None:
+        prec = _PREC.get(out_dtype)
+        if prec is None:
+            raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
+        out, ldc = empty((m, n), dtype=out_dtype, device=dev), n
+    else:
+        if out.shape != (m, n):
+            raise ValueError("out must be [a.rows, b.rows]")
+        _same_device(out, dev, "out")
+        prec, ldc = _prec(out, "out"), _row_stride_of(out, "out")
+    if status is not None:
+        _same_device(status, dev, "status")
+    _check(lib().ff_fp4_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), m, n, a.k,
+                               _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
+                               _ptr(status, torch.int32, "status"), on), "ff_fp4_matmul")
+    if bias is not None and bias.requires_grad:
+        _unrecorded("fp4_matmul")
+    return out
