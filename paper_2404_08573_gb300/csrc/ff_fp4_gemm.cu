@@ -1,7 +1,9 @@
 // The 4-bit matrix product C = act(A B^T + bias), A and B in e2m1 with a
 // power-of-two scale per block of 32 along the contraction.  The tensor cores
 // apply the scales themselves (kind::mxf4), so a tile is one fp32 accumulator
-// in TMEM over the whole contraction.
+// in TMEM over the whole contraction.  Large products run on CTA pairs
+// (k_fp4_pair), the others on single CTAs that may split the contraction
+// (k_fp4_split).
 //
 // A ring stage is 256 contraction indices: one 128-byte swizzled row of packed
 // e2m1 pairs per operand row, and two scale tiles (512 bytes: 128 rows x 4
@@ -54,6 +56,306 @@ struct Args {
 
 // MMAs of K = 64 in stage `s` of a contraction of K indices.
 __device__ __forceinline__ int steps_of(int K, int s) { return min(KS / 64, (K - s * KS + 63) / 64); }
+
+// ------------------------------------------------------- large products
+// CTA pairs (cta_group::2) on 256 x 256 tiles: each CTA loads 128 rows of A and
+// half of B's 256 columns per stage, the scales of its rows and those of all
+// 256 columns (35 KB for 8.4 MMAC a CTA), and holds 128 x 256 of the accumulator:
+// half of its TMEM, the rest of which cannot hold a second one beside the
+// scales.  So the epilogue warps first read all of it into registers (128
+// columns each), hand it back, and convert and store under the next tile's
+// MMAs.  Persistent: the copies run ahead over the tiles.  Warps: 0 producer,
+// 1 MMAs (the even CTA's), 2..9 epilogue.
+constexpr int LN = 256;
+constexpr int LSTAGES = 5;
+constexpr int LA = BM * KB, LB = LN / 2 * KB;         // bytes of a stage's operands
+constexpr int LSTAGE = LA + LB + SF + 2 * SF;
+constexpr int LCPW = LN / 2;                          // columns per epilogue warp
+constexpr int LSTAGING = 32 * 128;                    // per epilogue warp: a block of 32 rows x 128 bytes of C
+constexpr uint32_t LSFC = SFC + 2 * SFC;              // TMEM columns of a stage's scales
+static_assert(LN + 2 * LSFC <= 512, "the accumulator and two stages' scales");
+static_assert(LSTAGE % 1024 == 0, "swizzled tiles start on 1024 bytes");
+constexpr int L_SMEM = 1024 + LSTAGES * LSTAGE + EPI * LSTAGING + EPI * LCPW * 4 + 512;
+static_assert(L_SMEM > 113 * 1024 && L_SMEM <= 227 * 1024, "one GEMM CTA per SM, so that no TMEM allocation waits on another's");
+
+// Tile t of the raster: groups of 8 row tiles, columns outermost within a
+// group, so that the tiles in flight share operand panels in L2.
+__device__ __forceinline__ void tile_of(int t, int ntp, int ntq, int& tp, int& tq) {
+  constexpr int GROUP = 8;
+  const int per = GROUP * ntq, g = t / per, in = t - g * per;
+  const int rows = min(GROUP, ntp - g * GROUP);
+  tp = g * GROUP + in % rows;
+  tq = in / rows;
+}
+
+// A warp writes a staged block of 32 rows x 128 bytes (16-byte units swizzled
+// by the row) to C, `rows` and `left` of its rows and columns being there.
+template <typename U>
+__device__ __forceinline__ void rows_out(const uint8_t* from, U* c, long long ldc, int rows, int left, int lane) {
+  constexpr int J = 128 / 32 / (int)sizeof(U);
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += 8) {
+    U v[8][J];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int byte = (lane + 32 * j) * (int)sizeof(U);
+        v[i][j] = *reinterpret_cast<const U*>(from + (r0 + i) * 128 + (((byte >> 4) ^ i) << 4) + (byte & 15));
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (r0 + i < rows && lane + 32 * j < left) c[(r0 + i) * ldc + lane + 32 * j] = v[i][j];
+  }
+}
+
+// TMA_C: C's rows are 16-byte aligned and go out by TMA.  BF16: C's type.
+template <bool TMA_C, bool BF16>
+__global__ void __launch_bounds__(THREADS, 1)
+    k_fp4_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+               const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmSB,
+               const __grid_constant__ CUtensorMap tmC, Args g) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_s = ptx::smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + ((1024u - (raw_s & 1023u)) & 1023u);
+  uint8_t* staging = smem + LSTAGES * LSTAGE;
+  float* sbias = reinterpret_cast<float*>(staging + EPI * LSTAGING);  // [epilogue warp][LCPW]
+  uint64_t* full = reinterpret_cast<uint64_t*>(sbias + EPI * LCPW);
+  uint64_t* empty = full + LSTAGES;
+  uint64_t* tfull = empty + LSTAGES;   // a tile's products are done
+  uint64_t* tempty = tfull + 1;        // both CTAs have read them
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(tempty + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tslot + 1);
+  volatile int* never_set = reinterpret_cast<volatile int*>(tslot + 2);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+  const uint32_t crank = ptx::cluster_ctarank();
+  const bool lead = crank == 0;
+  const int nkb = (g.K + KS - 1) / KS;
+  const int ntiles = g.ntp * g.ntq;
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < LSTAGES; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    ptx::mbar_init(tfull, 1);
+    ptx::mbar_init(tempty, 2 * EPI);
+    *abort_flag = 0;
+    *never_set = 0;
+    ptx::fence_mbar_init();
+    ptx::prefetch_tmap(&tmA);
+    ptx::prefetch_tmap(&tmB);
+    ptx::prefetch_tmap(&tmSA);
+    ptx::prefetch_tmap(&tmSB);
+    ptx::prefetch_tmap(&tmC);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(tslot, 512);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync();
+  ptx::tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tslot, 0);
+  ptx::griddep_wait();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const uint32_t full0 = ptx::mapa_shared(ptx::smem_u32(&full[0]), 0);
+      int it = 0;
+      for (int t = pair; t < ntiles && !*abort_flag; t += npairs) {
+        int tp, tq;
+        tile_of(t, g.ntp, g.ntq, tp, tq);
+        const int ar = tp * 2 * BM + (int)crank * BM, br = tq * LN + (int)crank * (LN / 2);
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % LSTAGES;
+          if (!ptx::mbar_wait(&empty[s], (((uint32_t)(it / LSTAGES)) & 1u) ^ 1u, kWaitTimeoutNs, abort_flag)) {
+            latch(g.err, abort_flag);
+            break;
+          }
+          if (lead) ptx::mbar_arrive_expect_tx(&full[s], 2 * LSTAGE);
+          uint8_t* a = smem + s * LSTAGE;
+          const uint32_t bar = full0 + 8u * (uint32_t)s;
+          ptx::tma_load_2d_pair(a, &tmA, bar, kb * KB, ar);
+          ptx::tma_load_2d_pair(a + LA, &tmB, bar, kb * KB, br);
+          ptx::tma_load_2d_pair(a + LA + LB, &tmSA, bar, kb * SF_BOX, tp * 2 + (int)crank);
+          ptx::tma_load_2d_pair(a + LA + LB + SF, &tmSB, bar, kb * SF_BOX, tq * 2);
+        }
+      }
+      if (!*abort_flag) {
+        // the last stages' commits arrive here before the CTA goes away
+        for (int k = it; k < it + LSTAGES; ++k)
+          if (!ptx::mbar_wait(&empty[k % LSTAGES], (((uint32_t)(k / LSTAGES)) & 1u) ^ 1u, kWaitTimeoutNs, abort_flag)) {
+            latch(g.err, abort_flag);
+            break;
+          }
+      }
+      if (*abort_flag) {
+        // Copies issued earlier land before the shared memory goes away: on
+        // this CTA's own barriers (the pair's even CTA), or in bounded time.
+        if (lead) {
+          for (int k = it < LSTAGES ? 0 : it - LSTAGES; k < it; ++k)
+            ptx::mbar_wait(&full[k % LSTAGES], (uint32_t)(k / LSTAGES) & 1u, 10000000ull, never_set);
+        } else {
+          pause_1ms();
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lead) {
+      // The whole warp walks the loop, so that its variables are uniform, and
+      // one lane issues.  Descriptors differ from the first stage's by their
+      // address field only (16-byte units).
+      constexpr uint32_t idesc[2] = {ptx::idesc_mxf4(2 * BM, LN, 0), ptx::idesc_mxf4(2 * BM, LN, 2)};
+      const uint64_t ad0 = ptx::sdesc_sw128(ptx::smem_u32(smem), 16, 1024);
+      const uint64_t bd0 = ptx::sdesc_sw128(ptx::smem_u32(smem + LA), 16, 1024);
+      const uint64_t sd0 = ptx::sdesc_rows16(ptx::smem_u32(smem + LA + LB));
+      const int last_steps = steps_of(g.K, nkb - 1);
+      int it = 0;
+      uint32_t tile = 0;
+      bool live = true;
+      for (int t = pair; t < ntiles && live; t += npairs, ++tile) {
+        bool ok = ptx::mbar_wait_cluster(tempty, (tile & 1u) ^ 1u, kWaitTimeoutNs, abort_flag);
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const int s = it % LSTAGES;
+          ok = ok && ptx::mbar_wait(&full[s], (uint32_t)(it / LSTAGES) & 1u, kWaitTimeoutNs, abort_flag);
+          // two stages' scales fit TMEM: those of the stage before the last have been used
+          if (it >= 2)
+            ok = ok && ptx::mbar_wait(&empty[(it - 2) % LSTAGES], (uint32_t)((it - 2) / LSTAGES) & 1u, kWaitTimeoutNs, abort_flag);
+          if (!__all_sync(0xffffffffu, ok)) {
+            latch(g.err, abort_flag);
+            live = false;
+            break;
+          }
+          ptx::tc_fence_after();
+          const uint64_t at = (uint64_t)(s * (LSTAGE >> 4));
+          const uint32_t sfa = tmem + LN + (uint32_t)(it & 1) * LSFC, sfb = sfa + SFC;
+          const int steps = kb == nkb - 1 ? last_steps : KS / 64;
+          if (ptx::elect_one()) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint64_t from = sd0 + at + h * (kFp4ScaleTile >> 4);
+              ptx::tmem_cp_rows16_pair(sfa + 4 * h, from);
+              ptx::tmem_cp_rows16_pair(sfb + 8 * h, from + (SF >> 4));
+              ptx::tmem_cp_rows16_pair(sfb + 8 * h + 4, from + (2 * SF >> 4));
+            }
+#pragma unroll
+            for (int k = 0; k < KS / 64; ++k)
+              if (k < steps)
+                ptx::umma_mxf4_pair(tmem, ad0 + at + 2 * k, bd0 + at + 2 * k, idesc[k & 1], sfa + 4 * (k / 2), sfb + 8 * (k / 2),
+                                    kb > 0 || k > 0);
+            ptx::umma_commit_pair(&empty[s], 3);
+            if (kb == nkb - 1) ptx::umma_commit_pair(tfull, 3);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    const int q = warp & 3, ew = warp - 2, half = ew >> 2;
+    const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * LCPW);
+    const uint32_t te0 = ptx::mapa_shared(ptx::smem_u32(tempty), 0);
+    uint8_t* stage = staging + ew * LSTAGING;
+    float* bias = sbias + ew * LCPW;
+    uint32_t tile = 0;
+    for (int t = pair; t < ntiles; t += npairs, ++tile) {
+      int tp, tq;
+      tile_of(t, g.ntp, g.ntq, tp, tq);
+      const int rbase = tp * 2 * BM + (int)crank * BM + q * 32;
+      const int cbase = tq * LN + half * LCPW;
+      __syncwarp();  // the last tile's bias has been read
+#pragma unroll
+      for (int e = 0; e < LCPW; e += 32)
+        bias[e + lane] = g.bias && cbase + e + lane < g.Q ? __ldg(g.bias + cbase + e + lane) : 0.f;
+      const bool ok = ptx::mbar_wait(tfull, tile & 1u, 4 * kWaitTimeoutNs, abort_flag);
+      if (!ok) latch(g.err, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      ptx::tc_fence_after();
+      uint32_t acc[LCPW / 32][32];
+#pragma unroll
+      for (int c = 0; c < LCPW / 32; ++c) ptx::tmem_ld32(trow + c * 32, acc[c]);
+#pragma unroll
+      for (int c = 0; c < LCPW / 32; ++c) ptx::tmem_ld_wait_for(acc[c]);
+      ptx::tc_fence_before();
+      __syncwarp();
+      // TMEM reads that have completed: nothing to release, only an arrival
+      if (lane == 0) ptx::mbar_arrive_at(te0);
+      if (t + npairs >= ntiles && threadIdx.x == 64) ptx::griddep_launch_dependents();
+      // Store: 128 bytes of each of the warp's 32 rows at a time through the
+      // swizzled staging block, by TMA where C's rows are 16-byte aligned (it
+      // clips what lies past the matrix, and the warp need not wait for the
+      // memory), else by the lanes along a row, eight rows read before the
+      // first is written.
+      auto block = [&]() {  // the staging block, free again
+        if (TMA_C && lane == 0) ptx::bulk_wait_read0();
+        __syncwarp();
+        return stage;
+      };
+      auto flush = [&](uint8_t* from, int col0) {  // the staged columns of C from col0 on
+        if constexpr (TMA_C) {
+          ptx::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (rbase < g.P && col0 < g.Q) ptx::tma_store_2d(&tmC, from, col0, rbase);
+            ptx::bulk_commit();
+          }
+        } else {
+          __syncwarp();
+          const int rows = g.P - rbase, left = g.Q - col0;
+          const long long at = (long long)rbase * g.ldc + col0;
+          if constexpr (BF16)
+            rows_out(from, static_cast<uint16_t*>(g.c) + at, g.ldc, rows, left, lane);
+          else
+            rows_out(from, static_cast<uint32_t*>(g.c) + at, g.ldc, rows, left, lane);
+        }
+      };
+      // four accumulators with bias and activation
+      auto value = [&](int i) {
+        const float4 v = *reinterpret_cast<const float4*>(bias + i);
+        const uint32_t* r = acc[i / 32] + i % 32;
+        return make_float4(finish(__uint_as_float(r[0]) + v.x, g.relu), finish(__uint_as_float(r[1]) + v.y, g.relu),
+                           finish(__uint_as_float(r[2]) + v.z, g.relu), finish(__uint_as_float(r[3]) + v.w, g.relu));
+      };
+      if constexpr (BF16) {
+#pragma unroll
+        for (int ch = 0; ch < LCPW / 64; ++ch) {
+          uint8_t* to = block();
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float4 v = value(ch * 64 + u * 8), w = value(ch * 64 + u * 8 + 4);
+            const __nv_bfloat162 h[4] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w),
+                                         __floats2bfloat162_rn(w.x, w.y), __floats2bfloat162_rn(w.z, w.w)};
+            *reinterpret_cast<uint4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4*>(h);
+          }
+          flush(to, cbase + ch * 64);
+        }
+      } else {
+#pragma unroll
+        for (int ch = 0; ch < LCPW / 32; ++ch) {
+          uint8_t* to = block();
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            *reinterpret_cast<float4*>(to + lane * 128 + ((u ^ (lane & 7)) << 4)) = value(ch * 32 + u * 4);
+          flush(to, cbase + ch * 32);
+        }
+      }
+    }
+    if (TMA_C && lane == 0) ptx::bulk_wait_read0();
+    __syncwarp();
+  }
+
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) pause_1ms();  // MMAs issued before the abort finish before TMEM is released
+  __syncwarp();
+  ptx::cluster_sync();
+  ptx::tc_fence_after();
+  if (warp == 1) ptx::tmem_dealloc_pair(tmem, 512);
+}
 
 // ------------------------------------------------------- small products
 // One CTA per 128 x BN tile and slice of the contraction: the CTAs of a
@@ -333,18 +635,48 @@ int clusters_of(int dev, int bn, int ks_log) {
   }
 }
 
+// CTA pairs the GPU holds at once.
+template <bool TMA_C, bool BF16>
+int resident_pairs(int dev) {
+  static PerDevice<int> kept;
+  int n = 0;
+  const cudaError_t e = kept.get(dev, &n, [](int* pairs) {
+    constexpr auto kernel = k_fp4_pair<TMA_C, BF16>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = L_SMEM;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg);
+  });
+  if (e != cudaSuccess) cudaGetLastError();  // leave no error behind: the split kernel runs
+  return e == cudaSuccess ? n : 0;
+}
+
 // The shape of a product: tile, orientation and split with the least estimated
 // time: a wave of tiles takes a time per stage and a fixed one (launch, fill,
 // exchange, store), and no shape moves its operands faster than about 9 TB/s.
 struct Plan {
-  int bn;  // 0: no shape fits
+  int bn;  // 256: the pair kernel; 0: no shape fits
   bool swap;
   int ks_log;
 };
-Plan plan(int dev, int M, int N, int K) {
+Plan plan(int dev, int M, int N, int K, int pairs) {
   const double nkb = cdiv(K, KS);
   Plan best{0, false, 0};
   double t = 1e30;
+  if (pairs > 0) {
+    const double tiles = (double)cdiv(M, 2 * BM) * cdiv(N, LN);
+    t = 4.0 + std::ceil(tiles / pairs) * (nkb * 0.29 + 1.0);
+    best.bn = LN;
+  }
   struct Shape { int bn; bool swap; double step, fixed; };
   const Shape shapes[5] = {{16, true, 0.24, 2.9}, {32, true, 0.28, 3.2}, {64, true, 0.28, 4.6}, {128, true, 0.31, 6.0},
                            {128, false, 0.31, 7.0}};
@@ -380,7 +712,9 @@ cudaError_t run_split(const CUtensorMap (&m)[4], const Args& g, int ks_log, cuda
 ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
   int dev = 0;
   FF_TRY(cudaGetDevice(&dev), "4-bit matrix product");
-  const Plan pl = plan(dev, f.M, f.N, f.K);
+  const int pairs = f.out_bf16 ? std::min(resident_pairs<true, true>(dev), resident_pairs<false, true>(dev))
+                               : std::min(resident_pairs<true, false>(dev), resident_pairs<false, false>(dev));
+  const Plan pl = plan(dev, f.M, f.N, f.K, pairs);
   if (pl.bn == 0) return FF_ERR_UNSUPPORTED;
   Args g{};
   g.P = pl.swap ? f.N : f.M;
@@ -393,17 +727,30 @@ ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
   g.c = f.c;
   g.ldc = f.ldc;
   g.err = f.status;
-  g.ntp = cdiv(g.P, BM);
+  const bool pairk = pl.bn == LN;
+  g.ntp = cdiv(g.P, pairk ? 2 * BM : BM);
   g.ntq = cdiv(g.Q, pl.bn);
   if ((long long)g.ntp * g.ntq << pl.ks_log > 0x3FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const int ld = fp4_stride(f.K), words = cdiv(f.K, 128) * (kFp4ScaleTile / 4);
   CUtensorMap m[4];
   if (!make_sw128_map(&m[0], pl.swap ? f.b : f.a, 1, ld, g.P, ld, KB, BM) ||
-      !make_sw128_map(&m[1], pl.swap ? f.a : f.b, 1, ld, g.Q, ld, KB, pl.bn) ||
+      !make_sw128_map(&m[1], pl.swap ? f.a : f.b, 1, ld, g.Q, ld, KB, pairk ? LN / 2 : pl.bn) ||
       !make_plain_map(&m[2], pl.swap ? f.sb : f.sa, 4, words, cdiv(g.P, 128), words, SF_BOX, 1) ||
-      !make_plain_map(&m[3], pl.swap ? f.sa : f.sb, 4, words, cdiv(g.Q, 128), words, SF_BOX, 1))
+      !make_plain_map(&m[3], pl.swap ? f.sa : f.sb, 4, words, cdiv(g.Q, 128), words, SF_BOX, pairk ? 2 : 1))
     return FF_ERR_INVALID_ARG;
+  const int es = f.out_bf16 ? 2 : 4;
+  CUtensorMap c = m[0];
+  // whole 16-byte units a row: a row that ends inside one is written to the
+  // unit's end, into what lies between the rows
+  const bool tma_c = pairk && (long long)f.N * es % 16 == 0 && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N &&
+                     make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
   auto go = [&]() -> cudaError_t {
+    if (pairk) {
+      const unsigned grid = 2u * (unsigned)std::min((long long)pairs, (long long)g.ntp * g.ntq);
+      auto* const kernel = f.out_bf16 ? (tma_c ? k_fp4_pair<true, true> : k_fp4_pair<false, true>)
+                                      : (tma_c ? k_fp4_pair<true, false> : k_fp4_pair<false, false>);
+      return launch(kernel, grid, THREADS, 2, L_SMEM, st, m[0], m[1], m[2], m[3], c, g);
+    }
     switch (pl.bn) {
       case 16: return run_split<16>(m, g, pl.ks_log, st);
       case 32: return run_split<32>(m, g, pl.ks_log, st);
@@ -411,7 +758,7 @@ ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
       default: return run_split<128>(m, g, pl.ks_log, st);
     }
   };
-  FF_LAUNCH(K_FP4_GEMM, 2.0 * f.M * f.N * f.K, st, go(), "4-bit matrix product");
+  FF_LAUNCH(pairk ? K_FP4_PAIR : K_FP4_GEMM, 2.0 * f.M * f.N * f.K, st, go(), "4-bit matrix product");
   return FF_OK;
 }
 
