@@ -6,9 +6,7 @@
 //   dx = g (1[label] - p) - g' p (log p + entropy)   (g, g' from above)
 //
 // One pass: every thread carries (m, s, t) over its part of the row, rescaled
-// when m grows, and they are joined at the end.  The likeliest classes come
-// from the same pass: a warp keeps its best 32 in its lanes, and takes up a
-// value only if it beats the least of those it needs.
+// when m grows, and they are joined at the end.
 #include <algorithm>
 
 #include "ff_api_internal.h"
@@ -23,6 +21,7 @@ constexpr float kFar = -1e4f;  // e^d is zero in fp32 from here on: d is held ab
 constexpr float kLowest = -3.402823466e38f;
 constexpr int kMostTop = 32;
 constexpr int kMostWarps = 32;
+constexpr int kOwnRows = 8;  // rows a block with a warp a row
 
 __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
   float r;
@@ -68,64 +67,44 @@ __device__ __forceinline__ unsigned long long key_of(uint32_t o, uint32_t index)
   return (unsigned long long)o << 32 | (0xFFFFFFFFu - index);
 }
 
-// A warp's best 32 classes, lane i the i-th, and the value that a later class
-// has to beat to be among the first k: the k-th of the warp's own, or the k-th of
-// another warp of the block (which one with the same value may still precede).
-struct Best {
-  unsigned long long key;
-  uint32_t least;
-  int k;
-  __device__ __forceinline__ void insert(unsigned long long n, int lane) {
-    const int pos = __popc(__ballot_sync(0xffffffffu, key > n));
-    const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
-    key = lane < pos ? key : lane == pos ? n : up;
-  }
-  __device__ __forceinline__ uint32_t kth() const { return (uint32_t)(__shfl_sync(0xffffffffu, key, k - 1) >> 32); }
-};
-
-// N values of a vector into the warp's list: `top` is the largest of each
-// lane's, index0 the class of the lane's first.  A lane's classes, and the
-// lanes', follow each other in index order.
-template <int N>
-__device__ __forceinline__ void take(Best& b, const float (&v)[N], int count, uint32_t index0, int lane, uint32_t* shared) {
-  uint32_t left = count < N ? (1u << (count < 0 ? 0 : count)) - 1u : (1u << N) - 1u;
-  const uint32_t others = *reinterpret_cast<volatile uint32_t*>(shared);
-  uint32_t least = max(b.kth(), others ? others - 1u : 0u);
-  while (true) {
-    uint32_t o = 0, at = 0;
-#pragma unroll
-    for (int e = N - 1; e >= 0; --e) {
-      const uint32_t c = left >> e & 1u ? ordered(v[e]) : 0u;
-      if (c >= o && c > 0u) {
-        o = c;
-        at = (uint32_t)e;
-      }
-    }
-    const uint32_t most = __reduce_max_sync(0xffffffffu, o);
-    if (most <= least) break;
-    const int src = __ffs(__ballot_sync(0xffffffffu, o == most)) - 1;
-    const uint32_t index = __shfl_sync(0xffffffffu, index0 + at, src);
-    if (lane == src) left &= ~(1u << at);
-    b.insert(key_of(most, index), lane);
-    least = max(least, b.kth());
-  }
-  const uint32_t own = b.kth();
-  if (lane == 0 && own > others) atomicMax(shared, own);
-  b.least = max(own, others ? others - 1u : 0u);
+// A warp's 32 numbers, largest first: by a bitonic sort; and two such lists
+// into one (the larger of one and of the other reversed are the 32 largest, and
+// a bitonic merge orders them).
+template <typename K>
+__device__ __forceinline__ K step(K a, int o, bool keep_larger) {
+  const K p = __shfl_xor_sync(0xffffffffu, a, o);
+  return (a > p) == keep_larger ? a : p;
 }
-
-// Two warp lists into one: the larger of one and of the other reversed are the
-// 32 largest, and a bitonic merge orders them.
-__device__ __forceinline__ unsigned long long merge(unsigned long long a, unsigned long long b, int lane) {
-  const unsigned long long r = __shfl_sync(0xffffffffu, b, 31 - lane);
+template <typename K>
+__device__ __forceinline__ K sorted(K a, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int o = size / 2; o > 0; o /= 2) a = step(a, o, ((lane & o) == 0) == ((lane & size) == 0 || size == 32));
+  return a;
+}
+template <typename K>
+__device__ __forceinline__ K merged(K a, K b, int lane) {
+  const K r = __shfl_sync(0xffffffffu, b, 31 - lane);
   a = a > r ? a : r;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const unsigned long long p = __shfl_xor_sync(0xffffffffu, a, o);
-    const bool low = (lane & o) == 0;
-    a = (a > p) == low ? a : p;
-  }
+  for (int o = 16; o > 0; o /= 2) a = step(a, o, (lane & o) == 0);
   return a;
+}
+// The first 32 of `lists` lists in shared memory ([lists][32], largest first),
+// of which the first `top` of each count: as many lists at a time as their
+// firsts fill a warp.
+template <typename K>
+__device__ __forceinline__ K first_of(const K (*list)[32], int lists, int top, int lane) {
+  const int log = top > 1 ? 32 - __clz(top - 1) : 0, per = 32 >> log;  // 2^log >= top of each
+  K best = 0;
+  for (int i = 0; i < lists; i += per) {
+    const int l = i + (lane >> log);
+    K a = l < lists ? list[l][lane & ((1 << log) - 1)] : K(0);
+    if (per > 1) a = sorted(a, lane);
+    best = i == 0 ? a : merged(best, a, lane);
+  }
+  return best;
 }
 
 template <typename T>
@@ -144,31 +123,126 @@ struct Load {
   static constexpr int N = 16 / (int)sizeof(T);
 };
 
-// A row on `cluster` blocks of `warps` warps (or, warps == 1, several rows a
-// block).  The row's 16-byte aligned middle is read as vectors, its ends value
-// by value by the first block's first and the last block's last warp.
+// How a thread block reads its part of a row: the row's 16-byte aligned middle
+// as vectors, v0 .. v1 of them the block's, vector v0 + j step + 32 warp + lane
+// being the j-th of a thread; the row's ends value by value on a warp's lanes,
+// by the first block's first and the last block's last warp.
+template <typename T>
+struct Part {
+  const T* p;
+  int classes, head, vecs, v0, v1, step;
+  bool has_head, has_tail;  // this warp's
+  __device__ __forceinline__ Part(const T* row, int n, int rank, int blocks, int warp, int warps) : p(row), classes(n) {
+    constexpr int N = Load<T>::N;
+    const int off = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % N);
+    head = min(off ? N - off : 0, classes);
+    vecs = (classes - head) / N;
+    v0 = (int)((long long)vecs * rank / blocks);
+    v1 = (int)((long long)vecs * (rank + 1) / blocks);
+    step = warps * 32;
+    has_head = rank == 0 && warp == 0 && head > 0;
+    has_tail = rank == blocks - 1 && warp == warps - 1 && tail_at() < classes;
+  }
+  __device__ __forceinline__ int tail_at() const { return head + vecs * Load<T>::N; }
+  __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(p + head); }
+  // the lane's value of the row's head or tail, if it has one
+  __device__ __forceinline__ float end_value(int from, int to, int lane, bool* in) const {
+    float v[1] = {kLowest};
+    *in = from + lane < to;
+    if (*in) Vec<T, 1>::unpack(Vec<T, 1>::load(p + from + lane), v);
+    return v[0];
+  }
+};
+
+// The likeliest classes of a part of a row by one insertion after the other: a
+// warp keeps its best 32 in its lanes, and takes up a value only if it beats
+// the top-th of them.  For rows that the quick way below does not serve: many
+// equal values, or fewer than `top` above -infinity.  (A lane's classes, and the
+// lanes', follow each other in index order, so of equal values the first
+// found stays.)
+struct Best {
+  unsigned long long key;
+  uint32_t least;
+  int top;
+  template <int N>
+  __device__ __forceinline__ void take(const float (&v)[N], bool in, uint32_t index0, int lane) {
+    uint32_t left = in ? (1u << N) - 1u : 0u;
+    while (true) {
+      uint32_t o = 0, at = 0;
+#pragma unroll
+      for (int e = N - 1; e >= 0; --e) {
+        const uint32_t c = left >> e & 1u ? ordered(v[e]) : 0u;
+        if (c >= o && c > 0u) {
+          o = c;
+          at = (uint32_t)e;
+        }
+      }
+      const uint32_t most = __reduce_max_sync(0xffffffffu, o);
+      if (most <= least) break;
+      const int src = __ffs(__ballot_sync(0xffffffffu, o == most)) - 1;
+      const uint32_t index = __shfl_sync(0xffffffffu, index0 + at, src);
+      if (lane == src) left &= ~(1u << at);
+      const unsigned long long n = key_of(most, index);
+      const int pos = __popc(__ballot_sync(0xffffffffu, key > n));
+      const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
+      key = lane < pos ? key : lane == pos ? n : up;
+      least = (uint32_t)(__shfl_sync(0xffffffffu, key, top - 1) >> 32);
+    }
+  }
+};
+template <typename T>
+__device__ __noinline__ unsigned long long best_by_insertion(const Part<T> part, int top, int warp, int lane) {
+  constexpr int N = Load<T>::N;
+  Best best{0ull, 0u, top};
+  if (part.has_head) {
+    bool in;
+    const float v[1] = {part.end_value(0, part.head, lane, &in)};
+    best.template take<1>(v, in, (uint32_t)lane, lane);
+  }
+  for (long long first = part.v0 + warp * 32; first < part.v1; first += part.step) {
+    const long long i = first + lane;
+    float v[N];
+    Vec<T, N>::unpack(i < part.v1 ? part.vectors()[i] : make_uint4(0, 0, 0, 0), v);
+    best.template take<N>(v, i < part.v1, (uint32_t)(part.head + i * N), lane);
+  }
+  if (part.has_tail) {
+    bool in;
+    const float v[1] = {part.end_value(part.tail_at(), part.classes, lane, &in)};
+    best.template take<1>(v, in, (uint32_t)(part.tail_at() + lane), lane);
+  }
+  return best.key;
+}
+
+constexpr int kPool = 2048;               // candidates a block holds; a warp with a row of its own an eighth
+constexpr int kOwnPool = kPool / kOwnRows;
+
+// A row on `cluster` blocks of `warps` warps (or, warps == 1, kOwnRows rows a
+// block).
+//
+// The likeliest classes: each thread has its largest value from the sums' pass.
+// The top-th largest of these is at most the row's top-th largest value, so
+// every class wanted is at least that, and lies with one of the threads whose
+// largest is: about `top` of them, whose values are read again (from L2), 32
+// lanes to a thread's, and those large enough are sorted.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a) {
   constexpr int N = Load<T>::N;
   constexpr int AHEAD = 4;
   __shared__ Sums sums[kMostWarps];
   __shared__ Sums blocks[8];
-  __shared__ unsigned long long keys[TOP ? kMostWarps : 1][32];
+  __shared__ uint32_t largest[TOP ? kMostWarps : 1][32];
+  __shared__ unsigned long long pool[TOP ? kPool : 1];
   __shared__ unsigned long long block_keys[TOP ? 8 : 1][32];
-  __shared__ uint32_t least[8];
+  __shared__ uint32_t counts[kOwnRows];
   if (a.cluster > 1) ptx::cluster_arrive();  // so that the first block is known to run before it is written to
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const bool own = a.warps == 1;
   const int warp = own ? 0 : w;
   const int rank = a.cluster > 1 ? (int)ptx::cluster_ctarank() : 0;
-  const long long row = own ? (long long)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x / (unsigned)a.cluster;
-  uint32_t* shared_least = &least[own ? w : 0];
-  if (TOP) {
-    if (own ? lane == 0 : threadIdx.x == 0) *shared_least = 0;
-    if (own) __syncwarp();
-    else __syncthreads();
-  }
+  const long long row = own ? (long long)blockIdx.x * kOwnRows + w : blockIdx.x / (unsigned)a.cluster;
+  uint32_t* count = &counts[own ? w : 0];
+  if (TOP && (own ? lane == 0 : threadIdx.x == 0)) *count = 0;
   if (row >= a.rows) return;
   const T* p = a.x + row * a.ldx;
   const int label = a.labels ? __ldg(a.labels + row) : -1;
@@ -180,69 +254,58 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
     at_label = one[0];
   }
 
+  const Part<T> part(p, a.classes, rank, a.cluster, warp, a.warps);
   Sums f{kLowest, 0.f, 0.f};
-  Best best{0ull, 0u, a.top};
-  auto one_by_one = [&](int from, int to) {  // values from .. to of the row (fewer than a vector) on a warp's lanes
-    const int i = from + lane;
-    float v[1] = {kLowest};
-    const bool in = i < to;
-    if (in) {
-      Vec<T, 1>::unpack(Vec<T, 1>::load(p + i), v);
-      if (v[0] > f.m) raise(f, v[0]);
-      const float d = max_nan(v[0] - f.m, kFar), e = exp2_approx(d * kLog2e);
-      f.s += e;
-      f.t += e * d;
-    }
-    if (TOP) take<1>(best, v, in ? 1 : 0, (uint32_t)i, lane, shared_least);
+  auto one_value = [&](float v) {
+    if (v > f.m) raise(f, v);
+    const float d = max_nan(v - f.m, kFar), e = exp2_approx(d * kLog2e);
+    f.s += e;
+    f.t += e * d;
   };
-  const int off = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % N);
-  const int head = min(off ? N - off : 0, a.classes), vecs = (a.classes - head) / N;
-  const int v0 = (int)((long long)vecs * rank / a.cluster), v1 = (int)((long long)vecs * (rank + 1) / a.cluster);
-  if (rank == 0 && warp == 0 && head) one_by_one(0, head);
-  const uint4* src = reinterpret_cast<const uint4*>(p + head);
-  const int step = a.warps * 32;
-  for (long long i0 = v0; i0 < v1; i0 += (long long)AHEAD * step) {  // the same for a warp's lanes
+  bool in_head = false, in_tail = false;
+  float head = kLowest, tail = kLowest;
+  if (part.has_head) head = part.end_value(0, part.head, lane, &in_head);
+  if (part.has_tail) tail = part.end_value(part.tail_at(), a.classes, lane, &in_tail);
+  if (in_head) one_value(head);
+  if (in_tail) one_value(tail);
+  const uint4* src = part.vectors();
+  for (long long i0 = part.v0 + warp * 32 + lane; i0 < part.v1; i0 += (long long)AHEAD * part.step) {
     uint4 raw[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      const long long i = i0 + j * step + warp * 32 + lane;
-      if (i < v1) raw[j] = src[i];
-    }
+    for (int j = 0; j < AHEAD; ++j)
+      if (i0 + j * part.step < part.v1) raw[j] = src[i0 + j * part.step];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const long long first = i0 + j * step + warp * 32, i = first + lane;
-      if (first >= v1) break;
+      if (i0 + j * part.step >= part.v1) break;
       float v[N];
       Vec<T, N>::unpack(raw[j], v);
-      float most = kLowest;
-      if (i < v1) {
-        most = v[0];
+      float most = v[0];
 #pragma unroll
-        for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
-        if (most > f.m) raise(f, most);
-        const uint64_t m2 = ptx::pack2(-f.m, -f.m), l2 = ptx::pack2(kLog2e, kLog2e);
-        uint64_t s2 = 0, t2 = 0;
+      for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
+      if (most > f.m) raise(f, most);
+      const uint64_t m2 = ptx::pack2(-f.m, -f.m), l2 = ptx::pack2(kLog2e, kLog2e);
+      uint64_t s2 = 0, t2 = 0;
 #pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          float2 d = ptx::unpack2(ptx::add2(ptx::pack2(v[e], v[e + 1]), m2));
-          d.x = max_nan(d.x, kFar);
-          d.y = max_nan(d.y, kFar);
-          const uint64_t d2 = ptx::pack2(d.x, d.y);
-          const float2 g = ptx::unpack2(ptx::mul2(d2, l2));
-          const uint64_t e2 = ptx::pack2(exp2_approx(g.x), exp2_approx(g.y));
-          s2 = ptx::add2(s2, e2);
-          ptx::fma2_to(t2, e2, d2);
-        }
-        const float2 s = ptx::unpack2(s2), t = ptx::unpack2(t2);
-        f.s += s.x + s.y;
-        f.t += t.x + t.y;
+      for (int e = 0; e < N; e += 2) {
+        float2 d = ptx::unpack2(ptx::add2(ptx::pack2(v[e], v[e + 1]), m2));
+        d.x = max_nan(d.x, kFar);
+        d.y = max_nan(d.y, kFar);
+        const uint64_t d2 = ptx::pack2(d.x, d.y);
+        const float2 g = ptx::unpack2(ptx::mul2(d2, l2));
+        const uint64_t e2 = ptx::pack2(exp2_approx(g.x), exp2_approx(g.y));
+        s2 = ptx::add2(s2, e2);
+        ptx::fma2_to(t2, e2, d2);
       }
-      if (TOP && __any_sync(0xffffffffu, i < v1 && (ordered(most) > best.least || best.least == 0u)))
-        take<N>(best, v, i < v1 ? N : 0, (uint32_t)(head + i * N), lane, shared_least);
+      const float2 s = ptx::unpack2(s2), t = ptx::unpack2(t2);
+      f.s += s.x + s.y;
+      f.t += t.x + t.y;
     }
   }
-  if (rank == a.cluster - 1 && warp == a.warps - 1 && head + vecs * N < a.classes) one_by_one(head + vecs * N, a.classes);
+  __syncwarp();
 
+  const uint32_t mine = ordered(f.m);  // the thread's largest (the lowest finite value if it has none)
+  uint32_t in_order = 0;
+  if (TOP) in_order = sorted(mine, lane);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums b{__shfl_xor_sync(0xffffffffu, f.m, o), __shfl_xor_sync(0xffffffffu, f.s, o), __shfl_xor_sync(0xffffffffu, f.t, o)};
@@ -250,7 +313,7 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
   }
   if (!own) {
     if (lane == 0) sums[warp] = f;
-    if (TOP) keys[warp][lane] = best.key;
+    if (TOP) largest[warp][lane] = in_order;
     __syncthreads();
     if (warp == 0) {
       f = lane < a.warps ? sums[lane] : Sums{kLowest, 0.f, 0.f};
@@ -260,32 +323,80 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
                __shfl_xor_sync(0xffffffffu, f.t, o)};
         join(f, b);
       }
-      if (TOP)
-        for (int i = 1; i < a.warps; ++i) best.key = merge(best.key, keys[i][lane], lane);
     }
-    if (a.cluster > 1) {
-      ptx::cluster_wait();
-      if (warp == 0) {  // to the first block
-        if (lane == 0) {
-          ptx::st_remote_f32(&blocks[rank].m, 0, f.m);
-          ptx::st_remote_f32(&blocks[rank].s, 0, f.s);
-          ptx::st_remote_f32(&blocks[rank].t, 0, f.t);
-        }
-        if (TOP)
-          ptx::st_remote_u2(reinterpret_cast<uint2*>(&block_keys[rank][lane]), 0,
-                            make_uint2((uint32_t)best.key, (uint32_t)(best.key >> 32)));
-      }
-      __syncwarp();
-      ptx::cluster_sync();
-      if (rank == 0 && warp == 0) {
-        f = blocks[0];
-        for (int i = 1; i < a.cluster; ++i) join(f, blocks[i]);
-        if (TOP)
-          for (int i = 1; i < a.cluster; ++i) best.key = merge(best.key, block_keys[i][lane], lane);
-      }
-    }
-    if (rank != 0 || warp != 0) return;
   }
+
+  unsigned long long key = 0;  // of the part's classes, likeliest first, in the lanes of its first warp
+  if (TOP) {
+    unsigned long long* const to = pool + (own ? w * kOwnPool : 0);
+    const uint32_t room = own ? kOwnPool : kPool;
+    const uint32_t least = __shfl_sync(0xffffffffu, own ? in_order : first_of(largest, a.warps, a.top, lane), a.top - 1);
+    const float floor = unordered(least);
+    auto add = [&](float v, bool in, uint32_t index) {  // NaN is not at least anything
+      const bool hit = in && v >= floor;
+      const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+      if (!hits) return;
+      uint32_t at = 0;
+      if (lane == 0) at = atomicAdd(count, (uint32_t)__popc(hits));
+      at = __shfl_sync(0xffffffffu, at, 0) + (uint32_t)__popc(hits & ((1u << lane) - 1u));
+      if (hit && at < room) to[at] = key_of(ordered(v), index);
+    };
+    if (part.has_head) add(head, in_head, (uint32_t)lane);
+    if (part.has_tail) add(tail, in_tail, (uint32_t)(part.tail_at() + lane));
+    for (uint32_t who = __ballot_sync(0xffffffffu, mine >= least); who; who &= who - 1u) {
+      const long long from = part.v0 + warp * 32 + (__ffs(who) - 1);
+      for (long long first = from; first < part.v1; first += 32ll * part.step) {
+        const long long i = first + (long long)lane * part.step;
+        const bool in = i < part.v1;
+        float v[N];
+        Vec<T, N>::unpack(in ? src[i] : make_uint4(0, 0, 0, 0), v);
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < N; ++e) any |= in && v[e] >= floor;
+        if (__any_sync(0xffffffffu, any)) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) add(v[e], in, (uint32_t)(part.head + i * N + e));
+        }
+      }
+    }
+    if (own) __syncwarp();
+    else __syncthreads();
+    const uint32_t found = *reinterpret_cast<volatile uint32_t*>(count);
+    if (found < (uint32_t)a.top || found > room) {
+      key = best_by_insertion(part, a.top, warp, lane);
+      if (!own) {
+        __syncthreads();  // the pool is no longer read
+        pool[warp * 32 + lane] = key;
+        __syncthreads();
+        if (warp == 0) key = first_of(reinterpret_cast<const unsigned long long(*)[32]>(pool), a.warps, a.top, lane);
+      }
+    } else if (warp == 0) {
+      for (uint32_t i = 0; i < found; i += 32) {
+        const unsigned long long n = sorted(i + lane < found ? to[i + lane] : 0ull, lane);
+        key = i == 0 ? n : merged(key, n, lane);
+      }
+    }
+  }
+  if (a.cluster > 1) {
+    ptx::cluster_wait();
+    if (warp == 0) {  // to the first block
+      if (lane == 0) {
+        ptx::st_remote_f32(&blocks[rank].m, 0, f.m);
+        ptx::st_remote_f32(&blocks[rank].s, 0, f.s);
+        ptx::st_remote_f32(&blocks[rank].t, 0, f.t);
+      }
+      if (TOP)
+        ptx::st_remote_u2(reinterpret_cast<uint2*>(&block_keys[rank][lane]), 0, make_uint2((uint32_t)key, (uint32_t)(key >> 32)));
+    }
+    __syncwarp();
+    ptx::cluster_sync();
+    if (rank == 0 && warp == 0) {
+      f = blocks[0];
+      for (int i = 1; i < a.cluster; ++i) join(f, blocks[i]);
+      if (TOP) key = first_of(block_keys, a.cluster, a.top, lane);
+    }
+  }
+  if (rank != 0 || warp != 0) return;
   // an empty row, and one with a NaN or +infinity, has no distribution
   const bool none = !(f.s > 0.f);
   const float nan = __int_as_float(0x7FC00000), m = f.s == 0.f ? -INFINITY : f.m;
@@ -296,9 +407,9 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
     if (a.stats) a.stats[row] = make_float2(f.s != f.s ? nan : m, ln);
   }
   if (TOP && lane < a.top) {
-    const bool got = best.key != 0ull;
-    a.top_index[row * a.top + lane] = got ? (int)(0xFFFFFFFFu - (uint32_t)best.key) : lane;
-    a.top_logp[row * a.top + lane] = got ? (unordered((uint32_t)(best.key >> 32)) - m) - ln : nan;
+    const bool got = key != 0ull;
+    a.top_index[row * a.top + lane] = got ? (int)(0xFFFFFFFFu - (uint32_t)key) : lane;
+    a.top_logp[row * a.top + lane] = got ? (unordered((uint32_t)(key >> 32)) - m) - ln : nan;
   }
 }
 
@@ -411,8 +522,8 @@ ff_status logprobs_t(Args<T> a, cudaStream_t st) {
     while (a.warps < kMostWarps && (long long)a.warps * 2 * 32 <= vecs && (long long)a.rows * a.warps < 152 * 32) a.warps *= 2;
     while (a.cluster < 8 && (long long)a.cluster * 2 * a.warps * 32 <= vecs && (long long)a.rows * a.cluster * 2 <= 152) a.cluster *= 2;
   }
-  const unsigned threads = a.warps == 1 ? 256 : (unsigned)a.warps * 32;
-  const long long grid = a.warps == 1 ? cdiv(a.rows, 8) : (long long)a.rows * a.cluster;
+  const unsigned threads = a.warps == 1 ? kOwnRows * 32 : (unsigned)a.warps * 32;
+  const long long grid = a.warps == 1 ? cdiv(a.rows, kOwnRows) : (long long)a.rows * a.cluster;
   if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)a.rows * a.classes * sizeof(T);
   auto* const go = a.top ? launch<T, true> : launch<T, false>;
