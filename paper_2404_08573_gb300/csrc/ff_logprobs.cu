@@ -91,27 +91,45 @@ __device__ __forceinline__ K merged(K a, K b, int lane) {
   for (int o = 16; o > 0; o /= 2) a = step(a, o, (lane & o) == 0);
   return a;
 }
-// The first 32 of `lists` lists in shared memory ([lists][32], largest first),
-// of which the first `top` of each count: as many lists at a time as their
-// firsts fill a warp.
-template <typename K>
-__device__ __forceinline__ K first_of(const K (*list)[32], int lists, int top, int lane) {
-  const int log = top > 1 ? 32 - __clz(top - 1) : 0, per = 32 >> log;  // 2^log >= top of each
-  K best = 0;
-  for (int i = 0; i < lists; i += per) {
-    const int l = i + (lane >> log);
-    K a = l < lists ? list[l][lane & ((1 << log) - 1)] : K(0);
-    if (per > 1) a = sorted(a, lane);
+// The 32 largest of n keys in shared memory, largest first; `place` (32 of them)
+// is scratch.  A few by counting how many are larger (keys differ), which is one
+// broadcast read each; many by sorting and merging.
+__device__ __forceinline__ unsigned long long first_of(const unsigned long long* keys, int n, int lane, unsigned long long* place) {
+  if (n > 96) {
+    unsigned long long best = 0;
+    for (int i = 0; i < n; i += 32) {
+      const unsigned long long a = sorted(i + lane < n ? keys[i + lane] : 0ull, lane);
+      best = i == 0 ? a : merged(best, a, lane);
+    }
+    return best;
+  }
+  place[lane] = 0ull;
+  __syncwarp();
+  for (int i = lane; i < n; i += 32) {
+    const unsigned long long mine = keys[i];
+    int larger = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) larger += keys[j] > mine;
+    if (larger < 32 && mine != 0ull) place[larger] = mine;
+  }
+  __syncwarp();
+  return place[lane];
+}
+// The k-th largest of n <= 128 numbers in shared memory.
+__device__ __forceinline__ uint32_t kth_of(const uint32_t* numbers, int n, int k, int lane) {
+  uint32_t best = 0;
+  for (int i = 0; i < n; i += 32) {
+    const uint32_t a = sorted(i + lane < n ? numbers[i + lane] : 0u, lane);
     best = i == 0 ? a : merged(best, a, lane);
   }
-  return best;
+  return __shfl_sync(0xffffffffu, best, k - 1);
 }
 
 template <typename T>
 struct Args {
   const T* x;
   long long ldx;
-  int rows, classes, top, warps, cluster;
+  int rows, classes, top, warps, cluster, groups;
   const int* labels;
   float *logp, *entropy, *top_logp;
   int* top_index;
@@ -220,19 +238,22 @@ constexpr int kOwnPool = kPool / kOwnRows;
 // block).
 //
 // The likeliest classes: each thread has its largest value from the sums' pass.
-// The top-th largest of these is at most the row's top-th largest value, so
-// every class wanted is at least that, and lies with one of the threads whose
-// largest is: about `top` of them, whose values are read again (from L2), 32
-// lanes to a thread's, and those large enough are sorted.
+// Of any groups of threads, the top-th largest of the groups' largest values is
+// at most the row's top-th largest value, so every class wanted is at least
+// that, and lies with one of the threads whose largest is.  Their values are
+// read again (from L2) and those large enough are sorted.  Groups: whole warps,
+// or the lanes of a warp in `a.groups` classes, so that there are at least 1.5
+// top of them (then some 1.1 top values are found, 2 at worst).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a) {
   constexpr int N = Load<T>::N;
   constexpr int AHEAD = 4;
   __shared__ Sums sums[kMostWarps];
   __shared__ Sums blocks[8];
-  __shared__ uint32_t largest[TOP ? kMostWarps : 1][32];
+  __shared__ uint32_t largest[TOP ? 128 : 1];
   __shared__ unsigned long long pool[TOP ? kPool : 1];
-  __shared__ unsigned long long block_keys[TOP ? 8 : 1][32];
+  __shared__ unsigned long long place[TOP ? kOwnRows : 1][32];
+  __shared__ unsigned long long block_keys[TOP ? 8 * 32 : 1];
   __shared__ uint32_t counts[kOwnRows];
   if (a.cluster > 1) ptx::cluster_arrive();  // so that the first block is known to run before it is written to
   ptx::griddep_wait();
@@ -246,14 +267,6 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
   if (row >= a.rows) return;
   const T* p = a.x + row * a.ldx;
   const int label = a.labels ? __ldg(a.labels + row) : -1;
-  const bool has = label >= 0 && label < a.classes;
-  float at_label = 0.f;
-  if (has) {
-    float one[1];
-    Vec<T, 1>::unpack(Vec<T, 1>::load(p + label), one);
-    at_label = one[0];
-  }
-
   const Part<T> part(p, a.classes, rank, a.cluster, warp, a.warps);
   Sums f{kLowest, 0.f, 0.f};
   auto one_value = [&](float v) {
@@ -266,8 +279,6 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
   float head = kLowest, tail = kLowest;
   if (part.has_head) head = part.end_value(0, part.head, lane, &in_head);
   if (part.has_tail) tail = part.end_value(part.tail_at(), a.classes, lane, &in_tail);
-  if (in_head) one_value(head);
-  if (in_tail) one_value(tail);
   const uint4* src = part.vectors();
   for (long long i0 = part.v0 + warp * 32 + lane; i0 < part.v1; i0 += (long long)AHEAD * part.step) {
     uint4 raw[AHEAD];
@@ -301,11 +312,23 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
       f.t += t.x + t.y;
     }
   }
+  if (in_head) one_value(head);
+  if (in_tail) one_value(tail);
   __syncwarp();
+  const bool has = label >= 0 && label < a.classes;
+  float at_label = 0.f;
+  if (has && rank == 0 && warp == 0) {
+    float one[1];
+    Vec<T, 1>::unpack(Vec<T, 1>::load(p + label), one);
+    at_label = one[0];
+  }
 
   const uint32_t mine = ordered(f.m);  // the thread's largest (the lowest finite value if it has none)
-  uint32_t in_order = 0;
-  if (TOP) in_order = sorted(mine, lane);
+  uint32_t group = mine;
+  if (TOP && !own) {
+    for (int o = 16; o >= a.groups; o >>= 1) group = max(group, __shfl_xor_sync(0xffffffffu, group, o));
+    if (lane < a.groups) largest[warp * a.groups + lane] = group;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums b{__shfl_xor_sync(0xffffffffu, f.m, o), __shfl_xor_sync(0xffffffffu, f.s, o), __shfl_xor_sync(0xffffffffu, f.t, o)};
@@ -313,7 +336,6 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
   }
   if (!own) {
     if (lane == 0) sums[warp] = f;
-    if (TOP) largest[warp][lane] = in_order;
     __syncthreads();
     if (warp == 0) {
       f = lane < a.warps ? sums[lane] : Sums{kLowest, 0.f, 0.f};
@@ -330,7 +352,8 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
   if (TOP) {
     unsigned long long* const to = pool + (own ? w * kOwnPool : 0);
     const uint32_t room = own ? kOwnPool : kPool;
-    const uint32_t least = __shfl_sync(0xffffffffu, own ? in_order : first_of(largest, a.warps, a.top, lane), a.top - 1);
+    const uint32_t least =
+        own ? __shfl_sync(0xffffffffu, sorted(mine, lane), a.top - 1) : kth_of(largest, a.warps * a.groups, a.top, lane);
     const float floor = unordered(least);
     auto add = [&](float v, bool in, uint32_t index) {  // NaN is not at least anything
       const bool hit = in && v >= floor;
@@ -343,21 +366,26 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
     };
     if (part.has_head) add(head, in_head, (uint32_t)lane);
     if (part.has_tail) add(tail, in_tail, (uint32_t)(part.tail_at() + lane));
-    for (uint32_t who = __ballot_sync(0xffffffffu, mine >= least); who; who &= who - 1u) {
-      const long long from = part.v0 + warp * 32 + (__ffs(who) - 1);
-      for (long long first = from; first < part.v1; first += 32ll * part.step) {
-        const long long i = first + (long long)lane * part.step;
-        const bool in = i < part.v1;
-        float v[N];
-        Vec<T, N>::unpack(in ? src[i] : make_uint4(0, 0, 0, 0), v);
-        bool any = false;
+    auto add_all = [&](long long i) {  // vector i on each lane
+      const bool in = i < part.v1;
+      float v[N];
+      Vec<T, N>::unpack(in ? src[i] : make_uint4(0, 0, 0, 0), v);
+      bool any = false;
 #pragma unroll
-        for (int e = 0; e < N; ++e) any |= in && v[e] >= floor;
-        if (__any_sync(0xffffffffu, any)) {
+      for (int e = 0; e < N; ++e) any |= in && v[e] >= floor;
+      if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) add(v[e], in, (uint32_t)(part.head + i * N + e));
-        }
+        for (int e = 0; e < N; ++e) add(v[e], in, (uint32_t)(part.head + i * N + e));
       }
+    };
+    uint32_t who = __ballot_sync(0xffffffffu, mine >= least);
+    if (part.v1 - part.v0 <= 4 * part.step) {  // a few vectors a thread: each lane its own
+      if (who)
+        for (long long i = part.v0 + warp * 32; i < part.v1; i += part.step) add_all(i + lane);
+    } else {  // else 32 lanes to one's
+      for (; who; who &= who - 1u)
+        for (long long i = part.v0 + warp * 32 + (__ffs(who) - 1); i < part.v1; i += 32ll * part.step)
+          add_all(i + (long long)lane * part.step);
     }
     if (own) __syncwarp();
     else __syncthreads();
@@ -368,13 +396,10 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
         __syncthreads();  // the pool is no longer read
         pool[warp * 32 + lane] = key;
         __syncthreads();
-        if (warp == 0) key = first_of(reinterpret_cast<const unsigned long long(*)[32]>(pool), a.warps, a.top, lane);
+        if (warp == 0) key = first_of(pool, a.warps * 32, lane, place[0]);
       }
     } else if (warp == 0) {
-      for (uint32_t i = 0; i < found; i += 32) {
-        const unsigned long long n = sorted(i + lane < found ? to[i + lane] : 0ull, lane);
-        key = i == 0 ? n : merged(key, n, lane);
-      }
+      key = first_of(to, (int)found, lane, place[own ? w : 0]);
     }
   }
   if (a.cluster > 1) {
@@ -385,15 +410,16 @@ __global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a
         ptx::st_remote_f32(&blocks[rank].s, 0, f.s);
         ptx::st_remote_f32(&blocks[rank].t, 0, f.t);
       }
-      if (TOP)
-        ptx::st_remote_u2(reinterpret_cast<uint2*>(&block_keys[rank][lane]), 0, make_uint2((uint32_t)key, (uint32_t)(key >> 32)));
+      if (TOP && lane < a.top)
+        ptx::st_remote_u2(reinterpret_cast<uint2*>(&block_keys[rank * a.top + lane]), 0,
+                          make_uint2((uint32_t)key, (uint32_t)(key >> 32)));
     }
     __syncwarp();
     ptx::cluster_sync();
     if (rank == 0 && warp == 0) {
       f = blocks[0];
       for (int i = 1; i < a.cluster; ++i) join(f, blocks[i]);
-      if (TOP) key = first_of(block_keys, a.cluster, a.top, lane);
+      if (TOP) key = first_of(block_keys, a.cluster * a.top, lane, place[0]);
     }
   }
   if (rank != 0 || warp != 0) return;
@@ -522,6 +548,8 @@ ff_status logprobs_t(Args<T> a, cudaStream_t st) {
     while (a.warps < kMostWarps && (long long)a.warps * 2 * 32 <= vecs && (long long)a.rows * a.warps < 152 * 32) a.warps *= 2;
     while (a.cluster < 8 && (long long)a.cluster * 2 * a.warps * 32 <= vecs && (long long)a.rows * a.cluster * 2 <= 152) a.cluster *= 2;
   }
+  a.groups = 1;
+  while (a.groups < 32 && 2 * a.warps * a.groups < 3 * a.top) a.groups *= 2;
   const unsigned threads = a.warps == 1 ? kOwnRows * 32 : (unsigned)a.warps * 32;
   const long long grid = a.warps == 1 ? cdiv(a.rows, kOwnRows) : (long long)a.rows * a.cluster;
   if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
