@@ -244,8 +244,12 @@ constexpr int kOwnPool = kPool / kOwnRows;
 // read again (from L2) and those large enough are sorted.  Groups: whole warps,
 // or the lanes of a warp in `a.groups` classes, so that there are at least 1.5
 // top of them (then some 1.1 top values are found, 2 at worst).
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kMostWarps * 32, 1) k_logprobs(const Args<T> a) {
+//
+// WARPS: the most a block has.  Rows are many with 8: five blocks an SM keep
+// 80 KB of loads in flight while others select (2048 x 49999 fp32: top 0 66 us, with
+// four 71, with six, which spill, 73; top 4 77, 82, 88).
+template <typename T, bool TOP, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 5 : 1) k_logprobs(const Args<T> a) {
   constexpr int N = Load<T>::N;
   constexpr int AHEAD = 4;
   __shared__ Sums sums[kMostWarps];
@@ -518,7 +522,7 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(const GradArgs<T> a) {
 }
 
 // ------------------------------------------------------------------ host
-template <typename T, bool TOP>
+template <typename T, bool TOP, int WARPS>
 cudaError_t launch(const Args<T>& a, unsigned grid, unsigned threads, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
@@ -532,17 +536,18 @@ cudaError_t launch(const Args<T>& a, unsigned grid, unsigned threads, cudaStream
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, k_logprobs<T, TOP>, a);
+  return cudaLaunchKernelEx(&cfg, k_logprobs<T, TOP, WARPS>, a);
 }
 
 template <typename T>
 ff_status logprobs_t(Args<T> a, cudaStream_t st) {
   constexpr int N = Load<T>::N;
   const int vecs = cdiv(a.classes, N);
-  // Short rows take a warp each.  Others a block of 8 warps; with fewer rows
+  // Short rows take a warp each (few rows only if it has two rounds of loads at
+  // most).  Others a block of 8 warps; with fewer rows
   // than the GPU has room for, more warps and then more blocks, as long as
   // each thread has a vector or two to read.
-  a.warps = vecs <= 256 && a.rows >= 152 ? 1 : 8;
+  a.warps = vecs <= (a.rows >= 152 ? 256 : 64) ? 1 : 8;
   a.cluster = 1;
   if (a.warps == 8 && a.rows < 152 * 4) {
     while (a.warps < kMostWarps && (long long)a.warps * 2 * 32 <= vecs && (long long)a.rows * a.warps < 152 * 32) a.warps *= 2;
@@ -554,7 +559,8 @@ ff_status logprobs_t(Args<T> a, cudaStream_t st) {
   const long long grid = a.warps == 1 ? cdiv(a.rows, kOwnRows) : (long long)a.rows * a.cluster;
   if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)a.rows * a.classes * sizeof(T);
-  auto* const go = a.top ? launch<T, true> : launch<T, false>;
+  auto* const go = a.warps > 8 ? (a.top ? launch<T, true, kMostWarps> : launch<T, false, kMostWarps>)
+                               : (a.top ? launch<T, true, 8> : launch<T, false, 8>);
   FF_LAUNCH(K_LOGPROBS, bytes, st, go(a, (unsigned)grid, threads, st), "label log-probabilities");
   return FF_OK;
 }

@@ -6,6 +6,10 @@
 //
 // A row is cut into units of 128 values, four to a lane, so that a warp holds
 // whole e4m3 blocks; `warps` warps share a row.
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
 #include "ff_api_internal.h"
 #include "ff_e4m3.cuh"
 #include "ff_ptx.cuh"
@@ -19,53 +23,87 @@ constexpr int kMaxWarps = 32;
 
 // A lane's four values of the unit at column c0, V of them consecutive: 16 or
 // 8 bytes (V = 4), a pair of bf16 (V = 2), or one (V = 1, the lanes side by
-// side), as the rows' alignment allows.
+// side), as the rows' alignment allows.  Held as loaded, bf16 in pairs.
+template <typename T>
+struct Held;
+template <>
+struct Held<float> {
+  float w[4];
+  __device__ __forceinline__ void pairs(uint64_t (&p)[2]) const {
+    p[0] = ptx::pack2(w[0], w[1]);
+    p[1] = ptx::pack2(w[2], w[3]);
+  }
+  __device__ __forceinline__ void set(const uint64_t (&p)[2]) {
+    const float2 a = ptx::unpack2(p[0]), b = ptx::unpack2(p[1]);
+    w[0] = a.x;
+    w[1] = a.y;
+    w[2] = b.x;
+    w[3] = b.y;
+  }
+  __device__ __forceinline__ void add(const Held& o) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] += o.w[e];
+  }
+};
+template <>
+struct Held<bf16> {
+  uint32_t w[2];
+  __device__ __forceinline__ void pairs(uint64_t (&p)[2]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = ptx::pack2(w[i] << 16, w[i] & 0xFFFF0000u);
+  }
+  __device__ __forceinline__ void set(const uint64_t (&p)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 f = ptx::unpack2(p[i]);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  // One rounding, which is also that of an fp32 sum rounded once more: where
+  // fp32 cannot hold the sum of two bf16 values exactly, one is below 2^-15 of the
+  // other, and the sum far from halfway between two of them.
+  __device__ __forceinline__ void add(const Held& o) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __nv_bfloat162 h = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), *reinterpret_cast<const __nv_bfloat162*>(&o.w[i]));
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+};
+
 template <typename T, int V>
-struct Unit {
-  static constexpr int N = 4 / V;
-  typename Vec<T, V>::Raw raw[N];
-  static __device__ __forceinline__ int col(int e, int lane) { return (e / V) * 32 * V + lane * V + e % V; }
-  __device__ __forceinline__ void load(const T* row, int c0, int lane, int cols) {
+struct Unit : Held<T> {
+  static constexpr int N = 4 / V;  // accesses
+  using Raw = typename Vec<T, V>::Raw;
+  static __device__ __forceinline__ int first(int i, int lane) { return i * 32 * V + lane * V; }
+  static __device__ __forceinline__ int col(int e, int lane) { return first(e / V, lane) + e % V; }
+  __device__ __forceinline__ Raw* raw() { return reinterpret_cast<Raw*>(this->w); }
+  __device__ __forceinline__ const Raw* raw() const { return reinterpret_cast<const Raw*>(this->w); }
+  // whole: the unit lies inside the row
+  __device__ __forceinline__ void load(const T* row, int c0, int lane, int cols, bool whole) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = c0 + i * 32 * V + lane * V;
-      if (c + V <= cols) {
-        raw[i] = Vec<T, V>::load(row + c);
+      const int c = c0 + first(i, lane);
+      if (whole || c + V <= cols) {
+        raw()[i] = Vec<T, V>::load(row + c);
       } else {
         T t[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) t[e] = c + e < cols ? row[c + e] : T(0.f);
-        memcpy(&raw[i], t, sizeof(raw[i]));
+        memcpy(&raw()[i], t, sizeof(Raw));
       }
     }
   }
-  __device__ __forceinline__ void values(float (&v)[4]) const {
+  __device__ __forceinline__ void store(T* row, int c0, int lane, int cols, bool whole) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float t[V];
-      Vec<T, V>::unpack(raw[i], t);
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[i * V + e] = t[e];
-    }
-  }
-  __device__ __forceinline__ void set(const float (&v)[4]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) t[e] = v[i * V + e];
-      Vec<T, V>::store(reinterpret_cast<T*>(&raw[i]), t);
-    }
-  }
-  __device__ __forceinline__ void store(T* row, int c0, int lane, int cols) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = c0 + i * 32 * V + lane * V;
-      if (c + V <= cols) {
-        *reinterpret_cast<typename Vec<T, V>::Raw*>(row + c) = raw[i];
+      const int c = c0 + first(i, lane);
+      if (whole || c + V <= cols) {
+        *reinterpret_cast<Raw*>(row + c) = raw()[i];
       } else {
         T t[V];
-        memcpy(t, &raw[i], sizeof(raw[i]));
+        memcpy(t, &raw()[i], sizeof(Raw));
 #pragma unroll
         for (int e = 0; e < V; ++e)
           if (c + e < cols) row[c + e] = t[e];
@@ -76,20 +114,26 @@ struct Unit {
 
 // A lane's four gammas of the unit (null: ones); zero past the row.
 template <int V>
-__device__ __forceinline__ void gammas(float (&g)[4], const float* gamma, int c0, int lane, int cols, bool wide) {
-  if (V == 4 && wide && gamma && c0 + lane * 4 + 4 <= cols) {
+__device__ __forceinline__ void gammas(uint64_t (&g)[2], const float* gamma, int c0, int lane, int cols, bool wide, bool whole) {
+  if (V == 4 && wide && gamma && (whole || c0 + lane * 4 + 4 <= cols)) {
     const float4 f = __ldg(reinterpret_cast<const float4*>(gamma + c0 + lane * 4));
-    g[0] = f.x;
-    g[1] = f.y;
-    g[2] = f.z;
-    g[3] = f.w;
+    g[0] = ptx::pack2(f.x, f.y);
+    g[1] = ptx::pack2(f.z, f.w);
     return;
   }
+  float v[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int c = c0 + Unit<float, V>::col(e, lane);
-    g[e] = c < cols ? (gamma ? __ldg(gamma + c) : 1.f) : 0.f;
+    v[e] = c < cols ? (gamma ? __ldg(gamma + c) : 1.f) : 0.f;
   }
+  g[0] = ptx::pack2(v[0], v[1]);
+  g[1] = ptx::pack2(v[2], v[3]);
+}
+__device__ __forceinline__ uint64_t both(float v) { return ptx::pack2(v, v); }
+__device__ __forceinline__ float sum_of(uint64_t v) {
+  const float2 f = ptx::unpack2(v);
+  return f.x + f.y;
 }
 
 // The sum over a row's warps of v, in a fixed order; `part` holds two rows'
@@ -119,46 +163,113 @@ struct RmsArgs {
   bool wide;  // gamma is 16-byte aligned
 };
 
-// One unit of a row's output from its h values.
+// y of one unit from its h values, zero past the row.
 template <typename T, int V>
-__device__ __forceinline__ void put_unit(const RmsArgs<T>& a, long long row, int c0, int lane, const float (&v)[4],
-                                         float rstd) {
-  float y[4], g[4];
-  gammas<V>(g, a.gamma, c0, lane, a.cols, a.wide);
+__device__ __forceinline__ void outputs(const RmsArgs<T>& a, uint64_t (&y)[2], int c0, int lane, float rstd, bool whole) {
+  uint64_t g[2];
+  gammas<V>(g, a.gamma, c0, lane, a.cols, a.wide, whole);
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    y[e] = c0 + Unit<T, V>::col(e, lane) < a.cols ? __fmul_rn(__fmul_rn(v[e], rstd), g[e]) : 0.f;
+  for (int i = 0; i < 2; ++i) y[i] = ptx::mul2(ptx::mul2(y[i], both(rstd)), g[i]);
+  if (!whole) {  // (a row with a NaN is NaN past its end too, without this)
+    float2 f[2] = {ptx::unpack2(y[0]), ptx::unpack2(y[1])};
+    float* v = &f[0].x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = c0 + Unit<T, V>::col(e, lane) < a.cols ? v[e] : 0.f;
+    y[0] = ptx::pack2(f[0].x, f[0].y);
+    y[1] = ptx::pack2(f[1].x, f[1].y);
+  }
+}
+// The bits of the largest magnitude over the warp (a NaN's above all others).
+__device__ __forceinline__ uint32_t amax_of(const uint64_t (&y)[2]) {
+  const float2 a = ptx::unpack2(y[0]), b = ptx::unpack2(y[1]);
+  float m, n;
+  asm("{\n\t.reg .f32 p, q;\n\tabs.f32 p, %1;\n\tabs.f32 q, %2;\n\tmax.NaN.f32 %0, p, q;\n\t}" : "=f"(m) : "f"(a.x), "f"(a.y));
+  asm("{\n\t.reg .f32 p, q;\n\tabs.f32 p, %1;\n\tabs.f32 q, %2;\n\tmax.NaN.f32 %0, p, q;\n\t}" : "=f"(n) : "f"(b.x), "f"(b.y));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(n));
+  return __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+}
+template <typename T, int V>
+__device__ __forceinline__ void put_fp8(const RmsArgs<T>& a, long long row, const uint64_t (&y)[2], int c0, int lane, float inv,
+                                        bool whole) {
+  const float2 f = ptx::unpack2(ptx::mul2(y[0], both(inv))), g = ptx::unpack2(ptx::mul2(y[1], both(inv)));
+  const uint32_t lo = e4m3x2(f.x, f.y), hi = e4m3x2(g.x, g.y);
+  uint8_t* q = a.q + row * a.ldq + c0;
+  // ldq is a multiple of 16: a vector lies inside or outside
+  if constexpr (V == 4) {
+    if (whole || c0 + 4 * lane < a.ldq) *reinterpret_cast<uint32_t*>(q + 4 * lane) = lo | hi << 16;
+  } else if constexpr (V == 2) {
+    if (whole || c0 + 2 * lane < a.ldq) *reinterpret_cast<uint16_t*>(q + 2 * lane) = (uint16_t)lo;
+    if (whole || c0 + 64 + 2 * lane < a.ldq) *reinterpret_cast<uint16_t*>(q + 64 + 2 * lane) = (uint16_t)hi;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (whole || c0 + 32 * e + lane < a.ldq) q[32 * e + lane] = (uint8_t)((e < 2 ? lo : hi) >> 8 * (e & 1));
+  }
+}
+__device__ __forceinline__ float rstd_of(float sum, int cols, float eps) { return __frsqrt_rn(__fdiv_rn(sum, (float)cols) + eps); }
+
+// NU units a warp, the row in registers.  blockDim: a row's warps, or with one
+// warp a row, several rows.  whole: all of the warp's units lie inside the row.
+template <typename T, int V, int NU>
+__device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int warp, int lane, float* part, bool whole) {
+  Unit<T, V> u[NU];
+  const int c0 = warp * NU * UNIT;
+#pragma unroll
+  for (int i = 0; i < NU; ++i) u[i].load(a.x + row * a.ldx, c0 + i * UNIT, lane, a.cols, whole);
+  if (a.r) {
+    Unit<T, V> t[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) t[i].load(a.r + row * a.ldr, c0 + i * UNIT, lane, a.cols, whole);
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      u[i].add(t[i]);
+      u[i].store(a.h + row * a.ldh, c0 + i * UNIT, lane, a.cols, whole);
+    }
+  }
+  uint64_t ss[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    uint64_t v[2];
+    u[i].pairs(v);
+    ptx::fma2_to(ss[0], v[0], v[0]);
+    ptx::fma2_to(ss[1], v[1], v[1]);
+  }
+  const float sum = row_sum(sum_of(ptx::add2(ss[0], ss[1])), a.warps, warp, lane, part);
+  const float rstd = rstd_of(sum, a.cols, a.eps);
+  if (a.rstd && warp == 0 && lane == 0) a.rstd[row] = rstd;
   if (a.y) {
-    Unit<T, V> u;
-    u.set(y);
-    u.store(a.y + row * a.ldy, c0, lane, a.cols);
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      uint64_t y[2];
+      u[i].pairs(y);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      Unit<T, V> o;
+      o.set(y);
+      o.store(a.y + row * a.ldy, c0 + i * UNIT, lane, a.cols, whole);
+    }
   }
   if (a.q) {
-    uint32_t m = 0;
+    // The units' maxima first, so that lane i divides for unit i once.
+    uint32_t mine = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
-    m = __reduce_max_sync(0xffffffffu, m);
-    const float s = scale_of(m), inv = __frcp_rn(s);
-    if (lane == 0) a.scale[(long long)(c0 / UNIT) * a.rows + row] = s;
-    uint8_t* q = a.q + row * a.ldq + c0;
-    const uint32_t lo = e4m3x2(__fmul_rn(y[0], inv), __fmul_rn(y[1], inv));
-    const uint32_t hi = e4m3x2(__fmul_rn(y[2], inv), __fmul_rn(y[3], inv));
-    // ldq is a multiple of 16: a vector lies inside or outside
-    if constexpr (V == 4) {
-      if (c0 + 4 * lane < a.ldq) *reinterpret_cast<uint32_t*>(q + 4 * lane) = lo | hi << 16;
-    } else if constexpr (V == 2) {
-      if (c0 + 2 * lane < a.ldq) *reinterpret_cast<uint16_t*>(q + 2 * lane) = (uint16_t)lo;
-      if (c0 + 64 + 2 * lane < a.ldq) *reinterpret_cast<uint16_t*>(q + 64 + 2 * lane) = (uint16_t)hi;
-    } else {
+    for (int i = 0; i < NU; ++i) {
+      uint64_t y[2];
+      u[i].pairs(y);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      const uint32_t m = amax_of(y);
+      mine = lane == i ? m : mine;
+    }
+    const float s = scale_of(mine), inv = __frcp_rn(s);
+    if (lane < NU && c0 + lane * UNIT < a.cols) a.scale[(long long)(c0 / UNIT + lane) * a.rows + row] = s;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c0 + 32 * e + lane < a.ldq) q[32 * e + lane] = (uint8_t)((e < 2 ? lo : hi) >> 8 * (e & 1));
+    for (int i = 0; i < NU; ++i) {
+      uint64_t y[2];
+      u[i].pairs(y);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      put_fp8<T, V>(a, row, y, c0 + i * UNIT, lane, __shfl_sync(0xffffffffu, inv, i), whole);
     }
   }
 }
-
-// NU units a warp, the row in registers.  blockDim: a row's warps, or with one
-// warp a row, several rows.
 template <typename T, int V, int NU>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const RmsArgs<T> a) {
   __shared__ float part[kMaxWarps];
@@ -167,42 +278,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const RmsArgs<T> a) {
   const int warp = a.warps == 1 ? 0 : w;
   const long long row = a.warps == 1 ? (long long)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
   if (row >= a.rows) return;
-  Unit<T, V> u[NU];
-  const int c0 = warp * NU * UNIT;
-#pragma unroll
-  for (int i = 0; i < NU; ++i) u[i].load(a.x + row * a.ldx, c0 + i * UNIT, lane, a.cols);
-  if (a.r) {
-    Unit<T, V> t[NU];
-#pragma unroll
-    for (int i = 0; i < NU; ++i) t[i].load(a.r + row * a.ldr, c0 + i * UNIT, lane, a.cols);
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      float v[4], s[4];
-      u[i].values(v);
-      t[i].values(s);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += s[e];
-      u[i].set(v);
-      u[i].store(a.h + row * a.ldh, c0 + i * UNIT, lane, a.cols);
-    }
-  }
-  float ss = 0.f;
-#pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    float v[4];
-    u[i].values(v);
-    ss += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
-  }
-  ss = row_sum(ss, a.warps, warp, lane, part);
-  const float rstd = __frsqrt_rn(__fdiv_rn(ss, (float)a.cols) + a.eps);
-  if (a.rstd && warp == 0 && lane == 0) a.rstd[row] = rstd;
-#pragma unroll
-  for (int i = 0; i < NU; ++i) {
-    if (c0 + i * UNIT >= a.cols) break;
-    float v[4];
-    u[i].values(v);
-    put_unit<T, V>(a, row, c0 + i * UNIT, lane, v, rstd);
-  }
+  // (both calls meet at the same barrier)
+  if ((warp + 1) * NU * UNIT <= a.cols)
+    rms_row<T, V, NU>(a, row, warp, lane, part, true);
+  else
+    rms_row<T, V, NU>(a, row, warp, lane, part, false);
 }
 
 // Rows too long for registers: read twice (the second time h, which is in L2).
@@ -212,33 +292,39 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_long(const RmsArgs<T> a)
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long row = blockIdx.x;
-  float ss = 0.f;
+  uint64_t ss[2] = {0, 0};
   for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
     Unit<T, V> u, t;
-    float v[4], s[4];
-    u.load(a.x + row * a.ldx, (int)c, lane, a.cols);
-    u.values(v);
+    uint64_t v[2];
+    u.load(a.x + row * a.ldx, (int)c, lane, a.cols, false);
     if (a.r) {
-      t.load(a.r + row * a.ldr, (int)c, lane, a.cols);
-      t.values(s);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += s[e];
-      u.set(v);
-      u.store(a.h + row * a.ldh, (int)c, lane, a.cols);
-      u.values(v);
+      t.load(a.r + row * a.ldr, (int)c, lane, a.cols, false);
+      u.add(t);
+      u.store(a.h + row * a.ldh, (int)c, lane, a.cols, false);
     }
-    ss += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
+    u.pairs(v);
+    ptx::fma2_to(ss[0], v[0], v[0]);
+    ptx::fma2_to(ss[1], v[1], v[1]);
   }
-  ss = row_sum(ss, kMaxWarps, warp, lane, part);
-  const float rstd = __frsqrt_rn(__fdiv_rn(ss, (float)a.cols) + a.eps);
+  const float sum = row_sum(sum_of(ptx::add2(ss[0], ss[1])), kMaxWarps, warp, lane, part);
+  const float rstd = rstd_of(sum, a.cols, a.eps);
   if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
   const T* h = a.r ? a.h + row * a.ldh : a.x + row * a.ldx;  // each thread reads what it wrote itself
   for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
     Unit<T, V> u;
-    float v[4];
-    u.load(h, (int)c, lane, a.cols);
-    u.values(v);
-    put_unit<T, V>(a, row, (int)c, lane, v, rstd);
+    uint64_t y[2];
+    u.load(h, (int)c, lane, a.cols, false);
+    u.pairs(y);
+    outputs<T, V>(a, y, (int)c, lane, rstd, false);
+    if (a.q) {
+      const float s = scale_of(amax_of(y));
+      if (lane == 0) a.scale[c / UNIT * a.rows + row] = s;
+      put_fp8<T, V>(a, row, y, (int)c, lane, __frcp_rn(s), false);
+    }
+    if (a.y) {
+      u.set(y);
+      u.store(a.y + row * a.ldy, (int)c, lane, a.cols, false);
+    }
   }
 }
 
@@ -251,92 +337,125 @@ struct GradArgs {
   float* part;  // [gridDim.x, cols] sums of dgamma, or null
   long long lddy, ldh, lddh, lddx;
   int rows, cols, warps;
+  int depth;    // rows on their way
   bool wide;
 };
 
+// Copies one lane's part of a unit to its own slot of shared memory, by the
+// bytes that the alignment allows (single bf16 values go through registers).
+template <typename T, int V>
+__device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane, int cols) {
+  if constexpr (sizeof(T) * V >= 4) {
+    constexpr int BYTES = (int)sizeof(T) * V;
+#pragma unroll
+    for (int i = 0; i < 4 / V; ++i) {
+      const int c = c0 + Unit<T, V>::first(i, lane);
+      const int left = min(max(cols - c, 0), V) * (int)sizeof(T);
+      ptx::cp_async_zfill<BYTES>(ptx::smem_u32(slot) + i * BYTES, row + (left ? c : 0), left);
+    }
+  } else {
+    Unit<T, V> u;
+    u.load(row, c0, lane, cols, false);
+    *static_cast<Held<T>*>(slot) = u;
+  }
+}
+
 // Rows blockIdx.x + i gridDim.x; each lane keeps its columns' sums of dgamma in
-// registers over the block's rows, so that dy and h are read once.  With one
-// warp a row the block's warps take rows of their own and join their sums in
-// shared memory ([warps][cols]).
+// registers over the block's rows, so that dy and h are read once.  The rows
+// to come are on their way into shared memory (`depth` rows, each thread its
+// own values, so that no barrier is needed) while this one is worked on.  With
+// one warp a row the block's warps take rows of their own and join their sums
+// in shared memory ([warps][cols]).
 template <typename T, int V, int NU>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a) {
-  extern __shared__ float joined[];
+  extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ float part[2][kMaxWarps];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const bool own = a.warps == 1;  // a warp a row
   const int warp = own ? 0 : w, team = own ? w : 0, teams = own ? blockDim.x >> 5 : 1;
   const int c0 = warp * NU * UNIT;
-  float acc[NU][4];
+  const int arrays = a.dh ? 3 : 2;
+  using Slot = Held<T>;
+  Slot* const slots = reinterpret_cast<Slot*>(dyn) + threadIdx.x;
+  auto slot = [&](int stage, int array, int i) { return slots + ((stage * arrays + array) * NU + i) * (int)blockDim.x; };
+  const long long step = (long long)gridDim.x * teams;
+  long long ahead = (long long)blockIdx.x * teams + team;
+  auto issue = [&](int stage) {
+    if (ahead < a.rows) {
 #pragma unroll
-  for (int i = 0; i < NU; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
-  int turn = 0;
-  for (long long row = (long long)blockIdx.x * teams + team; row < a.rows; row += (long long)gridDim.x * teams, turn ^= 1) {
-    Unit<T, V> h[NU], d[NU];
-    const float rstd = __ldg(a.rstd + row);
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      h[i].load(a.h + row * a.ldh, c0 + i * UNIT, lane, a.cols);
-      d[i].load(a.dy + row * a.lddy, c0 + i * UNIT, lane, a.cols);
-    }
-    float dot = 0.f;
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      float x[4], y[4], g[4];
-      h[i].values(x);
-      d[i].values(y);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float yn = y[e] * (x[e] * rstd);
-        acc[i][e] += yn;
-        dot += yn * g[e];
+      for (int i = 0; i < NU; ++i) {
+        fetch<T, V>(slot(stage, 0, i), a.h + ahead * a.ldh, c0 + i * UNIT, lane, a.cols);
+        fetch<T, V>(slot(stage, 1, i), a.dy + ahead * a.lddy, c0 + i * UNIT, lane, a.cols);
+        if (a.dh) fetch<T, V>(slot(stage, 2, i), a.dh + ahead * a.lddh, c0 + i * UNIT, lane, a.cols);
       }
     }
-    dot = row_sum(dot, a.warps, warp, lane, part[turn]) / (float)a.cols;
-    if (!a.dx) continue;
+    ahead += step;
+    ptx::cp_async_commit();
+  };
+  uint64_t acc[NU][2];
+#pragma unroll
+  for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
+  for (int d = 0; d < a.depth; ++d) issue(d);
+  int turn = 0, stage = 0;
+  for (long long row = (long long)blockIdx.x * teams + team; row < a.rows; row += step, turn ^= 1) {
+    const float rstd = __ldg(a.rstd + row);
+    if (a.depth >= 4) ptx::cp_async_wait<3>();
+    else if (a.depth == 3) ptx::cp_async_wait<2>();
+    else if (a.depth == 2) ptx::cp_async_wait<1>();
+    else ptx::cp_async_wait<0>();
+    uint64_t dot2 = 0;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      if (c0 + i * UNIT >= a.cols) break;
-      float x[4], y[4], g[4];
-      h[i].values(x);
-      d[i].values(y);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide);
+      uint64_t x[2], y[2], g[2];
+      slot(stage, 0, i)->pairs(x);
+      slot(stage, 1, i)->pairs(y);
+      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, false);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = rstd * (g[e] * y[e] - (x[e] * rstd) * dot);
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t yn = ptx::mul2(y[e], ptx::mul2(x[e], both(rstd)));
+        acc[i][e] = ptx::add2(acc[i][e], yn);
+        ptx::fma2_to(dot2, yn, g[e]);
+      }
+    }
+    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) / (float)a.cols;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      if (!a.dx || c0 + i * UNIT >= a.cols) break;
+      uint64_t x[2], y[2], g[2];
+      slot(stage, 0, i)->pairs(x);
+      slot(stage, 1, i)->pairs(y);
+      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, false);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        x[e] = ptx::mul2(both(rstd), ptx::fma2(ptx::mul2(x[e], both(rstd)), both(-dot), ptx::mul2(g[e], y[e])));
       if (a.dh) {
-        Unit<T, V> t;
-        t.load(a.dh + row * a.lddh, c0 + i * UNIT, lane, a.cols);
-        t.values(y);
+        slot(stage, 2, i)->pairs(y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += y[e];
+        for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
       }
       Unit<T, V> o;
       o.set(x);
-      o.store(a.dx + row * a.lddx, c0 + i * UNIT, lane, a.cols);
+      o.store(a.dx + row * a.lddx, c0 + i * UNIT, lane, a.cols, false);
     }
+    issue(stage);  // into the slots just read
+    if (++stage == a.depth) stage = 0;
   }
   if (!a.part) return;
   float* out = a.part + (long long)blockIdx.x * a.cols;
-  if (teams == 1) {
+  float* joined = reinterpret_cast<float*>(dyn);
+  if (teams > 1) __syncthreads();  // every warp is done with its slots
 #pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = c0 + i * UNIT + Unit<T, V>::col(e, lane);
-        if (c < a.cols) out[c] = acc[i][e];
-      }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < NU; ++i)
+  for (int i = 0; i < NU; ++i) {
+    const float2 f[2] = {ptx::unpack2(acc[i][0]), ptx::unpack2(acc[i][1])};
+    const float v[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = i * UNIT + Unit<T, V>::col(e, lane);
-      if (c < a.cols) joined[team * a.cols + c] = acc[i][e];
+      const int c = c0 + i * UNIT + Unit<T, V>::col(e, lane);
+      if (c < a.cols) (teams > 1 ? joined + team * a.cols : out)[c] = v[e];
     }
+  }
+  if (teams == 1) return;
   __syncthreads();
   for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
     float s = joined[c];
@@ -346,7 +465,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a
 }
 
 // Rows too long for registers, in two passes: <du n> of each row, then its
-// terms by strips of 32 x UNIT columns.
+// terms by strips of 8 x UNIT columns.
 template <typename T, int V>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_dot(const GradArgs<T> a, float* dots) {
   __shared__ float part[kMaxWarps];
@@ -354,20 +473,20 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_dot(const GradArgs<T> a,
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long row = blockIdx.x;
   const float rstd = __ldg(a.rstd + row);
-  float dot = 0.f;
+  uint64_t dot = 0;
   for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
     Unit<T, V> h, d;
-    float x[4], y[4], g[4];
-    h.load(a.h + row * a.ldh, (int)c, lane, a.cols);
-    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols);
-    h.values(x);
-    d.values(y);
-    gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide);
+    uint64_t x[2], y[2], g[2];
+    h.load(a.h + row * a.ldh, (int)c, lane, a.cols, false);
+    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols, false);
+    h.pairs(x);
+    d.pairs(y);
+    gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide, false);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dot += y[e] * (x[e] * rstd) * g[e];
+    for (int e = 0; e < 2; ++e) ptx::fma2_to(dot, ptx::mul2(y[e], ptx::mul2(x[e], both(rstd))), g[e]);
   }
-  dot = row_sum(dot, kMaxWarps, warp, lane, part);
-  if (threadIdx.x == 0) dots[row] = dot / (float)a.cols;
+  const float sum = row_sum(sum_of(dot), kMaxWarps, warp, lane, part);
+  if (threadIdx.x == 0) dots[row] = sum / (float)a.cols;
 }
 // Block (strip, rows blockIdx.y + i gridDim.y): a warp a unit.
 template <typename T, int V>
@@ -376,38 +495,40 @@ __global__ void __launch_bounds__(8 * 32) k_rms_strip(const GradArgs<T> a, const
   const int lane = threadIdx.x & 31;
   const long long c = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * UNIT;
   if (c >= a.cols) return;
-  float g[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
-  gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide);
+  uint64_t g[2], acc[2] = {0, 0};
+  gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide, false);
 #pragma unroll 4
   for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const float rstd = __ldg(a.rstd + row), dot = dots ? dots[row] : 0.f;
     Unit<T, V> h, d;
-    float x[4], y[4];
-    h.load(a.h + row * a.ldh, (int)c, lane, a.cols);
-    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols);
-    h.values(x);
-    d.values(y);
+    uint64_t x[2], y[2];
+    h.load(a.h + row * a.ldh, (int)c, lane, a.cols, false);
+    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols, false);
+    h.pairs(x);
+    d.pairs(y);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float n = x[e] * rstd;
-      acc[e] += y[e] * n;
-      x[e] = rstd * (g[e] * y[e] - n * dot);
+    for (int e = 0; e < 2; ++e) {
+      const uint64_t n = ptx::mul2(x[e], both(rstd));
+      ptx::fma2_to(acc[e], y[e], n);
+      x[e] = ptx::mul2(both(rstd), ptx::fma2(n, both(-dot), ptx::mul2(g[e], y[e])));
     }
     if (!a.dx) continue;
     if (a.dh) {
-      d.load(a.dh + row * a.lddh, (int)c, lane, a.cols);
-      d.values(y);
+      d.load(a.dh + row * a.lddh, (int)c, lane, a.cols, false);
+      d.pairs(y);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] += y[e];
+      for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
     }
     h.set(x);
-    h.store(a.dx + row * a.lddx, (int)c, lane, a.cols);
+    h.store(a.dx + row * a.lddx, (int)c, lane, a.cols, false);
   }
   if (a.part) {
+    const float2 f[2] = {ptx::unpack2(acc[0]), ptx::unpack2(acc[1])};
+    const float v[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int k = (int)c + Unit<T, V>::col(e, lane);
-      if (k < a.cols) a.part[(long long)blockIdx.y * a.cols + k] = acc[e];
+      if (k < a.cols) a.part[(long long)blockIdx.y * a.cols + k] = v[e];
     }
   }
 }
@@ -492,26 +613,37 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
   return FF_OK;
 }
 
-// Blocks of the gradient kernels along the rows: about two rounds' worth of
-// warps for the GPU, and at most kGradRows rows a thread.
+// The gradient's blocks: as many an SM as 1024 threads and two rows of shared
+// memory each allow, and at most kGradRows rows a thread; the rest of the
+// shared memory deepens the queue of rows on their way (depth 0: none fits).
+// (Sized for three arrays whether dh is there or not, so that the workspace
+// does not depend on it.)
+constexpr int kGradSmem = 200 * 1024;
 struct GradPlan {
-  int nu, warps, teams, blocks;
+  int nu, warps, teams, blocks, depth;
 };
-GradPlan grad_plan(int rows, int cols) {
+GradPlan grad_plan(int rows, int cols, int esize) {
   GradPlan p{};
   p.nu = units_per_warp(rows, cols, kGradUnits);
   const int units = cdiv(cols, UNIT);
   p.warps = p.nu ? cdiv(units, p.nu) : kMaxWarps;
   p.teams = p.nu && p.warps == 1 ? kOwnRows : 1;
-  const long long per = p.nu ? (long long)p.warps * p.teams : units;  // warps along the columns
-  const long long fill = 152ll * 32 / per < 1 ? 1 : 152ll * 32 / per;
   const long long sets = cdiv(rows, p.teams), least = cdiv(sets, kGradRows);
+  long long fill;
+  if (p.nu) {
+    const int threads = p.warps * p.teams * 32, stage = threads * p.nu * 4 * esize * 3;
+    const int room = std::max(1, std::min(1024 / threads, kGradSmem / (2 * stage)));
+    p.depth = std::max(1, std::min(4, kGradSmem / (room * stage)));
+    fill = 152ll * room;
+  } else {
+    fill = std::max(1, 152 * 32 / units);
+  }
   p.blocks = (int)(sets < fill ? sets : fill < least ? least : fill);
   if (!p.nu && p.blocks > 65535) p.blocks = 65535;
   return p;
 }
-long long grad_bytes(int rows, int cols) {
-  const GradPlan p = grad_plan(rows, cols);
+long long grad_bytes(int rows, int cols, int esize) {
+  const GradPlan p = grad_plan(rows, cols, esize);
   const long long part = p.blocks > 1 ? 4ll * p.blocks * cols : 0;
   return ((part + 15) & ~15ll) + (p.nu ? 0 : 4ll * rows);
 }
@@ -520,8 +652,9 @@ template <typename T>
 ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
   using P = std::pair<const void*, long long>;
   const int v = vector_of<T>(P{a.dy, a.lddy}, P{a.h, a.ldh}, P{a.dh, a.lddh}, P{a.dx, a.lddx});
-  const GradPlan p = grad_plan(a.rows, a.cols);
+  const GradPlan p = grad_plan(a.rows, a.cols, (int)sizeof(T));
   a.warps = p.warps;
+  a.depth = p.depth;
   a.wide = wide_of(a.gamma);
   a.part = !dgamma ? nullptr : p.blocks > 1 ? static_cast<float*>(ws) : dgamma;
   const double count = (double)a.rows * a.cols;
@@ -529,12 +662,18 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
   if (p.nu) {
     auto go = [&]() -> cudaError_t {
       return with_vector<T>(v, [&](auto V) {
-        const size_t smem = p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0;
-        PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)(p.teams > 1 ? p.teams : p.warps) * 32), st, smem);
+        const int threads = p.teams * p.warps * 32;
+        const size_t ring = (size_t)p.depth * (a.dh ? 3 : 2) * p.nu * threads * 4 * sizeof(T);
+        const size_t smem = std::max(ring, p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0);
+        PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)threads), st, smem);
+        auto go = [&](auto N) -> cudaError_t {
+          const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value>>(kGradSmem);
+          return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value>, a);
+        };
         switch (p.nu) {
-          case 1: return cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, 1>, a);
-          case 2: return cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, 2>, a);
-          default: return cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, 4>, a);
+          case 1: return go(std::integral_constant<int, 1>{});
+          case 2: return go(std::integral_constant<int, 2>{});
+          default: return go(std::integral_constant<int, 4>{});
         }
       });
     };
@@ -617,7 +756,7 @@ extern "C" FF_API ff_status ff_rms_norm(const void* x, long long ldx, const void
 
 extern "C" FF_API long long ff_rms_norm_workspace(int rows, int cols) {
   if (rows < 0 || cols < 1 || cols > 0x7FFFFF00) return -1;
-  return rows == 0 ? 0 : grad_bytes(rows, cols);
+  return rows == 0 ? 0 : std::max(grad_bytes(rows, cols, 2), grad_bytes(rows, cols, 4));
 }
 
 extern "C" FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy, const void* h, long long ldh, int rows,
@@ -633,7 +772,7 @@ extern "C" FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy,
     return FF_OK;
   }
   const int es = prec == FF_BF16 ? 2 : 4;
-  const long long need = grad_bytes(rows, cols);
+  const long long need = ff_rms_norm_workspace(rows, cols);
   if (!dy || !h || !rstd || !matrix_ok(dy, lddy, rows, cols, es) || !matrix_ok(h, ldh, rows, cols, es) ||
       !matrix_ok(dh, lddh, rows, cols, es) || !matrix_ok(dx, lddx, rows, cols, es) || !aligned(rstd, 4) ||
       !aligned(gamma, 4) || (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))))
