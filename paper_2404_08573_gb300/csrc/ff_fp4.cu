@@ -17,11 +17,19 @@ namespace {
 // its own exponent field and at least 2^-127 (field 0, also for a block of
 // zeros).  255 marks a block that holds an infinity or a NaN.
 __device__ __forceinline__ uint32_t scale_field(uint32_t field) { return field == 255u ? 255u : field < 2u ? 0u : field - 2u; }
-// 1 / scale: 2^(127 - field), exact in fp32 for every field but the mark.
-__device__ __forceinline__ float scale_inverse(uint32_t field) { return __uint_as_float((field > 253u ? 1u : 254u - field) << 23); }
+// 1 / scale: 2^(127 - field), exact in fp32 (for the mark -infinity: whatever the
+// block's codes are then, it stands for NaN).
+__device__ __forceinline__ float scale_inverse(uint32_t field) { return __uint_as_float((254u - field) << 23); }
 
-// Eight values as e2m1 codes (to nearest even, saturating), the first lowest.
-__device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8]) {
+// Four pairs times f as e2m1 codes (to nearest even, saturating), the first lowest.
+__device__ __forceinline__ uint32_t e2m1x8(const uint64_t (&p)[4], float f) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = ptx::unpack2(ptx::mul2(p[i], ptx::pack2(f, f)));
+    v[2 * i] = t.x;
+    v[2 * i + 1] = t.y;
+  }
   uint32_t r;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -61,6 +69,9 @@ struct Eight<bf16> {
     return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }
   static __device__ __forceinline__ uint32_t field(uint32_t w, int h) { return h ? w >> 23 : (w >> 7) & 0xFFu; }  // of a magnitude
+  static __device__ __forceinline__ uint64_t pair(const uint32_t (&w)[WORDS], int i) {  // values 2i, 2i + 1
+    return ptx::pack2(w[i] << 16, w[i] & 0xFFFF0000u);
+  }
 };
 template <>
 struct Eight<float> {
@@ -69,6 +80,7 @@ struct Eight<float> {
   static __device__ __forceinline__ uint32_t max_of(uint32_t a, uint32_t b) { return max(a, b); }
   static __device__ __forceinline__ float value(const uint32_t (&w)[WORDS], int e) { return __uint_as_float(w[e]); }
   static __device__ __forceinline__ uint32_t field(uint32_t w, int) { return w >> 23; }
+  static __device__ __forceinline__ uint64_t pair(const uint32_t (&w)[WORDS], int i) { return ptx::pack2(w[2 * i], w[2 * i + 1]); }
 };
 
 constexpr int QT = 128;  // a tile: 128 x 128 values, one scale tile each way
@@ -122,6 +134,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
       }
   }
   if (q) {
+    uint8_t* const to = q + (long long)row0 * ldq + c0 / 2;
     uint32_t m[8 / PER];  // word j: rows j PER .. (one per half of the word)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -142,12 +155,11 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t f = scale_field(E::field(m[i / PER], i % PER));
-      const float inv = scale_inverse(f);
-      float y[8];
+      uint64_t y[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = __fmul_rn(E::value(v[i], e), inv);
+      for (int e = 0; e < 4; ++e) y[e] = E::pair(v[i], e);
       // ldq covers whole blocks of 32: eight columns lie inside or outside
-      if (row0 + i < rows && c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(q + (long long)(row0 + i) * ldq + c0 / 2) = e2m1x8(y);
+      if (row0 + i < rows && c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(to + (long long)i * ldq) = e2m1x8(y, scale_inverse(f));
       if ((cg & 3) == 0) sc[(rg * 8 + i) * 16 + wr * 4 + wc * 2 + (cg >> 2)] = (uint8_t)f;
     }
   }
@@ -166,12 +178,11 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t f = scale_field(E::field(m[e / PER], e % PER));
-      const float inv = scale_inverse(f);
-      float y[8];
+      uint64_t y[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(E::value(v[i], e), inv);
+      for (int i = 0; i < 4; ++i) y[i] = ptx::pack2(E::value(v[2 * i], e), E::value(v[2 * i + 1], e));
       const int c = c_in + e;
-      tq[c * kPitch + wr * 4 + rg] = e2m1x8(y);
+      tq[c * kPitch + wr * 4 + rg] = e2m1x8(y, scale_inverse(f));
       if (rg == 0) sct[(c & 31) * 16 + (c >> 5) * 4 + wr] = (uint8_t)f;
     }
   }
@@ -196,59 +207,141 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
   }
 }
 
+// The rows alone: a lane takes eight values of a row at a time (four lanes a
+// block of 32), so a warp 256 columns, kRowsAhead rows of them with their loads in
+// flight together.  Bound by HBM: x once, its half-bytes once.
+constexpr int kRowsAhead = 4;
+template <typename T, int LOAD>
+__global__ void __launch_bounds__(kQThreads)
+    k_fp4_rows(const T* x, long long ldx, int rows, int k, uint8_t* q, uint8_t* scale, int ldq, int ktiles, int strips) {
+  using E = Eight<T>;
+  constexpr int W = E::WORDS, PER = E::PER;
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & 31;
+  const long long unit = (long long)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5);  // strip of 256 columns, rows
+  const int strip = (int)(unit % strips);
+  const long long row0 = unit / strips * kRowsAhead;
+  if (row0 >= rows) return;
+  const int c0 = strip * 256 + lane * 8;
+  const int n = (int)min((long long)kRowsAhead, rows - row0);
+  uint32_t v[kRowsAhead][W];
+#pragma unroll
+  for (int i = 0; i < kRowsAhead; ++i) {
+    const T* p = x + (row0 + i) * ldx + c0;
+    if (LOAD == 16 && c0 + 8 <= k) {
+#pragma unroll
+      for (int j = 0; j < W / 4; ++j)
+        *reinterpret_cast<uint4*>(&v[i][4 * j]) = i < n ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
+    } else if (LOAD == 4 && c0 + 8 <= k) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i][j] = i < n ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int h = 0; h < PER; ++h)
+          if (i < n && c0 + j * PER + h < k) w |= (uint32_t)Vec<T, 1>::load(p + j * PER + h) << (16 * h);
+        v[i][j] = w;
+      }
+    }
+  }
+  const int tile = strip * 2 + (lane >> 4);  // of 128 columns, along k
+#pragma unroll
+  for (int i = 0; i < kRowsAhead; ++i) {
+    if (i >= n) break;
+    const int row = (int)row0 + i;
+    uint32_t m = v[i][0] & E::ABS;
+#pragma unroll
+    for (int j = 1; j < W; ++j) m = E::max_of(m, v[i][j] & E::ABS);
+    if constexpr (PER == 2) m = max(m & 0xFFFFu, m >> 16);
+#pragma unroll
+    for (int o = 1; o <= 2; o *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const uint32_t f = scale_field(E::field(m, 0));
+    uint64_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = E::pair(v[i], e);
+    if (c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(q + (long long)row * ldq + c0 / 2) = e2m1x8(y, scale_inverse(f));
+    // the tile's four blocks' bytes of this row, to its first lane
+    uint32_t s = f | __shfl_down_sync(0xffffffffu, f, 4) << 8;
+    s |= __shfl_down_sync(0xffffffffu, s, 8) << 16;
+    if ((lane & 15) == 0 && tile < ktiles)
+      *reinterpret_cast<uint32_t*>(scale + ((long long)(row >> 7) * ktiles + tile) * kFp4ScaleTile + (row & 31) * 16 +
+                                   (row >> 5 & 3) * 4) = s;
+  }
+  // who has the last row clears the rows that fill its tiles up
+  if (row0 + n == rows && tile < ktiles)
+    for (int row = rows + (lane & 15); row >> 7 == (rows - 1) >> 7; row += 16)
+      *reinterpret_cast<uint32_t*>(scale + ((long long)(row >> 7) * ktiles + tile) * kFp4ScaleTile + (row & 31) * 16 +
+                                   (row >> 5 & 3) * 4) = 0u;
+}
+
 __device__ __forceinline__ float scale_value(uint32_t field) {  // 2^(field - 127)
   return __uint_as_float(field == 0u ? 0x00400000u : field == 255u ? 0x7FC00000u : field << 23);
 }
-__device__ __forceinline__ uint32_t scale_at(const uint8_t* scale, int ktiles, int row, int block) {
-  return __ldg(scale + ((long long)(row >> 7) * ktiles + (block >> 2)) * kFp4ScaleTile + (row & 31) * 16 + (row >> 5 & 3) * 4 +
-               (block & 3));
-}
 
-// y = value * scale, exact in either type.  WIDE: y's rows are 16-byte aligned,
-// and a thread takes 8 values (4 bytes) at a time; else one, the lanes side by
-// side.
+// y = value * scale, exact in either type.  A block of 256 threads covers
+// `lanes` units of a row's columns side by side and 4 * 256 / lanes rows, a
+// thread four of them with their loads in flight together.  WIDE: y's rows
+// are 16-byte aligned and a unit is 8 columns; else one column.
+constexpr int kDeqRows = 4;
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256)
-    k_fp4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int k, int ldq, int ktiles, T* y, long long ldy,
-                     int per_row) {
+    k_fp4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int k, int ldq, int ktiles, T* y, long long ldy, int lanes_log,
+                     int strips) {
   ptx::griddep_wait();
-  const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;  // a row's units of 8 columns, 32-bit words of q
-  if constexpr (WIDE) {
-    const long long r = unit / per_row;
-    if (r >= rows) return;
-    const int c = (int)(unit - r * per_row) * 8;
-    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(q + r * ldq + c / 2));
-    const float s = scale_value(scale_at(scale, ktiles, (int)r, c / kFp4Block));
-    float v[8];
+  const int lanes = 1 << lanes_log, per = 256 >> lanes_log;
+  const int strip = blockIdx.x % strips;
+  const long long row0 = (long long)(blockIdx.x / strips) * (kDeqRows * per) + (threadIdx.x >> lanes_log);
+  const long long unit = (long long)strip * lanes + (threadIdx.x & (lanes - 1));
+  const long long c = WIDE ? unit * 8 : unit;
+  if (c >= k) return;
+  uint32_t w[kDeqRows], f[kDeqRows];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = e2m1x2_values(w >> (8 * i));
-      v[2 * i] = f.x * s;
-      v[2 * i + 1] = f.y * s;
+  for (int i = 0; i < kDeqRows; ++i) {
+    const long long r = row0 + i * per;
+    w[i] = f[i] = 0u;
+    if (r < rows) {
+      const uint8_t* p = q + r * ldq + c / 2;
+      w[i] = WIDE ? __ldg(reinterpret_cast<const uint32_t*>(p)) : (uint32_t)__ldg(p);
+      f[i] = __ldg(scale + ((r >> 7) * ktiles + c / QT) * kFp4ScaleTile + (r & 31) * 16 + (r >> 5 & 3) * 4 + (c / kFp4Block & 3));
     }
+  }
+#pragma unroll
+  for (int i = 0; i < kDeqRows; ++i) {
+    const long long r = row0 + i * per;
+    if (r >= rows) break;
+    const float s = scale_value(f[i]);
     T* to = y + r * ldy + c;
-    if (c + 8 <= k) {
+    if constexpr (WIDE) {
+      float v[8];
 #pragma unroll
-      for (int h = 0; h < 8; h += 16 / (int)sizeof(T)) {
-        float t[16 / sizeof(T)];
+      for (int j = 0; j < 4; ++j) {
+        const float2 t = e2m1x2_values(w[i] >> (8 * j));
+        v[2 * j] = t.x * s;
+        v[2 * j + 1] = t.y * s;
+      }
+      if (c + 8 <= k) {
+        constexpr int N = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int e = 0; e < 16 / (int)sizeof(T); ++e) t[e] = v[h + e];
-        Vec<T, 16 / (int)sizeof(T)>::store(to + h, t);
+        for (int h = 0; h < 8; h += N) {
+          float t[N];
+#pragma unroll
+          for (int e = 0; e < N; ++e) t[e] = v[h + e];
+          Vec<T, N>::store(to + h, t);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float one[1] = {v[e]};
+          if (c + e < k) Vec<T, 1>::store(to + e, one);
+        }
       }
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float one[1] = {v[e]};
-        if (c + e < k) Vec<T, 1>::store(to + e, one);
-      }
+      const float2 t = e2m1x2_values(w[i]);
+      const float one[1] = {(c & 1 ? t.y : t.x) * s};
+      Vec<T, 1>::store(to, one);
     }
-  } else {
-    const long long r = unit / per_row;  // units of one column, padded to whole warps
-    const int c = (int)(unit - r * per_row);
-    if (r >= rows || c >= k) return;
-    const float2 f = e2m1x2_values(__ldg(q + r * ldq + c / 2));
-    const float one[1] = {(c & 1 ? f.y : f.x) * scale_value(scale_at(scale, ktiles, (int)r, c / kFp4Block))};
-    Vec<T, 1>::store(y + r * ldy + c, one);
   }
 }
 
@@ -260,13 +353,22 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, uint8_t* q, uin
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)rows * k * (sizeof(T) + (q ? 0.5 : 0) + (qt ? 0.5 : 0));
   const int ldq = fp4_stride(k), ldqt = fp4_stride(rows);
+  const int load = rows_aligned(x, ldx, sizeof(T), 16) ? 16 : rows_aligned(x, ldx, sizeof(T), 4) ? 4 : (int)sizeof(T);
+  if (!qt) {
+    const int strips = cdiv(k, 256);
+    const long long units = (long long)strips * cdiv(rows, kRowsAhead), grid = (units + kQThreads / 32 - 1) / (kQThreads / 32);
+    if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+    auto* const rows_kernel = load == 16 ? k_fp4_rows<T, 16> : load == 4 ? k_fp4_rows<T, 4> : k_fp4_rows<T, sizeof(T)>;
+    PdlLaunch l(dim3((unsigned)grid), dim3(kQThreads), st);
+    FF_LAUNCH(K_FP4_QUANT, bytes, st, cudaLaunchKernelEx(&l.cfg, rows_kernel, x, ldx, rows, k, q, scale, ldq, ktiles, strips),
+              "4-bit quantize");
+    return FF_OK;
+  }
   PdlLaunch l(dim3((unsigned)blocks), dim3(kQThreads), st);
   auto go = [&](auto* kernel) {
     return cudaLaunchKernelEx(&l.cfg, kernel, x, ldx, rows, k, q, scale, qt, scale_t, ldq, ldqt, ktiles, rtiles);
   };
-  auto* const kernel = rows_aligned(x, ldx, sizeof(T), 16)  ? k_fp4_quantize<T, 16>
-                       : rows_aligned(x, ldx, sizeof(T), 4) ? k_fp4_quantize<T, 4>
-                                                            : k_fp4_quantize<T, sizeof(T)>;
+  auto* const kernel = load == 16 ? k_fp4_quantize<T, 16> : load == 4 ? k_fp4_quantize<T, 4> : k_fp4_quantize<T, sizeof(T)>;
   FF_LAUNCH(K_FP4_QUANT, bytes, st, go(kernel), "4-bit quantize");
   return FF_OK;
 }
@@ -274,13 +376,16 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, uint8_t* q, uin
 template <typename T>
 ff_status dequantize_t(const uint8_t* q, const uint8_t* scale, int rows, int k, T* y, long long ldy, cudaStream_t st) {
   const bool wide = rows_aligned(y, rows > 1 ? ldy : 0, sizeof(T), 16);
-  const int per_row = wide ? cdiv(k, 8) : cdiv(k, 32) * 32;
-  const long long blocks = ((long long)rows * per_row + 255) / 256;
+  const int units = wide ? cdiv(k, 8) : k;
+  int lanes_log = 3;
+  while (lanes_log < 8 && (1 << lanes_log) < units) ++lanes_log;
+  const int strips = cdiv(units, 1 << lanes_log);
+  const long long blocks = (long long)strips * cdiv(rows, kDeqRows * (256 >> lanes_log));
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)rows * k * (sizeof(T) + 0.5);
   PdlLaunch l(dim3((unsigned)blocks), dim3(256), st);
   auto go = [&](auto* kernel) {
-    return cudaLaunchKernelEx(&l.cfg, kernel, q, scale, rows, k, fp4_stride(k), cdiv(k, QT), y, ldy, per_row);
+    return cudaLaunchKernelEx(&l.cfg, kernel, q, scale, rows, k, fp4_stride(k), cdiv(k, QT), y, ldy, lanes_log, strips);
   };
   auto* const kernel = wide ? k_fp4_dequantize<T, true> : k_fp4_dequantize<T, false>;
   FF_LAUNCH(K_FP4_DEQUANT, bytes, st, go(kernel), "4-bit dequantize");

@@ -457,18 +457,30 @@ struct GradArgs {
   int segments;  // segments a row is cut into
 };
 
-// What a row's gradient needs, and one value of it.
+// What a row's gradient needs: dx = -p (k + g' d) with d = x - m,
+// p = e^(d - ln s) and k = g + g' (entropy - ln s); the label's class adds g.
 struct Row {
-  float m, ln, scale, g, ge, h;
+  float m, ln, scale, g, ge, k;
   int label;
 };
+// bf16: one approximate exponential, whose argument's rounding is far below the
+// result's.  fp32: the full one, e^d / s.
 template <typename T>
-__device__ __forceinline__ float grad_of(const Row& r, float x, int c) {
-  const float d = max_nan(x - r.m, kFar);
-  const float p = (sizeof(T) == 4 ? expf(d) : exp2_approx(d * kLog2e)) * r.scale;
-  float v = -p * (r.g + r.ge * (d - r.ln + r.h));
-  if (c == r.label) v += r.g;
-  return v;
+__device__ __forceinline__ uint64_t grad_of(const Row& r, uint64_t x) {
+  float2 d = ptx::unpack2(ptx::add2(x, ptx::pack2(-r.m, -r.m)));
+  d.x = max_nan(d.x, kFar);
+  d.y = max_nan(d.y, kFar);
+  const uint64_t d2 = ptx::pack2(d.x, d.y);
+  uint64_t p;
+  if constexpr (sizeof(T) == 4) {
+    p = ptx::mul2(ptx::pack2(expf(d.x), expf(d.y)), ptx::pack2(-r.scale, -r.scale));
+    return ptx::mul2(p, ptx::fma2(d2, ptx::pack2(r.ge, r.ge), ptx::pack2(r.k, r.k)));
+  } else {
+    const float l = -r.ln * kLog2e;
+    const float2 e = ptx::unpack2(ptx::fma2(d2, ptx::pack2(kLog2e, kLog2e), ptx::pack2(l, l)));
+    p = ptx::pack2(exp2_approx(e.x), exp2_approx(e.y));
+    return ptx::mul2(p, ptx::fma2(d2, ptx::pack2(-r.ge, -r.ge), ptx::pack2(-r.k, -r.k)));
+  }
 }
 
 // WIDE: both rows lie alike to 16 bytes, and all but their ends go as vectors.
@@ -492,13 +504,16 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(const GradArgs<T> a) {
   if (r.label >= a.classes) r.label = -1;
   r.g = a.dlogp && r.label >= 0 ? __ldg(a.dlogp + row) : 0.f;
   r.ge = a.dentropy ? __ldg(a.dentropy + row) : 0.f;
-  r.h = a.dentropy ? __ldg(a.entropy + row) : 0.f;
+  r.k = a.dentropy ? r.g + r.ge * (__ldg(a.entropy + row) - st.y) : r.g;
   const bool zero = r.g == 0.f && r.ge == 0.f;  // nothing asked of the row: zeros, whatever it holds
+  auto put = [&](int c, float x) {
+    const float v[1] = {zero ? 0.f : ptx::unpack2(grad_of<T>(r, ptx::pack2(x, r.m))).x + (c == r.label ? r.g : 0.f)};
+    Vec<T, 1>::store(out + c, v);
+  };
   auto one = [&](int c) {
     float v[1];
     Vec<T, 1>::unpack(Vec<T, 1>::load(p + c), v);
-    v[0] = zero ? 0.f : grad_of<T>(r, v[0], c);
-    Vec<T, 1>::store(out + c, v);
+    put(c, v[0]);
   };
   if constexpr (WIDE) {
     const int off = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T) % N);
@@ -506,18 +521,52 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(const GradArgs<T> a) {
     const int v0 = (int)((long long)vecs * seg / a.segments), v1 = (int)((long long)vecs * (seg + 1) / a.segments);
     if (seg == 0 && tid < head) one(tid);
     if (seg == a.segments - 1 && head + vecs * N + tid < a.classes) one(head + vecs * N + tid);
-#pragma unroll 4
-    for (int i = v0 + tid; i < v1; i += a.team) {
-      float v[N];
-      Vec<T, N>::unpack(Vec<T, N>::load(p + head + (long long)i * N), v);
+    const uint4* src = reinterpret_cast<const uint4*>(p + head);
+    uint4* dst = reinterpret_cast<uint4*>(out + head);
+    if (zero) {
+      for (int i = v0 + tid; i < v1; i += a.team) dst[i] = make_uint4(0, 0, 0, 0);
+      return;
+    }
+    const int at = r.label - head, there = at >= 0 ? at / N : -1;  // the label's vector
+    for (int i0 = v0 + tid; i0 < v1; i0 += 4 * a.team) {
+      uint4 raw[4];  // loaded together (the stores may be to the same memory, so the compiler could not)
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = zero ? 0.f : grad_of<T>(r, v[e], head + i * N + e);
-      Vec<T, N>::store(out + head + (long long)i * N, v);
+      for (int j = 0; j < 4; ++j)
+        if (i0 + j * a.team < v1) raw[j] = src[i0 + j * a.team];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + j * a.team;
+        if (i >= v1) break;
+        float v[N];
+        Vec<T, N>::unpack(raw[j], v);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+          const float2 f = ptx::unpack2(grad_of<T>(r, ptx::pack2(v[e], v[e + 1])));
+          v[e] = f.x;
+          v[e + 1] = f.y;
+        }
+        if (i == there) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[e] += at - i * N == e ? r.g : 0.f;
+        }
+        Vec<T, N>::store(reinterpret_cast<T*>(dst + i), v);
+      }
     }
   } else {
     const int c0 = (int)((long long)a.classes * seg / a.segments), c1 = (int)((long long)a.classes * (seg + 1) / a.segments);
-#pragma unroll 8
-    for (int c = c0 + tid; c < c1; c += a.team) one(c);
+    for (int b = c0 + tid; b < c1; b += 8 * a.team) {
+      typename Vec<T, 1>::Raw raw[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (b + j * a.team < c1) raw[j] = Vec<T, 1>::load(p + b + j * a.team);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (b + j * a.team >= c1) break;
+        float v[1];
+        Vec<T, 1>::unpack(raw[j], v);
+        put(b + j * a.team, v[0]);
+      }
+    }
   }
 }
 

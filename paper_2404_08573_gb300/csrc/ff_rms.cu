@@ -344,18 +344,18 @@ struct GradArgs {
 // Copies one lane's part of a unit to its own slot of shared memory, by the
 // bytes that the alignment allows (single bf16 values go through registers).
 template <typename T, int V>
-__device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane, int cols) {
+__device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane, int cols, bool whole) {
   if constexpr (sizeof(T) * V >= 4) {
     constexpr int BYTES = (int)sizeof(T) * V;
 #pragma unroll
     for (int i = 0; i < 4 / V; ++i) {
       const int c = c0 + Unit<T, V>::first(i, lane);
-      const int left = min(max(cols - c, 0), V) * (int)sizeof(T);
-      ptx::cp_async_zfill<BYTES>(ptx::smem_u32(slot) + i * BYTES, row + (left ? c : 0), left);
+      const int left = whole ? BYTES : min(max(cols - c, 0), V) * (int)sizeof(T);
+      ptx::cp_async_zfill<BYTES>(ptx::smem_u32(slot) + i * BYTES, row + (whole || left ? c : 0), left);
     }
   } else {
     Unit<T, V> u;
-    u.load(row, c0, lane, cols, false);
+    u.load(row, c0, lane, cols, whole);
     *static_cast<Held<T>*>(slot) = u;
   }
 }
@@ -367,6 +367,79 @@ __device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane
 // one warp a row the block's warps take rows of their own and join their sums
 // in shared memory ([warps][cols]).
 template <typename T, int V, int NU>
+__device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[NU][2], Held<T>* slots, int teams, int team, int warp,
+                                          int lane, float (*part)[kMaxWarps], bool whole) {
+  const int c0 = warp * NU * UNIT, arrays = a.dh ? 3 : 2, threads = (int)blockDim.x;
+  const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
+  const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
+  long long ahead = first;
+  auto issue = [&](Held<T>* to) {
+    if (ahead < a.rows) {
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        fetch<T, V>(to + i * threads, hp, c0 + i * UNIT, lane, a.cols, whole);
+        fetch<T, V>(to + (NU + i) * threads, dp, c0 + i * UNIT, lane, a.cols, whole);
+        if (a.dh) fetch<T, V>(to + (2 * NU + i) * threads, tp, c0 + i * UNIT, lane, a.cols, whole);
+      }
+      hp += step * a.ldh;
+      dp += step * a.lddy;
+      if (a.dh) tp += step * a.lddh;
+    }
+    ahead += step;
+    ptx::cp_async_commit();
+  };
+  const int stage = arrays * NU * threads;  // slots a row
+  for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
+  T* out = a.dx ? a.dx + first * a.lddx : nullptr;
+  int turn = 0, at = 0;
+  for (long long row = first; row < a.rows; row += step, turn ^= 1) {
+    const float rstd = __ldg(a.rstd + row);
+    if (a.depth >= 4) ptx::cp_async_wait<3>();
+    else if (a.depth == 3) ptx::cp_async_wait<2>();
+    else if (a.depth == 2) ptx::cp_async_wait<1>();
+    else ptx::cp_async_wait<0>();
+    Held<T>* now = slots + at * stage;
+    uint64_t dot2 = 0;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      uint64_t x[2], y[2], g[2];
+      now[i * threads].pairs(x);
+      now[(NU + i) * threads].pairs(y);
+      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t yh = ptx::mul2(y[e], x[e]);
+        ptx::fma2_to(acc[i][e], yh, both(rstd));
+        ptx::fma2_to(dot2, yh, g[e]);
+      }
+    }
+    // <du n> rstd^2, what h is to be taken off by
+    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) / (float)a.cols;
+    const uint64_t off = both(-dot * rstd * rstd * rstd);
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      if (!out || (!whole && c0 + i * UNIT >= a.cols)) break;
+      uint64_t x[2], y[2], g[2];
+      now[i * threads].pairs(x);
+      now[(NU + i) * threads].pairs(y);
+      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[e] = ptx::fma2(x[e], off, ptx::mul2(both(rstd), ptx::mul2(g[e], y[e])));
+      if (a.dh) {
+        now[(2 * NU + i) * threads].pairs(y);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+      }
+      Unit<T, V> o;
+      o.set(x);
+      o.store(out, c0 + i * UNIT, lane, a.cols, whole);
+    }
+    if (out) out += step * a.lddx;
+    issue(now);  // into the slots just read
+    if (++at == a.depth) at = 0;
+  }
+}
+template <typename T, int V, int NU>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a) {
   extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ float part[2][kMaxWarps];
@@ -375,72 +448,15 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a
   const bool own = a.warps == 1;  // a warp a row
   const int warp = own ? 0 : w, team = own ? w : 0, teams = own ? blockDim.x >> 5 : 1;
   const int c0 = warp * NU * UNIT;
-  const int arrays = a.dh ? 3 : 2;
-  using Slot = Held<T>;
-  Slot* const slots = reinterpret_cast<Slot*>(dyn) + threadIdx.x;
-  auto slot = [&](int stage, int array, int i) { return slots + ((stage * arrays + array) * NU + i) * (int)blockDim.x; };
-  const long long step = (long long)gridDim.x * teams;
-  long long ahead = (long long)blockIdx.x * teams + team;
-  auto issue = [&](int stage) {
-    if (ahead < a.rows) {
-#pragma unroll
-      for (int i = 0; i < NU; ++i) {
-        fetch<T, V>(slot(stage, 0, i), a.h + ahead * a.ldh, c0 + i * UNIT, lane, a.cols);
-        fetch<T, V>(slot(stage, 1, i), a.dy + ahead * a.lddy, c0 + i * UNIT, lane, a.cols);
-        if (a.dh) fetch<T, V>(slot(stage, 2, i), a.dh + ahead * a.lddh, c0 + i * UNIT, lane, a.cols);
-      }
-    }
-    ahead += step;
-    ptx::cp_async_commit();
-  };
   uint64_t acc[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
-  for (int d = 0; d < a.depth; ++d) issue(d);
-  int turn = 0, stage = 0;
-  for (long long row = (long long)blockIdx.x * teams + team; row < a.rows; row += step, turn ^= 1) {
-    const float rstd = __ldg(a.rstd + row);
-    if (a.depth >= 4) ptx::cp_async_wait<3>();
-    else if (a.depth == 3) ptx::cp_async_wait<2>();
-    else if (a.depth == 2) ptx::cp_async_wait<1>();
-    else ptx::cp_async_wait<0>();
-    uint64_t dot2 = 0;
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      uint64_t x[2], y[2], g[2];
-      slot(stage, 0, i)->pairs(x);
-      slot(stage, 1, i)->pairs(y);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, false);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint64_t yn = ptx::mul2(y[e], ptx::mul2(x[e], both(rstd)));
-        acc[i][e] = ptx::add2(acc[i][e], yn);
-        ptx::fma2_to(dot2, yn, g[e]);
-      }
-    }
-    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) / (float)a.cols;
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      if (!a.dx || c0 + i * UNIT >= a.cols) break;
-      uint64_t x[2], y[2], g[2];
-      slot(stage, 0, i)->pairs(x);
-      slot(stage, 1, i)->pairs(y);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, false);
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        x[e] = ptx::mul2(both(rstd), ptx::fma2(ptx::mul2(x[e], both(rstd)), both(-dot), ptx::mul2(g[e], y[e])));
-      if (a.dh) {
-        slot(stage, 2, i)->pairs(y);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
-      }
-      Unit<T, V> o;
-      o.set(x);
-      o.store(a.dx + row * a.lddx, c0 + i * UNIT, lane, a.cols, false);
-    }
-    issue(stage);  // into the slots just read
-    if (++stage == a.depth) stage = 0;
-  }
+  Held<T>* slots = reinterpret_cast<Held<T>*>(dyn) + threadIdx.x;
+  // (both calls meet at the same barriers)
+  if (c0 + NU * UNIT <= a.cols)
+    grad_rows<T, V, NU>(a, acc, slots, teams, team, warp, lane, part, true);
+  else
+    grad_rows<T, V, NU>(a, acc, slots, teams, team, warp, lane, part, false);
   if (!a.part) return;
   float* out = a.part + (long long)blockIdx.x * a.cols;
   float* joined = reinterpret_cast<float*>(dyn);
