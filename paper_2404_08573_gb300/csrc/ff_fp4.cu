@@ -208,49 +208,49 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2)
 }
 
 // The rows alone: a lane takes eight values of a row at a time (four lanes a
-// block of 32), so a warp 256 columns, kRowsAhead rows of them with their loads in
-// flight together.  Bound by HBM: x once, its half-bytes once.
-constexpr int kRowsAhead = 4;
+// block of 32), so a warp 256 columns: of rows j, j + 32, j + 64 and j + 96 of a
+// scale tile, with their loads in flight together, since these rows' scale bytes
+// lie side by side (rows one after the other: 3 us of 18 for 4-byte stores all
+// over the tiles, 4096 x 8192 bf16).  Rows past the matrix write zero scales.
+// Bound by HBM: x once, its half-bytes once.
 template <typename T, int LOAD>
 __global__ void __launch_bounds__(kQThreads)
-    k_fp4_rows(const T* x, long long ldx, int rows, int k, uint8_t* q, uint8_t* scale, int ldq, int ktiles, int strips) {
+    k_fp4_rows(const T* x, long long ldx, int rows, int k, uint8_t* q, uint8_t* scale, int ldq, int ktiles, int strips, int units) {
   using E = Eight<T>;
   constexpr int W = E::WORDS, PER = E::PER;
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31;
-  const long long unit = (long long)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5);  // strip of 256 columns, rows
-  const int strip = (int)(unit % strips);
-  const long long row0 = unit / strips * kRowsAhead;
-  if (row0 >= rows) return;
-  const int c0 = strip * 256 + lane * 8;
-  const int n = (int)min((long long)kRowsAhead, rows - row0);
-  uint32_t v[kRowsAhead][W];
+  const int unit = blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5);  // (row tile, j, strip of 256 columns)
+  if (unit >= units) return;
+  const int strip = unit % strips, rj = unit / strips, j0 = rj & 31, rt = rj >> 5;
+  const int row0 = rt * QT + j0, c0 = strip * 256 + lane * 8;
+  uint32_t v[4][W];
+  const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
-  for (int i = 0; i < kRowsAhead; ++i) {
-    const T* p = x + (row0 + i) * ldx + c0;
+  for (int i = 0; i < 4; ++i, p += 32 * ldx) {
+    const bool in = row0 + 32 * i < rows;
     if (LOAD == 16 && c0 + 8 <= k) {
 #pragma unroll
       for (int j = 0; j < W / 4; ++j)
-        *reinterpret_cast<uint4*>(&v[i][4 * j]) = i < n ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(&v[i][4 * j]) = in ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
     } else if (LOAD == 4 && c0 + 8 <= k) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[i][j] = i < n ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
+      for (int j = 0; j < W; ++j) v[i][j] = in ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
     } else {
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         uint32_t w = 0;
 #pragma unroll
         for (int h = 0; h < PER; ++h)
-          if (i < n && c0 + j * PER + h < k) w |= (uint32_t)Vec<T, 1>::load(p + j * PER + h) << (16 * h);
+          if (in && c0 + j * PER + h < k) w |= (uint32_t)Vec<T, 1>::load(p + j * PER + h) << (16 * h);
         v[i][j] = w;
       }
     }
   }
-  const int tile = strip * 2 + (lane >> 4);  // of 128 columns, along k
+  uint32_t s[4];
+  uint8_t* to = q + (long long)row0 * ldq + c0 / 2;
 #pragma unroll
-  for (int i = 0; i < kRowsAhead; ++i) {
-    if (i >= n) break;
-    const int row = (int)row0 + i;
+  for (int i = 0; i < 4; ++i, to += 32ll * ldq) {
     uint32_t m = v[i][0] & E::ABS;
 #pragma unroll
     for (int j = 1; j < W; ++j) m = E::max_of(m, v[i][j] & E::ABS);
@@ -261,19 +261,14 @@ __global__ void __launch_bounds__(kQThreads)
     uint64_t y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = E::pair(v[i], e);
-    if (c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(q + (long long)row * ldq + c0 / 2) = e2m1x8(y, scale_inverse(f));
+    if (row0 + 32 * i < rows && c0 / 2 < ldq) *reinterpret_cast<uint32_t*>(to) = e2m1x8(y, scale_inverse(f));
     // the tile's four blocks' bytes of this row, to its first lane
-    uint32_t s = f | __shfl_down_sync(0xffffffffu, f, 4) << 8;
-    s |= __shfl_down_sync(0xffffffffu, s, 8) << 16;
-    if ((lane & 15) == 0 && tile < ktiles)
-      *reinterpret_cast<uint32_t*>(scale + ((long long)(row >> 7) * ktiles + tile) * kFp4ScaleTile + (row & 31) * 16 +
-                                   (row >> 5 & 3) * 4) = s;
+    s[i] = f | __shfl_down_sync(0xffffffffu, f, 4) << 8;
+    s[i] |= __shfl_down_sync(0xffffffffu, s[i], 8) << 16;
   }
-  // who has the last row clears the rows that fill its tiles up
-  if (row0 + n == rows && tile < ktiles)
-    for (int row = rows + (lane & 15); row >> 7 == (rows - 1) >> 7; row += 16)
-      *reinterpret_cast<uint32_t*>(scale + ((long long)(row >> 7) * ktiles + tile) * kFp4ScaleTile + (row & 31) * 16 +
-                                   (row >> 5 & 3) * 4) = 0u;
+  const int tile = strip * 2 + (lane >> 4);  // of 128 columns, along k
+  if ((lane & 15) == 0 && tile < ktiles)
+    *reinterpret_cast<uint4*>(scale + ((long long)rt * ktiles + tile) * kFp4ScaleTile + j0 * 16) = make_uint4(s[0], s[1], s[2], s[3]);
 }
 
 __device__ __forceinline__ float scale_value(uint32_t field) {  // 2^(field - 127)
@@ -356,12 +351,12 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, uint8_t* q, uin
   const int load = rows_aligned(x, ldx, sizeof(T), 16) ? 16 : rows_aligned(x, ldx, sizeof(T), 4) ? 4 : (int)sizeof(T);
   if (!qt) {
     const int strips = cdiv(k, 256);
-    const long long units = (long long)strips * cdiv(rows, kRowsAhead), grid = (units + kQThreads / 32 - 1) / (kQThreads / 32);
-    if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
+    const long long units = (long long)strips * rtiles * 32;
+    if (units > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
     auto* const rows_kernel = load == 16 ? k_fp4_rows<T, 16> : load == 4 ? k_fp4_rows<T, 4> : k_fp4_rows<T, sizeof(T)>;
-    PdlLaunch l(dim3((unsigned)grid), dim3(kQThreads), st);
-    FF_LAUNCH(K_FP4_QUANT, bytes, st, cudaLaunchKernelEx(&l.cfg, rows_kernel, x, ldx, rows, k, q, scale, ldq, ktiles, strips),
-              "4-bit quantize");
+    PdlLaunch l(dim3((unsigned)cdiv(units, kQThreads / 32)), dim3(kQThreads), st);
+    FF_LAUNCH(K_FP4_QUANT, bytes, st,
+              cudaLaunchKernelEx(&l.cfg, rows_kernel, x, ldx, rows, k, q, scale, ldq, ktiles, strips, (int)units), "4-bit quantize");
     return FF_OK;
   }
   PdlLaunch l(dim3((unsigned)blocks), dim3(kQThreads), st);

@@ -338,26 +338,41 @@ struct GradArgs {
   long long lddy, ldh, lddh, lddx;
   int rows, cols, warps;
   int depth;    // rows on their way
+  float inv_cols;
   bool wide;
 };
 
 // Copies one lane's part of a unit to its own slot of shared memory, by the
 // bytes that the alignment allows (single bf16 values go through registers).
 template <typename T, int V>
-__device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane, int cols, bool whole) {
+__device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int lane, int cols, bool whole) {
   if constexpr (sizeof(T) * V >= 4) {
     constexpr int BYTES = (int)sizeof(T) * V;
 #pragma unroll
     for (int i = 0; i < 4 / V; ++i) {
       const int c = c0 + Unit<T, V>::first(i, lane);
       const int left = whole ? BYTES : min(max(cols - c, 0), V) * (int)sizeof(T);
-      ptx::cp_async_zfill<BYTES>(ptx::smem_u32(slot) + i * BYTES, row + (whole || left ? c : 0), left);
+      ptx::cp_async_zfill<BYTES>(slot + i * BYTES, row + (whole || left ? c : 0), left);
     }
   } else {
     Unit<T, V> u;
     u.load(row, c0, lane, cols, whole);
-    *static_cast<Held<T>*>(slot) = u;
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot), "r"(u.w[0]), "r"(u.w[1]) : "memory");
   }
+}
+
+// The unit in a slot.
+__device__ __forceinline__ void read_slot(Held<bf16>& h, uint32_t slot) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(h.w[0]), "=r"(h.w[1]) : "r"(slot));
+}
+__device__ __forceinline__ void read_slot(Held<float>& h, uint32_t slot) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(h.w[0]), "=f"(h.w[1]), "=f"(h.w[2]), "=f"(h.w[3]) : "r"(slot));
+}
+template <typename T>
+__device__ __forceinline__ void slot_pairs(uint64_t (&p)[2], uint32_t slot) {
+  Held<T> h;
+  read_slot(h, slot);
+  h.pairs(p);
 }
 
 // Rows blockIdx.x + i gridDim.x; each lane keeps its columns' sums of dgamma in
@@ -367,19 +382,20 @@ __device__ __forceinline__ void fetch(void* slot, const T* row, int c0, int lane
 // one warp a row the block's warps take rows of their own and join their sums
 // in shared memory ([warps][cols]).
 template <typename T, int V, int NU>
-__device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[NU][2], Held<T>* slots, int teams, int team, int warp,
+__device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[NU][2], uint32_t slots, int teams, int team, int warp,
                                           int lane, float (*part)[kMaxWarps], bool whole) {
-  const int c0 = warp * NU * UNIT, arrays = a.dh ? 3 : 2, threads = (int)blockDim.x;
+  const int c0 = warp * NU * UNIT;
   const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
   const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
   long long ahead = first;
-  auto issue = [&](Held<T>* to) {
+  constexpr uint32_t ROW = 32 * sizeof(Held<T>);  // a warp's slots of one unit of one array
+  auto issue = [&](uint32_t to) {
     if (ahead < a.rows) {
 #pragma unroll
       for (int i = 0; i < NU; ++i) {
-        fetch<T, V>(to + i * threads, hp, c0 + i * UNIT, lane, a.cols, whole);
-        fetch<T, V>(to + (NU + i) * threads, dp, c0 + i * UNIT, lane, a.cols, whole);
-        if (a.dh) fetch<T, V>(to + (2 * NU + i) * threads, tp, c0 + i * UNIT, lane, a.cols, whole);
+        fetch<T, V>(to + i * ROW, hp, c0 + i * UNIT, lane, a.cols, whole);
+        fetch<T, V>(to + (NU + i) * ROW, dp, c0 + i * UNIT, lane, a.cols, whole);
+        if (a.dh) fetch<T, V>(to + (2 * NU + i) * ROW, tp, c0 + i * UNIT, lane, a.cols, whole);
       }
       hp += step * a.ldh;
       dp += step * a.lddy;
@@ -388,7 +404,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
     ahead += step;
     ptx::cp_async_commit();
   };
-  const int stage = arrays * NU * threads;  // slots a row
+  const uint32_t stage = (a.dh ? 3 : 2) * NU * blockDim.x * (uint32_t)sizeof(Held<T>);  // bytes a row
   for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
   T* out = a.dx ? a.dx + first * a.lddx : nullptr;
   int turn = 0, at = 0;
@@ -398,13 +414,13 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
     else if (a.depth == 3) ptx::cp_async_wait<2>();
     else if (a.depth == 2) ptx::cp_async_wait<1>();
     else ptx::cp_async_wait<0>();
-    Held<T>* now = slots + at * stage;
+    const uint32_t now = slots + at * stage;
     uint64_t dot2 = 0;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       uint64_t x[2], y[2], g[2];
-      now[i * threads].pairs(x);
-      now[(NU + i) * threads].pairs(y);
+      slot_pairs<T>(x, now + i * ROW);
+      slot_pairs<T>(y, now + (NU + i) * ROW);
       gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -414,19 +430,19 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
       }
     }
     // <du n> rstd^2, what h is to be taken off by
-    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) / (float)a.cols;
+    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) * a.inv_cols;
     const uint64_t off = both(-dot * rstd * rstd * rstd);
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       if (!out || (!whole && c0 + i * UNIT >= a.cols)) break;
       uint64_t x[2], y[2], g[2];
-      now[i * threads].pairs(x);
-      now[(NU + i) * threads].pairs(y);
+      slot_pairs<T>(x, now + i * ROW);
+      slot_pairs<T>(y, now + (NU + i) * ROW);
       gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
 #pragma unroll
       for (int e = 0; e < 2; ++e) x[e] = ptx::fma2(x[e], off, ptx::mul2(both(rstd), ptx::mul2(g[e], y[e])));
       if (a.dh) {
-        now[(2 * NU + i) * threads].pairs(y);
+        slot_pairs<T>(y, now + (2 * NU + i) * ROW);
 #pragma unroll
         for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
       }
@@ -451,7 +467,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a
   uint64_t acc[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
-  Held<T>* slots = reinterpret_cast<Held<T>*>(dyn) + threadIdx.x;
+  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * (a.dh ? 3 : 2) * NU * 32 + lane) * (uint32_t)sizeof(Held<T>);
   // (both calls meet at the same barriers)
   if (c0 + NU * UNIT <= a.cols)
     grad_rows<T, V, NU>(a, acc, slots, teams, team, warp, lane, part, true);
@@ -671,6 +687,7 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
   const GradPlan p = grad_plan(a.rows, a.cols, (int)sizeof(T));
   a.warps = p.warps;
   a.depth = p.depth;
+  a.inv_cols = 1.f / (float)a.cols;
   a.wide = wide_of(a.gamma);
   a.part = !dgamma ? nullptr : p.blocks > 1 ? static_cast<float*>(ws) : dgamma;
   const double count = (double)a.rows * a.cols;
