@@ -20,6 +20,7 @@ namespace {
 
 constexpr int UNIT = 128;
 constexpr int kMaxWarps = 32;
+constexpr int kGradWarps = 16;  // of the gradient's row kernel
 
 // A lane's four values of the unit at column c0, V of them consecutive: 16 or
 // 8 bytes (V = 4), a pair of bf16 (V = 2), or one (V = 1, the lanes side by
@@ -375,90 +376,132 @@ __device__ __forceinline__ void slot_pairs(uint64_t (&p)[2], uint32_t slot) {
   h.pairs(p);
 }
 
-// Rows blockIdx.x + i gridDim.x; each lane keeps its columns' sums of dgamma in
-// registers over the block's rows, so that dy and h are read once.  The rows
-// to come are on their way into shared memory (`depth` rows, each thread its
-// own values, so that no barrier is needed) while this one is worked on.  With
-// one warp a row the block's warps take rows of their own and join their sums
-// in shared memory ([warps][cols]).
-template <typename T, int V, int NU>
-__device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[NU][2], uint32_t slots, int teams, int team, int warp,
-                                          int lane, float (*part)[kMaxWarps], bool whole) {
-  const int c0 = warp * NU * UNIT;
-  const long long first = (long long)blockIdx.x * teams + team, step = (long long)gridDim.x * teams;
-  const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
-  long long ahead = first;
-  constexpr uint32_t ROW = 32 * sizeof(Held<T>);  // a warp's slots of one unit of one array
-  auto issue = [&](uint32_t to) {
-    if (ahead < a.rows) {
+// The sums over a row's warps of R values (rows), in a fixed order, in every
+// lane; of two, half a warp each.  `part` is [2][kMaxWarps], one of two that
+// callers use in turn (one barrier a call).
+template <int R>
+__device__ __forceinline__ void row_sums(float (&v)[R], int warps, int warp, int lane, float (*part)[kMaxWarps]) {
+  if constexpr (R == 1) {
+    v[0] = row_sum(v[0], warps, warp, lane, part[0]);
+  } else {
+    const int r = lane >> 4, i = lane & 15;
+    float s = (r ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, r ? v[0] : v[1], 16);
 #pragma unroll
-      for (int i = 0; i < NU; ++i) {
-        fetch<T, V>(to + i * ROW, hp, c0 + i * UNIT, lane, a.cols, whole);
-        fetch<T, V>(to + (NU + i) * ROW, dp, c0 + i * UNIT, lane, a.cols, whole);
-        if (a.dh) fetch<T, V>(to + (2 * NU + i) * ROW, tp, c0 + i * UNIT, lane, a.cols, whole);
-      }
-      hp += step * a.ldh;
-      dp += step * a.lddy;
-      if (a.dh) tp += step * a.lddh;
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (warps > 1) {
+      if (i == 0) part[r][warp] = s;
+      __syncthreads();
+      s = i < warps ? part[r][i] : 0.f;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     }
+    v[0] = __shfl_sync(0xffffffffu, s, 0);
+    v[1] = __shfl_sync(0xffffffffu, s, 16);
+  }
+}
+
+// A block takes R rows at a time, sets of them gridDim.x apart; each lane keeps
+// gamma and its columns' sums of dgamma in registers over all of them, so that
+// dy and h are read once.  The rows to come are on their way into shared memory
+// (`depth` sets, each thread its own values, so that no barrier is needed)
+// while these are worked on.  With one warp a row the block's warps take rows of
+// their own and join their sums in shared memory ([warps][cols]).
+// (gamma read anew each time came from L2, since the copies take L1's place:
+// 4096 x 8192 bf16 59 us in place of 50.)
+template <typename T, int V, int NU, int R>
+__device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[NU][2], uint32_t slots, int teams, int team, int warp,
+                                          int lane, float (*part)[2][kMaxWarps], bool whole) {
+  const int c0 = warp * NU * UNIT;
+  const long long first = ((long long)blockIdx.x * teams + team) * R, step = (long long)gridDim.x * teams * R;
+  const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
+  constexpr uint32_t UB = 32 * sizeof(Held<T>);  // bytes of a warp's slots of one unit of one array
+  const uint32_t rb = (a.dh ? 3 : 2) * NU * UB;  // of a row
+  const uint32_t stage = R * rb * (blockDim.x >> 5);
+  long long ahead = first;
+  auto issue = [&](uint32_t to) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (ahead + r < a.rows) {
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+          fetch<T, V>(to + r * rb + i * UB, hp + r * a.ldh, c0 + i * UNIT, lane, a.cols, whole);
+          fetch<T, V>(to + r * rb + (NU + i) * UB, dp + r * a.lddy, c0 + i * UNIT, lane, a.cols, whole);
+          if (a.dh) fetch<T, V>(to + r * rb + (2 * NU + i) * UB, tp + r * a.lddh, c0 + i * UNIT, lane, a.cols, whole);
+        }
+      }
+    }
+    hp += step * a.ldh;
+    dp += step * a.lddy;
+    if (a.dh) tp += step * a.lddh;
     ahead += step;
     ptx::cp_async_commit();
   };
-  const uint32_t stage = (a.dh ? 3 : 2) * NU * blockDim.x * (uint32_t)sizeof(Held<T>);  // bytes a row
   for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
+  uint64_t g[NU][2];
+#pragma unroll
+  for (int i = 0; i < NU; ++i) gammas<V>(g[i], a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
   T* out = a.dx ? a.dx + first * a.lddx : nullptr;
   int turn = 0, at = 0;
   for (long long row = first; row < a.rows; row += step, turn ^= 1) {
-    const float rstd = __ldg(a.rstd + row);
+    float rstd[R], dot[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = row + r < a.rows ? __ldg(a.rstd + row + r) : 0.f;
     if (a.depth >= 4) ptx::cp_async_wait<3>();
     else if (a.depth == 3) ptx::cp_async_wait<2>();
     else if (a.depth == 2) ptx::cp_async_wait<1>();
     else ptx::cp_async_wait<0>();
     const uint32_t now = slots + at * stage;
-    uint64_t dot2 = 0;
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      uint64_t x[2], y[2], g[2];
-      slot_pairs<T>(x, now + i * ROW);
-      slot_pairs<T>(y, now + (NU + i) * ROW);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
+    for (int r = 0; r < R; ++r) {
+      uint64_t dot2 = 0;
+      if (row + r < a.rows) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint64_t yh = ptx::mul2(y[e], x[e]);
-        ptx::fma2_to(acc[i][e], yh, both(rstd));
-        ptx::fma2_to(dot2, yh, g[e]);
+        for (int i = 0; i < NU; ++i) {
+          uint64_t x[2], y[2];
+          slot_pairs<T>(x, now + r * rb + i * UB);
+          slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint64_t yh = ptx::mul2(y[e], x[e]);
+            ptx::fma2_to(acc[i][e], yh, both(rstd[r]));
+            ptx::fma2_to(dot2, yh, g[i][e]);
+          }
+        }
       }
+      dot[r] = sum_of(dot2);
     }
-    // <du n> rstd^2, what h is to be taken off by
-    const float dot = row_sum(sum_of(dot2), a.warps, warp, lane, part[turn]) * a.inv_cols;
-    const uint64_t off = both(-dot * rstd * rstd * rstd);
+    row_sums<R>(dot, a.warps, warp, lane, part[turn]);
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      if (!out || (!whole && c0 + i * UNIT >= a.cols)) break;
-      uint64_t x[2], y[2], g[2];
-      slot_pairs<T>(x, now + i * ROW);
-      slot_pairs<T>(y, now + (NU + i) * ROW);
-      gammas<V>(g, a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= a.rows || !out) break;
+      const uint64_t off = both(-dot[r] * a.inv_cols * rstd[r] * rstd[r] * rstd[r]);  // what h is taken off by
 #pragma unroll
-      for (int e = 0; e < 2; ++e) x[e] = ptx::fma2(x[e], off, ptx::mul2(both(rstd), ptx::mul2(g[e], y[e])));
-      if (a.dh) {
-        slot_pairs<T>(y, now + (2 * NU + i) * ROW);
+      for (int i = 0; i < NU; ++i) {
+        if (!whole && c0 + i * UNIT >= a.cols) break;
+        uint64_t x[2], y[2];
+        slot_pairs<T>(x, now + r * rb + i * UB);
+        slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+        for (int e = 0; e < 2; ++e) x[e] = ptx::fma2(x[e], off, ptx::mul2(both(rstd[r]), ptx::mul2(g[i][e], y[e])));
+        if (a.dh) {
+          slot_pairs<T>(y, now + r * rb + (2 * NU + i) * UB);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+        }
+        Unit<T, V> o;
+        o.set(x);
+        o.store(out + r * a.lddx, c0 + i * UNIT, lane, a.cols, whole);
       }
-      Unit<T, V> o;
-      o.set(x);
-      o.store(out, c0 + i * UNIT, lane, a.cols, whole);
     }
     if (out) out += step * a.lddx;
     issue(now);  // into the slots just read
     if (++at == a.depth) at = 0;
   }
 }
-template <typename T, int V, int NU>
-__global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a) {
+template <typename T, int V, int NU, int R>
+__global__ void __launch_bounds__(kGradWarps * 32) k_rms_grad(const GradArgs<T> a) {
   extern __shared__ __align__(16) uint8_t dyn[];
-  __shared__ float part[2][kMaxWarps];
+  __shared__ float part[2][2][kMaxWarps];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const bool own = a.warps == 1;  // a warp a row
@@ -467,12 +510,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_grad(const GradArgs<T> a
   uint64_t acc[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
-  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * (a.dh ? 3 : 2) * NU * 32 + lane) * (uint32_t)sizeof(Held<T>);
+  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2) * NU * 32 + lane) * (uint32_t)sizeof(Held<T>);
   // (both calls meet at the same barriers)
   if (c0 + NU * UNIT <= a.cols)
-    grad_rows<T, V, NU>(a, acc, slots, teams, team, warp, lane, part, true);
+    grad_rows<T, V, NU, R>(a, acc, slots, teams, team, warp, lane, part, true);
   else
-    grad_rows<T, V, NU>(a, acc, slots, teams, team, warp, lane, part, false);
+    grad_rows<T, V, NU, R>(a, acc, slots, teams, team, warp, lane, part, false);
+  ptx::griddep_launch_dependents();  // the fold's blocks may take their places
   if (!a.part) return;
   float* out = a.part + (long long)blockIdx.x * a.cols;
   float* joined = reinterpret_cast<float*>(dyn);
@@ -588,18 +632,18 @@ __global__ void __launch_bounds__(1024) k_rms_fold(const float* part, int rows, 
 // Units per warp of the row kernels: the most (fewest barriers, most loads in
 // flight a thread) that still give the GPU 16 warps an SM, else the fewest
 // (2432 = 152 x 16; 0: the row does not fit `most` units a warp).
-int units_per_warp(long long rows, int cols, int most) {
+int units_per_warp(long long rows, int cols, int most, int warps) {
   const int units = cdiv(cols, UNIT);
-  if (cdiv(units, most) > kMaxWarps) return 0;
+  if (cdiv(units, most) > warps) return 0;
   for (int nu = most; nu > 1; nu /= 2) {
     if (rows * cdiv(units, nu) >= 2432) return nu;
-    if (cdiv(units, nu / 2) > kMaxWarps) return nu;
+    if (cdiv(units, nu / 2) > warps) return nu;
   }
   return 1;
 }
 constexpr int kOwnRows = 8;      // rows a block with one warp a row
 constexpr int kGradRows = 128;   // rows whose terms of dgamma one thread adds up in a row
-constexpr int kFwdUnits = 8, kGradUnits = 4;
+constexpr int kFwdUnits = 8;
 
 // The vector that every array's rows are aligned for.
 template <typename T, typename... P>
@@ -621,7 +665,7 @@ template <typename T>
 ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
   using P = std::pair<const void*, long long>;
   const int v = vector_of<T>(P{a.x, a.ldx}, P{a.r, a.ldr}, P{a.h, a.ldh}, P{a.y, a.ldy});
-  const int nu = units_per_warp(a.rows, a.cols, kFwdUnits);
+  const int nu = units_per_warp(a.rows, a.cols, kFwdUnits, kMaxWarps);
   const double bytes = (double)a.rows * a.cols * (sizeof(T) * (1 + (a.r ? 2 : 0) + (a.y ? 1 : 0)) + (a.q ? 1 : 0));
   a.wide = wide_of(a.gamma);
   auto go = [&]() -> cudaError_t {
@@ -645,31 +689,41 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
   return FF_OK;
 }
 
-// The gradient's blocks: as many an SM as 1024 threads and two rows of shared
-// memory each allow, and at most kGradRows rows a thread; the rest of the
-// shared memory deepens the queue of rows on their way (depth 0: none fits).
-// (Sized for three arrays whether dh is there or not, so that the workspace
-// does not depend on it.)
+// The gradient's blocks: as many an SM as 512 threads (128 registers each) and
+// two sets of rows in shared memory allow, and at most kGradRows rows a thread.
+// Two rows a set where they fit; the rest of the shared memory deepens the
+// queue.  (Sized for three arrays whether dh is there or not, so that the
+// workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
 struct GradPlan {
-  int nu, warps, teams, blocks, depth;
+  int nu, warps, teams, set, blocks, depth;
 };
 GradPlan grad_plan(int rows, int cols, int esize) {
   GradPlan p{};
-  p.nu = units_per_warp(rows, cols, kGradUnits);
+  // four units a warp, or eight where four do not reach
+  p.nu = units_per_warp(rows, cols, 4, kGradWarps);
+  if (!p.nu) p.nu = units_per_warp(rows, cols, 8, kGradWarps);
   const int units = cdiv(cols, UNIT);
-  p.warps = p.nu ? cdiv(units, p.nu) : kMaxWarps;
-  p.teams = p.nu && p.warps == 1 ? kOwnRows : 1;
-  const long long sets = cdiv(rows, p.teams), least = cdiv(sets, kGradRows);
+  int row = 0, threads = 0;
+  if (p.nu) {
+    p.warps = cdiv(units, p.nu);
+    p.teams = p.warps == 1 ? kOwnRows : 1;
+    threads = p.warps * p.teams * 32;
+    row = threads * p.nu * 4 * esize * 3;  // bytes
+    if (row > kGradSmem) p.nu = 0;
+  }
   long long fill;
   if (p.nu) {
-    const int threads = p.warps * p.teams * 32, stage = threads * p.nu * 4 * esize * 3;
-    const int room = std::max(1, std::min(1024 / threads, kGradSmem / (2 * stage)));
-    p.depth = std::max(1, std::min(4, kGradSmem / (room * stage)));
+    p.set = 4 * row <= kGradSmem ? 2 : 1;
+    const int room = std::max(1, std::min(kGradWarps * 32 / threads, kGradSmem / (2 * p.set * row)));
+    p.depth = std::max(1, std::min(4, kGradSmem / (room * p.set * row)));
     fill = 152ll * room;
   } else {
+    p.warps = kMaxWarps;
+    p.teams = p.set = 1;
     fill = std::max(1, 152 * 32 / units);
   }
+  const long long sets = cdiv(rows, p.teams * p.set), least = cdiv(rows, (long long)p.teams * kGradRows);
   p.blocks = (int)(sets < fill ? sets : fill < least ? least : fill);
   if (!p.nu && p.blocks > 65535) p.blocks = 65535;
   return p;
@@ -696,17 +750,22 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
     auto go = [&]() -> cudaError_t {
       return with_vector<T>(v, [&](auto V) {
         const int threads = p.teams * p.warps * 32;
-        const size_t ring = (size_t)p.depth * (a.dh ? 3 : 2) * p.nu * threads * 4 * sizeof(T);
+        const size_t ring = (size_t)p.depth * p.set * (a.dh ? 3 : 2) * p.nu * threads * 4 * sizeof(T);
         const size_t smem = std::max(ring, p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0);
         PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)threads), st, smem);
-        auto go = [&](auto N) -> cudaError_t {
-          const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value>>(kGradSmem);
-          return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value>, a);
+        auto go = [&](auto N, auto R) -> cudaError_t {
+          const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem);
+          return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value, R.value>, a);
         };
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        using Four = std::integral_constant<int, 4>;
+        using Eight = std::integral_constant<int, 8>;
         switch (p.nu) {
-          case 1: return go(std::integral_constant<int, 1>{});
-          case 2: return go(std::integral_constant<int, 2>{});
-          default: return go(std::integral_constant<int, 4>{});
+          case 1: return p.set == 2 ? go(One{}, Two{}) : go(One{}, One{});
+          case 2: return p.set == 2 ? go(Two{}, Two{}) : go(Two{}, One{});
+          case 4: return p.set == 2 ? go(Four{}, Two{}) : go(Four{}, One{});
+          default: return p.set == 2 ? go(Eight{}, Two{}) : go(Eight{}, One{});
         }
       });
     };
