@@ -3,9 +3,11 @@
 //
 // The tensors are cut into pieces of 16 KB that thread groups of 256 take in
 // turn.  Few pieces: one cluster of blocks keeps them in registers between the
-// sum and the product (one read).  Many: a pass for the sums, one partial a
-// block, and a pass in the opposite order for the products, which finds the
-// last pieces in L2.
+// sum and the product (one read; 24010 fp32 values: 4.2 us).  Many: a pass for the
+// sums, one partial a block, and a pass in the opposite order for the products,
+// which finds the last pieces in L2 (all others are read and written as first to
+// be evicted).  Bound by HBM, two reads and a write: 268 M fp32 values in 486 us, 6.6 TB/s
+// (without the policies 503).
 #include <algorithm>
 #include <vector>
 
@@ -20,7 +22,9 @@ constexpr int GROUP = 256;             // threads that take a piece
 constexpr int VECS = 4;                // 16-byte vectors of it per thread
 constexpr int PIECE = GROUP * VECS * 16;  // bytes
 constexpr int kTable = 120;            // tensors a launch
-constexpr int kBlocks = 152 * 8;       // blocks of the two passes, one group each
+constexpr int kResident = 5;           // blocks of the two passes an SM holds (one group each): 80 KB of loads in flight
+constexpr int kBlocks = 152 * kResident;
+constexpr int kKeep = (64 << 20) / PIECE;  // pieces that the first pass leaves in L2 for the second
 constexpr int kClusterBlocks = 8, kClusterGroups = 4, kKept = 2;  // pieces kept: 8 * 4 * 2
 
 struct Table {
@@ -46,12 +50,12 @@ __device__ __forceinline__ int tensor_of(const Table& t, int piece) {
 template <typename T>
 struct Piece {
   static constexpr int N = 16 / (int)sizeof(T);
-  static __device__ __forceinline__ void load(uint4 (&r)[VECS], const T* p, long long left, int tid, bool wide) {
+  static __device__ __forceinline__ void load(uint4 (&r)[VECS], const T* p, long long left, int tid, bool wide, uint64_t policy) {
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
       const int i = (j * GROUP + tid) * N;
       if (wide && i + N <= left) {
-        r[j] = *reinterpret_cast<const uint4*>(p + i);
+        r[j] = ptx::ld_hint(p + i, policy);
       } else {
         T v[N];
 #pragma unroll
@@ -71,7 +75,8 @@ struct Piece {
     }
     return s;
   }
-  static __device__ __forceinline__ void store(const uint4 (&r)[VECS], T* p, long long left, int tid, bool wide, float by) {
+  static __device__ __forceinline__ void store(const uint4 (&r)[VECS], T* p, long long left, int tid, bool wide, float by,
+                                               uint64_t policy) {
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
       const int i = (j * GROUP + tid) * N;
@@ -80,7 +85,9 @@ struct Piece {
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] *= by;
       if (wide && i + N <= left) {
-        Vec<T, N>::store(p + i, v);
+        uint4 o;
+        Vec<T, N>::store(reinterpret_cast<T*>(&o), v);
+        ptx::st_hint(p + i, o, policy);
       } else {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -105,24 +112,45 @@ __device__ __forceinline__ At at_piece(const Table& t, int piece) {
   a.left = t.count[a.t] - a.from;
   return a;
 }
-__device__ __forceinline__ void load_piece(const Table& t, const At& a, uint4 (&r)[VECS], int tid) {
+__device__ __forceinline__ void load_piece(const Table& t, const At& a, uint4 (&r)[VECS], int tid, uint64_t policy) {
   const bool wide = wide_at(t.in[a.t]);
-  if (t.bf16s[a.t]) Piece<bf16>::load(r, static_cast<const bf16*>(t.in[a.t]) + a.from, a.left, tid, wide);
-  else Piece<float>::load(r, static_cast<const float*>(t.in[a.t]) + a.from, a.left, tid, wide);
+  if (t.bf16s[a.t]) Piece<bf16>::load(r, static_cast<const bf16*>(t.in[a.t]) + a.from, a.left, tid, wide, policy);
+  else Piece<float>::load(r, static_cast<const float*>(t.in[a.t]) + a.from, a.left, tid, wide, policy);
 }
 __device__ __forceinline__ float piece_squares(const Table& t, const At& a, const uint4 (&r)[VECS]) {
   return t.bf16s[a.t] ? Piece<bf16>::squares(r) : Piece<float>::squares(r);
 }
-__device__ __forceinline__ void store_piece(const Table& t, const At& a, const uint4 (&r)[VECS], int tid, float by) {
+__device__ __forceinline__ void store_piece(const Table& t, const At& a, const uint4 (&r)[VECS], int tid, float by, uint64_t policy) {
   const bool wide = wide_at(t.out[a.t]);
-  if (t.bf16s[a.t]) Piece<bf16>::store(r, static_cast<bf16*>(t.out[a.t]) + a.from, a.left, tid, wide, by);
-  else Piece<float>::store(r, static_cast<float*>(t.out[a.t]) + a.from, a.left, tid, wide, by);
+  if (t.bf16s[a.t]) Piece<bf16>::store(r, static_cast<bf16*>(t.out[a.t]) + a.from, a.left, tid, wide, by, policy);
+  else Piece<float>::store(r, static_cast<float*>(t.out[a.t]) + a.from, a.left, tid, wide, by, policy);
 }
 
-__device__ __forceinline__ double warp_sum(double v) {
+// The fp64 units take two lanes a clock and SM, so a thread's sums are fp32 (two
+// of them: the sum and what its roundings lost), a warp's too, and only one lane
+// a warp goes on in fp64, one thread to the square root (with both on every
+// thread 24010 values took 8.2 us in place of 4.2, 2 M 24 in place of 15).
+struct Sum {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float v) {  // Knuth's two-sum
+    const float s = __fadd_rn(hi, v), t = __fsub_rn(s, hi);
+    lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fsub_rn(v, t)));
+    hi = s;
+  }
+  // an infinite or NaN sum has no meaningful rest
+  __device__ __forceinline__ float value() const { return isfinite(hi) ? hi + lo : hi; }
+};
+template <typename F>
+__device__ __forceinline__ F warp_sum(F v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+// sqrt of a sum of squares, in fp32: past its range either way, by powers of two.
+__device__ __forceinline__ float norm_of(double s) {
+  const bool big = s > 1e38, small = s < 1e-30;
+  const float r = __fsqrt_rn((float)(s * (big ? 0x1p-128 : small ? 0x1p128 : 1.0)));
+  return big ? r * 0x1p64f : small ? r * 0x1p-64f : r;  // an infinity and NaN stay
 }
 // The factor: 1 where nothing is to be clipped; NaN for a NaN norm.
 __device__ __forceinline__ float factor(float norm, float max_norm) {
@@ -134,88 +162,97 @@ __device__ __forceinline__ float factor(float norm, float max_norm) {
 __global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
     k_clip_small(const __grid_constant__ Table t, float max_norm, float* norm_out, int pieces, int nblocks) {
   __shared__ double part[kClusterBlocks];
-  __shared__ double warps[GROUP * kClusterGroups / 32];
+  __shared__ float warps[GROUP * kClusterGroups / 32];
+  __shared__ float shared_norm;
   if (nblocks > 1) ptx::cluster_arrive();
   ptx::griddep_wait();
   const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int groups = blockDim.x / GROUP, tid = threadIdx.x & (GROUP - 1);
   const int first = rank * groups + threadIdx.x / GROUP, step = groups * nblocks;
   uint4 r[kKept][VECS];
-  double s = 0.0;
-#pragma unroll
-  for (int k = 0; k < kKept; ++k)
-    if (first + k * step < pieces) load_piece(t, at_piece(t, first + k * step), r[k], tid);
-#pragma unroll
-  for (int k = 0; k < kKept; ++k)
-    if (first + k * step < pieces) s += piece_squares(t, at_piece(t, first + k * step), r[k]);
-  s = warp_sum(s);
-  if (lane == 0) warps[warp] = s;
-  __syncthreads();
-  if (nblocks > 1) ptx::cluster_wait();
-  if (warp == 0) {
-    s = warp_sum(lane < (int)(blockDim.x >> 5) ? warps[lane] : 0.0);
-    if (nblocks == 1) {
-      if (lane == 0) part[0] = s;
-    } else if (lane < nblocks) {
-      const uint2 w = make_uint2((uint32_t)__double2loint(s), (uint32_t)__double2hiint(s));
-      ptx::st_remote_u2(reinterpret_cast<uint2*>(&part[rank]), (uint32_t)lane, w);
-    }
-  }
-  if (nblocks > 1) ptx::cluster_sync();
-  else __syncthreads();
-  s = 0.0;
-  for (int b = 0; b < nblocks; ++b) s += part[b];
-  const float norm = (float)sqrt(s);
-  if (rank == 0 && threadIdx.x == 0) *norm_out = norm;
-  const float by = factor(norm, max_norm);
+  At at[kKept];
+  Sum s;
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
     if (first + k * step < pieces) {
-      const At a = at_piece(t, first + k * step);
-      if (by != 1.f || t.in[a.t] != t.out[a.t]) store_piece(t, a, r[k], tid, by);
+      at[k] = at_piece(t, first + k * step);
+      load_piece(t, at[k], r[k], tid, ptx::l2_evict_normal());
     }
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if (first + k * step < pieces) s.add(piece_squares(t, at[k], r[k]));
+  const float f = warp_sum(s.value());
+  if (lane == 0) warps[warp] = f;
+  __syncthreads();
+  if (nblocks > 1) ptx::cluster_wait();
+  if (warp == 0) {
+    const double d = warp_sum(lane < (int)(blockDim.x >> 5) ? (double)warps[lane] : 0.0);
+    if (nblocks == 1) {
+      if (lane == 0) part[0] = d;
+    } else if (lane < nblocks) {
+      const uint2 w = make_uint2((uint32_t)__double2loint(d), (uint32_t)__double2hiint(d));
+      ptx::st_remote_u2(reinterpret_cast<uint2*>(&part[rank]), (uint32_t)lane, w);
+    }
+    __syncwarp();
+  }
+  if (nblocks > 1) ptx::cluster_sync();
+  if (threadIdx.x == 0) {
+    double d = part[0];
+    for (int b = 1; b < nblocks; ++b) d += part[b];
+    shared_norm = norm_of(d);
+    if (rank == 0) *norm_out = shared_norm;
+  }
+  __syncthreads();
+  const float by = factor(shared_norm, max_norm);
+#pragma unroll
+  for (int k = 0; k < kKept; ++k)
+    if (first + k * step < pieces && (by != 1.f || t.in[at[k].t] != t.out[at[k].t])) store_piece(t, at[k], r[k], tid, by, ptx::l2_evict_normal());
 }
 
 // part[blockIdx.x] = the sum of squares of the block's pieces.
-__global__ void __launch_bounds__(GROUP) k_clip_sums(const __grid_constant__ Table t, int pieces, double* part) {
-  __shared__ double warps[GROUP / 32];
+__global__ void __launch_bounds__(GROUP, kResident) k_clip_sums(const __grid_constant__ Table t, int pieces, int keep_from, double* part) {
+  __shared__ float warps[GROUP / 32];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  double s = 0.0;
+  const uint64_t first = ptx::l2_evict_first(), last = ptx::l2_evict_last();
+  Sum s;
   for (int p = blockIdx.x; p < pieces; p += gridDim.x) {
     uint4 r[VECS];
     const At a = at_piece(t, p);
-    load_piece(t, a, r, threadIdx.x);
-    s += piece_squares(t, a, r);
+    load_piece(t, a, r, threadIdx.x, p >= keep_from ? last : first);
+    s.add(piece_squares(t, a, r));
   }
-  s = warp_sum(s);
-  if (lane == 0) warps[warp] = s;
+  const float f = warp_sum(s.value());
+  if (lane == 0) warps[warp] = f;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < GROUP / 32; ++w) s += warps[w];
-    part[blockIdx.x] = s;
+    double d = warps[0];
+    for (int w = 1; w < GROUP / 32; ++w) d += warps[w];
+    part[blockIdx.x] = d;
   }
 }
-__global__ void __launch_bounds__(GROUP)
+__global__ void __launch_bounds__(GROUP, kResident)
     k_clip_scale(const __grid_constant__ Table t, int pieces, const double* part, int parts, float max_norm, float* norm_out) {
-  __shared__ double warps[GROUP / 32];
+  __shared__ float shared_norm;
   ptx::griddep_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  double s = 0.0;
-  for (int i = threadIdx.x; i < parts; i += GROUP) s += part[i];
-  s = warp_sum(s);
-  if (lane == 0) warps[warp] = s;
+  if (threadIdx.x < 32) {
+    double d = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 32) d += part[i];
+    d = warp_sum(d);
+    if (threadIdx.x == 0) {
+      shared_norm = norm_of(d);
+      if (blockIdx.x == 0) *norm_out = shared_norm;
+    }
+  }
   __syncthreads();
-  s = 0.0;
-  for (int w = 0; w < GROUP / 32; ++w) s += warps[w];
-  const float norm = (float)sqrt(s), by = factor(norm, max_norm);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  const float by = factor(shared_norm, max_norm);
+  const uint64_t first = ptx::l2_evict_first();
   for (int p = pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {
     const At a = at_piece(t, p);
     if (by == 1.f && t.in[a.t] == t.out[a.t]) continue;
     uint4 r[VECS];
-    load_piece(t, a, r, threadIdx.x);
-    store_piece(t, a, r, threadIdx.x, by);
+    load_piece(t, a, r, threadIdx.x, first);
+    store_piece(t, a, r, threadIdx.x, by, first);
   }
 }
 
@@ -273,7 +310,7 @@ ff_status clip(const std::vector<Tensor>& all, float max_norm, float* norm, doub
   for (int k = 0; k < tables; ++k) {
     PdlLaunch l(dim3(kBlocks), dim3(GROUP), st);
     FF_LAUNCH(K_CLIP, (double)bytes[k], st,
-              cudaLaunchKernelEx(&l.cfg, k_clip_sums, ts[k], ts[k].first[ts[k].n], part + (long long)k * kBlocks),
+              cudaLaunchKernelEx(&l.cfg, k_clip_sums, ts[k], ts[k].first[ts[k].n], std::max(0, ts[k].first[ts[k].n] - kKeep), part + (long long)k * kBlocks),
               "gradient clipping");
   }
   for (int k = tables - 1; k >= 0; --k) {

@@ -1084,13 +1084,14 @@ def fp8_selftest_wait(timeout_us: int, stream=None):
 # ------------------------------------------------- RMS norm, log-probabilities, clipping
 def _matrix_sizes(x, what):
     """rows, last dimension and row stride of x seen as a matrix [rows, last dimension]."""
-    if x.dim() < 1 or x.shape[-1] < 1:
+    shape = x.shape
+    if not shape or shape[-1] < 1:
         raise ValueError(f"{what} must be [..., columns] with at least one column")
-    cols = x.shape[-1]
-    rows = x.numel() // cols
-    if max(rows, cols) > 0x7FFFFF00:
+    cols = shape[-1]
+    rows = shape[0] if len(shape) == 2 else x.numel() // cols
+    if rows > 0x7FFFFF00 or cols > 0x7FFFFF00:
         raise ValueError(f"{what}: rows and columns must each fit 32 bits")
-    return rows, cols, _row_stride_of(x, what)
+    return rows, cols, cols if x.is_contiguous() else _row_stride_of(x, what)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -1257,7 +1258,8 @@ def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy
 
 @functools.lru_cache(maxsize=256)
 def _clip_arrays(n):
-    return c_void_p * n, c_longlong * n, c_int * n
+    """Types of the call's host arrays (pointers in, out and counts in one; types) and the workspace's bytes."""
+    return c_longlong * (3 * n), c_int * n, lib().ff_clip_grad_norm_workspace(n)
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
@@ -1271,34 +1273,40 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     if n == 0 or not isinstance(grads[0], torch.Tensor):
         raise ValueError("grads must be a non-empty list of tensors")
     dev = grads[0].device
-    if dev.type != "cuda":
+    index = grads[0].get_device()
+    if index < 0:
         raise ValueError("grads must be CUDA tensors")
-    if dev.index != torch._C._cuda_getDevice():
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return clip_grad_norm(grads, max_norm, out, stream)
-    ptrs, sizes, kinds = [], [], []
-    for g in grads:
-        if not isinstance(g, torch.Tensor) or g.device != dev or not g.is_contiguous():
-            raise ValueError(f"grads must be contiguous tensors on {dev}")
-        kinds.append(_prec(g, "grads"))
-        ptrs.append(g.data_ptr())
-        sizes.append(g.numel())
-    to = ptrs
+    try:
+        kinds = [_PREC[g.dtype] for g in grads]
+        fits = all([g.is_contiguous() and g.get_device() == index for g in grads])
+    except KeyError:
+        raise TypeError("grads must be torch.bfloat16 or torch.float32") from None
+    except AttributeError:
+        fits = False
+    if not fits:
+        raise ValueError(f"grads must be contiguous tensors on {dev}")
+    into = grads
     if out is not None:
-        to, out = [], list(out)
-        if len(out) != n:
+        into = list(out)
+        if len(into) != n:
             raise ValueError("out must have a tensor for each of grads")
-        for o, g in zip(out, grads):
-            if (not isinstance(o, torch.Tensor) or o.shape != g.shape or o.dtype != g.dtype or o.device != dev
+        for o, g in zip(into, grads):
+            if (not isinstance(o, torch.Tensor) or o.dtype is not g.dtype or o.get_device() != index or o.shape != g.shape
                     or not o.is_contiguous()):
                 raise ValueError("out must match grads in shape, type and device, and be contiguous")
-            to.append(o.data_ptr())
-    on, empty = _on(stream, dev, *grads, *(out or ()))
+    if stream is None:
+        on, empty = torch._C._cuda_getCurrentRawStream(index), torch.empty
+    else:
+        on, empty = _on(stream, dev, *grads, *into)
+    A, K, need = _clip_arrays(n)
+    host = A(*[g.data_ptr() for g in grads], *[o.data_ptr() for o in into], *[g.numel() for g in grads])
+    at = ctypes.addressof(host)
     norm = empty((1,), dtype=torch.float32, device=dev)
-    need = lib().ff_clip_grad_norm_workspace(n)
     ws = empty((need,), dtype=torch.uint8, device=dev)
-    P, N, K = _clip_arrays(n)
-    _check(lib().ff_clip_grad_norm(P(*ptrs), P(*to), N(*sizes), K(*kinds), n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
+    _check(lib().ff_clip_grad_norm(at, at + 8 * n, at + 16 * n, K(*kinds), n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
                                    on), "ff_clip_grad_norm")
     return norm
 
