@@ -67,7 +67,7 @@ __device__ __forceinline__ int steps_of(int K, int s) { return min(KS / 64, (K -
 // MMAs.  Persistent: the copies run ahead over the tiles.  Warps: 0 producer,
 // 1 MMAs (the even CTA's), 2..9 epilogue.
 constexpr int LN = 256;
-constexpr int LSTAGES = 5;
+constexpr int LSTAGES = 5;  // (4, and two staging blocks a warp: 87 us for 77 at 4096 x 8192 x 8192)
 constexpr int LA = BM * KB, LB = LN / 2 * KB;         // bytes of a stage's operands
 constexpr int LSTAGE = LA + LB + SF + 2 * SF;
 constexpr int LCPW = LN / 2;                          // columns per epilogue warp
@@ -368,16 +368,16 @@ __global__ void __launch_bounds__(THREADS, 1)
 //   warp 1      allocates TMEM, one lane copies the scales and issues the MMAs
 //   warps 2..9  epilogue: TMEM lane quarter warp % 4, half of the columns each
 //
-// A tile of BN < 128 columns takes its scales from a whole scale tile of 128,
-// from column (q0 % 128) / 32 of it on, which must be even: BN < 64 serves
-// products of one column tile only.
+// A tile takes its columns' scales from a whole scale tile of 128, from TMEM
+// column (q0 % 128) / 32 of it on, which must be even: BN < 64 serves products of
+// one column tile only.
 template <int BN>
 struct SCfg {
   static constexpr int STAGE = (BM + BN) * KB + 2 * SF;
-  static constexpr int STAGES = BN >= 128 ? 6 : BN >= 64 ? 8 : 9;
+  static constexpr int STAGES = BN >= 64 ? 8 : 9;
   static constexpr int CPW = BN / 2;
   static constexpr uint32_t ACC = BN < 32 ? 32 : BN;       // TMEM columns of the accumulator
-  static constexpr uint32_t TCOLS = BN >= 128 ? 256 : BN >= 64 ? 128 : 64;
+  static constexpr uint32_t TCOLS = BN >= 64 ? 128 : 64;
   static_assert(ACC + 4 * SFC <= TCOLS, "the accumulator and two stages' scales");
   static constexpr int PITCH = BM + 1;                     // floats per column of the exchange buffer
   static constexpr int SMEM = 1024 + STAGES * STAGE + 512;
@@ -630,8 +630,7 @@ int clusters_of(int dev, int bn, int ks_log) {
   switch (bn) {
     case 16: return resident_clusters<16>(dev, ks_log);
     case 32: return resident_clusters<32>(dev, ks_log);
-    case 64: return resident_clusters<64>(dev, ks_log);
-    default: return resident_clusters<128>(dev, ks_log);
+    default: return resident_clusters<64>(dev, ks_log);
   }
 }
 
@@ -661,8 +660,12 @@ int resident_pairs(int dev) {
 }
 
 // The shape of a product: tile, orientation and split with the least estimated
-// time: a wave of tiles takes a time per stage and a fixed one (launch, fill,
-// exchange, store), and no shape moves its operands faster than about 9 TB/s.
+// time (us): a wave of tiles takes a time per stage, each wave after the first a
+// fixed one, and a split its exchange.  The constants are least-squares readings
+// of a sweep of all shapes over 64 sizes from 1 x 500 x 500 to 4096 x 8192 x 8192 (of
+// tiles without swap, BN = 64's), within 16 % of them; of the sizes swept this
+// picks what is fastest in all but one, and there within 2 %.  Single CTAs on 128 x
+// 128 tiles were never the fastest.
 struct Plan {
   int bn;  // 256: the pair kernel; 0: no shape fits
   bool swap;
@@ -674,22 +677,21 @@ Plan plan(int dev, int M, int N, int K, int pairs) {
   double t = 1e30;
   if (pairs > 0) {
     const double tiles = (double)cdiv(M, 2 * BM) * cdiv(N, LN);
-    t = 4.0 + std::ceil(tiles / pairs) * (nkb * 0.29 + 1.0);
+    t = 2.7 + std::ceil(tiles / pairs) * (nkb * 0.29 + 2.0);
     best.bn = LN;
   }
-  struct Shape { int bn; bool swap; double step, fixed; };
-  const Shape shapes[5] = {{16, true, 0.24, 2.9}, {32, true, 0.28, 3.2}, {64, true, 0.28, 4.6}, {128, true, 0.31, 6.0},
-                           {128, false, 0.31, 7.0}};
+  struct Shape { int bn; bool swap; double step, first, wave, split; };
+  const Shape shapes[6] = {{16, true, 0.23, 2.5, 4.1, 1.3},  {32, true, 0.23, 2.9, 4.9, 1.5},  {64, true, 0.25, 3.7, 5.2, 1.8},
+                           {16, false, 0.23, 3.6, 4.6, 0.8}, {32, false, 0.23, 4.0, 5.4, 0.8}, {64, false, 0.26, 4.8, 5.7, 0.8}};
   for (const Shape& sh : shapes) {
     const int P = sh.swap ? N : M, Q = sh.swap ? M : N;
     if (sh.bn < 64 && Q > sh.bn) continue;
     const double tiles = (double)cdiv(P, BM) * cdiv(Q, sh.bn);
-    const double moved = tiles * nkb * (BM + sh.bn) * KB / 9e6;
     for (int l = 0; l < 4; ++l) {
       const int room = clusters_of(dev, sh.bn, l);
       if ((1 << l) > nkb || room < 1) break;
       const double waves = std::ceil(tiles / room), per = std::ceil(nkb / (1 << l));
-      const double c = sh.fixed + (l ? 0.5 : 0.0) + std::max(moved, waves * per * sh.step + (waves - 1) * sh.fixed);
+      const double c = sh.first + (l ? sh.split : 0.0) + waves * per * sh.step + (waves - 1) * sh.wave;
       if (c < t) {
         t = c;
         best = Plan{sh.bn, sh.swap, l};
@@ -754,8 +756,7 @@ ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
     switch (pl.bn) {
       case 16: return run_split<16>(m, g, pl.ks_log, st);
       case 32: return run_split<32>(m, g, pl.ks_log, st);
-      case 64: return run_split<64>(m, g, pl.ks_log, st);
-      default: return run_split<128>(m, g, pl.ks_log, st);
+      default: return run_split<64>(m, g, pl.ks_log, st);
     }
   };
   FF_LAUNCH(pairk ? K_FP4_PAIR : K_FP4_GEMM, 2.0 * f.M * f.N * f.K, st, go(), "4-bit matrix product");
