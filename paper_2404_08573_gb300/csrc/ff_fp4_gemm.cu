@@ -61,25 +61,32 @@ struct Args {
 __device__ __forceinline__ int steps_of(int K, int s) { return min(KS / 64, (K - s * KS + 63) / 64); }
 
 // ------------------------------------------------------- large products
-// CTA pairs (cta_group::2) on 256 x 256 tiles: each CTA loads 128 rows of A and
-// half of B's 256 columns per stage, the scales of its rows and those of all
-// 256 columns (35 KB for 8.4 MMAC a CTA), and holds 128 x 256 of the accumulator:
+constexpr int LSTAGING = 32 * 128;  // per epilogue warp: a block of 32 rows x 128 bytes of C
+
+// CTA pairs (cta_group::2) on 256 x LN tiles: each CTA loads 128 rows of A and
+// half of B's LN columns per stage, the scales of its rows and those of all LN
+// columns (LN = 256: 35 KB for 8.4 MMAC a CTA), and holds 128 x LN of the accumulator:
 // half of its TMEM, the rest of which cannot hold a second one beside the
 // scales.  So the epilogue warps first read all of it into registers (128
 // columns each), hand it back, and convert and store under the next tile's
 // MMAs.  Persistent: the copies run ahead over the tiles.  Warps: 0 producer,
 // 1 MMAs (the even CTA's), 2..9 epilogue.
-constexpr int LN = 256;
-constexpr int LSTAGES = 5;  // (4, and two staging blocks a warp: 87 us for 77 at 4096 x 8192 x 8192)
-constexpr int LA = BM * KB, LB = LN / 2 * KB;         // bytes of a stage's operands
-constexpr int LSTAGE = LA + LB + SF + 2 * SF;
-constexpr int LCPW = LN / 2;                          // columns per epilogue warp
-constexpr int LSTAGING = 32 * 128;                    // per epilogue warp: a block of 32 rows x 128 bytes of C
-constexpr uint32_t LSFC = SFC + 2 * SFC;              // TMEM columns of a stage's scales
-static_assert(LN + LSTAGES * LSFC <= 512, "the accumulator and the stages' scales");
-static_assert(LSTAGE % 1024 == 0, "swizzled tiles start on 1024 bytes");
-constexpr int L_SMEM = 1024 + LSTAGES * LSTAGE + EPI * LSTAGING + EPI * LCPW * 4 + 512;
-static_assert(L_SMEM > 113 * 1024 && L_SMEM <= 227 * 1024, "one GEMM CTA per SM, so that no TMEM allocation waits on another's");
+//
+// LN columns a tile: 128 where tiles of 256 would leave pairs without one (their
+// MMAs read A twice as often for their operations).
+template <int LN>
+struct LCfg {
+  static constexpr int STAGES = LN == 256 ? 5 : 7;  // (256: 4, and two staging blocks a warp: 87 us for 77 at 4096 x 8192 x 8192)
+  static constexpr int A = BM * KB, B = LN / 2 * KB;  // bytes of a stage's operands
+  static constexpr int SB = LN / 128;                 // scale tiles' rows of B's columns
+  static constexpr int STAGE = A + B + SF + SB * SF;
+  static constexpr int CPW = LN / 2;                  // columns per epilogue warp
+  static constexpr uint32_t SCOLS = SFC + SB * SFC;   // TMEM columns of a stage's scales
+  static_assert(LN + STAGES * SCOLS <= 512, "the accumulator and the stages' scales");
+  static_assert(STAGE % 1024 == 0, "swizzled tiles start on 1024 bytes");
+  static constexpr int SMEM = 1024 + STAGES * STAGE + EPI * LSTAGING + EPI * CPW * 4 + 512;
+  static_assert(SMEM > 113 * 1024 && SMEM <= 227 * 1024, "one GEMM CTA per SM, so that no TMEM allocation waits on another's");
+};
 
 // Tile t of the raster: groups of 8 row tiles, columns outermost within a
 // group, so that the tiles in flight share operand panels in L2.
@@ -92,34 +99,50 @@ __device__ __forceinline__ void tile_of(int t, int ntp, int ntq, int& tp, int& t
 }
 
 // A warp writes a staged block of 32 rows x 128 bytes (16-byte units swizzled
-// by the row) to C, `rows` and `left` of its rows and columns being there.
+// by the row) to C, `rows` and `left` of its rows and columns being there, the
+// lanes along a row.
 template <typename U>
-__device__ __forceinline__ void rows_out(const uint8_t* from, U* c, long long ldc, int rows, int left, int lane) {
+__device__ __forceinline__ void rows_out(uint32_t from, U* c, long long ldc, int rows, int left, int lane) {
   constexpr int J = 128 / 32 / (int)sizeof(U);
+  c += lane;
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += 8) {
-    U v[8][J];
+    uint32_t v[8][J];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int byte = (lane + 32 * j) * (int)sizeof(U);
-        v[i][j] = *reinterpret_cast<const U*>(from + (r0 + i) * 128 + (((byte >> 4) ^ i) << 4) + (byte & 15));
+        const uint32_t at = from + (r0 + i) * 128 + (((byte >> 4) ^ i) << 4) + (byte & 15);
+        if constexpr (sizeof(U) == 4)
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[i][j]) : "r"(at));
+        else
+          asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v[i][j]) : "r"(at));
       }
+    if (rows >= 32 && left >= 32 * J) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 8; ++i, c += ldc)
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (r0 + i < rows && lane + 32 * j < left) c[(r0 + i) * ldc + lane + 32 * j] = v[i][j];
+        for (int j = 0; j < J; ++j) c[32 * j] = (U)v[i][j];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i, c += ldc)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+          if (r0 + i < rows && lane + 32 * j < left) c[32 * j] = (U)v[i][j];
+    }
   }
 }
 
 // TMA_C: C's rows are 16-byte aligned and go out by TMA.  BF16: C's type.
-template <bool TMA_C, bool BF16>
+template <int LN, bool TMA_C, bool BF16>
 __global__ void __launch_bounds__(THREADS, 1)
     k_fp4_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmSA, const __grid_constant__ CUtensorMap tmSB,
                const __grid_constant__ CUtensorMap tmC, Args g) {
+  using C = LCfg<LN>;
+  constexpr int LSTAGES = C::STAGES, LSTAGE = C::STAGE, LA = C::A, LB = C::B, LCPW = C::CPW;
+  constexpr uint32_t LSFC = C::SCOLS;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_s = ptx::smem_u32(smem_raw);
   uint8_t* smem = smem_raw + ((1024u - (raw_s & 1023u)) & 1023u);
@@ -186,7 +209,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           ptx::tma_load_2d_pair(a, &tmA, bar, kb * KB, ar);
           ptx::tma_load_2d_pair(a + LA, &tmB, bar, kb * KB, br);
           ptx::tma_load_2d_pair(a + LA + LB, &tmSA, bar, kb * SF_BOX, tp * 2 + (int)crank);
-          ptx::tma_load_2d_pair(a + LA + LB + SF, &tmSB, bar, kb * SF_BOX, tq * 2);
+          ptx::tma_load_2d_pair(a + LA + LB + SF, &tmSB, bar, kb * SF_BOX, tq * C::SB);
         }
       }
       if (!*abort_flag) {
@@ -240,13 +263,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int h = 0; h < 2; ++h) {
               const uint64_t from = sd0 + at + h * (kFp4ScaleTile >> 4);
               ptx::tmem_cp_rows16_pair(sfa + 4 * h, from);
-              ptx::tmem_cp_rows16_pair(sfb + 8 * h, from + (SF >> 4));
-              ptx::tmem_cp_rows16_pair(sfb + 8 * h + 4, from + (2 * SF >> 4));
+#pragma unroll
+              for (int r = 0; r < C::SB; ++r)
+                ptx::tmem_cp_rows16_pair(sfb + (h * C::SB + r) * 4, from + ((r + 1) * SF >> 4));
             }
 #pragma unroll
             for (int k = 0; k < KS / 64; ++k)
               if (k < steps)
-                ptx::umma_mxf4_pair(tmem, ad0 + at + 2 * k, bd0 + at + 2 * k, idesc[k & 1], sfa + 4 * (k / 2), sfb + 8 * (k / 2),
+                ptx::umma_mxf4_pair(tmem, ad0 + at + 2 * k, bd0 + at + 2 * k, idesc[k & 1], sfa + 4 * (k / 2), sfb + C::SB * 4 * (k / 2),
                                     kb > 0 || k > 0);
             ptx::umma_commit_pair(&empty[s], 3);
             if (kb == nkb - 1) ptx::umma_commit_pair(tfull, 3);
@@ -308,9 +332,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int rows = g.P - rbase, left = g.Q - col0;
           const long long at = (long long)rbase * g.ldc + col0;
           if constexpr (BF16)
-            rows_out(from, static_cast<uint16_t*>(g.c) + at, g.ldc, rows, left, lane);
+            rows_out(ptx::smem_u32(from), static_cast<uint16_t*>(g.c) + at, g.ldc, rows, left, lane);
           else
-            rows_out(from, static_cast<uint32_t*>(g.c) + at, g.ldc, rows, left, lane);
+            rows_out(ptx::smem_u32(from), static_cast<uint32_t*>(g.c) + at, g.ldc, rows, left, lane);
         }
       };
       // four accumulators with bias and activation
@@ -632,18 +656,18 @@ int clusters_of(int dev, int bn, int ks_log) {
 }
 
 // CTA pairs the GPU holds at once.
-template <bool TMA_C, bool BF16>
+template <int LN, bool TMA_C, bool BF16>
 int resident_pairs(int dev) {
   static PerDevice<int> kept;
   int n = 0;
   const cudaError_t e = kept.get(dev, &n, [](int* pairs) {
-    constexpr auto kernel = k_fp4_pair<TMA_C, BF16>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L_SMEM);
+    constexpr auto kernel = k_fp4_pair<LN, TMA_C, BF16>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LCfg<LN>::SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = L_SMEM;
+    cfg.dynamicSmemBytes = LCfg<LN>::SMEM;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
@@ -655,31 +679,48 @@ int resident_pairs(int dev) {
   if (e != cudaSuccess) cudaGetLastError();  // leave no error behind: the split kernel runs
   return e == cudaSuccess ? n : 0;
 }
+template <bool BF16>
+int pairs_of(int dev) {
+  return std::min(std::min(resident_pairs<256, true, BF16>(dev), resident_pairs<256, false, BF16>(dev)),
+                  std::min(resident_pairs<128, true, BF16>(dev), resident_pairs<128, false, BF16>(dev)));
+}
+template <int LN>
+cudaError_t run_pair(const CUtensorMap (&m)[4], const CUtensorMap& c, const Args& g, int pairs, bool tma_c, cudaStream_t st) {
+  const unsigned grid = 2u * (unsigned)std::min((long long)pairs, (long long)g.ntp * g.ntq);
+  auto* const kernel = g.out_bf16 ? (tma_c ? k_fp4_pair<LN, true, true> : k_fp4_pair<LN, false, true>)
+                                  : (tma_c ? k_fp4_pair<LN, true, false> : k_fp4_pair<LN, false, false>);
+  return launch(kernel, grid, THREADS, 2, LCfg<LN>::SMEM, st, m[0], m[1], m[2], m[3], c, g);
+}
 
 // The shape of a product: tile, orientation and split with the least estimated
 // time (us): a wave of tiles takes a time per stage, each wave after the first a
 // fixed one, and a split its exchange.  The constants are least-squares readings
-// of a sweep of all shapes over 64 sizes from 1 x 500 x 500 to 4096 x 8192 x 8192 (of
-// tiles without swap, BN = 64's), within 16 % of them; of the sizes swept this
-// picks what is fastest in all but one, and there within 2 %.  Single CTAs on 128 x
-// 128 tiles were never the fastest.
+// of a sweep of all shapes over 88 sizes from 1 x 10 x 2000 to 4096 x 8192 x 8192, within
+// 13 % of them (root mean square); what this picks is within 3 % of the fastest
+// shape of a size on average.  Single CTAs on 128 x 128 tiles were never that.
 struct Plan {
-  int bn;  // 256: the pair kernel; 0: no shape fits
+  int bn;  // columns; 0: no shape fits
   bool swap;
   int ks_log;
+  bool pair;
 };
 Plan plan(int dev, int M, int N, int K, int pairs) {
   const double nkb = cdiv(K, KS);
-  Plan best{0, false, 0};
+  Plan best{0, false, 0, false};
   double t = 1e30;
   if (pairs > 0) {
-    const double tiles = (double)cdiv(M, 2 * BM) * cdiv(N, LN);
-    t = 2.7 + std::ceil(tiles / pairs) * (nkb * 0.29 + 2.0);
-    best.bn = LN;
+    const double tiles = (double)cdiv(M, 2 * BM) * cdiv(N, 256), narrow = (double)cdiv(M, 2 * BM) * cdiv(N, 128);
+    t = 2.9 + std::ceil(tiles / pairs) * (nkb * 0.30 + 2.04);
+    best = Plan{256, false, 0, true};
+    const double c = 2.9 + std::ceil(narrow / pairs) * (nkb * 0.27 + 1.03);
+    if (c < t) {
+      t = c;
+      best.bn = 128;
+    }
   }
   struct Shape { int bn; bool swap; double step, first, wave, split; };
-  const Shape shapes[6] = {{16, true, 0.23, 2.5, 4.1, 1.3},  {32, true, 0.23, 2.9, 4.9, 1.5},  {64, true, 0.25, 3.7, 5.2, 1.8},
-                           {16, false, 0.23, 3.6, 4.6, 0.8}, {32, false, 0.23, 4.0, 5.4, 0.8}, {64, false, 0.26, 4.8, 5.7, 0.8}};
+  const Shape shapes[6] = {{16, true, 0.25, 2.4, 4.9, 1.2},  {32, true, 0.24, 2.7, 5.4, 1.5},  {64, true, 0.23, 3.7, 5.2, 1.7},
+                           {16, false, 0.27, 2.5, 6.9, 1.1}, {32, false, 0.25, 3.0, 7.7, 1.3}, {64, false, 0.24, 4.7, 5.8, 0.9}};
   for (const Shape& sh : shapes) {
     const int P = sh.swap ? N : M, Q = sh.swap ? M : N;
     if (sh.bn < 64 && Q > sh.bn) continue;
@@ -691,7 +732,7 @@ Plan plan(int dev, int M, int N, int K, int pairs) {
       const double c = sh.first + (l ? sh.split : 0.0) + waves * per * sh.step + (waves - 1) * sh.wave;
       if (c < t) {
         t = c;
-        best = Plan{sh.bn, sh.swap, l};
+        best = Plan{sh.bn, sh.swap, l, false};
       }
     }
   }
@@ -711,8 +752,7 @@ cudaError_t run_split(const CUtensorMap (&m)[4], const Args& g, int ks_log, cuda
 ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
   int dev = 0;
   FF_TRY(cudaGetDevice(&dev), "4-bit matrix product");
-  const int pairs = f.out_bf16 ? std::min(resident_pairs<true, true>(dev), resident_pairs<false, true>(dev))
-                               : std::min(resident_pairs<true, false>(dev), resident_pairs<false, false>(dev));
+  const int pairs = f.out_bf16 ? pairs_of<true>(dev) : pairs_of<false>(dev);
   const Plan pl = plan(dev, f.M, f.N, f.K, pairs);
   if (pl.bn == 0) return FF_ERR_UNSUPPORTED;
   Args g{};
@@ -726,37 +766,31 @@ ff_status fp4_gemm(const Fp4Gemm& f, cudaStream_t st) {
   g.c = f.c;
   g.ldc = f.ldc;
   g.err = f.status;
-  const bool pairk = pl.bn == LN;
-  g.ntp = cdiv(g.P, pairk ? 2 * BM : BM);
+  g.ntp = cdiv(g.P, pl.pair ? 2 * BM : BM);
   g.ntq = cdiv(g.Q, pl.bn);
   if ((long long)g.ntp * g.ntq << pl.ks_log > 0x3FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const int ld = fp4_stride(f.K), words = cdiv(f.K, 128) * (kFp4ScaleTile / 4);
   CUtensorMap m[4];
   if (!make_sw128_map(&m[0], pl.swap ? f.b : f.a, 1, ld, g.P, ld, KB, BM) ||
-      !make_sw128_map(&m[1], pl.swap ? f.a : f.b, 1, ld, g.Q, ld, KB, pairk ? LN / 2 : pl.bn) ||
+      !make_sw128_map(&m[1], pl.swap ? f.a : f.b, 1, ld, g.Q, ld, KB, pl.pair ? pl.bn / 2 : pl.bn) ||
       !make_plain_map(&m[2], pl.swap ? f.sb : f.sa, 4, words, cdiv(g.P, 128), words, SF_BOX, 1) ||
-      !make_plain_map(&m[3], pl.swap ? f.sa : f.sb, 4, words, cdiv(g.Q, 128), words, SF_BOX, pairk ? 2 : 1))
+      !make_plain_map(&m[3], pl.swap ? f.sa : f.sb, 4, words, cdiv(g.Q, 128), words, SF_BOX, pl.pair && pl.bn == 256 ? 2 : 1))
     return FF_ERR_INVALID_ARG;
   const int es = f.out_bf16 ? 2 : 4;
   CUtensorMap c = m[0];
   // whole 16-byte units a row: a row that ends inside one is written to the
   // unit's end, into what lies between the rows
-  const bool tma_c = pairk && (long long)f.N * es % 16 == 0 && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N &&
+  const bool tma_c = pl.pair && (long long)f.N * es % 16 == 0 && f.ldc <= 0x7FFFFFFFll && f.ldc >= f.N &&
                      make_sw128_map(&c, f.c, es, f.N, f.M, (int)f.ldc, 128 / es, 32);
   auto go = [&]() -> cudaError_t {
-    if (pairk) {
-      const unsigned grid = 2u * (unsigned)std::min((long long)pairs, (long long)g.ntp * g.ntq);
-      auto* const kernel = f.out_bf16 ? (tma_c ? k_fp4_pair<true, true> : k_fp4_pair<false, true>)
-                                      : (tma_c ? k_fp4_pair<true, false> : k_fp4_pair<false, false>);
-      return launch(kernel, grid, THREADS, 2, L_SMEM, st, m[0], m[1], m[2], m[3], c, g);
-    }
+    if (pl.pair) return pl.bn == 256 ? run_pair<256>(m, c, g, pairs, tma_c, st) : run_pair<128>(m, c, g, pairs, tma_c, st);
     switch (pl.bn) {
       case 16: return run_split<16>(m, g, pl.ks_log, st);
       case 32: return run_split<32>(m, g, pl.ks_log, st);
       default: return run_split<64>(m, g, pl.ks_log, st);
     }
   };
-  FF_LAUNCH(pairk ? K_FP4_PAIR : K_FP4_GEMM, 2.0 * f.M * f.N * f.K, st, go(), "4-bit matrix product");
+  FF_LAUNCH(pl.pair ? K_FP4_PAIR : K_FP4_GEMM, 2.0 * f.M * f.N * f.K, st, go(), "4-bit matrix product");
   return FF_OK;
 }
 
