@@ -629,7 +629,7 @@ FF_API ff_status ff_fp8_matmul(const void* a, const float* a_scale, const void* 
                                ff_fp8_blocks b_blocks, int m, int n, int k, const float* bias, int relu,
                                ff_precision out_prec, void* c, long long ldc, int* device_status, void* stream);
 
-/* Waits for `stream` and returns FF_ERR_TIMEOUT if a wait of an 8-bit product
+/* Waits for `stream` and returns FF_ERR_TIMEOUT if a wait of an 8- or 4-bit product
  * without a device_status of its own timed out on the current device since the
  * last check (on whatever stream), then clears that. */
 FF_API ff_status ff_fp8_check(void* stream);

@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(const GradArgs<T> a) {
     }
   } else {
     const int c0 = (int)((long long)a.classes * seg / a.segments), c1 = (int)((long long)a.classes * (seg + 1) / a.segments);
-    for (int b = c0 + tid; b < c1; b += 8 * a.team) {
+    for (long long b = c0 + tid; b < c1; b += 8 * a.team) {
       typename Vec<T, 1>::Raw raw[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(256) k_logprobs_grad(const GradArgs<T> a) {
         if (b + j * a.team >= c1) break;
         float v[1];
         Vec<T, 1>::unpack(raw[j], v);
-        put(b + j * a.team, v[0]);
+        put((int)b + j * a.team, v[0]);
       }
     }
   }
