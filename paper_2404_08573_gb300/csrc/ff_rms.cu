@@ -81,42 +81,31 @@ struct Unit : Held<T> {
   static __device__ __forceinline__ int col(int e, int lane) { return first(e / V, lane) + e % V; }
   __device__ __forceinline__ Raw* raw() { return reinterpret_cast<Raw*>(this->w); }
   __device__ __forceinline__ const Raw* raw() const { return reinterpret_cast<const Raw*>(this->w); }
-  // whole: the unit lies inside the row
-  __device__ __forceinline__ void load(const T* row, int c0, int lane, int cols, bool whole) {
+  // (cols is a multiple of V: a vector lies inside the row or outside, where it
+  // reads as zero; whole: the unit lies inside)
+  __device__ __forceinline__ void load(const T* row, int c0, int lane, int cols, bool whole = false) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = c0 + first(i, lane);
-      if (whole || c + V <= cols) {
+      if (whole || c < cols)
         raw()[i] = Vec<T, V>::load(row + c);
-      } else {
-        T t[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) t[e] = c + e < cols ? row[c + e] : T(0.f);
-        memcpy(&raw()[i], t, sizeof(Raw));
-      }
+      else
+        memset(&raw()[i], 0, sizeof(Raw));
     }
   }
-  __device__ __forceinline__ void store(T* row, int c0, int lane, int cols, bool whole) const {
+  __device__ __forceinline__ void store(T* row, int c0, int lane, int cols, bool whole = false) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = c0 + first(i, lane);
-      if (whole || c + V <= cols) {
-        *reinterpret_cast<Raw*>(row + c) = raw()[i];
-      } else {
-        T t[V];
-        memcpy(t, &raw()[i], sizeof(Raw));
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (c + e < cols) row[c + e] = t[e];
-      }
+      if (whole || c < cols) *reinterpret_cast<Raw*>(row + c) = raw()[i];
     }
   }
 };
 
 // A lane's four gammas of the unit (null: ones); zero past the row.
 template <int V>
-__device__ __forceinline__ void gammas(uint64_t (&g)[2], const float* gamma, int c0, int lane, int cols, bool wide, bool whole) {
-  if (V == 4 && wide && gamma && (whole || c0 + lane * 4 + 4 <= cols)) {
+__device__ __forceinline__ void gammas(uint64_t (&g)[2], const float* gamma, int c0, int lane, int cols, bool wide) {
+  if (V == 4 && wide && gamma && c0 + lane * 4 < cols) {
     const float4 f = __ldg(reinterpret_cast<const float4*>(gamma + c0 + lane * 4));
     g[0] = ptx::pack2(f.x, f.y);
     g[1] = ptx::pack2(f.z, f.w);
@@ -164,21 +153,14 @@ struct RmsArgs {
   bool wide;  // gamma is 16-byte aligned
 };
 
-// y of one unit from its h values, zero past the row.
+// y of one unit from its h values.  (Past the row h and gamma are zero and so is
+// y, but for a row with a NaN, which is NaN there too.)
 template <typename T, int V>
-__device__ __forceinline__ void outputs(const RmsArgs<T>& a, uint64_t (&y)[2], int c0, int lane, float rstd, bool whole) {
+__device__ __forceinline__ void outputs(const RmsArgs<T>& a, uint64_t (&y)[2], int c0, int lane, float rstd) {
   uint64_t g[2];
-  gammas<V>(g, a.gamma, c0, lane, a.cols, a.wide, whole);
+  gammas<V>(g, a.gamma, c0, lane, a.cols, a.wide);
 #pragma unroll
   for (int i = 0; i < 2; ++i) y[i] = ptx::mul2(ptx::mul2(y[i], both(rstd)), g[i]);
-  if (!whole) {  // (a row with a NaN is NaN past its end too, without this)
-    float2 f[2] = {ptx::unpack2(y[0]), ptx::unpack2(y[1])};
-    float* v = &f[0].x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c0 + Unit<T, V>::col(e, lane) < a.cols ? v[e] : 0.f;
-    y[0] = ptx::pack2(f[0].x, f[0].y);
-    y[1] = ptx::pack2(f[1].x, f[1].y);
-  }
 }
 // The bits of the largest magnitude over the warp (a NaN's above all others).
 __device__ __forceinline__ uint32_t amax_of(const uint64_t (&y)[2]) {
@@ -191,7 +173,7 @@ __device__ __forceinline__ uint32_t amax_of(const uint64_t (&y)[2]) {
 }
 template <typename T, int V>
 __device__ __forceinline__ void put_fp8(const RmsArgs<T>& a, long long row, const uint64_t (&y)[2], int c0, int lane, float inv,
-                                        bool whole) {
+                                        bool whole = false) {
   const float2 f = ptx::unpack2(ptx::mul2(y[0], both(inv))), g = ptx::unpack2(ptx::mul2(y[1], both(inv)));
   const uint32_t lo = e4m3x2(f.x, f.y), hi = e4m3x2(g.x, g.y);
   uint8_t* q = a.q + row * a.ldq + c0;
@@ -210,7 +192,9 @@ __device__ __forceinline__ void put_fp8(const RmsArgs<T>& a, long long row, cons
 __device__ __forceinline__ float rstd_of(float sum, int cols, float eps) { return __frsqrt_rn(__fdiv_rn(sum, (float)cols) + eps); }
 
 // NU units a warp, the row in registers.  blockDim: a row's warps, or with one
-// warp a row, several rows.  whole: all of the warp's units lie inside the row.
+// warp a row, several rows.  whole: all of the warp's units lie inside the row
+// (without this twin the rows of single values, with four comparisons a unit,
+// took half as long again).
 template <typename T, int V, int NU>
 __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int warp, int lane, float* part, bool whole) {
   Unit<T, V> u[NU];
@@ -243,7 +227,7 @@ __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int 
     for (int i = 0; i < NU; ++i) {
       uint64_t y[2];
       u[i].pairs(y);
-      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd);
       Unit<T, V> o;
       o.set(y);
       o.store(a.y + row * a.ldy, c0 + i * UNIT, lane, a.cols, whole);
@@ -256,7 +240,7 @@ __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int 
     for (int i = 0; i < NU; ++i) {
       uint64_t y[2];
       u[i].pairs(y);
-      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd);
       const uint32_t m = amax_of(y);
       mine = lane == i ? m : mine;
     }
@@ -266,7 +250,7 @@ __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int 
     for (int i = 0; i < NU; ++i) {
       uint64_t y[2];
       u[i].pairs(y);
-      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd, whole);
+      outputs<T, V>(a, y, c0 + i * UNIT, lane, rstd);
       put_fp8<T, V>(a, row, y, c0 + i * UNIT, lane, __shfl_sync(0xffffffffu, inv, i), whole);
     }
   }
@@ -297,11 +281,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_long(const RmsArgs<T> a)
   for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
     Unit<T, V> u, t;
     uint64_t v[2];
-    u.load(a.x + row * a.ldx, (int)c, lane, a.cols, false);
+    u.load(a.x + row * a.ldx, (int)c, lane, a.cols);
     if (a.r) {
-      t.load(a.r + row * a.ldr, (int)c, lane, a.cols, false);
+      t.load(a.r + row * a.ldr, (int)c, lane, a.cols);
       u.add(t);
-      u.store(a.h + row * a.ldh, (int)c, lane, a.cols, false);
+      u.store(a.h + row * a.ldh, (int)c, lane, a.cols);
     }
     u.pairs(v);
     ptx::fma2_to(ss[0], v[0], v[0]);
@@ -314,17 +298,17 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_long(const RmsArgs<T> a)
   for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
     Unit<T, V> u;
     uint64_t y[2];
-    u.load(h, (int)c, lane, a.cols, false);
+    u.load(h, (int)c, lane, a.cols);
     u.pairs(y);
-    outputs<T, V>(a, y, (int)c, lane, rstd, false);
+    outputs<T, V>(a, y, (int)c, lane, rstd);
     if (a.q) {
       const float s = scale_of(amax_of(y));
       if (lane == 0) a.scale[c / UNIT * a.rows + row] = s;
-      put_fp8<T, V>(a, row, y, (int)c, lane, __frcp_rn(s), false);
+      put_fp8<T, V>(a, row, y, (int)c, lane, __frcp_rn(s));
     }
     if (a.y) {
       u.set(y);
-      u.store(a.y + row * a.ldy, (int)c, lane, a.cols, false);
+      u.store(a.y + row * a.ldy, (int)c, lane, a.cols);
     }
   }
 }
@@ -343,22 +327,28 @@ struct GradArgs {
   bool wide;
 };
 
-// Copies one lane's part of a unit to its own slot of shared memory, by the
-// bytes that the alignment allows (single bf16 values go through registers).
-template <typename T, int V>
-__device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int lane, int cols, bool whole) {
+// Copies a lane's part of NU units of a row to its own slots of shared memory,
+// `pitch` bytes apart, by the bytes that the alignment allows (single bf16 values
+// go through registers, all of the row's before the first is stored).
+template <typename T, int V, int NU>
+__device__ __forceinline__ void fetch(uint32_t slot, uint32_t pitch, const T* row, int c0, int lane, int cols, bool whole) {
   if constexpr (sizeof(T) * V >= 4) {
     constexpr int BYTES = (int)sizeof(T) * V;
 #pragma unroll
-    for (int i = 0; i < 4 / V; ++i) {
-      const int c = c0 + Unit<T, V>::first(i, lane);
-      const int left = whole ? BYTES : min(max(cols - c, 0), V) * (int)sizeof(T);
-      ptx::cp_async_zfill<BYTES>(slot + i * BYTES, row + (whole || left ? c : 0), left);
-    }
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int i = 0; i < 4 / V; ++i) {
+        const int c = c0 + u * UNIT + Unit<T, V>::first(i, lane);
+        const bool in = whole || c < cols;
+        ptx::cp_async_zfill<BYTES>(slot + u * pitch + i * BYTES, row + (in ? c : 0), in ? BYTES : 0);
+      }
   } else {
-    Unit<T, V> u;
-    u.load(row, c0, lane, cols, whole);
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot), "r"(u.w[0]), "r"(u.w[1]) : "memory");
+    Unit<T, V> u[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) u[i].load(row, c0 + i * UNIT, lane, cols, whole);
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot + i * pitch), "r"(u[i].w[0]), "r"(u[i].w[1]) : "memory");
   }
 }
 
@@ -422,12 +412,9 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (ahead + r < a.rows) {
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-          fetch<T, V>(to + r * rb + i * UB, hp + r * a.ldh, c0 + i * UNIT, lane, a.cols, whole);
-          fetch<T, V>(to + r * rb + (NU + i) * UB, dp + r * a.lddy, c0 + i * UNIT, lane, a.cols, whole);
-          if (a.dh) fetch<T, V>(to + r * rb + (2 * NU + i) * UB, tp + r * a.lddh, c0 + i * UNIT, lane, a.cols, whole);
-        }
+        fetch<T, V, NU>(to + r * rb, UB, hp + r * a.ldh, c0, lane, a.cols, whole);
+        fetch<T, V, NU>(to + r * rb + NU * UB, UB, dp + r * a.lddy, c0, lane, a.cols, whole);
+        if (a.dh) fetch<T, V, NU>(to + r * rb + 2 * NU * UB, UB, tp + r * a.lddh, c0, lane, a.cols, whole);
       }
     }
     hp += step * a.ldh;
@@ -439,7 +426,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
   for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
   uint64_t g[NU][2];
 #pragma unroll
-  for (int i = 0; i < NU; ++i) gammas<V>(g[i], a.gamma, c0 + i * UNIT, lane, a.cols, a.wide, whole);
+  for (int i = 0; i < NU; ++i) gammas<V>(g[i], a.gamma, c0 + i * UNIT, lane, a.cols, a.wide);
   T* out = a.dx ? a.dx + first * a.lddx : nullptr;
   int turn = 0, at = 0;
   for (long long row = first; row < a.rows; row += step, turn ^= 1) {
@@ -550,16 +537,27 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_dot(const GradArgs<T> a,
   const long long row = blockIdx.x;
   const float rstd = __ldg(a.rstd + row);
   uint64_t dot = 0;
-  for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
-    Unit<T, V> h, d;
-    uint64_t x[2], y[2], g[2];
-    h.load(a.h + row * a.ldh, (int)c, lane, a.cols, false);
-    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols, false);
-    h.pairs(x);
-    d.pairs(y);
-    gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide, false);
+  for (long long at = (long long)warp * UNIT; at < a.cols; at += 4 * kMaxWarps * UNIT) {
+    Unit<T, V> h[4], d[4];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) ptx::fma2_to(dot, ptx::mul2(y[e], ptx::mul2(x[e], both(rstd))), g[e]);
+    for (int j = 0; j < 4; ++j) {
+      const long long c = at + j * (kMaxWarps * UNIT);
+      if (c < a.cols) {
+        h[j].load(a.h + row * a.ldh, (int)c, lane, a.cols);
+        d[j].load(a.dy + row * a.lddy, (int)c, lane, a.cols);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long c = at + j * (kMaxWarps * UNIT);
+      if (c >= a.cols) break;
+      uint64_t x[2], y[2], g[2];
+      h[j].pairs(x);
+      d[j].pairs(y);
+      gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) ptx::fma2_to(dot, ptx::mul2(y[e], ptx::mul2(x[e], both(rstd))), g[e]);
+    }
   }
   const float sum = row_sum(sum_of(dot), kMaxWarps, warp, lane, part);
   if (threadIdx.x == 0) dots[row] = sum / (float)a.cols;
@@ -572,31 +570,42 @@ __global__ void __launch_bounds__(8 * 32) k_rms_strip(const GradArgs<T> a, const
   const long long c = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * UNIT;
   if (c >= a.cols) return;
   uint64_t g[2], acc[2] = {0, 0};
-  gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide, false);
-#pragma unroll 4
-  for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
-    const float rstd = __ldg(a.rstd + row), dot = dots ? dots[row] : 0.f;
-    Unit<T, V> h, d;
-    uint64_t x[2], y[2];
-    h.load(a.h + row * a.ldh, (int)c, lane, a.cols, false);
-    d.load(a.dy + row * a.lddy, (int)c, lane, a.cols, false);
-    h.pairs(x);
-    d.pairs(y);
+  gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide);
+  for (long long row0 = blockIdx.y; row0 < a.rows; row0 += 4ll * gridDim.y) {
+    Unit<T, V> h[4], d[4], t[4];  // four rows' loads together
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint64_t n = ptx::mul2(x[e], both(rstd));
-      ptx::fma2_to(acc[e], y[e], n);
-      x[e] = ptx::mul2(both(rstd), ptx::fma2(n, both(-dot), ptx::mul2(g[e], y[e])));
+    for (int j = 0; j < 4; ++j) {
+      const long long row = row0 + (long long)j * gridDim.y;
+      if (row < a.rows) {
+        h[j].load(a.h + row * a.ldh, (int)c, lane, a.cols);
+        d[j].load(a.dy + row * a.lddy, (int)c, lane, a.cols);
+        if (a.dh) t[j].load(a.dh + row * a.lddh, (int)c, lane, a.cols);
+      }
     }
-    if (!a.dx) continue;
-    if (a.dh) {
-      d.load(a.dh + row * a.lddh, (int)c, lane, a.cols, false);
-      d.pairs(y);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+    for (int j = 0; j < 4; ++j) {
+      const long long row = row0 + (long long)j * gridDim.y;
+      if (row >= a.rows) break;
+      const float rstd = __ldg(a.rstd + row), dot = dots ? dots[row] : 0.f;
+      uint64_t x[2], y[2];
+      h[j].pairs(x);
+      d[j].pairs(y);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint64_t n = ptx::mul2(x[e], both(rstd));
+        ptx::fma2_to(acc[e], y[e], n);
+        x[e] = ptx::mul2(both(rstd), ptx::fma2(n, both(-dot), ptx::mul2(g[e], y[e])));
+      }
+      if (!a.dx) continue;
+      if (a.dh) {
+        t[j].pairs(y);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+      }
+      Unit<T, V> o;
+      o.set(x);
+      o.store(a.dx + row * a.lddx, (int)c, lane, a.cols);
     }
-    h.set(x);
-    h.store(a.dx + row * a.lddx, (int)c, lane, a.cols, false);
   }
   if (a.part) {
     const float2 f[2] = {ptx::unpack2(acc[0]), ptx::unpack2(acc[1])};
@@ -635,6 +644,7 @@ __global__ void __launch_bounds__(1024) k_rms_fold(const float* part, int rows, 
 int units_per_warp(long long rows, int cols, int most, int warps) {
   const int units = cdiv(cols, UNIT);
   if (cdiv(units, most) > warps) return 0;
+  while (most > 1 && most / 2 >= units) most /= 2;
   for (int nu = most; nu > 1; nu /= 2) {
     if (rows * cdiv(units, nu) >= 2432) return nu;
     if (cdiv(units, nu / 2) > warps) return nu;
@@ -645,12 +655,12 @@ constexpr int kOwnRows = 8;      // rows a block with one warp a row
 constexpr int kGradRows = 128;   // rows whose terms of dgamma one thread adds up in a row
 constexpr int kFwdUnits = 8;
 
-// The vector that every array's rows are aligned for.
+// The vector that every array's rows are aligned for and the columns fill.
 template <typename T, typename... P>
-int vector_of(const P&... p) {
+int vector_of(int cols, const P&... p) {
   auto all = [&](int bytes) { return ((!p.first || rows_aligned(p.first, p.second, sizeof(T), bytes)) && ...); };
-  if (all(4 * (int)sizeof(T))) return 4;
-  return sizeof(T) == 2 && all(4) ? 2 : 1;
+  if (cols % 4 == 0 && all(4 * (int)sizeof(T))) return 4;
+  return sizeof(T) == 2 && cols % 2 == 0 && all(4) ? 2 : 1;
 }
 template <typename T, typename F>
 auto with_vector(int v, F f) {
@@ -664,7 +674,7 @@ bool wide_of(const float* gamma) { return reinterpret_cast<uintptr_t>(gamma) % 1
 template <typename T>
 ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
   using P = std::pair<const void*, long long>;
-  const int v = vector_of<T>(P{a.x, a.ldx}, P{a.r, a.ldr}, P{a.h, a.ldh}, P{a.y, a.ldy});
+  const int v = vector_of<T>(a.cols, P{a.x, a.ldx}, P{a.r, a.ldr}, P{a.h, a.ldh}, P{a.y, a.ldy});
   const int nu = units_per_warp(a.rows, a.cols, kFwdUnits, kMaxWarps);
   const double bytes = (double)a.rows * a.cols * (sizeof(T) * (1 + (a.r ? 2 : 0) + (a.y ? 1 : 0)) + (a.q ? 1 : 0));
   a.wide = wide_of(a.gamma);
@@ -691,8 +701,8 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 
 // The gradient's blocks: as many an SM as 512 threads (128 registers each) and
 // two sets of rows in shared memory allow, and at most kGradRows rows a thread.
-// Two rows a set where they fit; the rest of the shared memory deepens the
-// queue.  (Sized for three arrays whether dh is there or not, so that the
+// Two rows a set where that costs no block; the rest of the shared memory deepens
+// the queue.  (Sized for three arrays whether dh is there or not, so that the
 // workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
 struct GradPlan {
@@ -700,10 +710,11 @@ struct GradPlan {
 };
 GradPlan grad_plan(int rows, int cols, int esize) {
   GradPlan p{};
-  // four units a warp, or eight where four do not reach
-  p.nu = units_per_warp(rows, cols, 4, kGradWarps);
-  if (!p.nu) p.nu = units_per_warp(rows, cols, 8, kGradWarps);
+  // four units a warp, or eight where four do not reach or their warps leave a
+  // quarter of an SM's empty
   const int units = cdiv(cols, UNIT);
+  p.nu = units_per_warp(rows, cols, 4, kGradWarps);
+  if (!p.nu || (p.nu == 4 && kGradWarps % cdiv(units, 4) > kGradWarps / 4)) p.nu = units_per_warp(rows, cols, 8, kGradWarps);
   int row = 0, threads = 0;
   if (p.nu) {
     p.warps = cdiv(units, p.nu);
@@ -714,8 +725,10 @@ GradPlan grad_plan(int rows, int cols, int esize) {
   }
   long long fill;
   if (p.nu) {
-    p.set = 4 * row <= kGradSmem ? 2 : 1;
-    const int room = std::max(1, std::min(kGradWarps * 32 / threads, kGradSmem / (2 * p.set * row)));
+    const int most = kGradWarps * 32 / threads;
+    auto room_of = [&](int set) { return std::max(1, std::min(most, kGradSmem / (2 * set * row))); };
+    p.set = 4 * row <= kGradSmem && room_of(2) == room_of(1) ? 2 : 1;
+    const int room = room_of(p.set);
     p.depth = std::max(1, std::min(4, kGradSmem / (room * p.set * row)));
     fill = 152ll * room;
   } else {
@@ -737,7 +750,7 @@ long long grad_bytes(int rows, int cols, int esize) {
 template <typename T>
 ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
   using P = std::pair<const void*, long long>;
-  const int v = vector_of<T>(P{a.dy, a.lddy}, P{a.h, a.ldh}, P{a.dh, a.lddh}, P{a.dx, a.lddx});
+  const int v = vector_of<T>(a.cols, P{a.dy, a.lddy}, P{a.h, a.ldh}, P{a.dh, a.lddh}, P{a.dx, a.lddx});
   const GradPlan p = grad_plan(a.rows, a.cols, (int)sizeof(T));
   a.warps = p.warps;
   a.depth = p.depth;
