@@ -1082,6 +1082,36 @@ def fp8_selftest_wait(timeout_us: int, stream=None):
 
 
 # ------------------------------------------------- RMS norm, log-probabilities, clipping
+# (These calls take a few us of host time in all, so buffers come from the
+# shortest way there is to one on the current device: size, stride, type.)
+try:
+    _new_cuda = torch._C._dynamo.guards._empty_strided_cuda
+except AttributeError:
+    def _new_cuda(size, stride, dtype):
+        return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
+
+
+def _place(stream, index, used):
+    """The stream of a call on device `index`, the current one, and what makes its dense buffers, as _on's."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index), _new_cuda
+    dev = torch.device("cuda", index)
+    on, empty = _on(stream, dev, *used)
+    if empty is torch.empty:
+        return on, _new_cuda
+    return on, lambda size, stride, dtype: empty(size, dtype=dtype, device=dev)
+
+
+@functools.lru_cache(maxsize=4096)
+def _dense(shape):
+    """Size and strides of a dense tensor, as plain tuples."""
+    stride, n = [], 1
+    for d in reversed(shape):
+        stride.append(n)
+        n *= max(d, 1)
+    return tuple(shape), tuple(reversed(stride))
+
+
 def _matrix_sizes(x, what):
     """rows, last dimension and row stride of x seen as a matrix [rows, last dimension]."""
     shape = x.shape
@@ -1099,35 +1129,43 @@ def _rms_workspace(rows, cols):
     return lib().ff_rms_norm_workspace(rows, cols)
 
 
+@functools.lru_cache(maxsize=4096)
+def _fp8_shapes(rows, k):
+    """Sizes and strides of an Fp8Matrix in row blocks."""
+    return (rows, (k + 15) & ~15), ((k + 15) & ~15, 1), ((k + 127) // 128, rows), (max(rows, 1), 1)
+
+
 def _rms_norm(x, gamma, residual, eps, out, h, fp8, stream):
-    prec, dev = _prec(x, "x"), x.device
+    prec, dev, dt = _prec(x, "x"), x.device, x.dtype
     rows, cols, ldx = _matrix_sizes(x, "x")
-    on, empty = _on(stream, dev, x, gamma, residual, out, h)
+    on, new = _place(stream, dev.index, (x, gamma, residual, out, h))
     ldr = ldh = ldy = 0
-    if residual is None:
-        if h is not None:
-            raise ValueError("h goes with a residual (without one it is x)")
-        kept, ph = x, None
-    else:
-        ldr = _like(residual, x, "residual")
+    pr = ph = py = pq = ps = None
+    kept = x
+    if residual is not None:
+        ldr, pr = _like(residual, x, "residual"), residual.data_ptr()
         if h is None:
-            h, ldh = empty(x.shape, dtype=x.dtype, device=dev), cols
+            kept, ldh = new(*_dense(x.shape), dt), cols
         else:
-            ldh = _like(h, x, "h")
-        kept, ph = h, h.data_ptr()
+            kept, ldh = h, _like(h, x, "h")
+        ph = kept.data_ptr()
+    elif h is not None:
+        raise ValueError("h goes with a residual (without one it is x)")
     if fp8:
-        out, py = _fp8_new(empty, rows, cols, False, dev), None
+        out = object.__new__(Fp8Matrix)
+        q, qs, s, ss = _fp8_shapes(rows, cols)
+        out.q, out.scale = new(q, qs, torch.float8_e4m3fn), new(s, ss, torch.float32)
+        out.rows, out.k, out.tile = rows, cols, False
         pq, ps = out.q.data_ptr(), out.scale.data_ptr()
     else:
         if out is None:
-            out, ldy = empty(x.shape, dtype=x.dtype, device=dev), cols
+            out, ldy = new(*_dense(x.shape), dt), cols
         else:
             ldy = _like(out, x, "out")
-        py, pq, ps = out.data_ptr(), None, None
-    rstd = empty((rows,), dtype=torch.float32, device=dev)
-    _check(lib().ff_rms_norm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, rows, cols,
-                             _vector(gamma, cols, "gamma", dev), eps, prec, ph, ldh, py, ldy, pq, ps, rstd.data_ptr(), on),
-           "ff_rms_norm")
+        py = out.data_ptr()
+    rstd = new((rows,), (1,), torch.float32)
+    _check(lib().ff_rms_norm(x.data_ptr(), ldx, pr, ldr, rows, cols, _vector(gamma, cols, "gamma", dev), eps, prec, ph, ldh, py,
+                             ldy, pq, ps, rstd.data_ptr(), on), "ff_rms_norm")
     if (x.requires_grad or (gamma is not None and gamma.requires_grad)
             or (residual is not None and residual.requires_grad)):
         _unrecorded("rms_norm_fp8" if fp8 else "rms_norm", depth=5)
@@ -1160,18 +1198,18 @@ def rms_norm_backward(dy, h, rstd, gamma, dh=None, out=None, stream=None):
     be dy, h or dh."""
     prec, dev = _prec(dy, "dy"), dy.device
     rows, cols, lddy = _matrix_sizes(dy, "dy")
-    on, empty = _on(stream, dev, dy, h, rstd, gamma, dh, out)
+    on, new = _place(stream, dev.index, (dy, h, rstd, gamma, dh, out))
     ldh = _like(h, dy, "h")
     lddh = 0 if dh is None else _like(dh, dy, "dh")
     if rstd is None:
         raise ValueError("rstd of the forward pass is needed")
     if out is None:
-        out, lddx = empty(dy.shape, dtype=dy.dtype, device=dev), cols
+        out, lddx = new(*_dense(dy.shape), dy.dtype), cols
     else:
         lddx = _like(out, dy, "out")
-    dgamma = empty((cols,), dtype=torch.float32, device=dev)
+    dgamma = new((cols,), (1,), torch.float32)
     need = _rms_workspace(rows, cols)
-    ws = empty((need,), dtype=torch.uint8, device=dev) if need > 0 else None
+    ws = new((need,), (1,), torch.uint8) if need > 0 else None
     _check(lib().ff_rms_norm_backward(dy.data_ptr(), lddy, h.data_ptr(), ldh, rows, cols, _vector(rstd, rows, "rstd", dev),
                                       _vector(gamma, cols, "gamma", dev), None if dh is None else dh.data_ptr(), lddh, prec,
                                       out.data_ptr(), lddx, dgamma.data_ptr(), None if ws is None else ws.data_ptr(), need,
@@ -1210,18 +1248,18 @@ def label_logprobs(logits, labels, top: int = 0, stream=None):
     top = int(top)
     if not 0 <= top <= min(32, classes):
         raise ValueError("top must be 0 .. min(32, classes)")
-    on, empty = _on(stream, dev, logits, labels)
+    on, new = _place(stream, dev.index, (logits, labels))
+    f32 = torch.float32
     r = object.__new__(LabelLogprobs)
-    pl, pp = None, None
-    r.logp = None
+    pl = pp = r.logp = None
     if labels is not None:
         pl = _labels(labels, rows, dev)
-        r.logp = empty((rows,), dtype=torch.float32, device=dev)
+        r.logp = new((rows,), (1,), f32)
         pp = r.logp.data_ptr()
-    r.entropy = empty((rows,), dtype=torch.float32, device=dev)
-    r.top_logp = empty((rows, top), dtype=torch.float32, device=dev)
-    r.top_index = empty((rows, top), dtype=torch.int32, device=dev)
-    r.stats = empty((rows, 2), dtype=torch.float32, device=dev)
+    r.entropy = new((rows,), (1,), f32)
+    r.top_logp = new((rows, top), (top or 1, 1), f32)
+    r.top_index = new((rows, top), (top or 1, 1), torch.int32)
+    r.stats = new((rows, 2), (2, 1), f32)
     _check(lib().ff_label_logprobs(logits.data_ptr(), ld, rows, classes, prec, pl, pp, r.entropy.data_ptr(), top,
                                    r.top_logp.data_ptr(), r.top_index.data_ptr(), r.stats.data_ptr(), on),
            "ff_label_logprobs")
@@ -1244,9 +1282,9 @@ def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy
         raise ValueError("dlogp needs the labels")
     if dentropy is not None and entropy is None:
         raise ValueError("dentropy needs the forward pass's entropy")
-    on, empty = _on(stream, dev, logits, labels, stats, dlogp, entropy, dentropy, out)
+    on, new = _place(stream, dev.index, (logits, labels, stats, dlogp, entropy, dentropy, out))
     if out is None:
-        out, ldo = empty(logits.shape, dtype=logits.dtype, device=dev), classes
+        out, ldo = new(*_dense(logits.shape), logits.dtype), classes
     else:
         ldo = _like(out, logits, "out")
     _check(lib().ff_label_logprobs_backward(
@@ -1272,40 +1310,38 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     n = len(grads)
     if n == 0 or not isinstance(grads[0], torch.Tensor):
         raise ValueError("grads must be a non-empty list of tensors")
-    dev = grads[0].device
     index = grads[0].get_device()
     if index < 0:
         raise ValueError("grads must be CUDA tensors")
     if index != torch._C._cuda_getDevice():
-        with torch.cuda.device(dev):
+        with torch.cuda.device(index):
             return clip_grad_norm(grads, max_norm, out, stream)
     try:
         kinds = [_PREC[g.dtype] for g in grads]
-        fits = all([g.is_contiguous() and g.get_device() == index for g in grads])
+        for g in grads:
+            if g.get_device() != index or not g.is_contiguous():
+                raise AttributeError
+        ptrs = [g.data_ptr() for g in grads]
     except KeyError:
         raise TypeError("grads must be torch.bfloat16 or torch.float32") from None
     except AttributeError:
-        fits = False
-    if not fits:
-        raise ValueError(f"grads must be contiguous tensors on {dev}")
-    into = grads
+        raise ValueError(f"grads must be contiguous tensors on cuda:{index}") from None
+    to = ptrs
     if out is not None:
-        into = list(out)
-        if len(into) != n:
+        out = list(out)
+        if len(out) != n:
             raise ValueError("out must have a tensor for each of grads")
-        for o, g in zip(into, grads):
-            if (not isinstance(o, torch.Tensor) or o.dtype is not g.dtype or o.get_device() != index or o.shape != g.shape
+        for o, g in zip(out, grads):
+            if (not isinstance(o, torch.Tensor) or o.shape != g.shape or o.dtype is not g.dtype or o.get_device() != index
                     or not o.is_contiguous()):
                 raise ValueError("out must match grads in shape, type and device, and be contiguous")
-    if stream is None:
-        on, empty = torch._C._cuda_getCurrentRawStream(index), torch.empty
-    else:
-        on, empty = _on(stream, dev, *grads, *into)
+        to = [o.data_ptr() for o in out]
+    on, new = _place(stream, index, () if stream is None else (*grads, *(out or ())))
     A, K, need = _clip_arrays(n)
-    host = A(*[g.data_ptr() for g in grads], *[o.data_ptr() for o in into], *[g.numel() for g in grads])
+    host = A(*ptrs, *to, *[g.numel() for g in grads])
     at = ctypes.addressof(host)
-    norm = empty((1,), dtype=torch.float32, device=dev)
-    ws = empty((need,), dtype=torch.uint8, device=dev)
+    norm = new((1,), (1,), torch.float32)
+    ws = new((need,), (1,), torch.uint8)
     _check(lib().ff_clip_grad_norm(at, at + 8 * n, at + 16 * n, K(*kinds), n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
                                    on), "ff_clip_grad_norm")
     return norm
@@ -1333,11 +1369,17 @@ class Fp4Matrix:
         return self.q.get_device()
 
 
-def _fp4_new(empty, rows, k, dev):
+@functools.lru_cache(maxsize=4096)
+def _fp4_shapes(rows, k):
+    """Sizes and strides of an Fp4Matrix."""
+    stride, tiles = (k + 31) // 32 * 16, ((rows + 127) // 128, (k + 127) // 128, 32, 4, 4)
+    return ((rows, stride), (stride, 1)) + _dense(tiles)
+
+
+def _fp4_new(new, rows, k):
+    q, qs, s, ss = _fp4_shapes(rows, k)
     m = object.__new__(Fp4Matrix)
-    m.q = empty((rows, (k + 31) // 32 * 16), dtype=torch.uint8, device=dev)
-    m.scale = empty(((rows + 127) // 128, (k + 127) // 128, 32, 4, 4), dtype=torch.uint8, device=dev)
-    m.rows, m.k = rows, k
+    m.q, m.scale, m.rows, m.k = new(q, qs, torch.uint8), new(s, ss, torch.uint8), rows, k
     return m
 
 
@@ -1346,16 +1388,18 @@ def _fp4_quantize(x, straight, transposed, stream):
     prec = _prec(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be [rows, k] with k >= 1")
-    dev = x.device
     rows, k, ldx = _matrix_sizes(x, "x")
     if transposed and rows < 1:
         raise ValueError("the transpose needs at least one row")
-    on, empty = _on(stream, dev, x)
-    a = _fp4_new(empty, rows, k, dev) if straight else None
-    t = _fp4_new(empty, k, rows, dev) if transposed else None
-    _check(lib().ff_fp4_quantize(x.data_ptr(), ldx, rows, k, prec, a.q.data_ptr() if a else None,
-                                 a.scale.data_ptr() if a else None, t.q.data_ptr() if t else None,
-                                 t.scale.data_ptr() if t else None, on), "ff_fp4_quantize")
+    on, new = _place(stream, x.get_device(), (x,))
+    a = t = pa = sa = pt = st = None
+    if straight:
+        a = _fp4_new(new, rows, k)
+        pa, sa = a.q.data_ptr(), a.scale.data_ptr()
+    if transposed:
+        t = _fp4_new(new, k, rows)
+        pt, st = t.q.data_ptr(), t.scale.data_ptr()
+    _check(lib().ff_fp4_quantize(x.data_ptr(), ldx, rows, k, prec, pa, sa, pt, st, on), "ff_fp4_quantize")
     if x.requires_grad:
         _unrecorded("fp4_quantize", depth=5)
     return a, t
@@ -1379,19 +1423,19 @@ def fp4_dequantize(m, out=None, out_dtype=torch.bfloat16, stream=None):
     exactly, in out_dtype (torch.bfloat16 or torch.float32) or out's type."""
     if not isinstance(m, Fp4Matrix):
         raise TypeError("m must be a Fp4Matrix")
-    dev = m.q.device
-    on, empty = _on(stream, dev, m.q, m.scale, out)
+    rows, k = m.rows, m.k
+    on, new = _place(stream, m.q.get_device(), (m.q, m.scale, out))
     if out is None:
         prec = _PREC.get(out_dtype)
         if prec is None:
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-        out, ldy = empty((m.rows, m.k), dtype=out_dtype, device=dev), m.k
+        out, ldy = new((rows, k), (k, 1), out_dtype), k
     else:
-        if out.shape != (m.rows, m.k):
+        if out.shape != (rows, k):
             raise ValueError("out must be [rows, k]")
-        _same_device(out, dev, "out")
+        _same_device(out, m.q.device, "out")
         prec, ldy = _prec(out, "out"), _row_stride_of(out, "out")
-    _check(lib().ff_fp4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), m.rows, m.k, prec, out.data_ptr(), ldy, on),
+    _check(lib().ff_fp4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), rows, k, prec, out.data_ptr(), ldy, on),
            "ff_fp4_dequantize")
     return out
 
@@ -1408,13 +1452,13 @@ def fp4_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
         raise ValueError("a and b must have the same k")
     dev = a.q.device
     _same_device(b.q, dev, "b")
-    on, empty = _on(stream, dev, a.q, a.scale, b.q, b.scale, bias, out, status)
+    on, new = _place(stream, dev.index, (a.q, a.scale, b.q, b.scale, bias, out, status))
     m, n = a.rows, b.rows
     if out is None:
         prec = _PREC.get(out_dtype)
         if prec is None:
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-        out, ldc = empty((m, n), dtype=out_dtype, device=dev), n
+        out, ldc = new((m, n), (n or 1, 1), out_dtype), n
     else:
         if out.shape != (m, n):
             raise ValueError("out must be [a.rows, b.rows]")
