@@ -708,8 +708,10 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 
 // The gradient's blocks: as many an SM as 512 threads (128 registers each) and
 // two sets of rows in shared memory allow, and at most kGradRows rows a thread.
-// Two rows a set where that costs no block; the rest of the shared memory deepens
-// the queue.  (Sized for three arrays whether dh is there or not, so that the
+// Two rows a set where that leaves two blocks an SM or costs none (16384 x 2000 fp32: 88
+// us, one a set 108); of rows that fill an SM alone with eight units a warp, two
+// without a queue (2097 x 16000 bf16: 62 us, one with a queue 70).  The rest of the shared
+// memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
 // workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
 struct GradPlan {
@@ -734,7 +736,8 @@ GradPlan grad_plan(int rows, int cols, int esize) {
   if (p.nu) {
     const int most = kGradWarps * 32 / threads;
     auto room_of = [&](int set) { return std::max(1, std::min(most, kGradSmem / (2 * set * row))); };
-    p.set = 4 * row <= kGradSmem && room_of(2) == room_of(1) ? 2 : 1;
+    const bool queued = 4 * row <= kGradSmem && (room_of(2) >= 2 || room_of(2) == room_of(1));
+    p.set = queued || (p.nu == 8 && most == 1 && 2 * row <= kGradSmem) ? 2 : 1;
     const int room = room_of(p.set);
     p.depth = std::max(1, std::min(4, kGradSmem / (room * p.set * row)));
     fill = 152ll * room;
