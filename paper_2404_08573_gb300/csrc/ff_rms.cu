@@ -131,14 +131,18 @@ __device__ __forceinline__ float sum_of(uint64_t v) {
   return f.x + f.y;
 }
 
-// The sum over a row's warps of v, in a fixed order; `part` holds two rows'
-// worth of [kMaxWarps] in turn (one barrier a row).
+// The warps of one row meet.  A named barrier, since warps come to it from either
+// twin of the code below (a block-wide one has to be one place for all threads).
+__device__ __forceinline__ void row_barrier(int warps) { ptx::named_bar(1, warps * 32); }
+
+// The sum over a row's warps of v, in a fixed order, through part[kMaxWarps]
+// (not used again before the row's warps have met once more).
 __device__ __forceinline__ float row_sum(float v, int warps, int warp, int lane, float* part) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   if (warps == 1) return v;
   if (lane == 0) part[warp] = v;
-  __syncthreads();
+  row_barrier(warps);
   v = lane < warps ? part[lane] : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -268,7 +272,6 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const RmsArgs<T> a) {
   const int warp = a.warps == 1 ? 0 : w;
   const long long row = a.warps == 1 ? (long long)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
   if (row >= a.rows) return;
-  // (both calls meet at the same barrier)
   if ((warp + 1) * NU * UNIT <= a.cols)
     rms_row<T, V, NU>(a, row, warp, lane, part, true);
   else
@@ -385,7 +388,7 @@ __device__ __forceinline__ void row_sums(float (&v)[R], int warps, int warp, int
     for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (warps > 1) {
       if (i == 0) part[r][warp] = s;
-      __syncthreads();
+      row_barrier(warps);
       s = i < warps ? part[r][i] : 0.f;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -505,7 +508,6 @@ __global__ void __launch_bounds__(kGradWarps * 32) k_rms_grad(const GradArgs<T> 
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
   const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2) * NU * 32 + lane) * (uint32_t)sizeof(Held<T>);
-  // (both calls meet at the same barriers)
   if (c0 + NU * UNIT <= a.cols)
     grad_rows<T, V, NU, R>(a, acc, slots, teams, team, warp, lane, part, true);
   else
@@ -708,7 +710,7 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 
 // The gradient's blocks: as many an SM as 512 threads (128 registers each) and
 // two sets of rows in shared memory allow, and at most kGradRows rows a thread.
-// Two rows a set where that leaves two blocks an SM or costs none (16384 x 2000 fp32: 88
+// Two rows a set where that leaves two blocks an SM or costs none (16384 x 2000 fp32: 85
 // us, one a set 108); of rows that fill an SM alone with eight units a warp, two
 // without a queue (2097 x 16000 bf16: 62 us, one with a queue 70).  The rest of the shared
 // memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
