@@ -646,7 +646,8 @@ FF_API ff_status ff_fp8_selftest_wait(unsigned int timeout_us, void* stream);
  * quantized as ff_fp8_quantize does, from fp32.  Either may be NULL, not both.
  * gamma [cols] fp32, NULL: ones.  h is required with a residual and NULL
  * without.  rstd [rows] fp32 or NULL.  y may be x or the residual itself, and
- * so may h (but not both the same).  Squares are formed in fp32: magnitudes past
+ * so may h (but not both the same); where they share values in another way the
+ * call is refused.  Squares are formed in fp32: magnitudes past
  * 2^63 overflow (rstd is then 0); a NaN in a row makes the whole row NaN. */
 FF_API ff_status ff_rms_norm(const void* x, long long ldx, const void* residual, long long ldr, int rows, int cols,
                              const float* gamma, float eps, ff_precision prec, void* h, long long ldh, void* y,
@@ -660,8 +661,8 @@ FF_API long long ff_rms_norm_workspace(int rows, int cols);
  * rstd.  With n = h rstd and du = gamma dy, and <.> the average over a row:
  *   dx = rstd (du - n <du n>) + dh,   dgamma = sum over rows of dy n.
  * dx is the gradient of x and of the residual alike; dh [rows, cols] is what
- * the residual stream hands back, or NULL.  dx may be dy, h or dh itself; dx or
- * dgamma [cols] fp32 may be NULL.  Sums have a fixed order.  No rows: dgamma
+ * the residual stream hands back, or NULL.  dx may be dy, h or dh itself, but may
+ * not share values with them in another way; dx or dgamma [cols] fp32 may be NULL.  Sums have a fixed order.  No rows: dgamma
  * is set to zero. */
 FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy, const void* h, long long ldh, int rows, int cols,
                                       const float* rstd, const float* gamma, const void* dh, long long lddh,
@@ -686,7 +687,8 @@ FF_API ff_status ff_label_logprobs(const void* logits, long long ld, int rows, i
 /* Its gradient, from the forward call's logits, labels and stats:
  *   dx = dlogp (1[label] - p) - dentropy p (ln p + entropy)
  * dlogp, dentropy [rows] fp32 or NULL (none); dentropy needs the forward call's
- * entropy, dlogp the labels.  dlogits (type prec) may be the logits.  A row of
+ * entropy, dlogp the labels.  dlogits (type prec) may be the logits (else none of
+ * their values).  A row of
  * which nothing is asked (no label or dlogp 0, and dentropy 0) gets zeros,
  * whatever its logits hold. */
 FF_API ff_status ff_label_logprobs_backward(const void* logits, long long ld, int rows, int classes, ff_precision prec,

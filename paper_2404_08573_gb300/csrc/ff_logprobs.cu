@@ -686,7 +686,8 @@ extern "C" FF_API ff_status ff_label_logprobs_backward(const void* logits, long 
   const int es = prec == FF_BF16 ? 2 : 4;
   if (!logits || !dlogits || !stats || !aligned(logits, es) || !aligned(dlogits, es) || !aligned(stats, 8) ||
       ((ld < classes || lddx < classes) && rows > 1) || (dlogp && !labels) || (dentropy && !entropy) || !aligned(labels, 4) ||
-      !aligned(dlogp, 4) || !aligned(entropy, 4) || !aligned(dentropy, 4))
+      !aligned(dlogp, 4) || !aligned(entropy, 4) || !aligned(dentropy, 4) ||
+      !apart_or_one(dlogits, lddx, logits, ld, rows, classes, es))
     return FF_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto run = [&](auto t) {

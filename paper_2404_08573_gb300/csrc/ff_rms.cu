@@ -843,8 +843,10 @@ extern "C" FF_API ff_status ff_rms_norm(const void* x, long long ldx, const void
   const int es = prec == FF_BF16 ? 2 : 4;
   if (!x || (residual == nullptr) != (h == nullptr) || (q == nullptr) != (scale == nullptr) || (!y && !q) ||
       !matrix_ok(x, ldx, rows, cols, es) || !matrix_ok(residual, ldr, rows, cols, es) ||
-      !matrix_ok(h, ldh, rows, cols, es) || !matrix_ok(y, ldy, rows, cols, es) || (y && y == h) || !aligned(q, 16) ||
-      !aligned(scale, 4) || !aligned(gamma, 4) || !aligned(rstd, 4))
+      !matrix_ok(h, ldh, rows, cols, es) || !matrix_ok(y, ldy, rows, cols, es) || !aligned(q, 16) || !aligned(scale, 4) ||
+      !aligned(gamma, 4) || !aligned(rstd, 4) || !apart(y, ldy, h, ldh, rows, cols, es) ||
+      !apart_or_one(y, ldy, x, ldx, rows, cols, es) || !apart_or_one(y, ldy, residual, ldr, rows, cols, es) ||
+      !apart_or_one(h, ldh, x, ldx, rows, cols, es) || !apart_or_one(h, ldh, residual, ldr, rows, cols, es))
     return FF_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto run = [&](auto t) {
@@ -892,7 +894,9 @@ extern "C" FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy,
   const long long need = ff_rms_norm_workspace(rows, cols);
   if (!dy || !h || !rstd || !matrix_ok(dy, lddy, rows, cols, es) || !matrix_ok(h, ldh, rows, cols, es) ||
       !matrix_ok(dh, lddh, rows, cols, es) || !matrix_ok(dx, lddx, rows, cols, es) || !aligned(rstd, 4) ||
-      !aligned(gamma, 4) || (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))))
+      !aligned(gamma, 4) || (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) ||
+      !apart_or_one(dx, lddx, dy, lddy, rows, cols, es) || !apart_or_one(dx, lddx, h, ldh, rows, cols, es) ||
+      !apart_or_one(dx, lddx, dh, lddh, rows, cols, es))
     return FF_ERR_INVALID_ARG;
   auto run = [&](auto t) {
     using T = decltype(t);

@@ -64,4 +64,23 @@ inline bool rows_aligned(const void* p, long long ld, int esize, int bytes) {
   return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (ld * esize) % bytes == 0;
 }
 
+// Whether two matrices of the same sizes (either may be null) share no value:
+// one ends before the other begins, or with one row stride they lie side by
+// side in each other's gaps.
+inline bool apart(const void* p, long long ldp, const void* q, long long ldq, int rows, int cols, int esize) {
+  if (!p || !q) return true;
+  if (rows <= 1) ldp = ldq = cols;
+  const unsigned long long a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q), es = (unsigned)esize;
+  const unsigned long long wide = cols * es, below = (unsigned long long)(rows - 1);
+  if (a + below * ldp * es + wide <= b || b + below * ldq * es + wide <= a) return true;
+  if (ldp != ldq) return false;
+  const unsigned long long ld = ldp * es, off = (a > b ? a - b : b - a) % ld;
+  return off >= wide && off + wide <= ld;
+}
+// The same for a matrix that is written element by element where the other has
+// been read: the two may also be one.
+inline bool apart_or_one(const void* p, long long ldp, const void* q, long long ldq, int rows, int cols, int esize) {
+  return (p == q && (ldp == ldq || rows <= 1)) || apart(p, ldp, q, ldq, rows, cols, esize);
+}
+
 }  // namespace ff

@@ -170,6 +170,25 @@ def test_in_place_and_inside_larger_buffers(cols):
         assert all(bool((t == 7.0).all()) for t in bufs)
 
 
+def test_matrices_side_by_side_in_one_buffer():
+    torch = torch_cuda()
+    ff = lib_ready()
+    cols = 500
+    x, r, dy = (data(torch, 37, cols, torch.bfloat16, 0, 0, s) for s in (1, 2, 3))
+    gamma = gamma_of(torch, cols, 1)
+    y, h, rstd = ff.rms_norm(x, gamma, residual=r)
+    wide = torch.zeros(37, 4 * cols, dtype=torch.bfloat16, device="cuda")
+    a, b, c, d = (wide[:, i * cols:(i + 1) * cols] for i in range(4))
+    a.copy_(x), b.copy_(r)
+    ff.rms_norm(a, gamma, residual=b, out=d, h=c)
+    assert torch.equal(c, h) and torch.equal(d, y) and torch.equal(a, x) and torch.equal(b, r)
+    dx, dg = ff.rms_norm_backward(dy, h, rstd, gamma)
+    a.copy_(dy)
+    assert ff.rms_norm_backward(a, c, rstd, gamma, out=b)[0] is b and torch.equal(b, dx) and torch.equal(c, h)
+    with pytest.raises(ff.FFError):
+        ff.rms_norm(a, gamma, out=wide[:, 4:cols + 4])
+
+
 def test_rows_that_are_not_finite_and_rows_of_zeros():
     torch = torch_cuda()
     ff = lib_ready()

@@ -80,6 +80,19 @@ def test_label_logprobs_backward_refuses(L, bad):
     assert logprobs_grad(L, **bad) == BAD
 
 
+# rows of 8 bf16 values are 16 bytes: two rows at P end at P + 32 (apart by 16: 48)
+@pytest.mark.parametrize("call,shared", [
+    (rms, dict(y=P + 16)), (rms, dict(y=P + 2)), (rms, dict(y=P, ldy=16)), (rms, dict(x=P, ldx=16, y=P + 8, ldy=16)),
+    (rms, dict(x=P, ldx=16, y=P + 30, ldy=16)), (rms, dict(rows=1, y=P + 8)),
+    (rms, dict(x=P + 4096, r=P, h=P + 16, y=P + 8192)), (rms, dict(x=P, r=P + 4096, h=P + 16, y=P + 8192)),
+    (rms, dict(x=P + 4096, r=P, h=P + 8192, y=P + 16)), (rms, dict(x=P + 4096, r=P + 8192, h=P, y=P + 16)),
+    (rms, dict(x=P, ldx=16, r=P + 4096, h=P, ldh=8, y=P + 8192)), (rms_grad, dict(dx=P + 16, h=P + 4096)),
+    (rms_grad, dict(dy=P + 4096, dx=P + 16)), (rms_grad, dict(dy=P + 4096, h=P + 8192, dh=P + 16)), (rms_grad, dict(lddx=16)),
+    (logprobs_grad, dict(dx=P + 16)), (logprobs_grad, dict(lddx=16)), (logprobs_grad, dict(ld=16, dx=P + 14, lddx=16))])
+def test_outputs_that_share_values_in_part_are_refused(L, call, shared):
+    assert call(L, **shared) == BAD
+
+
 def test_empty_logprobs(L):
     assert logprobs(L, rows=0, x=None) == OK and logprobs_grad(L, rows=0, x=None, dx=None, stats=None) == OK
 
