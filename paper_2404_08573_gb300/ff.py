@@ -17,6 +17,7 @@ passes, ``clip_grad_norm``, ``fp4_quantize``, ``fp4_dequantize`` and
 
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import inspect
@@ -1295,9 +1296,8 @@ def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy
 
 
 @functools.lru_cache(maxsize=256)
-def _clip_arrays(n):
-    """Types of the call's host arrays (pointers in, out and counts in one; types) and the workspace's bytes."""
-    return c_longlong * (3 * n), c_int * n, lib().ff_clip_grad_norm_workspace(n)
+def _clip_workspace(n):
+    return lib().ff_clip_grad_norm_workspace(n)
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
@@ -1318,13 +1318,12 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
             return clip_grad_norm(grads, max_norm, out, stream)
     try:
         kinds = [_PREC[g.dtype] for g in grads]
-        for g in grads:
-            if g.get_device() != index or not g.is_contiguous():
-                raise AttributeError
-        ptrs = [g.data_ptr() for g in grads]
+        if set(map(torch.Tensor.get_device, grads)) != {index} or not all(map(torch.Tensor.is_contiguous, grads)):
+            raise AttributeError
+        ptrs, counts = list(map(torch.Tensor.data_ptr, grads)), list(map(torch.Tensor.numel, grads))
     except KeyError:
         raise TypeError("grads must be torch.bfloat16 or torch.float32") from None
-    except AttributeError:
+    except (AttributeError, TypeError):
         raise ValueError(f"grads must be contiguous tensors on cuda:{index}") from None
     to = ptrs
     if out is not None:
@@ -1337,12 +1336,13 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
                 raise ValueError("out must match grads in shape, type and device, and be contiguous")
         to = [o.data_ptr() for o in out]
     on, new = _place(stream, index, () if stream is None else (*grads, *(out or ())))
-    A, K, need = _clip_arrays(n)
-    host = A(*ptrs, *to, *[g.numel() for g in grads])
-    at = ctypes.addressof(host)
+    need = _clip_workspace(n)
+    # (the array module's: ctypes' own arrays take four times as long to fill, 15 us for 60 tensors)
+    host, types = array.array("q", ptrs + to + counts), array.array("i", kinds)
+    at = host.buffer_info()[0]
     norm = new((1,), (1,), torch.float32)
     ws = new((need,), (1,), torch.uint8)
-    _check(lib().ff_clip_grad_norm(at, at + 8 * n, at + 16 * n, K(*kinds), n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
+    _check(lib().ff_clip_grad_norm(at, at + 8 * n, at + 16 * n, types.buffer_info()[0], n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
                                    on), "ff_clip_grad_norm")
     return norm
 
