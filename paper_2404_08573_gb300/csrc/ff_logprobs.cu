@@ -136,6 +136,24 @@ struct Args {
   float2* stats;
 };
 
+__device__ __forceinline__ float nan_value() { return __int_as_float(0x7FC00000); }
+
+// What a row's sums come to.  An empty row, and one with a NaN or +infinity, has
+// no distribution.
+struct Result {
+  float m, s, t, ln;
+  __device__ __forceinline__ Result(float most, float sum, float dsum) : m(sum == 0.f ? -INFINITY : most), s(sum), t(dsum) {
+    ln = sum > 0.f ? logf(sum) : nan_value();
+  }
+  __device__ __forceinline__ float logp(float x) const { return (x - m) - ln; }
+  template <typename T>
+  __device__ __forceinline__ void put(const Args<T>& a, long long row, bool has, float at_label) const {
+    if (a.logp) a.logp[row] = has ? logp(at_label) : 0.f;
+    if (a.entropy) a.entropy[row] = ln - t / s;
+    if (a.stats) a.stats[row] = make_float2(s != s ? nan_value() : m, ln);
+  }
+};
+
 template <typename T>
 struct Load {
   static constexpr int N = 16 / (int)sizeof(T);
@@ -431,19 +449,98 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 5 : 1) k_logprobs(con
     }
   }
   if (rank != 0 || warp != 0) return;
-  // an empty row, and one with a NaN or +infinity, has no distribution
-  const bool none = !(f.s > 0.f);
-  const float nan = __int_as_float(0x7FC00000), m = f.s == 0.f ? -INFINITY : f.m;
-  const float ln = none ? nan : logf(f.s);
-  if (lane == 0) {
-    if (a.logp) a.logp[row] = has ? (at_label - m) - ln : 0.f;
-    if (a.entropy) a.entropy[row] = ln - f.t / f.s;
-    if (a.stats) a.stats[row] = make_float2(f.s != f.s ? nan : m, ln);
-  }
+  const Result r(f.m, f.s, f.t);
+  if (lane == 0) r.put(a, row, has, at_label);
   if (TOP && lane < a.top) {
     const bool got = key != 0ull;
     a.top_index[row * a.top + lane] = got ? (int)(0xFFFFFFFFu - (uint32_t)key) : lane;
-    a.top_logp[row * a.top + lane] = got ? (unordered((uint32_t)(key >> 32)) - m) - ln : nan;
+    a.top_logp[row * a.top + lane] = got ? r.logp(unordered((uint32_t)(key >> 32))) : nan_value();
+  }
+}
+
+// Rows of up to 32 E classes: 2^lanes_log lanes a row (32 if E > 1), lane l with
+// the classes l, l + 32, ..  The likeliest: a class's place is the number of larger
+// ones, counted over the row's keys in shared memory, four a load.  Bound by latency
+// and, with many rows, by this counting: bf16, 11562 x 8, top 1: 2.4 us (by a warp a row
+// below 11.5); 60000 x 10: 6.2 (26), with top 8 9.5 (58); 16384 x 64, top 8: 13 (20);
+// 16384 x 100: 4.7 (8.9), but with top 8 29 (19), so that rows with the likeliest
+// classes wanted come here up to 64.
+template <typename T, bool TOP, int E>
+__global__ void __launch_bounds__(256) k_logprobs_short(const Args<T> a, int lanes_log) {
+  ptx::griddep_wait();
+  const int lanes = 1 << lanes_log, l = threadIdx.x & (lanes - 1);
+  const long long row = (long long)blockIdx.x * (256 >> lanes_log) + (threadIdx.x >> lanes_log);
+  const bool in = row < a.rows;  // (lanes without a row take part in the shuffles)
+  const T* p = a.x + (in ? row : 0) * a.ldx;
+  int label = -1;
+  if (a.labels && in) label = __ldg(a.labels + row);
+  float x[E], m = kLowest;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    x[e] = -INFINITY;
+    if (in && l + 32 * e < a.classes) {
+      float one[1];
+      Vec<T, 1>::unpack(Vec<T, 1>::load(p + l + 32 * e), one);
+      x[e] = one[0];
+    }
+    m = fmaxf(m, x[e]);
+  }
+  for (int o = lanes >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float d = max_nan(x[e] - m, kFar), y = exp2_approx(d * kLog2e);
+    s += y;
+    t += y * d;
+  }
+  for (int o = lanes >> 1; o > 0; o >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    t += __shfl_xor_sync(0xffffffffu, t, o);
+  }
+  const Result r(m, s, t);
+  const bool has = label >= 0 && label < a.classes;
+  float at_label = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float v = __shfl_sync(0xffffffffu, x[e], label & (lanes - 1), lanes);
+    if (e == label >> 5) at_label = v;
+  }
+  if (l == 0 && in) r.put(a, row, has, at_label);
+  if constexpr (TOP) {
+    // Of classes in other sets a comparison knows which comes first; in a class's own
+    // set the equal ones are all counted, and those from itself on taken off again.
+    __shared__ __align__(16) uint32_t keys[256 * E];
+    uint32_t* const to = keys + (threadIdx.x & ~31u) * E;
+    const int lane = threadIdx.x & 31, row0 = lane - l;
+    // the row's lanes from this one on
+    const uint32_t rest = (lanes == 32 ? 0xFFFFFFFFu : ((1u << lanes) - 1u) << row0) >> lane << lane;
+    uint32_t mine[E];
+    int place[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      mine[e] = l + 32 * e < a.classes ? ordered(x[e]) : 0u;
+      to[32 * e + lane] = mine[e];
+      place[e] = -__popc(__match_any_sync(0xffffffffu, mine[e]) & rest);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int f = 0; f < E; ++f) {
+      const uint4* from = reinterpret_cast<const uint4*>(to + 32 * f + row0);
+      for (int n = min(lanes, a.classes - 32 * f); n > 0; n -= 4, ++from) {
+        const uint4 o = *from;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (f <= e) place[e] += (o.x >= mine[e]) + (o.y >= mine[e]) + (o.z >= mine[e]) + (o.w >= mine[e]);
+          else place[e] += (o.x > mine[e]) + (o.y > mine[e]) + (o.z > mine[e]) + (o.w > mine[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (!in || l + 32 * e >= a.classes || place[e] >= a.top) continue;
+      a.top_index[row * a.top + place[e]] = l + 32 * e;
+      a.top_logp[row * a.top + place[e]] = r.logp(unordered(mine[e]));
+    }
   }
 }
 
@@ -487,7 +584,7 @@ __device__ __forceinline__ uint64_t grad_of(const Row& r, uint64_t x) {
   }
 }
 
-// Bound by HBM: 4096 x 65536 bf16 with entropy 167 us, 0.95 of the floor at the copy
+// Bound by HBM: 4096 x 65536 bf16 with entropy 157 us, the floor at the copy
 // rate (on single values and with one load in flight a thread 186).
 // WIDE: both rows lie alike to 16 bytes, and all but their ends go as vectors.
 template <typename T, bool WIDE>
@@ -594,9 +691,25 @@ cudaError_t launch(const Args<T>& a, unsigned grid, unsigned threads, cudaStream
   return cudaLaunchKernelEx(&cfg, k_logprobs<T, TOP, WARPS>, a);
 }
 
+template <typename T, bool TOP, int E>
+cudaError_t launch_short(const Args<T>& a, cudaStream_t st) {
+  int lanes_log = 2;
+  while (lanes_log < 5 && (1 << lanes_log) < a.classes) ++lanes_log;
+  PdlLaunch l(dim3((unsigned)cdiv(a.rows, 256 >> lanes_log)), dim3(256), st);
+  return cudaLaunchKernelEx(&l.cfg, k_logprobs_short<T, TOP, E>, a, lanes_log);
+}
+
 template <typename T>
 ff_status logprobs_t(Args<T> a, cudaStream_t st) {
   constexpr int N = Load<T>::N;
+  const double bytes = (double)a.rows * a.classes * sizeof(T);
+  if (a.classes <= (a.top ? 64 : 128)) {
+    const int each = cdiv(a.classes, 32);
+    auto* const go = a.top ? (each == 1 ? launch_short<T, true, 1> : launch_short<T, true, 2>)
+                           : (each == 1 ? launch_short<T, false, 1> : each == 2 ? launch_short<T, false, 2> : launch_short<T, false, 4>);
+    FF_LAUNCH(K_LOGPROBS, bytes, st, go(a, st), "label log-probabilities");
+    return FF_OK;
+  }
   const int vecs = cdiv(a.classes, N);
   // Short rows take a warp each (few rows only if it has two rounds of loads at
   // most).  Others a block of 8 warps; with fewer rows
@@ -613,7 +726,6 @@ ff_status logprobs_t(Args<T> a, cudaStream_t st) {
   const unsigned threads = a.warps == 1 ? kOwnRows * 32 : (unsigned)a.warps * 32;
   const long long grid = a.warps == 1 ? cdiv(a.rows, kOwnRows) : (long long)a.rows * a.cluster;
   if (grid > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
-  const double bytes = (double)a.rows * a.classes * sizeof(T);
   auto* const go = a.warps > 8 ? (a.top ? launch<T, true, kMostWarps> : launch<T, false, kMostWarps>)
                                : (a.top ? launch<T, true, 8> : launch<T, false, 8>);
   FF_LAUNCH(K_LOGPROBS, bytes, st, go(a, (unsigned)grid, threads, st), "label log-probabilities");
@@ -626,9 +738,17 @@ ff_status grad_t(GradArgs<T> a, cudaStream_t st) {
   const bool wide = (reinterpret_cast<uintptr_t>(a.x) - reinterpret_cast<uintptr_t>(a.dx)) % 16 == 0 &&
                     (a.rows == 1 || (a.ldx - a.lddx) * (long long)sizeof(T) % 16 == 0);
   const int units = wide ? cdiv(a.classes, N) : a.classes;
-  a.team = 32;
-  while (a.team < 256 && a.team * 4 <= units) a.team *= 2;
-  a.segments = std::max(1, cdiv(units, (long long)a.team * (wide ? 8 : 16)));
+  // As few threads a row as leave each 16 loads (16384 x 500 bf16: 7.4 us, with 4 loads 13),
+  // and 16 loads a segment, or half of that and so on down to two while the
+  // blocks are fewer than 2.5 an SM (4096 x 65536: 157 us, with 8 loads 167; but 500 x 8000
+  // fp32: 7.5 us with 16, 6.6 with 8; 1 x 131072: 2.0 with 2, 2.8 with 8).  Single
+  // values count half.
+  a.team = 8;
+  while (a.team < 256 && a.team * 16 <= units) a.team *= 2;
+  for (int loads = 16; loads >= 2; loads /= 2) {
+    a.segments = std::max(1, cdiv(units, (long long)a.team * loads * (wide ? 1 : 2)));
+    if ((long long)a.rows * a.segments * a.team >= 380ll * 256) break;
+  }
   const long long blocks = ((long long)a.rows * a.segments + 256 / a.team - 1) / (256 / a.team);
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = 2.0 * a.rows * a.classes * sizeof(T);

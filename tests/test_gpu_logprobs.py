@@ -111,6 +111,53 @@ def test_ties_go_to_the_lowest_index():
                 assert torch.equal(ff.label_logprobs(x.to(dt), None, top=32).top_index.long(), want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("classes", [1, 2, 3, 4, 5, 8, 9, 16, 17, 31, 32, 33, 48, 63, 64, 65, 97, 128, 129])
+def test_short_rows(classes, dtype):
+    """Several rows a warp: labels everywhere, rows of few values, masks that leave less than `top`, and rows
+    without a distribution beside proper ones."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator().manual_seed(classes)
+    rows = 2 * classes + 75
+    x = torch.randn(rows, classes, generator=gen) * 3
+    x[::3] = x[::3].round()
+    x[1::4][torch.rand(len(x[1::4]), classes, generator=gen) < 0.6] = float("-inf")
+    labels = torch.arange(rows, dtype=torch.int32) % (classes + 2) - 1
+    x[torch.arange(rows), labels.clamp(0, classes - 1).long()] = 0.5
+    x[40] = float("-inf")
+    x[41, classes // 2] = float("nan")
+    x[42, classes - 1] = float("inf")
+    x = x.to(dt).cuda()
+    labels = labels.cuda()
+    proper = torch.tensor([r for r in range(rows) if not 40 <= r < 43], device="cuda")
+    logp, entropy, m, ln, p, lp, d, has, e_ln, e_h = definition(torch, x[proper], labels[proper], classes)
+    order = torch.sort(x.double() + 0.0, dim=1, descending=True, stable=True).indices
+    for top in sorted({0, 1, min(3, classes), min(32, classes)}):
+        r = ff.label_logprobs(x, labels, top=top)
+        assert bool(((r.logp[proper].double() - logp).abs() <= torch.where(has, e_ln + 2 * U * (logp.abs() + ln), 0.0)).all())
+        assert bool(((r.entropy[proper].double() - entropy).abs() <= e_h).all())
+        assert torch.equal(r.stats[proper, 0].double(), m) and bool(((r.stats[proper, 1].double() - ln).abs() <= e_ln).all())
+        assert torch.equal(r.top_index[proper].long(), order[proper, :top])
+        want = lp.gather(1, order[proper, :top])
+        got, tol = r.top_logp[proper].double(), e_ln[:, None] + 2 * U * (want.abs() + ln[:, None])
+        assert bool(((got == want) | ((got - want).abs() <= tol)).all())
+        odd = slice(40, 43)
+        assert bool(r.entropy[odd].isnan().all()) and bool(r.stats[odd, 1].isnan().all()) and bool(r.top_logp[odd].isnan().all())
+        assert bool(((r.top_index[odd] >= 0) & (r.top_index[odd] < classes)).all())
+        for one in r.top_index[odd].tolist():
+            assert len(set(one)) == top
+    g = torch.rand(rows, generator=gen).cuda()
+    dx = ff.label_logprobs_backward(x, labels, r.stats, g)[proper].double()
+    a = torch.where(has, g[proper].double(), 0.0)[:, None]
+    q = torch.where(p > 0, (d - r.stats[proper, 1:].double()).exp(), 0.0)
+    want = -q * a
+    want[has, labels[proper][has].long()] += a[has, 0]
+    tol = q * a * (2 * EXP + 4 * U * (d.abs() + ln[:, None]) + 6 * U) + U * a + want.abs() * (torch.finfo(dt).eps / 2)
+    assert bool(((dx - want).abs() <= tol + 2.0 ** -120).all())
+
+
 def test_sorted_rows():
     torch = torch_cuda()
     ff = lib_ready()
