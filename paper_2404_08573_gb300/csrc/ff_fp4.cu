@@ -241,25 +241,50 @@ __global__ void __launch_bounds__(kQThreads)
   const int strip = unit % strips, rj = unit / strips, j0 = rj & 31, rt = rj >> 5;
   const int row0 = rt * QT + j0, c0 = strip * 256 + lane * 8;
   uint32_t v[4][W];
-  const T* p = x + (long long)row0 * ldx + c0;
+  if constexpr (sizeof(T) == 4 && LOAD == 4) {
+    // A lane's own values from rows that only four bytes align would be eight
+    // times the wavefronts (4096 x 8191: 36 us, so 25): the warp loads them side by side.
+    // (bf16, with half the bytes, was not faster so, nor were the tiles above.)
+    __shared__ __align__(16) uint32_t staged[kQThreads / 32][4 * 256];
+    uint32_t* const own = staged[threadIdx.x >> 5];
 #pragma unroll
-  for (int i = 0; i < 4; ++i, p += 32 * ldx) {
-    const bool in = row0 + 32 * i < rows;
-    if (LOAD == 16 && c0 + 8 <= k) {
+    for (int h = 0; h < 4; h += 2) {
+      uint32_t t[16];
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        const int r = row0 + (h + n / 8) * 32, c = strip * 256 + n % 8 * 32 + lane;
+        t[n] = r < rows && c < k ? Vec<T, 1>::load(x + (long long)r * ldx + c) : 0u;
+      }
+#pragma unroll
+      for (int n = 0; n < 16; ++n) own[(h * 8 + n) * 32 + lane] = t[n];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < W / 4; ++j)
-        *reinterpret_cast<uint4*>(&v[i][4 * j]) = in ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
-    } else if (LOAD == 4 && c0 + 8 <= k) {
+        *reinterpret_cast<uint4*>(&v[i][4 * j]) = reinterpret_cast<const uint4*>(own + i * 256 + lane * 8)[j];
+  } else {
+    const T* p = x + (long long)row0 * ldx + c0;
 #pragma unroll
-      for (int j = 0; j < W; ++j) v[i][j] = in ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
-    } else {
+    for (int i = 0; i < 4; ++i, p += 32 * ldx) {
+      const bool in = row0 + 32 * i < rows;
+      if (LOAD == 16 && c0 + 8 <= k) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        uint32_t w = 0;
+        for (int j = 0; j < W / 4; ++j)
+          *reinterpret_cast<uint4*>(&v[i][4 * j]) = in ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
+      } else if (LOAD == 4 && c0 + 8 <= k) {
 #pragma unroll
-        for (int h = 0; h < PER; ++h)
-          if (in && c0 + j * PER + h < k) w |= (uint32_t)Vec<T, 1>::load(p + j * PER + h) << (16 * h);
-        v[i][j] = w;
+        for (int j = 0; j < W; ++j) v[i][j] = in ? reinterpret_cast<const uint32_t*>(p)[j] : 0u;
+      } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          uint32_t w = 0;
+#pragma unroll
+          for (int h = 0; h < PER; ++h)
+            if (in && c0 + j * PER + h < k) w |= (uint32_t)Vec<T, 1>::load(p + j * PER + h) << (16 * h);
+          v[i][j] = w;
+        }
       }
     }
   }
@@ -291,61 +316,69 @@ __device__ __forceinline__ float scale_value(uint32_t field) {  // 2^(field - 12
   return __uint_as_float(field == 0u ? 0x00400000u : field == 255u ? 0x7FC00000u : field << 23);
 }
 
+// The values of a unit of N columns from its N / 2 bytes.
+template <int N>
+__device__ __forceinline__ void unit_values(float (&v)[N], uint32_t w, float s) {
+#pragma unroll
+  for (int h = 0; h < N / 2; ++h) {
+    const float2 t = e2m1x2_values(w >> (8 * h));
+    v[2 * h] = t.x * s;
+    v[2 * h + 1] = t.y * s;
+  }
+}
+struct DequantArgs {
+  const uint8_t *q, *scale;
+  int rows, k, ldq, ktiles;
+  long long ldy;
+  int lanes_log, strips, groups;
+};
+
 // y = value * scale, exact in either type.  A thread takes the same unit of
 // columns of rows j, j + 32, j + 64 and j + 96 of a scale tile, with their loads in
 // flight together: their scales come with one load.  A block of 256 covers
 // 2^lanes_log units side by side and the rest of its threads' j.  WIDE: y's rows
-// are 16-byte aligned and a unit is 8 columns; else one column.  (Rows one after
+// are 16-byte aligned and a unit is that many; else one column.  (Rows one after
 // the other, each with its own scale load, left it bound by the instructions of
-// their addresses: 4096 x 8192 to bf16 13.5 us, now 11.7, at 7.2 TB/s HBM's.)
+// their addresses: 4096 x 8192 to bf16 13.5 us, now 11.7, at 7.2 TB/s HBM's.  To fp32
+// 24; with units of 8 there, stores of half sectors, 34.)
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256)
-    k_fp4_dequantize(const uint8_t* q, const uint8_t* scale, int rows, int k, int ldq, int ktiles, T* y, long long ldy, int lanes_log,
-                     int strips, int groups) {
+__global__ void __launch_bounds__(256) k_fp4_dequantize(const DequantArgs a, T* y) {
+  constexpr int UNIT = WIDE ? 16 / (int)sizeof(T) : 1;
   ptx::griddep_wait();
-  const int lanes = 1 << lanes_log, per = 256 >> lanes_log;
-  const int strip = blockIdx.x % strips, g = blockIdx.x / strips;
-  const int j = g % groups * per + (threadIdx.x >> lanes_log), rt = g / groups;
+  const int lanes = 1 << a.lanes_log, per = 256 >> a.lanes_log;
+  const int strip = blockIdx.x % a.strips, g = blockIdx.x / a.strips;
+  const int j = g % a.groups * per + (threadIdx.x >> a.lanes_log), rt = g / a.groups;
   const long long row0 = (long long)rt * QT + j;
-  const long long c = ((long long)strip * lanes + (threadIdx.x & (lanes - 1))) * (WIDE ? 8 : 1);
-  if (c >= k || row0 >= rows) return;
-  const uint8_t* p = q + row0 * ldq + c / 2;
+  const long long c = ((long long)strip * lanes + (threadIdx.x & (lanes - 1))) * UNIT;
+  if (c >= a.k || row0 >= a.rows) return;
+  const uint8_t* p = a.q + row0 * a.ldq + c / 2;
   uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i, p += 32ll * ldq) {
+  for (int i = 0; i < 4; ++i, p += 32ll * a.ldq) {
     w[i] = 0u;
-    if (row0 + 32 * i < rows) w[i] = WIDE ? __ldg(reinterpret_cast<const uint32_t*>(p)) : (uint32_t)__ldg(p);
+    if (row0 + 32 * i < a.rows)
+      w[i] = UNIT == 8   ? __ldg(reinterpret_cast<const uint32_t*>(p))
+             : UNIT == 4 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p))
+                         : (uint32_t)__ldg(p);
   }
-  const uint4 s4 = __ldg(reinterpret_cast<const uint4*>(scale + ((long long)rt * ktiles + c / QT) * kFp4ScaleTile + j * 16));
+  const uint4 s4 = __ldg(reinterpret_cast<const uint4*>(a.scale + ((long long)rt * a.ktiles + c / QT) * kFp4ScaleTile + j * 16));
   const uint32_t fields[4] = {s4.x, s4.y, s4.z, s4.w};
   const int shift = (int)(c / kFp4Block & 3) * 8;
-  T* to = y + row0 * ldy + c;
+  T* to = y + row0 * a.ldy + c;
 #pragma unroll
-  for (int i = 0; i < 4; ++i, to += 32 * ldy) {
-    if (row0 + 32 * i >= rows) break;
+  for (int i = 0; i < 4; ++i, to += 32 * a.ldy) {
+    if (row0 + 32 * i >= a.rows) break;
     const float s = scale_value(fields[i] >> shift & 0xFFu);
     if constexpr (WIDE) {
-      float v[8];
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float2 t = e2m1x2_values(w[i] >> (8 * h));
-        v[2 * h] = t.x * s;
-        v[2 * h + 1] = t.y * s;
-      }
-      if (c + 8 <= k) {
-        constexpr int N = 16 / (int)sizeof(T);
-#pragma unroll
-        for (int h = 0; h < 8; h += N) {
-          float t[N];
-#pragma unroll
-          for (int e = 0; e < N; ++e) t[e] = v[h + e];
-          Vec<T, N>::store(to + h, t);
-        }
+      float v[UNIT];
+      unit_values<UNIT>(v, w[i], s);
+      if (c + UNIT <= a.k) {
+        Vec<T, UNIT>::store(to, v);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < UNIT; ++e) {
           const float one[1] = {v[e]};
-          if (c + e < k) Vec<T, 1>::store(to + e, one);
+          if (c + e < a.k) Vec<T, 1>::store(to + e, one);
         }
       }
     } else {
@@ -354,6 +387,61 @@ __global__ void __launch_bounds__(256)
       Vec<T, 1>::store(to, one);
     }
   }
+}
+
+// The same where y's rows are not 16-byte aligned and there are many: units of 8
+// columns (2^lanes_log <= 32 of them), which a warp passes through shared memory,
+// so that its stores of STORE bytes lie side by side: 4096 x 8191 to bf16 32 us, 4095 x
+// 8190 22, to fp32 32; a value a thread 55 each.  (But 154 x 1789 3.0 for 1.7: a
+// million values divide them.)
+template <typename T, int STORE>
+__global__ void __launch_bounds__(256) k_fp4_dequantize_staged(const DequantArgs a, T* y) {
+  constexpr int A = STORE / (int)sizeof(T), N = 16 / (int)sizeof(T);  // values a store; and a staging store
+  __shared__ __align__(16) T staged[256 / 32][4][256];
+  ptx::griddep_wait();
+  const int lane = threadIdx.x & 31, lanes = 1 << a.lanes_log, per = 256 >> a.lanes_log, wide_log = a.lanes_log + 3;
+  const int strip = blockIdx.x % a.strips, g = blockIdx.x / a.strips;
+  const int j = g % a.groups * per + (threadIdx.x >> a.lanes_log), rt = g / a.groups;
+  const long long row0 = (long long)rt * QT + j, c0 = (long long)strip << wide_log;
+  const long long c = c0 + (threadIdx.x & (lanes - 1)) * 8;
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  uint4 s4 = make_uint4(0, 0, 0, 0);
+  if (c < a.k && row0 < a.rows) {
+    const uint8_t* p = a.q + row0 * a.ldq + c / 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i, p += 32ll * a.ldq)
+      if (row0 + 32 * i < a.rows) w[i] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    s4 = __ldg(reinterpret_cast<const uint4*>(a.scale + ((long long)rt * a.ktiles + c / QT) * kFp4ScaleTile + j * 16));
+  }
+  const uint32_t fields[4] = {s4.x, s4.y, s4.z, s4.w};
+  const int shift = (int)(c / kFp4Block & 3) * 8;
+  auto& own = staged[threadIdx.x >> 5];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v[8];
+    unit_values<8>(v, w[i], scale_value(fields[i] >> shift & 0xFFu));
+#pragma unroll
+    for (int h = 0; h < 8; h += N) {
+      float t[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) t[e] = v[h + e];
+      Vec<T, N>::store(&own[i][lane * 8 + h], t);
+    }
+  }
+  __syncwarp();
+  // the warp's 256 values of each i: 2^wide_log columns of one row or of several
+  const int j0 = g % a.groups * per + ((threadIdx.x & ~31) >> a.lanes_log);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int n = 0; n < 256 / 32 / A; ++n) {
+      const int at = (n * 32 + lane) * A;
+      const long long row = (long long)rt * QT + 32 * i + j0 + (at >> wide_log), col = c0 + (at & ((1 << wide_log) - 1));
+      if (row >= a.rows || col >= a.k) continue;
+      T* const to = y + row * a.ldy + col;
+      if (col + A <= a.k) *reinterpret_cast<typename Vec<T, A>::Raw*>(to) = *reinterpret_cast<const typename Vec<T, A>::Raw*>(&own[i][at]);
+      else *to = own[i][at];
+    }
 }
 
 template <typename T>
@@ -386,22 +474,24 @@ ff_status quantize_t(const T* x, long long ldx, int rows, int k, uint8_t* q, uin
 
 template <typename T>
 ff_status dequantize_t(const uint8_t* q, const uint8_t* scale, int rows, int k, T* y, long long ldy, cudaStream_t st) {
-  const bool wide = rows_aligned(y, rows > 1 ? ldy : 0, sizeof(T), 16);
-  const int units = wide ? cdiv(k, 8) : k;
-  int lanes_log = 3;
-  while (lanes_log < 8 && (1 << lanes_log) < units) ++lanes_log;
-  const int strips = cdiv(units, 1 << lanes_log);
+  if (rows == 1) ldy = 0;
+  const bool wide = rows_aligned(y, ldy, sizeof(T), 16), staged = !wide && (long long)rows * k >= 1 << 20;
+  const int units = wide ? cdiv(k, 16 / (int)sizeof(T)) : staged ? cdiv(k, 8) : k, most = staged ? 5 : 8;
+  DequantArgs a{q, scale, rows, k, fp4_stride(k), cdiv(k, QT), ldy, 3, 0, 0};
+  while (a.lanes_log < most && (1 << a.lanes_log) < units) ++a.lanes_log;
+  a.strips = cdiv(units, 1 << a.lanes_log);
   // (a matrix of less than 32 rows leaves the other j out)
-  const int per = 256 >> lanes_log, groups = rows < QT ? cdiv(std::min(rows, 32), per) : 32 / per;
-  const long long blocks = (long long)strips * cdiv(rows, QT) * groups;
+  const int per = 256 >> a.lanes_log;
+  a.groups = rows < QT ? cdiv(std::min(rows, 32), per) : 32 / per;
+  const long long blocks = (long long)a.strips * cdiv(rows, QT) * a.groups;
   if (blocks > 0x7FFFFFFFll) return FF_ERR_UNSUPPORTED;
   const double bytes = (double)rows * k * (sizeof(T) + 0.5);
   PdlLaunch l(dim3((unsigned)blocks), dim3(256), st);
-  auto go = [&](auto* kernel) {
-    return cudaLaunchKernelEx(&l.cfg, kernel, q, scale, rows, k, fp4_stride(k), cdiv(k, QT), y, ldy, lanes_log, strips, groups);
-  };
-  auto* const kernel = wide ? k_fp4_dequantize<T, true> : k_fp4_dequantize<T, false>;
-  FF_LAUNCH(K_FP4_DEQUANT, bytes, st, go(kernel), "4-bit dequantize");
+  auto* const kernel = wide      ? k_fp4_dequantize<T, true>
+                       : !staged ? k_fp4_dequantize<T, false>
+                       : rows_aligned(y, ldy, sizeof(T), 4) ? k_fp4_dequantize_staged<T, 4>
+                                                            : k_fp4_dequantize_staged<T, sizeof(T)>;
+  FF_LAUNCH(K_FP4_DEQUANT, bytes, st, cudaLaunchKernelEx(&l.cfg, kernel, a, y), "4-bit dequantize");
   return FF_OK;
 }
 

@@ -95,6 +95,32 @@ def test_quantize_bit_for_bit(size, dtype):
             assert bool((buf == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [(5, 641), (33, 2049), (130, 1337), (257, 300), (300, 78), (640, 37), (1030, 1021),
+                                  (40000, 37), (9001, 130)])
+def test_rows_of_every_alignment(size, dtype):
+    torch = torch_cuda()
+    ff = lib_ready()
+    rows, k = size
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.randn(rows, k, generator=torch.Generator().manual_seed(rows)).to(dt)
+    refs = [pack_ref(*quantize_ref(r)) for r in (x.float().numpy(), x.float().numpy().T)]
+    v, e = quantize_ref(x.float().numpy())
+    want = torch.from_numpy((v * np.repeat(2.0 ** e, 32, axis=1))[:, :k]).cuda()
+    for pad, lead in ((0, 0), (1, 0), (2, 2), (3, 1), (4, 4), (8, 8)):
+        xg = strided(torch, x, pad, lead)
+        both = ff.fp4_quantize_both(xg)
+        for got, (q, scale) in ((both[0], refs[0]), (both[1], refs[1]), (ff.fp4_quantize(xg), refs[0])):
+            assert np.array_equal(got.scale.cpu().numpy(), scale) and np.array_equal(got.q.cpu().numpy(), q)
+        for out_dt in (torch.bfloat16, torch.float32):
+            buf = torch.full((lead + rows * (k + pad) + 64,), 7.0, dtype=out_dt, device="cuda")
+            view = buf[lead:lead + rows * (k + pad)].view(rows, -1)[:, :k]
+            ff.fp4_dequantize(both[0], out=view)
+            assert torch.equal(view.double(), want)  # both types hold every value
+            view.fill_(7.0)
+            assert bool((buf == 7.0).all())
+
+
 def test_every_code_and_midpoint():
     torch = torch_cuda()
     ff = lib_ready()
