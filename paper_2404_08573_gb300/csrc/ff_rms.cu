@@ -335,20 +335,34 @@ struct GradArgs {
   bool wide;
 };
 
-// Copies a lane's part of NU units of a row to its own slots of shared memory,
-// `pitch` bytes apart, by the bytes that the alignment allows (single bf16 values
-// go through registers, all of the row's before the first is stored).
+// How a lane's part of NU units of a row lies in the row and in its own slots of
+// shared memory.  V = 8 (bf16, NU even): units in twos of 2 x UNIT columns, a
+// lane's eight values of which are one 16-byte copy, which goes past L1 (8-byte
+// copies go through it, and L1 is what the slots leave: 16384 x 2000 60 us, so 49).
+template <typename T, int V>
+struct Lay {
+  static constexpr int P = V == 8 ? 2 : 1;  // units together
+  static constexpr uint32_t BYTES = P * sizeof(Held<T>), PITCH = 32 * sizeof(Held<T>);  // of a slot; of a unit's slots
+  static __device__ __forceinline__ int col(int i, int e, int lane) {  // of value e of unit i
+    if constexpr (V == 8) return (i & ~1) * UNIT + lane * 8 + (i & 1) * 4 + e;
+    else return i * UNIT + Unit<T, V>::col(e, lane);
+  }
+};
+
+// Copies these by the bytes that the alignment allows (single bf16 values go
+// through registers, all of the row's before the first is stored).
 template <typename T, int V, int NU>
-__device__ __forceinline__ void fetch(uint32_t slot, uint32_t pitch, const T* row, int c0, int lane, int cols, bool whole) {
+__device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int lane, int cols, bool whole) {
+  using L = Lay<T, V>;
   if constexpr (sizeof(T) * V >= 4) {
     constexpr int BYTES = (int)sizeof(T) * V;
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+    for (int u = 0; u < NU; u += L::P)
 #pragma unroll
-      for (int i = 0; i < 4 / V; ++i) {
-        const int c = c0 + u * UNIT + Unit<T, V>::first(i, lane);
+      for (int i = 0; i < 4 * L::P / V; ++i) {
+        const int c = c0 + L::col(u, i * V, lane);
         const bool in = whole || c < cols;
-        ptx::cp_async_zfill<BYTES>(slot + u * pitch + i * BYTES, row + (in ? c : 0), in ? BYTES : 0);
+        ptx::cp_async_zfill<BYTES>(slot + u * L::PITCH + i * BYTES, row + (in ? c : 0), in ? BYTES : 0);
       }
   } else {
     Unit<T, V> u[NU];
@@ -356,22 +370,30 @@ __device__ __forceinline__ void fetch(uint32_t slot, uint32_t pitch, const T* ro
     for (int i = 0; i < NU; ++i) u[i].load(row, c0 + i * UNIT, lane, cols, whole);
 #pragma unroll
     for (int i = 0; i < NU; ++i)
-      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot + i * pitch), "r"(u[i].w[0]), "r"(u[i].w[1]) : "memory");
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot + i * L::PITCH), "r"(u[i].w[0]), "r"(u[i].w[1]) : "memory");
   }
 }
 
-// The unit in a slot.
-__device__ __forceinline__ void read_slot(Held<bf16>& h, uint32_t slot) {
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(h.w[0]), "=r"(h.w[1]) : "r"(slot));
+// The units in a slot.
+__device__ __forceinline__ void read_slot(Held<bf16> (&h)[1], uint32_t slot) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(h[0].w[0]), "=r"(h[0].w[1]) : "r"(slot));
 }
-__device__ __forceinline__ void read_slot(Held<float>& h, uint32_t slot) {
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(h.w[0]), "=f"(h.w[1]), "=f"(h.w[2]), "=f"(h.w[3]) : "r"(slot));
+__device__ __forceinline__ void read_slot(Held<bf16> (&h)[2], uint32_t slot) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(h[0].w[0]), "=r"(h[0].w[1]), "=r"(h[1].w[0]), "=r"(h[1].w[1])
+               : "r"(slot));
 }
-template <typename T>
-__device__ __forceinline__ void slot_pairs(uint64_t (&p)[2], uint32_t slot) {
-  Held<T> h;
+__device__ __forceinline__ void read_slot(Held<float> (&h)[1], uint32_t slot) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(h[0].w[0]), "=f"(h[0].w[1]), "=f"(h[0].w[2]), "=f"(h[0].w[3])
+               : "r"(slot));
+}
+template <typename T, int P>
+__device__ __forceinline__ void slot_pairs(uint64_t (&p)[P][2], uint32_t slot) {
+  Held<T> h[P];
   read_slot(h, slot);
-  h.pairs(p);
+#pragma unroll
+  for (int j = 0; j < P; ++j) h[j].pairs(p[j]);
 }
 
 // The sums over a row's warps of R values (rows), in a fixed order, in every
@@ -404,8 +426,8 @@ __device__ __forceinline__ void row_sums(float (&v)[R], int warps, int warp, int
 // (`depth` sets, each thread its own values, so that no barrier is needed)
 // while these are worked on.  With one warp a row the block's warps take rows of
 // their own and join their sums in shared memory ([warps][cols]).
-// Bound by HBM in fp32 (4096 x 8192 with dh: 93 us, floor 80) and in bf16 by the
-// latency of a set's two halves and the barrier between them (50 us and the fold's
+// Bound by HBM in fp32 (4096 x 8192 with dh: 86 us, floor 80) and in bf16 by the
+// latency of a set's two halves and the barrier between them (42 us and the fold's
 // 5, floor 40).  (gamma read anew each time came from L2, since the copies take
 // L1's place, and one row at a time pays the barrier for each: 60 us in all.)
 template <typename T, int V, int NU, int R>
@@ -414,7 +436,9 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
   const int c0 = warp * NU * UNIT;
   const long long first = ((long long)blockIdx.x * teams + team) * R, step = (long long)gridDim.x * teams * R;
   const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
-  constexpr uint32_t UB = 32 * sizeof(Held<T>);  // bytes of a warp's slots of one unit of one array
+  using L = Lay<T, V>;
+  constexpr uint32_t UB = L::PITCH;
+  constexpr int P = L::P;
   const uint32_t rb = (a.dh ? 3 : 2) * NU * UB;  // of a row
   const uint32_t stage = R * rb * (blockDim.x >> 5);
   long long ahead = first;
@@ -422,9 +446,9 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (ahead + r < a.rows) {
-        fetch<T, V, NU>(to + r * rb, UB, hp + r * a.ldh, c0, lane, a.cols, whole);
-        fetch<T, V, NU>(to + r * rb + NU * UB, UB, dp + r * a.lddy, c0, lane, a.cols, whole);
-        if (a.dh) fetch<T, V, NU>(to + r * rb + 2 * NU * UB, UB, tp + r * a.lddh, c0, lane, a.cols, whole);
+        fetch<T, V, NU>(to + r * rb, hp + r * a.ldh, c0, lane, a.cols, whole);
+        fetch<T, V, NU>(to + r * rb + NU * UB, dp + r * a.lddy, c0, lane, a.cols, whole);
+        if (a.dh) fetch<T, V, NU>(to + r * rb + 2 * NU * UB, tp + r * a.lddh, c0, lane, a.cols, whole);
       }
     }
     hp += step * a.ldh;
@@ -436,13 +460,28 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
   for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
   uint64_t g[NU][2];
 #pragma unroll
-  for (int i = 0; i < NU; ++i) gammas<V>(g[i], a.gamma, c0 + i * UNIT, lane, a.cols, a.wide);
+  for (int i = 0; i < NU; ++i) {
+    if constexpr (V == 8) gammas<4>(g[i], a.gamma, c0 + L::col(i, 0, lane) - lane * 4, lane, a.cols, a.wide);
+    else gammas<V>(g[i], a.gamma, c0 + i * UNIT, lane, a.cols, a.wide);
+  }
   T* out = a.dx ? a.dx + first * a.lddx : nullptr;
   int turn = 0, at = 0;
+  float coming[R];  // the next set's rstd, so that its load is not waited for either (4096 x 8192: 2 us)
+  auto rstds = [&](float (&to)[R], long long row) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) to[r] = row + r < a.rows ? __ldg(a.rstd + row + r) : 0.f;
+  };
+  constexpr bool AHEAD = sizeof(T) * V >= 4;  // (the others have no registers for it and wait for their copies anyway)
+  if constexpr (AHEAD) rstds(coming, first);
   for (long long row = first; row < a.rows; row += step, turn ^= 1) {
     float rstd[R], dot[R];
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) rstd[r] = row + r < a.rows ? __ldg(a.rstd + row + r) : 0.f;
+      for (int r = 0; r < R; ++r) rstd[r] = coming[r];
+      rstds(coming, row + step);
+    } else {
+      rstds(rstd, row);
+    }
     if (a.depth >= 4) ptx::cp_async_wait<3>();
     else if (a.depth == 3) ptx::cp_async_wait<2>();
     else if (a.depth == 2) ptx::cp_async_wait<1>();
@@ -453,16 +492,18 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
       uint64_t dot2 = 0;
       if (row + r < a.rows) {
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-          uint64_t x[2], y[2];
+        for (int i = 0; i < NU; i += P) {
+          uint64_t x[P][2], y[P][2];
           slot_pairs<T>(x, now + r * rb + i * UB);
           slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint64_t yh = ptx::mul2(y[e], x[e]);
-            ptx::fma2_to(acc[i][e], yh, both(rstd[r]));
-            ptx::fma2_to(dot2, yh, g[i][e]);
-          }
+          for (int j = 0; j < P; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint64_t yh = ptx::mul2(y[j][e], x[j][e]);
+              ptx::fma2_to(acc[i + j][e], yh, both(rstd[r]));
+              ptx::fma2_to(dot2, yh, g[i + j][e]);
+            }
         }
       }
       dot[r] = sum_of(dot2);
@@ -473,21 +514,35 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
       if (row + r >= a.rows || !out) break;
       const uint64_t off = both(-dot[r] * a.inv_cols * rstd[r] * rstd[r] * rstd[r]);  // what h is taken off by
 #pragma unroll
-      for (int i = 0; i < NU; ++i) {
+      for (int i = 0; i < NU; i += P) {
         if (!whole && c0 + i * UNIT >= a.cols) break;
-        uint64_t x[2], y[2];
+        uint64_t x[P][2], y[P][2];
         slot_pairs<T>(x, now + r * rb + i * UB);
         slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = ptx::fma2(x[e], off, ptx::mul2(both(rstd[r]), ptx::mul2(g[i][e], y[e])));
+        for (int j = 0; j < P; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            x[j][e] = ptx::fma2(x[j][e], off, ptx::mul2(both(rstd[r]), ptx::mul2(g[i + j][e], y[j][e])));
         if (a.dh) {
           slot_pairs<T>(y, now + r * rb + (2 * NU + i) * UB);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) x[e] = ptx::add2(x[e], y[e]);
+          for (int j = 0; j < P; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[j][e] = ptx::add2(x[j][e], y[j][e]);
         }
-        Unit<T, V> o;
-        o.set(x);
-        o.store(out + r * a.lddx, c0 + i * UNIT, lane, a.cols, whole);
+        if constexpr (V == 8) {
+          Held<T> o[2];
+          o[0].set(x[0]);
+          o[1].set(x[1]);
+          const int c = c0 + L::col(i, 0, lane);
+          if (whole || c < a.cols)
+            *reinterpret_cast<uint4*>(out + r * a.lddx + c) = make_uint4(o[0].w[0], o[0].w[1], o[1].w[0], o[1].w[1]);
+        } else {
+          Unit<T, V> o;
+          o.set(x[0]);
+          o.store(out + r * a.lddx, c0 + i * UNIT, lane, a.cols, whole);
+        }
       }
     }
     if (out) out += step * a.lddx;
@@ -507,7 +562,7 @@ __global__ void __launch_bounds__(kGradWarps * 32) k_rms_grad(const GradArgs<T> 
   uint64_t acc[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
-  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2) * NU * 32 + lane) * (uint32_t)sizeof(Held<T>);
+  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2) * NU) * Lay<T, V>::PITCH + lane * Lay<T, V>::BYTES;
   if (c0 + NU * UNIT <= a.cols)
     grad_rows<T, V, NU, R>(a, acc, slots, teams, team, warp, lane, part, true);
   else
@@ -517,14 +572,24 @@ __global__ void __launch_bounds__(kGradWarps * 32) k_rms_grad(const GradArgs<T> 
   float* out = a.part + (long long)blockIdx.x * a.cols;
   float* joined = reinterpret_cast<float*>(dyn);
   if (teams > 1) __syncthreads();  // every warp is done with its slots
+  float* const to = teams > 1 ? joined + team * a.cols : out;
+  const bool wide = reinterpret_cast<uintptr_t>(to) % 16 == 0;  // (dgamma itself may not be)
 #pragma unroll
   for (int i = 0; i < NU; ++i) {
     const float2 f[2] = {ptx::unpack2(acc[i][0]), ptx::unpack2(acc[i][1])};
+    if constexpr (V >= 4) {
+      // (single values here, 16 or 32 bytes apart, cost 3 us of 50 at 4096 x 8192)
+      const int c = c0 + Lay<T, V>::col(i, 0, lane);
+      if (wide && c < a.cols) {
+        *reinterpret_cast<float4*>(to + c) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+        continue;
+      }
+    }
     const float v[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = c0 + i * UNIT + Unit<T, V>::col(e, lane);
-      if (c < a.cols) (teams > 1 ? joined + team * a.cols : out)[c] = v[e];
+      const int c = c0 + Lay<T, V>::col(i, e, lane);
+      if (c < a.cols) to[c] = v[e];
     }
   }
   if (teams == 1) return;
@@ -582,6 +647,7 @@ __global__ void __launch_bounds__(8 * 32) k_rms_strip(const GradArgs<T> a, const
   gammas<V>(g, a.gamma, (int)c, lane, a.cols, a.wide);
   for (long long row0 = blockIdx.y; row0 < a.rows; row0 += 4ll * gridDim.y) {
     Unit<T, V> h[4], d[4], t[4];  // four rows' loads together
+    float rstd[4], dot[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const long long row = row0 + (long long)j * gridDim.y;
@@ -589,21 +655,22 @@ __global__ void __launch_bounds__(8 * 32) k_rms_strip(const GradArgs<T> a, const
         h[j].load(a.h + row * a.ldh, (int)c, lane, a.cols);
         d[j].load(a.dy + row * a.lddy, (int)c, lane, a.cols);
         if (a.dh) t[j].load(a.dh + row * a.lddh, (int)c, lane, a.cols);
+        rstd[j] = __ldg(a.rstd + row);
+        dot[j] = dots ? dots[row] : 0.f;
       }
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const long long row = row0 + (long long)j * gridDim.y;
       if (row >= a.rows) break;
-      const float rstd = __ldg(a.rstd + row), dot = dots ? dots[row] : 0.f;
       uint64_t x[2], y[2];
       h[j].pairs(x);
       d[j].pairs(y);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint64_t n = ptx::mul2(x[e], both(rstd));
+        const uint64_t n = ptx::mul2(x[e], both(rstd[j]));
         ptx::fma2_to(acc[e], y[e], n);
-        x[e] = ptx::mul2(both(rstd), ptx::fma2(n, both(-dot), ptx::mul2(g[e], y[e])));
+        x[e] = ptx::mul2(both(rstd[j]), ptx::fma2(n, both(-dot[j]), ptx::mul2(g[e], y[e])));
       }
       if (!a.dx) continue;
       if (a.dh) {
@@ -619,31 +686,48 @@ __global__ void __launch_bounds__(8 * 32) k_rms_strip(const GradArgs<T> a, const
   if (a.part) {
     const float2 f[2] = {ptx::unpack2(acc[0]), ptx::unpack2(acc[1])};
     const float v[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
+    float* const to = a.part + (long long)blockIdx.y * a.cols;
+    if (V == 4 && reinterpret_cast<uintptr_t>(to) % 16 == 0) {
+      const int k = (int)c + Unit<T, V>::col(0, lane);
+      if (k < a.cols) *reinterpret_cast<float4*>(to + k) = make_float4(v[0], v[1], v[2], v[3]);
+      return;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int k = (int)c + Unit<T, V>::col(e, lane);
-      if (k < a.cols) a.part[(long long)blockIdx.y * a.cols + k] = v[e];
+      if (k < a.cols) to[k] = v[e];
     }
   }
 }
 
-// dgamma[c] = sum of `rows` partial sums, 32 columns a block: 32 threads a
-// column add up every 32nd, and then each other's, in a fixed order.
+// dgamma[c] = sum of `rows` partial sums, W columns a block: 1024 / W threads a
+// column add up every (1024 / W)th, and then each other's, in a fixed order.
+template <int W>
 __global__ void __launch_bounds__(1024) k_rms_fold(const float* part, int rows, int cols, float* out) {
-  __shared__ float s[32][33];
+  constexpr int G = 1024 / W, AHEAD = 4;
+  __shared__ float s[32][W + 1];
   ptx::griddep_wait();
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const long long c = (long long)blockIdx.x * 32 + tx;
+  const int tx = threadIdx.x % W, ty = threadIdx.x / W, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long c = (long long)blockIdx.x * W + tx;
   float v = 0.f;
   if (c < cols)
-    for (int r = ty; r < rows; r += 32) v += part[(long long)r * cols + c];
-  s[tx][ty] = v;
+    for (int r = ty; r < rows; r += AHEAD * G) {
+      float t[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) t[i] = r + i * G < rows ? part[(long long)(r + i * G) * cols + c] : 0.f;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) v += t[i];
+    }
+#pragma unroll
+  for (int o = 16; o >= W; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane < W) s[warp][lane] = v;
   __syncthreads();
-  v = s[ty][tx];
+  if (warp >= W) return;
+  v = s[lane][warp];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  const long long k = (long long)blockIdx.x * 32 + ty;
-  if (tx == 0 && k < cols) out[k] = v;
+  const long long k = (long long)blockIdx.x * W + warp;
+  if (lane == 0 && k < cols) out[k] = v;
 }
 
 // ------------------------------------------------------------------ host
@@ -710,10 +794,8 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 
 // The gradient's blocks: as many an SM as 512 threads (128 registers each) and
 // two sets of rows in shared memory allow, and at most kGradRows rows a thread.
-// Two rows a set where that leaves two blocks an SM or costs none (16384 x 2000 fp32: 85
-// us, one a set 108); of rows that fill an SM alone with eight units a warp, two
-// without a queue (2097 x 16000 bf16: 62 us, one with a queue 70).  The rest of the shared
-// memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
+// Two rows a set where that leaves two blocks an SM or costs none (16384 x 3000 bf16: 72
+// us, one a set 79).  The rest of the shared memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
 // workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
 struct GradPlan {
@@ -738,8 +820,7 @@ GradPlan grad_plan(int rows, int cols, int esize) {
   if (p.nu) {
     const int most = kGradWarps * 32 / threads;
     auto room_of = [&](int set) { return std::max(1, std::min(most, kGradSmem / (2 * set * row))); };
-    const bool queued = 4 * row <= kGradSmem && (room_of(2) >= 2 || room_of(2) == room_of(1));
-    p.set = queued || (p.nu == 8 && most == 1 && 2 * row <= kGradSmem) ? 2 : 1;
+    p.set = 4 * row <= kGradSmem && (room_of(2) >= 2 || room_of(2) == room_of(1)) ? 2 : 1;
     const int room = room_of(p.set);
     p.depth = std::max(1, std::min(4, kGradSmem / (room * p.set * row)));
     fill = 152ll * room;
@@ -773,14 +854,27 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
   const double bytes = count * sizeof(T) * (2 + (a.dx ? 1 : 0) + (a.dh ? 1 : 0));
   if (p.nu) {
     auto go = [&]() -> cudaError_t {
-      return with_vector<T>(v, [&](auto V) {
+      // (eight bf16 values a vector where two units go together)
+      const bool eight = sizeof(T) == 2 && v == 4 && p.nu > 1 && a.cols % 8 == 0 && rows_aligned(a.dy, a.lddy, 2, 16) &&
+                         rows_aligned(a.h, a.ldh, 2, 16) && (!a.dh || rows_aligned(a.dh, a.lddh, 2, 16)) &&
+                         (!a.dx || rows_aligned(a.dx, a.lddx, 2, 16));
+      auto with = [&](auto f) -> cudaError_t {
+        if constexpr (sizeof(T) == 2)
+          if (eight) return f(std::integral_constant<int, 8>{});
+        return with_vector<T>(v, f);
+      };
+      return with([&](auto V) {
         const int threads = p.teams * p.warps * 32;
         const size_t ring = (size_t)p.depth * p.set * (a.dh ? 3 : 2) * p.nu * threads * 4 * sizeof(T);
         const size_t smem = std::max(ring, p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0);
         PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)threads), st, smem);
         auto go = [&](auto N, auto R) -> cudaError_t {
-          const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem);
-          return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value, R.value>, a);
+          if constexpr (V.value == 8 && N.value == 1) {
+            return cudaErrorInvalidValue;  // (see `eight`)
+          } else {
+            const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem);
+            return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value, R.value>, a);
+          }
         };
         using One = std::integral_constant<int, 1>;
         using Two = std::integral_constant<int, 2>;
@@ -816,9 +910,12 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
     FF_LAUNCH(K_RMS_GRAD, bytes, st, strip(), "RMS norm gradient");
   }
   if (dgamma && p.blocks > 1) {
-    PdlLaunch l(dim3((unsigned)cdiv(a.cols, 32)), dim3(1024), st);
+    // (16384 x 1000: 33.7 us in all with 8, 35.1 with 32; x 3000 71.0 and 70.1)
+    const int w = a.cols < 32 * 76 ? 8 : 32;
+    PdlLaunch l(dim3((unsigned)cdiv(a.cols, w)), dim3(1024), st);
+    auto* const fold = w == 32 ? k_rms_fold<32> : k_rms_fold<8>;
     FF_LAUNCH(K_RMS_GRAD, 4.0 * p.blocks * a.cols, st,
-              cudaLaunchKernelEx(&l.cfg, k_rms_fold, (const float*)a.part, p.blocks, a.cols, dgamma), "RMS norm gradient");
+              cudaLaunchKernelEx(&l.cfg, fold, (const float*)a.part, p.blocks, a.cols, dgamma), "RMS norm gradient");
   }
   return FF_OK;
 }
