@@ -711,14 +711,24 @@ ff_status logprobs_t(Args<T> a, cudaStream_t st) {
     return FF_OK;
   }
   const int vecs = cdiv(a.classes, N);
-  // Short rows take a warp each (few rows only if it has two rounds of loads at
-  // most).  Others a block of 8 warps; with fewer rows
-  // than the GPU has room for, more warps and then more blocks, as long as
-  // each thread has a vector or two to read.
-  a.warps = vecs <= (a.rows >= 152 ? 256 : 64) ? 1 : 8;
+  // Many rows take few warps each, so that what a row costs besides its bytes (the
+  // joins, the barrier, the selection) is shared by more rows at a time: 16384 x 2500
+  // bf16 on 1, 4 and 8 warps 22, 39 and 67 us, with top 8 50, 86 and 128; 1000 x 5000 7.4,
+  // 5.8 and 6.7; 1500 x 16000 20, 12 and 14.  The selection of long rows wants more:
+  // 2048 x 49999 fp32, top 4: 1, 4 and 8 warps 187, 148 and 81; and two warps are no good
+  // there.  So do more than 16 of the likeliest, for which a warp's 32 largest
+  // values are few: 3000 x 1000 fp32, top 32: 1 and 4 warps 40 and 18.  A thread has one
+  // and a half vectors at least (with the last: one).
+  if (a.top)
+    a.warps = a.top <= 16 && a.rows >= 1800 && vecs <= 1300 ? 1 : a.rows >= 700 && vecs <= 3000 ? 4 : 8;
+  else
+    a.warps = vecs > 4000 ? 8 : a.rows >= 4000 ? 1 : a.rows >= 1500 ? 2 : a.rows >= 700 ? 4 : 8;
+  while (a.warps > 1 && a.warps * (a.top > 16 ? 32 : 46) > vecs) a.warps = a.top && a.warps == 4 ? 1 : a.warps / 2;
+  // With fewer rows than the GPU has room for, more warps and then more
+  // blocks, as long as each thread has a vector or two to read.
   a.cluster = 1;
-  if (a.warps == 8 && a.rows < 152 * 4) {
-    while (a.warps < kMostWarps && (long long)a.warps * 2 * 32 <= vecs && (long long)a.rows * a.warps < 152 * 32) a.warps *= 2;
+  if (a.warps == 8) {
+    while (a.warps < kMostWarps && (long long)a.warps * 2 * 32 <= vecs && (long long)a.rows * a.warps * 2 <= 152 * 32) a.warps *= 2;
     while (a.cluster < 8 && (long long)a.cluster * 2 * a.warps * 32 <= vecs && (long long)a.rows * a.cluster * 2 <= 152) a.cluster *= 2;
   }
   a.groups = 1;

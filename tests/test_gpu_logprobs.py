@@ -35,8 +35,8 @@ def logits_of(torch, rows, classes, dt, i, masked=0.0):
     return view, labels.cuda()
 
 
-def definition(torch, x, labels, classes):
-    """logp, entropy, z, p, ln p of x in 64 bits, and the bounds of the sums' and the entropy's errors."""
+def definition(torch, x, labels, classes, threads=256):
+    """logp, entropy, z, p, ln p of x in 64 bits, and the bounds of the sums' and the entropy's errors (`threads` a row)."""
     x = x.double()
     m = x.amax(1, keepdim=True)
     z = torch.logsumexp(x, 1, keepdim=True)
@@ -47,8 +47,8 @@ def definition(torch, x, labels, classes):
     logp = torch.where(has, lp.gather(1, labels.clamp(0, classes - 1).long()[:, None])[:, 0], 0.0)
     entropy = -torch.where(p > 0, p * lp, 0.0).sum(1)
     e1 = EXP + 3 * U * d.abs()
-    raises = classes // (4 * 256) + 14
-    sums = raises * (EXP + 8 * U) + (classes // 256 + 40) * U
+    raises = classes // (4 * threads) + 14
+    sums = raises * (EXP + 8 * U) + (classes // threads + 40) * U
     es = (p * e1).sum(1) + sums
     t = (p * d.abs()).sum(1)
     et = (p * d.abs() * e1).sum(1) + t * sums
@@ -156,6 +156,31 @@ def test_short_rows(classes, dtype):
     want[has, labels[proper][has].long()] += a[has, 0]
     tol = q * a * (2 * EXP + 4 * U * (d.abs() + ln[:, None]) + 6 * U) + U * a + want.abs() * (torch.finfo(dt).eps / 2)
     assert bool(((dx - want).abs() <= tol + 2.0 ** -120).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("size", [(4100, 3001), (1900, 5001), (2000, 997), (1600, 2500), (750, 9000), (720, 700), (300, 1500)])
+def test_many_rows(size, dtype):
+    """One, two, four and eight warps a row; every other row of few values, one of them with a mask."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    rows, classes = size
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x, labels = logits_of(torch, rows, classes, dt, classes % 4, 0.0)
+    x[::2] = (x[::2].float() * 2).round().to(dt) / 2
+    x[4, 9:] = float("-inf")
+    labels[4] = 3
+    logp, entropy, m, ln, p, lp, d, has, e_ln, e_h = definition(torch, x, labels, classes, threads=32)
+    order = torch.sort(x.double(), dim=1, descending=True, stable=True).indices
+    for top in (0, 3, 16, 20, 32):
+        r = ff.label_logprobs(x, labels, top=top)
+        assert bool(((r.logp.double() - logp).abs() <= torch.where(has, e_ln + 2 * U * (logp.abs() + ln), 0.0)).all())
+        assert bool(((r.entropy.double() - entropy).abs() <= e_h).all())
+        assert torch.equal(r.stats[:, 0].double(), m) and bool(((r.stats[:, 1].double() - ln).abs() <= e_ln).all())
+        assert torch.equal(r.top_index.long(), order[:, :top])
+        want = lp.gather(1, order[:, :top])
+        tol = e_ln[:, None] + 2 * U * (want.abs() + ln[:, None])
+        assert bool(((r.top_logp.double() == want) | ((r.top_logp.double() - want).abs() <= tol)).all())
 
 
 def test_sorted_rows():
