@@ -332,26 +332,33 @@ struct GradArgs {
   bool wide;
 };
 
-// How a lane's part of NU units of a row lies in the row and in its own slots of
-// shared memory.  V = 8 (bf16, NU even): units in twos of 2 x UNIT columns, a
-// lane's eight values of which are one 16-byte copy, which goes past L1 (8-byte
-// copies go through it, and L1 is what the slots leave: 16384 x 2000 60 us, so 49).
+// How NU units of a row lie in the row and in shared memory.  V = 8 (bf16, NU
+// even): units in twos of 2 x UNIT columns, a lane's eight values of which are one
+// 16-byte copy, which goes past L1 (8-byte copies go through it, and L1 is what
+// the slots leave: 16384 x 2000 60 us, so 49).  A lane reads back its own copies,
+// but for single bf16 values (WORDS), which come as the 4-byte words that cover
+// them, in the row's order, with half a word more at either end.
 template <typename T, int V>
 struct Lay {
+  static constexpr bool WORDS = sizeof(T) * V < 4;
   static constexpr int P = V == 8 ? 2 : 1;  // units together
-  static constexpr uint32_t BYTES = P * sizeof(Held<T>), PITCH = 32 * sizeof(Held<T>);  // of a slot; of a unit's slots
-  static __device__ __forceinline__ int col(int i, int e, int lane) {  // of value e of unit i
+  static constexpr uint32_t PITCH = 32 * sizeof(Held<T>);               // bytes of a warp's unit
+  static constexpr uint32_t LANE = WORDS ? 0 : P * sizeof(Held<T>);     // from a lane's slot to the next one's
+  static __host__ __device__ constexpr uint32_t part(int nu) { return nu * PITCH + (WORDS ? 16 : 0); }  // of a warp's units
+  static __device__ __forceinline__ int col(int i, int e, int lane) {   // of value e of unit i
     if constexpr (V == 8) return (i & ~1) * UNIT + lane * 8 + (i & 1) * 4 + e;
     else return i * UNIT + Unit<T, V>::col(e, lane);
   }
 };
+// Whether a row of bf16 values starts in the middle of a word.
+__device__ __forceinline__ uint32_t odd_at(const void* p) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) >> 1) & 1u; }
 
-// Copies these by the bytes that the alignment allows (single bf16 values go
-// through registers, all of the row's before the first is stored).
+// Copies these by the bytes that the alignment allows.  A word before an odd row's
+// first value belongs to the row before; matrix_start: there is none.
 template <typename T, int V, int NU>
-__device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int lane, int cols, bool whole) {
+__device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int lane, int cols, bool whole, bool matrix_start) {
   using L = Lay<T, V>;
-  if constexpr (sizeof(T) * V >= 4) {
+  if constexpr (!L::WORDS) {
     constexpr int BYTES = (int)sizeof(T) * V;
 #pragma unroll
     for (int u = 0; u < NU; u += L::P)
@@ -362,12 +369,22 @@ __device__ __forceinline__ void fetch(uint32_t slot, const T* row, int c0, int l
         ptx::cp_async_zfill<BYTES>(slot + u * L::PITCH + i * BYTES, row + (in ? c : 0), in ? BYTES : 0);
       }
   } else {
-    Unit<T, V> u[NU];
+    const int odd = (int)odd_at(row);
+    const char* from = reinterpret_cast<const char*>(row + c0 - odd);
+    auto word = [&](int w, int most) {
+      const int n = whole ? most : max(0, min(most, (cols - c0 + odd - 2 * w) * 2));
+      ptx::cp_async_zfill<4>(slot + 4 * w, n > 0 ? from + 4 * w : reinterpret_cast<const char*>(row - odd), n);  // (of none: not read)
+    };
 #pragma unroll
-    for (int i = 0; i < NU; ++i) u[i].load(row, c0 + i * UNIT, lane, cols, whole);
-#pragma unroll
-    for (int i = 0; i < NU; ++i)
-      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot + i * L::PITCH), "r"(u[i].w[0]), "r"(u[i].w[1]) : "memory");
+    for (int i = 0; i < NU * 2; ++i) {
+      if (i == 0 && odd && matrix_start && c0 == 0 && lane == 0) {
+        const uint16_t v = Vec<T, 1>::load(row);
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(slot + 2), "h"(v) : "memory");
+        continue;
+      }
+      word(i * 32 + lane, 4);
+    }
+    if (odd && lane == 0) word(NU * 64, 2);
   }
 }
 
@@ -385,12 +402,24 @@ __device__ __forceinline__ void read_slot(Held<float> (&h)[1], uint32_t slot) {
                : "=f"(h[0].w[0]), "=f"(h[0].w[1]), "=f"(h[0].w[2]), "=f"(h[0].w[3])
                : "r"(slot));
 }
-template <typename T, int P>
-__device__ __forceinline__ void slot_pairs(uint64_t (&p)[P][2], uint32_t slot) {
-  Held<T> h[P];
-  read_slot(h, slot);
+// Unit i (and the next, if they lie together) of a warp's part.
+template <typename T, int V, int P>
+__device__ __forceinline__ void part_pairs(uint64_t (&p)[P][2], uint32_t slot, int i, uint32_t odd, int lane) {
+  if constexpr (Lay<T, V>::WORDS) {
+    uint32_t v[4];
 #pragma unroll
-  for (int j = 0; j < P; ++j) h[j].pairs(p[j]);
+    for (int e = 0; e < 4; ++e)
+      asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}"
+                   : "=r"(v[e])
+                   : "r"(slot + 2 * (odd + Lay<T, V>::col(i, e, lane))));
+    p[0][0] = ptx::pack2(v[0] << 16, v[1] << 16);
+    p[0][1] = ptx::pack2(v[2] << 16, v[3] << 16);
+  } else {
+    Held<T> h[P];
+    read_slot(h, slot + i * Lay<T, V>::PITCH);
+#pragma unroll
+    for (int j = 0; j < P; ++j) h[j].pairs(p[j]);
+  }
 }
 
 // The sums over a row's warps of R values (rows), in a fixed order, in every
@@ -434,18 +463,18 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
   const long long first = ((long long)blockIdx.x * teams + team) * R, step = (long long)gridDim.x * teams * R;
   const T *hp = a.h + first * a.ldh, *dp = a.dy + first * a.lddy, *tp = a.dh ? a.dh + first * a.lddh : nullptr;
   using L = Lay<T, V>;
-  constexpr uint32_t UB = L::PITCH;
+  constexpr uint32_t part1 = L::part(NU);
   constexpr int P = L::P;
-  const uint32_t rb = (a.dh ? 3 : 2) * NU * UB;  // of a row
+  const uint32_t rb = (a.dh ? 3 : 2) * part1;  // of a row
   const uint32_t stage = R * rb * (blockDim.x >> 5);
   long long ahead = first;
   auto issue = [&](uint32_t to) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (ahead + r < a.rows) {
-        fetch<T, V, NU>(to + r * rb, hp + r * a.ldh, c0, lane, a.cols, whole);
-        fetch<T, V, NU>(to + r * rb + NU * UB, dp + r * a.lddy, c0, lane, a.cols, whole);
-        if (a.dh) fetch<T, V, NU>(to + r * rb + 2 * NU * UB, tp + r * a.lddh, c0, lane, a.cols, whole);
+        fetch<T, V, NU>(to + r * rb, hp + r * a.ldh, c0, lane, a.cols, whole, ahead + r == 0);
+        fetch<T, V, NU>(to + r * rb + part1, dp + r * a.lddy, c0, lane, a.cols, whole, ahead + r == 0);
+        if (a.dh) fetch<T, V, NU>(to + r * rb + 2 * part1, tp + r * a.lddh, c0, lane, a.cols, whole, ahead + r == 0);
       }
     }
     hp += step * a.ldh;
@@ -455,6 +484,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
     ptx::cp_async_commit();
   };
   for (int d = 0; d < a.depth; ++d) issue(slots + d * stage);
+  auto odd = [](const T* m, long long ld, long long row) { return L::WORDS ? odd_at(m + row * ld) : 0u; };
   uint64_t g[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) {
@@ -468,7 +498,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
 #pragma unroll
     for (int r = 0; r < R; ++r) to[r] = row + r < a.rows ? __ldg(a.rstd + row + r) : 0.f;
   };
-  constexpr bool AHEAD = sizeof(T) * V >= 4;  // (the others have no registers for it and wait for their copies anyway)
+  constexpr bool AHEAD = !L::WORDS;  // (those have no registers for it)
   if constexpr (AHEAD) rstds(coming, first);
   for (long long row = first; row < a.rows; row += step, turn ^= 1) {
     float rstd[R], dot[R];
@@ -483,6 +513,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
     else if (a.depth == 3) ptx::cp_async_wait<2>();
     else if (a.depth == 2) ptx::cp_async_wait<1>();
     else ptx::cp_async_wait<0>();
+    if constexpr (L::WORDS) __syncwarp();  // the other lanes' copies too
     const uint32_t now = slots + at * stage;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -491,8 +522,8 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
 #pragma unroll
         for (int i = 0; i < NU; i += P) {
           uint64_t x[P][2], y[P][2];
-          slot_pairs<T>(x, now + r * rb + i * UB);
-          slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
+          part_pairs<T, V>(x, now + r * rb, i, odd(a.h, a.ldh, row + r), lane);
+          part_pairs<T, V>(y, now + r * rb + part1, i, odd(a.dy, a.lddy, row + r), lane);
 #pragma unroll
           for (int j = 0; j < P; ++j)
 #pragma unroll
@@ -514,15 +545,15 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
       for (int i = 0; i < NU; i += P) {
         if (!whole && c0 + i * UNIT >= a.cols) break;
         uint64_t x[P][2], y[P][2];
-        slot_pairs<T>(x, now + r * rb + i * UB);
-        slot_pairs<T>(y, now + r * rb + (NU + i) * UB);
+        part_pairs<T, V>(x, now + r * rb, i, odd(a.h, a.ldh, row + r), lane);
+        part_pairs<T, V>(y, now + r * rb + part1, i, odd(a.dy, a.lddy, row + r), lane);
 #pragma unroll
         for (int j = 0; j < P; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
             x[j][e] = ptx::fma2(x[j][e], off, ptx::mul2(both(rstd[r]), ptx::mul2(g[i + j][e], y[j][e])));
         if (a.dh) {
-          slot_pairs<T>(y, now + r * rb + (2 * NU + i) * UB);
+          part_pairs<T, V>(y, now + r * rb + 2 * part1, i, odd(a.dh, a.lddh, row + r), lane);
 #pragma unroll
           for (int j = 0; j < P; ++j)
 #pragma unroll
@@ -543,6 +574,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
       }
     }
     if (out) out += step * a.lddx;
+    if constexpr (L::WORDS) __syncwarp();
     issue(now);  // into the slots just read
     if (++at == a.depth) at = 0;
   }
@@ -559,7 +591,7 @@ __global__ void __launch_bounds__(kGradWarps * 32) k_rms_grad(const GradArgs<T> 
   uint64_t acc[NU][2];
 #pragma unroll
   for (int i = 0; i < NU; ++i) acc[i][0] = acc[i][1] = 0;
-  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2) * NU) * Lay<T, V>::PITCH + lane * Lay<T, V>::BYTES;
+  const uint32_t slots = ptx::smem_u32(dyn) + (uint32_t)(w * R * (a.dh ? 3 : 2)) * Lay<T, V>::part(NU) + lane * Lay<T, V>::LANE;
   if (c0 + NU * UNIT <= a.cols)
     grad_rows<T, V, NU, R>(a, acc, slots, teams, team, warp, lane, part, true);
   else
@@ -797,6 +829,7 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 // us, one a set 79).  The rest of the shared memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
 // workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
+constexpr int kGradEnds = 4 * 2 * 3 * kGradWarps * 16;  // and at most what single bf16 values add to their copies
 struct GradPlan {
   int nu, warps, teams, set, blocks, depth;
 };
@@ -864,14 +897,16 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
       };
       return with([&](auto V) {
         const int threads = p.teams * p.warps * 32;
-        const size_t ring = (size_t)p.depth * p.set * (a.dh ? 3 : 2) * p.nu * threads * 4 * sizeof(T);
+        // (single bf16 values: 16384 x 2001 70 us with one row a set, with two 83)
+        const int set = Lay<T, V.value>::WORDS && p.blocks >= 152 ? 1 : p.set;
+        const size_t ring = (size_t)p.depth * set * (a.dh ? 3 : 2) * (threads / 32) * Lay<T, V.value>::part(p.nu);
         const size_t smem = std::max(ring, p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0);
         PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)threads), st, smem);
         auto go = [&](auto N, auto R) -> cudaError_t {
           if constexpr (V.value == 8 && N.value == 1) {
             return cudaErrorInvalidValue;  // (see `eight`)
           } else {
-            const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem);
+            const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem + kGradEnds);
             return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value, R.value>, a);
           }
         };
@@ -880,10 +915,10 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
         using Four = std::integral_constant<int, 4>;
         using Eight = std::integral_constant<int, 8>;
         switch (p.nu) {
-          case 1: return p.set == 2 ? go(One{}, Two{}) : go(One{}, One{});
-          case 2: return p.set == 2 ? go(Two{}, Two{}) : go(Two{}, One{});
-          case 4: return p.set == 2 ? go(Four{}, Two{}) : go(Four{}, One{});
-          default: return p.set == 2 ? go(Eight{}, Two{}) : go(Eight{}, One{});
+          case 1: return set == 2 ? go(One{}, Two{}) : go(One{}, One{});
+          case 2: return set == 2 ? go(Two{}, Two{}) : go(Two{}, One{});
+          case 4: return set == 2 ? go(Four{}, Two{}) : go(Four{}, One{});
+          default: return set == 2 ? go(Eight{}, Two{}) : go(Eight{}, One{});
         }
       });
     };

@@ -189,6 +189,31 @@ def test_matrices_side_by_side_in_one_buffer():
         ff.rms_norm(a, gamma, out=wide[:, 4:cols + 4])
 
 
+@pytest.mark.parametrize("size", [(5, 1), (37, 129), (900, 301), (170, 4097), (2000, 2001), (40, 9001), (3, 15999), (700, 7)])
+def test_gradient_of_odd_rows_at_every_offset(size):
+    """Rows of single bf16 values that start anywhere: the same bits, whatever lies around them."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    rows, cols = size
+    gamma = gamma_of(torch, cols, 1)
+    dy, h, dh = (data(torch, rows, cols, torch.bfloat16, 0, 0, s) for s in (1, 2, 3))
+    rstd = torch.rand(rows, generator=torch.Generator().manual_seed(4)).cuda() + 0.5
+
+    def at(t, pad, lead):
+        buf = torch.full((lead + rows * (cols + pad) + 3,), float("nan"), dtype=torch.bfloat16, device="cuda")
+        view = buf[lead:lead + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+        view.copy_(t)
+        return view
+
+    for joined in (dh, None):
+        dx, dg = ff.rms_norm_backward(dy, h, rstd, gamma, dh=joined)
+        for k, (pads, leads) in enumerate((((0, 0, 0), (1, 1, 1)), ((1, 3, 0), (1, 0, 3)), ((2, 1, 5), (0, 1, 2)), ((0, 4, 1), (3, 5, 0)))):
+            a, b = at(dy, pads[0], leads[0]), at(h, pads[1], leads[1])
+            c = None if joined is None else at(dh, pads[2], leads[2])
+            got, dg2 = ff.rms_norm_backward(a, b, rstd, gamma, dh=c, out=(None, a, b, None)[k])
+            assert torch.equal(got, dx) and torch.equal(dg2, dg), (pads, leads)
+
+
 def test_rows_that_are_not_finite_and_rows_of_zeros():
     torch = torch_cuda()
     ff = lib_ready()
