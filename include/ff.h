@@ -709,7 +709,7 @@ FF_API long long ff_clip_grad_norm_workspace(int n);
  * Squares are formed in fp32 and added up in fp64, in a fixed order: a
  * magnitude past 2^63 makes the norm infinite (and finite gradients zero), a NaN
  * everything NaN.  Empty tensors are skipped.  max_norm >= 0 (infinity: only
- * the norm is wanted). */
+ * the norm is wanted; the factor is then 1, also where the norm is infinite or NaN). */
 FF_API ff_status ff_clip_grad_norm(const void* const* grads, void* const* out, const long long* counts, const int* precs,
                                    int n, float max_norm, float* norm, void* workspace, long long workspace_bytes,
                                    void* stream);

@@ -152,10 +152,11 @@ __device__ __forceinline__ float norm_of(double s) {
   const float r = __fsqrt_rn((float)(s * (big ? 0x1p-128 : small ? 0x1p128 : 1.0)));
   return big ? r * 0x1p64f : small ? r * 0x1p-64f : r;  // an infinity and NaN stay
 }
-// The factor: 1 where nothing is to be clipped; NaN for a NaN norm.
+// The factor: 1 where nothing is to be clipped, as with an infinite max_norm whatever
+// the norm is; else NaN for a NaN norm.
 __device__ __forceinline__ float factor(float norm, float max_norm) {
   const float by = __fdiv_rn(max_norm, norm);
-  return norm == 0.f || by > 1.f ? 1.f : by;
+  return isinf(max_norm) || norm == 0.f || by > 1.f ? 1.f : by;
 }
 
 // All pieces in one cluster's registers.

@@ -1304,8 +1304,10 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     """ff_clip_grad_norm: the 2-norm over all tensors of grads (bf16 or fp32,
     contiguous, one device) together, and the tensors scaled so that it is at
     most max_norm, in place or into `out` (a list of tensors like them).
-    Returns the norm before clipping, fp32 [1], without a wait.  A tensor given
-    twice, or outputs that overlap, are refused."""
+    Returns the norm before clipping, fp32 [1], without a wait.  max_norm
+    math.inf leaves the values as they are, whatever the norm.  Outputs that
+    overlap each other, or gradients other than their own, are refused (so a
+    tensor comes twice only with an output for each)."""
     grads = list(grads)
     n = len(grads)
     if n == 0 or not isinstance(grads[0], torch.Tensor):
