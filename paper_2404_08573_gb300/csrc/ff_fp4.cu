@@ -288,9 +288,6 @@ __global__ void __launch_bounds__(kQThreads)
       }
     }
   }
-  // the rows are in registers: a product that follows may set itself up (1024 x 2000 x
-  // 2000 with it 10.0 us, else 10.8)
-  ptx::griddep_launch_dependents();
   uint32_t s[4];
   uint8_t* to = q + (long long)row0 * ldq + c0 / 2;
 #pragma unroll
