@@ -706,8 +706,10 @@ FF_API long long ff_clip_grad_norm_workspace(int n);
  * returns; the pointers in them are device pointers of dense tensors.  out[i]
  * may be grads[i] (where nothing is clipped it is then not written); other
  * overlaps of outputs are FF_ERR_INVALID_ARG, so no tensor may come twice.
- * Squares are formed in fp32 and added up in fp64, in a fixed order: a
- * magnitude past 2^63 makes the norm infinite (and finite gradients zero), a NaN
+ * Sums of squares are fp32 over a warp and fp64 from there on, in a fixed
+ * order; where fp32 could not hold one, a thread forms it again times a power of
+ * two.  So the norm is right for all finite gradients, and infinite (and finite
+ * gradients zero) only past fp32's range or with an infinity; a NaN makes
  * everything NaN.  Empty tensors are skipped.  max_norm >= 0 (infinity: only
  * the norm is wanted; the factor is then 1, also where the norm is infinite or NaN). */
 FF_API ff_status ff_clip_grad_norm(const void* const* grads, void* const* out, const long long* counts, const int* precs,

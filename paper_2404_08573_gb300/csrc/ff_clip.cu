@@ -46,6 +46,24 @@ __device__ __forceinline__ int tensor_of(const Table& t, int piece) {
   return lo;
 }
 
+// min(1, max_norm / norm) as two factors, the first a power of two: 1, but where the
+// ratio lies near or below the end of fp32's normal range and would be rounded to
+// few bits.  Gradients are brought to the norm's order of magnitude there.
+struct Factor {
+  float first, then;
+  __device__ __forceinline__ bool one() const { return then == 1.f && first == 1.f; }
+};
+// 1 where nothing is to be clipped, as with an infinite max_norm whatever the
+// norm is; else NaN for a NaN norm.
+__device__ __forceinline__ Factor factor(float norm, float max_norm) {
+  const float by = __fdiv_rn(max_norm, norm);
+  if (isinf(max_norm) || norm == 0.f || by > 1.f) return Factor{1.f, 1.f};
+  if (!(by < 0x1p-100f) || isinf(norm) || max_norm == 0.f) return Factor{1.f, by};
+  // 2^-floor(log2 norm), at least 2^-126 (norm > 2^-49, since no max_norm is below 2^-149)
+  const float first = __uint_as_float(max(254u - (__float_as_uint(norm) >> 23), 1u) << 23);
+  return Factor{first, __fdiv_rn(max_norm, norm * first)};
+}
+
 // One thread's part of a piece, as loaded.  Past the end: zeros.
 template <typename T>
 struct Piece {
@@ -64,18 +82,23 @@ struct Piece {
       }
     }
   }
-  static __device__ __forceinline__ float squares(const uint4 (&r)[VECS]) {
+  // The sum of the squares; SCALED: of the values times `by`.
+  template <bool SCALED>
+  static __device__ __forceinline__ float squares(const uint4 (&r)[VECS], float by) {
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
       float v[N];
       Vec<T, N>::unpack(r[j], v);
 #pragma unroll
-      for (int e = 0; e < N; ++e) s = fmaf(v[e], v[e], s);
+      for (int e = 0; e < N; ++e) {
+        if (SCALED) v[e] *= by;
+        s = fmaf(v[e], v[e], s);
+      }
     }
     return s;
   }
-  static __device__ __forceinline__ void store(const uint4 (&r)[VECS], T* p, long long left, int tid, bool wide, float by,
+  static __device__ __forceinline__ void store(const uint4 (&r)[VECS], T* p, long long left, int tid, bool wide, Factor by,
                                                uint64_t policy) {
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
@@ -83,7 +106,7 @@ struct Piece {
       float v[N];
       Vec<T, N>::unpack(r[j], v);
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] *= by;
+      for (int e = 0; e < N; ++e) v[e] = v[e] * by.first * by.then;
       if (wide && i + N <= left) {
         uint4 o;
         Vec<T, N>::store(reinterpret_cast<T*>(&o), v);
@@ -117,10 +140,11 @@ __device__ __forceinline__ void load_piece(const Table& t, const At& a, uint4 (&
   if (t.bf16s[a.t]) Piece<bf16>::load(r, static_cast<const bf16*>(t.in[a.t]) + a.from, a.left, tid, wide, policy);
   else Piece<float>::load(r, static_cast<const float*>(t.in[a.t]) + a.from, a.left, tid, wide, policy);
 }
-__device__ __forceinline__ float piece_squares(const Table& t, const At& a, const uint4 (&r)[VECS]) {
-  return t.bf16s[a.t] ? Piece<bf16>::squares(r) : Piece<float>::squares(r);
+template <bool SCALED>
+__device__ __forceinline__ float piece_squares(const Table& t, const At& a, const uint4 (&r)[VECS], float by) {
+  return t.bf16s[a.t] ? Piece<bf16>::template squares<SCALED>(r, by) : Piece<float>::template squares<SCALED>(r, by);
 }
-__device__ __forceinline__ void store_piece(const Table& t, const At& a, const uint4 (&r)[VECS], int tid, float by, uint64_t policy) {
+__device__ __forceinline__ void store_piece(const Table& t, const At& a, const uint4 (&r)[VECS], int tid, Factor by, uint64_t policy) {
   const bool wide = wide_at(t.out[a.t]);
   if (t.bf16s[a.t]) Piece<bf16>::store(r, static_cast<bf16*>(t.out[a.t]) + a.from, a.left, tid, wide, by, policy);
   else Piece<float>::store(r, static_cast<float*>(t.out[a.t]) + a.from, a.left, tid, wide, by, policy);
@@ -130,15 +154,31 @@ __device__ __forceinline__ void store_piece(const Table& t, const At& a, const u
 // of them: the sum and what its roundings lost), a warp's too, and only one lane
 // a warp goes on in fp64, one thread to the square root (with both on every
 // thread 24010 values took 8.2 us in place of 4.2, 2 M 24 in place of 15).
+//
+// fp32 holds these sums where a piece's lies in [2^-90, 2^96]: what underflowed
+// in it is then nothing beside it, and neither 2^22 of them nor a warp's
+// overflow.  A thread whose piece lies elsewhere (zeros, vanished or exploding
+// gradients) squares it again, times a power of two that brings every fp32
+// magnitude of that side into range, and adds that to `far` in fp64.
 struct Sum {
   float hi = 0.f, lo = 0.f;
+  double far = 0.0;
   __device__ __forceinline__ void add(float v) {  // Knuth's two-sum
     const float s = __fadd_rn(hi, v), t = __fsub_rn(s, hi);
     lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fsub_rn(v, t)));
     hi = s;
   }
-  // an infinite or NaN sum has no meaningful rest
-  __device__ __forceinline__ float value() const { return isfinite(hi) ? hi + lo : hi; }
+  __device__ __forceinline__ void add(const Table& t, const At& a, const uint4 (&r)[VECS]) {
+    const float s = piece_squares<false>(t, a, r, 1.f);
+    if (s >= 0x1p-90f && s <= 0x1p96f) {
+      add(s);
+    } else {  // (a NaN comes here too)
+      const bool small = s < 1.f;
+      const float q = piece_squares<true>(t, a, r, small ? 0x1p96f : 0x1p-70f);
+      if (q != 0.f) far = fma((double)q, small ? 0x1p-192 : 0x1p140, far);
+    }
+  }
+  __device__ __forceinline__ float value() const { return hi + lo; }
 };
 template <typename F>
 __device__ __forceinline__ F warp_sum(F v) {
@@ -146,24 +186,23 @@ __device__ __forceinline__ F warp_sum(F v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+// A warp's sum, in every lane.
+__device__ __forceinline__ double warp_total(const Sum& s) {
+  const float f = warp_sum(s.value());
+  return __any_sync(0xffffffffu, s.far != 0.0) ? f + warp_sum(s.far) : (double)f;
+}
 // sqrt of a sum of squares, in fp32: past its range either way, by powers of two.
 __device__ __forceinline__ float norm_of(double s) {
   const bool big = s > 1e38, small = s < 1e-30;
-  const float r = __fsqrt_rn((float)(s * (big ? 0x1p-128 : small ? 0x1p128 : 1.0)));
-  return big ? r * 0x1p64f : small ? r * 0x1p-64f : r;  // an infinity and NaN stay
-}
-// The factor: 1 where nothing is to be clipped, as with an infinite max_norm whatever
-// the norm is; else NaN for a NaN norm.
-__device__ __forceinline__ float factor(float norm, float max_norm) {
-  const float by = __fdiv_rn(max_norm, norm);
-  return isinf(max_norm) || norm == 0.f || by > 1.f ? 1.f : by;
+  const float r = __fsqrt_rn((float)(s * (big ? 0x1p-128 : small ? 0x1p192 : 1.0)));
+  return big ? r * 0x1p64f : small ? r * 0x1p-96f : r;  // an infinity and NaN stay
 }
 
 // All pieces in one cluster's registers.
 __global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
     k_clip_small(const __grid_constant__ Table t, float max_norm, float* norm_out, int pieces, int nblocks) {
   __shared__ double part[kClusterBlocks];
-  __shared__ float warps[GROUP * kClusterGroups / 32];
+  __shared__ double warps[GROUP * kClusterGroups / 32];
   __shared__ float shared_norm;
   if (nblocks > 1) ptx::cluster_arrive();
   ptx::griddep_wait();
@@ -181,13 +220,13 @@ __global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
     }
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
-    if (first + k * step < pieces) s.add(piece_squares(t, at[k], r[k]));
-  const float f = warp_sum(s.value());
-  if (lane == 0) warps[warp] = f;
+    if (first + k * step < pieces) s.add(t, at[k], r[k]);
+  const double total = warp_total(s);
+  if (lane == 0) warps[warp] = total;
   __syncthreads();
   if (nblocks > 1) ptx::cluster_wait();
   if (warp == 0) {
-    const double d = warp_sum(lane < (int)(blockDim.x >> 5) ? (double)warps[lane] : 0.0);
+    const double d = warp_sum(lane < (int)(blockDim.x >> 5) ? warps[lane] : 0.0);
     if (nblocks == 1) {
       if (lane == 0) part[0] = d;
     } else if (lane < nblocks) {
@@ -204,15 +243,15 @@ __global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
     if (rank == 0) *norm_out = shared_norm;
   }
   __syncthreads();
-  const float by = factor(shared_norm, max_norm);
+  const Factor by = factor(shared_norm, max_norm);
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
-    if (first + k * step < pieces && (by != 1.f || t.in[at[k].t] != t.out[at[k].t])) store_piece(t, at[k], r[k], tid, by, ptx::l2_evict_normal());
+    if (first + k * step < pieces && (!by.one() || t.in[at[k].t] != t.out[at[k].t])) store_piece(t, at[k], r[k], tid, by, ptx::l2_evict_normal());
 }
 
 // part[blockIdx.x] = the sum of squares of the block's pieces.
 __global__ void __launch_bounds__(GROUP, kResident) k_clip_sums(const __grid_constant__ Table t, int pieces, int keep_from, double* part) {
-  __shared__ float warps[GROUP / 32];
+  __shared__ double warps[GROUP / 32];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint64_t first = ptx::l2_evict_first(), last = ptx::l2_evict_last();
@@ -221,10 +260,10 @@ __global__ void __launch_bounds__(GROUP, kResident) k_clip_sums(const __grid_con
     uint4 r[VECS];
     const At a = at_piece(t, p);
     load_piece(t, a, r, threadIdx.x, p >= keep_from ? last : first);
-    s.add(piece_squares(t, a, r));
+    s.add(t, a, r);
   }
-  const float f = warp_sum(s.value());
-  if (lane == 0) warps[warp] = f;
+  const double total = warp_total(s);
+  if (lane == 0) warps[warp] = total;
   __syncthreads();
   if (threadIdx.x == 0) {
     double d = warps[0];
@@ -246,11 +285,11 @@ __global__ void __launch_bounds__(GROUP, kResident)
     }
   }
   __syncthreads();
-  const float by = factor(shared_norm, max_norm);
+  const Factor by = factor(shared_norm, max_norm);
   const uint64_t first = ptx::l2_evict_first();
   for (int p = pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {
     const At a = at_piece(t, p);
-    if (by == 1.f && t.in[a.t] == t.out[a.t]) continue;
+    if (by.one() && t.in[a.t] == t.out[a.t]) continue;
     uint4 r[VECS];
     load_piece(t, a, r, threadIdx.x, first);
     store_piece(t, a, r, threadIdx.x, by, first);
