@@ -3,7 +3,7 @@
 //
 // The tensors are cut into pieces of 16 KB that thread groups of 256 take in
 // turn.  Few pieces: one cluster of blocks keeps them in registers between the
-// sum and the product (one read; 24010 fp32 values: 4.2 us).  Many: a pass for the
+// sum and the product (one read; 24010 fp32 values: 4.6 us).  Many: a pass for the
 // sums, one partial a block, and a pass in the opposite order for the products,
 // which finds the last pieces in L2 (all others are read and written as first to
 // be evicted).  Bound by HBM, two reads and a write: 268 M fp32 values in 486 us, 6.6 TB/s
@@ -57,6 +57,7 @@ struct Factor {
 // norm is; else NaN for a NaN norm.
 __device__ __forceinline__ Factor factor(float norm, float max_norm) {
   const float by = __fdiv_rn(max_norm, norm);
+  if (by >= 0x1p-100f && by < INFINITY) return Factor{1.f, fminf(by, 1.f)};
   if (isinf(max_norm) || norm == 0.f || by > 1.f) return Factor{1.f, 1.f};
   if (!(by < 0x1p-100f) || isinf(norm) || max_norm == 0.f) return Factor{1.f, by};
   // 2^-floor(log2 norm), at least 2^-126 (norm > 2^-49, since no max_norm is below 2^-149)
@@ -153,16 +154,23 @@ __device__ __forceinline__ void store_piece(const Table& t, const At& a, const u
 // The fp64 units take two lanes a clock and SM, so a thread's sums are fp32 (two
 // of them: the sum and what its roundings lost), a warp's too, and only one lane
 // a warp goes on in fp64, one thread to the square root (with both on every
-// thread 24010 values took 8.2 us in place of 4.2, 2 M 24 in place of 15).
+// thread 24010 values took 8.2 us, 2 M 24).
 //
 // fp32 holds these sums where a piece's lies in [2^-90, 2^96]: what underflowed
 // in it is then nothing beside it, and neither 2^22 of them nor a warp's
-// overflow.  A thread whose piece lies elsewhere (zeros, vanished or exploding
-// gradients) squares it again, times a power of two that brings every fp32
-// magnitude of that side into range, and adds that to `far` in fp64.
+// overflow.  A thread whose piece lies elsewhere (vanished or exploding gradients)
+// squares it again, times a power of two that brings every fp32 magnitude of
+// that side into range, and adds that to `far` in fp64.
+__device__ __forceinline__ bool any_bit(const uint4 (&r)[VECS]) {
+  uint32_t o = 0;
+#pragma unroll
+  for (int j = 0; j < VECS; ++j) o |= r[j].x | r[j].y | r[j].z | r[j].w;
+  return o != 0;
+}
 struct Sum {
   float hi = 0.f, lo = 0.f;
   double far = 0.0;
+  bool has_far = false;  // (the comparison far != 0 takes the fp64 units a quarter us in a block of 1024)
   __device__ __forceinline__ void add(float v) {  // Knuth's two-sum
     const float s = __fadd_rn(hi, v), t = __fsub_rn(s, hi);
     lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fsub_rn(v, t)));
@@ -172,10 +180,13 @@ struct Sum {
     const float s = piece_squares<false>(t, a, r, 1.f);
     if (s >= 0x1p-90f && s <= 0x1p96f) {
       add(s);
-    } else {  // (a NaN comes here too)
+    } else if (s != 0.f || any_bit(r)) {  // (a NaN comes here too)
       const bool small = s < 1.f;
       const float q = piece_squares<true>(t, a, r, small ? 0x1p96f : 0x1p-70f);
-      if (q != 0.f) far = fma((double)q, small ? 0x1p-192 : 0x1p140, far);
+      if (q != 0.f) {
+        far = fma((double)q, small ? 0x1p-192 : 0x1p140, far);
+        has_far = true;
+      }
     }
   }
   __device__ __forceinline__ float value() const { return hi + lo; }
@@ -186,10 +197,15 @@ __device__ __forceinline__ F warp_sum(F v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// A warp's sum, in every lane.
-__device__ __forceinline__ double warp_total(const Sum& s) {
+// The block's warps' sums, to be read after the call.
+__device__ __forceinline__ void warp_totals(const Sum& s, double* warps, int warp, int lane) {
   const float f = warp_sum(s.value());
-  return __any_sync(0xffffffffu, s.far != 0.0) ? f + warp_sum(s.far) : (double)f;
+  if (lane == 0) warps[warp] = f;
+  if (__syncthreads_or(s.has_far)) {
+    const double d = warp_sum(s.far);
+    if (lane == 0) warps[warp] += d;
+    __syncthreads();
+  }
 }
 // sqrt of a sum of squares, in fp32: past its range either way, by powers of two.
 __device__ __forceinline__ float norm_of(double s) {
@@ -221,9 +237,7 @@ __global__ void __launch_bounds__(GROUP * kClusterGroups, 1)
 #pragma unroll
   for (int k = 0; k < kKept; ++k)
     if (first + k * step < pieces) s.add(t, at[k], r[k]);
-  const double total = warp_total(s);
-  if (lane == 0) warps[warp] = total;
-  __syncthreads();
+  warp_totals(s, warps, warp, lane);
   if (nblocks > 1) ptx::cluster_wait();
   if (warp == 0) {
     const double d = warp_sum(lane < (int)(blockDim.x >> 5) ? warps[lane] : 0.0);
@@ -262,9 +276,7 @@ __global__ void __launch_bounds__(GROUP, kResident) k_clip_sums(const __grid_con
     load_piece(t, a, r, threadIdx.x, p >= keep_from ? last : first);
     s.add(t, a, r);
   }
-  const double total = warp_total(s);
-  if (lane == 0) warps[warp] = total;
-  __syncthreads();
+  warp_totals(s, warps, warp, lane);
   if (threadIdx.x == 0) {
     double d = warps[0];
     for (int w = 1; w < GROUP / 32; ++w) d += warps[w];
