@@ -151,6 +151,14 @@ __device__ __forceinline__ void store_piece(const Table& t, const At& a, const u
   else Piece<float>::store(r, static_cast<float*>(t.out[a.t]) + a.from, a.left, tid, wide, by, policy);
 }
 
+// Takes back the priority with which a piece was left in L2.
+__device__ __forceinline__ void release_piece(const Table& t, const At& a, int tid) {
+  const int es = t.bf16s[a.t] ? 2 : 4;
+  const char* const p = static_cast<const char*>(t.in[a.t]) + a.from * es;
+  const char* const line = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(127)) + 128 * tid;
+  if (line < p + min((long long)PIECE, a.left * es)) ptx::l2_evict_normal_line(line);
+}
+
 // The fp64 units take two lanes a clock and SM, so a thread's sums are fp32 (two
 // of them: the sum and what its roundings lost), a warp's too, and only one lane
 // a warp goes on in fp64, one thread to the square root (with both on every
@@ -284,7 +292,8 @@ __global__ void __launch_bounds__(GROUP, kResident) k_clip_sums(const __grid_con
   }
 }
 __global__ void __launch_bounds__(GROUP, kResident)
-    k_clip_scale(const __grid_constant__ Table t, int pieces, const double* part, int parts, float max_norm, float* norm_out) {
+    k_clip_scale(const __grid_constant__ Table t, int pieces, int keep_from, const double* part, int parts, float max_norm,
+                 float* norm_out) {
   __shared__ float shared_norm;
   ptx::griddep_wait();
   if (threadIdx.x < 32) {
@@ -301,7 +310,10 @@ __global__ void __launch_bounds__(GROUP, kResident)
   const uint64_t first = ptx::l2_evict_first();
   for (int p = pieces - 1 - (int)blockIdx.x; p >= 0; p -= gridDim.x) {
     const At a = at_piece(t, p);
-    if (by.one() && t.in[a.t] == t.out[a.t]) continue;
+    if (by.one() && t.in[a.t] == t.out[a.t]) {
+      if (p >= keep_from) release_piece(t, a, threadIdx.x);
+      continue;
+    }
     uint4 r[VECS];
     load_piece(t, a, r, threadIdx.x, first);
     store_piece(t, a, r, threadIdx.x, by, first);
@@ -368,8 +380,8 @@ ff_status clip(const std::vector<Tensor>& all, float max_norm, float* norm, doub
   for (int k = tables - 1; k >= 0; --k) {
     PdlLaunch l(dim3(kBlocks), dim3(GROUP), st);
     FF_LAUNCH(K_CLIP, 2.0 * bytes[k], st,
-              cudaLaunchKernelEx(&l.cfg, k_clip_scale, ts[k], ts[k].first[ts[k].n], (const double*)part, tables * kBlocks,
-                                 max_norm, norm),
+              cudaLaunchKernelEx(&l.cfg, k_clip_scale, ts[k], ts[k].first[ts[k].n], std::max(0, ts[k].first[ts[k].n] - kKeep),
+                                 (const double*)part, tables * kBlocks, max_norm, norm),
               "gradient clipping");
   }
   return FF_OK;

@@ -200,6 +200,10 @@ __device__ __forceinline__ uint64_t l2_evict_last() {
   asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
   return p;
 }
+// Gives the 128-byte L2 line at p (128-byte aligned) that was read to be evicted last its ordinary priority again.
+__device__ __forceinline__ void l2_evict_normal_line(const void* p) {
+  asm volatile("applypriority.global.L2::evict_normal [%0], 128;" ::"l"(p) : "memory");
+}
 __device__ __forceinline__ uint4 ld_hint(const void* p, uint64_t policy) {
   uint4 v;
   asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"

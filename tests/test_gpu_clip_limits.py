@@ -99,3 +99,17 @@ def test_large_small_and_moderate_gradients_together(path):
         assert abs(norm - exact) <= 21 * 2.0 ** -24 * exact
         want = t.double() * (float(torch.tensor(exact / 2)) / exact)
         assert bool(((out.double() - want).abs() <= 24 * 2.0 ** -24 * want.abs() + 2.0 ** -148).all())
+
+
+@pytest.mark.parametrize("lead", [0, 1, 61, 64])
+def test_gradients_left_alone_keep_their_neighbours(lead):
+    """Nothing is clipped: what the second pass does with the lines that the first one left in L2 changes no value, at
+    whatever place in a line the tensors start and end."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    for dt in (torch.float32, torch.bfloat16):
+        buf = torch.randn(3_000_001, device="cuda").to(dt)
+        keep, g = buf.clone(), [buf[lead:lead + 1_000_003], buf[1_500_000:1_500_003], buf[1_500_007:2_999_999]]
+        for limit in (math.inf, 1e9):
+            ff.clip_grad_norm(g, limit)
+            assert torch.equal(buf, keep)
