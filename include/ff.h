@@ -647,8 +647,11 @@ FF_API ff_status ff_fp8_selftest_wait(unsigned int timeout_us, void* stream);
  * gamma [cols] fp32, NULL: ones.  h is required with a residual and NULL
  * without.  rstd [rows] fp32 or NULL.  y may be x or the residual itself, and
  * so may h (but not both the same); where they share values in another way the
- * call is refused.  Squares are formed in fp32: magnitudes past
- * 2^63 overflow (rstd is then 0); a NaN in a row makes the whole row NaN. */
+ * call is refused.  Squares are formed in fp32, and where a row's sum of them is
+ * past its range, again of h 2^-80, so that all finite rows have their rstd (in
+ * fewer bits past a root mean square of 2^126, where it is below 2^-126).  Squares
+ * below 2^-149 vanish, which an eps near them would show.  An infinity in a row
+ * makes its rstd 0, a NaN the whole row NaN. */
 FF_API ff_status ff_rms_norm(const void* x, long long ldx, const void* residual, long long ldr, int rows, int cols,
                              const float* gamma, float eps, ff_precision prec, void* h, long long ldh, void* y,
                              long long ldy, void* q, float* scale, float* rstd, void* stream);
@@ -662,8 +665,9 @@ FF_API long long ff_rms_norm_workspace(int rows, int cols);
  *   dx = rstd (du - n <du n>) + dh,   dgamma = sum over rows of dy n.
  * dx is the gradient of x and of the residual alike; dh [rows, cols] is what
  * the residual stream hands back, or NULL.  dx may be dy, h or dh itself, but may
- * not share values with them in another way; dx or dgamma [cols] fp32 may be NULL.  Sums have a fixed order.  No rows: dgamma
- * is set to zero. */
+ * not share values with them in another way; dx or dgamma [cols] fp32 may be
+ * NULL.  Sums have a fixed order, in fp32: n, du and sums of their products have
+ * to be in its range.  No rows: dgamma is set to zero. */
 FF_API ff_status ff_rms_norm_backward(const void* dy, long long lddy, const void* h, long long ldh, int rows, int cols,
                                       const float* rstd, const float* gamma, const void* dh, long long lddh,
                                       ff_precision prec, void* dx, long long lddx, float* dgamma, void* workspace,

@@ -136,7 +136,8 @@ __device__ __forceinline__ float sum_of(uint64_t v) {
 __device__ __forceinline__ void row_barrier(int warps) { ptx::named_bar(1, warps * 32); }
 
 // The sum over a row's warps of v, in a fixed order, through part[kMaxWarps]
-// (not used again before the row's warps have met once more).
+// (not used again before the row's warps have met once more), the same bits in
+// every lane.
 __device__ __forceinline__ float row_sum(float v, int warps, int warp, int lane, float* part) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -199,13 +200,66 @@ __device__ __forceinline__ void put_fp8(const RmsArgs<T>& a, long long row, cons
   }
 }
 __device__ __forceinline__ float rstd_of(float sum, int cols, float eps) { return __frsqrt_rn(__fdiv_rn(sum, (float)cols) + eps); }
+// A row that is not held in registers: a warp reads its units at columns c0,
+// c0 + step, .. before `end` (and before the row's) again.
+struct Units {
+  long long c0, end;
+  int step;
+};
+template <typename T>
+__device__ __forceinline__ const T* h_of(const RmsArgs<T>& a, long long row) {  // each thread reads what it wrote itself
+  return a.r ? a.h + row * a.ldh : a.x + row * a.ldx;
+}
+// rstd from the squares of h 2^-80, for a row whose own squares' sum is past
+// fp32's range: of no finite row theirs is, and all that vanishes in it does so
+// beside a value of 2^64 / sqrt(cols) at least.
+template <typename T, int V>
+__device__ __forceinline__ float far_rstd(const RmsArgs<T>& a, long long row, Units at, int warps, int warp, int lane, float* part) {
+  constexpr float by = 0x1p-80f;
+  const T* h = h_of(a, row);
+  uint64_t ss = 0;
+#pragma unroll 1
+  for (long long c = at.c0; c < at.end; c += at.step) {
+    Unit<T, V> u;
+    uint64_t v[2];
+    u.load(h, (int)c, lane, a.cols);
+    u.pairs(v);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint64_t w = ptx::mul2(v[e], both(by));
+      ptx::fma2_to(ss, w, w);
+    }
+  }
+  return rstd_of(row_sum(sum_of(ss), warps, warp, lane, part), a.cols, a.eps * by * by) * by;
+}
+template <typename T, int V>
+__device__ __forceinline__ void outputs_from_memory(const RmsArgs<T>& a, long long row, Units at, int lane, float rstd) {
+  const T* h = h_of(a, row);
+  for (long long c = at.c0; c < at.end; c += at.step) {
+    Unit<T, V> u;
+    uint64_t y[2];
+    u.load(h, (int)c, lane, a.cols);
+    u.pairs(y);
+    outputs<T, V>(a, y, (int)c, lane, rstd);
+    if (a.q) {
+      const float s = scale_of(amax_of(y));
+      if (lane == 0) a.scale[c / UNIT * a.rows + row] = s;
+      put_fp8<T, V>(a, row, y, (int)c, lane, __frcp_rn(s));
+    }
+    if (a.y) {
+      u.set(y);
+      u.store(a.y + row * a.ldy, (int)c, lane, a.cols);
+    }
+  }
+}
 
 // NU units a warp, the row in registers.  blockDim: a row's warps, or with one
 // warp a row, several rows.  whole: all of the warp's units lie inside the row
 // (without this twin the rows of single values, with four comparisons a unit,
-// took half as long again).
+// took half as long again).  Returns false, for all of the row's warps, where the
+// squares are past fp32's range; rstd and outputs are then still to be written.
 template <typename T, int V, int NU>
-__device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int warp, int lane, float* part, bool whole) {
+__device__ __forceinline__ bool rms_row(const RmsArgs<T>& a, long long row, int warp, int lane, float* part, bool whole) {
   Unit<T, V> u[NU];
   const int c0 = warp * NU * UNIT;
 #pragma unroll
@@ -229,6 +283,7 @@ __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int 
     ptx::fma2_to(ss[1], v[1], v[1]);
   }
   const float sum = row_sum(sum_of(ptx::add2(ss[0], ss[1])), a.warps, warp, lane, part);
+  if (sum == INFINITY) return false;
   const float rstd = rstd_of(sum, a.cols, a.eps);
   if (a.rstd && warp == 0 && lane == 0) a.rstd[row] = rstd;
   if (a.y) {
@@ -260,25 +315,35 @@ __device__ __forceinline__ void rms_row(const RmsArgs<T>& a, long long row, int 
     for (int i = 0; i < NU; ++i)
       put_fp8<T, V>(a, row, y[i], c0 + i * UNIT, lane, __shfl_sync(0xffffffffu, inv, i), whole);
   }
+  return true;
+}
+// The rest of such a row, apart from the kernel's own code, whose registers it
+// would take (in line, on the values held, 8000 x 4097 out of L2 took 37.5 us for 36.2).
+template <typename T, int V>
+__device__ __noinline__ void far_row(const RmsArgs<T>& a, long long row, long long c0, long long end, float* part) {
+  const int lane = threadIdx.x & 31, warp = a.warps == 1 ? 0 : threadIdx.x >> 5;
+  const Units at{c0, end, UNIT};
+  const float rstd = far_rstd<T, V>(a, row, at, a.warps, warp, lane, part);
+  if (a.rstd && warp == 0 && lane == 0) a.rstd[row] = rstd;
+  outputs_from_memory<T, V>(a, row, at, lane, rstd);
 }
 template <typename T, int V, int NU>
-__global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const RmsArgs<T> a) {
-  __shared__ float part[kMaxWarps];
+__global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const __grid_constant__ RmsArgs<T> a) {
+  __shared__ float part[2 * kMaxWarps];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int warp = a.warps == 1 ? 0 : w;
   const long long row = a.warps == 1 ? (long long)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
   if (row >= a.rows) return;
-  if ((warp + 1) * NU * UNIT <= a.cols)
-    rms_row<T, V, NU>(a, row, warp, lane, part, true);
-  else
-    rms_row<T, V, NU>(a, row, warp, lane, part, false);
+  const bool done = (warp + 1) * NU * UNIT <= a.cols ? rms_row<T, V, NU>(a, row, warp, lane, part, true)
+                                                    : rms_row<T, V, NU>(a, row, warp, lane, part, false);
+  if (!done) far_row<T, V>(a, row, (long long)warp * NU * UNIT, min((long long)a.cols, (warp + 1ll) * NU * UNIT), part + kMaxWarps);
 }
 
 // Rows too long for registers: read twice (the second time h, which is in L2).
 template <typename T, int V>
 __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_long(const RmsArgs<T> a) {
-  __shared__ float part[kMaxWarps];
+  __shared__ float part[2 * kMaxWarps];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long row = blockIdx.x;
@@ -297,25 +362,11 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms_long(const RmsArgs<T> a)
     ptx::fma2_to(ss[1], v[1], v[1]);
   }
   const float sum = row_sum(sum_of(ptx::add2(ss[0], ss[1])), kMaxWarps, warp, lane, part);
-  const float rstd = rstd_of(sum, a.cols, a.eps);
+  float rstd = rstd_of(sum, a.cols, a.eps);
+  const Units at{(long long)warp * UNIT, a.cols, kMaxWarps * UNIT};
+  if (sum == INFINITY) rstd = far_rstd<T, V>(a, row, at, kMaxWarps, warp, lane, part + kMaxWarps);
   if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-  const T* h = a.r ? a.h + row * a.ldh : a.x + row * a.ldx;  // each thread reads what it wrote itself
-  for (long long c = (long long)warp * UNIT; c < a.cols; c += kMaxWarps * UNIT) {
-    Unit<T, V> u;
-    uint64_t y[2];
-    u.load(h, (int)c, lane, a.cols);
-    u.pairs(y);
-    outputs<T, V>(a, y, (int)c, lane, rstd);
-    if (a.q) {
-      const float s = scale_of(amax_of(y));
-      if (lane == 0) a.scale[c / UNIT * a.rows + row] = s;
-      put_fp8<T, V>(a, row, y, (int)c, lane, __frcp_rn(s));
-    }
-    if (a.y) {
-      u.set(y);
-      u.store(a.y + row * a.ldy, (int)c, lane, a.cols);
-    }
-  }
+  outputs_from_memory<T, V>(a, row, at, lane, rstd);
 }
 
 // -------------------------------------------------------------- gradient
@@ -528,9 +579,9 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
           for (int j = 0; j < P; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const uint64_t yh = ptx::mul2(y[j][e], x[j][e]);
-              ptx::fma2_to(acc[i + j][e], yh, both(rstd[r]));
-              ptx::fma2_to(dot2, yh, g[i + j][e]);
+              const uint64_t yn = ptx::mul2(y[j][e], ptx::mul2(x[j][e], both(rstd[r])));
+              acc[i + j][e] = ptx::add2(acc[i + j][e], yn);
+              ptx::fma2_to(dot2, yn, g[i + j][e]);
             }
         }
       }
@@ -540,7 +591,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (row + r >= a.rows || !out) break;
-      const uint64_t off = both(-dot[r] * a.inv_cols * rstd[r] * rstd[r] * rstd[r]);  // what h is taken off by
+      const uint64_t off = both(-dot[r] * a.inv_cols * rstd[r]), by = both(rstd[r]);  // -<du n> rstd
 #pragma unroll
       for (int i = 0; i < NU; i += P) {
         if (!whole && c0 + i * UNIT >= a.cols) break;
@@ -551,7 +602,7 @@ __device__ __forceinline__ void grad_rows(const GradArgs<T>& a, uint64_t (&acc)[
         for (int j = 0; j < P; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            x[j][e] = ptx::fma2(x[j][e], off, ptx::mul2(both(rstd[r]), ptx::mul2(g[i + j][e], y[j][e])));
+            x[j][e] = ptx::mul2(by, ptx::fma2(x[j][e], off, ptx::mul2(g[i + j][e], y[j][e])));
         if (a.dh) {
           part_pairs<T, V>(y, now + r * rb + 2 * part1, i, odd(a.dh, a.lddh, row + r), lane);
 #pragma unroll
