@@ -1163,6 +1163,8 @@ def _rms_norm(x, gamma, residual, eps, out, h, fp8, stream):
             out, ldy = new(*_dense(x.shape), dt), cols
         else:
             ldy = _like(out, x, "out")
+            if residual is None and rows and out.data_ptr() == x.data_ptr():
+                kept = None  # x's values are gone
         py = out.data_ptr()
     rstd = new((rows,), (1,), torch.float32)
     _check(lib().ff_rms_norm(x.data_ptr(), ldx, pr, ldr, rows, cols, _vector(gamma, cols, "gamma", dev), eps, prec, ph, ldh, py,
@@ -1178,7 +1180,8 @@ def rms_norm(x, gamma, residual=None, eps: float = 1e-5, out=None, h=None, strea
     """ff_rms_norm: h = x + residual, y = gamma * h * rstd with rstd = 1 /
     sqrt(mean h^2 + eps) over the last dimension.  x, residual [..., cols] (bf16
     or fp32, evenly spaced rows), gamma fp32 [cols] or None.  Returns (y, h,
-    rstd): h is x itself without a residual, rstd fp32 [rows].  out and h are
+    rstd): h is x itself without a residual (None if out is x: the gradient
+    needs the values that are then gone), rstd fp32 [rows].  out and h are
     optional buffers; either may be x or the residual, not both the same.  Not
     recorded by autograd: its gradient is rms_norm_backward."""
     return _rms_norm(x, gamma, residual, eps, out, h, False, stream)
