@@ -818,6 +818,11 @@ def _unrecorded(name, depth=4):
                       f"own; use torch.no_grad() or detach() where that is meant)", stacklevel=depth)
 
 
+# Calls write buffers that they are given behind autograd's back: this lets it
+# refuse a later backward pass that would read a tensor's values from before.
+_written = torch.autograd.graph.increment_version
+
+
 def _vector(t, size, what, device):
     if t is None:
         return None
@@ -871,6 +876,7 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
     n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 0)
     on, empty = _on(stream, dev, x, gamma, beta, out, mean, rstd)
     ldx = _row_stride_of(x, "x")
+    given = [t for t in (out, mean, rstd) if t is not None]
     if out is None:
         out, ldy = empty(x.shape, dtype=x.dtype, device=dev), C
     else:
@@ -890,6 +896,8 @@ def group_norm_act(x, gamma, beta, groups: int, act: str = "silu", eps: float = 
         x.data_ptr(), ldx, n, spatial, C, groups, _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
         eps, kind, prec, out.data_ptr(), ldy, pm, pr, None if ws is None else ws.data_ptr(), need, on),
         "ff_group_norm_act")
+    if given:
+        _written(given)
     if x.requires_grad or (gamma is not None and gamma.requires_grad) or (beta is not None and beta.requires_grad):
         _unrecorded("group_norm_act")
     return out, mean, rstd
@@ -904,6 +912,7 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
     n, spatial, C, groups, kind, need = _norm_sizes(x.shape, groups, act, prec, 1)
     on, empty = _on(stream, dev, dy, x, mean, rstd, gamma, beta, out)
     ldx, lddy = _row_stride_of(x, "x"), _like(dy, x, "dy")
+    given = out
     if out is None:
         out, lddx = empty(x.shape, dtype=x.dtype, device=dev), C
     else:
@@ -918,6 +927,8 @@ def group_norm_act_backward(dy, x, mean, rstd, gamma, beta, groups: int, act: st
         _vector(rstd, n * groups, "rstd", dev), _vector(gamma, C, "gamma", dev), _vector(beta, C, "beta", dev),
         kind, prec, out.data_ptr(), lddx, dgamma.data_ptr(), dbeta.data_ptr(),
         None if ws is None else ws.data_ptr(), need, on), "ff_group_norm_act_backward")
+    if given is not None:
+        _written(given)
     return out, dgamma, dbeta
 
 
@@ -943,6 +954,7 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     rows = x.numel() // cols if cols else 0
     ldx = _row_stride_of(x, "x")
     ldr = _like(residual, x, "residual") if residual is not None else 0
+    given = out
     if out is None:
         out, ldy = empty(x.shape, dtype=x.dtype, device=dev), cols
     else:
@@ -958,6 +970,8 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, out=None, stream=No
     _check(lib().ff_dropout(x.data_ptr(), ldx, rows, cols, p, int(seed) & 0xFFFFFFFFFFFFFFFF, host, odev,
                             None if residual is None else residual.data_ptr(), ldr, prec, out.data_ptr(), ldy,
                             on), "ff_dropout")
+    if given is not None:
+        _written(given)
     if x.requires_grad or (residual is not None and residual.requires_grad):
         _unrecorded("dropout")
     return out
@@ -1050,6 +1064,7 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _same_device(b.q, dev, "b")
     on, empty = _on(stream, dev, a.q, a.scale, b.q, b.scale, bias, out, status)
     m, n = a.rows, b.rows
+    given = out
     if out is None:
         prec = _PREC.get(out_dtype)
         if prec is None:
@@ -1065,6 +1080,8 @@ def fp8_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _check(lib().ff_fp8_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), b.blocks, m,
                                n, a.k, _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
                                _ptr(status, torch.int32, "status"), on), "ff_fp8_matmul")
+    if given is not None:
+        _written(given)
     if bias is not None and bias.requires_grad:
         _unrecorded("fp8_matmul")
     return out
@@ -1142,7 +1159,7 @@ def _rms_norm(x, gamma, residual, eps, out, h, fp8, stream):
     on, new = _place(stream, dev.index, (x, gamma, residual, out, h))
     ldr = ldh = ldy = 0
     pr = ph = py = pq = ps = None
-    kept = x
+    kept, given = x, None if out is None and h is None else [t for t in (out, h) if t is not None]
     if residual is not None:
         ldr, pr = _like(residual, x, "residual"), residual.data_ptr()
         if h is None:
@@ -1169,6 +1186,8 @@ def _rms_norm(x, gamma, residual, eps, out, h, fp8, stream):
     rstd = new((rows,), (1,), torch.float32)
     _check(lib().ff_rms_norm(x.data_ptr(), ldx, pr, ldr, rows, cols, _vector(gamma, cols, "gamma", dev), eps, prec, ph, ldh, py,
                              ldy, pq, ps, rstd.data_ptr(), on), "ff_rms_norm")
+    if given:
+        _written(given)
     if (x.requires_grad or (gamma is not None and gamma.requires_grad)
             or (residual is not None and residual.requires_grad)):
         _unrecorded("rms_norm_fp8" if fp8 else "rms_norm", depth=5)
@@ -1207,6 +1226,7 @@ def rms_norm_backward(dy, h, rstd, gamma, dh=None, out=None, stream=None):
     lddh = 0 if dh is None else _like(dh, dy, "dh")
     if rstd is None:
         raise ValueError("rstd of the forward pass is needed")
+    given = out
     if out is None:
         out, lddx = new(*_dense(dy.shape), dy.dtype), cols
     else:
@@ -1218,6 +1238,8 @@ def rms_norm_backward(dy, h, rstd, gamma, dh=None, out=None, stream=None):
                                       _vector(gamma, cols, "gamma", dev), None if dh is None else dh.data_ptr(), lddh, prec,
                                       out.data_ptr(), lddx, dgamma.data_ptr(), None if ws is None else ws.data_ptr(), need,
                                       on), "ff_rms_norm_backward")
+    if given is not None:
+        _written(given)
     return out, dgamma
 
 
@@ -1287,6 +1309,7 @@ def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy
     if dentropy is not None and entropy is None:
         raise ValueError("dentropy needs the forward pass's entropy")
     on, new = _place(stream, dev.index, (logits, labels, stats, dlogp, entropy, dentropy, out))
+    given = out
     if out is None:
         out, ldo = new(*_dense(logits.shape), logits.dtype), classes
     else:
@@ -1295,6 +1318,8 @@ def label_logprobs_backward(logits, labels, stats, dlogp, entropy=None, dentropy
         logits.data_ptr(), ld, rows, classes, prec, None if labels is None else _labels(labels, rows, dev),
         _vector(stats, 2 * rows, "stats", dev), _vector(dlogp, rows, "dlogp", dev), _vector(entropy, rows, "entropy", dev),
         _vector(dentropy, rows, "dentropy", dev), out.data_ptr(), ldo, on), "ff_label_logprobs_backward")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1335,11 +1360,14 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
         out = list(out)
         if len(out) != n:
             raise ValueError("out must have a tensor for each of grads")
-        for o, g in zip(out, grads):
-            if (not isinstance(o, torch.Tensor) or o.shape != g.shape or o.dtype is not g.dtype or o.get_device() != index
-                    or not o.is_contiguous()):
-                raise ValueError("out must match grads in shape, type and device, and be contiguous")
-        to = [o.data_ptr() for o in out]
+        try:
+            like = (set(map(torch.Tensor.get_device, out)) == {index} and all(map(torch.Tensor.is_contiguous, out))
+                    and [o.shape for o in out] == [g.shape for g in grads] and [o.dtype for o in out] == [g.dtype for g in grads])
+        except TypeError:  # not a tensor
+            like = False
+        if not like:
+            raise ValueError("out must match grads in shape, type and device, and be contiguous")
+        to = list(map(torch.Tensor.data_ptr, out))
     on, new = _place(stream, index, () if stream is None else (*grads, *(out or ())))
     need = _clip_workspace(n)
     # (the array module's: ctypes' own arrays take four times as long to fill, 15 us for 60 tensors)
@@ -1349,6 +1377,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, stream=None):
     ws = new((need,), (1,), torch.uint8)
     _check(lib().ff_clip_grad_norm(at, at + 8 * n, at + 16 * n, types.buffer_info()[0], n, max_norm, norm.data_ptr(), ws.data_ptr(), need,
                                    on), "ff_clip_grad_norm")
+    _written(grads if out is None else out)
     return norm
 
 
@@ -1430,6 +1459,7 @@ def fp4_dequantize(m, out=None, out_dtype=torch.bfloat16, stream=None):
         raise TypeError("m must be a Fp4Matrix")
     rows, k = m.rows, m.k
     on, new = _place(stream, m.q.get_device(), (m.q, m.scale, out))
+    given = out
     if out is None:
         prec = _PREC.get(out_dtype)
         if prec is None:
@@ -1442,6 +1472,8 @@ def fp4_dequantize(m, out=None, out_dtype=torch.bfloat16, stream=None):
         prec, ldy = _prec(out, "out"), _row_stride_of(out, "out")
     _check(lib().ff_fp4_dequantize(m.q.data_ptr(), m.scale.data_ptr(), rows, k, prec, out.data_ptr(), ldy, on),
            "ff_fp4_dequantize")
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1459,6 +1491,7 @@ def fp4_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _same_device(b.q, dev, "b")
     on, new = _place(stream, dev.index, (a.q, a.scale, b.q, b.scale, bias, out, status))
     m, n = a.rows, b.rows
+    given = out
     if out is None:
         prec = _PREC.get(out_dtype)
         if prec is None:
@@ -1474,6 +1507,8 @@ def fp4_matmul(a, b, bias=None, relu: bool = False, out=None, out_dtype=torch.bf
     _check(lib().ff_fp4_matmul(a.q.data_ptr(), a.scale.data_ptr(), b.q.data_ptr(), b.scale.data_ptr(), m, n, a.k,
                                _vector(bias, n, "bias", dev), 1 if relu else 0, prec, out.data_ptr(), ldc,
                                _ptr(status, torch.int32, "status"), on), "ff_fp4_matmul")
+    if given is not None:
+        _written(given)
     if bias is not None and bias.requires_grad:
         _unrecorded("fp4_matmul")
     return out
