@@ -880,6 +880,7 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
 // us, one a set 79).  The rest of the shared memory deepens the queue.  (Sized for three arrays whether dh is there or not, so that the
 // workspace does not depend on it.)
 constexpr int kGradSmem = 200 * 1024;
+static_assert(kGradWarps * 8 * 32 * (int)sizeof(Held<float>) * 3 <= kGradSmem, "the longest row of the row kernel");
 constexpr int kGradEnds = 4 * 2 * 3 * kGradWarps * 16;  // and at most what single bf16 values add to their copies
 struct GradPlan {
   int nu, warps, teams, set, blocks, depth;
@@ -897,7 +898,6 @@ GradPlan grad_plan(int rows, int cols, int esize) {
     p.teams = p.warps == 1 ? kOwnRows : 1;
     threads = p.warps * p.teams * 32;
     row = threads * p.nu * 4 * esize * 3;  // bytes
-    if (row > kGradSmem) p.nu = 0;
   }
   long long fill;
   if (p.nu) {
@@ -954,8 +954,12 @@ ff_status rms_grad_t(GradArgs<T> a, float* dgamma, void* ws, cudaStream_t st) {
         const size_t smem = std::max(ring, p.teams > 1 && a.part ? (size_t)p.teams * a.cols * 4 : 0);
         PdlLaunch l(dim3((unsigned)p.blocks), dim3((unsigned)threads), st, smem);
         auto go = [&](auto N, auto R) -> cudaError_t {
-          if constexpr (V.value == 8 && N.value == 1) {
-            return cudaErrorInvalidValue;  // (see `eight`)
+          // what grad_plan gives: one row a set with eight units, with four of fp32 and
+          // with single bf16 values; two with less than eight (and see `eight`)
+          constexpr bool planned =
+              R.value == 2 ? N.value < 8 : N.value == 8 || (N.value == 4 && sizeof(T) == 4) || Lay<T, V.value>::WORDS;
+          if constexpr (!planned || (V.value == 8 && N.value == 1)) {
+            return cudaErrorInvalidValue;
           } else {
             const cudaError_t e = allow_smem<k_rms_grad<T, V.value, N.value, R.value>>(kGradSmem + kGradEnds);
             return e != cudaSuccess ? e : cudaLaunchKernelEx(&l.cfg, k_rms_grad<T, V.value, N.value, R.value>, a);
