@@ -84,3 +84,30 @@ def test_backward(cols, h_scale, dy_scale, dtype):
         assert bool(((dx.double() - want).abs() <= tol + 2.0 ** -130).all())
         terms = dy.double() * n
         assert bool(((dgamma.double() - terms.sum(0)).abs() <= 20 * U * terms.abs().sum(0) + 2.0 ** -140).all())
+
+
+@pytest.mark.parametrize("cols", [500, 2001, 8192, 40000])
+def test_in_place(cols):
+    """Rows past fp32's range are read again after their residual's sum is written, and before their output is."""
+    torch = torch_cuda()
+    ff = lib_ready()
+    gamma = torch.randn(cols, generator=torch.Generator().manual_seed(2)).cuda()
+    for dt in (torch.bfloat16, torch.float32):
+        x = rows_of(torch, cols, 2.0 ** 80, dt, 1)
+        r = x.flip(1).contiguous() * 0.0625
+        y, _, rstd = ff.rms_norm(x, gamma)
+        a = x.clone()
+        assert torch.equal(ff.rms_norm(a, gamma, out=a)[2], rstd) and torch.equal(a, y)
+        y, h, rstd = ff.rms_norm(x, gamma, residual=r)
+        a, b = x.clone(), r.clone()
+        ff.rms_norm(a, gamma, residual=b, out=a, h=b)
+        assert torch.equal(a, y) and torch.equal(b, h)
+        a, b = x.clone(), r.clone()
+        ff.rms_norm(a, gamma, residual=b, out=b, h=a)
+        assert torch.equal(b, y) and torch.equal(a, h)
+        graph, a = torch.cuda.CUDAGraph(), torch.zeros_like(x)
+        with torch.cuda.graph(graph):
+            held = ff.rms_norm(a, gamma, residual=r)
+        a.copy_(x)
+        graph.replay()
+        assert torch.equal(held[0], y) and torch.equal(held[1], h) and torch.equal(held[2], rstd)
