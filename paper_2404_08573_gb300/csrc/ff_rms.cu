@@ -318,18 +318,27 @@ __device__ __forceinline__ bool rms_row(const RmsArgs<T>& a, long long row, int 
   return true;
 }
 // The rest of such a row, apart from the kernel's own code, whose registers it
-// would take (in line, on the values held, 8000 x 4097 out of L2 took 37.5 us for 36.2).
+// would take.  The arguments by reference to the kernel's own (a __grid_constant__)
+// where units are whole vectors, else by value: the other way round, or with all of it
+// in line, one or another of the kernels spills and takes 5 to 12 % longer
+// (4096 x 8192 fp32 43.2 and 45.2 us; 8000 x 4097 fp32 with a residual 83.0 and 92.6).
 template <typename T, int V>
-__device__ __noinline__ void far_row(const RmsArgs<T>& a, long long row, long long c0, long long end, float* part) {
-  const int lane = threadIdx.x & 31, warp = a.warps == 1 ? 0 : threadIdx.x >> 5;
-  const Units at{c0, end, UNIT};
+using FarArgs = std::conditional_t<V == 4, const RmsArgs<T>&, const RmsArgs<T>>;
+template <typename T, int V, int NU>
+__device__ __noinline__ void far_row(FarArgs<T, V> a) {
+  __shared__ float part[kMaxWarps];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int warp = a.warps == 1 ? 0 : w;
+  const long long row = a.warps == 1 ? (long long)blockIdx.x * (blockDim.x >> 5) + w : blockIdx.x;
+  const long long c0 = (long long)warp * NU * UNIT;
+  const Units at{c0, min((long long)a.cols, c0 + NU * UNIT), UNIT};
   const float rstd = far_rstd<T, V>(a, row, at, a.warps, warp, lane, part);
   if (a.rstd && warp == 0 && lane == 0) a.rstd[row] = rstd;
   outputs_from_memory<T, V>(a, row, at, lane, rstd);
 }
 template <typename T, int V, int NU>
-__global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const __grid_constant__ RmsArgs<T> a) {
-  __shared__ float part[2 * kMaxWarps];
+__device__ __forceinline__ void rms_rows(const RmsArgs<T>& a) {
+  __shared__ float part[kMaxWarps];
   ptx::griddep_wait();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int warp = a.warps == 1 ? 0 : w;
@@ -337,7 +346,15 @@ __global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const __grid_constant__ 
   if (row >= a.rows) return;
   const bool done = (warp + 1) * NU * UNIT <= a.cols ? rms_row<T, V, NU>(a, row, warp, lane, part, true)
                                                     : rms_row<T, V, NU>(a, row, warp, lane, part, false);
-  if (!done) far_row<T, V>(a, row, (long long)warp * NU * UNIT, min((long long)a.cols, (warp + 1ll) * NU * UNIT), part + kMaxWarps);
+  if (!done) far_row<T, V, NU>(a);
+}
+template <typename T, int NU>
+__global__ void __launch_bounds__(kMaxWarps * 32) k_rms(const __grid_constant__ RmsArgs<T> a) {
+  rms_rows<T, 4, NU>(a);
+}
+template <typename T, int V, int NU>
+__global__ void __launch_bounds__(kMaxWarps * 32) k_rms_narrow(const RmsArgs<T> a) {
+  rms_rows<T, V, NU>(a);
 }
 
 // Rows too long for registers: read twice (the second time h, which is in L2).
@@ -862,11 +879,15 @@ ff_status rms_t(RmsArgs<T> a, cudaStream_t st) {
       a.warps = cdiv(cdiv(a.cols, UNIT), nu);
       PdlLaunch l(dim3((unsigned)(a.warps == 1 ? cdiv(a.rows, kOwnRows) : a.rows)),
                   dim3((unsigned)(a.warps == 1 ? kOwnRows : a.warps) * 32), st);
+      auto go_on = [&](auto N) {
+        if constexpr (V.value == 4) return cudaLaunchKernelEx(&l.cfg, k_rms<T, N.value>, a);
+        else return cudaLaunchKernelEx(&l.cfg, k_rms_narrow<T, V.value, N.value>, a);
+      };
       switch (nu) {
-        case 1: return cudaLaunchKernelEx(&l.cfg, k_rms<T, V.value, 1>, a);
-        case 2: return cudaLaunchKernelEx(&l.cfg, k_rms<T, V.value, 2>, a);
-        case 4: return cudaLaunchKernelEx(&l.cfg, k_rms<T, V.value, 4>, a);
-        default: return cudaLaunchKernelEx(&l.cfg, k_rms<T, V.value, 8>, a);
+        case 1: return go_on(std::integral_constant<int, 1>{});
+        case 2: return go_on(std::integral_constant<int, 2>{});
+        case 4: return go_on(std::integral_constant<int, 4>{});
+        default: return go_on(std::integral_constant<int, 8>{});
       }
     });
   };
