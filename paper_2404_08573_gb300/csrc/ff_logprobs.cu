@@ -28,6 +28,10 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either i
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+// 2^v to 2^-22 of itself, below 2^-126 zero: enough for the sums of either type,
+// since a class's error counts by its probability, as does that of rounding the
+// exponent (|d| e^d 2^-24, at most 2^-25), and ln s and t / s are then within some
+// 2^-21.  The fp32 gradient, whose elements stand for themselves, has expf.
 __device__ __forceinline__ float exp2_approx(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -269,7 +273,8 @@ constexpr int kOwnPool = kPool / kOwnRows;
 //
 // WARPS: the most a block has.  Rows are many with 8: five blocks an SM keep
 // 80 KB of loads in flight while others select (2048 x 49999 fp32: top 0 66 us, with
-// four 71, with six, which spill, 73; top 4 77, 82, 88).
+// four 71, with six 73; top 4 77, 82, 88).  bf16 with the likeliest spills a few words
+// at five, all of them at six.
 template <typename T, bool TOP, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 5 : 1) k_logprobs(const Args<T> a) {
   constexpr int N = Load<T>::N;

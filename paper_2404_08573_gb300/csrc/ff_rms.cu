@@ -10,7 +10,8 @@
 // Fewer instructions made it so (169 us before): sums and products on pairs of
 // values, the residual added in bf16, one division a lane for all of a warp's
 // scales.  A single row is a launch (1 x 2000: 2.1 us).  Rows that are aligned to
-// single values only take twice as long (8000 x 4097 bf16 to e4m3: 67 us, floor 34).
+// single values only take 1.6 times as long (8000 x 4097 bf16 with a residual to
+// e4m3: 55 us, floor 34).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -517,10 +518,12 @@ __device__ __forceinline__ void row_sums(float (&v)[R], int warps, int warp, int
 // A block takes R rows at a time, sets of them gridDim.x apart; each lane keeps
 // gamma and its columns' sums of dgamma in registers over all of them, so that
 // dy and h are read once.  The rows to come are on their way into shared memory
-// (`depth` sets, each thread its own values, so that no barrier is needed)
-// while these are worked on.  With one warp a row the block's warps take rows of
+// (`depth` sets, each thread its own values, so that no barrier is needed; of
+// single bf16 values a warp's words, and a __syncwarp) while these are worked on.  With one warp a row the block's warps take rows of
 // their own and join their sums in shared memory ([warps][cols]).
-// Bound by HBM in fp32 (4096 x 8192 with dh: 86 us, floor 80) and in bf16 by the
+// h comes into products as n = h rstd (0.2 us of 47, bf16): dy h or rstd^2 may
+// leave fp32's range where n, dy and dx do not.
+// Bound by HBM in fp32 (4096 x 8192 with dh: 85 us, floor 80) and in bf16 by the
 // latency of a set's two halves and the barrier between them (42 us and the fold's
 // 5, floor 40).  (gamma read anew each time came from L2, since the copies take
 // L1's place, and one row at a time pays the barrier for each: 60 us in all.)
