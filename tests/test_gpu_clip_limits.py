@@ -32,7 +32,7 @@ def test_an_infinite_limit_asks_for_the_norm_alone(path, dtype, value):
 # Magnitudes: squares that overflow fp32 alone (1e30, 2^127) or added up (2^62 by
 # the thread, 2^58 by the warp or the block), lose bits (1e-20) or vanish (1e-25, 1e-38,
 # and 2^-140, which fp32 itself holds in nine bits).
-SCALES = {"2^127": 2.0 ** 127, "1e30": 1e30, "2^62": 2.0 ** 62, "2^60": 2.0 ** 60, "2^58": 2.0 ** 58, "2^48": 2.0 ** 48, "2^-45": 2.0 ** -45,
+SCALES = {"2^127": 2.0 ** 127, "1e30": 1e30, "2^62": 2.0 ** 62, "2^60": 2.0 ** 60, "2^58": 2.0 ** 58, "2^48": 2.0 ** 48, "2^-45": 2.0 ** -45, "2^-57": 2.0 ** -57, "2^-60": 2.0 ** -60,
           "1e-20": 1e-20, "2^-70": 2.0 ** -70, "1e-25": 1e-25, "1e-38": 1e-38, "2^-140": 2.0 ** -140}
 
 
